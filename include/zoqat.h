@@ -614,6 +614,124 @@ int zoqat_op_decode_gemv(const void* packed_dev, const void* qparams_dev, int64_
                          const void* act_codes_dev, const float* row_step_dev, int batch, const float* bias_dev,
                          int accumulate, float* out_dev, void* nibble_scratch_dev, void* stream);
 
+/* ---- serving drafted tokens over a paged key/value cache ---------------------------------
+ * What one step of a batch of requests needs around the linears when every request has a length
+ * of its own, brings one or several new tokens (drafts, arranged as a tree) and keeps its keys and
+ * values in pages of a shared pool.  (The paper's decode table feeds one token per sequence; this is
+ * the deployment side carried on, the operations are those of the forward pass.)  A step calls, in order,
+ *     zoqat_op_cache_plan       once: pages, slots, positions and tree masks from the lengths
+ *     zoqat_op_cache_append     per layer: rotary embedding, new keys and values into their slots
+ *     zoqat_op_tree_attention   per layer: drafts attend to the cached positions and their ancestors
+ *     zoqat_op_logit_rules      once: penalties, biases, grammar masks, greedy choice
+ * and zoqat_decode_tree_step() is that step for a packed model.  Lengths and tables are device data:
+ * no call reads them on the host, so a step can be captured in a CUDA graph and replayed as they change.
+ * Inputs that only the device can check are reported in an int32 word (err_flag_dev / status_dev; zeroed by
+ * the caller, never cleared here), and the access in question is skipped.  Output buffers must not overlap
+ * inputs except where it is said.  All calls are asynchronous. */
+#define ZOQAT_TYPE_F32  0
+#define ZOQAT_TYPE_BF16 1
+#define ZOQAT_TYPE_F16  2
+
+/* One layer's pages.  Element (page, slot, head, i) of K or V is at page * page_stride + slot * slot_stride +
+ * head * head_stride + i, in elements: [page][slot][head][d_head] and [page][head][slot][d_head] are both
+ * layouts of this form, as is the cache of zoqat_decode_begin (a page per sequence).  Strides are multiples of 16 bytes,
+ * k and v 16-byte aligned. */
+typedef struct zoqat_paged_cache {
+    void*   k;             /* dev */
+    void*   v;             /* dev */
+    int32_t type;          /* ZOQAT_TYPE_*                                                            */
+    int32_t n_pages;
+    int32_t page_size;     /* slots per page; n_pages * page_size <= 2^31 - 1                          */
+    int32_t n_kv_heads;
+    int32_t d_head;        /* 64 or 128                                                               */
+    int32_t reserved;
+    int64_t page_stride, slot_stride, head_stride;
+} zoqat_paged_cache_t;
+
+/* Plan of a step: request b has cached_len_dev[b] tokens in the cache and brings new_len_dev[b] (0: it sits this step out).
+ * Pages a request holds already (the first ceil(cached / page_size) entries of its row of block_table_dev [batch, max_pages])
+ * are kept; further ones are taken from the end of free_pages_dev[0 .. *n_free_dev), request by request in order, and written
+ * behind them (entries beyond stay as they are).  free_capacity: entries of free_pages_dev.  Rows of all requests stand back to
+ * back:
+ *   kv_len_dev [batch]            cached + new
+ *   row_start_dev [batch + 1]     first row of each request; the last entry is the number of rows
+ *   row_request_dev, row_pos_dev, slot_dev [max_rows]   request, position (rotary) and slot (page * page_size + offset) of
+ *                                 each row; -1 in the rows behind the last
+ *   tree_mask_dev [max_rows, mask_words]  bit j: the row sees draft j of its request (itself and its ancestors); 0 behind the
+ *                                 last row.  NULL with mask_words = 0: not wanted
+ *   n_free_out_dev [1]            pages left (not n_free_dev itself: the call may be repeated on the same inputs)
+ * parents_dev [max_rows] (may be NULL: each draft follows the one before it) names each draft's parent by its index within the
+ * request, -1 for one that follows the cached context; a parent stands before its children.  position = cached + depth.
+ * status_dev is or-ed with 1 (a length negative or too long for the table, more than 32 * mask_words drafts with a mask, more rows
+ * than max_rows, a bad *n_free_dev: nothing is planned), 2 (too few pages: nothing is planned), 4 (a page outside [0, n_pages):
+ * the row gets slot -1), 8 (a parent not before its child: the walk ends there).  "Nothing is planned" leaves the table as it is,
+ * row_start and kv_len are all 0 and every row is padding.  batch <= 16384, mask_words <= 32. */
+int zoqat_op_cache_plan(const int32_t* cached_len_dev, const int32_t* new_len_dev, int batch, int page_size, int n_pages,
+                        const int32_t* free_pages_dev, int free_capacity, const int32_t* n_free_dev,
+                        int32_t* block_table_dev, int max_pages, const int32_t* parents_dev, int max_rows, int mask_words,
+                        int32_t* kv_len_dev, int32_t* row_start_dev, int32_t* row_request_dev, int32_t* row_pos_dev,
+                        int32_t* slot_dev, uint32_t* tree_mask_dev, int32_t* n_free_out_dev, int32_t* status_dev, void* stream);
+
+/* The new rows of one layer: qkv_dev fp32 [rows, (n_heads + 2 * n_kv_heads) * d_head], rows ld elements apart (16-byte
+ * aligned, ld % 4 == 0): q heads, k heads, v heads.  q and k are rotated by the tables' row row_pos_dev[r] (cos_dev / sin_dev fp32
+ * [rope_len, d_head / 2], pairs (i, i + d_head / 2); both NULL: no rotation, row_pos_dev unused), rounded once to the cache's
+ * type; q goes to q_out_dev (of that type, [rows, n_heads, d_head], rows q_stride elements apart), k and v into slot slot_dev[r].
+ * A row with a negative slot is skipped, its q_out row left as it is; a slot or position outside the cache / the tables is
+ * skipped too and sets *err_flag_dev to 40.  Two rows with the same slot: either may win, element by element. */
+int zoqat_op_cache_append(const float* qkv_dev, int64_t ld, const int32_t* row_pos_dev, const int32_t* slot_dev, int rows,
+                          int n_heads, const float* cos_dev, const float* sin_dev, int rope_len,
+                          const zoqat_paged_cache_t* cache, void* q_out_dev, int64_t q_stride, int32_t* err_flag_dev, void* stream);
+
+/* out[r, h] = softmax(scale * q[r, h] . K) V over what row r sees: with n rows and L = kv_len_dev[b] keys (drafts last, their K
+ * and V in the cache already) the keys t < L - n, and draft j (t = L - n + j) if bit j of the row's tree_mask_dev [rows,
+ * mask_words] is set (bits beyond mask_words count as 0; tree_mask_dev = NULL: if j is not behind the row).  Query head h reads key
+ * head h / (n_heads / n_kv_heads).  A row that sees nothing gives zeros; what a row does not see does not reach it, whatever it
+ * holds (NaN, inf).  q_dev and out_dev have the cache's type, [rows, n_heads, d_head] with rows q_stride / out_stride elements
+ * apart (16-byte aligned, strides multiples of 16 bytes).  Rows outside row_start_dev's ranges are left as they are.
+ * Sums and the softmax are held in fp32; in bf16 / fp16 the softmax weights are rounded to the cache's type for the product with
+ * V.  The keys are dealt out evenly over the SMs, long contexts in several pieces that are joined in a fixed order: the same
+ * call gives the same bits.  bf16 and fp16 need page_size 8, 16, 32, 64 or a multiple of 128 and lcm(8, n_heads / n_kv_heads)
+ * <= 128 (ZOQAT_ERR_UNSUPPORTED otherwise).  scratch_dev: zoqat_op_tree_attention_scratch_bytes() bytes, 256-byte aligned, for one
+ * call at a time (calls that may overlap, e.g. two graphs in flight, each need their own).  *err_flag_dev is set to 41 (a request
+ * whose lengths or rows contradict each other: it is left out), 42 (a page outside the pool: its keys and values count as zeros), 43 (a
+ * bounded device wait ran out). */
+int zoqat_op_tree_attention_scratch_bytes(int type, int d_head, size_t* bytes);
+int zoqat_op_tree_attention(const void* q_dev, int64_t q_stride, const zoqat_paged_cache_t* cache, const int32_t* block_table_dev,
+                            int max_pages, const int32_t* kv_len_dev, const int32_t* row_start_dev, const uint32_t* tree_mask_dev,
+                            int mask_words, int batch, int rows, int n_heads, float scale, void* out_dev, int64_t out_stride,
+                            void* scratch_dev, size_t scratch_bytes, int32_t* err_flag_dev, void* stream);
+
+/* Rules on logits.  Every pointer is device memory; a NULL group is off. */
+typedef struct zoqat_logit_rules {
+    const int32_t* row_request;    /* [rows] request of each row, -1: the row is left as it is; NULL: row r is request r */
+    const float*   repetition;     /* [batch] fp32; NULL: 1                                                        */
+    const float*   presence;       /* [batch] fp32; NULL: 0                                                        */
+    const float*   frequency;      /* [batch] fp32; NULL: 0                                                        */
+    const int32_t* history;        /* [batch, history_stride] token ids: prompt, then what was generated            */
+    const int32_t* history_len;    /* [batch]                                                                      */
+    const int32_t* prompt_len;     /* [batch] how many of them are the prompt; NULL: 0                             */
+    const int32_t* bias_token;     /* [batch, bias_stride]                                                         */
+    const float*   bias_value;     /* [batch, bias_stride]                                                         */
+    const int32_t* bias_len;       /* [batch]                                                                      */
+    const uint32_t* allowed;       /* [rows, allowed_stride] bit v of a row: token v is allowed                     */
+    const int32_t* draft_token;    /* [rows] the token of each row; with row_start and tree_mask a row's ancestors and
+                                      itself count as generated (the history does not hold them yet)               */
+    const int32_t* row_start;      /* [batch + 1]                                                                  */
+    const uint32_t* tree_mask;     /* [rows, mask_words]                                                           */
+    int64_t history_stride, allowed_stride;
+    int32_t bias_stride, mask_words, batch, reserved;
+} zoqat_logit_rules_t;
+
+/* For every row r and token v, each step one fp32 rounding, in this order:
+ *   x = logits[r, v];  if v is in the prompt or n > 0: x = x > 0 ? x / repetition : x * repetition, with n = times v was generated;
+ *   x -= frequency * n;  if n > 0: x -= presence;  x += the sum of the request's biases for v;  x = -inf if v is not allowed
+ * out_dev[r, v] = x in the logits' type (may be logits_dev itself with out_ld == ld; NULL: only the choice is wanted) and
+ * token_dev[r] = the lowest v with the largest out value (-1 if none is above -inf; NULL: not wanted).  Tokens outside [0, vocab)
+ * in the history, drafts or biases are ignored; NaN logits are never chosen.  type: ZOQAT_TYPE_* of logits and out;
+ * rows ld / out_ld elements apart; 1 <= rows <= 65535. */
+int zoqat_op_logit_rules(const void* logits_dev, int type, int64_t ld, int rows, int vocab, const zoqat_logit_rules_t* rules,
+                         void* out_dev, int64_t out_ld, int32_t* token_dev, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

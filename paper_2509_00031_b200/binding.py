@@ -23,6 +23,8 @@ TENSOR_TRAINABLE, TENSOR_QUANTIZED, TENSOR_FROZEN_PACKED, TENSOR_ADAPTIVE = 1, 2
 GEMM_TCGEN05, GEMM_SIMT, GEMM_TCGEN05_1CTA, GEMM_TCGEN05_I8 = 0, 1, 2, 3
 BUF_RESIDUAL, BUF_QKV, BUF_ATTN, BUF_FFN, BUF_TOKEN_LOSS = range(5)
 PROF_GEMM, PROF_WEIGHT, PROF_ACT, PROF_ATTENTION, PROF_LOSS, PROF_UPDATE = range(6)
+TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
+PLAN_BAD_LENGTH, PLAN_NO_PAGES, PLAN_BAD_PAGE, PLAN_BAD_PARENT = 1, 2, 4, 8
 PROF_NAMES = ["gemm", "weight_operand", "act_operand", "attention", "loss", "update"]
 
 EXPORTS = [
@@ -37,6 +39,8 @@ EXPORTS = [
     "zoqat_op_head_loss_scratch_bytes",
     "zoqat_op_head_loss", "zoqat_op_head_loss_static",
     "zoqat_decode_bytes", "zoqat_decode_begin", "zoqat_decode_step", "zoqat_op_decode_gemv",
+    "zoqat_op_cache_plan", "zoqat_op_cache_append", "zoqat_op_tree_attention_scratch_bytes", "zoqat_op_tree_attention",
+    "zoqat_op_logit_rules",
 ]
 
 
@@ -55,6 +59,19 @@ class TensorDesc(ctypes.Structure):
 class StepResult(ctypes.Structure):
     _fields_ = [("loss_plus", ctypes.c_float), ("loss_minus", ctypes.c_float), ("proj_grad", ctypes.c_float),
                 ("update_scale", ctypes.c_float), ("status", ctypes.c_int32), ("n_labels", ctypes.c_int32)]
+
+
+class PagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + [(n, ctypes.c_int32) for n in (
+        "type", "n_pages", "page_size", "n_kv_heads", "d_head", "reserved")] + [(n, ctypes.c_int64) for n in (
+            "page_stride", "slot_stride", "head_stride")]
+
+
+class LogitRulesDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in (
+        "row_request", "repetition", "presence", "frequency", "history", "history_len", "prompt_len", "bias_token", "bias_value", "bias_len",
+        "allowed", "draft_token", "row_start", "tree_mask")] + [(n, ctypes.c_int64) for n in ("history_stride", "allowed_stride")] + [
+            (n, ctypes.c_int32) for n in ("bias_stride", "mask_words", "batch", "reserved")]
 
 
 class ZoqatError(RuntimeError):
@@ -142,6 +159,11 @@ def lib():
             "zoqat_decode_begin": [vp, vp, sz, i32, i32, vp],
             "zoqat_decode_step": [vp, vp, i32, vp, vp, vp],
             "zoqat_op_decode_gemv": [vp, vp, i64, i64, i32, i32, vp, vp, i32, vp, i32, vp, vp, vp],
+            "zoqat_op_cache_plan": [vp, vp, i32, i32, i32, vp, i32, vp, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp],
+            "zoqat_op_cache_append": [vp, i64, vp, vp, i32, i32, vp, vp, i32, P(PagedCache), vp, i64, vp, vp],
+            "zoqat_op_tree_attention_scratch_bytes": [i32, i32, P(sz)],
+            "zoqat_op_tree_attention": [vp, i64, P(PagedCache), vp, i32, vp, vp, vp, i32, i32, i32, i32, f32, vp, i64, vp, sz, vp, vp],
+            "zoqat_op_logit_rules": [vp, i32, i64, i32, i32, P(LogitRulesDesc), vp, i64, vp, vp],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -415,6 +437,179 @@ def zoqat_op_head_loss_static(a, b, labels, token_loss, loss_sum, count, err, im
     _check(lib().zoqat_op_head_loss_static(_p(a), _p(b), _p(labels), T, V, d, _p(token_loss), _p(loss_sum), _p(count),
                                            impl, _p(err), _stream()))
     return token_loss, loss_sum, count, err
+
+
+# ---- serving drafted tokens over a paged cache ---------------------------------------------
+_TYPES = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
+
+
+def _refuse(cond, text):
+    if cond:
+        raise ZoqatError(ERR_INVALID_ARG, text)
+
+
+def _need(name, t, dtype, shape=None):
+    """A contiguous tensor of this type (and shape; None entries are free) on the current CUDA device."""
+    _refuse(t.dtype != dtype or not t.is_contiguous(), f"{name}: a contiguous {dtype} tensor is needed")
+    _refuse(not t.is_cuda or t.device.index != torch.cuda.current_device(), f"{name}: not on the current CUDA device")
+    _refuse(shape is not None and (t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape))),
+            f"{name}: shape {tuple(t.shape)}, {shape} is needed")
+
+
+def _rows(name, t, dtype, heads, d_head):
+    """[rows, heads, d_head] whose rows may stand apart."""
+    _refuse(t.dtype != dtype or t.dim() != 3 or tuple(t.shape[1:]) != (heads, d_head), f"{name}: [rows, {heads}, {d_head}] of {dtype} is needed")
+    _refuse(t.stride(2) != 1 or (heads > 1 and t.stride(1) != d_head), f"{name}: heads must stand back to back")
+    _refuse(not t.is_cuda or t.device.index != torch.cuda.current_device(), f"{name}: not on the current CUDA device")
+    return t.stride(0) if t.shape[0] > 1 else heads * d_head
+
+
+def paged_cache(k_cache, v_cache):
+    """zoqat_paged_cache_t of two tensors [n_pages, page_size, n_kv_heads, d_head] with the same strides (a cache laid out head by
+    head is passed as its transposed view)."""
+    _refuse(k_cache.dtype not in _TYPES or k_cache.dtype != v_cache.dtype, "caches must both be float32, bfloat16 or float16")
+    _refuse(k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride() or k_cache.stride(3) != 1,
+            "caches must be [n_pages, page_size, n_kv_heads, d_head] with the same strides and contiguous heads")
+    for t in (k_cache, v_cache):
+        _refuse(not t.is_cuda or t.device.index != torch.cuda.current_device(), "caches: not on the current CUDA device")
+    n, ps, kv, dh = k_cache.shape
+    return PagedCache(k_cache.data_ptr(), v_cache.data_ptr(), _TYPES[k_cache.dtype], n, ps, kv, dh, 0, k_cache.stride(0), k_cache.stride(1),
+                      k_cache.stride(2))
+
+
+def zoqat_op_cache_plan(cached_len, new_len, page_size, n_pages, free_pages, n_free, block_table, max_rows, parents=None, mask_words=0, out=None):
+    """-> dict of int32 tensors: kv_len, row_start, row_request, row_pos, slot, n_free, status and, with mask_words, tree_mask.
+    block_table is extended in place.  out: such a dict of an earlier call to write into (its status word is or-ed)."""
+    batch = cached_len.shape[0]
+    dev = cached_len.device
+    if out is None:
+        shapes = dict(kv_len=(batch,), row_start=(batch + 1,), row_request=(max_rows,), row_pos=(max_rows,), slot=(max_rows,), n_free=(1,))
+        if mask_words:
+            shapes["tree_mask"] = (max_rows, mask_words)
+        out = {n: torch.empty(s, dtype=torch.int32, device=dev) for n, s in shapes.items()}
+        out["status"] = torch.zeros(1, dtype=torch.int32, device=dev)
+    i32 = torch.int32
+    _need("cached_len", cached_len, i32, (None,))
+    _need("new_len", new_len, i32, (batch,))
+    _need("free_pages", free_pages, i32, (None,))
+    _need("n_free", n_free, i32, (1,))
+    _need("block_table", block_table, i32, (batch, None))
+    if parents is not None:
+        _need("parents", parents, i32, (max_rows,))
+    for n, shape in (("kv_len", (batch,)), ("row_start", (batch + 1,)), ("row_request", (max_rows,)), ("row_pos", (max_rows,)), ("slot", (max_rows,)),
+                     ("n_free", (1,)), ("status", (1,))):
+        _need(n, out[n], i32, shape)
+    mask = out["tree_mask"] if mask_words else None
+    if mask is not None:
+        _need("tree_mask", mask, i32, (max_rows, mask_words))
+    _check(lib().zoqat_op_cache_plan(_p(cached_len), _p(new_len), batch, page_size, n_pages, _p(free_pages), free_pages.shape[0], _p(n_free),
+                                     _p(block_table), block_table.shape[1], _p(parents), max_rows, mask_words, _p(out["kv_len"]),
+                                     _p(out["row_start"]), _p(out["row_request"]), _p(out["row_pos"]), _p(out["slot"]), _p(mask),
+                                     _p(out["n_free"]), _p(out["status"]), _stream()))
+    return out
+
+
+def zoqat_op_cache_append(qkv, row_pos, slot, k_cache, v_cache, n_heads, cos=None, sin=None, q_out=None, err=None):
+    """qkv float32 [rows, (n_heads + 2 n_kv_heads) * d_head] -> (q_out [rows, n_heads, d_head] of the caches' type, err)."""
+    cache = paged_cache(k_cache, v_cache)
+    rows, dh = qkv.shape[0], cache.d_head
+    _refuse(qkv.dtype != torch.float32 or qkv.dim() != 2 or qkv.shape[1] != (n_heads + 2 * cache.n_kv_heads) * dh or qkv.stride(1) != 1,
+            "qkv: float32 [rows, (n_heads + 2 n_kv_heads) * d_head] is needed")
+    _refuse(qkv.device != k_cache.device, "qkv: not on the caches' device")
+    _need("slot", slot, torch.int32, (rows,))
+    if cos is not None:
+        _need("row_pos", row_pos, torch.int32, (rows,))
+        _need("cos", cos, torch.float32, (None, dh // 2))
+        _need("sin", sin, torch.float32, (cos.shape[0], dh // 2))
+    if q_out is None:
+        q_out = torch.empty((rows, n_heads, dh), dtype=k_cache.dtype, device=qkv.device)
+    if err is None:
+        err = torch.zeros(1, dtype=torch.int32, device=qkv.device)
+    q_stride = _rows("q_out", q_out, k_cache.dtype, n_heads, dh)
+    _refuse(q_out.shape[0] < rows, "q_out: too few rows")
+    _check(lib().zoqat_op_cache_append(_p(qkv), qkv.stride(0) if rows > 1 else qkv.shape[1], _p(row_pos), _p(slot), rows, n_heads, _p(cos), _p(sin),
+                                       cos.shape[0] if cos is not None else 0, ctypes.byref(cache), _p(q_out), q_stride, _p(err), _stream()))
+    return q_out, err
+
+
+def zoqat_op_tree_attention(q, k_cache, v_cache, block_table, kv_len, row_start, tree_mask=None, scale=None, out=None, scratch=None, err=None):
+    """q [rows, n_heads, d_head] of the caches' type -> (out of the same form, err).  scale: 1 / sqrt(d_head) by default."""
+    cache = paged_cache(k_cache, v_cache)
+    rows, heads, dh = q.shape
+    batch = kv_len.shape[0]
+    q_stride = _rows("q", q, k_cache.dtype, heads, cache.d_head)
+    _need("block_table", block_table, torch.int32, (batch, None))
+    _need("kv_len", kv_len, torch.int32, (batch,))
+    _need("row_start", row_start, torch.int32, (batch + 1,))
+    words = 0
+    if tree_mask is not None:
+        _need("tree_mask", tree_mask, torch.int32, (None, None))
+        _refuse(tree_mask.shape[0] < rows, "tree_mask: too few rows")
+        words = tree_mask.shape[1]
+    if out is None:
+        out = torch.empty((rows, heads, dh), dtype=q.dtype, device=q.device)
+    out_stride = _rows("out", out, k_cache.dtype, heads, dh)
+    _refuse(out.shape[0] < rows, "out: too few rows")
+    if scratch is None:
+        nb = ctypes.c_size_t()
+        _check(lib().zoqat_op_tree_attention_scratch_bytes(cache.type, dh, ctypes.byref(nb)))
+        scratch = torch.empty(nb.value, dtype=torch.uint8, device=q.device)
+    if err is None:
+        err = torch.zeros(1, dtype=torch.int32, device=q.device)
+    _check(lib().zoqat_op_tree_attention(_p(q), q_stride, ctypes.byref(cache), _p(block_table), block_table.shape[1], _p(kv_len), _p(row_start),
+                                         _p(tree_mask), words, batch, rows, heads, dh ** -0.5 if scale is None else scale, _p(out), out_stride,
+                                         _p(scratch), scratch.numel() * scratch.element_size(), _p(err), _stream()))
+    return out, err
+
+
+class LogitRules:
+    """zoqat_logit_rules_t over tensors, which it keeps alive; every group may be left out."""
+
+    def __init__(self, batch=None, row_request=None, repetition=None, presence=None, frequency=None, history=None, history_len=None,
+                 prompt_len=None, bias_token=None, bias_value=None, bias_len=None, allowed=None, draft_token=None, row_start=None, tree_mask=None):
+        i32, f32 = torch.int32, torch.float32
+        if batch is None:
+            sized = [t for t in (history_len, repetition, presence, frequency, bias_len) if t is not None]
+            _refuse(not sized, "batch is needed when no rule is per request")
+            batch = sized[0].shape[0]
+        for n, t, dtype, shape in (("row_request", row_request, i32, (None,)), ("repetition", repetition, f32, (batch,)), ("presence", presence, f32, (batch,)),
+                                   ("frequency", frequency, f32, (batch,)), ("history", history, i32, (batch, None)), ("history_len", history_len, i32, (batch,)),
+                                   ("prompt_len", prompt_len, i32, (batch,)), ("bias_token", bias_token, i32, (batch, None)),
+                                   ("bias_value", bias_value, f32, None if bias_token is None else tuple(bias_token.shape)), ("bias_len", bias_len, i32, (batch,)),
+                                   ("allowed", allowed, i32, (None, None)), ("draft_token", draft_token, i32, (None,)), ("row_start", row_start, i32, (batch + 1,)),
+                                   ("tree_mask", tree_mask, i32, (None, None))):
+            if t is not None:
+                _need(n, t, dtype, shape)
+        self.tensors = (row_request, repetition, presence, frequency, history, history_len, prompt_len, bias_token, bias_value, bias_len, allowed,
+                        draft_token, row_start, tree_mask)
+        self.row_request, self.allowed, self.draft_token, self.tree_mask = row_request, allowed, draft_token, tree_mask
+        self.desc = LogitRulesDesc(*[t.data_ptr() if t is not None else None for t in self.tensors], history.shape[1] if history is not None else 0,
+                                   allowed.shape[1] if allowed is not None else 0, bias_token.shape[1] if bias_token is not None else 0,
+                                   tree_mask.shape[1] if tree_mask is not None else 0, batch, 0)
+
+    def check_rows(self, rows):
+        for n in ("row_request", "allowed", "draft_token", "tree_mask"):
+            t = getattr(self, n)
+            _refuse(t is not None and t.shape[0] < rows, f"{n}: too few rows")
+
+
+def zoqat_op_logit_rules(logits, rules, out=None, token=None, want_logits=True):
+    """logits [rows, vocab] (rows may stand apart) -> (out of the same type or None, token int32 [rows]).  out may be logits."""
+    _refuse(logits.dtype not in _TYPES or logits.dim() != 2 or logits.stride(1) != 1, "logits: [rows, vocab] of float32, bfloat16 or float16 is needed")
+    _refuse(not logits.is_cuda or logits.device.index != torch.cuda.current_device(), "logits: not on the current CUDA device")
+    rows, vocab = logits.shape
+    rules.check_rows(rows)
+    if out is None and want_logits:
+        out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+    if token is None:
+        token = torch.empty(rows, dtype=torch.int32, device=logits.device)
+    _need("token", token, torch.int32, (rows,))
+    if out is not None:
+        _refuse(out.dtype != logits.dtype or out.shape != logits.shape or out.stride(1) != 1 or out.device != logits.device, "out: not like logits")
+    ld = lambda t: t.stride(0) if t.shape[0] > 1 else max(t.stride(0), vocab)  # noqa: E731
+    _check(lib().zoqat_op_logit_rules(_p(logits), _TYPES[logits.dtype], ld(logits), rows, vocab, ctypes.byref(rules.desc), _p(out),
+                                      ld(out) if out is not None else 0, _p(token), _stream()))
+    return out, token
 
 
 # ---- the model handle -------------------------------------------------------------------

@@ -3,6 +3,7 @@
 // two-pass schedule of Eq. (1) and the update of Eq. (2).  Host code only; every
 // arithmetic step of the path runs in the kernels of this directory.
 #include "common.cuh"
+#include "serve.cuh"
 #include "../../include/zoqat.h"
 
 #include <cmath>
@@ -1786,6 +1787,156 @@ int zoqat_decode_step(zoqat_model_t* m, const int32_t* tokens_dev, int pos, floa
     float* logits = logits_dev ? logits_dev : D.logits;
     if (launch_decode_head(D.head, c.vocab, d, B, w.xa, logits, s) != 0) return fail(ZOQAT_ERR_UNSUPPORTED, "vocabulary projection rejected");
     if (next_token_dev) launch_decode_argmax(logits, B, c.vocab, next_token_dev, s);
+    CUDA_TRY(cudaGetLastError());
+    return ZOQAT_OK;
+}
+
+}  // extern "C"
+
+// ---- serving drafted tokens over a paged cache --------------------------------------------------------------------
+namespace {
+
+inline bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) & (a - 1); }
+
+// Checks a cache description and turns it into what the kernels take.
+int paged_cache(const zoqat_paged_cache_t* c, PagedCache& out) {
+    if (!c || !c->k || !c->v) return fail(ZOQAT_ERR_INVALID_ARG, "cache is NULL");
+    if (c->type != ZOQAT_TYPE_F32 && c->type != ZOQAT_TYPE_BF16 && c->type != ZOQAT_TYPE_F16) return fail(ZOQAT_ERR_INVALID_ARG, "unknown cache type %d", c->type);
+    if (c->n_pages <= 0 || c->page_size <= 0 || c->n_kv_heads <= 0) return fail(ZOQAT_ERR_INVALID_ARG, "cache sizes must be positive");
+    if ((int64_t)c->n_pages * c->page_size > INT32_MAX) return fail(ZOQAT_ERR_UNSUPPORTED, "more than 2^31 - 1 slots");
+    if (c->d_head != 64 && c->d_head != 128) return fail(ZOQAT_ERR_UNSUPPORTED, "head size %d (supported: 64, 128)", c->d_head);
+    const int64_t e = type_bytes(c->type);
+    out = PagedCache{c->k, c->v, c->type, c->n_pages, c->page_size, c->n_kv_heads, c->d_head, c->page_stride, c->slot_stride, c->head_stride};
+    // the stride of a dimension with one entry is never used
+    if (c->n_kv_heads == 1) out.head_stride = c->d_head;
+    if (c->page_size == 1) out.slot_stride = c->d_head;
+    if (c->n_pages == 1) out.page_stride = c->d_head;
+    const int64_t st[3] = {out.page_stride, out.slot_stride, out.head_stride};
+    for (int i = 0; i < 3; ++i)
+        if (st[i] < c->d_head || (st[i] * e) % 16 || st[i] >= ((int64_t)1 << 38)) return fail(ZOQAT_ERR_INVALID_ARG, "cache strides must be at least d_head and multiples of 16 bytes");
+    if (misaligned(c->k, 16) || misaligned(c->v, 16)) return fail(ZOQAT_ERR_INVALID_ARG, "cache pointers must be 16-byte aligned");
+    return ZOQAT_OK;
+}
+
+int logit_rules(const zoqat_logit_rules_t* c, int rows, int vocab, LogitRules& r) {
+    if (!c) return fail(ZOQAT_ERR_INVALID_ARG, "rules are NULL");
+    if (rows <= 0 || rows > 65535 || vocab <= 0 || vocab > (1 << 30)) return fail(ZOQAT_ERR_UNSUPPORTED, "rows %d (1..65535), vocab %d (1..2^30)", rows, vocab);
+    if (c->batch <= 0) return fail(ZOQAT_ERR_INVALID_ARG, "rules need the number of requests (batch)");
+    if (!c->row_request && rows > c->batch) return fail(ZOQAT_ERR_INVALID_ARG, "more rows than requests: row_request is needed");
+    if (c->history && (!c->history_len || c->history_stride <= 0 || c->history_stride > INT32_MAX)) return fail(ZOQAT_ERR_INVALID_ARG, "history needs history_len and history_stride");
+    if (c->bias_token && (!c->bias_value || !c->bias_len || c->bias_stride <= 0)) return fail(ZOQAT_ERR_INVALID_ARG, "biases need bias_value, bias_len and bias_stride");
+    if (c->allowed && c->allowed_stride < (vocab + 31) / 32) return fail(ZOQAT_ERR_INVALID_ARG, "allowed_stride must cover the vocabulary's bits");
+    if (c->draft_token && (!c->row_start || !c->tree_mask || c->mask_words <= 0 || c->mask_words > 32)) return fail(ZOQAT_ERR_INVALID_ARG, "drafts need row_start, tree_mask and mask_words (1..32)");
+    r = LogitRules{c->row_request, c->batch, c->repetition, c->presence, c->frequency, c->history, c->history_len, c->prompt_len, c->history_stride,
+                   c->bias_token, c->bias_value, c->bias_len, c->bias_stride, c->allowed, c->allowed_stride, c->draft_token, c->row_start, c->tree_mask,
+                   c->mask_words};
+    return ZOQAT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int zoqat_op_cache_plan(const int32_t* cached_len_dev, const int32_t* new_len_dev, int batch, int page_size, int n_pages,
+                        const int32_t* free_pages_dev, int free_capacity, const int32_t* n_free_dev, int32_t* block_table_dev,
+                        int max_pages, const int32_t* parents_dev, int max_rows, int mask_words, int32_t* kv_len_dev,
+                        int32_t* row_start_dev, int32_t* row_request_dev, int32_t* row_pos_dev, int32_t* slot_dev,
+                        uint32_t* tree_mask_dev, int32_t* n_free_out_dev, int32_t* status_dev, void* stream) {
+    if (!cached_len_dev || !new_len_dev || !n_free_dev || !block_table_dev || !kv_len_dev || !row_start_dev || !row_request_dev ||
+        !row_pos_dev || !slot_dev || !n_free_out_dev || !status_dev)
+        return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
+    if (batch <= 0 || page_size <= 0 || n_pages <= 0 || max_pages <= 0 || max_rows <= 0 || free_capacity < 0) return fail(ZOQAT_ERR_INVALID_ARG, "sizes must be positive");
+    if (free_capacity > 0 && !free_pages_dev) return fail(ZOQAT_ERR_INVALID_ARG, "free_pages_dev is NULL");
+    if (batch > kMaxPlanBatch) return fail(ZOQAT_ERR_UNSUPPORTED, "batch %d (supported: up to %d)", batch, kMaxPlanBatch);
+    if (mask_words < 0 || mask_words > 32) return fail(ZOQAT_ERR_UNSUPPORTED, "mask_words %d (supported: 0..32)", mask_words);
+    if ((mask_words != 0) != (tree_mask_dev != nullptr)) return fail(ZOQAT_ERR_INVALID_ARG, "tree_mask_dev and mask_words must both be given or neither");
+    if ((int64_t)n_pages * page_size > INT32_MAX || (int64_t)max_pages * page_size > INT32_MAX) return fail(ZOQAT_ERR_UNSUPPORTED, "more than 2^31 - 1 slots");
+    // CTAs read the inputs while others write: an output may not be an input
+    if (kv_len_dev == cached_len_dev || kv_len_dev == new_len_dev || n_free_out_dev == n_free_dev || block_table_dev == free_pages_dev ||
+        (parents_dev && (parents_dev == row_request_dev || parents_dev == row_pos_dev || parents_dev == slot_dev)))
+        return fail(ZOQAT_ERR_INVALID_ARG, "an output buffer is an input buffer");
+    CachePlanArgs a{cached_len_dev, new_len_dev, batch, page_size, n_pages, max_pages, free_pages_dev, free_capacity, n_free_dev,
+                    block_table_dev, parents_dev, max_rows, mask_words, kv_len_dev, row_start_dev, row_request_dev, row_pos_dev,
+                    slot_dev, tree_mask_dev, n_free_out_dev, status_dev};
+    if (launch_cache_plan(a, static_cast<cudaStream_t>(stream)) != 0) return fail(ZOQAT_ERR_CUDA, "cache plan: kernel set-up failed");
+    CUDA_TRY(cudaGetLastError());
+    return ZOQAT_OK;
+}
+
+int zoqat_op_cache_append(const float* qkv_dev, int64_t ld, const int32_t* row_pos_dev, const int32_t* slot_dev, int rows, int n_heads,
+                          const float* cos_dev, const float* sin_dev, int rope_len, const zoqat_paged_cache_t* cache, void* q_out_dev,
+                          int64_t q_stride, int32_t* err_flag_dev, void* stream) {
+    PagedCache c;
+    if (int rc = paged_cache(cache, c)) return rc;
+    if (!qkv_dev || !slot_dev || !q_out_dev || !err_flag_dev) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
+    if (rows < 0 || n_heads <= 0 || n_heads > 65536 || c.n_kv_heads > 65536) return fail(ZOQAT_ERR_INVALID_ARG, "bad sizes (rows %d, heads %d)", rows, n_heads);
+    if ((cos_dev == nullptr) != (sin_dev == nullptr)) return fail(ZOQAT_ERR_INVALID_ARG, "cos/sin tables must both be given or both NULL");
+    if (cos_dev && (!row_pos_dev || rope_len <= 0)) return fail(ZOQAT_ERR_INVALID_ARG, "rotary tables need row_pos_dev and rope_len");
+    if (ld < (int64_t)(n_heads + 2 * c.n_kv_heads) * c.d_head || ld % 4) return fail(ZOQAT_ERR_INVALID_ARG, "ld must cover q | k | v and be a multiple of 4");
+    const int64_t e = type_bytes(c.type);
+    if (q_stride < (int64_t)n_heads * c.d_head || (q_stride * e) % 16) return fail(ZOQAT_ERR_INVALID_ARG, "q_stride must cover the heads and be a multiple of 16 bytes");
+    if (misaligned(qkv_dev, 16) || misaligned(q_out_dev, 16) || misaligned(cos_dev, 16) || misaligned(sin_dev, 16))
+        return fail(ZOQAT_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+    if (rows == 0) return ZOQAT_OK;
+    launch_cache_append(qkv_dev, ld, row_pos_dev, slot_dev, rows, n_heads, cos_dev, sin_dev, rope_len, c, q_out_dev, q_stride, err_flag_dev,
+                        static_cast<cudaStream_t>(stream));
+    CUDA_TRY(cudaGetLastError());
+    return ZOQAT_OK;
+}
+
+int zoqat_op_tree_attention_scratch_bytes(int type, int d_head, size_t* bytes) {
+    if (!bytes || (type != ZOQAT_TYPE_F32 && type != ZOQAT_TYPE_BF16 && type != ZOQAT_TYPE_F16)) return fail(ZOQAT_ERR_INVALID_ARG, "bad attention scratch query");
+    if (d_head != 64 && d_head != 128) return fail(ZOQAT_ERR_UNSUPPORTED, "head size %d (supported: 64, 128)", d_head);
+    *bytes = align_up(tree_attention_scratch_bytes(type, d_head));
+    return ZOQAT_OK;
+}
+
+int zoqat_op_tree_attention(const void* q_dev, int64_t q_stride, const zoqat_paged_cache_t* cache, const int32_t* block_table_dev,
+                            int max_pages, const int32_t* kv_len_dev, const int32_t* row_start_dev, const uint32_t* tree_mask_dev,
+                            int mask_words, int batch, int rows, int n_heads, float scale, void* out_dev, int64_t out_stride,
+                            void* scratch_dev, size_t scratch_bytes, int32_t* err_flag_dev, void* stream) {
+    TreeAttnArgs a{};
+    if (int rc = paged_cache(cache, a.cache)) return rc;
+    const PagedCache& c = a.cache;
+    if (!q_dev || !block_table_dev || !kv_len_dev || !row_start_dev || !out_dev || !scratch_dev || !err_flag_dev) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
+    if (batch <= 0 || rows < 0 || n_heads <= 0 || max_pages <= 0) return fail(ZOQAT_ERR_INVALID_ARG, "sizes must be positive");
+    if (n_heads % c.n_kv_heads) return fail(ZOQAT_ERR_INVALID_ARG, "n_kv_heads must divide n_heads");
+    if ((int64_t)max_pages * c.page_size > INT32_MAX - 256 || (int64_t)rows * n_heads > INT32_MAX) return fail(ZOQAT_ERR_UNSUPPORTED, "sizes pass 2^31");
+    if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(ZOQAT_ERR_INVALID_ARG, "scale must be positive");
+    if (tree_mask_dev ? mask_words <= 0 || mask_words > (1 << 20) : mask_words != 0) return fail(ZOQAT_ERR_INVALID_ARG, "tree_mask_dev and mask_words must both be given or neither");
+    const int64_t e = type_bytes(c.type), wide = (int64_t)n_heads * c.d_head;
+    if (q_stride < wide || out_stride < wide || (q_stride * e) % 16 || (out_stride * e) % 16 || q_stride >= ((int64_t)1 << 38)) return fail(ZOQAT_ERR_INVALID_ARG, "row strides must cover the heads and be multiples of 16 bytes");
+    if (misaligned(q_dev, 16) || misaligned(out_dev, 16)) return fail(ZOQAT_ERR_INVALID_ARG, "q_dev and out_dev must be 16-byte aligned");
+    if (q_dev == out_dev) return fail(ZOQAT_ERR_INVALID_ARG, "out_dev may not be q_dev");
+    if (misaligned(scratch_dev, 256)) return fail(ZOQAT_ERR_INVALID_ARG, "scratch_dev must be 256-byte aligned");
+    const size_t need = tree_attention_scratch_bytes(c.type, c.d_head);
+    if (scratch_bytes < need) return fail(ZOQAT_ERR_WORKSPACE_SMALL, "attention scratch %zu < %zu bytes", scratch_bytes, need);
+    const bool tc = c.type != ZOQAT_TYPE_F32;
+    if (tc && c.page_size % 128 && c.page_size != 8 && c.page_size != 16 && c.page_size != 32 && c.page_size != 64)
+        return fail(ZOQAT_ERR_UNSUPPORTED, "page_size %d (bf16 / fp16: 8, 16, 32, 64 or a multiple of 128)", c.page_size);
+    if (rows == 0) return ZOQAT_OK;
+    a.q = q_dev; a.q_stride = q_stride; a.block_table = block_table_dev; a.max_pages = max_pages; a.kv_len = kv_len_dev; a.row_start = row_start_dev;
+    a.tree_mask = tree_mask_dev; a.mask_words = mask_words; a.batch = batch; a.rows = rows; a.n_heads = n_heads; a.scale = scale;
+    a.out = out_dev; a.out_stride = out_stride; a.scratch = static_cast<uint8_t*>(scratch_dev); a.err_flag = err_flag_dev;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int rc = tc ? launch_tree_attention_tc(a, s, false) : launch_tree_attention_simt(a, s, false);
+    if (rc != ZOQAT_OK) return fail(rc, "tree attention rejected (%d query heads per key head; bf16 / fp16 need lcm(8, heads per key head) <= 128)", n_heads / c.n_kv_heads);
+    CUDA_TRY(cudaGetLastError());
+    return ZOQAT_OK;
+}
+
+int zoqat_op_logit_rules(const void* logits_dev, int type, int64_t ld, int rows, int vocab, const zoqat_logit_rules_t* rules, void* out_dev,
+                         int64_t out_ld, int32_t* token_dev, void* stream) {
+    LogitRules r;
+    if (int rc = logit_rules(rules, rows, vocab, r)) return rc;
+    if (!logits_dev || (!out_dev && !token_dev)) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
+    if (type != ZOQAT_TYPE_F32 && type != ZOQAT_TYPE_BF16 && type != ZOQAT_TYPE_F16) return fail(ZOQAT_ERR_INVALID_ARG, "unknown logits type %d", type);
+    if (ld < vocab || (out_dev && out_ld < vocab)) return fail(ZOQAT_ERR_INVALID_ARG, "ld and out_ld must cover the vocabulary");
+    if (out_dev == logits_dev && out_ld != ld) return fail(ZOQAT_ERR_INVALID_ARG, "in place needs out_ld == ld");
+    const size_t e = (size_t)type_bytes(type);
+    if (misaligned(logits_dev, e) || misaligned(out_dev, e)) return fail(ZOQAT_ERR_INVALID_ARG, "misaligned pointer");
+    if (launch_logit_rules(logits_dev, type, ld, rows, vocab, r, out_dev, out_ld, token_dev, static_cast<cudaStream_t>(stream)) != 0)
+        return fail(ZOQAT_ERR_CUDA, "logit rules: launch failed");
     CUDA_TRY(cudaGetLastError());
     return ZOQAT_OK;
 }

@@ -1,0 +1,559 @@
+"""GPU parity of the serving operators (plan of a step, append to a paged cache, attention of drafted tokens over the pages,
+rules on the logits) against plain implementations written from their definitions, in Python integers and 64-bit floats."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def zq():
+    from paper_2509_00031_b200 import binding
+    binding.lib()
+    return binding
+
+
+def ints(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def rand_parents(rng, new):
+    """Per request: draft 0 follows the context, draft i one of the drafts before it or the context."""
+    out = []
+    for n in new:
+        out += [-1 if i == 0 else int(rng.integers(max(-1, i - 6), i)) for i in range(n)]
+    return out
+
+
+def ancestors(parents, i):
+    seen = []
+    while i >= 0:
+        seen.append(i)
+        i = parents[i]
+    return seen
+
+
+def words_of(bits, words):
+    """Set of bit numbers -> signed 32-bit words."""
+    out = [0] * words
+    for b in bits:
+        out[b // 32] |= 1 << (b % 32)
+    return [w - 2 ** 32 if w >= 2 ** 31 else w for w in out]
+
+
+# ---- plan -----------------------------------------------------------------------------------------------------------
+def plan_oracle(cached, new, page, free, n_free, table, max_rows, parents, words):
+    table = [list(r) for r in table]
+    top, start, request, pos, slot, mask = n_free, [0], [], [], [], []
+    for b, (c, n) in enumerate(zip(cached, new)):
+        for k in range(-(-c // page), -(-(c + n) // page)):
+            top -= 1
+            table[b][k] = free[top]
+        mine = parents[start[-1]:start[-1] + n] if parents else list(range(-1, n - 1))
+        for i in range(n):
+            line = ancestors(mine, i)
+            request.append(b)
+            pos.append(c + len(line) - 1)
+            slot.append(table[b][(c + i) // page] * page + (c + i) % page)
+            mask.append(words_of(line, words) if words else [])
+        start.append(start[-1] + n)
+    pad = max_rows - start[-1]
+    return dict(kv_len=[c + n for c, n in zip(cached, new)], row_start=start, row_request=request + [-1] * pad, row_pos=pos + [-1] * pad,
+                slot=slot + [-1] * pad, tree_mask=mask + [[0] * words] * pad, n_free=[top], table=table)
+
+
+def plan_inputs(rng, cached, new, page, spare=4):
+    held = [-(-c // page) for c in cached]
+    need = sum(-(-(c + n) // page) - h for c, n, h in zip(cached, new, held))
+    max_pages = max(max(-(-(c + n) // page) for c, n in zip(cached, new)), 1) + 1
+    order = rng.permutation(sum(held) + need + spare).tolist()
+    table = []
+    for h in held:
+        table.append(order[:h] + [-7] * (max_pages - h))
+        order = order[h:]
+    return table, order, max_pages, sum(held) + need + spare
+
+
+@pytest.mark.parametrize("batch,page,hi_cached,hi_new,words,tree", [
+    (1, 16, 0, 1, 0, False), (1, 1, 5, 3, 1, True), (3, 16, 40, 5, 0, False), (7, 8, 100, 33, 2, True), (7, 8, 100, 33, 2, False),
+    (64, 128, 2000, 9, 1, True), (1025, 16, 300, 3, 1, True), (2500, 32, 70, 2, 0, True), (5, 48, 97, 1023, 32, True), (9, 64, 0, 700, 0, False)])
+def test_plan_matches_the_definition(zq, batch, page, hi_cached, hi_new, words, tree):
+    rng = np.random.default_rng(batch + page)
+    cached = rng.integers(0, hi_cached + 1, batch).tolist()
+    new = rng.integers(0, hi_new + 1, batch).tolist()
+    new[-1] = hi_new                                   # (requests without a token are among the others)
+    table, free, max_pages, n_pages = plan_inputs(rng, cached, new, page)
+    rows = sum(new)
+    max_rows = rows + 3
+    parents = rand_parents(rng, new) if tree else None
+    want = plan_oracle(cached, new, page, free, len(free), table, max_rows, parents, words)
+    t = ints(table)
+    run = lambda out=None: zq.zoqat_op_cache_plan(ints(cached), ints(new), page, n_pages, ints(free), ints([len(free)]), t, max_rows,  # noqa: E731
+                                                  parents=ints(parents + [-1] * 3) if tree else None, mask_words=words, out=out)
+    got = run()
+    for again in range(2):
+        assert got["status"].item() == 0
+        for n in ("kv_len", "row_start", "row_request", "row_pos", "slot", "n_free"):
+            assert got[n].tolist() == want[n], n
+        if words:
+            assert got["tree_mask"].tolist() == want["tree_mask"]
+        assert t.tolist() == want["table"]
+        got = run(out=got)                             # the same call on its own results: nothing changes
+
+
+def test_plan_reports_what_it_cannot_serve_and_leaves_the_tables(zq):
+    table = [[4, -7, -7], [-7, -7, -7]]
+
+    def call(cached, new, free=(0, 1, 2, 3), n_free=None, n_pages=5, max_rows=40, parents=None, words=0):
+        t = ints(table)
+        got = zq.zoqat_op_cache_plan(ints(cached), ints(new), 16, n_pages, ints(list(free)), ints([len(free) if n_free is None else n_free]), t, max_rows,
+                                     parents=None if parents is None else ints(parents), mask_words=words)
+        return got, t.tolist()
+
+    for kw, status in ((dict(cached=[3, -1], new=[1, 1]), 1), (dict(cached=[3, 0], new=[1, -2]), 1), (dict(cached=[3, 0], new=[46, 0]), 1),
+                       (dict(cached=[3, 0], new=[20, 21]), 1), (dict(cached=[3, 0], new=[33, 0], words=1), 1),
+                       (dict(cached=[3, 0], new=[1, 1], n_free=5), 1), (dict(cached=[3, 0], new=[1, 1], n_free=-1), 1),
+                       (dict(cached=[2 ** 31 - 1, 0], new=[2 ** 31 - 1, 2 ** 31 - 1]), 1),
+                       (dict(cached=[3, 0], new=[14, 17], free=(0, 1)), 2), (dict(cached=[3, 0], new=[0, 1], free=(), n_free=0), 2)):
+        got, t = call(**kw)
+        assert got["status"].item() == status, kw
+        assert t == table and got["row_start"].tolist() == [0, 0, 0] and got["kv_len"].tolist() == [0, 0]
+        assert set(got["slot"].tolist()) == {-1} and set(got["row_request"].tolist()) == {-1}
+    # a page outside the pool costs the rows on it their slots and nothing else
+    got, t = call(cached=[3, 0], new=[1, 2], free=(0, 1, 2, 77))
+    assert got["status"].item() == 4 and got["slot"].tolist()[:3] == [4 * 16 + 3, -1, -1] and got["row_start"].tolist() == [0, 1, 3]
+    # a parent that is not before its child ends the walk there
+    got, _ = call(cached=[3, 0], new=[3, 0], parents=[-1, 1, 0] + [-1] * 37, words=1)
+    assert got["status"].item() == 8 and [r[0] for r in got["tree_mask"].tolist()[:3]] == [1, 2, 5]
+    got, _ = call(cached=[3, 0], new=[2, 0], parents=[-1, -2] + [-1] * 38, words=1)
+    assert got["status"].item() == 8
+
+
+# ---- append ---------------------------------------------------------------------------------------------------------
+def make_cache(n_pages, page, kv, dh, dtype, layout, fill=float("nan")):
+    if layout == "token":
+        return [torch.full((n_pages, page, kv, dh), fill, dtype=TYPES[dtype], device="cuda") for _ in range(2)]
+    if layout == "head":
+        return [torch.full((n_pages, kv, page, dh), fill, dtype=TYPES[dtype], device="cuda").transpose(1, 2) for _ in range(2)]
+    both = torch.full((n_pages, page, 2, kv, dh), fill, dtype=TYPES[dtype], device="cuda")      # k and v of a page side by side
+    return [both[:, :, 0], both[:, :, 1]]
+
+
+@pytest.mark.parametrize("dtype,rows,heads,kv,dh,page,layout,rope", [
+    ("f32", 1, 1, 1, 64, 16, "token", True), ("bf16", 5, 4, 2, 128, 16, "head", True), ("f16", 33, 7, 1, 64, 1, "token", False),
+    ("bf16", 8, 32, 32, 128, 64, "joint", True), ("f16", 300, 12, 4, 128, 128, "head", True), ("f32", 17, 6, 3, 128, 24, "joint", True)])
+def test_append_matches_the_definition(zq, dtype, rows, heads, kv, dh, page, layout, rope):
+    rng = np.random.default_rng(rows + heads)
+    n_pages = -(-rows // page) + 2
+    k, v = make_cache(n_pages, page, kv, dh, dtype, layout)
+    wide = (heads + 2 * kv) * dh
+    slab = torch.from_numpy(rng.standard_normal((rows, wide + 8)).astype(np.float32)).cuda()
+    qkv = slab[:, :wide]                                                # rows that stand apart
+    slot = rng.permutation(n_pages * page)[:rows]
+    pos = rng.integers(0, 50, rows)
+    if rows > 4:
+        slot[2] = -1
+    cos, sin = [torch.from_numpy(f(np.arange(50)[:, None] * 10000.0 ** (-np.arange(dh // 2) / (dh // 2))).astype(np.float32)).cuda() for f in (np.cos, np.sin)]
+    q_out = torch.full((rows, heads + 1, dh), 7.0, dtype=TYPES[dtype], device="cuda")[:, :heads]
+    q, err = zq.zoqat_op_cache_append(qkv, ints(pos.tolist()), ints(slot.tolist()), k, v, heads, cos=cos if rope else None, sin=sin if rope else None, q_out=q_out)
+    assert err.item() == 0
+    x = qkv.double().reshape(rows, heads + 2 * kv, dh).clone()
+    turned = x[:, :heads + kv].clone()
+    size = x.abs()
+    if rope:
+        c, s = cos.double()[pos][:, None], sin.double()[pos][:, None]
+        a, b = x[:, :heads + kv, :dh // 2], x[:, :heads + kv, dh // 2:]
+        turned = torch.cat([a * c - b * s, b * c + a * s], -1)
+        size = x.clone()
+        size[:, :heads + kv] = torch.cat([(a * c).abs() + (b * s).abs(), (b * c).abs() + (a * s).abs()], -1)
+        size = size.abs()
+    # one rounding to the type, two binary32 operations before it (three roundings of at most half a step of the parts)
+    half = torch.finfo(TYPES[dtype]).eps / 2
+    tiny = {"f32": 0.0, "bf16": 0.0, "f16": 2.0 ** -25}[dtype]
+    near = lambda got, want, sz: bool(((got.double() - want).abs() <= half * want.abs() + 3 * 2.0 ** -24 * sz * (1 + half) + tiny).all())  # noqa: E731
+    live = slot >= 0
+    assert near(q[live], turned[live][:, :heads], size[live][:, :heads])
+    assert bool((q[~live] == 7.0).all())
+    pg, off = slot[live] // page, slot[live] % page
+    assert near(k[pg, off], turned[live][:, heads:], size[live][:, heads:heads + kv])
+    assert near(v[pg, off], x[live][:, heads + kv:], torch.zeros_like(x[live][:, heads + kv:]))
+    # every other slot is as it was
+    other = torch.ones((n_pages, page), dtype=torch.bool)
+    other[pg, off] = False
+    assert bool(torch.isnan(k[other.cuda()]).all()) and bool(torch.isnan(v[other.cuda()]).all())
+
+
+def test_append_skips_and_reports_slots_and_positions_outside(zq):
+    k, v = make_cache(2, 16, 1, 64, "f32", "token", fill=3.0)
+    qkv = torch.ones((4, 3 * 64), device="cuda")
+    cos = torch.ones((8, 32), device="cuda")
+    q = torch.full((4, 1, 64), 7.0, device="cuda")
+    for pos, slot in (([0, 1, 2, 3], [0, 32, -1, 2 ** 30]), ([0, 8, -1, 99], [0, 5, 6, 7])):
+        k.fill_(3.0); v.fill_(3.0); q.fill_(7.0)
+        _, err = zq.zoqat_op_cache_append(qkv, ints(pos), ints(slot), k, v, 1, cos=cos, sin=cos, q_out=q)
+        assert err.item() == 40
+        assert bool((q[1:] == 7.0).all()) and bool((q[0] != 7.0).all())
+        if pos[1] == 1:
+            assert bool((k.view(32, 64)[1:] == 3.0).all()) and bool((v.view(32, 64)[1:] == 3.0).all())
+        else:
+            assert bool((k.view(32, 64)[1:] == 3.0).all())              # (v needs no position)
+
+
+# ---- attention --------------------------------------------------------------------------------------------------------
+def attention_problem(seed, dtype, heads, kv, dh, page, layout, cached, new, mask="tree", pad=2, gap=0, q_scale=1.0):
+    """Everything that no row may see is NaN: unused pages, the slots behind each request's end."""
+    rng = np.random.default_rng(seed)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    batch, rows = len(cached), sum(new)
+    L = [c + n for c, n in zip(cached, new)]
+    pages = [-(-x // page) for x in L]
+    max_pages, n_pages = max(pages) + 1, sum(pages) + 2
+    order = rng.permutation(n_pages).tolist()
+    k, v = make_cache(n_pages, page, kv, dh, dtype, layout)
+    table, keys, vals = [], [], []
+    for x, n in zip(L, pages):
+        mine, order = order[:n], order[n:]
+        table.append(mine + [-3] * (max_pages - n))
+        t = torch.arange(x, device="cuda")
+        pg, off = torch.tensor(mine + [0], device="cuda")[t // page], t % page
+        keys.append(torch.randn((x, kv, dh), generator=gen, device="cuda").to(TYPES[dtype]))
+        vals.append(torch.randn((x, kv, dh), generator=gen, device="cuda").to(TYPES[dtype]))
+        k[pg, off], v[pg, off] = keys[-1], vals[-1]
+    q = torch.full((rows + pad, heads + gap, dh), float("nan"), dtype=TYPES[dtype], device="cuda")[:, :heads]
+    q[:rows] = (q_scale * torch.randn((rows, heads, dh), generator=gen, device="cuda")).to(TYPES[dtype])
+    words = -(-max(new) // 32) if max(new) else 1
+    seen = []
+    for n in new:
+        if mask == "tree":
+            par = rand_parents(rng, [n])
+            seen.append([set(ancestors(par, i)) for i in range(n)])
+        elif mask == "random":                                          # rows that see no draft, not even themselves, among them
+            seen.append([set(np.nonzero(rng.random(n) < 0.3)[0].tolist()) if i % 3 else set() for i in range(n)])
+        else:
+            seen.append([set(range(i + 1)) for i in range(n)])
+    bits = [words_of(s, words) for r in seen for s in r] + [[-1] * words] * pad
+    start = [0]
+    for n in new:
+        start.append(start[-1] + n)
+    return dict(dtype=dtype, q=q, k=k, v=v, table=ints(table), kv_len=ints(L), row_start=ints(start), mask=ints(bits) if mask else None, rows=rows,
+                start=start, new=new, L=L, keys=keys, vals=vals, seen=seen, heads=heads, kv=kv, dh=dh, scale=1.0 / math.sqrt(dh))
+
+
+def attention_oracle(pr):
+    """(out, bound) in 64 bits.  bound: how far a correct evaluation may be off, element by element - see the test."""
+    out = torch.zeros((pr["rows"], pr["heads"], pr["dh"]), dtype=torch.float64, device="cuda")
+    bound = torch.zeros_like(out)
+    g, eps = pr["heads"] // pr["kv"], 2.0 ** -24
+    half = torch.finfo(TYPES[pr["dtype"]]).eps / 2
+    for b, (n, L) in enumerate(zip(pr["new"], pr["L"])):
+        if n == 0:
+            continue
+        vis = torch.zeros((n, L), dtype=torch.bool)
+        vis[:, :L - n] = True
+        for i, s in enumerate(pr["seen"][b]):
+            for j in s:
+                vis[i, L - n + j] = True
+        vis = vis.cuda()[:, None]
+        r = slice(pr["start"][b], pr["start"][b + 1])
+        for h in range(pr["kv"]):
+            hs = slice(h * g, (h + 1) * g)
+            q, k, v = pr["q"][r, hs].double(), pr["keys"][b][:, h].double(), pr["vals"][b][:, h].double()
+            s = torch.einsum("ngd,td->ngt", q, k) * pr["scale"]
+            mag = (torch.einsum("ngd,td->ngt", q.abs(), k.abs()) * pr["scale"]).amax(-1, keepdim=True)
+            s = s.masked_fill(~vis, -math.inf)
+            top = s.amax(-1, keepdim=True)
+            p = torch.exp(s - torch.where(torch.isinf(top), 0.0, top)).masked_fill(~vis, 0.0)
+            total = p.sum(-1, keepdim=True)
+            w = torch.where(total > 0, p / total, 0.0)
+            o = torch.einsum("ngt,td->ngd", w, torch.where(torch.isfinite(v), v, 0.0))
+            a = torch.einsum("ngt,td->ngd", w, torch.where(torch.isfinite(v), v.abs(), 0.0))
+            # scores: d products and sums in binary32, scaled, turned into base 2 (each a rounding of the score's size); the
+            # exponential 2^-22; sums over the keys in binary32; each moves the weights relatively by the sum of these
+            rel = 2 * ((pr["dh"] + 8) * eps * mag + 4 * 2.0 ** -22) + (L / 4 + 64) * eps
+            e = rel * 2 * a
+            if pr["dtype"] != "f32":
+                e = e + half * a * (1 + 2 * half)                       # the weights, rounded for the second product
+            if pr["dtype"] == "f16":
+                # weights under the subnormal step of binary16, after the scaling by 2^7
+                e = e + 2.0 ** -25 / 2.0 ** 7 * torch.where(torch.isfinite(v), v.abs(), 0.0).sum(0)[None, None] + 2.0 ** -25
+            out[r, hs], bound[r, hs] = o, e + half * (o.abs() + e)
+    return out, bound
+
+
+def run_attention(zq, pr, **kw):
+    rows, pad = pr["rows"], pr["q"].shape[0] - pr["rows"]
+    out = torch.full_like(pr["q"], 5.0) if "out" not in kw else kw.pop("out")
+    got, err = zq.zoqat_op_tree_attention(pr["q"], pr["k"], pr["v"], pr["table"], pr["kv_len"], pr["row_start"], tree_mask=pr["mask"], out=out, **kw)
+    assert err.item() == 0
+    if pad:
+        assert bool((got[rows:] == 5.0).all())                          # rows behind the last request
+    return got
+
+
+ATTENTION = [
+    # dtype, heads, kv, dh, page, layout, cached, new, mask
+    ("f32", 2, 2, 128, 16, "token", [37], [1], "tree"),
+    ("bf16", 2, 2, 128, 16, "token", [37], [1], "tree"),
+    ("f16", 2, 2, 64, 16, "token", [0], [1], "tree"),                       # nothing but the draft itself
+    ("f32", 4, 1, 64, 24, "joint", [0, 5, 63, 64, 65, 200], [1, 3, 0, 7, 2, 9], "tree"),
+    ("bf16", 4, 1, 64, 8, "joint", [0, 5, 127, 128, 129, 300], [1, 3, 0, 7, 2, 9], "tree"),
+    ("f16", 8, 2, 128, 64, "head", [0, 1, 255, 256, 511], [4, 4, 4, 4, 4], "random"),
+    ("f32", 8, 2, 128, 1, "head", [0, 1, 61, 62, 130], [4, 3, 4, 5, 4], "random"),
+    ("bf16", 8, 8, 128, 32, "token", [100, 0, 7], [33, 64, 40], "tree"),    # masks of two words, drafts across tile borders
+    ("bf16", 6, 2, 64, 128, "head", [500, 20], [50, 100], None),            # no mask; more than 128 queries per key head
+    ("f16", 14, 2, 128, 256, "joint", [300, 129, 0], [20, 37, 19], "tree"), # 7 query heads per key head
+    ("f16", 16, 1, 128, 16, "token", [90], [17], "random"),                 # one key head
+    ("f32", 14, 2, 64, 16, "token", [90, 3], [5, 2], "random"),
+    ("bf16", 3, 3, 128, 16, "token", [5000], [2], "tree"),                  # one context split over many CTAs
+    ("f32", 1, 1, 128, 64, "head", [9000], [3], "tree"),
+    ("f16", 4, 4, 64, 64, "token", [3] * 300, [1] * 300, None),             # many short requests
+    ("bf16", 20, 1, 128, 16, "token", [130, 1], [9, 2], "tree"),            # 20 query heads per key head
+]
+
+
+@pytest.mark.parametrize("case", ATTENTION, ids=lambda c: "-".join(str(x) for x in c[:6]) + f"-b{len(c[6])}-{c[8]}")
+def test_attention_matches_the_definition(zq, case):
+    dtype, heads, kv, dh, page, layout, cached, new, mask = case
+    pr = attention_problem(7, dtype, heads, kv, dh, page, layout, cached, new, mask)
+    got = run_attention(zq, pr)
+    want, bound = attention_oracle(pr)
+    off = (got[:pr["rows"]].double() - want).abs()
+    assert bool((off <= bound).all()), (float(off.max()), float((off / bound.clamp(min=1e-30)).max()))
+    if mask == "random" and cached[0] == 0:
+        assert bool((got[0] == 0).all())                                # a row that sees nothing
+    again = run_attention(zq, pr)
+    assert torch.equal(again[:pr["rows"]], got[:pr["rows"]])            # the same bits
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_attention_with_steep_scores_and_strided_rows(zq, dtype):
+    # scores of some hundreds: the running reference moves often, most weights vanish
+    pr = attention_problem(11, dtype, 4, 2, 128, 16, "token", [700, 45], [6, 9], "tree", gap=1, q_scale=30.0)
+    scratch = torch.full((24 << 20,), 255, dtype=torch.uint8, device="cuda")
+    got = run_attention(zq, pr, scratch=scratch)                        # (scratch full of NaN)
+    want, bound = attention_oracle(pr)
+    off = (got[:pr["rows"]].double() - want).abs()
+    assert bool((off <= bound).all()), (float(off.max()), float((off / bound.clamp(min=1e-30)).max()))
+
+
+@pytest.mark.parametrize("dtype,page", [("f32", 16), ("bf16", 16), ("f16", 128)])
+def test_unseen_drafts_may_hold_anything_and_seen_ones_count(zq, dtype, page):
+    # drafts 0 <- 1, 0 <- 2; draft 2's value holds infinities and NaN, its key NaN: rows 0 and 1 do not see it, row 2 does
+    for C in (0, 126, 300):
+        pr = attention_problem(5, dtype, 4, 2, 64, page, "token", [C], [3], "tree")
+        pr["mask"][:3] = ints([[1], [3], [5]])
+        pr["seen"] = [[{0}, {0, 1}, {0, 2}]]
+        want, bound = attention_oracle(pr)
+        at = C + 2
+        pg = pr["table"][0, at // page].item()
+        pr["v"][pg, at % page, :, 5] = float("inf")
+        pr["v"][pg, at % page, :, 6] = -float("inf")
+        pr["v"][pg, at % page, :, 7] = float("nan")
+        got = run_attention(zq, pr)
+        off = (got[:2].double() - want[:2]).abs()
+        assert bool((off <= bound[:2]).all())
+        assert bool((got[2, :, 5] == float("inf")).all()) and bool((got[2, :, 6] == -float("inf")).all()) and bool(torch.isnan(got[2, :, 7]).all())
+        clean = [e for e in range(64) if e not in (5, 6, 7)]
+        assert bool(((got[2][:, clean].double() - want[2][:, clean]).abs() <= bound[2][:, clean]).all())
+        pr["k"][pg, at % page] = float("nan")
+        got = run_attention(zq, pr)
+        assert bool(((got[:2].double() - want[:2]).abs() <= bound[:2]).all()) and bool(torch.isnan(got[2]).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_reports_bad_pages_and_requests(zq, dtype):
+    pr = attention_problem(3, dtype, 2, 2, 64, 16, "token", [40, 40, 40], [2, 2, 2], "tree")
+    good = run_attention(zq, pr).clone()
+    table = pr["table"].clone()
+    for bad in (-1, pr["k"].shape[0], 2 ** 31 - 1):
+        pr["table"][1, 1] = bad
+        out, err = zq.zoqat_op_tree_attention(pr["q"], pr["k"], pr["v"], pr["table"], pr["kv_len"], pr["row_start"], tree_mask=pr["mask"])
+        assert err.item() == 42 and bool(torch.isfinite(out[:6]).all())
+        assert torch.equal(out[:2], good[:2]) and torch.equal(out[4:6], good[4:6])
+    pr["table"].copy_(table)
+    for kv_len, start in (([42, 1, 42], [0, 2, 4, 6]), ([42, -5, 42], [0, 2, 4, 6]), ([42, 10 ** 6, 42], [0, 2, 4, 6]), ([42, 42, 42], [0, 2, 900, 902])):
+        out = torch.full_like(pr["q"], 5.0)
+        _, err = zq.zoqat_op_tree_attention(pr["q"], pr["k"], pr["v"], pr["table"], ints(kv_len), ints(start), tree_mask=pr["mask"], out=out)
+        assert err.item() == 41
+        assert torch.equal(out[:2], good[:2]) and bool((out[2:4] == 5.0).all())
+
+
+def test_attention_captured_and_replayed_as_lengths_change(zq):
+    # one graph; the lengths, tables and rows in its buffers change between replays (fewer tokens, other requests, none at all)
+    big = attention_problem(9, "bf16", 8, 2, 128, 16, "token", [900, 40, 3], [5, 5, 5], "tree")
+    out, err = torch.zeros_like(big["q"]), torch.zeros(1, dtype=torch.int32, device="cuda")
+    scratch = torch.empty(24 << 20, dtype=torch.uint8, device="cuda")
+    call = lambda: zq.zoqat_op_tree_attention(big["q"], big["k"], big["v"], big["table"], big["kv_len"], big["row_start"], tree_mask=big["mask"],  # noqa: E731
+                                              out=out, scratch=scratch, err=err)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for L, new, start in (([905, 45, 8], [5, 5, 5], [0, 5, 10, 15]), ([300, 0, 8], [2, 0, 5], [0, 2, 2, 7]), ([0, 0, 0], [0, 0, 0], [0, 0, 0, 0])):
+        big["kv_len"].copy_(ints(L))
+        big["row_start"].copy_(ints(start))
+        out.fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert err.item() == 0
+        pr = dict(big, rows=sum(new), start=start, new=new, L=L, keys=[k[:x] for k, x in zip(big["keys"], L)], vals=[v[:x] for v, x in zip(big["vals"], L)])
+        words = big["mask"].tolist()
+        pr["seen"] = [[{j for j in range(n) if (words[s + i][0] >> j) & 1} for i in range(n)] for n, s in zip(new, start)]
+        want, bound = attention_oracle(pr)
+        rows = sum(new)
+        assert bool(((out[:rows].double() - want).abs() <= bound).all()) and bool((out[rows:] == 5.0).all())
+
+
+def test_attention_on_another_stream(zq):
+    pr = attention_problem(2, "f16", 4, 4, 64, 32, "head", [200, 10], [3, 3], "tree")
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = run_attention(zq, pr)
+    side.synchronize()
+    want, bound = attention_oracle(pr)
+    assert bool(((got[:pr["rows"]].double() - want).abs() <= bound).all())
+
+
+def test_attention_reads_the_decode_paths_own_cache_layout(zq):
+    # [batch][heads][max_len][d_head] in fp32: a page per sequence
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    B, H, M, dh, L = 3, 2, 50, 64, [50, 17, 1]
+    k, v = [torch.randn((B, H, M, dh), generator=gen, device="cuda") for _ in range(2)]
+    q = torch.randn((B, H, dh), generator=gen, device="cuda")
+    out, err = zq.zoqat_op_tree_attention(q, k.transpose(1, 2), v.transpose(1, 2), ints([[0], [1], [2]]), ints(L), ints([0, 1, 2, 3]))
+    assert err.item() == 0
+    for b in range(B):
+        w = torch.softmax(torch.einsum("hd,htd->ht", q[b].double(), k[b, :, :L[b]].double()) / 8.0, -1)
+        want = torch.einsum("ht,htd->hd", w, v[b, :, :L[b]].double())
+        assert float((out[b].double() - want).abs().max()) < 2e-5
+
+
+# ---- rules ------------------------------------------------------------------------------------------------------------
+def rules_oracle(x, dtype, request, rules, V):
+    """The formula in numpy binary32, one rounding per operation, in the documented order."""
+    x = x.float().cpu().numpy().copy()
+    tokens = np.full(len(request), 99, dtype=np.int64)
+    for r, b in enumerate(request):
+        if b < 0:
+            continue
+        made, asked, bias, touched = np.zeros(V, dtype=np.int64), np.zeros(V, dtype=bool), np.zeros(V, dtype=np.float32), rules.get("bias") is not None
+        if rules.get("history") is not None:
+            hist, n, p = rules["history"][b], rules["history_len"][b], rules["prompt_len"][b] if rules.get("prompt_len") is not None else 0
+            for k, t in enumerate(hist[:n]):
+                if 0 <= t < V:
+                    if k < p:
+                        asked[t] = True
+                    else:
+                        made[t] += 1
+        if rules.get("drafts") is not None:
+            for j in rules["seen"][r]:
+                t = rules["drafts"][rules["row_start"][b] + j]
+                if 0 <= t < V:
+                    made[t] += 1
+        if touched:
+            for t, w in rules["bias"][b]:
+                if 0 <= t < V:
+                    bias[t] = np.float32(bias[t] + np.float32(w))
+        rep, freq, pres = [np.float32(rules[k][b]) if rules.get(k) is not None else np.float32(d) for k, d in (("repetition", 1), ("frequency", 0), ("presence", 0))]
+        row = x[r]
+        old = asked | (made > 0)
+        with np.errstate(divide="ignore", invalid="ignore", over="ignore"):
+            row = np.where(old, np.where(row > 0, row / rep, row * rep), row).astype(np.float32)
+            row = np.where(old, row - freq * made.astype(np.float32), row).astype(np.float32)
+            row = np.where(made > 0, row - pres, row).astype(np.float32)
+            if touched and len(rules["bias"][b]):
+                row = (row + bias).astype(np.float32)
+        if rules.get("allowed") is not None:
+            row = np.where(rules["allowed"][r], row, np.float32(-np.inf))
+        x[r] = row
+        y = torch.from_numpy(row).to(TYPES[dtype]).float().numpy()
+        best = -1
+        for t in np.argsort(-np.where(np.isnan(y), -np.inf, y), kind="stable")[:1]:
+            best = int(t) if y[t] > -np.inf else -1
+        tokens[r] = best
+    return torch.from_numpy(x).to(TYPES[dtype]), tokens
+
+
+def pack_bits(ok):
+    n = -(-ok.shape[1] // 32) * 32
+    full = np.zeros((ok.shape[0], n), dtype=np.uint8)
+    full[:, :ok.shape[1]] = ok
+    return torch.from_numpy(np.packbits(full, axis=1, bitorder="little").view(np.int32).copy()).cuda()
+
+
+@pytest.mark.parametrize("dtype,V,batch,per,groups", [
+    ("f32", 1, 1, 1, "h"), ("f32", 1000, 3, 1, ""), ("f32", 32000, 2, 3, "hpdba"), ("bf16", 50257, 2, 2, "hpdba"), ("f16", 777, 5, 4, "hpdb"),
+    ("f32", 131072, 1, 1, "hpb"), ("bf16", 4097, 40, 1, "a"), ("f32", 65537, 2, 1, "b"), ("f16", 8193, 3, 2, "d"), ("f32", 5000, 3, 1, "hba")])
+def test_rules_match_the_formula_bit_for_bit(zq, dtype, V, batch, per, groups):
+    rng = np.random.default_rng(V)
+    rows = batch * per
+    request = [r // per for r in range(rows)]
+    if rows > 3:
+        request[1] = -1                                                  # a padded row is left as it is
+    slab = torch.from_numpy((4 * rng.standard_normal((rows, V + 3))).astype(np.float32)).to(TYPES[dtype]).cuda()
+    logits = slab[:, :V]
+    R, kw = {}, {}
+    if "h" in groups:
+        H = 600
+        hist = np.minimum((V * rng.random((batch, H)) ** 6).astype(np.int64), V - 1)
+        hist[:, 7], hist[:, 11] = V, -1                                  # not tokens
+        R.update(history=hist.tolist(), history_len=rng.integers(0, H + 1, batch).tolist())
+        kw.update(history=ints(hist.tolist()), history_len=ints(R["history_len"]))
+        if "p" in groups:
+            R["prompt_len"] = [n // 3 for n in R["history_len"]]
+            kw["prompt_len"] = ints(R["prompt_len"])
+    if "h" in groups or "d" in groups:
+        for n, lo, hi in (("repetition", 0.8, 1.7), ("presence", -0.5, 1.0), ("frequency", 0.0, 0.3)):
+            R[n] = rng.uniform(lo, hi, batch).astype(np.float32).tolist()
+            kw[n] = torch.tensor(R[n], dtype=torch.float32, device="cuda")
+    if "b" in groups:
+        B = 70
+        tok = rng.integers(0, V, (batch, B))
+        tok[:, 1::3] = tok[:, :1]                                         # the same token many times
+        tok[:, 5], tok[:, 6] = V + 5, -1
+        val = (3 * rng.standard_normal((batch, B))).astype(np.float32)
+        n = rng.integers(0, B + 1, batch)
+        n[0] = B
+        R["bias"] = [list(zip(tok[b, :n[b]].tolist(), val[b, :n[b]].tolist())) for b in range(batch)]
+        kw.update(bias_token=ints(tok.tolist()), bias_value=torch.from_numpy(val).cuda(), bias_len=ints(n.tolist()))
+    if "a" in groups:
+        ok = rng.random((rows, V)) < 0.5
+        ok[0] = False                                                     # nothing is allowed
+        R["allowed"] = ok
+        kw["allowed"] = pack_bits(ok)
+    if "d" in groups:
+        R["drafts"] = rng.integers(-1, V + 1, rows).tolist()
+        R["row_start"] = [per * b for b in range(batch + 1)]
+        R["seen"] = [{j for j in range(r % per + 1) if j == r % per or rng.random() < 0.5} for r in range(rows)]
+        kw.update(draft_token=ints(R["drafts"]), row_start=ints(R["row_start"]), tree_mask=ints([words_of(s, 1) for s in R["seen"]]))
+    want, token = rules_oracle(logits, dtype, request, R, V)
+    rules = zq.LogitRules(batch=batch, row_request=ints(request), **kw)
+    out, tok = zq.zoqat_op_logit_rules(logits, rules, out=torch.full_like(logits, 3.0), token=ints([99] * rows))
+    want[[r for r in range(rows) if request[r] < 0]] = 3.0
+    assert tok.tolist() == token.tolist()
+    assert torch.equal(out.cpu(), want)
+    _, only = zq.zoqat_op_logit_rules(logits, rules, want_logits=False, token=ints([99] * rows))
+    assert only.tolist() == token.tolist()
+    keep = slab.clone()
+    zq.zoqat_op_logit_rules(logits, rules, out=logits, token=ints([99] * rows))                     # in place
+    live = [r for r in range(rows) if request[r] >= 0]
+    assert torch.equal(logits[live].cpu(), want[live]) and torch.equal(slab[:, V:], keep[:, V:])
+
+
+def test_rules_choice_with_ties_infinities_and_nan(zq):
+    V = 9000
+    x = torch.zeros((4, V), device="cuda")
+    x[1] = -float("inf")
+    x[2] = float("nan")
+    x[2, 8999] = -5.0
+    x[3, 4000:] = float("inf")
+    _, tok = zq.zoqat_op_logit_rules(x, zq.LogitRules(batch=4))
+    assert tok.tolist() == [0, -1, 8999, 4000]
