@@ -441,174 +441,176 @@ def zoqat_op_head_loss_static(a, b, labels, token_loss, loss_sum, count, err, im
 
 # ---- serving drafted tokens over a paged cache ---------------------------------------------
 _TYPES = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
+_I32, _F32 = torch.int32, torch.float32
 
 
-def _refuse(cond, text):
-    if cond:
-        raise ZoqatError(ERR_INVALID_ARG, text)
+def _refuse(text):
+    raise ZoqatError(ERR_INVALID_ARG, text)
 
 
-def _need(name, t, dtype, shape=None):
-    """A contiguous tensor of this type (and shape; None entries are free) on the current CUDA device."""
-    _refuse(t.dtype != dtype or not t.is_contiguous(), f"{name}: a contiguous {dtype} tensor is needed")
-    _refuse(not t.is_cuda or t.device.index != torch.cuda.current_device(), f"{name}: not on the current CUDA device")
-    _refuse(shape is not None and (t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape))),
-            f"{name}: shape {tuple(t.shape)}, {shape} is needed")
+def _here():
+    """(index of the current device, its current stream): looked up once per call, these calls run in decode loops."""
+    dev = torch.cuda.current_device()
+    return dev, torch._C._cuda_getCurrentRawStream(dev)
 
 
-def _rows(name, t, dtype, heads, d_head):
-    """[rows, heads, d_head] whose rows may stand apart."""
-    _refuse(t.dtype != dtype or t.dim() != 3 or tuple(t.shape[1:]) != (heads, d_head), f"{name}: [rows, {heads}, {d_head}] of {dtype} is needed")
-    _refuse(t.stride(2) != 1 or (heads > 1 and t.stride(1) != d_head), f"{name}: heads must stand back to back")
-    _refuse(not t.is_cuda or t.device.index != torch.cuda.current_device(), f"{name}: not on the current CUDA device")
-    return t.stride(0) if t.shape[0] > 1 else heads * d_head
+def _flat(dev, name, t, dtype, n0, n1=None):
+    """Address of a contiguous [n0] (or [n0, n1]) tensor of this type on device `dev`; sizes of -1 are free.  None -> NULL."""
+    if t is None:
+        return None
+    s = t.shape
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        _refuse(f"{name}: a contiguous {dtype} tensor on the current CUDA device is needed")
+    if len(s) != (1 if n1 is None else 2) or (n0 >= 0 and s[0] != n0) or (n1 is not None and n1 >= 0 and s[1] != n1):
+        _refuse(f"{name}: shape {tuple(s)}, {(n0,) if n1 is None else (n0, n1)} is needed")
+    return t.data_ptr()
+
+
+def _rows(dev, name, t, dtype, rows, heads, d_head):
+    """(address, row stride) of [>= rows, heads, d_head] whose rows may stand apart."""
+    s, st = t.shape, t.stride()
+    if t.dtype is not dtype or t.get_device() != dev or len(s) != 3 or s[0] < rows or s[1] != heads or s[2] != d_head:
+        _refuse(f"{name}: [{rows}, {heads}, {d_head}] of {dtype} on the current CUDA device is needed")
+    if st[2] != 1 or (heads > 1 and st[1] != d_head):
+        _refuse(f"{name}: heads must stand back to back")
+    return t.data_ptr(), st[0] if s[0] > 1 else heads * d_head
+
+
+def _caches(dev, k, v):
+    s, st, ty = k.shape, k.stride(), _TYPES.get(k.dtype, -1)
+    if ty < 0 or v.dtype is not k.dtype or k.get_device() != dev or v.get_device() != dev:
+        _refuse("caches must both be float32, bfloat16 or float16 tensors on the current CUDA device")
+    if len(s) != 4 or v.shape != s or v.stride() != st or st[3] != 1:
+        _refuse("caches must be [n_pages, page_size, n_kv_heads, d_head] with the same strides and contiguous heads")
+    return PagedCache(k.data_ptr(), v.data_ptr(), ty, s[0], s[1], s[2], s[3], 0, st[0], st[1], st[2])
 
 
 def paged_cache(k_cache, v_cache):
     """zoqat_paged_cache_t of two tensors [n_pages, page_size, n_kv_heads, d_head] with the same strides (a cache laid out head by
     head is passed as its transposed view)."""
-    _refuse(k_cache.dtype not in _TYPES or k_cache.dtype != v_cache.dtype, "caches must both be float32, bfloat16 or float16")
-    _refuse(k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride() or k_cache.stride(3) != 1,
-            "caches must be [n_pages, page_size, n_kv_heads, d_head] with the same strides and contiguous heads")
-    for t in (k_cache, v_cache):
-        _refuse(not t.is_cuda or t.device.index != torch.cuda.current_device(), "caches: not on the current CUDA device")
-    n, ps, kv, dh = k_cache.shape
-    return PagedCache(k_cache.data_ptr(), v_cache.data_ptr(), _TYPES[k_cache.dtype], n, ps, kv, dh, 0, k_cache.stride(0), k_cache.stride(1),
-                      k_cache.stride(2))
+    return _caches(torch.cuda.current_device(), k_cache, v_cache)
 
 
 def zoqat_op_cache_plan(cached_len, new_len, page_size, n_pages, free_pages, n_free, block_table, max_rows, parents=None, mask_words=0, out=None):
     """-> dict of int32 tensors: kv_len, row_start, row_request, row_pos, slot, n_free, status and, with mask_words, tree_mask.
     block_table is extended in place.  out: such a dict of an earlier call to write into (its status word is or-ed)."""
+    dev, stream = _here()
     batch = cached_len.shape[0]
-    dev = cached_len.device
     if out is None:
         shapes = dict(kv_len=(batch,), row_start=(batch + 1,), row_request=(max_rows,), row_pos=(max_rows,), slot=(max_rows,), n_free=(1,))
         if mask_words:
             shapes["tree_mask"] = (max_rows, mask_words)
-        out = {n: torch.empty(s, dtype=torch.int32, device=dev) for n, s in shapes.items()}
-        out["status"] = torch.zeros(1, dtype=torch.int32, device=dev)
-    i32 = torch.int32
-    _need("cached_len", cached_len, i32, (None,))
-    _need("new_len", new_len, i32, (batch,))
-    _need("free_pages", free_pages, i32, (None,))
-    _need("n_free", n_free, i32, (1,))
-    _need("block_table", block_table, i32, (batch, None))
-    if parents is not None:
-        _need("parents", parents, i32, (max_rows,))
-    for n, shape in (("kv_len", (batch,)), ("row_start", (batch + 1,)), ("row_request", (max_rows,)), ("row_pos", (max_rows,)), ("slot", (max_rows,)),
-                     ("n_free", (1,)), ("status", (1,))):
-        _need(n, out[n], i32, shape)
-    mask = out["tree_mask"] if mask_words else None
-    if mask is not None:
-        _need("tree_mask", mask, i32, (max_rows, mask_words))
-    _check(lib().zoqat_op_cache_plan(_p(cached_len), _p(new_len), batch, page_size, n_pages, _p(free_pages), free_pages.shape[0], _p(n_free),
-                                     _p(block_table), block_table.shape[1], _p(parents), max_rows, mask_words, _p(out["kv_len"]),
-                                     _p(out["row_start"]), _p(out["row_request"]), _p(out["row_pos"]), _p(out["slot"]), _p(mask),
-                                     _p(out["n_free"]), _p(out["status"]), _stream()))
+        out = {n: torch.empty(s, dtype=_I32, device=cached_len.device) for n, s in shapes.items()}
+        out["status"] = torch.zeros(1, dtype=_I32, device=cached_len.device)
+    _check(lib().zoqat_op_cache_plan(
+        _flat(dev, "cached_len", cached_len, _I32, batch), _flat(dev, "new_len", new_len, _I32, batch), batch, page_size, n_pages,
+        _flat(dev, "free_pages", free_pages, _I32, -1), free_pages.shape[0], _flat(dev, "n_free", n_free, _I32, 1),
+        _flat(dev, "block_table", block_table, _I32, batch, -1), block_table.shape[1], _flat(dev, "parents", parents, _I32, max_rows), max_rows, mask_words,
+        _flat(dev, "kv_len", out["kv_len"], _I32, batch), _flat(dev, "row_start", out["row_start"], _I32, batch + 1),
+        _flat(dev, "row_request", out["row_request"], _I32, max_rows), _flat(dev, "row_pos", out["row_pos"], _I32, max_rows),
+        _flat(dev, "slot", out["slot"], _I32, max_rows), _flat(dev, "tree_mask", out["tree_mask"], _I32, max_rows, mask_words) if mask_words else None,
+        _flat(dev, "n_free", out["n_free"], _I32, 1), _flat(dev, "status", out["status"], _I32, 1), stream))
     return out
 
 
 def zoqat_op_cache_append(qkv, row_pos, slot, k_cache, v_cache, n_heads, cos=None, sin=None, q_out=None, err=None):
     """qkv float32 [rows, (n_heads + 2 n_kv_heads) * d_head] -> (q_out [rows, n_heads, d_head] of the caches' type, err)."""
-    cache = paged_cache(k_cache, v_cache)
-    rows, dh = qkv.shape[0], cache.d_head
-    _refuse(qkv.dtype != torch.float32 or qkv.dim() != 2 or qkv.shape[1] != (n_heads + 2 * cache.n_kv_heads) * dh or qkv.stride(1) != 1,
-            "qkv: float32 [rows, (n_heads + 2 n_kv_heads) * d_head] is needed")
-    _refuse(qkv.device != k_cache.device, "qkv: not on the caches' device")
-    _need("slot", slot, torch.int32, (rows,))
-    if cos is not None:
-        _need("row_pos", row_pos, torch.int32, (rows,))
-        _need("cos", cos, torch.float32, (None, dh // 2))
-        _need("sin", sin, torch.float32, (cos.shape[0], dh // 2))
+    dev, stream = _here()
+    cache = _caches(dev, k_cache, v_cache)
+    rows, dh, st = qkv.shape[0], cache.d_head, qkv.stride()
+    if qkv.dtype is not _F32 or qkv.get_device() != dev or len(st) != 2 or qkv.shape[1] != (n_heads + 2 * cache.n_kv_heads) * dh or st[1] != 1:
+        _refuse("qkv: float32 [rows, (n_heads + 2 n_kv_heads) * d_head] on the current CUDA device is needed")
     if q_out is None:
         q_out = torch.empty((rows, n_heads, dh), dtype=k_cache.dtype, device=qkv.device)
     if err is None:
-        err = torch.zeros(1, dtype=torch.int32, device=qkv.device)
-    q_stride = _rows("q_out", q_out, k_cache.dtype, n_heads, dh)
-    _refuse(q_out.shape[0] < rows, "q_out: too few rows")
-    _check(lib().zoqat_op_cache_append(_p(qkv), qkv.stride(0) if rows > 1 else qkv.shape[1], _p(row_pos), _p(slot), rows, n_heads, _p(cos), _p(sin),
-                                       cos.shape[0] if cos is not None else 0, ctypes.byref(cache), _p(q_out), q_stride, _p(err), _stream()))
+        err = torch.zeros(1, dtype=_I32, device=qkv.device)
+    q_ptr, q_stride = _rows(dev, "q_out", q_out, k_cache.dtype, rows, n_heads, dh)
+    n_rope = cos.shape[0] if cos is not None else 0
+    _check(lib().zoqat_op_cache_append(
+        qkv.data_ptr(), st[0] if rows > 1 else qkv.shape[1], _flat(dev, "row_pos", row_pos, _I32, rows) if n_rope else None,
+        _flat(dev, "slot", slot, _I32, rows), rows, n_heads, _flat(dev, "cos", cos, _F32, n_rope, dh // 2), _flat(dev, "sin", sin, _F32, n_rope, dh // 2),
+        n_rope, cache, q_ptr, q_stride, _flat(dev, "err", err, _I32, 1), stream))
     return q_out, err
 
 
 def zoqat_op_tree_attention(q, k_cache, v_cache, block_table, kv_len, row_start, tree_mask=None, scale=None, out=None, scratch=None, err=None):
     """q [rows, n_heads, d_head] of the caches' type -> (out of the same form, err).  scale: 1 / sqrt(d_head) by default."""
-    cache = paged_cache(k_cache, v_cache)
+    dev, stream = _here()
+    cache = _caches(dev, k_cache, v_cache)
     rows, heads, dh = q.shape
     batch = kv_len.shape[0]
-    q_stride = _rows("q", q, k_cache.dtype, heads, cache.d_head)
-    _need("block_table", block_table, torch.int32, (batch, None))
-    _need("kv_len", kv_len, torch.int32, (batch,))
-    _need("row_start", row_start, torch.int32, (batch + 1,))
+    q_ptr, q_stride = _rows(dev, "q", q, k_cache.dtype, rows, heads, cache.d_head)
     words = 0
     if tree_mask is not None:
-        _need("tree_mask", tree_mask, torch.int32, (None, None))
-        _refuse(tree_mask.shape[0] < rows, "tree_mask: too few rows")
         words = tree_mask.shape[1]
+        if tree_mask.shape[0] < rows:
+            _refuse("tree_mask: too few rows")
     if out is None:
         out = torch.empty((rows, heads, dh), dtype=q.dtype, device=q.device)
-    out_stride = _rows("out", out, k_cache.dtype, heads, dh)
-    _refuse(out.shape[0] < rows, "out: too few rows")
+    out_ptr, out_stride = _rows(dev, "out", out, k_cache.dtype, rows, heads, dh)
     if scratch is None:
         nb = ctypes.c_size_t()
         _check(lib().zoqat_op_tree_attention_scratch_bytes(cache.type, dh, ctypes.byref(nb)))
         scratch = torch.empty(nb.value, dtype=torch.uint8, device=q.device)
     if err is None:
-        err = torch.zeros(1, dtype=torch.int32, device=q.device)
-    _check(lib().zoqat_op_tree_attention(_p(q), q_stride, ctypes.byref(cache), _p(block_table), block_table.shape[1], _p(kv_len), _p(row_start),
-                                         _p(tree_mask), words, batch, rows, heads, dh ** -0.5 if scale is None else scale, _p(out), out_stride,
-                                         _p(scratch), scratch.numel() * scratch.element_size(), _p(err), _stream()))
+        err = torch.zeros(1, dtype=_I32, device=q.device)
+    if scratch.get_device() != dev or not scratch.is_contiguous():
+        _refuse("scratch: a contiguous tensor on the current CUDA device is needed")
+    _check(lib().zoqat_op_tree_attention(
+        q_ptr, q_stride, cache, _flat(dev, "block_table", block_table, _I32, batch, -1), block_table.shape[1], _flat(dev, "kv_len", kv_len, _I32, batch),
+        _flat(dev, "row_start", row_start, _I32, batch + 1), _flat(dev, "tree_mask", tree_mask, _I32, -1, words), words, batch, rows, heads,
+        dh ** -0.5 if scale is None else scale, out_ptr, out_stride, scratch.data_ptr(), scratch.numel() * scratch.element_size(),
+        _flat(dev, "err", err, _I32, 1), stream))
     return out, err
 
 
 class LogitRules:
     """zoqat_logit_rules_t over tensors, which it keeps alive; every group may be left out."""
+    __slots__ = ("desc", "tensors", "max_rows", "dev")
 
     def __init__(self, batch=None, row_request=None, repetition=None, presence=None, frequency=None, history=None, history_len=None,
                  prompt_len=None, bias_token=None, bias_value=None, bias_len=None, allowed=None, draft_token=None, row_start=None, tree_mask=None):
-        i32, f32 = torch.int32, torch.float32
         if batch is None:
-            sized = [t for t in (history_len, repetition, presence, frequency, bias_len) if t is not None]
-            _refuse(not sized, "batch is needed when no rule is per request")
-            batch = sized[0].shape[0]
-        for n, t, dtype, shape in (("row_request", row_request, i32, (None,)), ("repetition", repetition, f32, (batch,)), ("presence", presence, f32, (batch,)),
-                                   ("frequency", frequency, f32, (batch,)), ("history", history, i32, (batch, None)), ("history_len", history_len, i32, (batch,)),
-                                   ("prompt_len", prompt_len, i32, (batch,)), ("bias_token", bias_token, i32, (batch, None)),
-                                   ("bias_value", bias_value, f32, None if bias_token is None else tuple(bias_token.shape)), ("bias_len", bias_len, i32, (batch,)),
-                                   ("allowed", allowed, i32, (None, None)), ("draft_token", draft_token, i32, (None,)), ("row_start", row_start, i32, (batch + 1,)),
-                                   ("tree_mask", tree_mask, i32, (None, None))):
-            if t is not None:
-                _need(n, t, dtype, shape)
+            sized = next((t for t in (history_len, repetition, presence, frequency, bias_len) if t is not None), None)
+            if sized is None:
+                _refuse("batch is needed when no rule is per request")
+            batch = sized.shape[0]
+        dev = self.dev = torch.cuda.current_device()
+        n_bias = bias_token.shape[1] if bias_token is not None else 0
         self.tensors = (row_request, repetition, presence, frequency, history, history_len, prompt_len, bias_token, bias_value, bias_len, allowed,
                         draft_token, row_start, tree_mask)
-        self.row_request, self.allowed, self.draft_token, self.tree_mask = row_request, allowed, draft_token, tree_mask
-        self.desc = LogitRulesDesc(*[t.data_ptr() if t is not None else None for t in self.tensors], history.shape[1] if history is not None else 0,
-                                   allowed.shape[1] if allowed is not None else 0, bias_token.shape[1] if bias_token is not None else 0,
-                                   tree_mask.shape[1] if tree_mask is not None else 0, batch, 0)
-
-    def check_rows(self, rows):
-        for n in ("row_request", "allowed", "draft_token", "tree_mask"):
-            t = getattr(self, n)
-            _refuse(t is not None and t.shape[0] < rows, f"{n}: too few rows")
+        self.max_rows = min([t.shape[0] for t in (row_request, allowed, draft_token, tree_mask) if t is not None], default=1 << 30)
+        self.desc = LogitRulesDesc(
+            _flat(dev, "row_request", row_request, _I32, -1), _flat(dev, "repetition", repetition, _F32, batch), _flat(dev, "presence", presence, _F32, batch),
+            _flat(dev, "frequency", frequency, _F32, batch), _flat(dev, "history", history, _I32, batch, -1), _flat(dev, "history_len", history_len, _I32, batch),
+            _flat(dev, "prompt_len", prompt_len, _I32, batch), _flat(dev, "bias_token", bias_token, _I32, batch, n_bias),
+            _flat(dev, "bias_value", bias_value, _F32, batch, n_bias), _flat(dev, "bias_len", bias_len, _I32, batch), _flat(dev, "allowed", allowed, _I32, -1, -1),
+            _flat(dev, "draft_token", draft_token, _I32, -1), _flat(dev, "row_start", row_start, _I32, batch + 1), _flat(dev, "tree_mask", tree_mask, _I32, -1, -1),
+            history.shape[1] if history is not None else 0, allowed.shape[1] if allowed is not None else 0, n_bias,
+            tree_mask.shape[1] if tree_mask is not None else 0, batch, 0)
 
 
 def zoqat_op_logit_rules(logits, rules, out=None, token=None, want_logits=True):
     """logits [rows, vocab] (rows may stand apart) -> (out of the same type or None, token int32 [rows]).  out may be logits."""
-    _refuse(logits.dtype not in _TYPES or logits.dim() != 2 or logits.stride(1) != 1, "logits: [rows, vocab] of float32, bfloat16 or float16 is needed")
-    _refuse(not logits.is_cuda or logits.device.index != torch.cuda.current_device(), "logits: not on the current CUDA device")
-    rows, vocab = logits.shape
-    rules.check_rows(rows)
+    dev, stream = _here()
+    s, st, ty = logits.shape, logits.stride(), _TYPES.get(logits.dtype, -1)
+    if ty < 0 or logits.get_device() != dev or rules.dev != dev or len(s) != 2 or st[1] != 1:
+        _refuse("logits: [rows, vocab] of float32, bfloat16 or float16 on the current CUDA device (the rules' one) is needed")
+    rows, vocab = s
+    if rules.max_rows < rows:
+        _refuse("rules: row_request, allowed, draft_token or tree_mask has too few rows")
     if out is None and want_logits:
         out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
     if token is None:
-        token = torch.empty(rows, dtype=torch.int32, device=logits.device)
-    _need("token", token, torch.int32, (rows,))
+        token = torch.empty(rows, dtype=_I32, device=logits.device)
+    out_ptr = out_ld = 0
     if out is not None:
-        _refuse(out.dtype != logits.dtype or out.shape != logits.shape or out.stride(1) != 1 or out.device != logits.device, "out: not like logits")
-    ld = lambda t: t.stride(0) if t.shape[0] > 1 else max(t.stride(0), vocab)  # noqa: E731
-    _check(lib().zoqat_op_logit_rules(_p(logits), _TYPES[logits.dtype], ld(logits), rows, vocab, ctypes.byref(rules.desc), _p(out),
-                                      ld(out) if out is not None else 0, _p(token), _stream()))
+        so = out.stride()
+        if out.dtype is not logits.dtype or out.get_device() != dev or out.shape != s or so[1] != 1:
+            _refuse("out: not like logits")
+        out_ptr, out_ld = out.data_ptr(), so[0] if rows > 1 else max(so[0], vocab)
+    _check(lib().zoqat_op_logit_rules(logits.data_ptr(), ty, st[0] if rows > 1 else max(st[0], vocab), rows, vocab, rules.desc, out_ptr, out_ld,
+                                      _flat(dev, "token", token, _I32, rows), stream))
     return out, token
 
 

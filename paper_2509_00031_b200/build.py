@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libzoqat.so")
 SOURCES = ["api.cu", "weights.cu", "activations.cu", "attention.cu", "attention_tc.cu", "gemm_simt.cu", "gemm_tc.cu", "decode.cu",
-           "serve_plan.cu", "tree_attention.cu", "tree_attention_tc.cu", "logit_rules.cu"]
+           "serve_plan.cu", "tree_attention.cu", "tree_attention_tc.cu", "tree_attention_keys.cu", "logit_rules.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 

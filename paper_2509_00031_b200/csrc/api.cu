@@ -1920,7 +1920,7 @@ int zoqat_op_tree_attention(const void* q_dev, int64_t q_stride, const zoqat_pag
     a.out = out_dev; a.out_stride = out_stride; a.scratch = static_cast<uint8_t*>(scratch_dev); a.err_flag = err_flag_dev;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int rc = tc ? launch_tree_attention_tc(a, s, false) : launch_tree_attention_simt(a, s, false);
-    if (rc != ZOQAT_OK) return fail(rc, "tree attention rejected (%d query heads per key head; bf16 / fp16 need lcm(8, heads per key head) <= 128)", n_heads / c.n_kv_heads);
+    if (rc != ZOQAT_OK) return fail(rc, "tree attention launch failed");
     CUDA_TRY(cudaGetLastError());
     return ZOQAT_OK;
 }

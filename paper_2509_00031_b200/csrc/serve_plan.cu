@@ -138,15 +138,23 @@ cache_plan_kernel(PlanParams p) {
         else atomicOr(p.status, kPlanBadPage);
         p.row_request[r] = b;
         p.slot[r] = slot;
+        uint32_t* mask = p.tree_mask + (size_t)r * p.mask_words;
+        if (!p.parents) {                       // a chain: everything up to the row itself
+            for (int w = 0; w < p.mask_words; ++w) {
+                const int upto = i + 1 - 32 * w;
+                mask[w] = upto <= 0 ? 0u : (upto >= 32 ? 0xFFFFFFFFu : (1u << upto) - 1u);
+            }
+            p.row_pos[r] = t;
+            continue;
+        }
         // the draft and its ancestors, from itself down: parents come before their children, so the words of the mask are
         // finished one after the other
         int depth = 0, j = i, word = p.mask_words - 1;
         uint32_t bits = 0;
-        uint32_t* mask = p.tree_mask + (size_t)r * p.mask_words;
         while (true) {
             while (word >= 0 && word > (j >> 5)) { mask[word--] = bits; bits = 0; }
             bits |= 1u << (j & 31);
-            const int up = p.parents ? __ldg(p.parents + start + j) : j - 1;
+            const int up = __ldg(p.parents + start + j);
             if (up < -1 || up >= j) { atomicOr(p.status, kPlanBadParent); break; }
             if (up < 0) break;
             ++depth;

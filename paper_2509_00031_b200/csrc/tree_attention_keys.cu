@@ -1,0 +1,544 @@
+// Attention of drafted rows over a paged bf16 / fp16 cache on the tensor cores, for few queries per key head (up to 64 in a tile:
+// single tokens, small trees).  The keys are the rows of both products:
+//
+//   S^T[key, query] = K Q^T            one thread per key reads its N scores from TMEM
+//   P^T[key, query] = 2^(S^T - ref)    rounded to the cache's type, to shared memory
+//   O^T[column, query] += V^T P^T      V as it lies in the page
+//   l[query] += 1^T P^T                the sums of the weights, by a third product with a matrix of ones: every TMEM lane has
+//                                      them where it needs them at the end, and no thread adds up anything
+//
+// so the softmax costs 128 * N exponentials per tile of 128 keys, spread over all four schedulers, whatever the tile's number of
+// live queries N = 16, 32 or 64 is; with queries as rows (tree_attention_tc.cu) a single query would cost a whole warp's 128
+// exponentials on one scheduler, and the kernel would be bound by them instead of by reading the cache.  What bounds it is
+// the cache: 64 KB a tile at d_head 128, some 2800 cycles of an SM's share of the memory, against about 600 of the tensor pipe
+// and 64 N of the exponential units.
+//
+// One persistent CTA per SM, 12 warps; the key tiles of all requests are dealt out in equal runs (tree_attention.cuh):
+//   warp 0      K and V tiles by TMA into a ring; warps 2, 3: query tiles into two buffers, a piece ahead
+//   warp 1      one thread issues the products, the scores one tile ahead
+//   warps 4-7   softmax.  All keys of a query share one reference; it moves only when a score passes it by more than 2^8, which
+//               the warps tell one another through four flags per tile while they compute the exponentials as if it did not.
+//               Maxima over the keys are formed only when a piece begins or a reference moves.
+//   warps 8-11  outputs of a finished piece, from the other one of two TMEM accumulators, while the next piece runs
+// Rounding, masked values and bounded waits as in tree_attention_tc.cu, but for the sums, which are those of the rounded weights.
+#include "tree_attention_tc.cuh"
+#include "../../include/zoqat.h"
+
+namespace zq {
+namespace {
+
+constexpr int kKeyThreads = 384;
+constexpr float kNoRef = -1.0e30f;       // reference of a query that has seen nothing: any score passes it
+
+template <int DH, int N> struct KeyCfg {
+    static constexpr int kTileBytes = kKeys * DH * 2;
+    static constexpr int kQBytes = N * DH * 2, kPBytes = N * kKeys * 2;
+    static constexpr int kFixed = 1024 + 2 * kQBytes + 2 * kPBytes + N * 16 + 6 * N * 4 + 1024;
+    static constexpr int kFit = (232448 - kFixed) / kTileBytes;
+    static constexpr int kStages = kFit > 10 ? 10 : kFit;
+    static constexpr int kOffQ = kStages * kTileBytes;
+    static constexpr int kOffP = kOffQ + 2 * kQBytes;
+    static constexpr int kOffOnes = kOffP + 2 * kPBytes;                    // one 1024-byte group of ones
+    static constexpr int kOffRed = kOffOnes + 1024;                         // [N][4 warps] floats
+    static constexpr int kOffRef = kOffRed + N * 16;                        // [2][N] floats, then [4][N]: those of the last pieces
+    static constexpr int kOffBar = kOffRef + 6 * N * 4;
+    // ring, q full / empty, s full, p full, o full, o empty, out full (2 each), piece done (4), flags, joint
+    static constexpr int kBars = 2 * kStages + 14 + 4 + 2;
+    static constexpr int kOffMisc = kOffBar + kBars * 8;
+    static constexpr int kUsedBytes = kOffMisc + 64 + 96 + (int)sizeof(TreeRun);
+    static constexpr int kSmemBytes = kUsedBytes + 1024 > 232448 ? 232448 : kUsedBytes + 1024;
+    static_assert(kUsedBytes <= 232448 && kStages >= 4, "shared memory");
+};
+
+// N scores of the thread's key
+template <int N> __device__ __forceinline__ void load_scores(uint32_t taddr, uint32_t (&v)[N]);
+template <> __device__ __forceinline__ void load_scores<16>(uint32_t taddr, uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr) : "memory");
+}
+template <> __device__ __forceinline__ void load_scores<32>(uint32_t taddr, uint32_t (&v)[32]) { tmem_ld32(taddr, v); }
+template <> __device__ __forceinline__ void load_scores<64>(uint32_t taddr, uint32_t (&v)[64]) {
+    uint32_t a[32], b[32];
+    tmem_ld32(taddr, a);
+    tmem_ld32(taddr + 32u, b);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) { v[e] = a[e]; v[32 + e] = b[e]; }
+}
+__device__ __forceinline__ void store16(uint32_t taddr, const uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+          "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+
+// Largest v[i] over the warp's 32 lanes, for i = 0 .. 31 at once: the return value of lane i is that of v[i].
+__device__ __forceinline__ float largest32(float (&v)[32]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int h = 16; h >= 1; h >>= 1) {
+        const bool up = lane & h;
+#pragma unroll
+        for (int i = 0; i < h; ++i) {
+            const float keep = up ? v[i + h] : v[i], give = up ? v[i] : v[i + h];
+            v[i] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, h));
+        }
+    }
+    return v[0];
+}
+// the same for 16 values: lanes 2 i and 2 i + 1 hold that of v[i]
+__device__ __forceinline__ float largest16(float (&v)[16]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int h = 8; h >= 1; h >>= 1) {
+        const bool up = lane & (2 * h);
+#pragma unroll
+        for (int i = 0; i < h; ++i) {
+            const float keep = up ? v[i + h] : v[i], give = up ? v[i] : v[i + h];
+            v[i] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, 2 * h));
+        }
+    }
+    return fmaxf(v[0], __shfl_xor_sync(0xffffffffu, v[0], 1));
+}
+// Largest value per query over the warp's keys into red[n][warp].
+template <int N>
+__device__ __forceinline__ void largest_into(const float (&v)[N], float* red, int warp) {
+    const int lane = threadIdx.x & 31;
+    if constexpr (N == 16) {
+        float t[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t[i] = v[i];
+        const float r = largest16(t);
+        if (!(lane & 1)) red[(lane >> 1) * 4 + warp] = r;
+    } else {
+#pragma unroll
+        for (int q = 0; q < N / 32; ++q) {
+            float t[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) t[i] = v[32 * q + i];
+            red[(32 * q + lane) * 4 + warp] = largest32(t);
+        }
+    }
+}
+
+// Shared-memory descriptor of the weights: query-major cores of 8 queries x 8 keys (128 bytes), no swizzle; the next 8 keys
+// 128 bytes further, the next 8 queries 128 keys * 16 bytes.
+__device__ __forceinline__ uint64_t smem_desc_weights(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(128 >> 4) << 16;
+    d |= (uint64_t)((kKeys * 16) >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    return d;
+}
+
+// Descriptor of the matrix of ones: K-major with 128-byte swizzle, every group of 8 rows the same one.
+__device__ __forceinline__ uint64_t smem_desc_ones(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)1 << 16;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+
+template <int DH, int N, typename T>
+__global__ void __launch_bounds__(kKeyThreads, 1)
+tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const TcParams p) {
+    using Cfg = KeyCfg<DH, N>;
+    using Ops = HalfOps<T>;
+    constexpr int NS = Cfg::kStages;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    uint8_t* const sp = smem_raw + (base - raw);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if ((base - raw) + (uint32_t)Cfg::kUsedBytes > p.smem_bytes) {           // uniform: nothing has been set up yet
+        if (tid == 0) atomicExch(p.w.err_flag, kErrTreeWait);
+        if (tid == 0) reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x].last_cta = -1;
+        return;
+    }
+    const uint32_t bars = base + Cfg::kOffBar;
+    auto ring_full = [&](int s) { return bars + 8u * s; };
+    auto ring_empty = [&](int s) { return bars + 8u * (NS + s); };
+    auto q_full = [&](int s) { return bars + 8u * (2 * NS + s); };
+    auto q_empty = [&](int s) { return bars + 8u * (2 * NS + 2 + s); };
+    auto s_full = [&](int b) { return bars + 8u * (2 * NS + 4 + b); };
+    auto p_full = [&](int b) { return bars + 8u * (2 * NS + 6 + b); };
+    auto o_full = [&](int b) { return bars + 8u * (2 * NS + 8 + b); };       // the product of a tile (by its parity) has completed
+    auto o_empty = [&](int b) { return bars + 8u * (2 * NS + 10 + b); };     // the output of a piece (by its parity) has been read
+    auto out_full = [&](int b) { return bars + 8u * (2 * NS + 12 + b); };    // every product of a piece (by its parity) has completed
+    auto piece_done = [&](int i) { return bars + 8u * (2 * NS + 14 + i); };  // the softmax warps are through with a piece (mod 4)
+    const uint32_t flag_bar = bars + 8u * (2 * NS + 18), joint_bar = flag_bar + 8u;
+    volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc);
+    volatile uint32_t* odd_piece = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 16);    // [4]: piece + 1 with a non-finite draft value
+    volatile uint32_t* flags = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 32);        // [2 tiles][4 warps]
+    float* const refs = reinterpret_cast<float*>(sp + Cfg::kOffRef);
+    long long* part = reinterpret_cast<long long*>(sp + Cfg::kOffMisc + 64);
+    TreeRun* run = reinterpret_cast<TreeRun*>(sp + Cfg::kOffMisc + 64 + 96);
+
+    if (tid == 0) {
+        for (int s = 0; s < NS; ++s) { mbar_init(ring_full(s), 1); mbar_init(ring_empty(s), 1); }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(q_full(s), 2); mbar_init(q_empty(s), 1); mbar_init(s_full(s), 1); mbar_init(p_full(s), 4);
+            mbar_init(o_full(s), 1); mbar_init(o_empty(s), 4); mbar_init(out_full(s), 1);
+        }
+        for (int i = 0; i < 4; ++i) { mbar_init(piece_done(i), 4); odd_piece[i] = 0; }
+        mbar_init(flag_bar, 4);
+        mbar_init(joint_bar, 4);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        prefetch_tmap(&map_k); prefetch_tmap(&map_v);
+    }
+    if (warp == 1) {
+        tmem_alloc(base + Cfg::kOffMisc, 512);
+        tmem_relinquish();
+    }
+    for (int i = tid; i < 256; i += kKeyThreads) reinterpret_cast<uint32_t*>(sp + Cfg::kOffOnes)[i] = Ops::pack(1.0f, 1.0f);
+    fence_async_smem();
+    grid_dependency_wait();                    // lengths, queries and the drafts' keys come from the kernels before
+    tree_find_run(p.w, part, run);
+    if (tid == 0) reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x].last_cta = -1;
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem_s = tmem, tmem_o = tmem + 2u * N, tmem_l = tmem + 4u * N;      // scores of a tile by parity, outputs and sums of a piece by parity
+    const int n_tiles = (int)(run->end - run->begin);
+
+    if (warp == 0 && n_tiles > 0) {
+        tree_load_keys<DH, NS>(p, &map_k, &map_v, run, base, ring_full(0), ring_empty(0));
+    } else if ((warp == 2 || warp == 3) && n_tiles > 0) {
+        tree_load_queries<DH, N, T>(p, run, sp + Cfg::kOffQ, q_full(0), q_empty(0), tid - 64);
+    } else if (warp == 1 && n_tiles > 0) {
+        // ---------------- MMA issuer
+        if (lane == 0) {
+            constexpr uint32_t kIdesc = (1u << 4) | (Ops::kFormat << 7) | (Ops::kFormat << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+            constexpr uint32_t kIdescL = kIdesc | (1u << 16), kIdescO = kIdescL | (1u << 15);   // V^T (15) and P^T (16) run along their rows, not along the keys
+            TreeCursor c = run->at;                    // of the next S
+            uint32_t seq = 0, piece = 0, out_piece = 0;
+            bool ok = true, ends = false;
+            auto issue_s = [&](int t) -> bool {
+                const int slot = seq % NS;
+                if (t == 0 || c.item_begins()) {
+                    if (!mbar_wait(q_full(piece & 1u), (piece >> 1) & 1u)) return false;
+                    ++piece;
+                }
+                const uint32_t b = (piece - 1) & 1u;
+                if (!mbar_wait(ring_full(slot), (seq / NS) & 1u)) return false;
+                tc_fence_after();
+                const uint32_t qa = base + Cfg::kOffQ + b * Cfg::kQBytes, ka = base + slot * Cfg::kTileBytes;
+#pragma unroll
+                for (int k = 0; k < DH / 16; ++k) {
+                    const uint64_t da = smem_desc_sw128(ka + (k >> 2) * (kKeys * 128)) + (uint64_t)(2 * (k & 3));
+                    const uint64_t db = smem_desc_sw128(qa + (k >> 2) * (N * 128)) + (uint64_t)(2 * (k & 3));
+                    umma_bf16(tmem_s + (uint32_t)((t & 1) * N), da, db, kIdesc, k > 0 ? 1u : 0u);
+                }
+                umma_commit(s_full(t & 1));
+                umma_commit(ring_empty(slot));
+                ends = c.item_ends();
+                if (ends || t == n_tiles - 1) umma_commit(q_empty(b));
+                ++seq;
+                c.next(p.w);
+                return true;
+            };
+            bool first = true;                         // the tile opens its piece
+            if (!issue_s(0)) ok = false;
+            for (int t = 0; t < n_tiles && ok; ++t) {
+                const bool last = ends;
+                if (t + 1 < n_tiles && !issue_s(t + 1)) { ok = false; break; }
+                const uint32_t b = out_piece & 1u;
+                if (first && out_piece >= 2 && !mbar_wait(o_empty(b), ((out_piece >> 1) & 1u) ^ 1u)) { ok = false; break; }
+                const int slot = seq % NS;
+                if (!mbar_wait(p_full(t & 1), (t >> 1) & 1u) || !mbar_wait(ring_full(slot), (seq / NS) & 1u)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t va = base + slot * Cfg::kTileBytes, pa = base + Cfg::kOffP + (t & 1) * Cfg::kPBytes;
+#pragma unroll
+                for (int k = 0; k < kKeys / 16; ++k)
+                    // (at d_head 64 the rows behind 64 repeat the tile: their results are not read)
+                    umma_bf16(tmem_o + (uint32_t)(b * N), smem_desc_sw128_mn(va + k * 2048, DH == 128 ? kKeys * 128 : 0), smem_desc_weights(pa + k * 256),
+                              kIdescO, (!first || k > 0) ? 1u : 0u);
+                umma_commit(ring_empty(slot));
+#pragma unroll
+                for (int k = 0; k < kKeys / 16; ++k)
+                    umma_bf16(tmem_l + (uint32_t)(b * N), smem_desc_ones(base + Cfg::kOffOnes), smem_desc_weights(pa + k * 256), kIdescL,
+                              (!first || k > 0) ? 1u : 0u);
+                umma_commit(o_full(t & 1));
+                if (last || t == n_tiles - 1) umma_commit(out_full(b));
+                ++seq;
+                first = last;
+                if (last) ++out_piece;
+            }
+            if (!ok) atomicExch(p.w.err_flag, kErrTreeWait);
+        }
+    } else if (warp >= 4 && warp < 8 && n_tiles > 0) {
+        // ---------------- softmax: thread = key of the tile
+        const int quarter = warp & 3, me = quarter * 32 + lane;
+        const uint32_t t_lane = (uint32_t)(quarter * 32) << 16;
+        float* const red = reinterpret_cast<float*>(sp + Cfg::kOffRed);
+        TreeCursor c = run->at;
+        bool ok = true, opens = true;
+        int q0 = 0, nq = 0;
+        uint32_t piece = 0, checks = 0, joins = 0, cur = 0;      // cur: which copy of the references is in use
+        auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)) != 0; };
+        auto meet = [&]() -> bool {                              // the four warps
+            __syncwarp();
+            if (lane == 0) mbar_arrive(joint_bar);
+            return wait_all(joint_bar, joins++ & 1u);
+        };
+        for (int t = 0; t < n_tiles && ok; ++t) {
+            const int buf = t & 1;
+            if (opens) { q0 = c.first_query(p.w); nq = c.queries(p.w); }
+            const int C = c.r.L - c.r.n;
+            const uint32_t s_at = tmem_s + (uint32_t)(buf * N) + t_lane;
+            uint64_t vis = ~0ull;                                // queries that see this key
+            if ((c.kt + 1) * kKeys > C) {                        // drafts in the tile, or its end
+                const int key = c.kt * kKeys + me, j = key - C;
+                if (key >= C) {
+                    vis = 0;
+                    if (key < c.r.L) {
+                        const int tok0 = q0 / p.w.group, n_tok = (q0 + nq - 1) / p.w.group - tok0 + 1;
+                        for (int i0 = 0; i0 < n_tok; i0 += 8) {  // eight drafts' mask words in flight
+                            uint32_t word[8];
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) {
+                                word[u] = 0;
+                                if (p.tree_mask && i0 + u < n_tok && j < 32 * p.mask_words)
+                                    word[u] = __ldg(p.tree_mask + (size_t)(c.r.row0 + tok0 + i0 + u) * p.mask_words + (j >> 5)) >> (j & 31);
+                            }
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) {
+                                const int tok = tok0 + i0 + u, at = tok * p.w.group - q0;      // the draft's first query, from the tile's start
+                                if (i0 + u >= n_tok || !(p.tree_mask ? word[u] & 1u : j <= tok)) continue;
+                                const int lo = max(at, 0), hi = min(at + p.w.group, N);
+                                vis |= (hi - lo >= 64 ? ~0ull : ((1ull << (hi - lo)) - 1ull)) << lo;
+                            }
+                        }
+                    }
+                }
+                const uint32_t vseq = t == n_tiles - 1 ? 2u * n_tiles - 1u : 2u * t + 2u;
+                if (!wait_all(s_full(buf), (t >> 1) & 1u) || !wait_all(ring_full(vseq % NS), (vseq / NS) & 1u)) { ok = false; break; }
+                if (tree_clean_values<DH, Ops::kExpMask>(sp + (vseq % NS) * Cfg::kTileBytes, max(C - c.kt * kKeys, 0), c.r.L - c.kt * kKeys, me))
+                    odd_piece[piece & 3u] = piece + 1;
+            } else if (!wait_all(s_full(buf), (t >> 1) & 1u)) { ok = false; break; }
+            tc_fence_after();
+            uint32_t w[N / 2];
+            bool move = opens;
+            if (!opens) {
+                // the weights as if no reference moved; whether one does, the warps find out meanwhile
+                uint32_t s[N];
+                float y[N], top = -INFINITY;
+                load_scores<N>(s_at, s);
+                tmem_ld_wait();
+                const float4* ref4 = reinterpret_cast<const float4*>(refs + cur * N);
+#pragma unroll
+                for (int n4 = 0; n4 < N / 4; ++n4) {
+                    const float4 r = ref4[n4];
+                    y[4 * n4] = fmaf(__uint_as_float(s[4 * n4]), p.scale_log2, -r.x);
+                    y[4 * n4 + 1] = fmaf(__uint_as_float(s[4 * n4 + 1]), p.scale_log2, -r.y);
+                    y[4 * n4 + 2] = fmaf(__uint_as_float(s[4 * n4 + 2]), p.scale_log2, -r.z);
+                    y[4 * n4 + 3] = fmaf(__uint_as_float(s[4 * n4 + 3]), p.scale_log2, -r.w);
+                }
+                if (vis != ~0ull) {
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+                        if (!((vis >> n) & 1ull)) y[n] = -INFINITY;
+                }
+#pragma unroll
+                for (int n = 0; n < N; ++n) top = fmaxf(top, y[n]);
+                const bool any = __any_sync(0xffffffffu, top > Ops::kBias + kTreeSlack);
+                if (lane == 0) { flags[buf * 4 + quarter] = any; mbar_arrive(flag_bar); }
+#pragma unroll
+                for (int n = 0; n < N; n += 2) w[n / 2] = Ops::pack(tree_ex2(y[n]), tree_ex2(y[n + 1]));
+                if (!wait_all(flag_bar, checks & 1u)) { ok = false; break; }
+                ++checks;
+                move = (flags[buf * 4] | flags[buf * 4 + 1] | flags[buf * 4 + 2] | flags[buf * 4 + 3]) != 0;
+            }
+            if (move) {
+                // maxima over the keys, new references, outputs and sums brought to them
+                uint32_t s[N];
+                float y[N];
+                load_scores<N>(s_at, s);
+                tmem_ld_wait();
+#pragma unroll
+                for (int n = 0; n < N; ++n) y[n] = (vis >> n) & 1ull ? __uint_as_float(s[n]) * p.scale_log2 : -INFINITY;
+                largest_into<N>(y, red, quarter);
+                if (!meet()) { ok = false; break; }
+                const float* old_ref = refs + cur * N;
+                float* new_ref = refs + (cur ^ 1u) * N;
+                if (me < N) {
+                    const float4 r = *reinterpret_cast<const float4*>(red + me * 4);
+                    const float top = fmaxf(fmaxf(r.x, r.y), fmaxf(r.z, r.w)) - Ops::kBias;
+                    new_ref[me] = me < nq ? fmaxf(top, opens ? kNoRef : old_ref[me]) : INFINITY;     // columns without a query: weight 0
+                }
+                if (!meet()) { ok = false; break; }
+                if (!opens) {
+                    if (!wait_all(o_full(buf ^ 1), ((t - 1) >> 1) & 1u)) { ok = false; break; }         // the products before
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int n0 = 0; n0 < N; n0 += 16) {
+                        uint32_t o[16], l[16];
+                        const uint32_t at = (uint32_t)((piece & 1u) * N + n0) + t_lane;
+                        load_scores<16>(tmem_o + at, o);
+                        load_scores<16>(tmem_l + at, l);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const float f = tree_ex2(old_ref[n0 + e] - new_ref[n0 + e]);
+                            o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            l[e] = __float_as_uint(__uint_as_float(l[e]) * f);
+                        }
+                        store16(tmem_o + at, o);
+                        store16(tmem_l + at, l);
+                    }
+                    tmem_store_wait();
+                }
+#pragma unroll
+                for (int n = 0; n < N; n += 2) w[n / 2] = Ops::pack(tree_ex2(y[n] - new_ref[n]), tree_ex2(y[n + 1] - new_ref[n + 1]));
+                cur ^= 1u;
+            }
+            // P^T into the buffer that the products two tiles ago have read
+            if (t >= 2 && !wait_all(o_full(buf), ((t >> 1) & 1u) ^ 1u)) { ok = false; break; }
+            uint8_t* pt = sp + Cfg::kOffP + buf * Cfg::kPBytes + me * 16;
+#pragma unroll
+            for (int ch = 0; ch < N / 8; ++ch)
+                *reinterpret_cast<uint4*>(pt + ch * (kKeys * 16)) = make_uint4(w[4 * ch], w[4 * ch + 1], w[4 * ch + 2], w[4 * ch + 3]);
+            fence_async_smem();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full(buf));
+            opens = c.item_ends();
+            if (opens || t == n_tiles - 1) {
+                if (me < N) refs[(2 + (piece & 3u)) * N + me] = refs[cur * N + me];        // (a warp behind may still read the copy in use)
+                __syncwarp();
+                if (lane == 0) mbar_arrive(piece_done(piece & 3u));
+                ++piece;
+            }
+            c.next(p.w);
+        }
+        if (!ok && lane == 0) atomicExch(p.w.err_flag, kErrTreeWait);
+    } else if (warp >= 8 && n_tiles > 0) {
+        // ---------------- outputs of a piece: thread = column of d_head
+        const int quarter = warp & 3, me = quarter * 32 + lane;
+        const uint32_t t_lane = (uint32_t)(quarter * 32) << 16;
+        TreeCursor c = run->at;
+        bool split_front = !c.item_begins(), ok = true;
+        uint32_t piece = 0;
+        int kt_first = c.kt;
+        auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)) != 0; };
+        for (int t = 0; t < n_tiles && ok; ++t) {
+            const bool item_ends = c.item_ends();
+            if (item_ends || t == n_tiles - 1) {
+                const int q0 = c.first_query(p.w), nq = c.queries(p.w), C = c.r.L - c.r.n;
+                const bool whole = item_ends && !split_front;
+                if (!wait_all(piece_done(piece & 3u), (piece >> 2) & 1u) || !wait_all(out_full(piece & 1u), (piece >> 1) & 1u)) { ok = false; break; }
+                tc_fence_after();
+                const bool repair = odd_piece[piece & 3u] == piece + 1;
+                float* slot = tree_slot(p.scratch, split_front ? 2 * blockIdx.x : 2 * blockIdx.x + 1, N, DH);
+                const float* ref = refs + (2 + (piece & 3u)) * N;
+                int tok = q0 / p.w.group, hg = q0 - tok * p.w.group;
+                T* dst = static_cast<T*>(p.out) + (int64_t)(c.r.row0 + tok) * p.out_stride + (int64_t)(c.h * p.w.group + hg) * DH + me;
+#pragma unroll 1
+                for (int n0 = 0; n0 < nq; n0 += 16) {
+                    uint32_t o[16], l[16];
+                    const uint32_t at = (uint32_t)((piece & 1u) * N + n0) + t_lane;
+                    load_scores<16>(tmem_o + at, o);
+                    load_scores<16>(tmem_l + at, l);
+                    tmem_ld_wait();
+                    if (repair) {                                // what the non-finite values of drafts add to this column
+                        uint32_t last = 0xFFFFFFFFu;
+                        float odd = 0.0f;
+#pragma unroll 1
+                        for (int e = 0; e < 16 && n0 + e < nq; ++e) {
+                            const uint32_t tk = (uint32_t)((q0 + n0 + e) / p.w.group);
+                            if (tk != last) {
+                                last = tk;
+                                odd = 0.0f;
+                                const uint32_t* mask = p.tree_mask ? p.tree_mask + (size_t)(c.r.row0 + tk) * p.mask_words : nullptr;
+                                for (int j = 0; j < c.r.n && me < DH; ++j) {
+                                    const int key = C + j, kt = key / kKeys;
+                                    if (kt < kt_first || kt > c.kt || !(visible_word(key, C, c.r.n, (int)tk, mask, p.mask_words) & 1u)) continue;
+                                    const int64_t off = tree_value_offset(p, c, key);
+                                    if (off < 0) continue;
+                                    const float v = Ops::value(static_cast<const T*>(p.v)[off + me]);
+                                    if (!isfinite(v)) odd += v;
+                                }
+                            }
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                if (i == e) o[i] = __float_as_uint(__uint_as_float(o[i]) + odd);
+                        }
+                    }
+                    if (whole) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const float sum = __uint_as_float(l[e]), x = __uint_as_float(o[e]) * (1.0f / sum);
+                            if (n0 + e < nq && me < DH) *dst = tree_round<T>(sum == 0.0f ? 0.0f : x);
+                            dst += DH;
+                            if (++hg == p.w.group) { hg = 0; dst += p.out_stride - (int64_t)p.w.group * DH; }
+                        }
+                    } else if (me < DH) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (n0 + e < nq) {
+                                slot[2 * N + (size_t)(n0 + e) * DH + me] = __uint_as_float(o[e]);
+                                if (me == 0) { slot[n0 + e] = ref[n0 + e]; slot[N + n0 + e] = __uint_as_float(l[e]); }
+                            }
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(o_empty(piece & 1u));
+                if (!item_ends && !split_front && me == 0) {     // begins here, goes on in the next CTAs
+                    TreeTail tl{};
+                    tl.last_cta = tree_cta_of(run->end + (c.r.n_kt - 1 - c.kt) - 1, run->total, run->ctas);
+                    tl.queries = nq; tl.row0 = c.r.row0; tl.q0 = q0; tl.h = c.h;
+                    reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x] = tl;
+                }
+                split_front = false;
+                ++piece;
+            }
+            c.next(p.w);
+            kt_first = item_ends ? c.kt : kt_first;
+        }
+        if (!ok && lane == 0) atomicExch(p.w.err_flag, kErrTreeWait);
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+template <int DH, int N, typename T>
+int keys_launch(const TcParams& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int grid, cudaStream_t s, bool dependent) {
+    using Cfg = KeyCfg<DH, N>;
+    static DeviceOnce attr;
+    if (attr.first() && cudaFuncSetAttribute(tree_attention_keys_kernel<DH, N, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes) != cudaSuccess) {
+        attr.retry();
+        return ZOQAT_ERR_CUDA;
+    }
+    TcParams q = p;
+    q.smem_bytes = Cfg::kSmemBytes;
+    return launch_kernel(tree_attention_keys_kernel<DH, N, T>, dim3(grid), dim3(kKeyThreads), Cfg::kSmemBytes, s, dependent, map_k, map_v, q) == cudaSuccess
+               ? ZOQAT_OK : ZOQAT_ERR_CUDA;
+}
+
+}  // namespace
+
+int launch_tree_keys(const TcParams& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int dh, int type, int nq, int grid, cudaStream_t s, bool dependent) {
+#define ZQ_KEYS(DH, T) \
+    return nq == 16 ? keys_launch<DH, 16, T>(p, map_k, map_v, grid, s, dependent) \
+                    : (nq == 32 ? keys_launch<DH, 32, T>(p, map_k, map_v, grid, s, dependent) : keys_launch<DH, 64, T>(p, map_k, map_v, grid, s, dependent))
+    if (type == kTypeBf16) { if (dh == 64) { ZQ_KEYS(64, __nv_bfloat16); } ZQ_KEYS(128, __nv_bfloat16); }
+    if (dh == 64) { ZQ_KEYS(64, __half); }
+    ZQ_KEYS(128, __half);
+#undef ZQ_KEYS
+}
+
+}  // namespace zq

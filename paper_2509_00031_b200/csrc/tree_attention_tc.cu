@@ -3,14 +3,14 @@
 //   out[i, h] = sum_t softmax_t(scale q[i, h] . k[t, h / g]) v[t, h / g]      over the keys t < C cached before the step and
 //                                                                            the drafts j (t = C + j) whose mask bit is set
 //
-// The queries that read one key head - every draft times the g heads of the group - share one 128-row tile, so each cached
-// byte is fetched once per request, key head and 128 queries.  Up to about 100 queries per key head that fetch bounds the
-// kernel (a tile of 128 keys is 64 KB, some 2800 cycles of an SM's share of the memory; its two products are 1024 cycles of
-// the tensor pipe whatever the number of live rows); above, the tensor pipe and the exponentials do.
+// This file: many queries per key head (wide trees, grouped heads); the host sends fewer to tree_attention_keys.cu.  The queries
+// that read one key head - every draft times the g heads of the group - share 128-row tiles, so each cached byte is fetched once per
+// request, key head and 128 queries.  A tile of 128 keys at d_head 128 costs 1024 cycles of the tensor pipe and 1024 of the
+// exponential unit against some 2800 of an SM's share of the memory: the kernel is bound by the products from about three row
+// tiles per key head on, where the copies come from L2.
 //
 // One persistent CTA per SM, 12 warps; the key tiles of all requests are dealt out in equal runs (tree_attention.cuh):
-//   warp 0      TMA: every lane fetches one page (a 64-column half of it) of a K or V tile into a ring of tiles; the lanes
-//               read the block table themselves, one tile ahead.  Q tiles go into two buffers, a piece ahead.
+//   warp 0      K and V tiles by TMA into a ring; warps 2, 3: query tiles into two buffers, a piece ahead
 //   warp 1      one thread issues the products: S = Q K^T into one of two TMEM score buffers, O += P V with P read from TMEM
 //               and V as it lies in the page (keys along k, so no transposition).
 //   warps 4-7, 8-11  two softmax groups take alternate tiles.  A thread owns a query row: it reads the tile's 128 scores, and
@@ -24,15 +24,13 @@
 // not finite is set to zero as well and added again, at the end, to the rows that see the draft - so that 0 * inf of a
 // masked place never reaches a row.
 // Every wait is bounded and reports through *err_flag.
-#include "tree_attention.cuh"
-#include "tc_ptx.cuh"
+#include "tree_attention_tc.cuh"
 #include "../../include/zoqat.h"
 
 namespace zq {
 namespace {
 
-constexpr int kTcThreads = 384, kKeys = 128, kRows = 128;
-constexpr float kRefSlack = 8.0f;
+constexpr int kTcThreads = 384, kRows = 128;
 
 template <int DH> struct TcCfg {
     static constexpr int kTileBytes = kKeys * DH * 2;                       // one K, V or Q tile
@@ -46,80 +44,12 @@ template <int DH> struct TcCfg {
     static_assert(kUsedBytes <= 232448, "shared memory");
 };
 
-struct TcParams {
-    TreeWork w;
-    int q_unit, q_tokens;        // rows and drafts of one Q box
-    int box_keys;                // keys of one K / V box: a page, or 128 of a larger one
-    int n_pages, mask_words;
-    const uint32_t* tree_mask;
-    float scale_log2;
-    void* out;
-    int64_t out_stride;
-    uint8_t* scratch;
-    const void* v;               // (for the rare repair of non-finite values)
-    int64_t page_stride, slot_stride, head_stride;
-    uint32_t smem_bytes;
-};
-
-template <typename T> struct HalfOps;
-template <> struct HalfOps<__nv_bfloat16> {
-    static constexpr uint32_t kFormat = 1;                       // operand format of the instruction descriptor
-    static constexpr float kBias = 0.0f;                         // weights are scaled by 2^kBias
-    static constexpr uint32_t kExpMask = 0x7F80u;
-    static __device__ __forceinline__ uint32_t pack(float lo, float hi) { const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi); return *reinterpret_cast<const uint32_t*>(&h); }
-    static __device__ __forceinline__ float value(__nv_bfloat16 x) { return __bfloat162float(x); }
-};
-template <> struct HalfOps<__half> {
-    static constexpr uint32_t kFormat = 0;
-    static constexpr float kBias = 7.0f;
-    static constexpr uint32_t kExpMask = 0x7C00u;
-    static __device__ __forceinline__ uint32_t pack(float lo, float hi) { const __half2 h = __floats2half2_rn(lo, hi); return *reinterpret_cast<const uint32_t*>(&h); }
-    static __device__ __forceinline__ float value(__half x) { return __half2float(x); }
-};
-
-__device__ __forceinline__ void tmem_store32(uint32_t taddr, const uint32_t (&v)[32]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-        ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
-          "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
-          "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
-          "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
-        : "memory");
-}
-__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void mbar_arrive_n(uint32_t bar, uint32_t n) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
-}
-
-// Bits of the 32 keys from k0 on that draft i sees.
-__device__ __forceinline__ uint32_t visible_word(int k0, int C, int n, int i, const uint32_t* mask, int words) {
-    const int rel = k0 - C;                                      // draft index of bit 0
-    if (rel <= -32) return 0xFFFFFFFFu;
-    const int shift = rel < 0 ? -rel : 0, j0 = rel < 0 ? 0 : rel;
-    const uint32_t below = (1u << shift) - 1u;                   // cached keys (shift < 32)
-    if (j0 >= n) return below;
-    uint32_t d;
-    if (mask) {
-        const int wi = j0 >> 5;
-        const uint32_t lo = wi < words ? __ldg(mask + wi) : 0u, hi = wi + 1 < words ? __ldg(mask + wi + 1) : 0u;
-        d = __funnelshift_r(lo, hi, j0 & 31);
-    } else {
-        const int upto = i - j0 + 1;
-        d = upto <= 0 ? 0u : (upto >= 32 ? 0xFFFFFFFFu : (1u << upto) - 1u);
-    }
-    if (n - j0 < 32) d &= (1u << (n - j0)) - 1u;
-    return below | (d << shift);
-}
-
 template <int DH, typename T>
 __global__ void __launch_bounds__(kTcThreads, 1)
-tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                         const __grid_constant__ CUtensorMap map_v, const TcParams p) {
+tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const TcParams p) {
     using Cfg = TcCfg<DH>;
     using Ops = HalfOps<T>;
-    constexpr int HALVES = DH / 64, NS = Cfg::kStages;
+    constexpr int NS = Cfg::kStages;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
@@ -148,13 +78,13 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     if (tid == 0) {
         for (int s = 0; s < NS; ++s) { mbar_init(ring_full(s), 1); mbar_init(ring_empty(s), 1); }
         for (int s = 0; s < 2; ++s) {
-            mbar_init(q_full(s), 1); mbar_init(q_empty(s), 1); mbar_init(s_full(s), 1); mbar_init(p_full(s), 4);
+            mbar_init(q_full(s), 2); mbar_init(q_empty(s), 1); mbar_init(s_full(s), 1); mbar_init(p_full(s), 4);
             mbar_init(o_full(s), 1); mbar_init(o_empty(s), 8);
             odd_piece[s] = 0;
         }
         mbar_init(x_full, 8);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        prefetch_tmap(&map_q); prefetch_tmap(&map_k); prefetch_tmap(&map_v);
+        prefetch_tmap(&map_k); prefetch_tmap(&map_v);
     }
     if (warp == 1) {
         tmem_alloc(base + Cfg::kOffMisc, 512);
@@ -171,63 +101,9 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
     const int n_tiles = (int)(run->end - run->begin);
 
     if (warp == 0 && n_tiles > 0) {
-        // ---------------- TMA producer: K(0), K(1), V(0), K(2), V(1), ..., the order in which the products consume them
-        const int half = lane % HALVES, box = lane / HALVES;
-        const int n_box = kKeys / p.box_keys;
-        TreeCursor c = run->at;
-        uint32_t seq = 0, piece = 0;
-        bool ok = true;
-        int page = 0, off = 0, prev_page = 0, prev_off = 0, prev_h = 0, prev_live = 0;
-        bool prev_mine = false;
-        auto look_up = [&](int& pg, int& of) -> bool {           // page and slot of this lane's box of the cursor's tile
-            const int key0 = c.kt * kKeys + box * p.box_keys;
-            if (box >= n_box || key0 >= c.r.L) return false;
-            const int idx = key0 / p.w.page_size;
-            of = key0 - idx * p.w.page_size;
-            pg = __ldg(p.w.block_table + (size_t)c.b * p.w.max_pages + idx);
-            if (pg < 0 || pg >= p.n_pages) { atomicExch(p.w.err_flag, kErrBadPage); pg = p.n_pages; }   // behind the map's end: zeros
-            return true;
-        };
-        auto fetch = [&](const CUtensorMap* map, int h, int live, bool mine, int pg, int of) {
-            const int slot = seq % NS;
-            if (!__all_sync(0xffffffffu, mbar_wait(ring_empty(slot), ((seq / NS) & 1u) ^ 1u))) return false;
-            if (lane == 0) mbar_arrive_expect_tx(ring_full(slot), (uint32_t)(live * HALVES * p.box_keys * 128));
-            __syncwarp();
-            if (mine) tma_load_4d(base + Cfg::kOffRing + slot * Cfg::kTileBytes + half * (kKeys * 128) + box * p.box_keys * 128, map,
-                                  ring_full(slot), half * 64, of, h, pg);
-            ++seq;
-            return true;
-        };
-        bool mine = look_up(page, off);
-        for (int t = 0; t <= n_tiles && ok; ++t) {
-            int live = 0;
-            if (t < n_tiles) {
-                if (t == 0 || c.item_begins()) {                 // a piece begins: its queries
-                    const int b = piece & 1u;
-                    const int boxes = (c.queries(p.w) + p.q_unit - 1) / p.q_unit;
-                    if (!__all_sync(0xffffffffu, mbar_wait(q_empty(b), ((piece >> 1) & 1u) ^ 1u))) { ok = false; break; }
-                    if (lane == 0) mbar_arrive_expect_tx(q_full(b), (uint32_t)(boxes * HALVES * p.q_unit * 128));
-                    __syncwarp();
-                    if (box < boxes)
-                        tma_load_3d(base + b * Cfg::kTileBytes + half * (kRows * 128) + box * p.q_unit * 128, &map_q, q_full(b), half * 64,
-                                    c.h * p.w.group, c.r.row0 + c.first_query(p.w) / p.w.group + box * p.q_tokens);
-                    ++piece;
-                }
-                live = min(n_box, (c.r.L - c.kt * kKeys + p.box_keys - 1) / p.box_keys);
-                if (!fetch(&map_k, c.h, live, mine, page, off)) { ok = false; break; }
-            }
-            int next_page = 0, next_off = 0;
-            bool next_mine = false;
-            const int h = c.h;
-            if (t + 1 < n_tiles) { c.next(p.w); next_mine = look_up(next_page, next_off); }   // the next tile's pages, before the wait below
-            if (t > 0 && !fetch(&map_v, prev_h, prev_live, prev_mine, prev_page, prev_off)) { ok = false; break; }
-            prev_page = page; prev_off = off; prev_h = h; prev_live = live; prev_mine = mine;
-            page = next_page; off = next_off; mine = next_mine;
-        }
-        if (!ok && lane == 0) atomicExch(p.w.err_flag, kErrTreeWait);
-        // every load issued above has to land before the CTA may leave: each slot's last tile has been consumed
-        for (uint32_t k = seq > NS ? seq - NS : 0; k < seq; ++k)
-            if (!mbar_wait(ring_full(k % NS), (k / NS) & 1u)) break;
+        tree_load_keys<DH, NS>(p, &map_k, &map_v, run, base + Cfg::kOffRing, ring_full(0), ring_empty(0));
+    } else if ((warp == 2 || warp == 3) && n_tiles > 0) {
+        tree_load_queries<DH, kRows, T>(p, run, sp, q_full(0), q_empty(0), tid - 64);
     } else if (warp == 1 && n_tiles > 0) {
         // ---------------- MMA issuer
         if (lane == 0) {
@@ -319,57 +195,39 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                 tc_fence_after();
                 const bool tail = (c.kt + 1) * kKeys > C;
                 if (tail) {
-                    // the V tile's rows behind the end become zeros; a draft's non-finite element becomes zero and is marked
                     const uint32_t vseq = t == n_tiles - 1 ? 2u * n_tiles - 1u : 2u * t + 2u;
                     if (!wait_all(ring_full(vseq % NS), (vseq / NS) & 1u)) { ok = false; break; }
-                    uint8_t* v = sp + Cfg::kOffRing + (vseq % NS) * Cfg::kTileBytes;
-                    const int k_lo = max(C - c.kt * kKeys, 0), k_end = c.r.L - c.kt * kKeys;   // first draft, first key behind the end
-                    for (int x = tid & 127; x < (kKeys - k_lo) * (DH / 8); x += 128) {
-                        const int key = k_lo + x / (DH / 8), ch = x % (DH / 8);
-                        uint4* at = reinterpret_cast<uint4*>(v + (ch >> 3) * (kKeys * 128) + key * 128 + (((ch & 7) ^ (key & 7)) << 4));
-                        if (key >= k_end) { *at = make_uint4(0, 0, 0, 0); continue; }
-                        uint4 w = *at;
-                        uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-                        bool odd = false;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            if ((ww[e] & Ops::kExpMask) == Ops::kExpMask) { ww[e] &= 0xFFFF0000u; odd = true; }
-                            if (((ww[e] >> 16) & Ops::kExpMask) == Ops::kExpMask) { ww[e] &= 0x0000FFFFu; odd = true; }
-                        }
-                        if (odd) { *at = make_uint4(ww[0], ww[1], ww[2], ww[3]); odd_piece[piece & 1u] = piece + 1; }
-                    }
-                    fence_async_smem();
+                    if (tree_clean_values<DH, Ops::kExpMask>(sp + Cfg::kOffRing + (vseq % NS) * Cfg::kTileBytes, max(C - c.kt * kKeys, 0),
+                                                             c.r.L - c.kt * kKeys, tid & 127))
+                        odd_piece[piece & 1u] = piece + 1;
                 }
                 if (warp_live) {
-                    uint32_t s[4][32];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) tmem_ld32(ts + 32u * q, s[q]);
+                    uint32_t s0[32], s1[32], s2[32], s3[32];     // (one array each: together they would leave the registers)
+                    tmem_ld32(ts, s0); tmem_ld32(ts + 32u, s1); tmem_ld32(ts + 64u, s2); tmem_ld32(ts + 96u, s3);
                     tmem_ld_wait();
                     if (tail) {
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
+                        auto hide = [&](uint32_t (&s)[32], int q) {
                             const uint32_t vis = row < nq ? visible_word(c.kt * kKeys + 32 * q, C, c.r.n, tok, mask, p.mask_words) : 0u;
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
-                                if (!((vis >> e) & 1u)) s[q][e] = __float_as_uint(-INFINITY);
-                        }
+                                if (!((vis >> e) & 1u)) s[e] = __float_as_uint(-INFINITY);
+                        };
+                        hide(s0, 0); hide(s1, 1); hide(s2, 2); hide(s3, 3);
                     }
-                    float mx;
-                    {
-                        float t8[8];
+                    float t8[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) t8[e] = __uint_as_float(s[0][e]);
+                    for (int e = 0; e < 8; ++e) t8[e] = -INFINITY;
+                    auto largest = [&](const uint32_t (&s)[32]) {
 #pragma unroll
-                        for (int q = 0; q < 4; ++q)
-#pragma unroll
-                            for (int e = q == 0 ? 8 : 0; e < 32; ++e) t8[e & 7] = fmaxf(t8[e & 7], __uint_as_float(s[q][e]));
-                        mx = fmaxf(fmaxf(fmaxf(t8[0], t8[1]), fmaxf(t8[2], t8[3])), fmaxf(fmaxf(t8[4], t8[5]), fmaxf(t8[6], t8[7])));
-                    }
+                        for (int e = 0; e < 32; ++e) t8[e & 7] = fmaxf(t8[e & 7], __uint_as_float(s[e]));
+                    };
+                    largest(s0); largest(s1); largest(s2); largest(s3);
+                    float mx = fmaxf(fmaxf(fmaxf(t8[0], t8[1]), fmaxf(t8[2], t8[3])), fmaxf(fmaxf(t8[4], t8[5]), fmaxf(t8[6], t8[7])));
                     mx = mx * p.scale_log2 - Ops::kBias;         // weights 2^(score - reference): the largest is 2^kBias .. 2^(kBias + 8)
                     if (t - first < 2) {
                         m_ref = mx;                              // the group's first tile of the piece
                     } else {
-                        const bool grow = row < nq && mx > m_ref + kRefSlack;
+                        const bool grow = row < nq && mx > m_ref + kTreeSlack;
                         if (__any_sync(0xffffffffu, grow)) {
                             // rare: rescale the rows' outputs, after the group's previous product has completed
                             if (!wait_all(o_full(g), ((t >> 1) & 1u) ^ 1u)) { ok = false; break; }
@@ -392,19 +250,20 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                     }
                     const float ref = m_ref == -INFINITY ? 0.0f : m_ref;     // nothing seen yet: every weight is 0
                     float sum4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int hf = 0; hf < 2; ++hf) {
+                    auto weigh = [&](const uint32_t (&sa)[32], const uint32_t (&sb)[32], uint32_t at) {
                         uint32_t w[32];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const float a = tree_ex2(fmaf(__uint_as_float(s[2 * hf + (e >> 4)][2 * (e & 15)]), p.scale_log2, -ref));
-                            const float b = tree_ex2(fmaf(__uint_as_float(s[2 * hf + (e >> 4)][2 * (e & 15) + 1]), p.scale_log2, -ref));
-                            sum4[(2 * e) & 3] += a;
-                            sum4[(2 * e + 1) & 3] += b;
+                        for (int e = 0; e < 16; ++e) {
+                            const float a = tree_ex2(fmaf(__uint_as_float(sa[2 * e]), p.scale_log2, -ref)), b = tree_ex2(fmaf(__uint_as_float(sa[2 * e + 1]), p.scale_log2, -ref));
+                            const float c2 = tree_ex2(fmaf(__uint_as_float(sb[2 * e]), p.scale_log2, -ref)), d = tree_ex2(fmaf(__uint_as_float(sb[2 * e + 1]), p.scale_log2, -ref));
+                            sum4[0] += a; sum4[1] += b; sum4[2] += c2; sum4[3] += d;
                             w[e] = Ops::pack(a, b);
+                            w[16 + e] = Ops::pack(c2, d);
                         }
-                        tmem_store32(ts + 32u * hf, w);
-                    }
+                        tmem_store32(at, w);
+                    };
+                    weigh(s0, s1, ts);
+                    weigh(s2, s3, ts + 32u);
                     tmem_store_wait();
                     l_run += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
                 }
@@ -464,16 +323,12 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid
                                 if (repair) {                    // non-finite values of drafts this row sees, within the piece's tiles
                                     for (int j = 0; j < c.r.n; ++j) {
                                         const int key = C + j, kt = key / kKeys;
-                                        if (kt < kt_first || kt > c.kt) continue;
-                                        if (!(visible_word(key, C, c.r.n, tok, mask, p.mask_words) & 1u)) continue;
-                                        const int idx = key / p.w.page_size;
-                                        const int pg = __ldg(p.w.block_table + (size_t)c.b * p.w.max_pages + idx);
-                                        if (pg < 0 || pg >= p.n_pages) continue;
-                                        const T* v = static_cast<const T*>(p.v) + pg * p.page_stride + (key - idx * p.w.page_size) * p.slot_stride +
-                                                     c.h * p.head_stride + c0;
+                                        if (kt < kt_first || kt > c.kt || !(visible_word(key, C, c.r.n, tok, mask, p.mask_words) & 1u)) continue;
+                                        const int64_t off = tree_value_offset(p, c, key);
+                                        if (off < 0) continue;
 #pragma unroll
                                         for (int e = 0; e < 32; ++e) {
-                                            const float x = Ops::value(v[e]);
+                                            const float x = Ops::value(static_cast<const T*>(p.v)[off + c0 + e]);
                                             if (!isfinite(x)) o[e] += x;
                                         }
                                     }
@@ -552,55 +407,62 @@ bool encode(CUtensorMap* map, int type, const void* base, int rank, const cuuint
 }
 
 template <int DH, typename T>
-int tc_launch(const TreeAttnArgs& a, cudaStream_t s, bool dependent) {
-    using Cfg = TcCfg<DH>;
-    TcParams p{};
-    const int group = a.n_heads / a.cache.n_kv_heads;
-    int gcd8 = group % 8 == 0 ? 8 : (group % 4 == 0 ? 4 : (group % 2 == 0 ? 2 : 1));
-    p.q_tokens = 8 / gcd8;
-    p.q_unit = group * p.q_tokens;                     // a multiple of 8: the boxes of a Q tile keep the swizzle's rows aligned
-    if (p.q_unit > kRows) return ZOQAT_ERR_UNSUPPORTED;
-    p.w = TreeWork{a.kv_len, a.row_start, a.block_table, a.batch, a.rows, a.n_heads, a.cache.n_kv_heads, a.max_pages, a.cache.page_size,
-                   group, kRows / p.q_unit * p.q_unit, kKeys, a.err_flag};
-    p.box_keys = a.cache.page_size < kKeys ? a.cache.page_size : kKeys;
-    p.n_pages = a.cache.n_pages; p.mask_words = a.mask_words; p.tree_mask = a.tree_mask;
-    p.scale_log2 = (float)(1.4426950408889634 * (double)a.scale);
-    p.out = a.out; p.out_stride = a.out_stride; p.scratch = a.scratch;
-    p.v = a.cache.v; p.page_stride = a.cache.page_stride; p.slot_stride = a.cache.slot_stride; p.head_stride = a.cache.head_stride;
-    p.smem_bytes = Cfg::kSmemBytes;
-    alignas(64) CUtensorMap map_q, map_k, map_v;
-    const cuuint64_t qd[3] = {(cuuint64_t)DH, (cuuint64_t)a.n_heads, (cuuint64_t)a.rows};
-    const cuuint64_t qst[2] = {(cuuint64_t)DH * 2, (cuuint64_t)a.q_stride * 2};
-    const cuuint32_t qb[3] = {64, (cuuint32_t)group, (cuuint32_t)p.q_tokens};
-    const cuuint64_t kd[4] = {(cuuint64_t)DH, (cuuint64_t)a.cache.page_size, (cuuint64_t)a.cache.n_kv_heads, (cuuint64_t)a.cache.n_pages};
-    const cuuint64_t kst[3] = {(cuuint64_t)a.cache.slot_stride * 2, (cuuint64_t)a.cache.head_stride * 2, (cuuint64_t)a.cache.page_stride * 2};
-    const cuuint32_t kb[4] = {64, (cuuint32_t)p.box_keys, 1, 1};
-    if (!encode(&map_q, a.cache.type, a.q, 3, qd, qst, qb) || !encode(&map_k, a.cache.type, a.cache.k, 4, kd, kst, kb) ||
-        !encode(&map_v, a.cache.type, a.cache.v, 4, kd, kst, kb))
-        return ZOQAT_ERR_CUDA;
+int tc_launch(const TcParams& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int grid, cudaStream_t s, bool dependent) {
     static DeviceOnce attr;
     if (attr.first() &&
-        cudaFuncSetAttribute(tree_attention_tc_kernel<DH, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes) != cudaSuccess) {
+        cudaFuncSetAttribute(tree_attention_tc_kernel<DH, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcCfg<DH>::kSmemBytes) != cudaSuccess) {
         attr.retry();
         return ZOQAT_ERR_CUDA;
     }
-    const int grid = tree_grid();
-    if (launch_kernel(tree_attention_tc_kernel<DH, T>, dim3(grid), dim3(kTcThreads), Cfg::kSmemBytes, s, dependent, map_q, map_k, map_v, p) != cudaSuccess)
-        return ZOQAT_ERR_CUDA;
-    count_launch();
-    if (launch_kernel(tree_combine_kernel<T, DH>, dim3(grid, 16), dim3(256), 0, s, true, p.scratch, p.w.tile_rows, group, a.n_heads,
-                      static_cast<T*>(a.out), a.out_stride) != cudaSuccess)
-        return ZOQAT_ERR_CUDA;
-    count_launch();
-    return ZOQAT_OK;
+    TcParams q = p;
+    q.smem_bytes = TcCfg<DH>::kSmemBytes;
+    return launch_kernel(tree_attention_tc_kernel<DH, T>, dim3(grid), dim3(kTcThreads), TcCfg<DH>::kSmemBytes, s, dependent, map_k, map_v, q) == cudaSuccess
+               ? ZOQAT_OK : ZOQAT_ERR_CUDA;
+}
+
+template <int DH, typename T>
+int combine_launch(const TcParams& p, int grid, cudaStream_t s) {
+    const int y = p.w.tile_rows < 16 ? p.w.tile_rows : 16;
+    return launch_kernel(tree_combine_kernel<T, DH>, dim3(grid, y), dim3(256), 0, s, true, p.scratch, p.w.tile_rows, p.w.group, p.w.n_heads,
+                         static_cast<T*>(p.out), p.out_stride) == cudaSuccess ? ZOQAT_OK : ZOQAT_ERR_CUDA;
 }
 
 }  // namespace
 
 int launch_tree_attention_tc(const TreeAttnArgs& a, cudaStream_t s, bool dependent) {
-    if (a.cache.type == kTypeBf16)
-        return a.cache.d_head == 64 ? tc_launch<64, __nv_bfloat16>(a, s, dependent) : tc_launch<128, __nv_bfloat16>(a, s, dependent);
-    return a.cache.d_head == 64 ? tc_launch<64, __half>(a, s, dependent) : tc_launch<128, __half>(a, s, dependent);
+    const int dh = a.cache.d_head, type = a.cache.type;
+    TcParams p{};
+    const int group = a.n_heads / a.cache.n_kv_heads;
+    // Queries per tile, from the average number of drafts (the host does not know the lengths).  Up to 64 queries the keys are
+    // the rows of the products, which costs exponentials only for queries that exist; a tile that is too small reads the keys
+    // again for the next one (from L2), a tile that is too large costs exponentials of empty columns.
+    const long long drafts = (long long)a.rows * group;
+    const long long want = a.rows <= a.batch ? group : (3 * drafts + 2 * a.batch - 1) / (2 * a.batch);     // 1.5 x the average
+    const int nq = want <= 16 ? 16 : (want <= 32 ? 32 : (want <= 64 ? 64 : kRows));
+    p.w = TreeWork{a.kv_len, a.row_start, a.block_table, a.batch, a.rows, a.n_heads, a.cache.n_kv_heads, a.max_pages, a.cache.page_size,
+                   group, nq, kKeys, a.err_flag};
+    p.q = a.q; p.q_stride = a.q_stride;
+    p.box_keys = a.cache.page_size < kKeys ? a.cache.page_size : kKeys;
+    p.n_pages = a.cache.n_pages; p.mask_words = a.mask_words; p.tree_mask = a.tree_mask;
+    p.scale_log2 = (float)(1.4426950408889634 * (double)a.scale);
+    p.out = a.out; p.out_stride = a.out_stride; p.scratch = a.scratch;
+    p.v = a.cache.v; p.page_stride = a.cache.page_stride; p.slot_stride = a.cache.slot_stride; p.head_stride = a.cache.head_stride;
+    alignas(64) CUtensorMap map_k, map_v;
+    const cuuint64_t kd[4] = {(cuuint64_t)dh, (cuuint64_t)a.cache.page_size, (cuuint64_t)a.cache.n_kv_heads, (cuuint64_t)a.cache.n_pages};
+    const cuuint64_t kst[3] = {(cuuint64_t)a.cache.slot_stride * 2, (cuuint64_t)a.cache.head_stride * 2, (cuuint64_t)a.cache.page_stride * 2};
+    const cuuint32_t kb[4] = {64, (cuuint32_t)p.box_keys, 1, 1};
+    if (!encode(&map_k, type, a.cache.k, 4, kd, kst, kb) || !encode(&map_v, type, a.cache.v, 4, kd, kst, kb)) return ZOQAT_ERR_CUDA;
+    const int grid = tree_grid();
+    int rc;
+    if (nq < kRows) rc = launch_tree_keys(p, map_k, map_v, dh, type, nq, grid, s, dependent);
+    else if (type == kTypeBf16) rc = dh == 64 ? tc_launch<64, __nv_bfloat16>(p, map_k, map_v, grid, s, dependent) : tc_launch<128, __nv_bfloat16>(p, map_k, map_v, grid, s, dependent);
+    else rc = dh == 64 ? tc_launch<64, __half>(p, map_k, map_v, grid, s, dependent) : tc_launch<128, __half>(p, map_k, map_v, grid, s, dependent);
+    if (rc != ZOQAT_OK) return rc;
+    count_launch();
+    if (type == kTypeBf16) rc = dh == 64 ? combine_launch<64, __nv_bfloat16>(p, grid, s) : combine_launch<128, __nv_bfloat16>(p, grid, s);
+    else rc = dh == 64 ? combine_launch<64, __half>(p, grid, s) : combine_launch<128, __half>(p, grid, s);
+    if (rc == ZOQAT_OK) count_launch();
+    return rc;
 }
 
 }  // namespace zq

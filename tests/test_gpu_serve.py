@@ -314,6 +314,12 @@ ATTENTION = [
     ("f32", 1, 1, 128, 64, "head", [9000], [3], "tree"),
     ("f16", 4, 4, 64, 64, "token", [3] * 300, [1] * 300, None),             # many short requests
     ("bf16", 20, 1, 128, 16, "token", [130, 1], [9, 2], "tree"),            # 20 query heads per key head
+    ("f16", 20, 1, 128, 16, "token", [130, 1, 40, 700], [1, 1, 1, 1], "tree"),
+    ("bf16", 8, 2, 128, 16, "token", [700, 33], [8, 9], "tree"),
+    ("f16", 8, 2, 64, 128, "head", [1290, 0], [8, 9], "random"),
+    ("bf16", 14, 2, 64, 32, "joint", [300, 129, 0, 4], [1, 2, 5, 1], "tree"),   # tiles that cut a draft's heads apart
+    ("f16", 7, 1, 128, 16, "token", [300, 129, 0, 4], [3, 2, 5, 30], "random"),
+    ("bf16", 2, 2, 128, 16, "token", [4000] * 9, [1] * 9, None),
 ]
 
 
