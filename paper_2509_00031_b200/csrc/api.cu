@@ -1914,6 +1914,8 @@ int zoqat_op_tree_attention(const void* q_dev, int64_t q_stride, const zoqat_pag
     const bool tc = c.type != ZOQAT_TYPE_F32;
     if (tc && c.page_size % 128 && c.page_size != 8 && c.page_size != 16 && c.page_size != 32 && c.page_size != 64)
         return fail(ZOQAT_ERR_UNSUPPORTED, "page_size %d (bf16 / fp16: 8, 16, 32, 64 or a multiple of 128)", c.page_size);
+    if (tc && c.n_kv_heads > 1 && c.n_pages > 1 && c.page_stride % c.head_stride)
+        return fail(ZOQAT_ERR_UNSUPPORTED, "bf16 / fp16: page_stride must be a multiple of head_stride");
     if (rows == 0) return ZOQAT_OK;
     a.q = q_dev; a.q_stride = q_stride; a.block_table = block_table_dev; a.max_pages = max_pages; a.kv_len = kv_len_dev; a.row_start = row_start_dev;
     a.tree_mask = tree_mask_dev; a.mask_words = mask_words; a.batch = batch; a.rows = rows; a.n_heads = n_heads; a.scale = scale;

@@ -49,15 +49,26 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
     return true;
 }
 
+// The same for a thread on the critical path of a short chain (scores -> weights -> product): re-polls without the long
+// suspension, whose wake-up costs more than the chain's steps.
+__device__ __forceinline__ bool mbar_poll(uint32_t bar, uint32_t parity) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, parity)) {
+        if (clock64() - t0 > kWaitCycles) return false;
+    }
+    return true;
+}
+
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
         ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3, int c4) {
     asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-        ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+        ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4) : "memory");
 }
 // L2 eviction priorities for TMA traffic: an operand block that later waves re-read is loaded evict_last, what streams
 // through once (the other operand, results) evict_first, so that the stream does not push the block out of L2.
@@ -213,23 +224,23 @@ __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.
 // Shared-memory matrix descriptor: K-major operand tile whose rows are 128 bytes
 // (64 bf16) written by TMA with the 128-byte swizzle; 8-row groups are 1024 bytes
 // apart (stride byte offset); the leading byte offset is unused for this layout.
-__device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t saddr) {
+__device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t saddr, uint32_t group_bytes = 1024) {
     uint64_t d = 0;
     d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);        // bits  0-13 start address / 16
     d |= (uint64_t)1 << 16;                          // bits 16-29 leading byte offset / 16 (ignored)
-    d |= (uint64_t)(1024 >> 4) << 32;                // bits 32-45 stride byte offset / 16
+    d |= (uint64_t)(group_bytes >> 4) << 32;         // bits 32-45 stride byte offset / 16 (from one 8-row group to the next)
     d |= (uint64_t)1 << 46;                          // bits 46-47 descriptor version (sm_100)
     d |= (uint64_t)2 << 61;                          // bits 61-63 layout: 128-byte swizzle
     return d;
 }
 
-// The same for an operand whose rows (128 bytes, 64 elements) run along k: MN-major, 8 k-rows per 1024-byte group (stride
-// byte offset), the next 64 elements of the other dimension `block_bytes` further (leading byte offset).
-__device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t saddr, uint32_t block_bytes) {
+// The same for an operand whose rows (128 bytes, 64 elements) run along k: MN-major, groups of 8 k-rows `group_bytes` apart
+// (stride byte offset), the next 64 elements of the other dimension `block_bytes` further (leading byte offset).
+__device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t saddr, uint32_t block_bytes, uint32_t group_bytes) {
     uint64_t d = 0;
     d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
     d |= (uint64_t)(block_bytes >> 4) << 16;
-    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)(group_bytes >> 4) << 32;
     d |= (uint64_t)1 << 46;
     d |= (uint64_t)2 << 61;
     return d;

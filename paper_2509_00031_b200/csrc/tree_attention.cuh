@@ -66,7 +66,23 @@ struct TreeCursor {
     }
 };
 
+// a / b for a >= 0, b > 0; almost always in 32 bits, which is several times faster
+__device__ __forceinline__ long long tree_div(long long a, long long b) {
+    return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+}
+
 struct TreeRun { long long begin, end, total; int ctas; TreeCursor at; };   // ctas: CTAs that have a run
+
+// Run c of `total` tiles in `ctas` runs begins here: the first total % ctas runs have one tile more than the others.
+__device__ __forceinline__ long long tree_run_begin(long long total, int ctas, int c) {
+    const long long q = tree_div(total, ctas), r = total - q * ctas;
+    return q * c + (c < r ? c : r);
+}
+// The CTA whose run holds tile `x`.
+__device__ __forceinline__ int tree_cta_of(long long x, long long total, int ctas) {
+    const long long q = tree_div(total, ctas), r = total - q * ctas, wide = r * (q + 1);
+    return (int)(x < wide ? tree_div(x, q + 1) : r + tree_div(x - wide, q));
+}
 
 // The run of this CTA; called by all threads of the block (part: one word per warp, out: shared).  Ends with a barrier.
 __device__ __forceinline__ void tree_find_run(const TreeWork& w, long long* part, TreeRun* out) {
@@ -88,10 +104,10 @@ __device__ __forceinline__ void tree_find_run(const TreeWork& w, long long* part
         if (k == warp) upto += total;
         total += part[k];
     }
-    // run c is [c * total / G, (c + 1) * total / G), G = the CTAs or, where there are fewer tiles, the tiles: no run is empty
+    // the runs are those of the CTAs or, where there are fewer tiles, of as many CTAs as there are tiles: none is empty
     const int ctas = total < (long long)gridDim.x ? (int)total : (int)gridDim.x;
     const bool idle = (int)blockIdx.x >= ctas;
-    const long long begin = idle ? 0 : total * blockIdx.x / ctas, end = idle ? 0 : total * (blockIdx.x + 1) / ctas;
+    const long long begin = idle ? 0 : tree_run_begin(total, ctas, blockIdx.x), end = idle ? 0 : tree_run_begin(total, ctas, blockIdx.x + 1);
     if (tid == 0) { out->begin = begin; out->end = end; out->total = total; out->ctas = ctas; }
     if (begin < end && begin >= upto - mine && begin < upto) {       // exactly one thread
         long long rest = begin - (upto - mine);
@@ -102,10 +118,10 @@ __device__ __forceinline__ void tree_find_run(const TreeWork& w, long long* part
             if (rest < t) break;
             rest -= t;
         }
-        c.kt = (int)(rest % c.r.n_kt);
-        rest /= c.r.n_kt;
-        c.rt = (int)(rest % c.r.n_rt);
-        c.h = (int)(rest / c.r.n_rt);
+        const long long item = tree_div(rest, c.r.n_kt), head = tree_div(item, c.r.n_rt);
+        c.kt = (int)(rest - item * c.r.n_kt);
+        c.rt = (int)(item - head * c.r.n_rt);
+        c.h = (int)head;
         out->at = c;
     }
     __syncthreads();
@@ -121,13 +137,6 @@ __host__ __device__ inline size_t tree_slot_floats(int tile_rows, int dh) { retu
 
 __device__ __forceinline__ float* tree_slot(uint8_t* scratch, int index, int tile_rows, int dh) {
     return reinterpret_cast<float*>(scratch + kTailBytes) + (size_t)index * tree_slot_floats(tile_rows, dh);
-}
-
-// The CTA whose run holds tile `x` (run c begins at floor(c * total / ctas)).
-__device__ __forceinline__ int tree_cta_of(long long x, long long total, int ctas) {
-    int c = (int)(x * ctas / total);
-    while (total * (c + 1) / ctas <= x) ++c;
-    return c;
 }
 
 __device__ __forceinline__ float tree_ex2(float x) {

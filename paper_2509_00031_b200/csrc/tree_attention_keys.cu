@@ -14,8 +14,8 @@
 // and 64 N of the exponential units.
 //
 // One persistent CTA per SM, 12 warps; the key tiles of all requests are dealt out in equal runs (tree_attention.cuh):
-//   warp 0      K and V tiles by TMA into a ring; warps 2, 3: query tiles into two buffers, a piece ahead
-//   warp 1      one thread issues the products, the scores one tile ahead
+//   warp 0      K and V tiles by TMA into a ring; warp 3: query tiles into two buffers, a piece ahead
+//   warps 1, 2  one thread issues the scores, one tile ahead, another the products with the weights
 //   warps 4-7   softmax.  All keys of a query share one reference; it moves only when a score passes it by more than 2^8, which
 //               the warps tell one another through four flags per tile while they compute the exponentials as if it did not.
 //               Maxima over the keys are formed only when a piece begins or a reference moves.
@@ -33,17 +33,16 @@ constexpr float kNoRef = -1.0e30f;       // reference of a query that has seen n
 template <int DH, int N> struct KeyCfg {
     static constexpr int kTileBytes = kKeys * DH * 2;
     static constexpr int kQBytes = N * DH * 2, kPBytes = N * kKeys * 2;
-    static constexpr int kFixed = 1024 + 2 * kQBytes + 2 * kPBytes + N * 16 + 6 * N * 4 + 1024;
+    static constexpr int kFixed = 2 * kQBytes + 2 * kPBytes + N * 16 + 6 * N * 4 + 1024;
     static constexpr int kFit = (232448 - kFixed) / kTileBytes;
     static constexpr int kStages = kFit > 10 ? 10 : kFit;
     static constexpr int kOffQ = kStages * kTileBytes;
     static constexpr int kOffP = kOffQ + 2 * kQBytes;
-    static constexpr int kOffOnes = kOffP + 2 * kPBytes;                    // one 1024-byte group of ones
-    static constexpr int kOffRed = kOffOnes + 1024;                         // [N][4 warps] floats
+    static constexpr int kOffRed = kOffP + 2 * kPBytes;                     // [N][4 warps] floats
     static constexpr int kOffRef = kOffRed + N * 16;                        // [2][N] floats, then [4][N]: those of the last pieces
     static constexpr int kOffBar = kOffRef + 6 * N * 4;
-    // ring, q full / empty, s full, p full, o full, o empty, out full (2 each), piece done (4), flags, joint
-    static constexpr int kBars = 2 * kStages + 14 + 4 + 2;
+    // ring full, ring empty; q full, q empty, s full, s empty, p full, o full, o empty, out full (2 each), piece done (4), flags, joint
+    static constexpr int kBars = 2 * kStages + 16 + 4 + 2;
     static constexpr int kOffMisc = kOffBar + kBars * 8;
     static constexpr int kUsedBytes = kOffMisc + 64 + 96 + (int)sizeof(TreeRun);
     static constexpr int kSmemBytes = kUsedBytes + 1024 > 232448 ? 232448 : kUsedBytes + 1024;
@@ -135,14 +134,9 @@ __device__ __forceinline__ uint64_t smem_desc_weights(uint32_t saddr) {
     return d;
 }
 
-// Descriptor of the matrix of ones: K-major with 128-byte swizzle, every group of 8 rows the same one.
-__device__ __forceinline__ uint64_t smem_desc_ones(uint32_t saddr) {
-    uint64_t d = 0;
-    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)1 << 16;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
+// eight columns of all 32 lanes
+__device__ __forceinline__ void store8(uint32_t taddr, uint32_t v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %1, %1, %1, %1, %1, %1, %1};" ::"r"(taddr), "r"(v) : "memory");
 }
 
 template <int DH, int N, typename T>
@@ -167,12 +161,13 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
     auto q_full = [&](int s) { return bars + 8u * (2 * NS + s); };
     auto q_empty = [&](int s) { return bars + 8u * (2 * NS + 2 + s); };
     auto s_full = [&](int b) { return bars + 8u * (2 * NS + 4 + b); };
-    auto p_full = [&](int b) { return bars + 8u * (2 * NS + 6 + b); };
-    auto o_full = [&](int b) { return bars + 8u * (2 * NS + 8 + b); };       // the product of a tile (by its parity) has completed
-    auto o_empty = [&](int b) { return bars + 8u * (2 * NS + 10 + b); };     // the output of a piece (by its parity) has been read
-    auto out_full = [&](int b) { return bars + 8u * (2 * NS + 12 + b); };    // every product of a piece (by its parity) has completed
-    auto piece_done = [&](int i) { return bars + 8u * (2 * NS + 14 + i); };  // the softmax warps are through with a piece (mod 4)
-    const uint32_t flag_bar = bars + 8u * (2 * NS + 18), joint_bar = flag_bar + 8u;
+    auto s_empty = [&](int b) { return bars + 8u * (2 * NS + 6 + b); };
+    auto p_full = [&](int b) { return bars + 8u * (2 * NS + 8 + b); };
+    auto o_full = [&](int b) { return bars + 8u * (2 * NS + 10 + b); };      // the products of a tile (by its parity) have completed
+    auto o_empty = [&](int b) { return bars + 8u * (2 * NS + 12 + b); };     // the output of a piece (by its parity) has been read
+    auto out_full = [&](int b) { return bars + 8u * (2 * NS + 14 + b); };    // every product of a piece (by its parity) has completed
+    auto piece_done = [&](int i) { return bars + 8u * (2 * NS + 16 + i); };  // the softmax warps are through with a piece (mod 4)
+    const uint32_t flag_bar = bars + 8u * (2 * NS + 20), joint_bar = flag_bar + 8u;
     volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc);
     volatile uint32_t* odd_piece = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 16);    // [4]: piece + 1 with a non-finite draft value
     volatile uint32_t* flags = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 32);        // [2 tiles][4 warps]
@@ -180,96 +175,93 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
     long long* part = reinterpret_cast<long long*>(sp + Cfg::kOffMisc + 64);
     TreeRun* run = reinterpret_cast<TreeRun*>(sp + Cfg::kOffMisc + 64 + 96);
 
-    if (tid == 0) {
-        for (int s = 0; s < NS; ++s) { mbar_init(ring_full(s), 1); mbar_init(ring_empty(s), 1); }
-        for (int s = 0; s < 2; ++s) {
-            mbar_init(q_full(s), 2); mbar_init(q_empty(s), 1); mbar_init(s_full(s), 1); mbar_init(p_full(s), 4);
-            mbar_init(o_full(s), 1); mbar_init(o_empty(s), 4); mbar_init(out_full(s), 1);
-        }
-        for (int i = 0; i < 4; ++i) { mbar_init(piece_done(i), 4); odd_piece[i] = 0; }
-        mbar_init(flag_bar, 4);
-        mbar_init(joint_bar, 4);
+    if (tid < Cfg::kBars) {
+        const int i = tid - 2 * NS;              // one barrier a thread
+        const bool four = (i >= 6 && i < 10) || i == 12 || i == 13 || i >= 16;       // s empty, p full, o empty, piece done, flags, joint
+        mbar_init(bars + 8u * tid, four ? 4 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        prefetch_tmap(&map_k); prefetch_tmap(&map_v);
     }
+    if (tid < 4) odd_piece[tid] = 0;
+    if (tid == 64) { prefetch_tmap(&map_k); prefetch_tmap(&map_v); }
     if (warp == 1) {
         tmem_alloc(base + Cfg::kOffMisc, 512);
         tmem_relinquish();
     }
-    for (int i = tid; i < 256; i += kKeyThreads) reinterpret_cast<uint32_t*>(sp + Cfg::kOffOnes)[i] = Ops::pack(1.0f, 1.0f);
-    fence_async_smem();
     grid_dependency_wait();                    // lengths, queries and the drafts' keys come from the kernels before
     tree_find_run(p.w, part, run);
     if (tid == 0) reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x].last_cta = -1;
+    const uint32_t tmem = *tmem_slot;          // (allocated before the barriers in tree_find_run)
+    if (warp >= 4 && warp < 8) {               // the matrix of ones: 16 keys' worth, the same for every step
+        tc_fence_after();
+        store8(tmem + 6u * N + ((uint32_t)((warp & 3) * 32) << 16), Ops::pack(1.0f, 1.0f));
+        tmem_store_wait();
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
-    const uint32_t tmem_s = tmem, tmem_o = tmem + 2u * N, tmem_l = tmem + 4u * N;      // scores of a tile by parity, outputs and sums of a piece by parity
+    const uint32_t tmem_s = tmem, tmem_o = tmem + 2u * N, tmem_l = tmem + 4u * N, tmem_1 = tmem + 6u * N;   // scores of a tile by parity, outputs and sums of a piece by parity, ones
     const int n_tiles = (int)(run->end - run->begin);
+    constexpr uint32_t kIdesc = (1u << 4) | (Ops::kFormat << 7) | (Ops::kFormat << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 
     if (warp == 0 && n_tiles > 0) {
         tree_load_keys<DH, NS>(p, &map_k, &map_v, run, base, ring_full(0), ring_empty(0));
-    } else if ((warp == 2 || warp == 3) && n_tiles > 0) {
-        tree_load_queries<DH, N, T>(p, run, sp + Cfg::kOffQ, q_full(0), q_empty(0), tid - 64);
+    } else if (warp == 3 && n_tiles > 0) {
+        tree_load_queries<DH, N, 32, T>(p, run, sp + Cfg::kOffQ, q_full(0), q_empty(0), lane);
     } else if (warp == 1 && n_tiles > 0) {
-        // ---------------- MMA issuer
+        // ---------------- the scores: S^T of the next tile as soon as its buffer has been read
         if (lane == 0) {
-            constexpr uint32_t kIdesc = (1u << 4) | (Ops::kFormat << 7) | (Ops::kFormat << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-            constexpr uint32_t kIdescL = kIdesc | (1u << 16), kIdescO = kIdescL | (1u << 15);   // V^T (15) and P^T (16) run along their rows, not along the keys
-            TreeCursor c = run->at;                    // of the next S
-            uint32_t seq = 0, piece = 0, out_piece = 0;
-            bool ok = true, ends = false;
-            auto issue_s = [&](int t) -> bool {
-                const int slot = seq % NS;
+            TreeCursor c = run->at;
+            uint32_t piece = 0, b = 0;
+            bool ok = true;
+            for (int t = 0; t < n_tiles; ++t, c.next(p.w)) {
+                const uint32_t seq = t == 0 ? 0u : 2u * t - 1u;
+                const int slot = seq % NS, g = t & 1;
                 if (t == 0 || c.item_begins()) {
-                    if (!mbar_wait(q_full(piece & 1u), (piece >> 1) & 1u)) return false;
+                    b = piece & 1u;
+                    if (!mbar_poll(q_full(b), (piece >> 1) & 1u)) { ok = false; break; }
                     ++piece;
                 }
-                const uint32_t b = (piece - 1) & 1u;
-                if (!mbar_wait(ring_full(slot), (seq / NS) & 1u)) return false;
+                if (!mbar_poll(s_empty(g), ((t >> 1) & 1u) ^ 1u) || !mbar_poll(ring_full(slot), (seq / NS) & 1u)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t qa = base + Cfg::kOffQ + b * Cfg::kQBytes, ka = base + slot * Cfg::kTileBytes;
 #pragma unroll
                 for (int k = 0; k < DH / 16; ++k) {
-                    const uint64_t da = smem_desc_sw128(ka + (k >> 2) * (kKeys * 128)) + (uint64_t)(2 * (k & 3));
+                    const uint64_t da = smem_desc_sw128(ka + (k >> 2) * 1024, tree_group_bytes<DH>()) + (uint64_t)(2 * (k & 3));
                     const uint64_t db = smem_desc_sw128(qa + (k >> 2) * (N * 128)) + (uint64_t)(2 * (k & 3));
-                    umma_bf16(tmem_s + (uint32_t)((t & 1) * N), da, db, kIdesc, k > 0 ? 1u : 0u);
+                    umma_bf16(tmem_s + (uint32_t)(g * N), da, db, kIdesc, k > 0 ? 1u : 0u);
                 }
-                umma_commit(s_full(t & 1));
+                umma_commit(s_full(g));
                 umma_commit(ring_empty(slot));
-                ends = c.item_ends();
-                if (ends || t == n_tiles - 1) umma_commit(q_empty(b));
-                ++seq;
-                c.next(p.w);
-                return true;
-            };
-            bool first = true;                         // the tile opens its piece
-            if (!issue_s(0)) ok = false;
-            for (int t = 0; t < n_tiles && ok; ++t) {
-                const bool last = ends;
-                if (t + 1 < n_tiles && !issue_s(t + 1)) { ok = false; break; }
-                const uint32_t b = out_piece & 1u;
-                if (first && out_piece >= 2 && !mbar_wait(o_empty(b), ((out_piece >> 1) & 1u) ^ 1u)) { ok = false; break; }
-                const int slot = seq % NS;
-                if (!mbar_wait(p_full(t & 1), (t >> 1) & 1u) || !mbar_wait(ring_full(slot), (seq / NS) & 1u)) { ok = false; break; }
+                if (c.item_ends() || t == n_tiles - 1) umma_commit(q_empty(b));
+            }
+            if (!ok) atomicExch(p.w.err_flag, kErrTreeWait);
+        }
+    } else if (warp == 2 && n_tiles > 0) {
+        // ---------------- the outputs and sums: a thread of its own, so that waiting for weights holds no scores back
+        if (lane == 0) {
+            constexpr uint32_t kIdescL = kIdesc | (1u << 16), kIdescO = kIdescL | (1u << 15);   // V^T (15) and P^T (16) run along their rows, not along the keys
+            TreeCursor c = run->at;
+            uint32_t piece = 0;
+            bool ok = true, first = true;              // first: the tile opens its piece
+            for (int t = 0; t < n_tiles; ++t, c.next(p.w)) {
+                const uint32_t seq = t == n_tiles - 1 ? 2u * n_tiles - 1u : 2u * t + 2u, b = piece & 1u;
+                const int slot = seq % NS, g = t & 1;
+                if (first && piece >= 2 && !mbar_poll(o_empty(b), ((piece >> 1) & 1u) ^ 1u)) { ok = false; break; }
+                if (!mbar_poll(p_full(g), (t >> 1) & 1u) || !mbar_poll(ring_full(slot), (seq / NS) & 1u)) { ok = false; break; }
                 tc_fence_after();
-                const uint32_t va = base + slot * Cfg::kTileBytes, pa = base + Cfg::kOffP + (t & 1) * Cfg::kPBytes;
+                const uint32_t va = base + slot * Cfg::kTileBytes, pa = base + Cfg::kOffP + g * Cfg::kPBytes;
 #pragma unroll
                 for (int k = 0; k < kKeys / 16; ++k)
                     // (at d_head 64 the rows behind 64 repeat the tile: their results are not read)
-                    umma_bf16(tmem_o + (uint32_t)(b * N), smem_desc_sw128_mn(va + k * 2048, DH == 128 ? kKeys * 128 : 0), smem_desc_weights(pa + k * 256),
-                              kIdescO, (!first || k > 0) ? 1u : 0u);
+                    umma_bf16(tmem_o + b * N, smem_desc_sw128_mn(va + k * 2 * tree_group_bytes<DH>(), DH == 128 ? 1024 : 0, tree_group_bytes<DH>()), smem_desc_weights(pa + k * 256), kIdescO,
+                              (!first || k > 0) ? 1u : 0u);
                 umma_commit(ring_empty(slot));
 #pragma unroll
                 for (int k = 0; k < kKeys / 16; ++k)
-                    umma_bf16(tmem_l + (uint32_t)(b * N), smem_desc_ones(base + Cfg::kOffOnes), smem_desc_weights(pa + k * 256), kIdescL,
-                              (!first || k > 0) ? 1u : 0u);
-                umma_commit(o_full(t & 1));
-                if (last || t == n_tiles - 1) umma_commit(out_full(b));
-                ++seq;
-                first = last;
-                if (last) ++out_piece;
+                    umma_f16_ta(tmem_l + b * N, tmem_1, smem_desc_weights(pa + k * 256), kIdescL, (!first || k > 0) ? 1u : 0u);
+                umma_commit(o_full(g));
+                first = c.item_ends();
+                if (first || t == n_tiles - 1) { umma_commit(out_full(b)); ++piece; }
             }
             if (!ok) atomicExch(p.w.err_flag, kErrTreeWait);
         }
@@ -282,7 +274,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
         bool ok = true, opens = true;
         int q0 = 0, nq = 0;
         uint32_t piece = 0, checks = 0, joins = 0, cur = 0;      // cur: which copy of the references is in use
-        auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)) != 0; };
+        auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_poll(bar, parity)) != 0; };
         auto meet = [&]() -> bool {                              // the four warps
             __syncwarp();
             if (lane == 0) mbar_arrive(joint_bar);
@@ -355,6 +347,11 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                 if (!wait_all(flag_bar, checks & 1u)) { ok = false; break; }
                 ++checks;
                 move = (flags[buf * 4] | flags[buf * 4 + 1] | flags[buf * 4 + 2] | flags[buf * 4 + 3]) != 0;
+                if (!move) {                                     // the scores are no longer needed
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(s_empty(buf));
+                }
             }
             if (move) {
                 // maxima over the keys, new references, outputs and sums brought to them
@@ -364,6 +361,9 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                 tmem_ld_wait();
 #pragma unroll
                 for (int n = 0; n < N; ++n) y[n] = (vis >> n) & 1ull ? __uint_as_float(s[n]) * p.scale_log2 : -INFINITY;
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(s_empty(buf));
                 largest_into<N>(y, red, quarter);
                 if (!meet()) { ok = false; break; }
                 const float* old_ref = refs + cur * N;
@@ -427,7 +427,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
         bool split_front = !c.item_begins(), ok = true;
         uint32_t piece = 0;
         int kt_first = c.kt;
-        auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)) != 0; };
+        auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_poll(bar, parity)) != 0; };
         for (int t = 0; t < n_tiles && ok; ++t) {
             const bool item_ends = c.item_ends();
             if (item_ends || t == n_tiles - 1) {

@@ -75,17 +75,13 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     long long* part = reinterpret_cast<long long*>(sp + Cfg::kOffMisc + 32);
     TreeRun* run = reinterpret_cast<TreeRun*>(sp + Cfg::kOffMisc + 32 + 96);
 
-    if (tid == 0) {
-        for (int s = 0; s < NS; ++s) { mbar_init(ring_full(s), 1); mbar_init(ring_empty(s), 1); }
-        for (int s = 0; s < 2; ++s) {
-            mbar_init(q_full(s), 2); mbar_init(q_empty(s), 1); mbar_init(s_full(s), 1); mbar_init(p_full(s), 4);
-            mbar_init(o_full(s), 1); mbar_init(o_empty(s), 8);
-            odd_piece[s] = 0;
-        }
-        mbar_init(x_full, 8);
+    if (tid < 2 * NS + 13) {
+        const int i = tid - 2 * NS;              // one barrier a thread: ring full, ring empty; q full, q empty, s full, p full, o full, o empty, x full
+        mbar_init(bars + 8u * tid, i < 0 ? 1 : (i < 2 ? 2 : (i < 6 ? 1 : (i < 8 ? 4 : (i < 10 ? 1 : 8)))));
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        prefetch_tmap(&map_k); prefetch_tmap(&map_v);
     }
+    if (tid < 2) odd_piece[tid] = 0;
+    if (tid == 32) { prefetch_tmap(&map_k); prefetch_tmap(&map_v); }
     if (warp == 1) {
         tmem_alloc(base + Cfg::kOffMisc, 512);
         tmem_relinquish();
@@ -103,7 +99,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     if (warp == 0 && n_tiles > 0) {
         tree_load_keys<DH, NS>(p, &map_k, &map_v, run, base + Cfg::kOffRing, ring_full(0), ring_empty(0));
     } else if ((warp == 2 || warp == 3) && n_tiles > 0) {
-        tree_load_queries<DH, kRows, T>(p, run, sp, q_full(0), q_empty(0), tid - 64);
+        tree_load_queries<DH, kRows, 64, T>(p, run, sp, q_full(0), q_empty(0), tid - 64);
     } else if (warp == 1 && n_tiles > 0) {
         // ---------------- MMA issuer
         if (lane == 0) {
@@ -116,17 +112,17 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
             auto issue_s = [&](int t) -> bool {
                 const int slot = seq % NS, g = t & 1;
                 if (t == 0 || c.item_begins()) {
-                    if (!mbar_wait(q_full(piece & 1u), (piece >> 1) & 1u)) return false;
+                    if (!mbar_poll(q_full(piece & 1u), (piece >> 1) & 1u)) return false;
                     ++piece;
                 }
                 const uint32_t b = (piece - 1) & 1u;
-                if (!mbar_wait(ring_full(slot), (seq / NS) & 1u)) return false;
+                if (!mbar_poll(ring_full(slot), (seq / NS) & 1u)) return false;
                 tc_fence_after();
                 const uint32_t qa = base + b * Cfg::kTileBytes, ka = base + Cfg::kOffRing + slot * Cfg::kTileBytes;
 #pragma unroll
                 for (int k = 0; k < DH / 16; ++k) {
                     const uint64_t da = smem_desc_sw128(qa + (k >> 2) * (kRows * 128)) + (uint64_t)(2 * (k & 3));
-                    const uint64_t db = smem_desc_sw128(ka + (k >> 2) * (kKeys * 128)) + (uint64_t)(2 * (k & 3));
+                    const uint64_t db = smem_desc_sw128(ka + (k >> 2) * 1024, tree_group_bytes<DH>()) + (uint64_t)(2 * (k & 3));
                     umma_bf16(tmem_s + 128u * g, da, db, kIdescS, k > 0 ? 1u : 0u);
                 }
                 umma_commit(s_full(g));
@@ -146,16 +142,16 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 if (t + 1 < n_tiles && !issue_s(t + 1)) { ok = false; break; }
                 if (rel < 2) {                         // the accumulator's last piece has been read out
                     uint32_t& uses = g ? uses1 : uses0;
-                    if (uses > 0 && !mbar_wait(o_empty(g), (uses - 1) & 1u)) { ok = false; break; }
+                    if (uses > 0 && !mbar_poll(o_empty(g), (uses - 1) & 1u)) { ok = false; break; }
                     ++uses;
                 }
                 const int slot = seq % NS;
-                if (!mbar_wait(p_full(g), (t >> 1) & 1u) || !mbar_wait(ring_full(slot), (seq / NS) & 1u)) { ok = false; break; }
+                if (!mbar_poll(p_full(g), (t >> 1) & 1u) || !mbar_poll(ring_full(slot), (seq / NS) & 1u)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t va = base + Cfg::kOffRing + slot * Cfg::kTileBytes;
 #pragma unroll
                 for (int k = 0; k < kKeys / 16; ++k)
-                    umma_f16_ta(tmem_o + 128u * g, tmem_s + 128u * g + 8u * k, smem_desc_sw128_mn(va + k * 2048, kKeys * 128), kIdescO,
+                    umma_f16_ta(tmem_o + 128u * g, tmem_s + 128u * g + 8u * k, smem_desc_sw128_mn(va + k * 2 * tree_group_bytes<DH>(), 1024, tree_group_bytes<DH>()), kIdescO,
                                 (rel >= 2 || k > 0) ? 1u : 0u);
                 umma_commit(o_full(g));
                 umma_commit(ring_empty(slot));
@@ -179,7 +175,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         int q0 = 0, nq = 0, tok = 0, hg = 0;
         const uint32_t* mask = nullptr;
         bool ok = true;
-        auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)) != 0; };
+        auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_poll(bar, parity)) != 0; };
         for (int t = 0; t < n_tiles && ok; ++t) {
             if (t == first) {
                 q0 = c.first_query(p.w); nq = c.queries(p.w); kt_first = c.kt;
@@ -400,7 +396,7 @@ EncodeTiledFn tree_encode_fn() {
 bool encode(CUtensorMap* map, int type, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
     EncodeTiledFn fn = tree_encode_fn();
     if (!fn) return false;
-    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
     return fn(map, type == kTypeBf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank, const_cast<void*>(base),
               dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -421,8 +417,7 @@ int tc_launch(const TcParams& p, const CUtensorMap& map_k, const CUtensorMap& ma
 }
 
 template <int DH, typename T>
-int combine_launch(const TcParams& p, int grid, cudaStream_t s) {
-    const int y = p.w.tile_rows < 16 ? p.w.tile_rows : 16;
+int combine_launch(const TcParams& p, int grid, int y, cudaStream_t s) {
     return launch_kernel(tree_combine_kernel<T, DH>, dim3(grid, y), dim3(256), 0, s, true, p.scratch, p.w.tile_rows, p.w.group, p.w.n_heads,
                          static_cast<T*>(p.out), p.out_stride) == cudaSuccess ? ZOQAT_OK : ZOQAT_ERR_CUDA;
 }
@@ -448,19 +443,30 @@ int launch_tree_attention_tc(const TreeAttnArgs& a, cudaStream_t s, bool depende
     p.out = a.out; p.out_stride = a.out_stride; p.scratch = a.scratch;
     p.v = a.cache.v; p.page_stride = a.cache.page_stride; p.slot_stride = a.cache.slot_stride; p.head_stride = a.cache.head_stride;
     alignas(64) CUtensorMap map_k, map_v;
-    const cuuint64_t kd[4] = {(cuuint64_t)dh, (cuuint64_t)a.cache.page_size, (cuuint64_t)a.cache.n_kv_heads, (cuuint64_t)a.cache.n_pages};
-    const cuuint64_t kst[3] = {(cuuint64_t)a.cache.slot_stride * 2, (cuuint64_t)a.cache.head_stride * 2, (cuuint64_t)a.cache.page_stride * 2};
-    const cuuint32_t kb[4] = {64, (cuuint32_t)p.box_keys, 1, 1};
-    if (!encode(&map_k, type, a.cache.k, 4, kd, kst, kb) || !encode(&map_v, type, a.cache.v, 4, kd, kst, kb)) return ZOQAT_ERR_CUDA;
+    // {64 columns, 8 keys, halves, groups of 8 keys, heads of all pages}
+    const int64_t ss = a.cache.slot_stride, unit = a.cache.n_kv_heads > 1 ? a.cache.head_stride : a.cache.page_stride;
+    if (a.cache.n_pages > 1 && a.cache.page_stride % unit) return ZOQAT_ERR_UNSUPPORTED;
+    p.page_units = a.cache.n_pages > 1 ? (int)(a.cache.page_stride / unit) : 1;
+    const int64_t units = (int64_t)(a.cache.n_pages - 1) * p.page_units + a.cache.n_kv_heads;
+    if (a.cache.page_stride / unit > INT32_MAX || units >= INT32_MAX) return ZOQAT_ERR_UNSUPPORTED;
+    p.units = (int)units;
+    p.page_shift = -1;
+    for (int b = 3; b < 31; ++b)
+        if (a.cache.page_size == 1 << b) p.page_shift = b;
+    const cuuint64_t kd[5] = {64, 8, (cuuint64_t)dh / 64, (cuuint64_t)a.cache.page_size / 8, (cuuint64_t)units};
+    const cuuint64_t kst[4] = {(cuuint64_t)ss * 2, 128, (cuuint64_t)ss * 16, (cuuint64_t)unit * 2};
+    const cuuint32_t kb[5] = {64, 8, (cuuint32_t)dh / 64, (cuuint32_t)p.box_keys / 8, 1};
+    if (!encode(&map_k, type, a.cache.k, 5, kd, kst, kb) || !encode(&map_v, type, a.cache.v, 5, kd, kst, kb)) return ZOQAT_ERR_CUDA;
     const int grid = tree_grid();
+    const int y = want < 2 ? 1 : (want < 32 ? (int)(want + 1) / 2 : 16);      // CTAs that share the queries of a split item
     int rc;
     if (nq < kRows) rc = launch_tree_keys(p, map_k, map_v, dh, type, nq, grid, s, dependent);
     else if (type == kTypeBf16) rc = dh == 64 ? tc_launch<64, __nv_bfloat16>(p, map_k, map_v, grid, s, dependent) : tc_launch<128, __nv_bfloat16>(p, map_k, map_v, grid, s, dependent);
     else rc = dh == 64 ? tc_launch<64, __half>(p, map_k, map_v, grid, s, dependent) : tc_launch<128, __half>(p, map_k, map_v, grid, s, dependent);
     if (rc != ZOQAT_OK) return rc;
     count_launch();
-    if (type == kTypeBf16) rc = dh == 64 ? combine_launch<64, __nv_bfloat16>(p, grid, s) : combine_launch<128, __nv_bfloat16>(p, grid, s);
-    else rc = dh == 64 ? combine_launch<64, __half>(p, grid, s) : combine_launch<128, __half>(p, grid, s);
+    if (type == kTypeBf16) rc = dh == 64 ? combine_launch<64, __nv_bfloat16>(p, grid, y, s) : combine_launch<128, __nv_bfloat16>(p, grid, y, s);
+    else rc = dh == 64 ? combine_launch<64, __half>(p, grid, y, s) : combine_launch<128, __half>(p, grid, y, s);
     if (rc == ZOQAT_OK) count_launch();
     return rc;
 }

@@ -14,6 +14,8 @@ struct TcParams {
     const void* q;
     int64_t q_stride;
     int box_keys;                // keys of one K / V box: a page, or 128 of a larger one
+    int page_shift;              // log2 of the page size, or -1
+    int page_units, units;       // a page's step and the end of the maps' outermost dimension, which counts heads through all pages
     int n_pages, mask_words;
     const uint32_t* tree_mask;
     float scale_log2;
@@ -78,49 +80,57 @@ __device__ __forceinline__ uint32_t visible_word(int k0, int C, int n, int i, co
 }
 
 
+// A K or V tile in shared memory: groups of 8 keys, [16 groups][DH / 64 halves][8 keys][128 bytes], 128-byte swizzle, so that one
+// TMA box fetches all of a page's keys of a head.
+template <int DH> __host__ __device__ constexpr int tree_group_bytes() { return DH / 64 * 1024; }
+
 // K and V tiles, by a whole warp: K(0), K(1), V(0), K(2), V(1), ..., the order in which the products consume them.  Every lane
-// fetches one box (a page, or 128 keys of a larger one; one 64-column half) and reads the block table for it, one tile ahead.
-// A tile lies in the ring as [half][128 keys][128 bytes], 128-byte swizzle.
+// fetches one page (or 128 keys of a larger one), and reads its entry of the block table two tiles ahead.
 template <int DH, int NS>
 __device__ __forceinline__ void tree_load_keys(const TcParams& p, const CUtensorMap* map_k, const CUtensorMap* map_v, const TreeRun* run,
                                                uint32_t ring, uint32_t full, uint32_t empty) {
-    constexpr int HALVES = DH / 64, kTileBytes = kKeys * DH * 2;
-    const int lane = threadIdx.x & 31, half = lane % HALVES, box = lane / HALVES;
+    constexpr int kTileBytes = kKeys * DH * 2, kGroup = tree_group_bytes<DH>();
+    const int lane = threadIdx.x & 31;
     const int n_box = kKeys / p.box_keys, n_tiles = (int)(run->end - run->begin);
+    const uint32_t box_bytes = (uint32_t)(p.box_keys >> 3) * kGroup;
     TreeCursor c = run->at;
     uint32_t seq = 0;
     bool ok = true;
-    struct Box { int page, off, h, live; bool mine; };
+    struct Box { int page, group, h, live; bool mine; };         // page: as the table has it, looked at when the box is fetched
     auto look_up = [&](Box& x) {                                 // this lane's box of the cursor's tile
-        const int key0 = c.kt * kKeys + box * p.box_keys;
+        const int key0 = c.kt * kKeys + lane * p.box_keys, left = c.r.L - c.kt * kKeys;
         x.h = c.h;
-        x.live = min(n_box, (c.r.L - c.kt * kKeys + p.box_keys - 1) / p.box_keys);
-        x.mine = box < n_box && key0 < c.r.L;
-        x.page = x.off = 0;
+        x.live = left >= kKeys ? n_box : (left + p.box_keys - 1) / p.box_keys;
+        x.mine = lane < x.live;
         if (!x.mine) return;
-        const int idx = key0 / p.w.page_size;
-        x.off = key0 - idx * p.w.page_size;
+        const int idx = p.page_shift >= 0 ? key0 >> p.page_shift : key0 / p.w.page_size;
+        x.group = (key0 - idx * p.w.page_size) >> 3;
         x.page = __ldg(p.w.block_table + (size_t)c.b * p.w.max_pages + idx);
-        if (x.page < 0 || x.page >= p.n_pages) { atomicExch(p.w.err_flag, kErrBadPage); x.page = p.n_pages; }   // behind the map's end: zeros
     };
     auto fetch = [&](const CUtensorMap* map, const Box& x) -> bool {
         const int slot = seq % NS;
-        if (!__all_sync(0xffffffffu, mbar_wait(empty + 8u * slot, ((seq / NS) & 1u) ^ 1u))) return false;
-        if (lane == 0) mbar_arrive_expect_tx(full + 8u * slot, (uint32_t)(x.live * HALVES * p.box_keys * 128));
+        if (!__all_sync(0xffffffffu, mbar_poll(empty + 8u * slot, ((seq / NS) & 1u) ^ 1u))) return false;
+        if (lane == 0) mbar_arrive_expect_tx(full + 8u * slot, (uint32_t)x.live * box_bytes);
         __syncwarp();
-        if (x.mine) tma_load_4d(ring + slot * kTileBytes + half * (kKeys * 128) + box * p.box_keys * 128, map, full + 8u * slot, half * 64, x.off, x.h, x.page);
+        if (x.mine) {
+            int unit = p.units;                                  // behind the map's end: zeros
+            if (x.page >= 0 && x.page < p.n_pages) unit = x.page * p.page_units + x.h;
+            else atomicExch(p.w.err_flag, kErrBadPage);
+            tma_load_5d(ring + slot * kTileBytes + lane * box_bytes, map, full + 8u * slot, 0, 0, 0, x.group, unit);
+        }
         ++seq;
         return true;
     };
-    Box cur, prev, next;
+    Box prev{}, cur{}, next{}, after{};
     look_up(cur);
-    prev = next = cur;
+    if (n_tiles > 1) { c.next(p.w); look_up(next); }
     for (int t = 0; t <= n_tiles && ok; ++t) {
         if (t < n_tiles && !fetch(map_k, cur)) { ok = false; break; }
-        if (t + 1 < n_tiles) { c.next(p.w); look_up(next); }     // before the wait below
+        if (t + 2 < n_tiles) { c.next(p.w); look_up(after); }
         if (t > 0 && !fetch(map_v, prev)) { ok = false; break; }
         prev = cur;
         cur = next;
+        next = after;
     }
     if (!ok && lane == 0) atomicExch(p.w.err_flag, kErrTreeWait);
     // every load issued above has to land before the CTA may leave
@@ -128,9 +138,9 @@ __device__ __forceinline__ void tree_load_keys(const TcParams& p, const CUtensor
         if (!mbar_wait(full + 8u * (k % NS), (k / NS) & 1u)) break;
 }
 
-// Query tiles, by two warps (`lane` 0..63), a piece ahead of the products: rows of 128 bytes, 128-byte swizzle, [half][NQ rows].
+// Query tiles, by THREADS threads (whole warps; `lane`: which of them), a piece ahead of the products: rows of 128 bytes, 128-byte swizzle, [half][NQ rows].
 // Rows behind the tile's last query keep what they hold; their results are not used.  full counts one arrival per warp.
-template <int DH, int NQ, typename T>
+template <int DH, int NQ, int THREADS, typename T>
 __device__ __forceinline__ void tree_load_queries(const TcParams& p, const TreeRun* run, uint8_t* q_tiles, uint32_t full, uint32_t empty, int lane) {
     constexpr int kChunks = DH / 8, kTileBytes = NQ * DH * 2;
     const int n_tiles = (int)(run->end - run->begin);
@@ -143,11 +153,11 @@ __device__ __forceinline__ void tree_load_queries(const TcParams& p, const TreeR
         const int q0 = c.first_query(p.w), n = c.queries(p.w) * kChunks;
         uint8_t* dst = q_tiles + b * kTileBytes;
         const T* base = static_cast<const T*>(p.q) + (int64_t)c.r.row0 * p.q_stride + (int64_t)c.h * p.w.group * DH;
-        for (int x0 = lane; x0 < n; x0 += 4 * 64) {
+        for (int x0 = lane; x0 < n; x0 += 4 * THREADS) {
             uint4 w[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int x = x0 + 64 * u, r = x / kChunks;
+                const int x = x0 + THREADS * u, r = x / kChunks;
                 if (x < n) {
                     const int tok = (q0 + r) / p.w.group, hg = q0 + r - tok * p.w.group;
                     w[u] = __ldg(reinterpret_cast<const uint4*>(base + (int64_t)tok * p.q_stride + (int64_t)hg * DH) + x % kChunks);
@@ -155,7 +165,7 @@ __device__ __forceinline__ void tree_load_queries(const TcParams& p, const TreeR
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int x = x0 + 64 * u, r = x / kChunks, ch = x % kChunks;
+                const int x = x0 + THREADS * u, r = x / kChunks, ch = x % kChunks;
                 if (x < n) *reinterpret_cast<uint4*>(dst + (ch >> 3) * (NQ * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = w[u];
             }
         }
@@ -174,7 +184,7 @@ __device__ __forceinline__ bool tree_clean_values(uint8_t* v, int first_draft, i
     bool met = false;
     for (int x = thread; x < (kKeys - first_draft) * (DH / 8); x += 128) {
         const int key = first_draft + x / (DH / 8), ch = x % (DH / 8);
-        uint4* at = reinterpret_cast<uint4*>(v + (ch >> 3) * (kKeys * 128) + key * 128 + (((ch & 7) ^ (key & 7)) << 4));
+        uint4* at = reinterpret_cast<uint4*>(v + (key >> 3) * tree_group_bytes<DH>() + (ch >> 3) * 1024 + (key & 7) * 128 + (((ch & 7) ^ (key & 7)) << 4));
         if (key >= end) { *at = make_uint4(0, 0, 0, 0); continue; }
         uint4 w = *at;
         uint32_t ww[4] = {w.x, w.y, w.z, w.w};
