@@ -158,7 +158,7 @@ tree_attention_simt_kernel(SimtParams p) {
     using Cfg = SimtCfg<DH>;
     constexpr int VPL = DH / 32;
     extern __shared__ __align__(16) float sm[];
-    __shared__ long long part[8];
+    __shared__ long long part[16];
     __shared__ TreeRun run;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     float* qs = sm + Cfg::kOffQ;
@@ -169,7 +169,10 @@ tree_attention_simt_kernel(SimtParams p) {
     TreeTail* tails = reinterpret_cast<TreeTail*>(p.scratch);
     grid_dependency_wait();
     tree_find_run(p.w, part, &run);
-    if (tid == 0) tails[blockIdx.x].last_cta = -1;
+    if (tid == 0) {
+        tails[blockIdx.x].last_cta = -1;
+        tree_front(p.scratch)[blockIdx.x] = run.begin < run.end && !run.at.item_begins();
+    }
     if (run.begin >= run.end) return;
 
     TreeCursor c = run.at, ahead = run.at;
@@ -258,7 +261,7 @@ tree_attention_simt_kernel(SimtParams p) {
             }
             if (!ends && !split_front && tid == 0) {       // begins here, goes on in the next CTAs
                 TreeTail t{};
-                t.last_cta = tree_cta_of(run.end + (c.r.n_kt - 1 - c.kt) - 1, run.total, run.ctas);
+                t.last_cta = run.tail_cta;
                 t.queries = nq; t.row0 = c.r.row0; t.q0 = q0; t.h = c.h;
                 tails[blockIdx.x] = t;
             }
@@ -306,7 +309,7 @@ size_t tree_attention_scratch_bytes(int type, int d_head) {
 int launch_tree_attention_simt(const TreeAttnArgs& a, cudaStream_t s, bool dependent) {
     SimtParams p{};
     p.w = TreeWork{a.kv_len, a.row_start, a.block_table, a.batch, a.rows, a.n_heads, a.cache.n_kv_heads, a.max_pages, a.cache.page_size,
-                   a.n_heads / a.cache.n_kv_heads, kSimtRows, kSimtKeys, a.err_flag};
+                   a.n_heads / a.cache.n_kv_heads, kSimtRows, kSimtKeys, 2, a.err_flag};
     p.q = static_cast<const float*>(a.q); p.q_stride = a.q_stride; p.cache = a.cache;
     p.tree_mask = a.tree_mask; p.mask_words = a.mask_words;
     p.scale_log2 = (float)(1.4426950408889634 * (double)a.scale);

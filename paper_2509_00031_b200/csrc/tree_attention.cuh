@@ -2,10 +2,11 @@
 //
 // For request b with n new rows and L keys (C = L - n of them cached before this step, the drafts last) and g = n_heads /
 // n_kv_heads query heads per key head, the queries that read one key head are the n * g vectors (draft i, head in group) in
-// this order, cut into row tiles.  An item is (request, key head, row tile), its work is the number of key
-// tiles.  All items' key tiles, laid out one after the other, are cut into gridDim.x equal runs, one per CTA: long contexts
-// are split over as many CTAs as it takes, short ones are packed, and no length is needed on the host.  Every CTA finds its
-// run by scanning the requests' lengths.  A piece of an item that is not the whole item leaves (reference, sum, output) per
+// this order, cut into row tiles.  An item is (request, key head, row tile), its work the number of key tiles and a constant
+// for opening and closing it (in tiles' time: without it the CTAs that get short contexts finish last, measured at 145 against
+// 68 thousand cycles).  All items' work, laid out one after the other, is cut into gridDim.x equal runs, one per CTA: long
+// contexts are split over as many CTAs as it takes, short ones are packed, and no length is needed on the host.  Every CTA
+// finds its run by scanning the requests' lengths.  A piece of an item that is not the whole item leaves (reference, sum, output) per
 // query in the scratch, at most two pieces per CTA, and tree_combine_kernel joins them in the order of the keys, so results
 // do not depend on timing.
 #pragma once
@@ -21,6 +22,7 @@ struct TreeWork {
     int group;               // query heads per key head
     int tile_rows;           // queries per row tile
     int key_tile;            // keys per key tile
+    int item_cost;           // work of an item besides its key tiles, in tiles
     int32_t* err_flag;
 };
 
@@ -40,11 +42,6 @@ __device__ __forceinline__ TreeRequest tree_request(const TreeWork& w, int b) {
     r.n_kt = (r.L + w.key_tile - 1) / w.key_tile;
     return r;
 }
-__device__ __forceinline__ long long tree_tiles(const TreeWork& w, int b) {
-    const TreeRequest r = tree_request(w, b);
-    return (long long)w.n_kv * r.n_rt * r.n_kt;
-}
-
 // Position in the sequence of key tiles.  next() moves on by one tile; tiles of requests without work do not exist.
 struct TreeCursor {
     TreeRequest r;
@@ -71,69 +68,95 @@ __device__ __forceinline__ long long tree_div(long long a, long long b) {
     return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
 }
 
-struct TreeRun { long long begin, end, total; int ctas; TreeCursor at; };   // ctas: CTAs that have a run
+// The run of a CTA: the tiles [begin, end) of all tiles in order.  tail_cta: where the item ends that the run's end cuts in two.
+struct TreeRun { long long begin, end; int tail_cta; TreeCursor at; };
 
-// Run c of `total` tiles in `ctas` runs begins here: the first total % ctas runs have one tile more than the others.
+// Run c of `total` work in `ctas` runs begins here: the first total % ctas runs have one unit more than the others.
 __device__ __forceinline__ long long tree_run_begin(long long total, int ctas, int c) {
     const long long q = tree_div(total, ctas), r = total - q * ctas;
     return q * c + (c < r ? c : r);
 }
-// The CTA whose run holds tile `x`.
+// The CTA whose run holds unit `x`.
 __device__ __forceinline__ int tree_cta_of(long long x, long long total, int ctas) {
     const long long q = tree_div(total, ctas), r = total - q * ctas, wide = r * (q + 1);
     return (int)(x < wide ? tree_div(x, q + 1) : r + tree_div(x - wide, q));
 }
 
-// The run of this CTA; called by all threads of the block (part: one word per warp, out: shared).  Ends with a barrier.
+// The run of this CTA; called by all threads of the block (part: two words per warp, out: shared).  Ends with a barrier.
+// An item's units are its constant, then its tiles: a tile belongs to the CTA whose run holds its unit.
 __device__ __forceinline__ void tree_find_run(const TreeWork& w, long long* part, TreeRun* out) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
     const int per = (w.batch + blockDim.x - 1) / blockDim.x;
     const int b0 = min(tid * per, w.batch), b1 = min(b0 + per, w.batch);
-    long long mine = 0;
-    for (int b = b0; b < b1; ++b) mine += tree_tiles(w, b);
-    long long upto = mine;
+    long long tiles = 0, items = 0;
+    for (int b = b0; b < b1; ++b) {
+        const TreeRequest r = tree_request(w, b);
+        const long long n = r.n_kt ? (long long)w.n_kv * r.n_rt : 0;
+        items += n;
+        tiles += n * r.n_kt;
+    }
+    long long up_tiles = tiles, up_items = items;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const long long u = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += u;
+        const long long u = __shfl_up_sync(0xffffffffu, up_tiles, o), v = __shfl_up_sync(0xffffffffu, up_items, o);
+        if (lane >= o) { up_tiles += u; up_items += v; }
     }
-    if (lane == 31) part[warp] = upto;
+    if (lane == 31) { part[2 * warp] = up_tiles; part[2 * warp + 1] = up_items; }
     __syncthreads();
-    long long total = 0;
+    long long all_tiles = 0, all_items = 0;
     for (int k = 0; k < warps; ++k) {
-        if (k == warp) upto += total;
-        total += part[k];
+        if (k == warp) { up_tiles += all_tiles; up_items += all_items; }
+        all_tiles += part[2 * k];
+        all_items += part[2 * k + 1];
     }
-    // the runs are those of the CTAs or, where there are fewer tiles, of as many CTAs as there are tiles: none is empty
+    const long long total = all_tiles + w.item_cost * all_items;
     const int ctas = total < (long long)gridDim.x ? (int)total : (int)gridDim.x;
     const bool idle = (int)blockIdx.x >= ctas;
-    const long long begin = idle ? 0 : tree_run_begin(total, ctas, blockIdx.x), end = idle ? 0 : tree_run_begin(total, ctas, blockIdx.x + 1);
-    if (tid == 0) { out->begin = begin; out->end = end; out->total = total; out->ctas = ctas; }
-    if (begin < end && begin >= upto - mine && begin < upto) {       // exactly one thread
-        long long rest = begin - (upto - mine);
-        TreeCursor c;
-        for (c.b = b0; c.b < b1; ++c.b) {
-            c.load(w);
-            const long long t = (long long)w.n_kv * c.r.n_rt * c.r.n_kt;
-            if (rest < t) break;
-            rest -= t;
+    if (tid == 0 && idle) { out->begin = out->end = 0; }
+    if (!idle) {
+        const long long lo = (up_tiles - tiles) + w.item_cost * (up_items - items), hi = up_tiles + w.item_cost * up_items;   // this thread's units
+        const long long edge[2] = {tree_run_begin(total, ctas, blockIdx.x), tree_run_begin(total, ctas, blockIdx.x + 1)};
+        if (tid == 0 && edge[1] == total) { out->end = all_tiles; out->tail_cta = -1; }
+#pragma unroll 1
+        for (int e = 0; e < 2; ++e) {
+            if (edge[e] < lo || edge[e] >= hi) continue;           // exactly one thread goes on (none for the end of the last run)
+            long long rest = edge[e] - lo, at_tile = up_tiles - tiles, unit = lo;
+            TreeCursor c;
+            int cost = 1;
+            for (c.b = b0; c.b < b1; ++c.b) {
+                c.load(w);
+                if (c.r.n_kt == 0) continue;
+                cost = c.r.n_kt + w.item_cost;
+                const long long n = (long long)w.n_kv * c.r.n_rt;
+                if (rest < n * cost) break;
+                rest -= n * cost;
+                unit += n * cost;
+                at_tile += n * c.r.n_kt;
+            }
+            const long long item = tree_div(rest, cost), head = tree_div(item, c.r.n_rt);
+            const int off = (int)(rest - item * cost);
+            c.kt = max(0, off - w.item_cost);
+            c.rt = (int)(item - head * c.r.n_rt);
+            c.h = (int)head;
+            at_tile += item * c.r.n_kt + c.kt;
+            if (e == 0) { out->begin = at_tile; out->at = c; }
+            else { out->end = at_tile; out->tail_cta = c.kt > 0 ? tree_cta_of(unit + (item + 1) * cost - 1, total, ctas) : -1; }
         }
-        const long long item = tree_div(rest, c.r.n_kt), head = tree_div(item, c.r.n_rt);
-        c.kt = (int)(rest - item * c.r.n_kt);
-        c.rt = (int)(item - head * c.r.n_rt);
-        c.h = (int)head;
-        out->at = c;
     }
     __syncthreads();
 }
 
 // ---- partial results ------------------------------------------------------------------------------------------------
-// One descriptor per CTA, then 2 * G slots of [tile_rows] references, [tile_rows] sums and [tile_rows][d_head] outputs (fp32).
+// One descriptor per CTA, a word that says whether its front slot is in use, then 2 * G slots of [tile_rows] references, [tile_rows] sums and [tile_rows][d_head] outputs (fp32).
 struct TreeTail { int last_cta, queries, row0, q0, h, pad[3]; };   // an item that begins in this CTA and ends in last_cta; -1: none
-constexpr size_t kTailBytes = 8192;                      // room for the descriptors
 constexpr int kMaxTreeGrid = 148;                        // one CTA per SM
+constexpr size_t kTailBytes = 8192, kFrontOffset = kMaxTreeGrid * sizeof(TreeTail);
+static_assert(kFrontOffset + kMaxTreeGrid * sizeof(int) <= kTailBytes, "descriptors");
 
 __host__ __device__ inline size_t tree_slot_floats(int tile_rows, int dh) { return (size_t)tile_rows * (dh + 2); }
+
+// which CTAs have a front piece: one that continues an item of an earlier CTA (slot 2 c; slot 2 c + 1: one that goes on in the next)
+__device__ __forceinline__ int* tree_front(uint8_t* scratch) { return reinterpret_cast<int*>(scratch + kFrontOffset); }
 
 __device__ __forceinline__ float* tree_slot(uint8_t* scratch, int index, int tile_rows, int dh) {
     return reinterpret_cast<float*>(scratch + kTailBytes) + (size_t)index * tree_slot_floats(tile_rows, dh);
@@ -175,7 +198,7 @@ tree_combine_kernel(uint8_t* scratch, int tile_rows, int group, int n_heads, T* 
                 pm[u] = -INFINITY; pl[u] = 0.0f;
 #pragma unroll
                 for (int j = 0; j < VPL; ++j) po[u][j] = 0.0f;
-                if (p < pieces) {
+                if (p < pieces && (p == 0 || tree_front(scratch)[c0 + p])) {
                     const float* slot = tree_slot(scratch, p == 0 ? 2 * c0 + 1 : 2 * (c0 + p), tile_rows, DH);
                     pm[u] = slot[q];
                     pl[u] = slot[tile_rows + q];

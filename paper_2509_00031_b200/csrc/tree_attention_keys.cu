@@ -33,38 +33,32 @@ constexpr float kNoRef = -1.0e30f;       // reference of a query that has seen n
 template <int DH, int N> struct KeyCfg {
     static constexpr int kTileBytes = kKeys * DH * 2;
     static constexpr int kQBytes = N * DH * 2, kPBytes = N * kKeys * 2;
-    static constexpr int kFixed = 2 * kQBytes + 2 * kPBytes + N * 16 + 6 * N * 4 + 1024;
+    static constexpr int kFixed = 2 * kQBytes + 3 * kPBytes + N * 16 + 6 * N * 4 + 2 * N * kMaskWords * 4 + 1024;
     static constexpr int kFit = (232448 - kFixed) / kTileBytes;
-    static constexpr int kStages = kFit > 10 ? 10 : kFit;
+    // an even number: K tiles (odd places of the sequence) and V tiles (even places) then have slots of their own, so that each
+    // slot is consumed by one thread in order and no one can wait for a phase before the one ahead of it has completed
+    static constexpr int kStages = kFit > 10 ? 10 : kFit / 2 * 2;
     static constexpr int kOffQ = kStages * kTileBytes;
     static constexpr int kOffP = kOffQ + 2 * kQBytes;
-    static constexpr int kOffRed = kOffP + 2 * kPBytes;                     // [N][4 warps] floats
+    static constexpr int kOffRed = kOffP + 3 * kPBytes;                     // [N][4 warps] floats
     static constexpr int kOffRef = kOffRed + N * 16;                        // [2][N] floats, then [4][N]: those of the last pieces
-    static constexpr int kOffBar = kOffRef + 6 * N * 4;
-    // ring full, ring empty; q full, q empty, s full, s empty, p full, o full, o empty, out full (2 each), piece done (4), flags, joint
-    static constexpr int kBars = 2 * kStages + 16 + 4 + 2;
+    static constexpr int kOffMask = kOffRef + 6 * N * 4;                    // [2][N drafts][kMaskWords]
+    static constexpr int kOffBar = kOffMask + 2 * N * kMaskWords * 4;
+    // ring full, ring empty; q full, q empty, s full, s empty (2 each), p full, o full (3 each), o empty, out full (2), piece done (4), flags, joint
+    static constexpr int kBars = 2 * kStages + 18 + 4 + 2;
     static constexpr int kOffMisc = kOffBar + kBars * 8;
-    static constexpr int kUsedBytes = kOffMisc + 64 + 96 + (int)sizeof(TreeRun);
+    static constexpr int kUsedBytes = kOffMisc + 64 + 192 + (int)sizeof(TreeRun);
     static constexpr int kSmemBytes = kUsedBytes + 1024 > 232448 ? 232448 : kUsedBytes + 1024;
     static_assert(kUsedBytes <= 232448 && kStages >= 4, "shared memory");
 };
 
-// N scores of the thread's key
-template <int N> __device__ __forceinline__ void load_scores(uint32_t taddr, uint32_t (&v)[N]);
-template <> __device__ __forceinline__ void load_scores<16>(uint32_t taddr, uint32_t (&v)[16]) {
+// 16 scores of the thread's key (16 outputs or sums of its column)
+__device__ __forceinline__ void load16(uint32_t taddr, uint32_t (&v)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
         : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
           "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
         : "r"(taddr) : "memory");
-}
-template <> __device__ __forceinline__ void load_scores<32>(uint32_t taddr, uint32_t (&v)[32]) { tmem_ld32(taddr, v); }
-template <> __device__ __forceinline__ void load_scores<64>(uint32_t taddr, uint32_t (&v)[64]) {
-    uint32_t a[32], b[32];
-    tmem_ld32(taddr, a);
-    tmem_ld32(taddr + 32u, b);
-#pragma unroll
-    for (int e = 0; e < 32; ++e) { v[e] = a[e]; v[32 + e] = b[e]; }
 }
 __device__ __forceinline__ void store16(uint32_t taddr, const uint32_t (&v)[16]) {
     asm volatile(
@@ -74,21 +68,7 @@ __device__ __forceinline__ void store16(uint32_t taddr, const uint32_t (&v)[16])
         : "memory");
 }
 
-// Largest v[i] over the warp's 32 lanes, for i = 0 .. 31 at once: the return value of lane i is that of v[i].
-__device__ __forceinline__ float largest32(float (&v)[32]) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int h = 16; h >= 1; h >>= 1) {
-        const bool up = lane & h;
-#pragma unroll
-        for (int i = 0; i < h; ++i) {
-            const float keep = up ? v[i + h] : v[i], give = up ? v[i] : v[i + h];
-            v[i] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, h));
-        }
-    }
-    return v[0];
-}
-// the same for 16 values: lanes 2 i and 2 i + 1 hold that of v[i]
+// Largest v[i] over the warp's 32 lanes, for 16 values at once: lanes 2 i and 2 i + 1 return that of v[i].
 __device__ __forceinline__ float largest16(float (&v)[16]) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
@@ -101,26 +81,6 @@ __device__ __forceinline__ float largest16(float (&v)[16]) {
         }
     }
     return fmaxf(v[0], __shfl_xor_sync(0xffffffffu, v[0], 1));
-}
-// Largest value per query over the warp's keys into red[n][warp].
-template <int N>
-__device__ __forceinline__ void largest_into(const float (&v)[N], float* red, int warp) {
-    const int lane = threadIdx.x & 31;
-    if constexpr (N == 16) {
-        float t[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) t[i] = v[i];
-        const float r = largest16(t);
-        if (!(lane & 1)) red[(lane >> 1) * 4 + warp] = r;
-    } else {
-#pragma unroll
-        for (int q = 0; q < N / 32; ++q) {
-            float t[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) t[i] = v[32 * q + i];
-            red[(32 * q + lane) * 4 + warp] = largest32(t);
-        }
-    }
 }
 
 // Shared-memory descriptor of the weights: query-major cores of 8 queries x 8 keys (128 bytes), no swizzle; the next 8 keys
@@ -152,7 +112,10 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if ((base - raw) + (uint32_t)Cfg::kUsedBytes > p.smem_bytes) {           // uniform: nothing has been set up yet
         if (tid == 0) atomicExch(p.w.err_flag, kErrTreeWait);
-        if (tid == 0) reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x].last_cta = -1;
+        if (tid == 0) {
+            reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x].last_cta = -1;
+            tree_front(p.scratch)[blockIdx.x] = 0;
+        }
         return;
     }
     const uint32_t bars = base + Cfg::kOffBar;
@@ -163,21 +126,21 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
     auto s_full = [&](int b) { return bars + 8u * (2 * NS + 4 + b); };
     auto s_empty = [&](int b) { return bars + 8u * (2 * NS + 6 + b); };
     auto p_full = [&](int b) { return bars + 8u * (2 * NS + 8 + b); };
-    auto o_full = [&](int b) { return bars + 8u * (2 * NS + 10 + b); };      // the products of a tile (by its parity) have completed
-    auto o_empty = [&](int b) { return bars + 8u * (2 * NS + 12 + b); };     // the output of a piece (by its parity) has been read
-    auto out_full = [&](int b) { return bars + 8u * (2 * NS + 14 + b); };    // every product of a piece (by its parity) has completed
-    auto piece_done = [&](int i) { return bars + 8u * (2 * NS + 16 + i); };  // the softmax warps are through with a piece (mod 4)
-    const uint32_t flag_bar = bars + 8u * (2 * NS + 20), joint_bar = flag_bar + 8u;
+    auto o_full = [&](int b) { return bars + 8u * (2 * NS + 11 + b); };      // the products of a tile (mod 3, as the weights' buffers) have completed
+    auto o_empty = [&](int b) { return bars + 8u * (2 * NS + 14 + b); };     // the output of a piece (by its parity) has been read
+    auto out_full = [&](int b) { return bars + 8u * (2 * NS + 16 + b); };    // every product of a piece (by its parity) has completed
+    auto piece_done = [&](int i) { return bars + 8u * (2 * NS + 18 + i); };  // the softmax warps are through with a piece (mod 4)
+    const uint32_t flag_bar = bars + 8u * (2 * NS + 22), joint_bar = flag_bar + 8u;
     volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc);
     volatile uint32_t* odd_piece = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 16);    // [4]: piece + 1 with a non-finite draft value
     volatile uint32_t* flags = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 32);        // [2 tiles][4 warps]
     float* const refs = reinterpret_cast<float*>(sp + Cfg::kOffRef);
     long long* part = reinterpret_cast<long long*>(sp + Cfg::kOffMisc + 64);
-    TreeRun* run = reinterpret_cast<TreeRun*>(sp + Cfg::kOffMisc + 64 + 96);
+    TreeRun* run = reinterpret_cast<TreeRun*>(sp + Cfg::kOffMisc + 64 + 192);
 
     if (tid < Cfg::kBars) {
         const int i = tid - 2 * NS;              // one barrier a thread
-        const bool four = (i >= 6 && i < 10) || i == 12 || i == 13 || i >= 16;       // s empty, p full, o empty, piece done, flags, joint
+        const bool four = (i >= 6 && i < 11) || i == 14 || i == 15 || i >= 18;       // s empty, p full, o empty, piece done, flags, joint
         mbar_init(bars + 8u * tid, four ? 4 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -189,7 +152,10 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
     }
     grid_dependency_wait();                    // lengths, queries and the drafts' keys come from the kernels before
     tree_find_run(p.w, part, run);
-    if (tid == 0) reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x].last_cta = -1;
+    if (tid == 0) {
+        reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x].last_cta = -1;
+        tree_front(p.scratch)[blockIdx.x] = run->begin < run->end && !run->at.item_begins();
+    }
     const uint32_t tmem = *tmem_slot;          // (allocated before the barriers in tree_find_run)
     if (warp >= 4 && warp < 8) {               // the matrix of ones: 16 keys' worth, the same for every step
         tc_fence_after();
@@ -206,7 +172,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
     if (warp == 0 && n_tiles > 0) {
         tree_load_keys<DH, NS>(p, &map_k, &map_v, run, base, ring_full(0), ring_empty(0));
     } else if (warp == 3 && n_tiles > 0) {
-        tree_load_queries<DH, N, 32, T>(p, run, sp + Cfg::kOffQ, q_full(0), q_empty(0), lane);
+        tree_load_queries<DH, N, 32, T>(p, run, sp + Cfg::kOffQ, reinterpret_cast<uint32_t*>(sp + Cfg::kOffMask), piece_done(0), q_full(0), q_empty(0), lane);
     } else if (warp == 1 && n_tiles > 0) {
         // ---------------- the scores: S^T of the next tile as soon as its buffer has been read
         if (lane == 0) {
@@ -243,11 +209,12 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
             TreeCursor c = run->at;
             uint32_t piece = 0;
             bool ok = true, first = true;              // first: the tile opens its piece
+            uint32_t g = 0, round = 0;                 // buffer of the weights: t % 3, t / 3
             for (int t = 0; t < n_tiles; ++t, c.next(p.w)) {
                 const uint32_t seq = t == n_tiles - 1 ? 2u * n_tiles - 1u : 2u * t + 2u, b = piece & 1u;
-                const int slot = seq % NS, g = t & 1;
+                const int slot = seq % NS;
                 if (first && piece >= 2 && !mbar_poll(o_empty(b), ((piece >> 1) & 1u) ^ 1u)) { ok = false; break; }
-                if (!mbar_poll(p_full(g), (t >> 1) & 1u) || !mbar_poll(ring_full(slot), (seq / NS) & 1u)) { ok = false; break; }
+                if (!mbar_poll(p_full(g), round & 1u) || !mbar_poll(ring_full(slot), (seq / NS) & 1u)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t va = base + slot * Cfg::kTileBytes, pa = base + Cfg::kOffP + g * Cfg::kPBytes;
 #pragma unroll
@@ -260,6 +227,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                 for (int k = 0; k < kKeys / 16; ++k)
                     umma_f16_ta(tmem_l + b * N, tmem_1, smem_desc_weights(pa + k * 256), kIdescL, (!first || k > 0) ? 1u : 0u);
                 umma_commit(o_full(g));
+                if (++g == 3) { g = 0; ++round; }
                 first = c.item_ends();
                 if (first || t == n_tiles - 1) { umma_commit(out_full(b)); ++piece; }
             }
@@ -274,6 +242,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
         bool ok = true, opens = true;
         int q0 = 0, nq = 0;
         uint32_t piece = 0, checks = 0, joins = 0, cur = 0;      // cur: which copy of the references is in use
+        uint32_t pb = 0, round = 0;                              // buffer of the weights: t % 3, t / 3
         auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_poll(bar, parity)) != 0; };
         auto meet = [&]() -> bool {                              // the four warps
             __syncwarp();
@@ -285,6 +254,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
             if (opens) { q0 = c.first_query(p.w); nq = c.queries(p.w); }
             const int C = c.r.L - c.r.n;
             const uint32_t s_at = tmem_s + (uint32_t)(buf * N) + t_lane;
+            if (!wait_all(s_full(buf), (t >> 1) & 1u)) { ok = false; break; }
             uint64_t vis = ~0ull;                                // queries that see this key
             if ((c.kt + 1) * kKeys > C) {                        // drafts in the tile, or its end
                 const int key = c.kt * kKeys + me, j = key - C;
@@ -292,79 +262,93 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                     vis = 0;
                     if (key < c.r.L) {
                         const int tok0 = q0 / p.w.group, n_tok = (q0 + nq - 1) / p.w.group - tok0 + 1;
-                        for (int i0 = 0; i0 < n_tok; i0 += 8) {  // eight drafts' mask words in flight
-                            uint32_t word[8];
-#pragma unroll
-                            for (int u = 0; u < 8; ++u) {
-                                word[u] = 0;
-                                if (p.tree_mask && i0 + u < n_tok && j < 32 * p.mask_words)
-                                    word[u] = __ldg(p.tree_mask + (size_t)(c.r.row0 + tok0 + i0 + u) * p.mask_words + (j >> 5)) >> (j & 31);
+                        // (the masks came with the queries of this piece, whose scores have been seen: they are there)
+                        const uint32_t* near = reinterpret_cast<const uint32_t*>(sp + Cfg::kOffMask) + (piece & 1u) * N * kMaskWords + (j >> 5);
+                        for (int i = 0; i < n_tok; ++i) {
+                            const int tok = tok0 + i, at = tok * p.w.group - q0;               // the draft's first query, from the tile's start
+                            uint32_t sees = j <= tok;
+                            if (p.tree_mask) {
+                                sees = 0;
+                                if (j < 32 * kMaskWords) sees = near[i * kMaskWords] >> (j & 31);
+                                else if (j < 32 * p.mask_words) sees = __ldg(p.tree_mask + (size_t)(c.r.row0 + tok) * p.mask_words + (j >> 5)) >> (j & 31);
                             }
-#pragma unroll
-                            for (int u = 0; u < 8; ++u) {
-                                const int tok = tok0 + i0 + u, at = tok * p.w.group - q0;      // the draft's first query, from the tile's start
-                                if (i0 + u >= n_tok || !(p.tree_mask ? word[u] & 1u : j <= tok)) continue;
-                                const int lo = max(at, 0), hi = min(at + p.w.group, N);
-                                vis |= (hi - lo >= 64 ? ~0ull : ((1ull << (hi - lo)) - 1ull)) << lo;
-                            }
+                            if (!(sees & 1u)) continue;
+                            const int lo = max(at, 0), hi = min(at + p.w.group, N);
+                            vis |= (hi - lo >= 64 ? ~0ull : ((1ull << (hi - lo)) - 1ull)) << lo;
                         }
                     }
                 }
                 const uint32_t vseq = t == n_tiles - 1 ? 2u * n_tiles - 1u : 2u * t + 2u;
-                if (!wait_all(s_full(buf), (t >> 1) & 1u) || !wait_all(ring_full(vseq % NS), (vseq / NS) & 1u)) { ok = false; break; }
+                // the V tile's slot was last used at least two tiles ago: behind that product, only this tile's phase is open
+                if (t >= 2 && !wait_all(o_full(pb == 2 ? 0 : pb + 1), (pb == 2 ? round : round - 1u) & 1u)) { ok = false; break; }
+                if (!wait_all(ring_full(vseq % NS), (vseq / NS) & 1u)) { ok = false; break; }
                 if (tree_clean_values<DH, Ops::kExpMask>(sp + (vseq % NS) * Cfg::kTileBytes, max(C - c.kt * kKeys, 0), c.r.L - c.kt * kKeys, me))
                     odd_piece[piece & 3u] = piece + 1;
-            } else if (!wait_all(s_full(buf), (t >> 1) & 1u)) { ok = false; break; }
+            }
             tc_fence_after();
-            uint32_t w[N / 2];
+            // Queries in chunks of 16; chunks without a live query are left out (their columns of P and O hold anything, a column
+            // of the products depends on its own column only).
+            // P^T goes into the buffer that the products three tiles ago have read
+            if (round > 0 && !wait_all(o_full(pb), (round & 1u) ^ 1u)) { ok = false; break; }
+            uint8_t* const pt = sp + Cfg::kOffP + pb * Cfg::kPBytes + me * 16;
             bool move = opens;
             if (!opens) {
                 // the weights as if no reference moved; whether one does, the warps find out meanwhile
-                uint32_t s[N];
-                float y[N], top = -INFINITY;
-                load_scores<N>(s_at, s);
-                tmem_ld_wait();
                 const float4* ref4 = reinterpret_cast<const float4*>(refs + cur * N);
+                float top = -INFINITY;
+                uint32_t s[N / 16][16];
 #pragma unroll
-                for (int n4 = 0; n4 < N / 4; ++n4) {
-                    const float4 r = ref4[n4];
-                    y[4 * n4] = fmaf(__uint_as_float(s[4 * n4]), p.scale_log2, -r.x);
-                    y[4 * n4 + 1] = fmaf(__uint_as_float(s[4 * n4 + 1]), p.scale_log2, -r.y);
-                    y[4 * n4 + 2] = fmaf(__uint_as_float(s[4 * n4 + 2]), p.scale_log2, -r.z);
-                    y[4 * n4 + 3] = fmaf(__uint_as_float(s[4 * n4 + 3]), p.scale_log2, -r.w);
-                }
-                if (vis != ~0ull) {
+                for (int k = 0; k < N / 16; ++k)
+                    if (16 * k < nq) load16(s_at + 16u * k, s[k]);
+                tmem_ld_wait();
 #pragma unroll
-                    for (int n = 0; n < N; ++n)
-                        if (!((vis >> n) & 1ull)) y[n] = -INFINITY;
-                }
+                for (int k = 0; k < N / 16; ++k)
+                    if (16 * k < nq) {
 #pragma unroll
-                for (int n = 0; n < N; ++n) top = fmaxf(top, y[n]);
+                        for (int e4 = 0; e4 < 4; ++e4) {
+                            const float4 r = ref4[4 * k + e4];
+                            const float ref[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[k][4 * e4 + e] = __float_as_uint(fmaf(__uint_as_float(s[k][4 * e4 + e]), p.scale_log2, -ref[e]));
+                        }
+                        if (vis != ~0ull) {
+                            const uint32_t seen = (uint32_t)(vis >> (16 * k));
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                if (!((seen >> e) & 1u)) s[k][e] = __float_as_uint(-INFINITY);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) top = fmaxf(top, __uint_as_float(s[k][e]));
+                    }
                 const bool any = __any_sync(0xffffffffu, top > Ops::kBias + kTreeSlack);
                 if (lane == 0) { flags[buf * 4 + quarter] = any; mbar_arrive(flag_bar); }
 #pragma unroll
-                for (int n = 0; n < N; n += 2) w[n / 2] = Ops::pack(tree_ex2(y[n]), tree_ex2(y[n + 1]));
+                for (int k = 0; k < N / 16; ++k)
+                    if (16 * k < nq) {
+                        uint32_t w[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) w[e] = Ops::pack(tree_ex2(__uint_as_float(s[k][2 * e])), tree_ex2(__uint_as_float(s[k][2 * e + 1])));
+                        *reinterpret_cast<uint4*>(pt + (2 * k) * (kKeys * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4*>(pt + (2 * k + 1) * (kKeys * 16)) = make_uint4(w[4], w[5], w[6], w[7]);
+                    }
                 if (!wait_all(flag_bar, checks & 1u)) { ok = false; break; }
                 ++checks;
                 move = (flags[buf * 4] | flags[buf * 4 + 1] | flags[buf * 4 + 2] | flags[buf * 4 + 3]) != 0;
-                if (!move) {                                     // the scores are no longer needed
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(s_empty(buf));
-                }
             }
             if (move) {
-                // maxima over the keys, new references, outputs and sums brought to them
-                uint32_t s[N];
-                float y[N];
-                load_scores<N>(s_at, s);
-                tmem_ld_wait();
+                // maxima over the keys, new references, outputs and sums brought to them (rare: chunk by chunk, few registers)
+#pragma unroll 1
+                for (int k = 0; 16 * k < nq; ++k) {
+                    const uint32_t seen = (uint32_t)(vis >> (16 * k));
+                    uint32_t s[16];
+                    load16(s_at + 16u * k, s);
+                    tmem_ld_wait();
+                    float v[16];
 #pragma unroll
-                for (int n = 0; n < N; ++n) y[n] = (vis >> n) & 1ull ? __uint_as_float(s[n]) * p.scale_log2 : -INFINITY;
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(s_empty(buf));
-                largest_into<N>(y, red, quarter);
+                    for (int e = 0; e < 16; ++e) v[e] = (seen >> e) & 1u ? __uint_as_float(s[e]) * p.scale_log2 : -INFINITY;
+                    const float r = largest16(v);
+                    if (!(lane & 1)) red[(16 * k + (lane >> 1)) * 4 + quarter] = r;
+                }
                 if (!meet()) { ok = false; break; }
                 const float* old_ref = refs + cur * N;
                 float* new_ref = refs + (cur ^ 1u) * N;
@@ -375,14 +359,15 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                 }
                 if (!meet()) { ok = false; break; }
                 if (!opens) {
-                    if (!wait_all(o_full(buf ^ 1), ((t - 1) >> 1) & 1u)) { ok = false; break; }         // the products before
+                    // the products before (buffer pb - 1, a round earlier where that is 2)
+                    if (!wait_all(o_full(pb ? pb - 1 : 2), (pb ? round : round - 1u) & 1u)) { ok = false; break; }
                     tc_fence_after();
 #pragma unroll 1
-                    for (int n0 = 0; n0 < N; n0 += 16) {
+                    for (int n0 = 0; n0 < nq; n0 += 16) {
                         uint32_t o[16], l[16];
                         const uint32_t at = (uint32_t)((piece & 1u) * N + n0) + t_lane;
-                        load_scores<16>(tmem_o + at, o);
-                        load_scores<16>(tmem_l + at, l);
+                        load16(tmem_o + at, o);
+                        load16(tmem_l + at, l);
                         tmem_ld_wait();
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
@@ -395,20 +380,34 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                     }
                     tmem_store_wait();
                 }
+                const float4* ref4 = reinterpret_cast<const float4*>(new_ref);
+#pragma unroll 1
+                for (int k = 0; 16 * k < nq; ++k) {
+                    const uint32_t seen = (uint32_t)(vis >> (16 * k));
+                    uint32_t s[16], w[8];
+                    load16(s_at + 16u * k, s);
+                    tmem_ld_wait();
 #pragma unroll
-                for (int n = 0; n < N; n += 2) w[n / 2] = Ops::pack(tree_ex2(y[n] - new_ref[n]), tree_ex2(y[n + 1] - new_ref[n + 1]));
+                    for (int e4 = 0; e4 < 4; ++e4) {
+                        const float4 r = ref4[4 * k + e4];
+                        const float ref[4] = {r.x, r.y, r.z, r.w};
+                        float v[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            v[e] = (seen >> (4 * e4 + e)) & 1u ? tree_ex2(fmaf(__uint_as_float(s[4 * e4 + e]), p.scale_log2, -ref[e])) : 0.0f;
+                        w[2 * e4] = Ops::pack(v[0], v[1]);
+                        w[2 * e4 + 1] = Ops::pack(v[2], v[3]);
+                    }
+                    *reinterpret_cast<uint4*>(pt + (2 * k) * (kKeys * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    *reinterpret_cast<uint4*>(pt + (2 * k + 1) * (kKeys * 16)) = make_uint4(w[4], w[5], w[6], w[7]);
+                }
                 cur ^= 1u;
             }
-            // P^T into the buffer that the products two tiles ago have read
-            if (t >= 2 && !wait_all(o_full(buf), ((t >> 1) & 1u) ^ 1u)) { ok = false; break; }
-            uint8_t* pt = sp + Cfg::kOffP + buf * Cfg::kPBytes + me * 16;
-#pragma unroll
-            for (int ch = 0; ch < N / 8; ++ch)
-                *reinterpret_cast<uint4*>(pt + ch * (kKeys * 16)) = make_uint4(w[4 * ch], w[4 * ch + 1], w[4 * ch + 2], w[4 * ch + 3]);
             fence_async_smem();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(p_full(buf));
+            if (lane == 0) { mbar_arrive(s_empty(buf)); mbar_arrive(p_full(pb)); }
+            if (++pb == 3) { pb = 0; ++round; }
             opens = c.item_ends();
             if (opens || t == n_tiles - 1) {
                 if (me < N) refs[(2 + (piece & 3u)) * N + me] = refs[cur * N + me];        // (a warp behind may still read the copy in use)
@@ -427,7 +426,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
         bool split_front = !c.item_begins(), ok = true;
         uint32_t piece = 0;
         int kt_first = c.kt;
-        auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_poll(bar, parity)) != 0; };
+        auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)) != 0; };
         for (int t = 0; t < n_tiles && ok; ++t) {
             const bool item_ends = c.item_ends();
             if (item_ends || t == n_tiles - 1) {
@@ -444,8 +443,8 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                 for (int n0 = 0; n0 < nq; n0 += 16) {
                     uint32_t o[16], l[16];
                     const uint32_t at = (uint32_t)((piece & 1u) * N + n0) + t_lane;
-                    load_scores<16>(tmem_o + at, o);
-                    load_scores<16>(tmem_l + at, l);
+                    load16(tmem_o + at, o);
+                    load16(tmem_l + at, l);
                     tmem_ld_wait();
                     if (repair) {                                // what the non-finite values of drafts add to this column
                         uint32_t last = 0xFFFFFFFFu;
@@ -493,7 +492,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                 if (lane == 0) mbar_arrive(o_empty(piece & 1u));
                 if (!item_ends && !split_front && me == 0) {     // begins here, goes on in the next CTAs
                     TreeTail tl{};
-                    tl.last_cta = tree_cta_of(run->end + (c.r.n_kt - 1 - c.kt) - 1, run->total, run->ctas);
+                    tl.last_cta = run->tail_cta;
                     tl.queries = nq; tl.row0 = c.r.row0; tl.q0 = q0; tl.h = c.h;
                     reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x] = tl;
                 }

@@ -39,7 +39,7 @@ template <int DH> struct TcCfg {
     static constexpr int kOffX = kOffRing + kStages * kTileBytes;           // (reference, sum) of every row: [2 groups][128][2]
     static constexpr int kOffBar = kOffX + 2048;
     static constexpr int kOffMisc = kOffBar + (2 * kStages + 13) * 8;       // TMEM base, non-finite marks, run
-    static constexpr int kUsedBytes = kOffMisc + 32 + 96 + (int)sizeof(TreeRun);
+    static constexpr int kUsedBytes = kOffMisc + 32 + 192 + (int)sizeof(TreeRun);
     static constexpr int kSmemBytes = kUsedBytes + 1024 > 232448 ? 232448 : kUsedBytes + 1024;
     static_assert(kUsedBytes <= 232448, "shared memory");
 };
@@ -57,7 +57,10 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if ((base - raw) + (uint32_t)Cfg::kUsedBytes > p.smem_bytes) {           // uniform: nothing has been set up yet
         if (tid == 0) atomicExch(p.w.err_flag, kErrTreeWait);
-        if (tid == 0) reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x].last_cta = -1;
+        if (tid == 0) {
+            reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x].last_cta = -1;
+            tree_front(p.scratch)[blockIdx.x] = 0;
+        }
         return;
     }
     const uint32_t bars = base + Cfg::kOffBar;
@@ -73,7 +76,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc);
     volatile uint32_t* odd_piece = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 8);   // [2]: piece + 1 with a non-finite draft value
     long long* part = reinterpret_cast<long long*>(sp + Cfg::kOffMisc + 32);
-    TreeRun* run = reinterpret_cast<TreeRun*>(sp + Cfg::kOffMisc + 32 + 96);
+    TreeRun* run = reinterpret_cast<TreeRun*>(sp + Cfg::kOffMisc + 32 + 192);
 
     if (tid < 2 * NS + 13) {
         const int i = tid - 2 * NS;              // one barrier a thread: ring full, ring empty; q full, q empty, s full, p full, o full, o empty, x full
@@ -88,7 +91,10 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     }
     grid_dependency_wait();                    // lengths, queries and the drafts' keys come from the kernels before
     tree_find_run(p.w, part, run);
-    if (tid == 0) reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x].last_cta = -1;
+    if (tid == 0) {
+        reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x].last_cta = -1;
+        tree_front(p.scratch)[blockIdx.x] = run->begin < run->end && !run->at.item_begins();
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -99,7 +105,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     if (warp == 0 && n_tiles > 0) {
         tree_load_keys<DH, NS>(p, &map_k, &map_v, run, base + Cfg::kOffRing, ring_full(0), ring_empty(0));
     } else if ((warp == 2 || warp == 3) && n_tiles > 0) {
-        tree_load_queries<DH, kRows, 64, T>(p, run, sp, q_full(0), q_empty(0), tid - 64);
+        tree_load_queries<DH, kRows, 64, T>(p, run, sp, nullptr, 0u, q_full(0), q_empty(0), tid - 64);
     } else if (warp == 1 && n_tiles > 0) {
         // ---------------- MMA issuer
         if (lane == 0) {
@@ -355,7 +361,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 }
                 if (!item_ends && !split_front && tid == 128) {  // begins here, goes on in the next CTAs
                     TreeTail tl{};
-                    tl.last_cta = tree_cta_of(run->end + (c.r.n_kt - 1 - c.kt) - 1, run->total, run->ctas);
+                    tl.last_cta = run->tail_cta;
                     tl.queries = nq; tl.row0 = c.r.row0; tl.q0 = q0; tl.h = c.h;
                     reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x] = tl;
                 }
@@ -435,7 +441,7 @@ int launch_tree_attention_tc(const TreeAttnArgs& a, cudaStream_t s, bool depende
     const long long want = a.rows <= a.batch ? group : (3 * drafts + 2 * a.batch - 1) / (2 * a.batch);     // 1.5 x the average
     const int nq = want <= 16 ? 16 : (want <= 32 ? 32 : (want <= 64 ? 64 : kRows));
     p.w = TreeWork{a.kv_len, a.row_start, a.block_table, a.batch, a.rows, a.n_heads, a.cache.n_kv_heads, a.max_pages, a.cache.page_size,
-                   group, nq, kKeys, a.err_flag};
+                   group, nq, kKeys, 2, a.err_flag};
     p.q = a.q; p.q_stride = a.q_stride;
     p.box_keys = a.cache.page_size < kKeys ? a.cache.page_size : kKeys;
     p.n_pages = a.cache.n_pages; p.mask_words = a.mask_words; p.tree_mask = a.tree_mask;

@@ -7,6 +7,7 @@
 namespace zq {
 
 constexpr int kKeys = 128;           // keys per tile
+constexpr int kMaskWords = 4;        // words of a draft's mask that travel with its query tile (trees of up to 128 drafts)
 constexpr float kTreeSlack = 8.0f;   // a reference may lag the maximum by up to 2^8
 
 struct TcParams {
@@ -109,7 +110,7 @@ __device__ __forceinline__ void tree_load_keys(const TcParams& p, const CUtensor
     };
     auto fetch = [&](const CUtensorMap* map, const Box& x) -> bool {
         const int slot = seq % NS;
-        if (!__all_sync(0xffffffffu, mbar_poll(empty + 8u * slot, ((seq / NS) & 1u) ^ 1u))) return false;
+        if (!__all_sync(0xffffffffu, mbar_wait(empty + 8u * slot, ((seq / NS) & 1u) ^ 1u))) return false;
         if (lane == 0) mbar_arrive_expect_tx(full + 8u * slot, (uint32_t)x.live * box_bytes);
         __syncwarp();
         if (x.mine) {
@@ -138,11 +139,15 @@ __device__ __forceinline__ void tree_load_keys(const TcParams& p, const CUtensor
         if (!mbar_wait(full + 8u * (k % NS), (k / NS) & 1u)) break;
 }
 
-// Query tiles, by THREADS threads (whole warps; `lane`: which of them), a piece ahead of the products: rows of 128 bytes, 128-byte swizzle, [half][NQ rows].
-// Rows behind the tile's last query keep what they hold; their results are not used.  full counts one arrival per warp.
+// Query tiles, by THREADS threads (whole warps; `lane`: which of them), a piece ahead of the products: rows of 128 bytes, 128-byte
+// swizzle, [half][NQ rows].  Rows behind the tile's last query keep what they hold; their results are not used.  full counts one
+// arrival per warp.  masks (may be NULL): [2][NQ][kMaskWords], the first words of the drafts' masks, draft by draft; done: four
+// barriers, by piece modulo 4, after which a piece's masks are no longer read.
 template <int DH, int NQ, int THREADS, typename T>
-__device__ __forceinline__ void tree_load_queries(const TcParams& p, const TreeRun* run, uint8_t* q_tiles, uint32_t full, uint32_t empty, int lane) {
-    constexpr int kChunks = DH / 8, kTileBytes = NQ * DH * 2;
+__device__ __forceinline__ void tree_load_queries(const TcParams& p, const TreeRun* run, uint8_t* q_tiles, uint32_t* masks, uint32_t done, uint32_t full,
+                                                  uint32_t empty, int lane) {
+    constexpr int kChunks = DH / 8, kTileBytes = NQ * DH * 2, kRowsPer = THREADS / kChunks, kFly = NQ / kRowsPer < 8 ? NQ / kRowsPer : 8;
+    const int ch = lane % kChunks;               // a thread copies its 16 bytes of every kRowsPer-th row, kFly rows in flight
     const int n_tiles = (int)(run->end - run->begin);
     TreeCursor c = run->at;
     uint32_t piece = 0;
@@ -150,23 +155,33 @@ __device__ __forceinline__ void tree_load_queries(const TcParams& p, const TreeR
         if (t != 0 && !c.item_begins()) continue;
         const uint32_t b = piece & 1u;
         if (!__all_sync(0xffffffffu, mbar_wait(empty + 8u * b, ((piece >> 1) & 1u) ^ 1u))) { atomicExch(p.w.err_flag, kErrTreeWait); return; }
-        const int q0 = c.first_query(p.w), n = c.queries(p.w) * kChunks;
-        uint8_t* dst = q_tiles + b * kTileBytes;
-        const T* base = static_cast<const T*>(p.q) + (int64_t)c.r.row0 * p.q_stride + (int64_t)c.h * p.w.group * DH;
-        for (int x0 = lane; x0 < n; x0 += 4 * THREADS) {
-            uint4 w[4];
+        const int q0 = c.first_query(p.w), nq = c.queries(p.w);
+        const T* base = static_cast<const T*>(p.q) + (int64_t)c.r.row0 * p.q_stride + (int64_t)c.h * p.w.group * DH + 8 * ch;
+        uint8_t* dst = q_tiles + b * kTileBytes + (ch >> 3) * (NQ * 128);
+        for (int r0 = lane / kChunks; r0 < nq; r0 += kFly * kRowsPer) {
+            uint4 w[kFly];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int x = x0 + THREADS * u, r = x / kChunks;
-                if (x < n) {
+            for (int u = 0; u < kFly; ++u) {
+                const int r = r0 + u * kRowsPer;
+                if (r < nq) {
                     const int tok = (q0 + r) / p.w.group, hg = q0 + r - tok * p.w.group;
-                    w[u] = __ldg(reinterpret_cast<const uint4*>(base + (int64_t)tok * p.q_stride + (int64_t)hg * DH) + x % kChunks);
+                    w[u] = __ldg(reinterpret_cast<const uint4*>(base + (int64_t)tok * p.q_stride + (int64_t)hg * DH));
                 }
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int x = x0 + THREADS * u, r = x / kChunks, ch = x % kChunks;
-                if (x < n) *reinterpret_cast<uint4*>(dst + (ch >> 3) * (NQ * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = w[u];
+            for (int u = 0; u < kFly; ++u) {
+                const int r = r0 + u * kRowsPer;
+                if (r < nq) *reinterpret_cast<uint4*>(dst + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = w[u];
+            }
+        }
+        if (masks && p.tree_mask) {
+            const int tok0 = q0 / p.w.group, n_tok = (q0 + nq - 1) / p.w.group - tok0 + 1;
+            uint32_t* to = masks + b * NQ * kMaskWords;
+            const uint32_t old = piece - 2u;                     // the piece whose masks lie there
+            if (piece >= 2 && !__all_sync(0xffffffffu, mbar_wait(done + 8u * (old & 3u), (old >> 2) & 1u))) { atomicExch(p.w.err_flag, kErrTreeWait); return; }
+            for (int x = lane; x < n_tok * kMaskWords; x += THREADS) {
+                const int i = x / kMaskWords, k = x % kMaskWords;
+                to[x] = k < p.mask_words ? __ldg(p.tree_mask + (size_t)(c.r.row0 + tok0 + i) * p.mask_words + k) : 0u;
             }
         }
         fence_async_smem();

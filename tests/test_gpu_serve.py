@@ -320,6 +320,15 @@ ATTENTION = [
     ("bf16", 14, 2, 64, 32, "joint", [300, 129, 0, 4], [1, 2, 5, 1], "tree"),   # tiles that cut a draft's heads apart
     ("f16", 7, 1, 128, 16, "token", [300, 129, 0, 4], [3, 2, 5, 30], "random"),
     ("bf16", 2, 2, 128, 16, "token", [4000] * 9, [1] * 9, None),
+    # long runs of tiles for every tile width of the tensor-core kernels (16, 32, 64 and 128 queries)
+    ("bf16", 16, 4, 128, 64, "token", [5000, 20011, 9000, 16], [1, 1, 1, 1], "tree"),
+    ("bf16", 16, 4, 128, 64, "token", [5000, 20011, 9000, 16], [4, 4, 4, 4], "tree"),
+    ("f16", 16, 4, 64, 16, "head", [5000, 20011, 9000, 16], [4, 4, 4, 4], "tree"),
+    ("f16", 16, 4, 128, 64, "token", [5000, 20011, 9000, 16], [8, 8, 8, 8], "tree"),
+    ("bf16", 16, 4, 64, 16, "head", [5000, 20011, 9000, 16], [8, 9, 8, 8], "tree"),
+    ("bf16", 16, 4, 128, 16, "token", [5000, 20011, 9000, 16], [40, 33, 64, 20], "tree"),
+    ("f16", 16, 4, 64, 256, "joint", [5000, 20011, 9000, 16], [40, 33, 64, 20], "tree"),
+    ("f32", 16, 4, 128, 64, "token", [5000, 8011, 900, 16], [1, 2, 3, 1], "tree"),
 ]
 
 
