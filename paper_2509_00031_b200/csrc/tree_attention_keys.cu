@@ -286,51 +286,58 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                     odd_piece[piece & 3u] = piece + 1;
             }
             tc_fence_after();
-            // Queries in chunks of 16; chunks without a live query are left out (their columns of P and O hold anything, a column
-            // of the products depends on its own column only).
+            // Queries in chunks; those without a live query are left out (their columns of P and O hold anything, a column of the
+            // products depends on its own column only).  The chunks are a loop on purpose: unrolled for 64 queries the steady
+            // state no longer fits the schedulers' instruction caches (measured: 20 cycles per query and tile instead of 8).
             // P^T goes into the buffer that the products three tiles ago have read
             if (round > 0 && !wait_all(o_full(pb), (round & 1u) ^ 1u)) { ok = false; break; }
             uint8_t* const pt = sp + Cfg::kOffP + pb * Cfg::kPBytes + me * 16;
             bool move = opens;
             if (!opens) {
-                // the weights as if no reference moved; whether one does, the warps find out meanwhile
+                // the weights as if no reference moved; whether one does, the warps then tell one another
+                constexpr int CH = N == 16 ? 1 : 2;              // chunks of 16 or 32
                 const float4* ref4 = reinterpret_cast<const float4*>(refs + cur * N);
-                float top = -INFINITY;
-                uint32_t s[N / 16][16];
+                float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+                for (int n0 = 0; n0 < nq; n0 += 16 * CH) {
+                    uint32_t s[CH][16];
 #pragma unroll
-                for (int k = 0; k < N / 16; ++k)
-                    if (16 * k < nq) load16(s_at + 16u * k, s[k]);
-                tmem_ld_wait();
+                    for (int k = 0; k < CH; ++k) load16(s_at + (uint32_t)(n0 + 16 * k), s[k]);
+                    float4 r[4 * CH];
 #pragma unroll
-                for (int k = 0; k < N / 16; ++k)
-                    if (16 * k < nq) {
+                    for (int i = 0; i < 4 * CH; ++i) r[i] = ref4[(n0 >> 2) + i];
+                    tmem_ld_wait();
 #pragma unroll
-                        for (int e4 = 0; e4 < 4; ++e4) {
-                            const float4 r = ref4[4 * k + e4];
-                            const float ref[4] = {r.x, r.y, r.z, r.w};
+                    for (int i = 0; i < 4 * CH; ++i) {
+                        const float ref[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) s[k][4 * e4 + e] = __float_as_uint(fmaf(__uint_as_float(s[k][4 * e4 + e]), p.scale_log2, -ref[e]));
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t& x = s[i >> 2][4 * (i & 3) + e];
+                            x = __float_as_uint(fmaf(__uint_as_float(x), p.scale_log2, -ref[e]));
                         }
-                        if (vis != ~0ull) {
-                            const uint32_t seen = (uint32_t)(vis >> (16 * k));
-#pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                if (!((seen >> e) & 1u)) s[k][e] = __float_as_uint(-INFINITY);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) top = fmaxf(top, __uint_as_float(s[k][e]));
                     }
+                    if (vis != ~0ull) {
+                        const uint32_t seen = (uint32_t)(vis >> n0);
+#pragma unroll
+                        for (int e = 0; e < 16 * CH; ++e)
+                            if (!((seen >> e) & 1u)) s[e >> 4][e & 15] = __float_as_uint(-INFINITY);
+                    }
+                    uint8_t* at = pt + (n0 >> 3) * (kKeys * 16);
+#pragma unroll
+                    for (int k = 0; k < 2 * CH; ++k) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float a = __uint_as_float(s[k >> 1][8 * (k & 1) + 2 * e]), b = __uint_as_float(s[k >> 1][8 * (k & 1) + 2 * e + 1]);
+                            top4[e] = fmaxf(top4[e], fmaxf(a, b));
+                            w[e] = Ops::pack(tree_ex2(a), tree_ex2(b));
+                        }
+                        *reinterpret_cast<uint4*>(at + k * (kKeys * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+                const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
                 const bool any = __any_sync(0xffffffffu, top > Ops::kBias + kTreeSlack);
                 if (lane == 0) { flags[buf * 4 + quarter] = any; mbar_arrive(flag_bar); }
-#pragma unroll
-                for (int k = 0; k < N / 16; ++k)
-                    if (16 * k < nq) {
-                        uint32_t w[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) w[e] = Ops::pack(tree_ex2(__uint_as_float(s[k][2 * e])), tree_ex2(__uint_as_float(s[k][2 * e + 1])));
-                        *reinterpret_cast<uint4*>(pt + (2 * k) * (kKeys * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
-                        *reinterpret_cast<uint4*>(pt + (2 * k + 1) * (kKeys * 16)) = make_uint4(w[4], w[5], w[6], w[7]);
-                    }
                 if (!wait_all(flag_bar, checks & 1u)) { ok = false; break; }
                 ++checks;
                 move = (flags[buf * 4] | flags[buf * 4 + 1] | flags[buf * 4 + 2] | flags[buf * 4 + 3]) != 0;
@@ -380,7 +387,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                     }
                     tmem_store_wait();
                 }
-                const float4* ref4 = reinterpret_cast<const float4*>(new_ref);
+                const float4* moved = reinterpret_cast<const float4*>(new_ref);
 #pragma unroll 1
                 for (int k = 0; 16 * k < nq; ++k) {
                     const uint32_t seen = (uint32_t)(vis >> (16 * k));
@@ -389,7 +396,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                     tmem_ld_wait();
 #pragma unroll
                     for (int e4 = 0; e4 < 4; ++e4) {
-                        const float4 r = ref4[4 * k + e4];
+                        const float4 r = moved[4 * k + e4];
                         const float ref[4] = {r.x, r.y, r.z, r.w};
                         float v[4];
 #pragma unroll
