@@ -204,27 +204,27 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                         odd_piece[piece & 1u] = piece + 1;
                 }
                 if (warp_live) {
-                    uint32_t s0[32], s1[32], s2[32], s3[32];     // (one array each: together they would leave the registers)
-                    tmem_ld32(ts, s0); tmem_ld32(ts + 32u, s1); tmem_ld32(ts + 64u, s2); tmem_ld32(ts + 96u, s3);
-                    tmem_ld_wait();
-                    if (tail) {
-                        auto hide = [&](uint32_t (&s)[32], int q) {
-                            const uint32_t vis = row < nq ? visible_word(c.kt * kKeys + 32 * q, C, c.r.n, tok, mask, p.mask_words) : 0u;
+                    // Two passes over the scores, which stay in TMEM, in chunks of 32 columns.  Loops on purpose: unrolled, the
+                    // steady state does not fit the schedulers' instruction caches.
+                    auto fetch = [&](int q, uint32_t (&s)[32]) {
+                        tmem_ld32(ts + 32u * q, s);
+                        const uint32_t vis = !tail ? 0xFFFFFFFFu : (row < nq ? visible_word(c.kt * kKeys + 32 * q, C, c.r.n, tok, mask, p.mask_words) : 0u);
+                        tmem_ld_wait();
+                        if (tail) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
                                 if (!((vis >> e) & 1u)) s[e] = __float_as_uint(-INFINITY);
-                        };
-                        hide(s0, 0); hide(s1, 1); hide(s2, 2); hide(s3, 3);
-                    }
-                    float t8[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) t8[e] = -INFINITY;
-                    auto largest = [&](const uint32_t (&s)[32]) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) t8[e & 7] = fmaxf(t8[e & 7], __uint_as_float(s[e]));
+                        }
                     };
-                    largest(s0); largest(s1); largest(s2); largest(s3);
-                    float mx = fmaxf(fmaxf(fmaxf(t8[0], t8[1]), fmaxf(t8[2], t8[3])), fmaxf(fmaxf(t8[4], t8[5]), fmaxf(t8[6], t8[7])));
+                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t s[32];
+                        fetch(q, s);
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) t4[(e >> 1) & 3] = fmaxf(t4[(e >> 1) & 3], fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
+                    }
+                    float mx = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
                     mx = mx * p.scale_log2 - Ops::kBias;         // weights 2^(score - reference): the largest is 2^kBias .. 2^(kBias + 8)
                     if (t - first < 2) {
                         m_ref = mx;                              // the group's first tile of the piece
@@ -252,20 +252,19 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                     }
                     const float ref = m_ref == -INFINITY ? 0.0f : m_ref;     // nothing seen yet: every weight is 0
                     float sum4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                    auto weigh = [&](const uint32_t (&sa)[32], const uint32_t (&sb)[32], uint32_t at) {
-                        uint32_t w[32];
+#pragma unroll 1
+                    for (int q = 0; q < 4; ++q) {                // the weights go over scores that have been read
+                        uint32_t s[32], w[16];
+                        fetch(q, s);
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            const float a = tree_ex2(fmaf(__uint_as_float(sa[2 * e]), p.scale_log2, -ref)), b = tree_ex2(fmaf(__uint_as_float(sa[2 * e + 1]), p.scale_log2, -ref));
-                            const float c2 = tree_ex2(fmaf(__uint_as_float(sb[2 * e]), p.scale_log2, -ref)), d = tree_ex2(fmaf(__uint_as_float(sb[2 * e + 1]), p.scale_log2, -ref));
-                            sum4[0] += a; sum4[1] += b; sum4[2] += c2; sum4[3] += d;
+                            const float a = tree_ex2(fmaf(__uint_as_float(s[2 * e]), p.scale_log2, -ref)), b = tree_ex2(fmaf(__uint_as_float(s[2 * e + 1]), p.scale_log2, -ref));
+                            sum4[(2 * e) & 3] += a;
+                            sum4[(2 * e + 1) & 3] += b;
                             w[e] = Ops::pack(a, b);
-                            w[16 + e] = Ops::pack(c2, d);
                         }
-                        tmem_store32(at, w);
-                    };
-                    weigh(s0, s1, ts);
-                    weigh(s2, s3, ts + 32u);
+                        store16(ts + 16u * q, w);
+                    }
                     tmem_store_wait();
                     l_run += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
                 }
@@ -441,7 +440,7 @@ int launch_tree_attention_tc(const TreeAttnArgs& a, cudaStream_t s, bool depende
     const long long want = a.rows <= a.batch ? group : (3 * drafts + 2 * a.batch - 1) / (2 * a.batch);     // 1.5 x the average
     const int nq = want <= 16 ? 16 : (want <= 32 ? 32 : (want <= 64 ? 64 : kRows));
     p.w = TreeWork{a.kv_len, a.row_start, a.block_table, a.batch, a.rows, a.n_heads, a.cache.n_kv_heads, a.max_pages, a.cache.page_size,
-                   group, nq, kKeys, 2, a.err_flag};
+                   group, nq, kKeys, 4, a.err_flag};
     p.q = a.q; p.q_stride = a.q_stride;
     p.box_keys = a.cache.page_size < kKeys ? a.cache.page_size : kKeys;
     p.n_pages = a.cache.n_pages; p.mask_words = a.mask_words; p.tree_mask = a.tree_mask;
