@@ -149,8 +149,8 @@ __device__ __forceinline__ void tree_find_run(const TreeWork& w, long long* part
 // ---- partial results ------------------------------------------------------------------------------------------------
 // One descriptor per CTA, a word that says whether its front slot is in use, then 2 * G slots of [tile_rows] references, [tile_rows] sums and [tile_rows][d_head] outputs (fp32).
 struct TreeTail { int last_cta, queries, row0, q0, h, pad[3]; };   // an item that begins in this CTA and ends in last_cta; -1: none
-constexpr int kMaxTreeGrid = 148;                        // one CTA per SM
-constexpr size_t kTailBytes = 8192, kFrontOffset = kMaxTreeGrid * sizeof(TreeTail);
+constexpr int kMaxTreeGrid = 2 * 148;                    // one or two CTAs per SM
+constexpr size_t kTailBytes = 12288, kFrontOffset = kMaxTreeGrid * sizeof(TreeTail);
 static_assert(kFrontOffset + kMaxTreeGrid * sizeof(int) <= kTailBytes, "descriptors");
 
 __host__ __device__ inline size_t tree_slot_floats(int tile_rows, int dh) { return (size_t)tile_rows * (dh + 2); }
