@@ -732,6 +732,30 @@ typedef struct zoqat_logit_rules {
 int zoqat_op_logit_rules(const void* logits_dev, int type, int64_t ld, int rows, int vocab, const zoqat_logit_rules_t* rules,
                          void* out_dev, int64_t out_ld, int32_t* token_dev, void* stream);
 
+/* A step of drafted tokens through a packed model: zoqat_decode_step for requests of different lengths, with their keys and values
+ * in pages.  The step's plan (zoqat_op_cache_plan's outputs, device memory): */
+typedef struct zoqat_tree_batch {
+    const int32_t*  block_table;   /* [batch, max_pages]                                                      */
+    const int32_t*  kv_len;        /* [batch]                                                                 */
+    const int32_t*  row_start;     /* [batch + 1]                                                             */
+    const int32_t*  row_pos;       /* [rows], < max_seq of the model                                          */
+    const int32_t*  slot;          /* [rows]                                                                  */
+    const uint32_t* tree_mask;     /* [rows, mask_words], or NULL: each draft follows the one before it        */
+    int32_t batch, max_pages, mask_words, reserved;
+} zoqat_tree_batch_t;
+
+/* Feeds tokens_dev[rows] (rows in {1, 2, 4, 8}; of all requests, back to back; rows behind the last are padding) through the
+ * model and writes logits_dev fp32 [rows, vocab] - row r's prediction of the token after it - and / or next_token_dev int32
+ * [rows]: the greedy choice, under `rules` (zoqat_op_logit_rules, applied to the logits in place) unless that is NULL.
+ * caches: n_layers descriptions (host memory, read before the call returns), n_kv_heads = n_heads, any type; the rows' keys and values
+ * are written before they are attended to.  Needs zoqat_decode_begin (its batch is the most rows that may leave logits_dev
+ * NULL; the cache it lays out is not used).  scratch_dev as for zoqat_op_tree_attention.  Logits of padding rows are unspecified.
+ * What the device finds wrong in plan or pages is reported by zoqat_check() as ZOQAT_ERR_INVALID_ARG.  Asynchronous, no host
+ * synchronisation; can be captured in a CUDA graph. */
+int zoqat_decode_tree_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows, const zoqat_tree_batch_t* plan,
+                           const zoqat_paged_cache_t* caches, const zoqat_logit_rules_t* rules, float* logits_dev,
+                           int32_t* next_token_dev, void* scratch_dev, size_t scratch_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

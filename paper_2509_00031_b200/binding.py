@@ -40,7 +40,7 @@ EXPORTS = [
     "zoqat_op_head_loss", "zoqat_op_head_loss_static",
     "zoqat_decode_bytes", "zoqat_decode_begin", "zoqat_decode_step", "zoqat_op_decode_gemv",
     "zoqat_op_cache_plan", "zoqat_op_cache_append", "zoqat_op_tree_attention_scratch_bytes", "zoqat_op_tree_attention",
-    "zoqat_op_logit_rules",
+    "zoqat_op_logit_rules", "zoqat_decode_tree_step",
 ]
 
 
@@ -65,6 +65,11 @@ class PagedCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + [(n, ctypes.c_int32) for n in (
         "type", "n_pages", "page_size", "n_kv_heads", "d_head", "reserved")] + [(n, ctypes.c_int64) for n in (
             "page_stride", "slot_stride", "head_stride")]
+
+
+class TreeBatch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("block_table", "kv_len", "row_start", "row_pos", "slot", "tree_mask")] + [
+        (n, ctypes.c_int32) for n in ("batch", "max_pages", "mask_words", "reserved")]
 
 
 class LogitRulesDesc(ctypes.Structure):
@@ -163,6 +168,7 @@ def lib():
             "zoqat_op_cache_append": [vp, i64, vp, vp, i32, i32, vp, vp, i32, P(PagedCache), vp, i64, vp, vp],
             "zoqat_op_tree_attention_scratch_bytes": [i32, i32, P(sz)],
             "zoqat_op_tree_attention": [vp, i64, P(PagedCache), vp, i32, vp, vp, vp, i32, i32, i32, i32, f32, vp, i64, vp, sz, vp, vp],
+            "zoqat_decode_tree_step": [vp, vp, i32, P(TreeBatch), P(PagedCache), P(LogitRulesDesc), vp, vp, vp, sz, vp],
             "zoqat_op_logit_rules": [vp, i32, i64, i32, i32, P(LogitRulesDesc), vp, i64, vp, vp],
         }
         for name, args in sigs.items():
@@ -739,6 +745,35 @@ class ZoqatModel:
         if next_token is None:
             next_token = torch.empty(self.decode_batch, dtype=torch.int32, device="cuda")
         _check(lib().zoqat_decode_step(self.handle, _p(tokens), pos, _p(logits), _p(next_token), _stream()))
+        return logits, next_token
+
+    def zoqat_decode_tree_step(self, tokens, plan, block_table, caches, rules=None, logits=None, next_token=None, scratch=None):
+        """tokens int32 [rows] (1, 2, 4 or 8) at the rows of `plan` (the dict of zoqat_op_cache_plan); caches: (k, v) per layer, each
+        [n_pages, page_size, n_heads, d_head]; rules: LogitRules or None.  Returns (logits [rows, vocab], next_token [rows])."""
+        dev, stream = _here()
+        rows, batch = tokens.shape[0], plan["kv_len"].shape[0]
+        mask = plan.get("tree_mask")
+        if len(caches) != self.shape["n_layers"]:
+            _refuse("caches: one pair per layer is needed")
+        if plan["row_pos"].shape[0] < rows or plan["slot"].shape[0] < rows or (mask is not None and mask.shape[0] < rows) or (
+                rules is not None and (rules.max_rows < rows or rules.dev != dev)):
+            _refuse("the plan or the rules have too few rows")
+        tb = TreeBatch(_flat(dev, "block_table", block_table, _I32, batch, -1), _flat(dev, "kv_len", plan["kv_len"], _I32, batch),
+                       _flat(dev, "row_start", plan["row_start"], _I32, batch + 1), _flat(dev, "row_pos", plan["row_pos"], _I32, -1),
+                       _flat(dev, "slot", plan["slot"], _I32, -1), _flat(dev, "tree_mask", mask, _I32, -1, -1), batch, block_table.shape[1],
+                       mask.shape[1] if mask is not None else 0, 0)
+        descs = (PagedCache * len(caches))(*[_caches(dev, k, v) for k, v in caches])
+        if logits is None:
+            logits = torch.empty((rows, self.shape["vocab"]), dtype=torch.float32, device=tokens.device)
+        if next_token is None:
+            next_token = torch.empty(rows, dtype=torch.int32, device=tokens.device)
+        if scratch is None:
+            nb = ctypes.c_size_t()
+            _check(lib().zoqat_op_tree_attention_scratch_bytes(descs[0].type, descs[0].d_head, ctypes.byref(nb)))
+            scratch = torch.empty(nb.value, dtype=torch.uint8, device=tokens.device)
+        _check(lib().zoqat_decode_tree_step(self.handle, _flat(dev, "tokens", tokens, _I32, rows), rows, tb, descs, rules.desc if rules is not None else None,
+                                            _flat(dev, "logits", logits, _F32, rows, self.shape["vocab"]), _flat(dev, "next_token", next_token, _I32, rows),
+                                            scratch.data_ptr(), scratch.numel() * scratch.element_size(), stream))
         return logits, next_token
 
     def zoqat_init_qparams(self):

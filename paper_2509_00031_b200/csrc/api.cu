@@ -1158,6 +1158,9 @@ int zoqat_check(zoqat_model_t* m, void* stream) {
     if (flag != 0) {
         cudaMemsetAsync(m->ws.err_flag, 0, 4, s);
         if (flag == kErrBadLabel) return fail(ZOQAT_ERR_INVALID_ARG, "a label is >= vocab (its position was given loss 0)");
+        if (flag == kErrBadSlot) return fail(ZOQAT_ERR_INVALID_ARG, "a row's slot or position lies outside the cache or the position tables");
+        if (flag == kErrBadRequest) return fail(ZOQAT_ERR_INVALID_ARG, "a request's lengths and rows contradict each other");
+        if (flag == kErrBadPage) return fail(ZOQAT_ERR_INVALID_ARG, "a block table names a page outside the cache");
         if (flag == kErrCodeRange) return fail(ZOQAT_ERR_UNSUPPORTED, "8-bit integer GEMM: a weight row's code minus zero point left [-128, 127]");
         return fail(ZOQAT_ERR_TIMEOUT, "device wait ran out (code %d)", flag);
     }
@@ -1818,6 +1821,17 @@ int paged_cache(const zoqat_paged_cache_t* c, PagedCache& out) {
     return ZOQAT_OK;
 }
 
+// What the attention kernels need of a (checked) cache besides.
+int attention_limits(const PagedCache& c, int max_pages, int64_t rows, int n_heads) {
+    if ((int64_t)max_pages * c.page_size > INT32_MAX - 256 || rows * n_heads > INT32_MAX) return fail(ZOQAT_ERR_UNSUPPORTED, "sizes pass 2^31");
+    if (c.type == kTypeF32) return ZOQAT_OK;
+    if (c.page_size % 128 && c.page_size != 8 && c.page_size != 16 && c.page_size != 32 && c.page_size != 64)
+        return fail(ZOQAT_ERR_UNSUPPORTED, "page_size %d (bf16 / fp16: 8, 16, 32, 64 or a multiple of 128)", c.page_size);
+    if (c.n_kv_heads > 1 && c.n_pages > 1 && c.page_stride % c.head_stride)
+        return fail(ZOQAT_ERR_UNSUPPORTED, "bf16 / fp16: page_stride must be a multiple of head_stride");
+    return ZOQAT_OK;
+}
+
 int logit_rules(const zoqat_logit_rules_t* c, int rows, int vocab, LogitRules& r) {
     if (!c) return fail(ZOQAT_ERR_INVALID_ARG, "rules are NULL");
     if (rows <= 0 || rows > 65535 || vocab <= 0 || vocab > (1 << 30)) return fail(ZOQAT_ERR_UNSUPPORTED, "rows %d (1..65535), vocab %d (1..2^30)", rows, vocab);
@@ -1901,7 +1915,7 @@ int zoqat_op_tree_attention(const void* q_dev, int64_t q_stride, const zoqat_pag
     if (!q_dev || !block_table_dev || !kv_len_dev || !row_start_dev || !out_dev || !scratch_dev || !err_flag_dev) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
     if (batch <= 0 || rows < 0 || n_heads <= 0 || max_pages <= 0) return fail(ZOQAT_ERR_INVALID_ARG, "sizes must be positive");
     if (n_heads % c.n_kv_heads) return fail(ZOQAT_ERR_INVALID_ARG, "n_kv_heads must divide n_heads");
-    if ((int64_t)max_pages * c.page_size > INT32_MAX - 256 || (int64_t)rows * n_heads > INT32_MAX) return fail(ZOQAT_ERR_UNSUPPORTED, "sizes pass 2^31");
+    if (int rc = attention_limits(c, max_pages, rows, n_heads)) return rc;
     if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(ZOQAT_ERR_INVALID_ARG, "scale must be positive");
     if (tree_mask_dev ? mask_words <= 0 || mask_words > (1 << 20) : mask_words != 0) return fail(ZOQAT_ERR_INVALID_ARG, "tree_mask_dev and mask_words must both be given or neither");
     const int64_t e = type_bytes(c.type), wide = (int64_t)n_heads * c.d_head;
@@ -1912,10 +1926,6 @@ int zoqat_op_tree_attention(const void* q_dev, int64_t q_stride, const zoqat_pag
     const size_t need = tree_attention_scratch_bytes(c.type, c.d_head);
     if (scratch_bytes < need) return fail(ZOQAT_ERR_WORKSPACE_SMALL, "attention scratch %zu < %zu bytes", scratch_bytes, need);
     const bool tc = c.type != ZOQAT_TYPE_F32;
-    if (tc && c.page_size % 128 && c.page_size != 8 && c.page_size != 16 && c.page_size != 32 && c.page_size != 64)
-        return fail(ZOQAT_ERR_UNSUPPORTED, "page_size %d (bf16 / fp16: 8, 16, 32, 64 or a multiple of 128)", c.page_size);
-    if (tc && c.n_kv_heads > 1 && c.n_pages > 1 && c.page_stride % c.head_stride)
-        return fail(ZOQAT_ERR_UNSUPPORTED, "bf16 / fp16: page_stride must be a multiple of head_stride");
     if (rows == 0) return ZOQAT_OK;
     a.q = q_dev; a.q_stride = q_stride; a.block_table = block_table_dev; a.max_pages = max_pages; a.kv_len = kv_len_dev; a.row_start = row_start_dev;
     a.tree_mask = tree_mask_dev; a.mask_words = mask_words; a.batch = batch; a.rows = rows; a.n_heads = n_heads; a.scale = scale;
@@ -1939,6 +1949,86 @@ int zoqat_op_logit_rules(const void* logits_dev, int type, int64_t ld, int rows,
     if (misaligned(logits_dev, e) || misaligned(out_dev, e)) return fail(ZOQAT_ERR_INVALID_ARG, "misaligned pointer");
     if (launch_logit_rules(logits_dev, type, ld, rows, vocab, r, out_dev, out_ld, token_dev, static_cast<cudaStream_t>(stream)) != 0)
         return fail(ZOQAT_ERR_CUDA, "logit rules: launch failed");
+    CUDA_TRY(cudaGetLastError());
+    return ZOQAT_OK;
+}
+
+int zoqat_decode_tree_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows, const zoqat_tree_batch_t* plan,
+                           const zoqat_paged_cache_t* caches, const zoqat_logit_rules_t* rules, float* logits_dev,
+                           int32_t* next_token_dev, void* scratch_dev, size_t scratch_bytes, void* stream) {
+    if (!m || !tokens_dev || !plan || !caches || !scratch_dev) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
+    DecodeState& D = m->dec;
+    if (!D.ready) return fail(ZOQAT_ERR_BAD_STATE, "call zoqat_decode_begin first");
+    const zoqat_config_t& c = m->cfg;
+    if (rows != 1 && rows != 2 && rows != 4 && rows != 8) return fail(ZOQAT_ERR_UNSUPPORTED, "%d rows (supported: 1, 2, 4, 8)", rows);
+    if (rows > c.max_batch * c.max_seq) return fail(ZOQAT_ERR_INVALID_ARG, "rows exceed the workspace");
+    if (!logits_dev && (rows > D.batch || !next_token_dev)) return fail(ZOQAT_ERR_INVALID_ARG, "logits_dev may be NULL for up to %d rows and with next_token_dev", D.batch);
+    if (!plan->block_table || !plan->kv_len || !plan->row_start || !plan->row_pos || !plan->slot) return fail(ZOQAT_ERR_INVALID_ARG, "the plan has a NULL array");
+    if (plan->batch <= 0 || plan->max_pages <= 0 || (plan->tree_mask ? plan->mask_words <= 0 || plan->mask_words > (1 << 20) : plan->mask_words != 0))
+        return fail(ZOQAT_ERR_INVALID_ARG, "bad plan sizes");
+    if (misaligned(scratch_dev, 256)) return fail(ZOQAT_ERR_INVALID_ARG, "scratch_dev must be 256-byte aligned");
+    const bool llama = c.arch == ZOQAT_ARCH_LLAMA;
+    const int d = c.d_model, F = c.d_ffn, H = c.n_heads, dh = d / H, G = c.w_group;
+    LogitRules r{};
+    if (rules)
+        if (int rc = logit_rules(rules, rows, c.vocab, r)) return rc;
+    // every layer's cache is checked before anything is launched
+    PagedCache p;
+    for (int l = 0; l < c.n_layers; ++l) {
+        if (int rc = paged_cache(caches + l, p)) return rc;
+        if (p.n_kv_heads != H || p.d_head != dh) return fail(ZOQAT_ERR_INVALID_ARG, "layer %d: the cache has %d heads of %d, the model %d of %d", l, p.n_kv_heads, p.d_head, H, dh);
+        if (int rc = attention_limits(p, plan->max_pages, rows, H)) return rc;
+        if (scratch_bytes < tree_attention_scratch_bytes(p.type, dh)) return fail(ZOQAT_ERR_WORKSPACE_SMALL, "attention scratch %zu < %zu bytes", scratch_bytes, tree_attention_scratch_bytes(p.type, dh));
+    }
+    Workspace& w = m->ws;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int norm_kind = llama ? 1 : 2, n_up = llama ? 2 * F : F;
+    const bool planes = c.a_bits != 0;
+    auto gemv = [&](const void* wq, const float2* qp, int N, int K, const float* bias, int accumulate, float* out) {
+        const int rc = c.a_bits ? launch_decode_gemv(wq, qp, N, K, G, rows, w.xa, w.row_step, bias, accumulate, out, s)
+                                : launch_decode_gemv_fp(wq, qp, N, K, G, rows, w.xa, bias, accumulate, out, s);
+        if (rc != 0) return fail(ZOQAT_ERR_UNSUPPORTED, "decode matrix-vector product rejected (N=%d K=%d)", N, K);
+        return (int)ZOQAT_OK;
+    };
+    // rotated queries and 16-bit attention outputs live in the FFN buffer, which is free between the two halves of a layer
+    uint8_t* q_rot = reinterpret_cast<uint8_t*>(w.ffn);
+    uint8_t* att16 = q_rot + align_up((size_t)rows * d * 4);
+    if (align_up((size_t)rows * d * 4) + (size_t)rows * d * 2 > (size_t)2 * c.max_batch * c.max_seq * n_up * 4)
+        return fail(ZOQAT_ERR_UNSUPPORTED, "the FFN workspace is too small for %d rows (d_ffn far below d_model)", rows);
+    launch_embed_rows(tokens_dev, plan->row_pos, m->embed, m->pos, rows, d, c.vocab, c.max_seq, w.h, w.err_flag, s);
+    for (int l = 0; l < c.n_layers; ++l) {
+        const Layer& Ly = m->layers[l];
+        const DecodeLayer& dl = D.layers[l];
+        paged_cache(caches + l, p);
+        const bool half = p.type != kTypeF32;
+        launch_norm_act_operand(w.h, rows, d, norm_kind, Ly.vec[ZOQAT_ROLE_ATTN_NORM_G], Ly.vec[ZOQAT_ROLE_ATTN_NORM_B], c.norm_eps,
+                                c.a_bits, w.xa, w.row_step, nullptr, s, SmoothAct(), true, planes);
+        if (int rc = gemv(dl.w_qkv, dl.q_qkv, 3 * d, d, llama ? nullptr : w.bias_qkv + (size_t)l * 3 * d, 0, w.qkv)) return rc;
+        launch_cache_append(w.qkv, 3 * d, plan->row_pos, plan->slot, rows, H, llama ? w.rope_cos : nullptr, llama ? w.rope_sin : nullptr, c.max_seq,
+                            p, q_rot, d, w.err_flag, s, true);
+        TreeAttnArgs a{};
+        a.cache = p; a.q = q_rot; a.q_stride = d; a.block_table = plan->block_table; a.max_pages = plan->max_pages; a.kv_len = plan->kv_len;
+        a.row_start = plan->row_start; a.tree_mask = plan->tree_mask; a.mask_words = plan->mask_words; a.batch = plan->batch; a.rows = rows; a.n_heads = H;
+        a.scale = (float)(1.0 / std::sqrt((double)dh)); a.out = half ? static_cast<void*>(att16) : w.att; a.out_stride = d;
+        a.scratch = static_cast<uint8_t*>(scratch_dev); a.err_flag = w.err_flag;
+        if (int rc = half ? launch_tree_attention_tc(a, s, true) : launch_tree_attention_simt(a, s, true)) return fail(rc, "tree attention launch failed");
+        if (half) launch_widen(att16, p.type, (int64_t)rows * d, w.att, s);
+        launch_norm_act_operand(w.att, rows, d, 0, nullptr, nullptr, 0.f, c.a_bits, w.xa, w.row_step, nullptr, s, SmoothAct(), true, planes);
+        if (int rc = gemv(dl.w_o, dl.q_o, d, d, Ly.vec[ZOQAT_ROLE_BO], 1, w.h)) return rc;
+        launch_norm_act_operand(w.h, rows, d, norm_kind, Ly.vec[ZOQAT_ROLE_FFN_NORM_G], Ly.vec[ZOQAT_ROLE_FFN_NORM_B], c.norm_eps,
+                                c.a_bits, w.xa, w.row_step, nullptr, s, SmoothAct(), true, planes);
+        if (int rc = gemv(dl.w_up, dl.q_up, n_up, d, Ly.vec[ZOQAT_ROLE_B_FC1], 0, w.ffn)) return rc;
+        launch_ffn_act_operand(w.ffn, rows, F, llama ? 1 : 0, c.a_bits, w.xa, w.row_step, s, SmoothAct(), true, planes);
+        if (int rc = gemv(dl.w_down, dl.q_down, d, F, Ly.vec[ZOQAT_ROLE_B_FC2], 1, w.h)) return rc;
+    }
+    launch_norm_act_operand(w.h, rows, d, norm_kind, m->final_g, m->final_b, c.norm_eps, 0, w.xa, w.row_step, nullptr, s, SmoothAct(), true);
+    float* logits = logits_dev ? logits_dev : D.logits;
+    if (launch_decode_head(D.head, c.vocab, d, rows, w.xa, logits, s) != 0) return fail(ZOQAT_ERR_UNSUPPORTED, "vocabulary projection rejected");
+    if (rules) {
+        if (launch_logit_rules(logits, kTypeF32, c.vocab, rows, c.vocab, r, logits, c.vocab, next_token_dev, s) != 0) return fail(ZOQAT_ERR_CUDA, "logit rules: launch failed");
+    } else if (next_token_dev) {
+        launch_decode_argmax(logits, rows, c.vocab, next_token_dev, s);
+    }
     CUDA_TRY(cudaGetLastError());
     return ZOQAT_OK;
 }

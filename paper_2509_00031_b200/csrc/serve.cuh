@@ -46,7 +46,8 @@ void launch_cache_append(const float* qkv, int64_t ld, const int32_t* row_pos, c
                          const float* cos_t, const float* sin_t, int rope_len, const PagedCache& cache, void* q_out, int64_t q_stride,
                          int32_t* err_flag, cudaStream_t s, bool dependent = false);
 void launch_embed_rows(const int32_t* tokens, const int32_t* row_pos, const float* embed, const float* pos_embed, int rows, int d, int vocab,
-                       int max_pos, float* h, cudaStream_t s);
+                       int max_pos, float* h, int32_t* err_flag, cudaStream_t s);
+void launch_widen(const void* src, int type, int64_t n, float* dst, cudaStream_t s);      // n % 8 == 0, 16-byte aligned
 
 // Attention of drafted rows over the pages.
 struct TreeAttnArgs {

@@ -8,6 +8,7 @@
 //                         of the tables, so no CTA waits for another and no scratch is needed.
 //   cache_append_kernel   (a, b) -> (a cos - b sin, b cos + a sin) for q and k, then one rounding into the cache's type.
 //   embed_rows_kernel     the residual rows of drafted tokens (each row has a position of its own).
+//   widen_kernel          attention outputs of a 16-bit cache for the fp32 activation quantisers of a model's step.
 #include "common.cuh"
 #include "serve.cuh"
 
@@ -253,10 +254,11 @@ cache_append_kernel(const float* __restrict__ qkv, int64_t ld, const int32_t* __
 // h[r] = embed[token] (+ pos_embed[position of r]); a token outside the vocabulary and a padded row give zeros
 __global__ void __launch_bounds__(256)
 embed_rows_kernel(const int32_t* __restrict__ tokens, const int32_t* __restrict__ row_pos, const float* __restrict__ embed,
-                  const float* __restrict__ pos_embed, int d, int vocab, int max_pos, float* __restrict__ h) {
+                  const float* __restrict__ pos_embed, int d, int vocab, int max_pos, float* __restrict__ h, int32_t* __restrict__ err_flag) {
     const int r = blockIdx.x;
     const int tok = tokens[r], pos = row_pos[r];
     const bool live = pos >= 0 && pos < max_pos && tok >= 0 && tok < vocab;
+    if (threadIdx.x == 0 && pos >= max_pos) atomicExch(err_flag, kErrBadSlot);
     for (int i = threadIdx.x; i < d; i += 256) {
         float x = 0.0f;
         if (live) {
@@ -265,6 +267,20 @@ embed_rows_kernel(const int32_t* __restrict__ tokens, const int32_t* __restrict_
         }
         h[(size_t)r * d + i] = x;
     }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256)
+widen_kernel(const T* __restrict__ src, float* __restrict__ dst, int n8) {
+    grid_dependency_wait();
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= n8) return;
+    const uint4 w = reinterpret_cast<const uint4*>(src)[i];
+    const T* v = reinterpret_cast<const T*>(&w);
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = static_cast<float>(v[e]);
+    Pack8<float>::store(dst + 8 * (size_t)i, f);
 }
 
 }  // namespace
@@ -304,8 +320,15 @@ void launch_cache_append(const float* qkv, int64_t ld, const int32_t* row_pos, c
 }
 
 void launch_embed_rows(const int32_t* tokens, const int32_t* row_pos, const float* embed, const float* pos_embed, int rows, int d, int vocab,
-                       int max_pos, float* h, cudaStream_t s) {
-    embed_rows_kernel<<<rows, 256, 0, s>>>(tokens, row_pos, embed, pos_embed, d, vocab, max_pos, h);
+                       int max_pos, float* h, int32_t* err_flag, cudaStream_t s) {
+    embed_rows_kernel<<<rows, 256, 0, s>>>(tokens, row_pos, embed, pos_embed, d, vocab, max_pos, h, err_flag);
+    count_launch();
+}
+
+void launch_widen(const void* src, int type, int64_t n, float* dst, cudaStream_t s) {
+    const int n8 = (int)(n / 8);
+    if (type == kTypeBf16) launch_kernel(widen_kernel<__nv_bfloat16>, dim3((n8 + 255) / 256), dim3(256), 0, s, true, static_cast<const __nv_bfloat16*>(src), dst, n8);
+    else launch_kernel(widen_kernel<__half>, dim3((n8 + 255) / 256), dim3(256), 0, s, true, static_cast<const __half*>(src), dst, n8);
     count_launch();
 }
 

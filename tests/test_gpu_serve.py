@@ -572,3 +572,165 @@ def test_rules_choice_with_ties_infinities_and_nan(zq):
     x[3, 4000:] = float("inf")
     _, tok = zq.zoqat_op_logit_rules(x, zq.LogitRules(batch=4))
     assert tok.tolist() == [0, -1, 8999, 4000]
+
+
+# ---- the operators together ---------------------------------------------------------------------------------------------
+MODELS = {
+    "llama_w4a8": dict(arch="llama", n_layers=2, d_model=256, n_heads=2, d_ffn=512, vocab=600, w_bits=4, w_group=64, a_bits=8),
+    "llama_w4": dict(arch="llama", n_layers=2, d_model=128, n_heads=2, d_ffn=384, vocab=600, w_bits=4, w_group=128, a_bits=0),
+    "opt_w3a8": dict(arch="opt", n_layers=2, d_model=128, n_heads=2, d_ffn=256, vocab=333, w_bits=3, w_group=128, a_bits=8),
+}
+
+
+def packed_model(zq, name, batch, seq):
+    from paper_2509_00031_b200 import synth
+    shape = MODELS[name]
+    params = synth.make_params(shape, seed=5, max_seq=seq, jitter=True)
+    model = zq.ZoqatModel(shape, zq.params_to_device(params), max_batch=batch, max_seq=seq, first_trainable_layer=shape["n_layers"], head_trainable=False,
+                          packed_frozen=True)
+    model.zoqat_prequantize_frozen()
+    model.zoqat_decode_begin(batch, seq)
+    return shape, model
+
+
+class Serving:
+    """A serving loop's state: lengths, pages and their tables, advanced by the operators alone."""
+
+    def __init__(self, zq, shape, model, batch, page, dtype, max_rows=8):
+        self.zq, self.model, self.page, self.batch, self.rows = zq, model, page, batch, max_rows
+        self.cached, self.n_pages = [0] * batch, 40
+        dh = shape["d_model"] // shape["n_heads"]
+        self.caches = [make_cache(self.n_pages, page, shape["n_heads"], dh, dtype, "token") for _ in range(shape["n_layers"])]
+        self.table = torch.full((batch, 12), -1, dtype=torch.int32, device="cuda")
+        self.free = torch.randperm(self.n_pages, generator=torch.Generator().manual_seed(3)).to(torch.int32).cuda()
+        self.n_free = ints([self.n_pages])
+
+    def step(self, tokens, parents=None, rules=None, keep=True):
+        """tokens, parents: one list per request.  Returns logits and choices of the live rows, and the plan."""
+        flat = [t for r in tokens for t in r]
+        par = [t for r in parents for t in r] if parents else None
+        pad = self.rows - len(flat)
+        plan = self.zq.zoqat_op_cache_plan(ints(self.cached), ints([len(r) for r in tokens]), self.page, self.n_pages, self.free, self.n_free, self.table,
+                                           self.rows, parents=ints(par + [-1] * pad) if par else None, mask_words=1)
+        assert plan["status"].item() == 0
+        if rules is not None:
+            rules = self.zq.LogitRules(row_request=plan["row_request"], draft_token=ints(flat + [0] * pad), row_start=plan["row_start"],
+                                       tree_mask=plan["tree_mask"], batch=self.batch, **rules)
+        logits, choice = self.model.zoqat_decode_tree_step(ints(flat + [0] * pad), plan, self.table, self.caches, rules=rules)
+        self.model.zoqat_check()
+        if keep:
+            self.n_free = plan["n_free"]
+            self.cached = plan["kv_len"].tolist()
+        return logits[:len(flat)], choice[:len(flat)], plan
+
+
+def sequential_logits(model, tokens, batch):
+    """Logits after the last of `tokens`, by the one-token decode path."""
+    for pos, t in enumerate(tokens):
+        logits, _ = model.zoqat_decode_step(ints([t] * batch), pos)
+    return logits[0].clone()
+
+
+@pytest.mark.parametrize("name,dtype,page", [("llama_w4a8", "f32", 16), ("llama_w4", "bf16", 8), ("opt_w3a8", "f16", 16), ("llama_w4a8", "f32", 5),
+                                             ("opt_w3a8", "f32", 7)])
+def test_drafts_through_the_model_match_the_one_token_path(zq, name, dtype, page):
+    # three requests of different lengths, prompts fed in chunks, then one step with a tree per request: every row's logits against the
+    # one-token decode path fed the prompt and the row's ancestors
+    batch = 2
+    shape, model = packed_model(zq, name, batch, 64)
+    _, other = packed_model(zq, name, batch, 64)
+    rng = np.random.default_rng(1)
+    prompts = [rng.integers(0, shape["vocab"], n).tolist() for n in (9, 17, 1)]
+    sv = Serving(zq, shape, model, 3, page, dtype)
+    todo = [list(p) for p in prompts]
+    while any(todo):
+        share = [min(len(t), 3) for t in todo]
+        sv.step([t[:n] for t, n in zip(todo, share)])
+        todo = [t[n:] for t, n in zip(todo, share)]
+    assert sv.cached == [9, 17, 1]
+    drafts = [rng.integers(0, shape["vocab"], n).tolist() for n in (4, 3, 1)]
+    parents = [[-1, 0, 0, 2], [-1, -1, 1], [-1]]
+    logits, choice, plan = sv.step(drafts, parents, keep=False)
+    # a difference of one code in one activation moves a row by up to one step (1 / 127 of its largest value, 2^-8 of a bf16 value);
+    # 16-bit caches round every key and value once
+    tol = {"f32": 2e-2, "f16": 2e-2, "bf16": 5e-2}[dtype]
+    row = 0
+    for b in range(3):
+        for i in range(len(drafts[b])):
+            path = [drafts[b][j] for j in sorted(ancestors(parents[b], i))]
+            want = sequential_logits(other, prompts[b] + path, batch)
+            assert float((logits[row] - want).abs().max()) <= tol * float(want.abs().max()), (b, i)
+            assert choice[row].item() == int(torch.argmax(logits[row]))
+            row += 1
+    # the same step again, with rules: the choices are those of the rules on these logits
+    V = shape["vocab"]
+    history = torch.zeros((3, 20), dtype=torch.int32, device="cuda")
+    for b in range(3):
+        history[b, :len(prompts[b])] = ints(prompts[b])
+    rules = dict(history=history, history_len=ints([9, 17, 1]), prompt_len=ints([4, 17, 0]), repetition=torch.full((3,), 1.3, device="cuda"),
+                 presence=torch.full((3,), 0.2, device="cuda"), frequency=torch.full((3,), 0.1, device="cuda"))
+    ruled, token, plan = sv.step(drafts, parents, rules=dict(rules), keep=False)
+    seen = [set(ancestors(parents[b], i)) for b in range(3) for i in range(len(drafts[b]))]
+    want, best = rules_oracle(logits, "f32", plan["row_request"].tolist()[:8], dict(
+        history=history.tolist(), history_len=[9, 17, 1], prompt_len=[4, 17, 0], repetition=[1.3] * 3, presence=[0.2] * 3, frequency=[0.1] * 3,
+        drafts=[t for r in drafts for t in r], row_start=[0, 4, 7, 8], seen=seen), V)
+    assert torch.equal(ruled.cpu(), want) and token.tolist() == best.tolist()
+    # one request accepts a branch: its drafts' slots are overwritten by the next step, and the others go on as they were
+    sv.cached = [9, 17, 1]
+    logits2, _, _ = sv.step([[drafts[0][0]], [], [drafts[2][0], 5]])
+    assert float((logits2[0] - logits[0]).abs().max()) <= tol * float(logits[0].abs().max())
+
+
+def test_a_captured_tree_step_replays_with_new_lengths(zq):
+    shape, model = packed_model(zq, "llama_w4a8", 2, 64)
+    sv = Serving(zq, shape, model, 2, 16, "bf16", max_rows=4)
+    sv.step([[3, 4], [5]])
+    cached, new, tokens = ints(sv.cached), ints([1, 1]), ints([7, 8, 0, 0])
+    n_free = sv.n_free.clone()
+    out = {n: torch.empty(s, dtype=torch.int32, device="cuda") for n, s in dict(kv_len=(2,), row_start=(3,), row_request=(4,), row_pos=(4,), slot=(4,), n_free=(1,),
+                                                                               tree_mask=(4, 1)).items()}
+    out["status"] = torch.zeros(1, dtype=torch.int32, device="cuda")
+    logits, nxt = torch.empty((4, shape["vocab"]), device="cuda"), torch.empty(4, dtype=torch.int32, device="cuda")
+    scratch = torch.empty(48 << 20, dtype=torch.uint8, device="cuda")
+
+    def run():
+        zq.zoqat_op_cache_plan(cached, new, 16, sv.n_pages, sv.free, n_free, sv.table, 4, mask_words=1, out=out)
+        model.zoqat_decode_tree_step(tokens, out, sv.table, sv.caches, logits=logits, next_token=nxt, scratch=scratch)
+
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for lens, n in (([2, 1], [1, 1]), ([3, 2], [2, 1]), ([5, 3], [0, 3])):
+        cached.copy_(ints(lens)); new.copy_(ints(n)); tokens.copy_(ints([9, 10, 11, 12]))
+        logits.fill_(0.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        model.zoqat_check()
+        got = logits.clone()
+        run()
+        torch.cuda.synchronize()
+        rows = sum(n)
+        assert out["status"].item() == 0 and out["row_start"].tolist()[-1] == rows
+        assert torch.equal(got[:rows], logits[:rows]) and bool(torch.isfinite(got[:rows]).all())
+
+
+def test_tree_step_refuses_and_reports(zq):
+    shape, model = packed_model(zq, "llama_w4a8", 2, 64)
+    sv = Serving(zq, shape, model, 1, 16, "f32", max_rows=2)
+    _, _, plan = sv.step([[3]])
+    ok = lambda **kw: model.zoqat_decode_tree_step(kw.pop("tokens", ints([1, 2])), kw.pop("plan", plan), sv.table, kw.pop("caches", sv.caches), **kw)  # noqa: E731
+    ok()
+    for kw in (dict(tokens=ints([1, 2, 3])), dict(caches=sv.caches[:1]), dict(caches=[make_cache(4, 16, 1, 128, "f32", "token")] * 2),
+               dict(scratch=torch.empty(4096, dtype=torch.uint8, device="cuda")), dict(caches=[make_cache(4, 12, 2, 128, "bf16", "token")] * 2),
+               dict(logits=torch.empty((2, 5), device="cuda"))):
+        with pytest.raises(zq.ZoqatError):
+            ok(**kw)
+    # a position behind the tables is reported by the check
+    bad = dict(plan, row_pos=ints([64, -1]))
+    ok(plan=bad)
+    with pytest.raises(zq.ZoqatError) as e:
+        model.zoqat_check()
+    assert e.value.status == zq.ERR_INVALID_ARG
+    model.zoqat_check()
