@@ -10,13 +10,16 @@
 // tiles per key head on, where the copies come from L2.
 //
 // One persistent CTA per SM, 12 warps; the key tiles of all requests are dealt out in equal runs (tree_attention.cuh):
-//   warp 0      K and V tiles by TMA into a ring; warps 2, 3: query tiles into two buffers, a piece ahead
-//   warp 1      one thread issues the products: S = Q K^T into one of two TMEM score buffers, O += P V with P read from TMEM
-//               and V as it lies in the page (keys along k, so no transposition).
-//   warps 4-7, 8-11  two softmax groups take alternate tiles.  A thread owns a query row: it reads the tile's 128 scores, and
-//               writes the weights, rounded to the cache's type, over them.  Each group has a reference, a sum and an output
-//               accumulator of its own, so the groups need not agree on anything until the piece ends, when the two
-//               results are joined.  The reference moves only when a row's maximum has grown by more than 2^8 since.
+//   warp 0      K and V tiles by TMA into a ring; warp 3: query tiles into two buffers, a piece ahead
+//   warps 1, 2  one thread issues S = Q K^T into one of two TMEM score buffers as soon as its last scores have been read,
+//               another O += P V with P from shared memory and V as it lies in the page (keys along k, so no transposition): the
+//               waits and commits of one thread for both left the tensor pipe idle for more than half of the time
+//   warps 4-7, 8-11  two softmax groups take alternate tiles.  A thread owns a query row: it reads the tile's 128 scores and
+//               writes the weights, rounded to the cache's type, to the group's own P tile, so that the scores of its next
+//               tile form while the product with V runs.  Each group has a reference, a sum and an output accumulator of its
+//               own, so the groups need not agree on anything until the piece ends, when the two results are joined.  The
+//               weights are formed against the reference as it stands; where a row's maximum turns out to have grown by more
+//               than 2^8 the reference moves and the tile's weights are formed again.
 // Rounding: the products are exact in binary32 up to accumulation; the weights are rounded to 11 (fp16) or 8 (bf16) bits for
 // the second product, the sums are formed from the unrounded weights, the output is rounded once.  fp16 weights are scaled by
 // 2^7, which keeps small ones out of the subnormals; the largest is then 2^15.
@@ -31,14 +34,18 @@ namespace zq {
 namespace {
 
 constexpr int kTcThreads = 384, kRows = 128;
+constexpr float kNoRef = -1.0e30f;       // reference of a row that has seen nothing: any score passes it
 
 template <int DH> struct TcCfg {
     static constexpr int kTileBytes = kKeys * DH * 2;                       // one K, V or Q tile
-    static constexpr int kStages = DH == 128 ? 5 : 10;
+    static constexpr int kPBytes = kRows * kKeys * 2;                       // [half of the keys][128 rows][128 bytes], as Q
+    static constexpr int kStages = DH == 128 ? 3 : 7;
     static constexpr int kOffRing = 2 * kTileBytes;
-    static constexpr int kOffX = kOffRing + kStages * kTileBytes;           // (reference, sum) of every row: [2 groups][128][2]
+    static constexpr int kOffP = kOffRing + kStages * kTileBytes;
+    static constexpr int kOffX = kOffP + 2 * kPBytes;                       // (reference, sum) of every row: [2 groups][128][2]
     static constexpr int kOffBar = kOffX + 2048;
-    static constexpr int kOffMisc = kOffBar + (2 * kStages + 13) * 8;       // TMEM base, non-finite marks, run
+    static constexpr int kBars = 2 * kStages + 15;
+    static constexpr int kOffMisc = kOffBar + kBars * 8;                    // TMEM base, non-finite marks, run
     static constexpr int kUsedBytes = kOffMisc + 32 + 192 + (int)sizeof(TreeRun);
     static constexpr int kSmemBytes = kUsedBytes + 1024 > 232448 ? 232448 : kUsedBytes + 1024;
     static_assert(kUsedBytes <= 232448, "shared memory");
@@ -69,18 +76,19 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     auto q_full = [&](int s) { return bars + 8u * (2 * NS + s); };
     auto q_empty = [&](int s) { return bars + 8u * (2 * NS + 2 + s); };
     auto s_full = [&](int g) { return bars + 8u * (2 * NS + 4 + g); };
-    auto p_full = [&](int g) { return bars + 8u * (2 * NS + 6 + g); };
-    auto o_full = [&](int g) { return bars + 8u * (2 * NS + 8 + g); };
-    auto o_empty = [&](int g) { return bars + 8u * (2 * NS + 10 + g); };
-    const uint32_t x_full = bars + 8u * (2 * NS + 12);
+    auto s_empty = [&](int g) { return bars + 8u * (2 * NS + 6 + g); };
+    auto p_full = [&](int g) { return bars + 8u * (2 * NS + 8 + g); };
+    auto o_full = [&](int g) { return bars + 8u * (2 * NS + 10 + g); };
+    auto o_empty = [&](int g) { return bars + 8u * (2 * NS + 12 + g); };
+    const uint32_t x_full = bars + 8u * (2 * NS + 14);
     volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc);
     volatile uint32_t* odd_piece = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 8);   // [2]: piece + 1 with a non-finite draft value
     long long* part = reinterpret_cast<long long*>(sp + Cfg::kOffMisc + 32);
     TreeRun* run = reinterpret_cast<TreeRun*>(sp + Cfg::kOffMisc + 32 + 192);
 
-    if (tid < 2 * NS + 13) {
-        const int i = tid - 2 * NS;              // one barrier a thread: ring full, ring empty; q full, q empty, s full, p full, o full, o empty, x full
-        mbar_init(bars + 8u * tid, i < 0 ? 1 : (i < 2 ? 2 : (i < 6 ? 1 : (i < 8 ? 4 : (i < 10 ? 1 : 8)))));
+    if (tid < Cfg::kBars) {
+        const int i = tid - 2 * NS;              // one barrier a thread: ring full, ring empty; then as above
+        mbar_init(bars + 8u * tid, i < 6 ? 1 : (i < 10 ? 4 : (i < 12 ? 1 : 8)));
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (tid < 2) odd_piece[tid] = 0;
@@ -99,70 +107,78 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    const uint32_t tmem_s = tmem, tmem_o = tmem + 256u;          // S (then P) of group g at + 128 g, O of group g at + 128 g
+    const uint32_t tmem_s = tmem, tmem_o = tmem + 256u;          // S and O of group g at + 128 g
     const int n_tiles = (int)(run->end - run->begin);
 
+    constexpr uint32_t kIdesc = (1u << 4) | (Ops::kFormat << 7) | (Ops::kFormat << 10) | ((uint32_t)(kRows >> 4) << 24);
+    // Place `seq` of the ring's sequence has landed.  K and V share the slots and have consumers of their own, so a consumer may
+    // come to a slot whose use before is still to land: it first waits until that use has been consumed (the one before that was
+    // the consumer's own kind and is past), then for this one.
+    auto slot_filled = [&](int slot, uint32_t seq) -> bool {
+        if (seq >= (uint32_t)NS && !mbar_poll(ring_empty(slot), ((seq / NS) & 1u) ^ 1u)) return false;
+        return mbar_poll(ring_full(slot), (seq / NS) & 1u);
+    };
+
     if (warp == 0 && n_tiles > 0) {
-        tree_load_keys<DH, NS>(p, &map_k, &map_v, run, base + Cfg::kOffRing, ring_full(0), ring_empty(0));
-    } else if ((warp == 2 || warp == 3) && n_tiles > 0) {
-        tree_load_queries<DH, kRows, 64, T>(p, run, sp, nullptr, 0u, q_full(0), q_empty(0), tid - 64);
+        tree_load_keys<DH, NS, 2>(p, &map_k, &map_v, run, base + Cfg::kOffRing, ring_full(0), ring_empty(0));
+    } else if (warp == 3 && n_tiles > 0) {
+        tree_load_queries<DH, kRows, 32, T>(p, run, sp, nullptr, 0u, q_full(0), q_empty(0), lane);
     } else if (warp == 1 && n_tiles > 0) {
-        // ---------------- MMA issuer
+        // ---------------- the scores
         if (lane == 0) {
-            constexpr uint32_t kIdesc = (1u << 4) | (Ops::kFormat << 7) | (Ops::kFormat << 10) | ((uint32_t)(kRows >> 4) << 24);
-            constexpr uint32_t kIdescS = kIdesc | ((uint32_t)(kKeys >> 3) << 17);
-            constexpr uint32_t kIdescO = kIdesc | (1u << 16) | ((uint32_t)(DH >> 3) << 17);      // bit 16: B is MN-major
-            TreeCursor c = run->at;                    // of the next S
-            uint32_t seq = 0, piece = 0;
-            bool ok = true, ends = false;              // ends: the piece of the last S issued ends with it
-            auto issue_s = [&](int t) -> bool {
+            TreeCursor c = run->at;
+            uint32_t piece = 0, b = 0;
+            bool ok = true;
+            for (int t = 0; t < n_tiles; ++t, c.next(p.w)) {
+                const uint32_t seq = t < 2 ? t : 2u * t - 2u;
                 const int slot = seq % NS, g = t & 1;
                 if (t == 0 || c.item_begins()) {
-                    if (!mbar_poll(q_full(piece & 1u), (piece >> 1) & 1u)) return false;
+                    b = piece & 1u;
+                    if (!mbar_poll(q_full(b), (piece >> 1) & 1u)) { ok = false; break; }
                     ++piece;
                 }
-                const uint32_t b = (piece - 1) & 1u;
-                if (!mbar_poll(ring_full(slot), (seq / NS) & 1u)) return false;
+                if (!mbar_poll(s_empty(g), ((t >> 1) & 1u) ^ 1u) || !slot_filled(slot, seq)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t qa = base + b * Cfg::kTileBytes, ka = base + Cfg::kOffRing + slot * Cfg::kTileBytes;
 #pragma unroll
                 for (int k = 0; k < DH / 16; ++k) {
                     const uint64_t da = smem_desc_sw128(qa + (k >> 2) * (kRows * 128)) + (uint64_t)(2 * (k & 3));
                     const uint64_t db = smem_desc_sw128(ka + (k >> 2) * 1024, tree_group_bytes<DH>()) + (uint64_t)(2 * (k & 3));
-                    umma_bf16(tmem_s + 128u * g, da, db, kIdescS, k > 0 ? 1u : 0u);
+                    umma_bf16(tmem_s + 128u * g, da, db, kIdesc | ((uint32_t)(kKeys >> 3) << 17), k > 0 ? 1u : 0u);
                 }
                 umma_commit(s_full(g));
                 umma_commit(ring_empty(slot));
-                ends = c.item_ends();
-                if (ends || t == n_tiles - 1) umma_commit(q_empty(b));
-                ++seq;
-                c.next(p.w);
-                return true;
-            };
+                if (c.item_ends() || t == n_tiles - 1) umma_commit(q_empty(b));
+            }
+            if (!ok) atomicExch(p.w.err_flag, kErrTreeWait);
+        }
+    } else if (warp == 2 && n_tiles > 0) {
+        // ---------------- the outputs
+        if (lane == 0) {
+            TreeCursor c = run->at;
             uint32_t uses0 = 0, uses1 = 0;             // pieces that have used each output accumulator
             int rel = 0;                               // tile within its piece
-            if (!issue_s(0)) ok = false;
-            for (int t = 0; t < n_tiles && ok; ++t) {
+            bool ok = true;
+            for (int t = 0; t < n_tiles; ++t, c.next(p.w)) {
                 const int g = t & 1;
-                const bool last = ends;
-                if (t + 1 < n_tiles && !issue_s(t + 1)) { ok = false; break; }
                 if (rel < 2) {                         // the accumulator's last piece has been read out
                     uint32_t& uses = g ? uses1 : uses0;
                     if (uses > 0 && !mbar_poll(o_empty(g), (uses - 1) & 1u)) { ok = false; break; }
                     ++uses;
                 }
+                const uint32_t seq = t >= n_tiles - 2 ? (uint32_t)(n_tiles + t) : 2u * t + 3u;
                 const int slot = seq % NS;
-                if (!mbar_poll(p_full(g), (t >> 1) & 1u) || !mbar_poll(ring_full(slot), (seq / NS) & 1u)) { ok = false; break; }
+                if (!mbar_poll(p_full(g), (t >> 1) & 1u) || !slot_filled(slot, seq)) { ok = false; break; }
                 tc_fence_after();
-                const uint32_t va = base + Cfg::kOffRing + slot * Cfg::kTileBytes;
+                const uint32_t va = base + Cfg::kOffRing + slot * Cfg::kTileBytes, pa = base + Cfg::kOffP + g * Cfg::kPBytes;
 #pragma unroll
                 for (int k = 0; k < kKeys / 16; ++k)
-                    umma_f16_ta(tmem_o + 128u * g, tmem_s + 128u * g + 8u * k, smem_desc_sw128_mn(va + k * 2 * tree_group_bytes<DH>(), 1024, tree_group_bytes<DH>()), kIdescO,
-                                (rel >= 2 || k > 0) ? 1u : 0u);
+                    umma_bf16(tmem_o + 128u * g, smem_desc_sw128(pa + (k >> 2) * (kRows * 128)) + (uint64_t)(2 * (k & 3)),
+                              smem_desc_sw128_mn(va + k * 2 * tree_group_bytes<DH>(), 1024, tree_group_bytes<DH>()),
+                              kIdesc | (1u << 16) | ((uint32_t)(DH >> 3) << 17), (rel >= 2 || k > 0) ? 1u : 0u);      // bit 16: B is MN-major
                 umma_commit(o_full(g));
                 umma_commit(ring_empty(slot));
-                ++seq;
-                rel = last ? 0 : rel + 1;
+                rel = c.item_ends() ? 0 : rel + 1;
             }
             if (!ok) atomicExch(p.w.err_flag, kErrTreeWait);
         }
@@ -175,7 +191,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         float2* const xch = reinterpret_cast<float2*>(sp + Cfg::kOffX);      // [2][128]
         TreeCursor c = run->at;
         bool split_front = !c.item_begins();
-        float m_ref = -INFINITY, l_run = 0.0f;
+        float m_ref = kNoRef, l_run = 0.0f;
         int first = 0, kt_first = 0;                   // first tile of the piece, its key tile
         uint32_t piece = 0, merges = 0;
         int q0 = 0, nq = 0, tok = 0, hg = 0;
@@ -188,7 +204,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 tok = (q0 + row) / p.w.group;
                 hg = q0 + row - tok * p.w.group;
                 if (p.tree_mask && row < nq) mask = p.tree_mask + (size_t)(c.r.row0 + tok) * p.mask_words;
-                m_ref = -INFINITY; l_run = 0.0f;
+                m_ref = kNoRef; l_run = 0.0f;
             }
             const int C = c.r.L - c.r.n;
             const bool warp_live = quarter * 32 < nq;
@@ -196,16 +212,19 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 if (!wait_all(s_full(g), (t >> 1) & 1u)) { ok = false; break; }
                 tc_fence_after();
                 const bool tail = (c.kt + 1) * kKeys > C;
+                // the group's P tile and outputs: behind the product of its tile before
+                if (t >= 2 && !wait_all(o_full(g), ((t >> 1) & 1u) ^ 1u)) { ok = false; break; }
+                tc_fence_after();
                 if (tail) {
-                    const uint32_t vseq = t == n_tiles - 1 ? 2u * n_tiles - 1u : 2u * t + 2u;
-                    if (!wait_all(ring_full(vseq % NS), (vseq / NS) & 1u)) { ok = false; break; }
+                    const uint32_t vseq = t >= n_tiles - 2 ? (uint32_t)(n_tiles + t) : 2u * t + 3u;
+                    if (!__all_sync(0xffffffffu, slot_filled(vseq % NS, vseq))) { ok = false; break; }
                     if (tree_clean_values<DH, Ops::kExpMask>(sp + Cfg::kOffRing + (vseq % NS) * Cfg::kTileBytes, max(C - c.kt * kKeys, 0),
                                                              c.r.L - c.kt * kKeys, tid & 127))
                         odd_piece[piece & 1u] = piece + 1;
                 }
                 if (warp_live) {
-                    // Two passes over the scores, which stay in TMEM, in chunks of 32 columns.  Loops on purpose: unrolled, the
-                    // steady state does not fit the schedulers' instruction caches.
+                    // The scores stay in TMEM and are taken in chunks of 32 columns.  Loops on purpose: unrolled, the steady state does
+                    // not fit the schedulers' instruction caches.
                     auto fetch = [&](int q, uint32_t (&s)[32]) {
                         tmem_ld32(ts + 32u * q, s);
                         const uint32_t vis = !tail ? 0xFFFFFFFFu : (row < nq ? visible_word(c.kt * kKeys + 32 * q, C, c.r.n, tok, mask, p.mask_words) : 0u);
@@ -216,61 +235,70 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                                 if (!((vis >> e) & 1u)) s[e] = __float_as_uint(-INFINITY);
                         }
                     };
-                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    const bool opens = t - first < 2;            // the group's first tile of the piece
+                    if (opens) {
+                        float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll 1
-                    for (int q = 0; q < 4; ++q) {
-                        uint32_t s[32];
-                        fetch(q, s);
+                        for (int q = 0; q < 4; ++q) {
+                            uint32_t s[32];
+                            fetch(q, s);
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) t4[(e >> 1) & 3] = fmaxf(t4[(e >> 1) & 3], fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
+                            for (int e = 0; e < 32; e += 2) t4[(e >> 1) & 3] = fmaxf(t4[(e >> 1) & 3], fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
+                        }
+                        // weights 2^(score - reference): the largest is 2^kBias .. 2^(kBias + 8)
+                        m_ref = fmaxf(fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * p.scale_log2 - Ops::kBias, kNoRef);
                     }
-                    float mx = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
-                    mx = mx * p.scale_log2 - Ops::kBias;         // weights 2^(score - reference): the largest is 2^kBias .. 2^(kBias + 8)
-                    if (t - first < 2) {
-                        m_ref = mx;                              // the group's first tile of the piece
-                    } else {
-                        const bool grow = row < nq && mx > m_ref + kTreeSlack;
-                        if (__any_sync(0xffffffffu, grow)) {
-                            // rare: rescale the rows' outputs, after the group's previous product has completed
-                            if (!wait_all(o_full(g), ((t >> 1) & 1u) ^ 1u)) { ok = false; break; }
-                            tc_fence_after();
-                            const float f = grow ? tree_ex2(m_ref - mx) : 1.0f;
+                    uint8_t* const prow = sp + Cfg::kOffP + g * Cfg::kPBytes + row * 128;
+                    float sum4[4];
 #pragma unroll 1
-                            for (int c0 = 0; c0 < DH; c0 += 32) {
-                                uint32_t o[32];
-                                const uint32_t at = tmem_o + 128u * g + t_lane + (uint32_t)c0;
-                                tmem_ld32(at, o);
-                                tmem_ld_wait();
+                    for (int turn = 0; turn < 2; ++turn) {
+                        float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                                tmem_store32(at, o);
+                        for (int e = 0; e < 4; ++e) sum4[e] = 0.0f;
+#pragma unroll 1
+                        for (int q = 0; q < 4; ++q) {
+                            uint32_t s[32];
+                            fetch(q, s);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                uint32_t w[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const float sa = __uint_as_float(s[8 * i + 2 * e]), sb = __uint_as_float(s[8 * i + 2 * e + 1]);
+                                    t4[e] = fmaxf(t4[e], fmaxf(sa, sb));
+                                    const float a = tree_ex2(fmaf(sa, p.scale_log2, -m_ref)), b = tree_ex2(fmaf(sb, p.scale_log2, -m_ref));
+                                    sum4[e] += a + b;
+                                    w[e] = Ops::pack(a, b);
+                                }
+                                const int ch = 4 * (q & 1) + i;
+                                *reinterpret_cast<uint4*>(prow + (q >> 1) * (kRows * 128) + ((ch ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
                             }
-                            tmem_store_wait();
-                            l_run *= f;
-                            if (grow) m_ref = mx;
                         }
-                    }
-                    const float ref = m_ref == -INFINITY ? 0.0f : m_ref;     // nothing seen yet: every weight is 0
-                    float sum4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                        const float to = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * p.scale_log2 - Ops::kBias;
+                        const bool grow = !opens && row < nq && to > m_ref + kTreeSlack;
+                        if (turn || !__any_sync(0xffffffffu, grow)) break;
+                        // rare: move the reference, bring the row's outputs and sum to it, and form the weights again
+                        const float f = grow ? tree_ex2(m_ref - to) : 1.0f;
 #pragma unroll 1
-                    for (int q = 0; q < 4; ++q) {                // the weights go over scores that have been read
-                        uint32_t s[32], w[16];
-                        fetch(q, s);
+                        for (int c0 = 0; c0 < DH; c0 += 32) {
+                            uint32_t o[32];
+                            const uint32_t at = tmem_o + 128u * g + t_lane + (uint32_t)c0;
+                            tmem_ld32(at, o);
+                            tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const float a = tree_ex2(fmaf(__uint_as_float(s[2 * e]), p.scale_log2, -ref)), b = tree_ex2(fmaf(__uint_as_float(s[2 * e + 1]), p.scale_log2, -ref));
-                            sum4[(2 * e) & 3] += a;
-                            sum4[(2 * e + 1) & 3] += b;
-                            w[e] = Ops::pack(a, b);
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tmem_store32(at, o);
                         }
-                        store16(ts + 16u * q, w);
+                        tmem_store_wait();
+                        l_run *= f;
+                        if (grow) m_ref = to;
                     }
-                    tmem_store_wait();
                     l_run += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
                 }
+                fence_async_smem();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full(g));
+                if (lane == 0) { mbar_arrive(s_empty(g)); mbar_arrive(p_full(g)); }
             }
             const bool item_ends = c.item_ends();
             if (item_ends || t == n_tiles - 1) {
@@ -289,9 +317,8 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                         ++merges;
                         const float2 a = xch[row], b = xch[kRows + row];
                         m = fmaxf(a.x, b.x);
-                        const float ref = m == -INFINITY ? 0.0f : m;
-                        fa = tree_ex2(a.x - ref);
-                        fb = tree_ex2(b.x - ref);
+                        fa = tree_ex2(a.x - m);
+                        fb = tree_ex2(b.x - m);
                         l = a.y * fa + b.y * fb;
                     }
                     tc_fence_after();

@@ -92,9 +92,10 @@ __device__ __forceinline__ uint32_t visible_word(int k0, int C, int n, int i, co
 // TMA box fetches all of a page's keys of a head.
 template <int DH> __host__ __device__ constexpr int tree_group_bytes() { return DH / 64 * 1024; }
 
-// K and V tiles, by a whole warp: K(0), K(1), V(0), K(2), V(1), ..., the order in which the products consume them.  Every lane
-// fetches one page (or 128 keys of a larger one), and reads its entry of the block table two tiles ahead.
-template <int DH, int NS>
+// K and V tiles, by a whole warp, in the order in which the products consume them: K LEAD tiles ahead of V (LEAD = 1: K(0), K(1),
+// V(0), K(2), V(1), ...; 2: K(0), K(1), K(2), V(0), K(3), V(1), ...).  Every lane fetches one page (or 128 keys of a larger one), and
+// reads its entry of the block table two tiles ahead.
+template <int DH, int NS, int LEAD>
 __device__ __forceinline__ void tree_load_keys(const TcParams& p, const CUtensorMap* map_k, const CUtensorMap* map_v, const TreeRun* run,
                                                uint32_t ring, uint32_t full, uint32_t empty) {
     constexpr int kTileBytes = kKeys * DH * 2, kGroup = tree_group_bytes<DH>();
@@ -129,14 +130,16 @@ __device__ __forceinline__ void tree_load_keys(const TcParams& p, const CUtensor
         ++seq;
         return true;
     };
-    Box prev{}, cur{}, next{}, after{};
+    Box last[LEAD] = {}, cur{}, next{}, after{};               // last: the tiles whose V is still to come, latest first
     look_up(cur);
     if (n_tiles > 1) { c.next(p.w); look_up(next); }
-    for (int t = 0; t <= n_tiles && ok; ++t) {
+    for (int t = 0; t < n_tiles + LEAD && ok; ++t) {
         if (t < n_tiles && !fetch(map_k, cur)) { ok = false; break; }
         if (t + 2 < n_tiles) { c.next(p.w); look_up(after); }
-        if (t > 0 && !fetch(map_v, prev)) { ok = false; break; }
-        prev = cur;
+        if (t >= LEAD && !fetch(map_v, last[LEAD - 1])) { ok = false; break; }
+#pragma unroll
+        for (int i = LEAD - 1; i > 0; --i) last[i] = last[i - 1];
+        last[0] = cur;
         cur = next;
         next = after;
     }
