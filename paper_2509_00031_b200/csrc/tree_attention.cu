@@ -319,7 +319,7 @@ int tree_grid() {
 }
 
 size_t tree_attention_scratch_bytes(int type, int d_head) {
-    const int tile_rows = type == kTypeF32 ? kSimtRows : 128;
+    const int tile_rows = type == kTypeF32 ? kSimtRows : 256;
     return kTailBytes + 2 * (size_t)(type == kTypeF32 ? kMaxTreeGrid : kMaxTreeGrid / 2) * tree_slot_floats(tile_rows, d_head) * 4;
 }
 

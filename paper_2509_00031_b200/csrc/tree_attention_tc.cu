@@ -4,22 +4,21 @@
 //                                                                            the drafts j (t = C + j) whose mask bit is set
 //
 // This file: many queries per key head (wide trees, grouped heads); the host sends fewer to tree_attention_keys.cu.  The queries
-// that read one key head - every draft times the g heads of the group - share 128-row tiles, so each cached byte is fetched once per
-// request, key head and 128 queries.  A tile of 128 keys at d_head 128 costs 1024 cycles of the tensor pipe and 1024 of the
-// exponential unit against some 2800 of an SM's share of the memory: the kernel is bound by the products from about three row
-// tiles per key head on, where the copies come from L2.
+// that read one key head - every draft times the g heads of the group - share row tiles of 256, so each cached byte is fetched once
+// per request, key head and 256 queries.  For 256 queries a tile of 128 keys at d_head 128 costs 2048 cycles of the tensor pipe
+// and 2048 of the exponential unit against some 2800 of an SM's share of the memory.  (With two tiles of 128 queries apart the
+// second reads the keys again long after they have left L2: 4 contexts of 60-120 thousand keys, 64 drafts, 540 us.)
 //
 // One persistent CTA per SM, 12 warps; the key tiles of all requests are dealt out in equal runs (tree_attention.cuh):
-//   warp 0      K and V tiles by TMA into a ring; warp 3: query tiles into two buffers, a piece ahead
-//   warps 1, 2  one thread issues S = Q K^T into one of two TMEM score buffers as soon as its last scores have been read,
-//               another O += P V with P from shared memory and V as it lies in the page (keys along k, so no transposition): the
-//               waits and commits of one thread for both left the tensor pipe idle for more than half of the time
-//   warps 4-7, 8-11  two softmax groups take alternate tiles.  A thread owns a query row: it reads the tile's 128 scores and
-//               writes the weights, rounded to the cache's type, to the group's own P tile, so that the scores of its next
-//               tile form while the product with V runs.  Each group has a reference, a sum and an output accumulator of its
-//               own, so the groups need not agree on anything until the piece ends, when the two results are joined.  The
-//               weights are formed against the reference as it stands; where a row's maximum turns out to have grown by more
-//               than 2^8 the reference moves and the tile's weights are formed again.
+//   warp 0      K and V tiles by TMA into a ring; warp 3: the query tile of the next piece
+//   warps 1, 2  one thread issues S = Q K^T as soon as the scores before have been read, another O += P V with P from shared
+//               memory and V as it lies in the page (keys along k, so no transposition): the waits and commits of one thread for
+//               both left the tensor pipe idle for more than half of the time
+//   warps 4-7, 8-11  two softmax groups, each for 128 of the queries, with score, weight and output tiles of its own; while one
+//               forms weights, the tensor pipe works for the other.  A thread owns a query row: it reads the tile's 128 scores
+//               and writes the weights, rounded to the cache's type, to shared memory.  The weights are formed against the
+//               reference as it stands; where a row's maximum turns out to have grown by more than 2^8 the reference moves
+//               and the tile's weights are formed again.  A tile of up to 128 queries leaves the second group idle.
 // Rounding: the products are exact in binary32 up to accumulation; the weights are rounded to 11 (fp16) or 8 (bf16) bits for
 // the second product, the sums are formed from the unrounded weights, the output is rounded once.  fp16 weights are scaled by
 // 2^7, which keeps small ones out of the subnormals; the largest is then 2^15.
@@ -33,18 +32,17 @@
 namespace zq {
 namespace {
 
-constexpr int kTcThreads = 384, kRows = 128;
+constexpr int kTcThreads = 384, kRows = 128, kTileRows = 2 * kRows;     // rows per group, rows per tile
 constexpr float kNoRef = -1.0e30f;       // reference of a row that has seen nothing: any score passes it
 
 template <int DH> struct TcCfg {
-    static constexpr int kTileBytes = kKeys * DH * 2;                       // one K, V or Q tile
+    static constexpr int kTileBytes = kKeys * DH * 2;                       // one K or V tile
     static constexpr int kPBytes = kRows * kKeys * 2;                       // [half of the keys][128 rows][128 bytes], as Q
     static constexpr int kStages = DH == 128 ? 3 : 7;
-    static constexpr int kOffRing = 2 * kTileBytes;
+    static constexpr int kOffRing = kTileRows * DH * 2;                     // the query tile comes first
     static constexpr int kOffP = kOffRing + kStages * kTileBytes;
-    static constexpr int kOffX = kOffP + 2 * kPBytes;                       // (reference, sum) of every row: [2 groups][128][2]
-    static constexpr int kOffBar = kOffX + 2048;
-    static constexpr int kBars = 2 * kStages + 15;
+    static constexpr int kOffBar = kOffP + 2 * kPBytes;
+    static constexpr int kBars = 2 * kStages + 12;
     static constexpr int kOffMisc = kOffBar + kBars * 8;                    // TMEM base, non-finite marks, run
     static constexpr int kUsedBytes = kOffMisc + 32 + 192 + (int)sizeof(TreeRun);
     static constexpr int kSmemBytes = kUsedBytes + 1024 > 232448 ? 232448 : kUsedBytes + 1024;
@@ -73,22 +71,20 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     const uint32_t bars = base + Cfg::kOffBar;
     auto ring_full = [&](int s) { return bars + 8u * s; };
     auto ring_empty = [&](int s) { return bars + 8u * (NS + s); };
-    auto q_full = [&](int s) { return bars + 8u * (2 * NS + s); };
-    auto q_empty = [&](int s) { return bars + 8u * (2 * NS + 2 + s); };
-    auto s_full = [&](int g) { return bars + 8u * (2 * NS + 4 + g); };
-    auto s_empty = [&](int g) { return bars + 8u * (2 * NS + 6 + g); };
-    auto p_full = [&](int g) { return bars + 8u * (2 * NS + 8 + g); };
-    auto o_full = [&](int g) { return bars + 8u * (2 * NS + 10 + g); };
-    auto o_empty = [&](int g) { return bars + 8u * (2 * NS + 12 + g); };
-    const uint32_t x_full = bars + 8u * (2 * NS + 14);
+    const uint32_t q_full = bars + 8u * (2 * NS), q_empty = q_full + 8u;
+    auto s_full = [&](int g) { return bars + 8u * (2 * NS + 2 + g); };
+    auto s_empty = [&](int g) { return bars + 8u * (2 * NS + 4 + g); };
+    auto p_full = [&](int g) { return bars + 8u * (2 * NS + 6 + g); };
+    auto o_full = [&](int g) { return bars + 8u * (2 * NS + 8 + g); };
+    auto o_empty = [&](int g) { return bars + 8u * (2 * NS + 10 + g); };
     volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc);
     volatile uint32_t* odd_piece = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 8);   // [2]: piece + 1 with a non-finite draft value
     long long* part = reinterpret_cast<long long*>(sp + Cfg::kOffMisc + 32);
     TreeRun* run = reinterpret_cast<TreeRun*>(sp + Cfg::kOffMisc + 32 + 192);
 
     if (tid < Cfg::kBars) {
-        const int i = tid - 2 * NS;              // one barrier a thread: ring full, ring empty; then as above
-        mbar_init(bars + 8u * tid, i < 6 ? 1 : (i < 10 ? 4 : (i < 12 ? 1 : 8)));
+        const int i = tid - 2 * NS;              // one barrier a thread; s empty, p full and o empty count a group's warps
+        mbar_init(bars + 8u * tid, (i >= 4 && i < 8) || i >= 10 ? 4 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (tid < 2) odd_piece[tid] = 0;
@@ -120,35 +116,43 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     };
 
     if (warp == 0 && n_tiles > 0) {
-        tree_load_keys<DH, NS, 2>(p, &map_k, &map_v, run, base + Cfg::kOffRing, ring_full(0), ring_empty(0));
+        tree_load_keys<DH, NS, 1>(p, &map_k, &map_v, run, base + Cfg::kOffRing, ring_full(0), ring_empty(0));
     } else if (warp == 3 && n_tiles > 0) {
-        tree_load_queries<DH, kRows, 32, T>(p, run, sp, nullptr, 0u, q_full(0), q_empty(0), lane);
+        tree_load_queries<DH, kTileRows, 32, 1, T>(p, run, sp, nullptr, 0u, q_full, q_empty, lane);
     } else if (warp == 1 && n_tiles > 0) {
         // ---------------- the scores
         if (lane == 0) {
             TreeCursor c = run->at;
-            uint32_t piece = 0, b = 0;
+            uint32_t piece = 0, done[2] = {0, 0};      // score tiles issued for each group
+            int groups = 0;
             bool ok = true;
-            for (int t = 0; t < n_tiles; ++t, c.next(p.w)) {
-                const uint32_t seq = t < 2 ? t : 2u * t - 2u;
-                const int slot = seq % NS, g = t & 1;
+            for (int t = 0; t < n_tiles && ok; ++t, c.next(p.w)) {
+                const uint32_t seq = t == 0 ? 0u : 2u * t - 1u;
+                const int slot = seq % NS;
                 if (t == 0 || c.item_begins()) {
-                    b = piece & 1u;
-                    if (!mbar_poll(q_full(b), (piece >> 1) & 1u)) { ok = false; break; }
+                    if (!mbar_poll(q_full, piece & 1u)) { ok = false; break; }
                     ++piece;
+                    groups = c.queries(p.w) > kRows ? 2 : 1;
                 }
-                if (!mbar_poll(s_empty(g), ((t >> 1) & 1u) ^ 1u) || !slot_filled(slot, seq)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t qa = base + b * Cfg::kTileBytes, ka = base + Cfg::kOffRing + slot * Cfg::kTileBytes;
+                if (!slot_filled(slot, seq)) { ok = false; break; }
+                const uint32_t ka = base + Cfg::kOffRing + slot * Cfg::kTileBytes;
 #pragma unroll
-                for (int k = 0; k < DH / 16; ++k) {
-                    const uint64_t da = smem_desc_sw128(qa + (k >> 2) * (kRows * 128)) + (uint64_t)(2 * (k & 3));
-                    const uint64_t db = smem_desc_sw128(ka + (k >> 2) * 1024, tree_group_bytes<DH>()) + (uint64_t)(2 * (k & 3));
-                    umma_bf16(tmem_s + 128u * g, da, db, kIdesc | ((uint32_t)(kKeys >> 3) << 17), k > 0 ? 1u : 0u);
+                for (int g = 0; g < 2; ++g) {
+                    if (g == groups) break;
+                    if (done[g] > 0 && !mbar_poll(s_empty(g), (done[g] - 1) & 1u)) { ok = false; break; }
+                    ++done[g];
+                    tc_fence_after();
+#pragma unroll
+                    for (int k = 0; k < DH / 16; ++k) {
+                        const uint64_t da = smem_desc_sw128(base + g * (kRows * 128) + (k >> 2) * (kTileRows * 128)) + (uint64_t)(2 * (k & 3));
+                        const uint64_t db = smem_desc_sw128(ka + (k >> 2) * 1024, tree_group_bytes<DH>()) + (uint64_t)(2 * (k & 3));
+                        umma_bf16(tmem_s + 128u * g, da, db, kIdesc | ((uint32_t)(kKeys >> 3) << 17), k > 0 ? 1u : 0u);
+                    }
+                    umma_commit(s_full(g));
                 }
-                umma_commit(s_full(g));
+                if (!ok) break;
                 umma_commit(ring_empty(slot));
-                if (c.item_ends() || t == n_tiles - 1) umma_commit(q_empty(b));
+                if (c.item_ends() || t == n_tiles - 1) umma_commit(q_empty);
             }
             if (!ok) atomicExch(p.w.err_flag, kErrTreeWait);
         }
@@ -156,70 +160,76 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         // ---------------- the outputs
         if (lane == 0) {
             TreeCursor c = run->at;
-            uint32_t uses0 = 0, uses1 = 0;             // pieces that have used each output accumulator
-            int rel = 0;                               // tile within its piece
-            bool ok = true;
-            for (int t = 0; t < n_tiles; ++t, c.next(p.w)) {
-                const int g = t & 1;
-                if (rel < 2) {                         // the accumulator's last piece has been read out
-                    uint32_t& uses = g ? uses1 : uses0;
-                    if (uses > 0 && !mbar_poll(o_empty(g), (uses - 1) & 1u)) { ok = false; break; }
-                    ++uses;
+            uint32_t done[2] = {0, 0}, uses[2] = {0, 0};         // weight tiles taken, pieces begun, for each group
+            int groups = 0;
+            bool ok = true, first = true;                        // first: the tile opens its piece
+            for (int t = 0; t < n_tiles && ok; ++t, c.next(p.w)) {
+                if (first) {
+                    // the outputs of both groups' last pieces have been read (for an idle group too: none falls behind by more than a piece)
+                    groups = c.queries(p.w) > kRows ? 2 : 1;
+                    for (int g = 0; g < 2; ++g) {
+                        if (uses[g] > 0 && !mbar_poll(o_empty(g), (uses[g] - 1) & 1u)) { ok = false; break; }
+                        if (g < groups) ++uses[g];
+                    }
+                    if (!ok) break;
                 }
-                const uint32_t seq = t >= n_tiles - 2 ? (uint32_t)(n_tiles + t) : 2u * t + 3u;
+                const uint32_t seq = t == n_tiles - 1 ? 2u * n_tiles - 1u : 2u * t + 2u;
                 const int slot = seq % NS;
-                if (!mbar_poll(p_full(g), (t >> 1) & 1u) || !slot_filled(slot, seq)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t va = base + Cfg::kOffRing + slot * Cfg::kTileBytes, pa = base + Cfg::kOffP + g * Cfg::kPBytes;
 #pragma unroll
-                for (int k = 0; k < kKeys / 16; ++k)
-                    umma_bf16(tmem_o + 128u * g, smem_desc_sw128(pa + (k >> 2) * (kRows * 128)) + (uint64_t)(2 * (k & 3)),
-                              smem_desc_sw128_mn(va + k * 2 * tree_group_bytes<DH>(), 1024, tree_group_bytes<DH>()),
-                              kIdesc | (1u << 16) | ((uint32_t)(DH >> 3) << 17), (rel >= 2 || k > 0) ? 1u : 0u);      // bit 16: B is MN-major
-                umma_commit(o_full(g));
-                umma_commit(ring_empty(slot));
-                rel = c.item_ends() ? 0 : rel + 1;
+                for (int g = 0; g < 2; ++g) {
+                    if (g == groups) break;
+                    if (!mbar_poll(p_full(g), done[g] & 1u) || (g == 0 && !slot_filled(slot, seq))) { ok = false; break; }
+                    ++done[g];
+                    tc_fence_after();
+                    const uint32_t va = base + Cfg::kOffRing + slot * Cfg::kTileBytes, pa = base + Cfg::kOffP + g * Cfg::kPBytes;
+#pragma unroll
+                    for (int k = 0; k < kKeys / 16; ++k)
+                        umma_bf16(tmem_o + 128u * g, smem_desc_sw128(pa + (k >> 2) * (kRows * 128)) + (uint64_t)(2 * (k & 3)),
+                                  smem_desc_sw128_mn(va + k * 2 * tree_group_bytes<DH>(), 1024, tree_group_bytes<DH>()),
+                                  kIdesc | (1u << 16) | ((uint32_t)(DH >> 3) << 17), (!first || k > 0) ? 1u : 0u);      // bit 16: B is MN-major
+                    if (g == groups - 1) umma_commit(ring_empty(slot));
+                    umma_commit(o_full(g));                      // the last: once it has arrived, none of the thread's arrivals is to come
+                }
+                if (!ok) break;
+                first = c.item_ends();
             }
             if (!ok) atomicExch(p.w.err_flag, kErrTreeWait);
         }
     } else if (warp >= 4 && n_tiles > 0) {
         // ---------------- softmax groups
-        const int g = (warp >> 2) - 1;                 // 0: even tiles, 1: odd tiles
-        const int quarter = warp & 3, row = quarter * 32 + lane;
+        const int g = (warp >> 2) - 1, quarter = warp & 3, row = quarter * 32 + lane;        // row of the group
         const uint32_t t_lane = (uint32_t)(quarter * 32) << 16;
         const uint32_t ts = tmem_s + 128u * g + t_lane;
-        float2* const xch = reinterpret_cast<float2*>(sp + Cfg::kOffX);      // [2][128]
         TreeCursor c = run->at;
-        bool split_front = !c.item_begins();
+        bool split_front = !c.item_begins(), ok = true, opens = true;
         float m_ref = kNoRef, l_run = 0.0f;
-        int first = 0, kt_first = 0;                   // first tile of the piece, its key tile
-        uint32_t piece = 0, merges = 0;
-        int q0 = 0, nq = 0, tok = 0, hg = 0;
+        int kt_first = 0, q0 = 0, nq = 0, tok = 0, hg = 0;       // of the group: first query, queries
+        uint32_t piece = 0, done = 0;                            // tiles of this group
         const uint32_t* mask = nullptr;
-        bool ok = true;
         auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_poll(bar, parity)) != 0; };
         for (int t = 0; t < n_tiles && ok; ++t) {
-            if (t == first) {
-                q0 = c.first_query(p.w); nq = c.queries(p.w); kt_first = c.kt;
+            if (opens) {
+                q0 = c.first_query(p.w) + g * kRows;
+                nq = min(kRows, c.queries(p.w) - g * kRows);
+                kt_first = c.kt;
                 tok = (q0 + row) / p.w.group;
                 hg = q0 + row - tok * p.w.group;
                 if (p.tree_mask && row < nq) mask = p.tree_mask + (size_t)(c.r.row0 + tok) * p.mask_words;
                 m_ref = kNoRef; l_run = 0.0f;
             }
             const int C = c.r.L - c.r.n;
-            const bool warp_live = quarter * 32 < nq;
-            if ((t & 1) == g) {
-                if (!wait_all(s_full(g), (t >> 1) & 1u)) { ok = false; break; }
-                tc_fence_after();
+            const bool warp_live = quarter * 32 < nq, item_ends = c.item_ends(), piece_ends = item_ends || t == n_tiles - 1;
+            if (nq > 0) {
                 const bool tail = (c.kt + 1) * kKeys > C;
-                // the group's P tile and outputs: behind the product of its tile before
-                if (t >= 2 && !wait_all(o_full(g), ((t >> 1) & 1u) ^ 1u)) { ok = false; break; }
+                // the scores; and the group's weight tile and outputs are free: behind the product of its tile before
+                if (!wait_all(s_full(g), done & 1u) || (done > 0 && !wait_all(o_full(g), (done - 1) & 1u))) { ok = false; break; }
+                ++done;
                 tc_fence_after();
-                if (tail) {
-                    const uint32_t vseq = t >= n_tiles - 2 ? (uint32_t)(n_tiles + t) : 2u * t + 3u;
+                if (tail && g == 0) {                            // (the second group's product with this tile comes after the first's)
+                    const uint32_t vseq = t == n_tiles - 1 ? 2u * n_tiles - 1u : 2u * t + 2u;
                     if (!__all_sync(0xffffffffu, slot_filled(vseq % NS, vseq))) { ok = false; break; }
                     if (tree_clean_values<DH, Ops::kExpMask>(sp + Cfg::kOffRing + (vseq % NS) * Cfg::kTileBytes, max(C - c.kt * kKeys, 0),
-                                                             c.r.L - c.kt * kKeys, tid & 127))
+                                                             c.r.L - c.kt * kKeys, row))
                         odd_piece[piece & 1u] = piece + 1;
                 }
                 if (warp_live) {
@@ -235,7 +245,6 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                                 if (!((vis >> e) & 1u)) s[e] = __float_as_uint(-INFINITY);
                         }
                     };
-                    const bool opens = t - first < 2;            // the group's first tile of the piece
                     if (opens) {
                         float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll 1
@@ -299,102 +308,70 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) { mbar_arrive(s_empty(g)); mbar_arrive(p_full(g)); }
-            }
-            const bool item_ends = c.item_ends();
-            if (item_ends || t == n_tiles - 1) {
-                const bool both = t > first;                     // the piece used both groups
-                const bool whole = item_ends && !split_front;
-                if (both || (t & 1) == g) {
-                    const int mine = (t & 1) == g ? t : t - 1;   // this group's last tile
-                    if (!wait_all(o_full(g), (mine >> 1) & 1u)) { ok = false; break; }
-                    float m = m_ref, l = l_run, fa = 1.0f, fb = 0.0f;        // factors of O of group 0 and 1 (both) or of the own O
-                    if (both) {
-                        xch[g * kRows + row] = make_float2(m_ref, l_run);
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(x_full);
-                        if (!wait_all(x_full, merges & 1u)) { ok = false; break; }
-                        ++merges;
-                        const float2 a = xch[row], b = xch[kRows + row];
-                        m = fmaxf(a.x, b.x);
-                        fa = tree_ex2(a.x - m);
-                        fb = tree_ex2(b.x - m);
-                        l = a.y * fa + b.y * fb;
-                    }
+                if (piece_ends) {
+                    const bool whole = item_ends && !split_front;
+                    if (!wait_all(o_full(g), (done - 1) & 1u)) { ok = false; break; }
                     tc_fence_after();
                     const bool repair = odd_piece[piece & 1u] == piece + 1;
-                    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                    const int head = c.h * p.w.group + hg;
+                    const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
+                    const int head = c.h * p.w.group + hg, trow = g * kRows + row;
                     T* dst = static_cast<T*>(p.out) + (int64_t)(c.r.row0 + tok) * p.out_stride + (int64_t)head * DH;
-                    float* slot = tree_slot(p.scratch, split_front ? 2 * blockIdx.x : 2 * blockIdx.x + 1, p.w.tile_rows, DH);
-                    const int col0 = both ? g * (DH / 2) : 0, cols = both ? DH / 2 : DH;
+                    float* slot = tree_slot(p.scratch, split_front ? 2 * blockIdx.x : 2 * blockIdx.x + 1, kTileRows, DH);
                     if (warp_live) {
 #pragma unroll 1
-                        for (int c0 = col0; c0 < col0 + cols; c0 += 32) {
+                        for (int c0 = 0; c0 < DH; c0 += 32) {
+                            uint32_t oa[32];
                             float o[32];
-                            {
-                                uint32_t oa[32], ob[32];
-                                if (both) {
-                                    tmem_ld32(tmem_o + t_lane + (uint32_t)c0, oa);
-                                    tmem_ld32(tmem_o + 128u + t_lane + (uint32_t)c0, ob);
-                                    tmem_ld_wait();
+                            tmem_ld32(tmem_o + 128u * g + t_lane + (uint32_t)c0, oa);
+                            tmem_ld_wait();
 #pragma unroll
-                                    for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(oa[e]) * fa + __uint_as_float(ob[e]) * fb;
-                                } else {
-                                    tmem_ld32(tmem_o + 128u * g + t_lane + (uint32_t)c0, oa);
-                                    tmem_ld_wait();
+                            for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(oa[e]);
+                            if (row >= nq) continue;
+                            if (repair) {                        // non-finite values of drafts this row sees, within the piece's tiles
+                                for (int j = 0; j < c.r.n; ++j) {
+                                    const int key = C + j, kt = key / kKeys;
+                                    if (kt < kt_first || kt > c.kt || !(visible_word(key, C, c.r.n, tok, mask, p.mask_words) & 1u)) continue;
+                                    const int64_t off = tree_value_offset(p, c, key);
+                                    if (off < 0) continue;
 #pragma unroll
-                                    for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(oa[e]);
+                                    for (int e = 0; e < 32; ++e) {
+                                        const float x = Ops::value(static_cast<const T*>(p.v)[off + c0 + e]);
+                                        if (!isfinite(x)) o[e] += x;
+                                    }
                                 }
                             }
-                            if (row < nq) {
-                                if (repair) {                    // non-finite values of drafts this row sees, within the piece's tiles
-                                    for (int j = 0; j < c.r.n; ++j) {
-                                        const int key = C + j, kt = key / kKeys;
-                                        if (kt < kt_first || kt > c.kt || !(visible_word(key, C, c.r.n, tok, mask, p.mask_words) & 1u)) continue;
-                                        const int64_t off = tree_value_offset(p, c, key);
-                                        if (off < 0) continue;
+                            if (whole) {
 #pragma unroll
-                                        for (int e = 0; e < 32; ++e) {
-                                            const float x = Ops::value(static_cast<const T*>(p.v)[off + c0 + e]);
-                                            if (!isfinite(x)) o[e] += x;
-                                        }
-                                    }
+                                for (int e = 0; e < 32; e += 8) {
+                                    uint4 w;
+                                    w.x = Ops::pack(o[e] * inv, o[e + 1] * inv); w.y = Ops::pack(o[e + 2] * inv, o[e + 3] * inv);
+                                    w.z = Ops::pack(o[e + 4] * inv, o[e + 5] * inv); w.w = Ops::pack(o[e + 6] * inv, o[e + 7] * inv);
+                                    *reinterpret_cast<uint4*>(dst + c0 + e) = w;
                                 }
-                                if (whole) {
+                            } else {
+                                float* po = slot + 2 * kTileRows + (size_t)trow * DH + c0;
 #pragma unroll
-                                    for (int e = 0; e < 32; e += 8) {
-                                        uint4 w;
-                                        w.x = Ops::pack(o[e] * inv, o[e + 1] * inv); w.y = Ops::pack(o[e + 2] * inv, o[e + 3] * inv);
-                                        w.z = Ops::pack(o[e + 4] * inv, o[e + 5] * inv); w.w = Ops::pack(o[e + 6] * inv, o[e + 7] * inv);
-                                        *reinterpret_cast<uint4*>(dst + c0 + e) = w;
-                                    }
-                                } else {
-                                    float* po = slot + 2 * p.w.tile_rows + (size_t)row * DH + c0;
-#pragma unroll
-                                    for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(po + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-                                }
+                                for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(po + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                             }
                         }
-                        if (!whole && row < nq && col0 == 0) { slot[row] = m; slot[p.w.tile_rows + row] = l; }
+                        if (!whole && row < nq) { slot[trow] = m_ref; slot[kTileRows + trow] = l_run; }
                     }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) {
-                        if (both) { mbar_arrive(o_empty(0)); mbar_arrive(o_empty(1)); }
-                        else mbar_arrive_n(o_empty(g), 2);
-                    }
+                    if (lane == 0) mbar_arrive(o_empty(g));
                 }
+            }
+            if (piece_ends) {
                 if (!item_ends && !split_front && tid == 128) {  // begins here, goes on in the next CTAs
                     TreeTail tl{};
                     tl.last_cta = run->tail_cta;
-                    tl.queries = nq; tl.row0 = c.r.row0; tl.q0 = q0; tl.h = c.h;
+                    tl.queries = c.queries(p.w); tl.row0 = c.r.row0; tl.q0 = c.first_query(p.w); tl.h = c.h;
                     reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x] = tl;
                 }
                 split_front = false;
-                first = t + 1;
                 ++piece;
             }
+            opens = piece_ends;
             c.next(p.w);
         }
         if (!ok && lane == 0) atomicExch(p.w.err_flag, kErrTreeWait);
@@ -467,7 +444,7 @@ int launch_tree_attention_tc(const TreeAttnArgs& a, cudaStream_t s, bool depende
     const long long want = a.rows <= a.batch ? group : (3 * drafts + 2 * a.batch - 1) / (2 * a.batch);     // 1.5 x the average
     const int nq = want <= 16 ? 16 : (want <= 32 ? 32 : (want <= 64 ? 64 : kRows));
     p.w = TreeWork{a.kv_len, a.row_start, a.block_table, a.batch, a.rows, a.n_heads, a.cache.n_kv_heads, a.max_pages, a.cache.page_size,
-                   group, nq, kKeys, 4, a.err_flag};
+                   group, nq < kRows ? nq : kTileRows, kKeys, 4, a.err_flag};
     p.q = a.q; p.q_stride = a.q_stride;
     p.box_keys = a.cache.page_size < kKeys ? a.cache.page_size : kKeys;
     p.n_pages = a.cache.n_pages; p.mask_words = a.mask_words; p.tree_mask = a.tree_mask;

@@ -63,9 +63,6 @@ __device__ __forceinline__ void store16(uint32_t taddr, const uint32_t (&v)[16])
         : "memory");
 }
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void mbar_arrive_n(uint32_t bar, uint32_t n) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
-}
 
 // Bits of the 32 keys from k0 on that draft i sees.
 __device__ __forceinline__ uint32_t visible_word(int k0, int C, int n, int i, const uint32_t* mask, int words) {
@@ -150,10 +147,10 @@ __device__ __forceinline__ void tree_load_keys(const TcParams& p, const CUtensor
 }
 
 // Query tiles, by THREADS threads (whole warps; `lane`: which of them), a piece ahead of the products: rows of 128 bytes, 128-byte
-// swizzle, [half][NQ rows].  Rows behind the tile's last query keep what they hold; their results are not used.  full counts one
-// arrival per warp.  masks (may be NULL): [2][NQ][kMaskWords], the first words of the drafts' masks, draft by draft; done: four
+// swizzle, [half][NQ rows], BUFFERS buffers in turn.  Rows behind the tile's last query keep what they hold; their results are
+// not used.  full counts one arrival per warp.  masks (may be NULL): [2][NQ][kMaskWords], the first words of the drafts' masks, draft by draft; done: four
 // barriers, by piece modulo 4, after which a piece's masks are no longer read.
-template <int DH, int NQ, int THREADS, typename T>
+template <int DH, int NQ, int THREADS, int BUFFERS, typename T>
 __device__ __forceinline__ void tree_load_queries(const TcParams& p, const TreeRun* run, uint8_t* q_tiles, uint32_t* masks, uint32_t done, uint32_t full,
                                                   uint32_t empty, int lane) {
     constexpr int kChunks = DH / 8, kTileBytes = NQ * DH * 2, kRowsPer = THREADS / kChunks, kFly = NQ / kRowsPer < 8 ? NQ / kRowsPer : 8;
@@ -163,8 +160,8 @@ __device__ __forceinline__ void tree_load_queries(const TcParams& p, const TreeR
     uint32_t piece = 0;
     for (int t = 0; t < n_tiles; ++t, c.next(p.w)) {
         if (t != 0 && !c.item_begins()) continue;
-        const uint32_t b = piece & 1u;
-        if (!__all_sync(0xffffffffu, mbar_wait(empty + 8u * b, ((piece >> 1) & 1u) ^ 1u))) { atomicExch(p.w.err_flag, kErrTreeWait); return; }
+        const uint32_t b = piece % BUFFERS;
+        if (!__all_sync(0xffffffffu, mbar_wait(empty + 8u * b, ((piece / BUFFERS) & 1u) ^ 1u))) { atomicExch(p.w.err_flag, kErrTreeWait); return; }
         const int q0 = c.first_query(p.w), nq = c.queries(p.w);
         const T* base = static_cast<const T*>(p.q) + (int64_t)c.r.row0 * p.q_stride + (int64_t)c.h * p.w.group * DH + 8 * ch;
         uint8_t* dst = q_tiles + b * kTileBytes + (ch >> 3) * (NQ * 128);

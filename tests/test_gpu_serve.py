@@ -350,7 +350,7 @@ def test_attention_matches_the_definition(zq, case):
 def test_attention_with_steep_scores_and_strided_rows(zq, dtype):
     # scores of some hundreds: the running reference moves often, most weights vanish
     pr = attention_problem(11, dtype, 4, 2, 128, 16, "token", [700, 45], [6, 9], "tree", gap=1, q_scale=30.0)
-    scratch = torch.full((24 << 20,), 255, dtype=torch.uint8, device="cuda")
+    scratch = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")
     got = run_attention(zq, pr, scratch=scratch)                        # (scratch full of NaN)
     want, bound = attention_oracle(pr)
     off = (got[:pr["rows"]].double() - want).abs()
@@ -403,7 +403,7 @@ def test_attention_captured_and_replayed_as_lengths_change(zq):
     # one graph; the lengths, tables and rows in its buffers change between replays (fewer tokens, other requests, none at all)
     big = attention_problem(9, "bf16", 8, 2, 128, 16, "token", [900, 40, 3], [5, 5, 5], "tree")
     out, err = torch.zeros_like(big["q"]), torch.zeros(1, dtype=torch.int32, device="cuda")
-    scratch = torch.empty(24 << 20, dtype=torch.uint8, device="cuda")
+    scratch = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
     call = lambda: zq.zoqat_op_tree_attention(big["q"], big["k"], big["v"], big["table"], big["kv_len"], big["row_start"], tree_mask=big["mask"],  # noqa: E731
                                               out=out, scratch=scratch, err=err)
     call()
