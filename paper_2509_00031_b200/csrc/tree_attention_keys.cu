@@ -53,13 +53,6 @@ template <int DH, int N> struct KeyCfg {
 };
 
 // 16 scores of the thread's key (16 outputs or sums of its column)
-__device__ __forceinline__ void load16(uint32_t taddr, uint32_t (&v)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
-          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-        : "r"(taddr) : "memory");
-}
 // Largest v[i] over the warp's 32 lanes, for 16 values at once: lanes 2 i and 2 i + 1 return that of v[i].
 __device__ __forceinline__ float largest16(float (&v)[16]) {
     const int lane = threadIdx.x & 31;
@@ -162,7 +155,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
     constexpr uint32_t kIdesc = (1u << 4) | (Ops::kFormat << 7) | (Ops::kFormat << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 
     if (warp == 0 && n_tiles > 0) {
-        tree_load_keys<DH, NS, 1>(p, &map_k, &map_v, run, base, ring_full(0), ring_empty(0));
+        tree_load_keys<DH, NS>(p, &map_k, &map_v, run, base, ring_full(0), ring_empty(0));
     } else if (warp == 3 && n_tiles > 0) {
         tree_load_queries<DH, N, 32, 2, T>(p, run, sp + Cfg::kOffQ, reinterpret_cast<uint32_t*>(sp + Cfg::kOffMask), piece_done(0), q_full(0), q_empty(0), lane);
     } else if (warp == 1 && n_tiles > 0) {

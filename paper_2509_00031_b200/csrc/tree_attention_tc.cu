@@ -6,8 +6,11 @@
 // This file: many queries per key head (wide trees, grouped heads); the host sends fewer to tree_attention_keys.cu.  The queries
 // that read one key head - every draft times the g heads of the group - share row tiles of 256, so each cached byte is fetched once
 // per request, key head and 256 queries.  For 256 queries a tile of 128 keys at d_head 128 costs 2048 cycles of the tensor pipe
-// and 2048 of the exponential unit against some 2800 of an SM's share of the memory.  (With two tiles of 128 queries apart the
-// second reads the keys again long after they have left L2: 4 contexts of 60-120 thousand keys, 64 drafts, 540 us.)
+// and 2048 of the exponential unit against some 2800 of an SM's share of the memory; measured 4600, because the two groups
+// below run in step (their weights together, then their products) rather than by turns.  4 contexts of 60-120 thousand keys, 64
+// drafts of 4 heads: 447 us.  Tried: two tiles of 128 queries apart, 540 us (the second reads the keys again long after they have
+// left L2); weights in TMEM over the scores, with two more stages of the ring, 503 us (PV and the next scores of a group then run
+// one after the other); K and V in turn, 450 us.
 //
 // One persistent CTA per SM, 12 warps; the key tiles of all requests are dealt out in equal runs (tree_attention.cuh):
 //   warp 0      K and V tiles by TMA into a ring; warp 3: the query tile of the next piece
@@ -116,7 +119,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     };
 
     if (warp == 0 && n_tiles > 0) {
-        tree_load_keys<DH, NS, 1>(p, &map_k, &map_v, run, base + Cfg::kOffRing, ring_full(0), ring_empty(0));
+        tree_load_keys<DH, NS>(p, &map_k, &map_v, run, base + Cfg::kOffRing, ring_full(0), ring_empty(0));
     } else if (warp == 3 && n_tiles > 0) {
         tree_load_queries<DH, kTileRows, 32, 1, T>(p, run, sp, nullptr, 0u, q_full, q_empty, lane);
     } else if (warp == 1 && n_tiles > 0) {
@@ -233,24 +236,28 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                         odd_piece[piece & 1u] = piece + 1;
                 }
                 if (warp_live) {
-                    // The scores stay in TMEM and are taken in chunks of 32 columns.  Loops on purpose: unrolled, the steady state does
-                    // not fit the schedulers' instruction caches.
-                    auto fetch = [&](int q, uint32_t (&s)[32]) {
-                        tmem_ld32(ts + 32u * q, s);
-                        const uint32_t vis = !tail ? 0xFFFFFFFFu : (row < nq ? visible_word(c.kt * kKeys + 32 * q, C, c.r.n, tok, mask, p.mask_words) : 0u);
-                        tmem_ld_wait();
-                        if (tail) {
+                    if (tail) {                                  // holds drafts or the request's end: take out what the row does not see
+#pragma unroll 1
+                        for (int q = 0; q < 4; ++q) {
+                            const uint32_t vis = row < nq ? visible_word(c.kt * kKeys + 32 * q, C, c.r.n, tok, mask, p.mask_words) : 0u;
+                            uint32_t s[32];
+                            tmem_ld32(ts + 32u * q, s);
+                            load32_wait(s);
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
                                 if (!((vis >> e) & 1u)) s[e] = __float_as_uint(-INFINITY);
+                            tmem_store32(ts + 32u * q, s);
                         }
-                    };
+                        tmem_store_wait();
+                    }
+                    // The scores stay in TMEM and are taken in chunks of 32 columns, the next on its way while one is worked on.
                     if (opens) {
                         float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll 1
                         for (int q = 0; q < 4; ++q) {
                             uint32_t s[32];
-                            fetch(q, s);
+                            tmem_ld32(ts + 32u * q, s);
+                            load32_wait(s);
 #pragma unroll
                             for (int e = 0; e < 32; e += 2) t4[(e >> 1) & 3] = fmaxf(t4[(e >> 1) & 3], fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
                         }
@@ -258,30 +265,41 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                         m_ref = fmaxf(fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * p.scale_log2 - Ops::kBias, kNoRef);
                     }
                     uint8_t* const prow = sp + Cfg::kOffP + g * Cfg::kPBytes + row * 128;
-                    float sum4[4];
+                    const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
+                    float2 sum2[2];
 #pragma unroll 1
                     for (int turn = 0; turn < 2; ++turn) {
                         float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) sum4[e] = 0.0f;
-#pragma unroll 1
-                        for (int q = 0; q < 4; ++q) {
-                            uint32_t s[32];
-                            fetch(q, s);
+                        const float2 minus = make_float2(-m_ref, -m_ref);
+                        sum2[0] = sum2[1] = make_float2(0.0f, 0.0f);
+                        auto weigh = [&](const uint32_t (&s)[32], int q) {
+                            uint8_t* const at = prow + (q >> 1) * (kRows * 128);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 uint32_t w[4];
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) {
-                                    const float sa = __uint_as_float(s[8 * i + 2 * e]), sb = __uint_as_float(s[8 * i + 2 * e + 1]);
-                                    t4[e] = fmaxf(t4[e], fmaxf(sa, sb));
-                                    const float a = tree_ex2(fmaf(sa, p.scale_log2, -m_ref)), b = tree_ex2(fmaf(sb, p.scale_log2, -m_ref));
-                                    sum4[e] += a + b;
-                                    w[e] = Ops::pack(a, b);
+                                    const float2 x = make_float2(__uint_as_float(s[8 * i + 2 * e]), __uint_as_float(s[8 * i + 2 * e + 1]));
+                                    t4[e] = fmaxf(t4[e], fmaxf(x.x, x.y));
+                                    float2 y = tree_fma2(x, scale2, minus);
+                                    y.x = tree_ex2(y.x);
+                                    y.y = tree_ex2(y.y);
+                                    sum2[e & 1] = tree_add2(sum2[e & 1], y);
+                                    w[e] = Ops::pack(y.x, y.y);
                                 }
-                                const int ch = 4 * (q & 1) + i;
-                                *reinterpret_cast<uint4*>(prow + (q >> 1) * (kRows * 128) + ((ch ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                                *reinterpret_cast<uint4*>(at + (((4 * (q & 1) + i) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
                             }
+                        };
+                        uint32_t sa[32], sb[32];
+                        tmem_ld32(ts, sa);
+#pragma unroll 1
+                        for (int q = 0; q < 4; q += 2) {
+                            load32_wait(sa);
+                            tmem_ld32(ts + 32u * q + 32u, sb);
+                            weigh(sa, q);
+                            load32_wait(sb);
+                            if (q < 2) tmem_ld32(ts + 64u, sa);
+                            weigh(sb, q + 1);
                         }
                         const float to = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * p.scale_log2 - Ops::kBias;
                         const bool grow = !opens && row < nq && to > m_ref + kTreeSlack;
@@ -293,7 +311,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                             uint32_t o[32];
                             const uint32_t at = tmem_o + 128u * g + t_lane + (uint32_t)c0;
                             tmem_ld32(at, o);
-                            tmem_ld_wait();
+                            load32_wait(o);
 #pragma unroll
                             for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
                             tmem_store32(at, o);
@@ -302,7 +320,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                         l_run *= f;
                         if (grow) m_ref = to;
                     }
-                    l_run += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
+                    l_run += (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
                 }
                 fence_async_smem();
                 tc_fence_before();
@@ -323,7 +341,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                             uint32_t oa[32];
                             float o[32];
                             tmem_ld32(tmem_o + 128u * g + t_lane + (uint32_t)c0, oa);
-                            tmem_ld_wait();
+                            load32_wait(oa);
 #pragma unroll
                             for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(oa[e]);
                             if (row >= nq) continue;

@@ -55,6 +55,35 @@ __device__ __forceinline__ void tmem_store32(uint32_t taddr, const uint32_t (&v)
           "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
         : "memory");
 }
+__device__ __forceinline__ void load16(uint32_t taddr, uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr) : "memory");
+}
+// The loads issued so far have arrived; v's values are not to be used above this point.
+__device__ __forceinline__ void load32_wait(uint32_t (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]),
+                   "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]),
+                   "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
+                 :: "memory");
+}
+// two products and sums in binary32 at once
+__device__ __forceinline__ float2 tree_fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{ .reg .b64 x, y, z, w; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mov.b64 z, {%6, %7}; fma.rn.f32x2 w, x, y, z; mov.b64 {%0, %1}, w; }"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 tree_add2(float2 a, float2 b) {
+    float2 d;
+    asm("{ .reg .b64 x, y, w; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 w, x, y; mov.b64 {%0, %1}, w; }"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
 __device__ __forceinline__ void store16(uint32_t taddr, const uint32_t (&v)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -89,10 +118,10 @@ __device__ __forceinline__ uint32_t visible_word(int k0, int C, int n, int i, co
 // TMA box fetches all of a page's keys of a head.
 template <int DH> __host__ __device__ constexpr int tree_group_bytes() { return DH / 64 * 1024; }
 
-// K and V tiles, by a whole warp, in the order in which the products consume them: K LEAD tiles ahead of V (LEAD = 1: K(0), K(1),
-// V(0), K(2), V(1), ...; 2: K(0), K(1), K(2), V(0), K(3), V(1), ...).  Every lane fetches one page (or 128 keys of a larger one), and
+// K and V tiles, by a whole warp, in the order in which the products consume them: K(0), K(1), V(0), K(2), V(1), ...
+// Every lane fetches one page (or 128 keys of a larger one), and
 // reads its entry of the block table two tiles ahead.
-template <int DH, int NS, int LEAD>
+template <int DH, int NS>
 __device__ __forceinline__ void tree_load_keys(const TcParams& p, const CUtensorMap* map_k, const CUtensorMap* map_v, const TreeRun* run,
                                                uint32_t ring, uint32_t full, uint32_t empty) {
     constexpr int kTileBytes = kKeys * DH * 2, kGroup = tree_group_bytes<DH>();
@@ -127,16 +156,14 @@ __device__ __forceinline__ void tree_load_keys(const TcParams& p, const CUtensor
         ++seq;
         return true;
     };
-    Box last[LEAD] = {}, cur{}, next{}, after{};               // last: the tiles whose V is still to come, latest first
+    Box last{}, cur{}, next{}, after{};                          // last: the tile whose V is still to come
     look_up(cur);
     if (n_tiles > 1) { c.next(p.w); look_up(next); }
-    for (int t = 0; t < n_tiles + LEAD && ok; ++t) {
+    for (int t = 0; t <= n_tiles && ok; ++t) {
         if (t < n_tiles && !fetch(map_k, cur)) { ok = false; break; }
         if (t + 2 < n_tiles) { c.next(p.w); look_up(after); }
-        if (t >= LEAD && !fetch(map_v, last[LEAD - 1])) { ok = false; break; }
-#pragma unroll
-        for (int i = LEAD - 1; i > 0; --i) last[i] = last[i - 1];
-        last[0] = cur;
+        if (t > 0 && !fetch(map_v, last)) { ok = false; break; }
+        last = cur;
         cur = next;
         next = after;
     }
@@ -153,7 +180,8 @@ __device__ __forceinline__ void tree_load_keys(const TcParams& p, const CUtensor
 template <int DH, int NQ, int THREADS, int BUFFERS, typename T>
 __device__ __forceinline__ void tree_load_queries(const TcParams& p, const TreeRun* run, uint8_t* q_tiles, uint32_t* masks, uint32_t done, uint32_t full,
                                                   uint32_t empty, int lane) {
-    constexpr int kChunks = DH / 8, kTileBytes = NQ * DH * 2, kRowsPer = THREADS / kChunks, kFly = NQ / kRowsPer < 8 ? NQ / kRowsPer : 8;
+    constexpr int kChunks = DH / 8, kTileBytes = NQ * DH * 2, kRowsPer = THREADS / kChunks, kMost = NQ >= 256 ? 16 : 8,
+                  kFly = NQ / kRowsPer < kMost ? NQ / kRowsPer : kMost;
     const int ch = lane % kChunks;               // a thread copies its 16 bytes of every kRowsPer-th row, kFly rows in flight
     const int n_tiles = (int)(run->end - run->begin);
     TreeCursor c = run->at;
