@@ -10,13 +10,14 @@
 //
 // Every operation is one binary32 rounding in this order (no contraction), so the choice is the one the formula gives.
 //
-// A row belongs to a cluster of up to 8 CTAs; each takes slices of the vocabulary, whose logits it has requested while it worked
-// on the slice before.  A slice with penalties or biases passes through shared memory: the history tokens that fall into it are
-// counted (integer atomics: the order does not matter), whoever takes a token's count applies the penalties to its logit, one
-// warp adds the biases in list order - so the many tokens that nothing concerns cost no arithmetic for it -, then the slice is
-// masked, rounded, written and searched.  The cluster's choices are joined through distributed shared memory, so the choice
-// needs no second launch and no scratch.  The history (its first 4096 tokens) is read once and kept in registers; a dense table of
-// counts per request would instead add its own bytes to the logits' on every step.
+// A row belongs to a cluster of up to 8 CTAs; each takes a slice of the vocabulary.  The tokens that the history, the drafts or
+// the biases name are marked in a bitmap of the slice.  All others stream through registers, masked, written and searched,
+// with no arithmetic for rules that do not concern them; the marked ones are left out there and done by themselves: a marked
+// token's place in the bitmap is its place in dense arrays of counts and bias sums (integer atomics: the order does not matter;
+// one warp adds the biases up in list order), from which its logit is then computed once.  256 rows of 50272 binary32 logits
+// with histories of 3000, 200 biases and a mask take 36 us, without rules 25, a copy of the logits 17.  (Passing every slice through shared memory next to
+// dense counts took 64 us.)  The cluster's choices are joined through distributed shared memory, so the choice needs no second
+// launch and no scratch.  A table of counts per request would instead add its own bytes to the logits' on every step.
 #include "common.cuh"
 #include "serve.cuh"
 #include "tc_ptx.cuh"
@@ -27,7 +28,9 @@ namespace zq {
 namespace {
 
 constexpr int kRuleThreads = 512;
-constexpr int kMaxSlice = 8192;                 // 10 bytes of shared memory a token of the slice, 16 tokens a thread: two CTAs per SM
+constexpr int kMaxSlice = 65536;                // tokens whose places within a slice fit 16 bits; 1/4 byte each for marks and places
+constexpr int kMaxMarked = 4096;                // marked tokens at a time, 10 bytes each: two CTAs per SM
+constexpr int kCrew = 128;                      // threads that count while the others stream
 constexpr uint32_t kSeenPrompt = 0x80000000u;   // counts share their word with the prompt's mark
 
 template <typename T> __device__ __forceinline__ float to_f32(T v);
@@ -61,16 +64,20 @@ template <typename T, int VEC> struct alignas(VEC * sizeof(T)) Vec { T v[VEC]; }
 // logits and out may be the same rows: no __restrict__, and every element is read and written by one thread
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kRuleThreads, 2)
-logit_rules_kernel(const T* logits, int64_t ld, int rows, int vocab, int slice, LogitRules R, T* out, int64_t out_ld, int32_t* token) {
+logit_rules_kernel(const T* logits, int64_t ld, int rows, int vocab, int slice, int cap, LogitRules R, T* out, int64_t out_ld, int32_t* token) {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ float wv[kRuleThreads / 32];
     __shared__ int wi[kRuleThreads / 32];
     __shared__ __align__(8) uint32_t mine[2];
-    __shared__ int list_n[kRuleThreads / 32], met_n;
-    __shared__ float2 list[kRuleThreads];       // the slice's entries of the bias list, in its order
-    float* xs = reinterpret_cast<float*>(smem);                          // the slice's logits ...
-    uint32_t* cnt = reinterpret_cast<uint32_t*>(smem) + slice;           // ... how often their tokens occur (then: the sums of their biases) ...
-    uint16_t* met = reinterpret_cast<uint16_t*>(cnt + slice);            // ... and which tokens occur, in any order
+    __shared__ uint32_t warp_n[kCrew / 32];
+    __shared__ int next_tile, marks;
+    const int words = slice >> 5;
+    uint32_t* allow = reinterpret_cast<uint32_t*>(smem);                 // the mask's words
+    uint32_t* cnt = allow + (R.allowed ? words : 0);                     // how often marked tokens occur, in the order of the vocabulary,
+    float* sum = reinterpret_cast<float*>(cnt + cap);                    // their biases
+    uint32_t* bits = reinterpret_cast<uint32_t*>(sum + cap);             // the slice's marks
+    uint32_t* place = bits + words;                                      // marks before each word
+    uint16_t* tok = reinterpret_cast<uint16_t*>(place + words);          // and which tokens of the slice they are
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = cluster_ctarank(), ranks = cluster_nctarank();
     const int64_t row = blockIdx.y;
@@ -79,34 +86,26 @@ logit_rules_kernel(const T* logits, int64_t ld, int rows, int vocab, int slice, 
     if (req < 0 || req >= R.batch) return;      // the same answer in every CTA of the cluster: the row is left as it is
 
     const uint32_t* allowed = R.allowed ? R.allowed + row * R.allowed_stride : nullptr;
-    constexpr int kSteps = kMaxSlice / (kRuleThreads * VEC);
+    // loads a thread has in flight; 8 tokens at a time have registers for two (four spill: 47 against 41 us)
+    constexpr int kSteps = VEC == 1 ? 8 : (VEC == 4 ? 4 : 2), kTile = kSteps * 32 * VEC;  // tokens of a warp at a time
     Vec<T, VEC> raw[kSteps];
-    uint32_t ok[VEC == 1 ? 1 : kSteps];         // the mask's words of the thread's tokens
-    auto fetch = [&](int k, int lo) {           // step k of the slice at lo
-        const int u = lo + (tid + k * kRuleThreads) * VEC, end = min(lo + slice, vocab);
-        if (u + VEC <= end) {
-            raw[k] = *reinterpret_cast<const Vec<T, VEC>*>(logits + row * ld + u);
+    auto fetch = [&](int k, int lo, int tile, int size) {                // step k of a tile of the slice at lo
+        const int u = tile * kTile + (k * 32 + lane) * VEC;
+        if (u >= size) return;
+        const T* src = logits + row * ld + lo + u;
+        if (u + VEC <= size) {
+            raw[k] = *reinterpret_cast<const Vec<T, VEC>*>(src);
         } else {
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
-                if (u + e < end) raw[k].v[e] = logits[row * ld + u + e];
+                if (u + e < size) raw[k].v[e] = src[e];
         }
-    };
-    auto fetch_mask = [&](int k, int lo) {
-        const int u = lo + (tid + k * kRuleThreads) * VEC;
-        ok[VEC == 1 ? 0 : k] = allowed && u < min(lo + slice, vocab) ? __ldg(allowed + (u >> 5)) >> (u & 31) : 0xFFFFFFFFu;
-    };
-    // (single tokens) a warp's 32 tokens of step k share one word (slices begin at whole words): lane k keeps that of step k
-    auto fetch_words = [&](int lo) {
-        const int u = lo + warp * 32 + lane * kRuleThreads;
-        ok[0] = allowed && lane < kSteps && u < min(lo + slice, vocab) ? __ldg(allowed + (u >> 5)) : 0xFFFFFFFFu;
     };
     const int step = (int)ranks * slice;
     int lo = (int)rank * slice;
     if (lo < vocab) {
-        if (VEC == 1) fetch_words(lo);
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) { fetch(k, lo); if (VEC > 1) fetch_mask(k, lo); }
+        for (int k = 0; k < kSteps; ++k) fetch(k, lo, warp, min(slice, vocab - lo));
     }
 
     // the request's words, all at once
@@ -122,152 +121,158 @@ logit_rules_kernel(const T* logits, int64_t ld, int rows, int vocab, int slice, 
     n_bias = n_bias < 0 ? 0 : (n_bias > R.bias_stride ? R.bias_stride : n_bias);
     if (draft0 < 0 || n_draft < 0 || (int64_t)draft0 + n_draft > rows) n_draft = 0;
     if (n_draft > 32 * R.mask_words) n_draft = 32 * R.mask_words;
-    const bool counted = n_hist > 0 || n_draft > 0, sparse = counted || n_bias > 0;
+    const bool sparse = n_hist > 0 || n_draft > 0 || n_bias > 0;
     const int32_t* hist = R.history + (int64_t)req * R.history_stride;
+    const int32_t* bias_t = R.bias_token + (int64_t)req * R.bias_stride;
+    const float* bias_v = R.bias_value + (int64_t)req * R.bias_stride;
 
-    // The first tokens of the history, the drafts and the biases stay in registers through all slices.  Whatever is not there
-    // is -1, which falls into no slice.
-    constexpr int kHeld = 8;
-    int held[kHeld];
+    auto occurrences = [&](int threads, auto&& f) {      // f(token, in the prompt) for the history and the drafts that the row sees
+        for (int k0 = tid; k0 < n_hist; k0 += 8 * threads) {
+            int t[8];
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k) held[k] = tid + k * kRuleThreads < n_hist ? __ldg(hist + tid + k * kRuleThreads) : -1;
-    auto draft_at = [&](int j) {                // draft j's token if this row sees it
-        return (__ldg(R.tree_mask + row * R.mask_words + (j >> 5)) >> (j & 31)) & 1u ? __ldg(R.draft_token + draft0 + j) : -1;
+            for (int k = 0; k < 8; ++k) t[k] = k0 + k * threads < n_hist ? __ldg(hist + k0 + k * threads) : -1;      // -1 falls into no slice
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f(t[k], k0 + k * threads < n_prompt);
+        }
+        for (int j = tid; j < n_draft; j += threads)
+            if ((__ldg(R.tree_mask + row * R.mask_words + (j >> 5)) >> (j & 31)) & 1u) f(__ldg(R.draft_token + draft0 + j), false);
     };
-    const int draft = tid < n_draft ? draft_at(tid) : -1;
-    const int bias_token = tid < n_bias ? __ldg(R.bias_token + (int64_t)req * R.bias_stride + tid) : -1;
-    const float bias_value = tid < n_bias ? __ldg(R.bias_value + (int64_t)req * R.bias_stride + tid) : 0.0f;
-    if (tid == 0) met_n = 0;
-    if (sparse)
-        for (int u = tid; u < (slice >> 2); u += kRuleThreads) reinterpret_cast<uint4*>(cnt)[u] = make_uint4(0, 0, 0, 0);
+    auto crew_sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(kCrew) : "memory"); };
 
+    const T none = from_f32<T>(-INFINITY);
     Best best{-INFINITY, -1};
     for (; lo < vocab; lo += step) {
         const int size = min(slice, vocab - lo);
-        const bool more = lo + step < vocab;
-        T* dst = out ? out + row * out_ld + lo : nullptr;
+        auto inside = [&](int t) { return t >= 0 && (uint32_t)(t - lo) < (uint32_t)size; };
+        auto place_of = [&](int u) { return (int)(place[u >> 5] + __popc(bits[u >> 5] & ((1u << (u & 31)) - 1u))); };
+        __syncthreads();                        // the slice before has been read
+        if (tid == 0) { next_tile = kRuleThreads / 32; marks = 0; }
+        if (allowed)
+            for (int u = tid; u < (size + 31) >> 5; u += kRuleThreads) allow[u] = __ldg(allowed + (lo >> 5) + u);
         if (sparse) {
-            __syncthreads();                    // the counts are clear, the slice before has been read
+            for (int u = tid; u < words; u += kRuleThreads) bits[u] = 0;
+            for (int u = tid; u < 2 * cap; u += kRuleThreads) cnt[u] = 0;        // and the sums
+            __syncthreads();
+            auto mark = [&](int t, bool) { if (inside(t)) atomicOr(&bits[(t - lo) >> 5], 1u << ((t - lo) & 31)); };
+            occurrences(kRuleThreads, mark);
+            for (int k = tid; k < n_bias; k += kRuleThreads) mark(__ldg(bias_t + k), false);
+        }
+        __syncthreads();
+        auto count = [&](int first) {           // counts and bias sums of the marked tokens [first, first + cap); by the crew
+            occurrences(kCrew, [&](int t, bool prompt) {
+                if (!inside(t)) return;
+                const int i = place_of(t - lo) - first;
+                if (i < 0 || i >= cap) return;
+                if (prompt) atomicOr(&cnt[i], kSeenPrompt); else atomicAdd(&cnt[i], 1u);
+                tok[i] = (uint16_t)(t - lo);
+            });
+            if (warp == kCrew / 32 - 1) {
+                int t = lane < n_bias ? __ldg(bias_t + lane) : -1;
+                float v = lane < n_bias ? __ldg(bias_v + lane) : 0.0f;
+                for (int k = lane; k - lane < n_bias; k += 32) {
+                    const int t_next = k + 32 < n_bias ? __ldg(bias_t + k + 32) : -1;
+                    const float v_next = k + 32 < n_bias ? __ldg(bias_v + k + 32) : 0.0f;
+                    int i = inside(t) ? place_of(t - lo) - first : -1;
+                    const bool live = i >= 0 && i < cap;
+                    if (live) tok[i] = (uint16_t)(t - lo); else i = -1 - lane;
+                    const int turn = __popc(__match_any_sync(0xffffffffu, i) & ((1u << lane) - 1));      // entries of this token before
+                    for (int r = 0; __any_sync(0xffffffffu, live && r <= turn); ++r) {
+                        if (live && r == turn) sum[i] = __fadd_rn(sum[i], v);
+                        __syncwarp();
+                    }
+                    t = t_next; v = v_next;
+                }
+            }
+        };
+        if (sparse && tid < kCrew) {            // the marks' places, and the first counts
+            const int per = (words + kCrew - 1) / kCrew, u0 = min(tid * per, words), u1 = min(u0 + per, words);
+            uint32_t n = 0;
+            for (int u = u0; u < u1; ++u) n += __popc(bits[u]);
+            uint32_t up = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const uint32_t x = __shfl_up_sync(0xffffffffu, up, o); if (lane >= o) up += x; }
+            if (lane == 31) warp_n[warp] = up;
+            crew_sync();
+            up -= n;
+            for (int w = 0; w < warp; ++w) up += warp_n[w];
+            for (int u = u0; u < u1; ++u) { place[u] = up; up += __popc(bits[u]); }
+            if (tid == kCrew - 1) marks = (int)up;
+            crew_sync();
+            count(0);
+        }
+        // the tokens that nothing concerns, and their mask; the warps take the tiles in turn, the crew's when they get there
+        for (int tile = warp; tile * kTile < size;) {
+            int next = 0;
+            if (lane == 0) next = atomicAdd(&next_tile, 1);
+            next = __shfl_sync(0xffffffffu, next, 0);
 #pragma unroll
             for (int k = 0; k < kSteps; ++k) {
-                const int u = (tid + k * kRuleThreads) * VEC;
+                const int u = tile * kTile + (k * 32 + lane) * VEC;
+                uint32_t word = 0xFFFFFFFFu, left = u + VEC <= size ? 0xFFFFFFFFu : (1u << max(size - u, 0)) - 1u;
                 if (u < size) {
-                    Vec<float, VEC> x;
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) x.v[e] = to_f32<T>(raw[k].v[e]);
-                    *reinterpret_cast<Vec<float, VEC>*>(xs + u) = x;
+                    if (allowed) word = allow[u >> 5] >> (u & 31);
+                    if (sparse) left &= ~(bits[u >> 5] >> (u & 31));
                 }
-                if (more) fetch(k, lo + step);  // in flight while this slice is worked on
-            }
-            if (counted) {
-                auto count = [&](int t, bool prompt) {
-                    const uint32_t u = (uint32_t)(t - lo);
-                    if (t < 0 || u >= (uint32_t)size) return;
-                    const uint32_t old = prompt ? atomicOr(&cnt[u], kSeenPrompt) : atomicAdd(&cnt[u], 1u);
-                    if (!old) met[atomicAdd(&met_n, 1)] = (uint16_t)u;
-                };
+                Vec<T, VEC> y;
+                float top = -INFINITY, x[VEC];
+                const uint32_t both = word & left;
 #pragma unroll
-                for (int k = 0; k < kHeld; ++k) count(held[k], tid + k * kRuleThreads < n_prompt);
-                for (int k = kHeld * kRuleThreads + tid; k < n_hist; k += kRuleThreads) count(__ldg(hist + k), k < n_prompt);
-                for (int j = tid; j < n_draft; j += kRuleThreads) count(j == tid ? draft : draft_at(j), false);
+                for (int e = 0; e < VEC; ++e) {
+                    y.v[e] = (word >> e) & 1u ? raw[k].v[e] : none;
+                    x[e] = (both >> e) & 1u ? to_f32<T>(raw[k].v[e]) : -INFINITY;
+                    top = fmaxf(top, x[e]);
+                }
+                fetch(k, lo, next, size);
+                if (out) {
+                    T* dst = out + row * out_ld + lo + u;
+                    if ((left & ((1u << VEC) - 1u)) == (1u << VEC) - 1u) {
+                        *reinterpret_cast<Vec<T, VEC>*>(dst) = y;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e)
+                            if ((left >> e) & 1u) dst[e] = y.v[e];
+                    }
+                }
+                if (top > best.v) {                              // a thread sees its tokens in ascending order; NaN is never larger
+                    best.v = top;
+#pragma unroll
+                    for (int e = VEC - 1; e >= 0; --e)
+                        if (x[e] == top) best.i = lo + u + e;
+                }
+            }
+            tile = next;
+        }
+        if (lo + step < vocab) {
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) fetch(k, lo + step, warp, min(slice, vocab - lo - step));
+        }
+        if (!sparse) continue;
+        // the marked ones, `cap` at a time
+        __syncthreads();                        // places, counts and sums are complete
+        const int marked = marks;
+        for (int first = 0; first < marked; first += cap) {
+            if (first > 0) {
                 __syncthreads();
-                // the tokens that occur, spread over all threads: their penalties, and their counts cleared for the next slice
-                for (int i = tid; i < met_n; i += kRuleThreads) {
-                    const int u = met[i];
-                    const uint32_t c = cnt[u], n = c & ~kSeenPrompt;
-                    cnt[u] = 0;
-                    float x = xs[u];
+                for (int u = tid; u < 2 * cap; u += kRuleThreads) cnt[u] = 0;
+                __syncthreads();
+                if (tid < kCrew) count(first);
+                __syncthreads();
+            }
+            for (int i = tid; i < min(cap, marked - first); i += kRuleThreads) {
+                const int u = tok[i], v = lo + u;
+                const uint32_t c = cnt[i], n = c & ~kSeenPrompt;
+                float x = to_f32<T>(logits[row * ld + v]);
+                if (c) {
                     x = x > 0.0f ? __fdiv_rn(x, rep) : __fmul_rn(x, rep);
                     x = __fsub_rn(x, __fmul_rn(freq, (float)n));
                     if (n) x = __fsub_rn(x, pres);
-                    xs[u] = x;
                 }
-                if (n_bias) __syncthreads();
-            }
-            auto add_sum = [&](int u) {         // whoever takes a token's sum first (and clears it for the next slice) adds it
-                const float sum = __uint_as_float(atomicExch(&cnt[u], 0u));
-                if (sum != 0.0f) xs[u] = __fadd_rn(xs[u], sum);
-            };
-            for (int k0 = 0; k0 < n_bias; k0 += kRuleThreads) {
-                // the slice's entries, in the order of the list; then one warp sums them per token and adds the sums
-                const int k = k0 + tid;
-                const int t = k0 == 0 ? bias_token : (k < n_bias ? __ldg(R.bias_token + (int64_t)req * R.bias_stride + k) : -1);
-                const float v = k0 == 0 ? bias_value : (k < n_bias ? __ldg(R.bias_value + (int64_t)req * R.bias_stride + k) : 0.0f);
-                const uint32_t u = (uint32_t)(t - lo);
-                const bool in = t >= 0 && u < (uint32_t)size;
-                const uint32_t all = __ballot_sync(0xffffffffu, in);
-                if (lane == 0) list_n[warp] = __popc(all);
-                __syncthreads();
-                int at = __popc(all & ((1u << lane) - 1)), n = 0;
-                for (int w = 0; w < kRuleThreads / 32; ++w) { if (w < warp) at += list_n[w]; n += list_n[w]; }
-                if (in) list[at] = make_float2(__int_as_float((int)u), v);
-                __syncthreads();
-                if (warp == 0) {
-                    float* sum = reinterpret_cast<float*>(cnt);
-                    for (int i0 = 0; i0 < n; i0 += 32) {
-                        const bool live = i0 + lane < n;
-                        const float2 e = live ? list[i0 + lane] : make_float2(0.0f, 0.0f);
-                        const int x = live ? __float_as_int(e.x) : -1 - lane;
-                        const int turn = __popc(__match_any_sync(0xffffffffu, x) & ((1u << lane) - 1));      // entries of this token before
-                        for (int i = 0; __any_sync(0xffffffffu, live && i <= turn); ++i) {
-                            if (live && i == turn) sum[x] = __fadd_rn(sum[x], e.y);
-                            __syncwarp();
-                        }
-                    }
-                }
-                if (n_bias > kRuleThreads) __syncthreads();      // the list is written again
-                else if (warp == 0)
-                    for (int i = lane; i < n; i += 32) add_sum(__float_as_int(list[i].x));
-            }
-            if (n_bias > kRuleThreads)                           // (a long list: its tokens once more)
-                for (int k = tid; k < n_bias; k += kRuleThreads) {
-                    const int t = __ldg(R.bias_token + (int64_t)req * R.bias_stride + k);
-                    if (t >= 0 && (uint32_t)(t - lo) < (uint32_t)size) add_sum(t - lo);
-                }
-            __syncthreads();
-            if (tid == 0) met_n = 0;
-        }
-        const uint32_t words = ok[0];
-        if (VEC == 1 && more) fetch_words(lo + step);
-#pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-            const int u = (tid + k * kRuleThreads) * VEC;
-            const uint32_t word = VEC == 1 ? __shfl_sync(0xffffffffu, words, k) >> lane : ok[VEC == 1 ? 0 : k];
-            float x[VEC];
-            if (sparse) {
-                const Vec<float, VEC> s = u < size ? *reinterpret_cast<const Vec<float, VEC>*>(xs + u) : Vec<float, VEC>{};
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) x[e] = s.v[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) x[e] = to_f32<T>(raw[k].v[e]);
-                if (more) fetch(k, lo + step);
-            }
-            if (VEC > 1 && more) fetch_mask(k, lo + step);
-            if (u >= size) continue;
-            Vec<T, VEC> y;
-            float top = -INFINITY;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                if (!((word >> e) & 1u)) x[e] = -INFINITY;
-                y.v[e] = from_f32<T>(x[e]);
-                x[e] = to_f32<T>(y.v[e]);
-                if (u + e < size) top = fmaxf(top, x[e]);
-            }
-            if (dst) {
-                if (u + VEC <= size) {
-                    *reinterpret_cast<Vec<T, VEC>*>(dst + u) = y;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e)
-                        if (u + e < size) dst[u + e] = y.v[e];
-                }
-            }
-            if (top > best.v) {                                  // a thread sees its tokens in ascending order; NaN is never larger
-                best.v = top;
-#pragma unroll
-                for (int e = VEC - 1; e >= 0; --e)
-                    if (u + e < size && x[e] == top) best.i = lo + u + e;
+                if (sum[i] != 0.0f) x = __fadd_rn(x, sum[i]);
+                if (allowed && !((allow[u >> 5] >> (u & 31)) & 1u)) x = -INFINITY;
+                const T y = from_f32<T>(x);
+                x = to_f32<T>(y);
+                if (out) out[row * out_ld + v] = y;
+                if (x > -INFINITY) take_better(best, x, v);
             }
         }
     }
@@ -301,15 +306,14 @@ logit_rules_kernel(const T* logits, int64_t ld, int rows, int vocab, int slice, 
 template <typename T, int VEC>
 int launch_rules_vec(const T* logits, int64_t ld, int rows, int vocab, const LogitRules& r, T* out, int64_t out_ld, int32_t* token,
                  cudaStream_t s, bool dependent) {
-    // at least 1024 tokens to a CTA, and no more CTAs of a cluster than it takes to fill the SMs: a CTA with several slices
-    // requests each while it works on the one before
+    // at least 1024 tokens to a CTA, and no more CTAs of a cluster than it takes to fill the SMs
     int ranks = 1;
     while (ranks < 8 && vocab > 1024 * ranks && rows * ranks < 148) ranks *= 2;
     const int slices = (vocab + ranks * kMaxSlice - 1) / (ranks * kMaxSlice) * ranks;
-    const int slice = ((vocab + slices - 1) / slices + 31) / 32 * 32;
-    const size_t smem = (r.history || r.draft_token || r.bias_token) ? (size_t)slice * 10 : 0;
+    const int slice = ((vocab + slices - 1) / slices + 31) / 32 * 32, cap = slice < kMaxMarked ? slice : kMaxMarked;
+    const size_t smem = ((r.history || r.draft_token || r.bias_token) ? (size_t)cap * 10 + slice / 4 : 0) + (r.allowed ? slice / 8 : 0);
     static DeviceOnce attr;
-    if (attr.first() && cudaFuncSetAttribute(logit_rules_kernel<T, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSlice * 10) != cudaSuccess) {
+    if (attr.first() && cudaFuncSetAttribute(logit_rules_kernel<T, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxMarked * 10 + kMaxSlice / 8 * 3) != cudaSuccess) {
         attr.retry();
         return -1;
     }
@@ -325,7 +329,7 @@ int launch_rules_vec(const T* logits, int64_t ld, int rows, int vocab, const Log
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = dependent ? 2 : 1;
-    if (cudaLaunchKernelEx(&cfg, logit_rules_kernel<T, VEC>, logits, ld, rows, vocab, slice, r, out, out_ld, token) != cudaSuccess) return -1;
+    if (cudaLaunchKernelEx(&cfg, logit_rules_kernel<T, VEC>, logits, ld, rows, vocab, slice, cap, r, out, out_ld, token) != cudaSuccess) return -1;
     count_launch();
     return 0;
 }
