@@ -508,17 +508,29 @@ def pack_bits(ok):
     ("f32", 1, 1, 1, "h"), ("f32", 1000, 3, 1, ""), ("f32", 32000, 2, 3, "hpdba"), ("bf16", 50257, 2, 2, "hpdba"), ("f16", 777, 5, 4, "hpdb"),
     ("f32", 131072, 1, 1, "hpb"), ("bf16", 4097, 40, 1, "a"), ("f32", 65537, 2, 1, "b"), ("f16", 8193, 3, 2, "d"), ("f32", 5000, 3, 1, "hba")])
 def test_rules_match_the_formula_bit_for_bit(zq, dtype, V, batch, per, groups):
+    check_rules(zq, dtype, V, batch, per, groups)
+
+
+# rows on 16-byte boundaries, taken in vectors; histories of more distinct tokens than are counted at a time; a vocabulary of
+# several slices (one CTA per row)
+@pytest.mark.parametrize("dtype,V,batch,per,groups,hist,skew", [
+    ("f32", 1000, 3, 2, "hpdba", 600, 6), ("bf16", 50264, 2, 2, "hpdba", 600, 6), ("f16", 776, 5, 4, "hpdb", 600, 6), ("bf16", 8, 2, 1, "hba", 600, 6),
+    ("f32", 50272, 2, 2, "hpdba", 20000, 1), ("f16", 40000, 150, 1, "hpb", 9000, 1), ("f32", 70016, 150, 1, "hpa", 600, 1)])
+def test_rules_on_aligned_rows(zq, dtype, V, batch, per, groups, hist, skew):
+    check_rules(zq, dtype, V, batch, per, groups, pad=8, H=hist, skew=skew)
+
+
+def check_rules(zq, dtype, V, batch, per, groups, pad=3, H=600, skew=6):
     rng = np.random.default_rng(V)
     rows = batch * per
     request = [r // per for r in range(rows)]
     if rows > 3:
         request[1] = -1                                                  # a padded row is left as it is
-    slab = torch.from_numpy((4 * rng.standard_normal((rows, V + 3))).astype(np.float32)).to(TYPES[dtype]).cuda()
+    slab = torch.from_numpy((4 * rng.standard_normal((rows, V + pad))).astype(np.float32)).to(TYPES[dtype]).cuda()
     logits = slab[:, :V]
     R, kw = {}, {}
     if "h" in groups:
-        H = 600
-        hist = np.minimum((V * rng.random((batch, H)) ** 6).astype(np.int64), V - 1)
+        hist = np.minimum((V * rng.random((batch, H)) ** skew).astype(np.int64), V - 1)
         hist[:, 7], hist[:, 11] = V, -1                                  # not tokens
         R.update(history=hist.tolist(), history_len=rng.integers(0, H + 1, batch).tolist())
         kw.update(history=ints(hist.tolist()), history_len=ints(R["history_len"]))
