@@ -677,7 +677,8 @@ int zoqat_op_cache_plan(const int32_t* cached_len_dev, const int32_t* new_len_de
  * [rope_len, d_head / 2], pairs (i, i + d_head / 2); both NULL: no rotation, row_pos_dev unused), rounded once to the cache's
  * type; q goes to q_out_dev (of that type, [rows, n_heads, d_head], rows q_stride elements apart), k and v into slot slot_dev[r].
  * A row with a negative slot is skipped, its q_out row left as it is; a slot or position outside the cache / the tables is
- * skipped too and sets *err_flag_dev to 40.  Two rows with the same slot: either may win, element by element. */
+ * skipped too and sets *err_flag_dev to 40.  Two rows with the same slot: either may win, element by element.  rows = 0 is
+ * allowed (nothing is done). */
 int zoqat_op_cache_append(const float* qkv_dev, int64_t ld, const int32_t* row_pos_dev, const int32_t* slot_dev, int rows,
                           int n_heads, const float* cos_dev, const float* sin_dev, int rope_len,
                           const zoqat_paged_cache_t* cache, void* q_out_dev, int64_t q_stride, int32_t* err_flag_dev, void* stream);
@@ -690,11 +691,12 @@ int zoqat_op_cache_append(const float* qkv_dev, int64_t ld, const int32_t* row_p
  * apart (16-byte aligned, strides multiples of 16 bytes).  Rows outside row_start_dev's ranges are left as they are.
  * Sums and the softmax are held in fp32; in bf16 / fp16 the softmax weights are rounded to the cache's type for the product with
  * V.  The keys are dealt out evenly over the SMs, long contexts in several pieces that are joined in a fixed order: the same
- * call gives the same bits.  bf16 and fp16 need page_size 8, 16, 32, 64 or a multiple of 128, and
- * with several heads and pages a page_stride that is a multiple of head_stride (ZOQAT_ERR_UNSUPPORTED otherwise).  scratch_dev: zoqat_op_tree_attention_scratch_bytes() bytes, 256-byte aligned, for one
- * call at a time (calls that may overlap, e.g. two graphs in flight, each need their own).  *err_flag_dev is set to 41 (a request
- * whose lengths or rows contradict each other: it is left out), 42 (a page outside the pool: its keys and values count as zeros), 43 (a
- * bounded device wait ran out). */
+ * call gives the same bits.  bf16 and fp16 need page_size 8, 16, 32, 64 or a multiple of 128, and with several heads and pages a
+ * page_stride that is a multiple of head_stride (ZOQAT_ERR_UNSUPPORTED otherwise).  scratch_dev:
+ * zoqat_op_tree_attention_scratch_bytes() bytes, 256-byte aligned, for one call at a time (calls that may overlap, e.g. two graphs
+ * in flight, each need their own).  rows = 0 is allowed (nothing is done).  *err_flag_dev is set to 41 (a request whose lengths or
+ * rows contradict each other: it is left out), 42 (a page outside the pool: its keys and values count as zeros), 43 (a bounded
+ * device wait ran out). */
 int zoqat_op_tree_attention_scratch_bytes(int type, int d_head, size_t* bytes);
 int zoqat_op_tree_attention(const void* q_dev, int64_t q_stride, const zoqat_paged_cache_t* cache, const int32_t* block_table_dev,
                             int max_pages, const int32_t* kv_len_dev, const int32_t* row_start_dev, const uint32_t* tree_mask_dev,
@@ -707,7 +709,7 @@ typedef struct zoqat_logit_rules {
     const float*   repetition;     /* [batch] fp32; NULL: 1                                                        */
     const float*   presence;       /* [batch] fp32; NULL: 0                                                        */
     const float*   frequency;      /* [batch] fp32; NULL: 0                                                        */
-    const int32_t* history;        /* [batch, history_stride] token ids: prompt, then what was generated            */
+    const int32_t* history;        /* [batch, history_stride <= 2^30] token ids: prompt, then what was generated    */
     const int32_t* history_len;    /* [batch]                                                                      */
     const int32_t* prompt_len;     /* [batch] how many of them are the prompt; NULL: 0                             */
     const int32_t* bias_token;     /* [batch, bias_stride]                                                         */

@@ -1837,8 +1837,8 @@ int logit_rules(const zoqat_logit_rules_t* c, int rows, int vocab, LogitRules& r
     if (rows <= 0 || rows > 65535 || vocab <= 0 || vocab > (1 << 30)) return fail(ZOQAT_ERR_UNSUPPORTED, "rows %d (1..65535), vocab %d (1..2^30)", rows, vocab);
     if (c->batch <= 0) return fail(ZOQAT_ERR_INVALID_ARG, "rules need the number of requests (batch)");
     if (!c->row_request && rows > c->batch) return fail(ZOQAT_ERR_INVALID_ARG, "more rows than requests: row_request is needed");
-    if (c->history && (!c->history_len || c->history_stride <= 0 || c->history_stride > INT32_MAX)) return fail(ZOQAT_ERR_INVALID_ARG, "history needs history_len and history_stride");
-    if (c->bias_token && (!c->bias_value || !c->bias_len || c->bias_stride <= 0)) return fail(ZOQAT_ERR_INVALID_ARG, "biases need bias_value, bias_len and bias_stride");
+    if (c->history && (!c->history_len || c->history_stride <= 0 || c->history_stride > (1 << 30))) return fail(ZOQAT_ERR_INVALID_ARG, "history needs history_len and history_stride (up to 2^30)");
+    if (c->bias_token && (!c->bias_value || !c->bias_len || c->bias_stride <= 0 || c->bias_stride > (1 << 30))) return fail(ZOQAT_ERR_INVALID_ARG, "biases need bias_value, bias_len and bias_stride (up to 2^30)");
     if (c->allowed && c->allowed_stride < (vocab + 31) / 32) return fail(ZOQAT_ERR_INVALID_ARG, "allowed_stride must cover the vocabulary's bits");
     if (c->draft_token && (!c->row_start || !c->tree_mask || c->mask_words <= 0 || c->mask_words > 32)) return fail(ZOQAT_ERR_INVALID_ARG, "drafts need row_start, tree_mask and mask_words (1..32)");
     r = LogitRules{c->row_request, c->batch, c->repetition, c->presence, c->frequency, c->history, c->history_len, c->prompt_len, c->history_stride,
@@ -1882,10 +1882,10 @@ int zoqat_op_cache_append(const float* qkv_dev, int64_t ld, const int32_t* row_p
                           int64_t q_stride, int32_t* err_flag_dev, void* stream) {
     PagedCache c;
     if (int rc = paged_cache(cache, c)) return rc;
-    if (!qkv_dev || !slot_dev || !q_out_dev || !err_flag_dev) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
+    if (!err_flag_dev || (rows > 0 && (!qkv_dev || !slot_dev || !q_out_dev))) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
     if (rows < 0 || n_heads <= 0 || n_heads > 65536 || c.n_kv_heads > 65536) return fail(ZOQAT_ERR_INVALID_ARG, "bad sizes (rows %d, heads %d)", rows, n_heads);
     if ((cos_dev == nullptr) != (sin_dev == nullptr)) return fail(ZOQAT_ERR_INVALID_ARG, "cos/sin tables must both be given or both NULL");
-    if (cos_dev && (!row_pos_dev || rope_len <= 0)) return fail(ZOQAT_ERR_INVALID_ARG, "rotary tables need row_pos_dev and rope_len");
+    if (cos_dev && ((rows > 0 && !row_pos_dev) || rope_len <= 0)) return fail(ZOQAT_ERR_INVALID_ARG, "rotary tables need row_pos_dev and rope_len");
     if (ld < (int64_t)(n_heads + 2 * c.n_kv_heads) * c.d_head || ld % 4) return fail(ZOQAT_ERR_INVALID_ARG, "ld must cover q | k | v and be a multiple of 4");
     const int64_t e = type_bytes(c.type);
     if (q_stride < (int64_t)n_heads * c.d_head || (q_stride * e) % 16) return fail(ZOQAT_ERR_INVALID_ARG, "q_stride must cover the heads and be a multiple of 16 bytes");
@@ -1912,16 +1912,16 @@ int zoqat_op_tree_attention(const void* q_dev, int64_t q_stride, const zoqat_pag
     TreeAttnArgs a{};
     if (int rc = paged_cache(cache, a.cache)) return rc;
     const PagedCache& c = a.cache;
-    if (!q_dev || !block_table_dev || !kv_len_dev || !row_start_dev || !out_dev || !scratch_dev || !err_flag_dev) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
+    if (!block_table_dev || !kv_len_dev || !row_start_dev || !scratch_dev || !err_flag_dev || (rows > 0 && (!q_dev || !out_dev))) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
     if (batch <= 0 || rows < 0 || n_heads <= 0 || max_pages <= 0) return fail(ZOQAT_ERR_INVALID_ARG, "sizes must be positive");
     if (n_heads % c.n_kv_heads) return fail(ZOQAT_ERR_INVALID_ARG, "n_kv_heads must divide n_heads");
     if (int rc = attention_limits(c, max_pages, rows, n_heads)) return rc;
     if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(ZOQAT_ERR_INVALID_ARG, "scale must be positive");
-    if (tree_mask_dev ? mask_words <= 0 || mask_words > (1 << 20) : mask_words != 0) return fail(ZOQAT_ERR_INVALID_ARG, "tree_mask_dev and mask_words must both be given or neither");
+    if (tree_mask_dev ? mask_words <= 0 || mask_words > (1 << 20) : rows > 0 && mask_words != 0) return fail(ZOQAT_ERR_INVALID_ARG, "tree_mask_dev and mask_words must both be given or neither");
     const int64_t e = type_bytes(c.type), wide = (int64_t)n_heads * c.d_head;
     if (q_stride < wide || out_stride < wide || (q_stride * e) % 16 || (out_stride * e) % 16 || q_stride >= ((int64_t)1 << 38)) return fail(ZOQAT_ERR_INVALID_ARG, "row strides must cover the heads and be multiples of 16 bytes");
     if (misaligned(q_dev, 16) || misaligned(out_dev, 16)) return fail(ZOQAT_ERR_INVALID_ARG, "q_dev and out_dev must be 16-byte aligned");
-    if (q_dev == out_dev) return fail(ZOQAT_ERR_INVALID_ARG, "out_dev may not be q_dev");
+    if (q_dev && q_dev == out_dev) return fail(ZOQAT_ERR_INVALID_ARG, "out_dev may not be q_dev");
     if (misaligned(scratch_dev, 256)) return fail(ZOQAT_ERR_INVALID_ARG, "scratch_dev must be 256-byte aligned");
     const size_t need = tree_attention_scratch_bytes(c.type, c.d_head);
     if (scratch_bytes < need) return fail(ZOQAT_ERR_WORKSPACE_SMALL, "attention scratch %zu < %zu bytes", scratch_bytes, need);

@@ -320,7 +320,7 @@ ATTENTION = [
     ("bf16", 14, 2, 64, 32, "joint", [300, 129, 0, 4], [1, 2, 5, 1], "tree"),   # tiles that cut a draft's heads apart
     ("f16", 7, 1, 128, 16, "token", [300, 129, 0, 4], [3, 2, 5, 30], "random"),
     ("bf16", 2, 2, 128, 16, "token", [4000] * 9, [1] * 9, None),
-    # long runs of tiles for every tile width of the tensor-core kernels (16, 32, 64 and 128 queries)
+    # long runs of tiles for every tile width of the tensor-core kernels (16, 32, 64 and 256 queries)
     ("bf16", 16, 4, 128, 64, "token", [5000, 20011, 9000, 16], [1, 1, 1, 1], "tree"),
     ("bf16", 16, 4, 128, 64, "token", [5000, 20011, 9000, 16], [4, 4, 4, 4], "tree"),
     ("f16", 16, 4, 64, 16, "head", [5000, 20011, 9000, 16], [4, 4, 4, 4], "tree"),
@@ -424,6 +424,15 @@ def test_attention_captured_and_replayed_as_lengths_change(zq):
         want, bound = attention_oracle(pr)
         rows = sum(new)
         assert bool(((out[:rows].double() - want).abs() <= bound).all()) and bool((out[rows:] == 5.0).all())
+
+
+def test_no_rows(zq):
+    k, v = [torch.randn((4, 16, 2, 64), device="cuda").to(torch.bfloat16) for _ in range(2)]
+    keep = k.clone()
+    out, err = zq.zoqat_op_tree_attention(torch.empty((0, 4, 64), dtype=torch.bfloat16, device="cuda"), k, v, ints([[0]]), ints([0]), ints([0, 0]),
+                                          ints([[0]])[:0])
+    q, err2 = zq.zoqat_op_cache_append(torch.empty((0, 512), device="cuda"), ints([0])[:0], ints([0])[:0], k, v, 4)
+    assert out.shape == q.shape == (0, 4, 64) and err.item() == err2.item() == 0 and torch.equal(k, keep)
 
 
 def test_attention_on_another_stream(zq):

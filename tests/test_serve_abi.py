@@ -78,6 +78,13 @@ def attend(zq, c, **kw):
     return zq.lib().zoqat_op_tree_attention(*a.values(), ctypes.byref(c) if c is not None else None, *b.values())
 
 
+def test_no_rows_are_nothing_to_do(zq):
+    # an empty tensor's address is NULL
+    assert append(zq, cache(zq), rows=0, qkv=None, pos=None, slot=None, q=None) == zq.OK
+    assert attend(zq, cache(zq), rows=0, q=None, out=None, mask=None) == zq.OK
+    assert attend(zq, cache(zq), rows=0, q=None, out=None, kv=None) == zq.ERR_INVALID_ARG
+
+
 @pytest.mark.parametrize("kw", [dict(q=None), dict(table=None), dict(kv=None), dict(start=None), dict(out=None), dict(scratch=None), dict(err=None), dict(batch=0),
                                 dict(rows=-1), dict(heads=0), dict(heads=3), dict(max_pages=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")),
                                 dict(scale=float("nan")), dict(mask=None), dict(words=0), dict(words=-1), dict(q_stride=500), dict(q_stride=515), dict(out_stride=516),
@@ -115,8 +122,10 @@ def rules(zq, desc=None, **kw):
 
 @pytest.mark.parametrize("kw,desc", [(dict(logits=None), {}), (dict(out=None, token=None), {}), (dict(type=5), {}), (dict(ld=99), {}), (dict(out_ld=99), {}),
                                      (dict(out=A, out_ld=128), {}), (dict(logits=A + 2), {}), ({}, dict(batch=0)), ({}, dict(batch=3)),
-                                     ({}, dict(history=A)), ({}, dict(history=A, history_len=A)), ({}, dict(bias_token=A, bias_stride=4)),
-                                     ({}, dict(bias_token=A, bias_value=A, bias_len=A)), ({}, dict(allowed=A, allowed_stride=3)),
+                                     ({}, dict(history=A)), ({}, dict(history=A, history_len=A)), ({}, dict(history=A, history_len=A, history_stride=(1 << 30) + 1)),
+                                     ({}, dict(bias_token=A, bias_stride=4)),
+                                     ({}, dict(bias_token=A, bias_value=A, bias_len=A)), ({}, dict(bias_token=A, bias_value=A, bias_len=A, bias_stride=(1 << 30) + 1)),
+                                     ({}, dict(allowed=A, allowed_stride=3)),
                                      ({}, dict(draft_token=A)), ({}, dict(draft_token=A, row_start=A, tree_mask=A, mask_words=0))])
 def test_rules_refuse_bad_arguments(zq, kw, desc):
     assert rules(zq, desc, **kw) == zq.ERR_INVALID_ARG
