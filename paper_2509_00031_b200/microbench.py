@@ -6,6 +6,7 @@ between iterations) and prints one JSON line per kernel with its achieved rate.
   python -m paper_2509_00031_b200.microbench --op weight_learned --rows 11008 --cols 4096     (Section 4.2 producer)
   python -m paper_2509_00031_b200.microbench --op update --rows 11008 --cols 4096
   python -m paper_2509_00031_b200.microbench --op attention --batch 8 --seq 1024 --heads 32 --dh 128
+  python -m paper_2509_00031_b200.microbench --op tree_attention --batch 32 --context 4096 --drafts 4 --heads 32 --kv-heads 8 --dh 128
   python -m paper_2509_00031_b200.microbench --op norm_act --rows 8192 --cols 4096
   python -m paper_2509_00031_b200.microbench --op ffn_act --rows 8192 --cols 11008
   python -m paper_2509_00031_b200.microbench --op head_loss --M 8192 --N 32000 --K 4096
@@ -162,6 +163,10 @@ def main():
     ap.add_argument("--seq", type=int, default=1024)
     ap.add_argument("--heads", type=int, default=32)
     ap.add_argument("--dh", type=int, default=128)
+    ap.add_argument("--kv-heads", type=int, default=8)
+    ap.add_argument("--drafts", type=int, default=1, help="tree_attention: new rows per request")
+    ap.add_argument("--page", type=int, default=64)
+    ap.add_argument("--type", choices=("f32", "bf16", "f16"), default="bf16")
     ap.add_argument("--iters", type=int, default=10)
     ap.add_argument("--impl", type=int, default=0)
     ap.add_argument("--accumulate", action="store_true")
@@ -264,6 +269,21 @@ def main():
         flops = 2.0 * a.batch * a.seq * a.seq * d          # causal: half of 4*B*S^2*d
         out.update(batch=a.batch, seq=a.seq, heads=a.heads, dh=a.dh, impl=a.impl, ms=med, ms_best=best, tflops=flops / med / 1e9,
                    err_flag=int(err.item()))
+    elif a.op == "tree_attention":
+        # every request has --context keys in scattered pages, the last --drafts of them the new rows, a chain
+        dtype = dict(f32=torch.float32, bf16=torch.bfloat16, f16=torch.float16)[a.type]
+        per = -(-a.context // a.page)
+        k, v = [torch.randn(a.batch * per, a.page, a.kv_heads, a.dh, device=dev).to(dtype) for _ in range(2)]
+        table = torch.randperm(a.batch * per, device=dev).to(torch.int32).view(a.batch, per)
+        q = torch.randn(a.batch * a.drafts, a.heads, a.dh, device=dev).to(dtype)
+        kv_len = torch.full((a.batch,), a.context, dtype=torch.int32, device=dev)
+        row_start = (a.drafts * torch.arange(a.batch + 1, device=dev)).to(torch.int32)
+        got, err = zq.zoqat_op_tree_attention(q, k, v, table, kv_len, row_start)
+        fn = lambda: zq.zoqat_op_tree_attention(q, k, v, table, kv_len, row_start, out=got, err=err)
+        med, best = timed(fn, a.iters, flush)
+        nbytes = 2 * a.batch * a.context * a.kv_heads * a.dh * q.element_size() + 2 * q.numel() * q.element_size()
+        out.update(batch=a.batch, context=a.context, drafts=a.drafts, heads=a.heads, kv_heads=a.kv_heads, dh=a.dh, page=a.page, type=a.type, ms=med,
+                   ms_best=best, gbs=nbytes / med / 1e6, tflops=4.0 * a.batch * a.drafts * a.heads * a.dh * a.context / med / 1e9, err_flag=int(err.item()))
     elif a.op in ("norm_act", "ffn_act"):
         if a.op == "norm_act":
             x = torch.randn(a.rows, a.cols, device=dev)
