@@ -17,7 +17,7 @@
 //   warp 0      K and V tiles by TMA into a ring; warp 3: query tiles into two buffers, a piece ahead
 //   warps 1, 2  one thread issues the scores, one tile ahead, another the products with the weights
 //   warps 4-7   softmax.  All keys of a query share one reference; it moves only when a score passes it by more than 2^8, which
-//               the warps tell one another through four flags per tile while they compute the exponentials as if it did not.
+//               the warps tell one another once per tile, after computing the weights as if it did not.
 //               Maxima over the keys are formed only when a piece begins or a reference moves.
 //   warps 8-11  outputs of a finished piece, from the other one of two TMEM accumulators, while the next piece runs
 // Rounding, masked values and bounded waits as in tree_attention_tc.cu, but for the sums, which are those of the rounded weights.
@@ -44,10 +44,10 @@ template <int DH, int N> struct KeyCfg {
     static constexpr int kOffRef = kOffRed + N * 16;                        // [2][N] floats, then [4][N]: those of the last pieces
     static constexpr int kOffMask = kOffRef + 6 * N * 4;                    // [2][N drafts][kMaskWords]
     static constexpr int kOffBar = kOffMask + 2 * N * kMaskWords * 4;
-    // ring full, ring empty; q full, q empty, s full, s empty (2 each), p full, o full (3 each), o empty, out full (2), piece done (4), flags, joint
-    static constexpr int kBars = 2 * kStages + 18 + 4 + 2;
+    // ring full, ring empty; q full, q empty, s full, s empty (2 each), p full, o full (3 each), o empty, out full (2), piece done (4)
+    static constexpr int kBars = 2 * kStages + 18 + 4;
     static constexpr int kOffMisc = kOffBar + kBars * 8;
-    static constexpr int kUsedBytes = kOffMisc + 64 + 192 + (int)sizeof(TreeRun);
+    static constexpr int kUsedBytes = kOffMisc + 32 + 192 + (int)sizeof(TreeRun);
     static constexpr int kSmemBytes = kUsedBytes + 1024 > 232448 ? 232448 : kUsedBytes + 1024;
     static_assert(kUsedBytes <= 232448 && kStages >= 4, "shared memory");
 };
@@ -115,17 +115,15 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
     auto o_empty = [&](int b) { return bars + 8u * (2 * NS + 14 + b); };     // the output of a piece (by its parity) has been read
     auto out_full = [&](int b) { return bars + 8u * (2 * NS + 16 + b); };    // every product of a piece (by its parity) has completed
     auto piece_done = [&](int i) { return bars + 8u * (2 * NS + 18 + i); };  // the softmax warps are through with a piece (mod 4)
-    const uint32_t flag_bar = bars + 8u * (2 * NS + 22), joint_bar = flag_bar + 8u;
     volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc);
     volatile uint32_t* odd_piece = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 16);    // [4]: piece + 1 with a non-finite draft value
-    volatile uint32_t* flags = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 32);        // [2 tiles][4 warps]
     float* const refs = reinterpret_cast<float*>(sp + Cfg::kOffRef);
-    long long* part = reinterpret_cast<long long*>(sp + Cfg::kOffMisc + 64);
-    TreeRun* run = reinterpret_cast<TreeRun*>(sp + Cfg::kOffMisc + 64 + 192);
+    long long* part = reinterpret_cast<long long*>(sp + Cfg::kOffMisc + 32);
+    TreeRun* run = reinterpret_cast<TreeRun*>(sp + Cfg::kOffMisc + 32 + 192);
 
     if (tid < Cfg::kBars) {
         const int i = tid - 2 * NS;              // one barrier a thread
-        const bool four = (i >= 6 && i < 11) || i == 14 || i == 15 || i >= 18;       // s empty, p full, o empty, piece done, flags, joint
+        const bool four = (i >= 6 && i < 11) || i == 14 || i == 15 || i >= 18;       // s empty, p full, o empty, piece done
         mbar_init(bars + 8u * tid, four ? 4 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -226,20 +224,24 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
         TreeCursor c = run->at;
         bool ok = true, opens = true;
         int q0 = 0, nq = 0;
-        uint32_t piece = 0, checks = 0, joins = 0, cur = 0;      // cur: which copy of the references is in use
+        uint32_t piece = 0, cur = 0;                             // cur: which copy of the references is in use
         uint32_t pb = 0, round = 0;                              // buffer of the weights: t % 3, t / 3
-        auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_poll(bar, parity)) != 0; };
-        auto meet = [&]() -> bool {                              // the four warps
-            __syncwarp();
-            if (lane == 0) mbar_arrive(joint_bar);
-            return wait_all(joint_bar, joins++ & 1u);
+        // A wait that ran out ends nothing here: the four warps go on to meet at the same places, without waiting for or signalling
+        // anyone else.
+        auto await = [&](uint32_t bar, uint32_t parity) { if (ok) ok = __all_sync(0xffffffffu, mbar_poll(bar, parity)) != 0; };
+        auto meet = [] { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); };
+        auto any_of = [](bool mine) -> bool {                    // of the four warps
+            uint32_t any;
+            asm volatile("{ .reg .pred p, q; setp.ne.u32 p, %1, 0; barrier.cta.red.or.pred q, 1, 128, p; selp.u32 %0, 1, 0, q; }"
+                         : "=r"(any) : "r"((uint32_t)mine) : "memory");
+            return any != 0;
         };
-        for (int t = 0; t < n_tiles && ok; ++t) {
+        for (int t = 0; t < n_tiles; ++t) {
             const int buf = t & 1;
             if (opens) { q0 = c.first_query(p.w); nq = c.queries(p.w); }
             const int C = c.r.L - c.r.n;
             const uint32_t s_at = tmem_s + (uint32_t)(buf * N) + t_lane;
-            if (!wait_all(s_full(buf), (t >> 1) & 1u)) { ok = false; break; }
+            await(s_full(buf), (t >> 1) & 1u);
             uint64_t vis = ~0ull;                                // queries that see this key
             if ((c.kt + 1) * kKeys > C) {                        // drafts in the tile, or its end
                 const int key = c.kt * kKeys + me, j = key - C;
@@ -265,8 +267,8 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                 }
                 const uint32_t vseq = t == n_tiles - 1 ? 2u * n_tiles - 1u : 2u * t + 2u;
                 // the V tile's slot was last used at least two tiles ago: behind that product, only this tile's phase is open
-                if (t >= 2 && !wait_all(o_full(pb == 2 ? 0 : pb + 1), (pb == 2 ? round : round - 1u) & 1u)) { ok = false; break; }
-                if (!wait_all(ring_full(vseq % NS), (vseq / NS) & 1u)) { ok = false; break; }
+                if (t >= 2) await(o_full(pb == 2 ? 0 : pb + 1), (pb == 2 ? round : round - 1u) & 1u);
+                await(ring_full(vseq % NS), (vseq / NS) & 1u);
                 if (tree_clean_values<DH, Ops::kExpMask>(sp + (vseq % NS) * Cfg::kTileBytes, max(C - c.kt * kKeys, 0), c.r.L - c.kt * kKeys, me))
                     odd_piece[piece & 3u] = piece + 1;
             }
@@ -275,7 +277,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
             // products depends on its own column only).  The chunks are a loop on purpose: unrolled for 64 queries the steady
             // state no longer fits the schedulers' instruction caches (measured: 20 cycles per query and tile instead of 8).
             // P^T goes into the buffer that the products three tiles ago have read
-            if (round > 0 && !wait_all(o_full(pb), (round & 1u) ^ 1u)) { ok = false; break; }
+            if (round > 0) await(o_full(pb), (round & 1u) ^ 1u);
             uint8_t* const pt = sp + Cfg::kOffP + pb * Cfg::kPBytes + me * 16;
             bool move = opens;
             if (!opens) {
@@ -321,11 +323,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                     }
                 }
                 const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
-                const bool any = __any_sync(0xffffffffu, top > Ops::kBias + kTreeSlack);
-                if (lane == 0) { flags[buf * 4 + quarter] = any; mbar_arrive(flag_bar); }
-                if (!wait_all(flag_bar, checks & 1u)) { ok = false; break; }
-                ++checks;
-                move = (flags[buf * 4] | flags[buf * 4 + 1] | flags[buf * 4 + 2] | flags[buf * 4 + 3]) != 0;
+                move = any_of(top > Ops::kBias + kTreeSlack);
             }
             if (move) {
                 // maxima over the keys, new references, outputs and sums brought to them (rare: chunk by chunk, few registers)
@@ -341,7 +339,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                     const float r = largest16(v);
                     if (!(lane & 1)) red[(16 * k + (lane >> 1)) * 4 + quarter] = r;
                 }
-                if (!meet()) { ok = false; break; }
+                meet();
                 const float* old_ref = refs + cur * N;
                 float* new_ref = refs + (cur ^ 1u) * N;
                 if (me < N) {
@@ -349,10 +347,10 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                     const float top = fmaxf(fmaxf(r.x, r.y), fmaxf(r.z, r.w)) - Ops::kBias;
                     new_ref[me] = me < nq ? fmaxf(top, opens ? kNoRef : old_ref[me]) : INFINITY;     // columns without a query: weight 0
                 }
-                if (!meet()) { ok = false; break; }
+                meet();
                 if (!opens) {
                     // the products before (buffer pb - 1, a round earlier where that is 2)
-                    if (!wait_all(o_full(pb ? pb - 1 : 2), (pb ? round : round - 1u) & 1u)) { ok = false; break; }
+                    await(o_full(pb ? pb - 1 : 2), (pb ? round : round - 1u) & 1u);
                     tc_fence_after();
 #pragma unroll 1
                     for (int n0 = 0; n0 < nq; n0 += 16) {
@@ -398,13 +396,13 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
             fence_async_smem();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) { mbar_arrive(s_empty(buf)); mbar_arrive(p_full(pb)); }
+            if (ok && lane == 0) { mbar_arrive(s_empty(buf)); mbar_arrive(p_full(pb)); }
             if (++pb == 3) { pb = 0; ++round; }
             opens = c.item_ends();
             if (opens || t == n_tiles - 1) {
                 if (me < N) refs[(2 + (piece & 3u)) * N + me] = refs[cur * N + me];        // (a warp behind may still read the copy in use)
                 __syncwarp();
-                if (lane == 0) mbar_arrive(piece_done(piece & 3u));
+                if (ok && lane == 0) mbar_arrive(piece_done(piece & 3u));
                 ++piece;
             }
             c.next(p.w);
