@@ -4,14 +4,18 @@
 //   S^T[key, query] = K Q^T            one thread per key reads its N scores from TMEM
 //   P^T[key, query] = 2^(S^T - ref)    rounded to the cache's type, to shared memory
 //   O^T[column, query] += V^T P^T      V as it lies in the page
-//   l[query] += 1^T P^T                the sums of the weights, by a third product with a matrix of ones: every TMEM lane has
-//                                      them where it needs them at the end, and no thread adds up anything
+//   l[query] += sum_key P^T            N = 16: every thread adds up its keys' weights, the threads' sums are joined when a piece
+//                                      ends; else by a third product with a matrix of ones, which leaves the sums in every TMEM
+//                                      lane.  The tensor pipe spends some 45 cycles on a product of 128 x N x 16 however small N
+//                                      is, and at d_head 64 the third product is 8 of a tile's 20 (16 x 32 heads of 8192 keys:
+//                                      225 us with it, 187 without); joining 32 sums costs short pieces more than that
+//                                      (64 requests of 300 keys, 4 drafts of 4 heads: 51 us with it, 64 without).
 //
 // so the softmax costs 128 * N exponentials per tile of 128 keys, spread over all four schedulers, whatever the tile's number of
 // live queries N = 16, 32 or 64 is; with queries as rows (tree_attention_tc.cu) a single query would cost a whole warp's 128
 // exponentials on one scheduler, and the kernel would be bound by them instead of by reading the cache.  What bounds it is
 // the cache: 64 KB a tile at d_head 128, some 2800 cycles of an SM's share of the memory, against about 600 of the tensor pipe
-// and 64 N of the exponential units.
+// and 8 N of the exponential units.
 //
 // One persistent CTA per SM, 12 warps; the key tiles of all requests are dealt out in equal runs (tree_attention.cuh):
 //   warp 0      K and V tiles by TMA into a ring; warp 3: query tiles into two buffers, a piece ahead
@@ -33,7 +37,9 @@ constexpr float kNoRef = -1.0e30f;       // reference of a query that has seen n
 template <int DH, int N> struct KeyCfg {
     static constexpr int kTileBytes = kKeys * DH * 2;
     static constexpr int kQBytes = N * DH * 2, kPBytes = N * kKeys * 2;
-    static constexpr int kFixed = 2 * kQBytes + 3 * kPBytes + N * 16 + 6 * N * 4 + 2 * N * kMaskWords * 4 + 1024;
+    static constexpr bool kAdd = N == 16;                                   // the threads add up the weights
+    static constexpr int kSumBytes = kAdd ? 4 * N * 16 : 0;                 // [4 pieces][N][4 warps] floats
+    static constexpr int kFixed = 2 * kQBytes + 3 * kPBytes + N * 16 + 6 * N * 4 + 2 * N * kMaskWords * 4 + kSumBytes + 1024;
     static constexpr int kFit = (232448 - kFixed) / kTileBytes;
     // an even number: K tiles (odd places of the sequence) and V tiles (even places) then have slots of their own, so that each
     // slot is consumed by one thread in order and no one can wait for a phase before the one ahead of it has completed
@@ -43,7 +49,8 @@ template <int DH, int N> struct KeyCfg {
     static constexpr int kOffRed = kOffP + 3 * kPBytes;                     // [N][4 warps] floats
     static constexpr int kOffRef = kOffRed + N * 16;                        // [2][N] floats, then [4][N]: those of the last pieces
     static constexpr int kOffMask = kOffRef + 6 * N * 4;                    // [2][N drafts][kMaskWords]
-    static constexpr int kOffBar = kOffMask + 2 * N * kMaskWords * 4;
+    static constexpr int kOffSum = kOffMask + 2 * N * kMaskWords * 4;
+    static constexpr int kOffBar = kOffSum + kSumBytes;
     // ring full, ring empty; q full, q empty, s full, s empty (2 each), p full, o full (3 each), o empty, out full (2), piece done (4)
     static constexpr int kBars = 2 * kStages + 18 + 4;
     static constexpr int kOffMisc = kOffBar + kBars * 8;
@@ -52,9 +59,9 @@ template <int DH, int N> struct KeyCfg {
     static_assert(kUsedBytes <= 232448 && kStages >= 4, "shared memory");
 };
 
-// 16 scores of the thread's key (16 outputs or sums of its column)
-// Largest v[i] over the warp's 32 lanes, for 16 values at once: lanes 2 i and 2 i + 1 return that of v[i].
-__device__ __forceinline__ float largest16(float (&v)[16]) {
+// f over the warp's 32 lanes of v[i], for 16 values at once: lanes 2 i and 2 i + 1 return that of v[i].
+template <typename F>
+__device__ __forceinline__ float join16(float (&v)[16], F f) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int h = 8; h >= 1; h >>= 1) {
@@ -62,10 +69,10 @@ __device__ __forceinline__ float largest16(float (&v)[16]) {
 #pragma unroll
         for (int i = 0; i < h; ++i) {
             const float keep = up ? v[i + h] : v[i], give = up ? v[i] : v[i + h];
-            v[i] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, 2 * h));
+            v[i] = f(keep, __shfl_xor_sync(0xffffffffu, give, 2 * h));
         }
     }
-    return fmaxf(v[0], __shfl_xor_sync(0xffffffffu, v[0], 1));
+    return f(v[0], __shfl_xor_sync(0xffffffffu, v[0], 1));
 }
 
 // Shared-memory descriptor of the weights: query-major cores of 8 queries x 8 keys (128 bytes), no swizzle; the next 8 keys
@@ -140,7 +147,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
         tree_front(p.scratch)[blockIdx.x] = run->begin < run->end && !run->at.item_begins();
     }
     const uint32_t tmem = *tmem_slot;          // (allocated before the barriers in tree_find_run)
-    if (warp >= 4 && warp < 8) {               // the matrix of ones: 16 keys' worth, the same for every step
+    if (!Cfg::kAdd && warp >= 4 && warp < 8) { // the matrix of ones: 16 keys' worth, the same for every step
         tc_fence_after();
         store8(tmem + 6u * N + ((uint32_t)((warp & 3) * 32) << 16), Ops::pack(1.0f, 1.0f));
         tmem_store_wait();
@@ -207,7 +214,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                               (!first || k > 0) ? 1u : 0u);
                 umma_commit(ring_empty(slot));
 #pragma unroll
-                for (int k = 0; k < kKeys / 16; ++k)
+                for (int k = 0; k < kKeys / 16 && !Cfg::kAdd; ++k)
                     umma_f16_ta(tmem_l + b * N, tmem_1, smem_desc_weights(pa + k * 256), kIdescL, (!first || k > 0) ? 1u : 0u);
                 umma_commit(o_full(g));
                 if (++g == 3) { g = 0; ++round; }
@@ -224,6 +231,12 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
         TreeCursor c = run->at;
         bool ok = true, opens = true;
         int q0 = 0, nq = 0;
+        float sums[Cfg::kAdd ? N : 1] = {};                      // of this thread's weights
+        auto add = [&](int n, uint32_t w) {                      // queries n, n + 1
+            const T* x = reinterpret_cast<const T*>(&w);
+            sums[Cfg::kAdd ? n : 0] += Ops::value(x[0]);
+            sums[Cfg::kAdd ? n + 1 : 0] += Ops::value(x[1]);
+        };
         uint32_t piece = 0, cur = 0;                             // cur: which copy of the references is in use
         uint32_t pb = 0, round = 0;                              // buffer of the weights: t % 3, t / 3
         // A wait that ran out ends nothing here: the four warps go on to meet at the same places, without waiting for or signalling
@@ -285,8 +298,9 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                 constexpr int CH = N == 16 ? 1 : 2;              // chunks of 16 or 32
                 const float4* ref4 = reinterpret_cast<const float4*>(refs + cur * N);
                 float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                uint32_t w[2 * CH][4];
 #pragma unroll 1
-                for (int n0 = 0; n0 < nq; n0 += 16 * CH) {
+                for (int n0 = 0; n0 < nq; n0 += 16 * CH) {       // (once where the threads add up)
                     uint32_t s[CH][16];
 #pragma unroll
                     for (int k = 0; k < CH; ++k) load16(s_at + (uint32_t)(n0 + 16 * k), s[k]);
@@ -312,18 +326,23 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                     uint8_t* at = pt + (n0 >> 3) * (kKeys * 16);
 #pragma unroll
                     for (int k = 0; k < 2 * CH; ++k) {
-                        uint32_t w[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const float a = __uint_as_float(s[k >> 1][8 * (k & 1) + 2 * e]), b = __uint_as_float(s[k >> 1][8 * (k & 1) + 2 * e + 1]);
                             top4[e] = fmaxf(top4[e], fmaxf(a, b));
-                            w[e] = Ops::pack(tree_ex2(a), tree_ex2(b));
+                            w[k][e] = Ops::pack(tree_ex2(a), tree_ex2(b));
                         }
-                        *reinterpret_cast<uint4*>(at + k * (kKeys * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4*>(at + k * (kKeys * 16)) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
                     }
                 }
                 const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
                 move = any_of(top > Ops::kBias + kTreeSlack);
+                if (Cfg::kAdd && !move) {
+#pragma unroll
+                    for (int k = 0; k < 2 * CH; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) add(8 * k + 2 * e, w[k][e]);
+                }
             }
             if (move) {
                 // maxima over the keys, new references, outputs and sums brought to them (rare: chunk by chunk, few registers)
@@ -336,7 +355,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                     float v[16];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) v[e] = (seen >> e) & 1u ? __uint_as_float(s[e]) * p.scale_log2 : -INFINITY;
-                    const float r = largest16(v);
+                    const float r = join16(v, [](float a, float b) { return fmaxf(a, b); });
                     if (!(lane & 1)) red[(16 * k + (lane >> 1)) * 4 + quarter] = r;
                 }
                 meet();
@@ -357,20 +376,27 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                         uint32_t o[16], l[16];
                         const uint32_t at = (uint32_t)((piece & 1u) * N + n0) + t_lane;
                         load16(tmem_o + at, o);
-                        load16(tmem_l + at, l);
+                        if (!Cfg::kAdd) load16(tmem_l + at, l);
                         tmem_ld_wait();
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             const float f = tree_ex2(old_ref[n0 + e] - new_ref[n0 + e]);
                             o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                            l[e] = __float_as_uint(__uint_as_float(l[e]) * f);
+                            if (!Cfg::kAdd) l[e] = __float_as_uint(__uint_as_float(l[e]) * f);
                         }
                         store16(tmem_o + at, o);
-                        store16(tmem_l + at, l);
+                        if (!Cfg::kAdd) store16(tmem_l + at, l);
                     }
                     tmem_store_wait();
                 }
                 const float4* moved = reinterpret_cast<const float4*>(new_ref);
+                if (Cfg::kAdd && opens) {
+#pragma unroll
+                    for (int n = 0; n < N; ++n) sums[n] = 0.0f;
+                } else if (Cfg::kAdd) {
+#pragma unroll
+                    for (int n = 0; n < N; ++n) sums[n] *= tree_ex2(old_ref[n] - new_ref[n]);       // (anything in columns without a query)
+                }
 #pragma unroll 1
                 for (int k = 0; 16 * k < nq; ++k) {
                     const uint32_t seen = (uint32_t)(vis >> (16 * k));
@@ -390,6 +416,10 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                     }
                     *reinterpret_cast<uint4*>(pt + (2 * k) * (kKeys * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
                     *reinterpret_cast<uint4*>(pt + (2 * k + 1) * (kKeys * 16)) = make_uint4(w[4], w[5], w[6], w[7]);
+                    if (Cfg::kAdd) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) add(2 * i, w[i]);
+                    }
                 }
                 cur ^= 1u;
             }
@@ -401,6 +431,17 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
             opens = c.item_ends();
             if (opens || t == n_tiles - 1) {
                 if (me < N) refs[(2 + (piece & 3u)) * N + me] = refs[cur * N + me];        // (a warp behind may still read the copy in use)
+                if (Cfg::kAdd) {
+                    float* const to = reinterpret_cast<float*>(sp + Cfg::kOffSum) + (piece & 3u) * (4 * N);
+#pragma unroll
+                    for (int k = 0; k < N / 16; ++k) {
+                        float v[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) v[e] = sums[Cfg::kAdd ? 16 * k + e : 0];
+                        const float r = join16(v, [](float a, float b) { return a + b; });
+                        if (!(lane & 1)) to[(16 * k + (lane >> 1)) * 4 + quarter] = r;
+                    }
+                }
                 __syncwarp();
                 if (ok && lane == 0) mbar_arrive(piece_done(piece & 3u));
                 ++piece;
@@ -434,7 +475,13 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                     uint32_t o[16], l[16];
                     const uint32_t at = (uint32_t)((piece & 1u) * N + n0) + t_lane;
                     load16(tmem_o + at, o);
-                    load16(tmem_l + at, l);
+                    if (Cfg::kAdd) {
+                        const float4* of = reinterpret_cast<const float4*>(sp + Cfg::kOffSum) + (piece & 3u) * N + n0;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) { const float4 x = of[e]; l[e] = __float_as_uint((x.x + x.y) + (x.z + x.w)); }
+                    } else {
+                        load16(tmem_l + at, l);
+                    }
                     tmem_ld_wait();
                     if (repair) {                                // what the non-finite values of drafts add to this column
                         uint32_t last = 0xFFFFFFFFu;
