@@ -14,10 +14,11 @@
 // the biases name are marked in a bitmap of the slice.  All others stream through registers, masked, written and searched,
 // with no arithmetic for rules that do not concern them; the marked ones are left out there and done by themselves: a marked
 // token's place in the bitmap is its place in dense arrays of counts and bias sums (integer atomics: the order does not matter;
-// one warp adds the biases up in list order), from which its logit is then computed once.  256 rows of 50272 binary32 logits
-// with histories of 3000, 200 biases and a mask take 36 us, without rules 25, a copy of the logits 17.  (Passing every slice through shared memory next to
-// dense counts took 64 us.)  The cluster's choices are joined through distributed shared memory, so the choice needs no second
-// launch and no scratch.  A table of counts per request would instead add its own bytes to the logits' on every step.
+// one warp adds the biases up in list order), from which its logit is then computed once.  A crew of four warps counts while the
+// others stream.  256 rows of 50272 binary32 logits with histories of 3000, 200 biases and a mask take 36 us, without rules 25, a
+// copy of the logits 17 (passing every slice through shared memory next to dense counts took 64, counting before streaming 47).
+// The cluster's choices are joined through distributed shared memory, so the choice needs no second launch and no scratch.  A
+// table of counts per request would instead add its own bytes to the logits' on every step.
 #include "common.cuh"
 #include "serve.cuh"
 #include "tc_ptx.cuh"
@@ -306,7 +307,8 @@ logit_rules_kernel(const T* logits, int64_t ld, int rows, int vocab, int slice, 
 template <typename T, int VEC>
 int launch_rules_vec(const T* logits, int64_t ld, int rows, int vocab, const LogitRules& r, T* out, int64_t out_ld, int32_t* token,
                  cudaStream_t s, bool dependent) {
-    // at least 1024 tokens to a CTA, and no more CTAs of a cluster than it takes to fill the SMs
+    // at least 1024 tokens to a CTA, and no more CTAs of a cluster than it takes to fill the SMs (1 / 2 / 4 / 8 CTAs a row, histories
+    // of 700, us: 8 rows of 32000 16 / 14 / 14 / 13; 64 of 50272 21 / 16 / 16 / 25; 256 of 50272 29 / 35 / 47 / 74)
     int ranks = 1;
     while (ranks < 8 && vocab > 1024 * ranks && rows * ranks < 148) ranks *= 2;
     const int slices = (vocab + ranks * kMaxSlice - 1) / (ranks * kMaxSlice) * ranks;
