@@ -426,6 +426,38 @@ def test_attention_captured_and_replayed_as_lengths_change(zq):
         assert bool(((out[:rows].double() - want).abs() <= bound).all()) and bool((out[rows:] == 5.0).all())
 
 
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("f16", 64)])
+def test_unseen_drafts_of_wide_trees_may_hold_anything(zq, dtype, dh):
+    # 72 drafts of 4 heads are two tiles of queries, the first one full; drafts lie in one, two and two tiles of keys
+    for C in (0, 100, 700):
+        pr = attention_problem(C + 3, dtype, 8, 2, dh, 16, "token", [C], [72], "tree")
+        want, bound = attention_oracle(pr)
+        marks = {20: float("inf"), 41: -float("inf"), 71: float("nan")}
+        for j, x in marks.items():
+            pr["v"][pr["table"][0, (C + j) // 16].item(), (C + j) % 16, :, j % 64] = x
+        got = run_attention(zq, pr)
+        for i in range(72):
+            hit = {j % 64: x for j, x in marks.items() if j in pr["seen"][0][i]}
+            rest = [e for e in range(dh) if e not in hit]
+            assert bool(((got[i][:, rest].double() - want[i][:, rest]).abs() <= bound[i][:, rest]).all()), (C, i)
+            for e, x in hit.items():
+                assert bool(torch.isnan(got[i, :, e]).all() if math.isnan(x) else (got[i, :, e] == x).all()), (C, i, e)
+        pr["k"][pr["table"][0, (C + 71) // 16].item(), (C + 71) % 16] = float("nan")
+        got = run_attention(zq, pr)
+        for i in range(72):
+            assert bool(torch.isnan(got[i]).all()) == (71 in pr["seen"][0][i]), (C, i)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_wide_trees_with_steep_scores(zq, dtype):
+    # the running references of both groups of queries move often
+    pr = attention_problem(13, dtype, 16, 4, 128, 16, "token", [700, 2900], [48, 60], "tree", gap=1, q_scale=30.0)
+    got = run_attention(zq, pr)
+    want, bound = attention_oracle(pr)
+    off = (got[:pr["rows"]].double() - want).abs()
+    assert bool((off <= bound).all()), (float(off.max()), float((off / bound.clamp(min=1e-30)).max()))
+
+
 def test_no_rows(zq):
     k, v = [torch.randn((4, 16, 2, 64), device="cuda").to(torch.bfloat16) for _ in range(2)]
     keep = k.clone()
