@@ -244,9 +244,13 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
         // A wait that ran out ends nothing here: the four warps go on to meet at the same places, without waiting for or signalling
         // anyone else.
         auto await = [&](uint32_t bar, uint32_t parity) { if (ok) ok = __all_sync(0xffffffffu, mbar_poll(bar, parity)) != 0; };
-        auto meet = [] { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); };
+        auto meet = [] {
+            __syncwarp();
+            asm volatile("barrier.cta.sync 1, 128;" ::: "memory");
+        };
         auto any_of = [](bool mine) -> bool {                    // of the four warps
             uint32_t any;
+            __syncwarp();
             asm volatile("{ .reg .pred p, q; setp.ne.u32 p, %1, 0; barrier.cta.red.or.pred q, 1, 128, p; selp.u32 %0, 1, 0, q; }"
                          : "=r"(any) : "r"((uint32_t)mine) : "memory");
             return any != 0;
