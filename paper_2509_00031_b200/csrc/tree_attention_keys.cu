@@ -162,7 +162,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
     constexpr uint32_t kIdesc = (1u << 4) | (Ops::kFormat << 7) | (Ops::kFormat << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 
     if (warp == 0 && n_tiles > 0) {
-        tree_load_keys<DH, NS>(p, &map_k, &map_v, run, base, ring_full(0), ring_empty(0));
+        tree_load_keys<DH, NS, 1>(p, &map_k, &map_v, run, base, ring_full(0), ring_empty(0));
     } else if (warp == 3 && n_tiles > 0) {
         tree_load_queries<DH, N, 32, 2, T>(p, run, sp + Cfg::kOffQ, reinterpret_cast<uint32_t*>(sp + Cfg::kOffMask), piece_done(0), q_full(0), q_empty(0), lane);
     } else if (warp == 1 && n_tiles > 0) {

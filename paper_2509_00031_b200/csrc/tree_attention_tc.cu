@@ -6,22 +6,22 @@
 // This file: many queries per key head (wide trees, grouped heads); the host sends fewer to tree_attention_keys.cu.  The queries
 // that read one key head - every draft times the g heads of the group - share row tiles of 256, so each cached byte is fetched once
 // per request, key head and 256 queries.  For 256 queries a tile of 128 keys at d_head 128 costs 2048 cycles of the tensor pipe
-// and 2048 of the exponential unit against some 2800 of an SM's share of the memory; measured 4600, because the two groups
-// below run in step (their weights together, then their products) rather than by turns.  4 contexts of 60-120 thousand keys, 64
-// drafts of 4 heads: 447 us.  Tried: two tiles of 128 queries apart, 540 us (the second reads the keys again long after they have
-// left L2); weights in TMEM over the scores, with two more stages of the ring, 503 us (PV and the next scores of a group then run
-// one after the other); K and V in turn, 450 us.
+// and 2048 of the exponential unit against some 2800 of an SM's share of the memory; measured 4350: a group's weights, then its
+// two products of some 700 cycles each, half hidden behind the other group's.  4 contexts of 60-120 thousand keys, 64 drafts of
+// 4 heads: 430 us.  (Two tiles of 128 queries apart: 540, the second reads the keys again long after they have left L2.)
 //
 // One persistent CTA per SM, 12 warps; the key tiles of all requests are dealt out in equal runs (tree_attention.cuh):
 //   warp 0      K and V tiles by TMA into a ring; warp 3: the query tile of the next piece
-//   warps 1, 2  one thread issues S = Q K^T as soon as the scores before have been read, another O += P V with P from shared
-//               memory and V as it lies in the page (keys along k, so no transposition): the waits and commits of one thread for
-//               both left the tensor pipe idle for more than half of the time
-//   warps 4-7, 8-11  two softmax groups, each for 128 of the queries, with score, weight and output tiles of its own; while one
-//               forms weights, the tensor pipe works for the other.  A thread owns a query row: it reads the tile's 128 scores
-//               and writes the weights, rounded to the cache's type, to shared memory.  The weights are formed against the
-//               reference as it stands; where a row's maximum turns out to have grown by more than 2^8 the reference moves
-//               and the tile's weights are formed again.  A tile of up to 128 queries leaves the second group idle.
+//   warps 4-7, 8-11  two softmax groups, each for 128 of the queries.  A thread owns a query row: it reads the tile's 128 scores
+//               from TMEM twice, for the maximum and for the weights, and writes the weights, rounded to the cache's type, over
+//               the scores.  Where a row's maximum has grown by more than 2^8 its reference moves, and its outputs with it.
+//   warp 1      one thread issues the products of both groups by turns: O += P V with P from TMEM and V as it lies in the page
+//               (keys along k, so no transposition), then S = Q K^T of the group's next tile, while the other group forms its
+//               weights.  (A thread per group: the tensor pipe then serves both at once, the groups fall into step and nothing
+//               is hidden, 503 us; a thread for S, one for PV, P in shared memory: 447.)
+// A tile of up to 128 queries leaves the second group idle.  P from TMEM because shared memory feeds 128 bytes a cycle: the
+// products alone take 192 KB per tile of 256 queries (P from shared memory: 256, and 64 more to write it), the tiles' arrival
+// 64, and its place holds two more stages of the ring.
 // Rounding: the products are exact in binary32 up to accumulation; the weights are rounded to 11 (fp16) or 8 (bf16) bits for
 // the second product, the sums are formed from the unrounded weights, the output is rounded once.  fp16 weights are scaled by
 // 2^7, which keeps small ones out of the subnormals; the largest is then 2^15.
@@ -40,12 +40,10 @@ constexpr float kNoRef = -1.0e30f;       // reference of a row that has seen not
 
 template <int DH> struct TcCfg {
     static constexpr int kTileBytes = kKeys * DH * 2;                       // one K or V tile
-    static constexpr int kPBytes = kRows * kKeys * 2;                       // [half of the keys][128 rows][128 bytes], as Q
-    static constexpr int kStages = DH == 128 ? 3 : 7;
+    static constexpr int kStages = DH == 128 ? 5 : 8;
     static constexpr int kOffRing = kTileRows * DH * 2;                     // the query tile comes first
-    static constexpr int kOffP = kOffRing + kStages * kTileBytes;
-    static constexpr int kOffBar = kOffP + 2 * kPBytes;
-    static constexpr int kBars = 2 * kStages + 12;
+    static constexpr int kOffBar = kOffRing + kStages * kTileBytes;
+    static constexpr int kBars = 2 * kStages + 10;
     static constexpr int kOffMisc = kOffBar + kBars * 8;                    // TMEM base, non-finite marks, run
     static constexpr int kUsedBytes = kOffMisc + 32 + 192 + (int)sizeof(TreeRun);
     static constexpr int kSmemBytes = kUsedBytes + 1024 > 232448 ? 232448 : kUsedBytes + 1024;
@@ -76,21 +74,21 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     auto ring_empty = [&](int s) { return bars + 8u * (NS + s); };
     const uint32_t q_full = bars + 8u * (2 * NS), q_empty = q_full + 8u;
     auto s_full = [&](int g) { return bars + 8u * (2 * NS + 2 + g); };
-    auto s_empty = [&](int g) { return bars + 8u * (2 * NS + 4 + g); };
-    auto p_full = [&](int g) { return bars + 8u * (2 * NS + 6 + g); };
-    auto o_full = [&](int g) { return bars + 8u * (2 * NS + 8 + g); };
-    auto o_empty = [&](int g) { return bars + 8u * (2 * NS + 10 + g); };
+    auto p_full = [&](int g) { return bars + 8u * (2 * NS + 4 + g); };
+    auto o_full = [&](int g) { return bars + 8u * (2 * NS + 6 + g); };
+    auto o_empty = [&](int g) { return bars + 8u * (2 * NS + 8 + g); };
     volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc);
-    volatile uint32_t* odd_piece = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 8);   // [2]: piece + 1 with a non-finite draft value
+    // [4], by piece: piece + 1 with a non-finite draft value (the groups are within two tiles of one another)
+    volatile uint32_t* odd_piece = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 8);
     long long* part = reinterpret_cast<long long*>(sp + Cfg::kOffMisc + 32);
     TreeRun* run = reinterpret_cast<TreeRun*>(sp + Cfg::kOffMisc + 32 + 192);
 
     if (tid < Cfg::kBars) {
-        const int i = tid - 2 * NS;              // one barrier a thread; s empty, p full and o empty count a group's warps
-        mbar_init(bars + 8u * tid, (i >= 4 && i < 8) || i >= 10 ? 4 : 1);
+        const int i = tid - 2 * NS;              // one barrier a thread; a group's four warps arrive for p_full and o_empty
+        mbar_init(bars + 8u * tid, i == 4 || i == 5 || i >= 8 ? 4 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (tid < 2) odd_piece[tid] = 0;
+    if (tid < 4) odd_piece[tid] = 0;
     if (tid == 32) { prefetch_tmap(&map_k); prefetch_tmap(&map_v); }
     if (warp == 1) {
         tmem_alloc(base + Cfg::kOffMisc, 512);
@@ -110,91 +108,86 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     const int n_tiles = (int)(run->end - run->begin);
 
     constexpr uint32_t kIdesc = (1u << 4) | (Ops::kFormat << 7) | (Ops::kFormat << 10) | ((uint32_t)(kRows >> 4) << 24);
-    // Place `seq` of the ring's sequence has landed.  K and V share the slots and have consumers of their own, so a consumer may
-    // come to a slot whose use before is still to land: it first waits until that use has been consumed (the one before that was
-    // the consumer's own kind and is past), then for this one.
-    auto slot_filled = [&](int slot, uint32_t seq) -> bool {
-        if (seq >= (uint32_t)NS && !mbar_poll(ring_empty(slot), ((seq / NS) & 1u) ^ 1u)) return false;
-        return mbar_poll(ring_full(slot), (seq / NS) & 1u);
-    };
 
     if (warp == 0 && n_tiles > 0) {
-        tree_load_keys<DH, NS>(p, &map_k, &map_v, run, base + Cfg::kOffRing, ring_full(0), ring_empty(0));
+        tree_load_keys<DH, NS, 0>(p, &map_k, &map_v, run, base + Cfg::kOffRing, ring_full(0), ring_empty(0));
     } else if (warp == 3 && n_tiles > 0) {
         tree_load_queries<DH, kTileRows, 32, 1, T>(p, run, sp, nullptr, 0u, q_full, q_empty, lane);
     } else if (warp == 1 && n_tiles > 0) {
-        // ---------------- the scores
+        // ---------------- the products, of the groups by turns
         if (lane == 0) {
             TreeCursor c = run->at;
-            uint32_t piece = 0, done[2] = {0, 0};      // score tiles issued for each group
+            uint32_t piece = 0, seq = 0, done[2] = {0, 0}, uses[2] = {0, 0};     // pieces, tiles of the ring; tiles and pieces of each group
             int groups = 0;
-            bool ok = true;
-            for (int t = 0; t < n_tiles && ok; ++t, c.next(p.w)) {
-                const uint32_t seq = t == 0 ? 0u : 2u * t - 1u;
-                const int slot = seq % NS;
-                if (t == 0 || c.item_begins()) {
-                    if (!mbar_poll(q_full, piece & 1u)) { ok = false; break; }
-                    ++piece;
-                    groups = c.queries(p.w) > kRows ? 2 : 1;
-                }
-                if (!slot_filled(slot, seq)) { ok = false; break; }
-                const uint32_t ka = base + Cfg::kOffRing + slot * Cfg::kTileBytes;
+            bool ok = true, first = true, last = n_tiles == 1 || c.item_ends();  // the tile opens, closes its piece
+            auto scores = [&](int g, uint32_t at) {
+                tc_fence_after();
+                const uint32_t ka = base + Cfg::kOffRing + (at % NS) * Cfg::kTileBytes;
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    if (g == groups) break;
-                    if (done[g] > 0 && !mbar_poll(s_empty(g), (done[g] - 1) & 1u)) { ok = false; break; }
-                    ++done[g];
-                    tc_fence_after();
-#pragma unroll
-                    for (int k = 0; k < DH / 16; ++k) {
-                        const uint64_t da = smem_desc_sw128(base + g * (kRows * 128) + (k >> 2) * (kTileRows * 128)) + (uint64_t)(2 * (k & 3));
-                        const uint64_t db = smem_desc_sw128(ka + (k >> 2) * 1024, tree_group_bytes<DH>()) + (uint64_t)(2 * (k & 3));
-                        umma_bf16(tmem_s + 128u * g, da, db, kIdesc | ((uint32_t)(kKeys >> 3) << 17), k > 0 ? 1u : 0u);
-                    }
-                    umma_commit(s_full(g));
+                for (int k = 0; k < DH / 16; ++k) {
+                    const uint64_t da = smem_desc_sw128(base + g * (kRows * 128) + (k >> 2) * (kTileRows * 128)) + (uint64_t)(2 * (k & 3));
+                    const uint64_t db = smem_desc_sw128(ka + (k >> 2) * 1024, tree_group_bytes<DH>()) + (uint64_t)(2 * (k & 3));
+                    umma_bf16(tmem_s + 128u * g, da, db, kIdesc | ((uint32_t)(kKeys >> 3) << 17), k > 0 ? 1u : 0u);
                 }
-                if (!ok) break;
-                umma_commit(ring_empty(slot));
-                if (c.item_ends() || t == n_tiles - 1) umma_commit(q_empty);
+                umma_commit(s_full(g));
+            };
+            auto filled = [&](uint32_t at) { return mbar_poll(ring_full(at % NS), (at / NS) & 1u); };
+            ok = mbar_poll(q_full, 0u) && filled(0u);
+            if (ok) {
+                groups = c.queries(p.w) > kRows ? 2 : 1;
+                for (int g = 0; g < groups; ++g) scores(g, 0u);
+                umma_commit(ring_empty(0));
+                if (last) umma_commit(q_empty);
+                piece = seq = 1;
             }
-            if (!ok) atomicExch(p.w.err_flag, kErrTreeWait);
-        }
-    } else if (warp == 2 && n_tiles > 0) {
-        // ---------------- the outputs
-        if (lane == 0) {
-            TreeCursor c = run->at;
-            uint32_t done[2] = {0, 0}, uses[2] = {0, 0};         // weight tiles taken, pieces begun, for each group
-            int groups = 0;
-            bool ok = true, first = true;                        // first: the tile opens its piece
-            for (int t = 0; t < n_tiles && ok; ++t, c.next(p.w)) {
-                if (first) {
-                    // the outputs of both groups' last pieces have been read (for an idle group too: none falls behind by more than a piece)
-                    groups = c.queries(p.w) > kRows ? 2 : 1;
-                    for (int g = 0; g < 2; ++g) {
-                        if (uses[g] > 0 && !mbar_poll(o_empty(g), (uses[g] - 1) & 1u)) { ok = false; break; }
-                        if (g < groups) ++uses[g];
-                    }
-                    if (!ok) break;
+            // O += P V of this tile, then S of the next - over the weights: the products of one thread run in order - for one group,
+            // then for the other, which forms its weights meanwhile
+            for (int t = 0; t < n_tiles && ok; ++t) {
+                const bool more = t + 1 < n_tiles, next_opens = last;
+                const uint32_t v_at = seq, k_at = seq + 1;
+                int next_groups = groups;
+                bool next_last = false;
+                if (more) {
+                    c.next(p.w);
+                    if (next_opens) next_groups = c.queries(p.w) > kRows ? 2 : 1;
+                    next_last = t + 2 == n_tiles || c.item_ends();
                 }
-                const uint32_t seq = t == n_tiles - 1 ? 2u * n_tiles - 1u : 2u * t + 2u;
-                const int slot = seq % NS;
+                if (!filled(v_at)) { ok = false; break; }
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
-                    if (g == groups) break;
-                    if (!mbar_poll(p_full(g), done[g] & 1u) || (g == 0 && !slot_filled(slot, seq))) { ok = false; break; }
-                    ++done[g];
-                    tc_fence_after();
-                    const uint32_t va = base + Cfg::kOffRing + slot * Cfg::kTileBytes, pa = base + Cfg::kOffP + g * Cfg::kPBytes;
+                    if (g < groups) {
+                        // a new piece's first product overwrites outputs that have been read
+                        if ((first && uses[g] > 0 && !mbar_poll(o_empty(g), (uses[g] - 1) & 1u)) || !mbar_poll(p_full(g), done[g] & 1u)) { ok = false; break; }
+                        ++done[g];
+                        tc_fence_after();
+                        const uint32_t va = base + Cfg::kOffRing + (v_at % NS) * Cfg::kTileBytes;
 #pragma unroll
-                    for (int k = 0; k < kKeys / 16; ++k)
-                        umma_bf16(tmem_o + 128u * g, smem_desc_sw128(pa + (k >> 2) * (kRows * 128)) + (uint64_t)(2 * (k & 3)),
-                                  smem_desc_sw128_mn(va + k * 2 * tree_group_bytes<DH>(), 1024, tree_group_bytes<DH>()),
-                                  kIdesc | (1u << 16) | ((uint32_t)(DH >> 3) << 17), (!first || k > 0) ? 1u : 0u);      // bit 16: B is MN-major
-                    if (g == groups - 1) umma_commit(ring_empty(slot));
-                    umma_commit(o_full(g));                      // the last: once it has arrived, none of the thread's arrivals is to come
+                        for (int k = 0; k < kKeys / 16; ++k)
+                            umma_f16_ta(tmem_o + 128u * g, tmem_s + 128u * g + 8u * k,
+                                        smem_desc_sw128_mn(va + k * 2 * tree_group_bytes<DH>(), 1024, tree_group_bytes<DH>()),
+                                        kIdesc | (1u << 16) | ((uint32_t)(DH >> 3) << 17), (!first || k > 0) ? 1u : 0u);      // bit 16: B is MN-major
+                        if (g == groups - 1) umma_commit(ring_empty(v_at % NS));
+                        if (last) { umma_commit(o_full(g)); ++uses[g]; }
+                    }
+                    if (more && !next_opens && g < groups) {
+                        if (g == 0 && !filled(k_at)) { ok = false; break; }
+                        scores(g, k_at);
+                    }
                 }
                 if (!ok) break;
-                first = c.item_ends();
+                if (more && next_opens) {                        // other queries: behind the last products with the ones before
+                    if (!mbar_poll(q_full, piece & 1u) || !filled(k_at)) { ok = false; break; }
+                    ++piece;
+                    for (int g = 0; g < next_groups; ++g) scores(g, k_at);
+                }
+                if (more) {
+                    umma_commit(ring_empty(k_at % NS));
+                    if (next_last) umma_commit(q_empty);
+                }
+                seq += 2;
+                groups = next_groups;
+                first = next_opens;
+                last = next_last;
             }
             if (!ok) atomicExch(p.w.err_flag, kErrTreeWait);
         }
@@ -202,12 +195,12 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         // ---------------- softmax groups
         const int g = (warp >> 2) - 1, quarter = warp & 3, row = quarter * 32 + lane;        // row of the group
         const uint32_t t_lane = (uint32_t)(quarter * 32) << 16;
-        const uint32_t ts = tmem_s + 128u * g + t_lane;
+        const uint32_t ts = tmem_s + 128u * g + t_lane, to = tmem_o + 128u * g + t_lane;
         TreeCursor c = run->at;
         bool split_front = !c.item_begins(), ok = true, opens = true;
         float m_ref = kNoRef, l_run = 0.0f;
         int kt_first = 0, q0 = 0, nq = 0, tok = 0, hg = 0;       // of the group: first query, queries
-        uint32_t piece = 0, done = 0;                            // tiles of this group
+        uint32_t piece = 0, done = 0, uses = 0;                  // pieces; tiles and pieces of this group
         const uint32_t* mask = nullptr;
         auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_poll(bar, parity)) != 0; };
         for (int t = 0; t < n_tiles && ok; ++t) {
@@ -224,19 +217,19 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
             const bool warp_live = quarter * 32 < nq, item_ends = c.item_ends(), piece_ends = item_ends || t == n_tiles - 1;
             if (nq > 0) {
                 const bool tail = (c.kt + 1) * kKeys > C;
-                // the scores; and the group's weight tile and outputs are free: behind the product of its tile before
-                if (!wait_all(s_full(g), done & 1u) || (done > 0 && !wait_all(o_full(g), (done - 1) & 1u))) { ok = false; break; }
+                if (!wait_all(s_full(g), done & 1u)) { ok = false; break; }      // the product with V before has run as well
                 ++done;
                 tc_fence_after();
-                if (tail && g == 0) {                            // (the second group's product with this tile comes after the first's)
-                    const uint32_t vseq = t == n_tiles - 1 ? 2u * n_tiles - 1u : 2u * t + 2u;
-                    if (!__all_sync(0xffffffffu, slot_filled(vseq % NS, vseq))) { ok = false; break; }
-                    if (tree_clean_values<DH, Ops::kExpMask>(sp + Cfg::kOffRing + (vseq % NS) * Cfg::kTileBytes, max(C - c.kt * kKeys, 0),
+                if (tail && g == 0) {
+                    const int slot = (2 * t + 1) % NS;
+                    if (!wait_all(ring_full(slot), (uint32_t)((2 * t + 1) / NS) & 1u)) { ok = false; break; }
+                    if (tree_clean_values<DH, Ops::kExpMask>(sp + Cfg::kOffRing + slot * Cfg::kTileBytes, max(C - c.kt * kKeys, 0),
                                                              c.r.L - c.kt * kKeys, row))
-                        odd_piece[piece & 1u] = piece + 1;
+                        odd_piece[piece & 3u] = piece + 1;
                 }
                 if (warp_live) {
-                    if (tail) {                                  // holds drafts or the request's end: take out what the row does not see
+                    // Loops over chunks of 32 columns, the next on its way while one is worked on.
+                    if (tail) {                                  // take out what the row does not see
 #pragma unroll 1
                         for (int q = 0; q < 4; ++q) {
                             const uint32_t vis = row < nq ? visible_word(c.kt * kKeys + 32 * q, C, c.r.n, tok, mask, p.mask_words) : 0u;
@@ -250,87 +243,79 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                         }
                         tmem_store_wait();
                     }
-                    // The scores stay in TMEM and are taken in chunks of 32 columns, the next on its way while one is worked on.
+                    uint32_t sa[32], sb[32];
+                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    auto highest = [&](const uint32_t (&s)[32]) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) t4[(e >> 1) & 3] = fmaxf(t4[(e >> 1) & 3], fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
+                    };
+                    tmem_ld32(ts, sa);
+#pragma unroll
+                    for (int q = 0; q < 4; q += 2) {
+                        load32_wait(sa);
+                        tmem_ld32(ts + 32u * q + 32u, sb);
+                        highest(sa);
+                        load32_wait(sb);
+                        tmem_ld32(ts + (q < 2 ? 64u : 0u), sa);  // at last the first chunk again, for the weights
+                        highest(sb);
+                    }
+                    // weights 2^(score - reference): the largest is 2^kBias .. 2^(kBias + 8)
+                    const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * p.scale_log2 - Ops::kBias;
                     if (opens) {
-                        float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                        m_ref = fmaxf(top, kNoRef);
+                    } else {
+                        const bool grow = row < nq && top > m_ref + kTreeSlack;
+                        if (__any_sync(0xffffffffu, grow)) {     // rare: move the reference, bring the row's outputs and sum to it
+                            const float f = grow ? tree_ex2(m_ref - top) : 1.0f;
 #pragma unroll 1
-                        for (int q = 0; q < 4; ++q) {
-                            uint32_t s[32];
-                            tmem_ld32(ts + 32u * q, s);
-                            load32_wait(s);
+                            for (int c0 = 0; c0 < DH; c0 += 16) {
+                                uint32_t o[16];
+                                load16(to + (uint32_t)c0, o);
+                                load16_wait(o);
 #pragma unroll
-                            for (int e = 0; e < 32; e += 2) t4[(e >> 1) & 3] = fmaxf(t4[(e >> 1) & 3], fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
-                        }
-                        // weights 2^(score - reference): the largest is 2^kBias .. 2^(kBias + 8)
-                        m_ref = fmaxf(fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * p.scale_log2 - Ops::kBias, kNoRef);
-                    }
-                    uint8_t* const prow = sp + Cfg::kOffP + g * Cfg::kPBytes + row * 128;
-                    const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
-                    float2 sum2[2];
-#pragma unroll 1
-                    for (int turn = 0; turn < 2; ++turn) {
-                        float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                        const float2 minus = make_float2(-m_ref, -m_ref);
-                        sum2[0] = sum2[1] = make_float2(0.0f, 0.0f);
-                        auto weigh = [&](const uint32_t (&s)[32], int q) {
-                            uint8_t* const at = prow + (q >> 1) * (kRows * 128);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                uint32_t w[4];
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    const float2 x = make_float2(__uint_as_float(s[8 * i + 2 * e]), __uint_as_float(s[8 * i + 2 * e + 1]));
-                                    t4[e] = fmaxf(t4[e], fmaxf(x.x, x.y));
-                                    float2 y = tree_fma2(x, scale2, minus);
-                                    y.x = tree_ex2(y.x);
-                                    y.y = tree_ex2(y.y);
-                                    sum2[e & 1] = tree_add2(sum2[e & 1], y);
-                                    w[e] = Ops::pack(y.x, y.y);
-                                }
-                                *reinterpret_cast<uint4*>(at + (((4 * (q & 1) + i) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                store16(to + (uint32_t)c0, o);
                             }
-                        };
-                        uint32_t sa[32], sb[32];
-                        tmem_ld32(ts, sa);
-#pragma unroll 1
-                        for (int q = 0; q < 4; q += 2) {
-                            load32_wait(sa);
-                            tmem_ld32(ts + 32u * q + 32u, sb);
-                            weigh(sa, q);
-                            load32_wait(sb);
-                            if (q < 2) tmem_ld32(ts + 64u, sa);
-                            weigh(sb, q + 1);
+                            tmem_store_wait();
+                            l_run *= f;
+                            if (grow) m_ref = top;
                         }
-                        const float to = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * p.scale_log2 - Ops::kBias;
-                        const bool grow = !opens && row < nq && to > m_ref + kTreeSlack;
-                        if (turn || !__any_sync(0xffffffffu, grow)) break;
-                        // rare: move the reference, bring the row's outputs and sum to it, and form the weights again
-                        const float f = grow ? tree_ex2(m_ref - to) : 1.0f;
-#pragma unroll 1
-                        for (int c0 = 0; c0 < DH; c0 += 32) {
-                            uint32_t o[32];
-                            const uint32_t at = tmem_o + 128u * g + t_lane + (uint32_t)c0;
-                            tmem_ld32(at, o);
-                            load32_wait(o);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                            tmem_store32(at, o);
-                        }
-                        tmem_store_wait();
-                        l_run *= f;
-                        if (grow) m_ref = to;
                     }
+                    const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), minus = make_float2(-m_ref, -m_ref);
+                    float2 sum2[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+                    auto weigh = [&](const uint32_t (&s)[32], int q) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            float2 y = tree_fma2(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), scale2, minus);
+                            y.x = tree_ex2(y.x);
+                            y.y = tree_ex2(y.y);
+                            sum2[e & 1] = tree_add2(sum2[e & 1], y);
+                            w[e] = Ops::pack(y.x, y.y);
+                        }
+                        store16(ts + 16u * q, w);                // over scores that have been read
+                    };
+#pragma unroll 1
+                    for (int q = 0; q < 4; q += 2) {
+                        load32_wait(sa);
+                        tmem_ld32(ts + 32u * q + 32u, sb);
+                        weigh(sa, q);
+                        load32_wait(sb);
+                        if (q < 2) tmem_ld32(ts + 64u, sa);
+                        weigh(sb, q + 1);
+                    }
+                    tmem_store_wait();
                     l_run += (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
                 }
-                fence_async_smem();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) { mbar_arrive(s_empty(g)); mbar_arrive(p_full(g)); }
+                if (lane == 0) mbar_arrive(p_full(g));
                 if (piece_ends) {
-                    const bool whole = item_ends && !split_front;
-                    if (!wait_all(o_full(g), (done - 1) & 1u)) { ok = false; break; }
+                    if (!wait_all(o_full(g), uses & 1u)) { ok = false; break; }
+                    ++uses;
                     tc_fence_after();
-                    const bool repair = odd_piece[piece & 1u] == piece + 1;
+                    const bool whole = item_ends && !split_front;
+                    const bool repair = odd_piece[piece & 3u] == piece + 1;
                     const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
                     const int head = c.h * p.w.group + hg, trow = g * kRows + row;
                     T* dst = static_cast<T*>(p.out) + (int64_t)(c.r.row0 + tok) * p.out_stride + (int64_t)head * DH;
@@ -340,7 +325,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                         for (int c0 = 0; c0 < DH; c0 += 32) {
                             uint32_t oa[32];
                             float o[32];
-                            tmem_ld32(tmem_o + 128u * g + t_lane + (uint32_t)c0, oa);
+                            tmem_ld32(to + (uint32_t)c0, oa);
                             load32_wait(oa);
 #pragma unroll
                             for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(oa[e]);

@@ -63,6 +63,12 @@ __device__ __forceinline__ void load16(uint32_t taddr, uint32_t (&v)[16]) {
         : "r"(taddr) : "memory");
 }
 // The loads issued so far have arrived; v's values are not to be used above this point.
+__device__ __forceinline__ void load16_wait(uint32_t (&v)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+                 :: "memory");
+}
 __device__ __forceinline__ void load32_wait(uint32_t (&v)[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
@@ -118,10 +124,11 @@ __device__ __forceinline__ uint32_t visible_word(int k0, int C, int n, int i, co
 // TMA box fetches all of a page's keys of a head.
 template <int DH> __host__ __device__ constexpr int tree_group_bytes() { return DH / 64 * 1024; }
 
-// K and V tiles, by a whole warp, in the order in which the products consume them: K(0), K(1), V(0), K(2), V(1), ...
+// K and V tiles, by a whole warp, in the order in which the products consume them: K(0), V(0), K(1), V(1), ..., or with K LEAD = 1
+// tile ahead: K(0), K(1), V(0), K(2), V(1), ...
 // Every lane fetches one page (or 128 keys of a larger one), and
 // reads its entry of the block table two tiles ahead.
-template <int DH, int NS>
+template <int DH, int NS, int LEAD>
 __device__ __forceinline__ void tree_load_keys(const TcParams& p, const CUtensorMap* map_k, const CUtensorMap* map_v, const TreeRun* run,
                                                uint32_t ring, uint32_t full, uint32_t empty) {
     constexpr int kTileBytes = kKeys * DH * 2, kGroup = tree_group_bytes<DH>();
@@ -159,10 +166,11 @@ __device__ __forceinline__ void tree_load_keys(const TcParams& p, const CUtensor
     Box last{}, cur{}, next{}, after{};                          // last: the tile whose V is still to come
     look_up(cur);
     if (n_tiles > 1) { c.next(p.w); look_up(next); }
-    for (int t = 0; t <= n_tiles && ok; ++t) {
+    for (int t = 0; t < n_tiles + LEAD && ok; ++t) {
         if (t < n_tiles && !fetch(map_k, cur)) { ok = false; break; }
         if (t + 2 < n_tiles) { c.next(p.w); look_up(after); }
-        if (t > 0 && !fetch(map_v, last)) { ok = false; break; }
+        if (LEAD == 0) last = cur;
+        if (t >= LEAD && !fetch(map_v, last)) { ok = false; break; }
         last = cur;
         cur = next;
         next = after;
