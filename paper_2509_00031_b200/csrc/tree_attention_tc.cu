@@ -443,8 +443,8 @@ int launch_tree_attention_tc(const TreeAttnArgs& a, cudaStream_t s, bool depende
     // Queries per tile, from the average number of drafts (the host does not know the lengths).  Up to 64 queries the keys are
     // the rows of the products, which costs exponentials only for queries that exist; a tile that is too small reads the keys
     // again for the next one, a tile that is too large costs products and exponentials of empty columns.  16 requests of 4096
-    // keys, 8 key heads of 128, tiles of 16 / 32 / 64 / 256, us: 4 queries 68 / 69 / 69 / 81; 16: 71 / 73 / 73 / 83; 32: 110 / 79 /
-    // 79 / 89; 48: 149 / 113 / 89 / 95; 64: 185 / 116 / 95 / 101; 96: 239 / 155 / 126 / 114.  Too small costs far more than too
+    // keys, 8 key heads of 128, tiles of 16 / 32 / 64 / 256, us: 4 queries 67 / 68 / 71 / 83; 16: 71 / 71 / 73 / 87; 32: 109 / 79 /
+    // 81 / 91; 48: 149 / 112 / 89 / 99; 64: 185 / 116 / 97 / 106; 96: 237 / 155 / 126 / 118.  Too small costs far more than too
     // large, hence the margin of a half for batches whose trees differ.
     const long long drafts = (long long)a.rows * group;
     const long long want = a.rows <= a.batch ? group : (3 * drafts + 2 * a.batch - 1) / (2 * a.batch);     // 1.5 x the average
