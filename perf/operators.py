@@ -180,7 +180,7 @@ def _prepare_plan(c, host, gen):
     free = order[sum(held):]
     i32 = lambda *shape: torch.empty(shape, dtype=torch.int32, device="cuda")  # noqa: E731
     out = dict(kv_len=i32(batch), row_start=i32(batch + 1), row_request=i32(rows), row_pos=i32(rows), slot=i32(rows), n_free=i32(1),
-               status=torch.zeros(1, dtype=torch.int32, device="cuda"))
+               status=i32(1))
     parents = None
     if c["words"]:
         out["tree_mask"] = i32(rows, c["words"])
