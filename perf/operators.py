@@ -267,8 +267,11 @@ def run(state):
 
 def _own_plan(s):
     from paper_2509_00031_b200 import binding as zq
+    if "status" not in s:                                     # the call or-s into this word: a program zeroes it once
+        s["status"] = torch.zeros(1, dtype=torch.int32, device="cuda")
     out = zq.zoqat_op_cache_plan(s["cached"], s["new"], s["case"]["page"], s["n_pages"], s["free"], s["n_free"], s["table"], s["rows"],
-                                 parents=s["parents"], mask_words=s["case"]["words"], out=s["out"])
+                                 parents=s["parents"], mask_words=s["case"]["words"],
+                                 out=dict(s["out"], status=s["status"]))
     return dict(out, table=s["table"])
 
 
