@@ -214,6 +214,14 @@ cache_append_kernel(const float* __restrict__ qkv, int64_t ld, const int32_t* __
         if (item == 0) atomicExch(err_flag, kErrBadSlot);
         return;
     }
+    int pos = 0;
+    if (cos_t) {                                                    // a row without a rotation is skipped whole, its v as well
+        pos = __ldg(row_pos + row);
+        if (pos < 0 || pos >= rope_len) {
+            if (item == 0) atomicExch(err_flag, kErrBadSlot);
+            return;
+        }
+    }
     const float* src = qkv + row * ld + (int64_t)head * cache.d_head + 8 * ch;
     float a[8], b[8];
 #pragma unroll
@@ -222,11 +230,6 @@ cache_append_kernel(const float* __restrict__ qkv, int64_t ld, const int32_t* __
         *reinterpret_cast<float4*>(b + 4 * i) = __ldg(reinterpret_cast<const float4*>(src + half) + i);
     }
     if (cos_t && head < n_heads + n_kv) {
-        const int pos = __ldg(row_pos + row);
-        if (pos < 0 || pos >= rope_len) {
-            if (item == 0) atomicExch(err_flag, kErrBadSlot);
-            return;
-        }
         const float* cp = cos_t + (int64_t)pos * half + 8 * ch;
         const float* sp = sin_t + (int64_t)pos * half + 8 * ch;
         float c[8], s[8];

@@ -205,6 +205,22 @@ def test_append_skips_and_reports_slots_and_positions_outside(zq):
             assert bool((k.view(32, 64)[1:] == 3.0).all())              # (v needs no position)
 
 
+@pytest.mark.parametrize("dtype,heads,kv,dh,layout", [("f32", 1, 1, 64, "token"), ("bf16", 40, 8, 128, "head"), ("f16", 4, 2, 64, "joint")])
+def test_append_skips_rows_with_a_bad_position_whole(zq, dtype, heads, kv, dh, layout):
+    # the slot of such a row keeps its old key and its old value; the rows around it are written
+    k, v = make_cache(3, 16, kv, dh, dtype, layout, fill=3.0)
+    qkv = torch.ones((6, (heads + 2 * kv) * dh), device="cuda")
+    cos, sin = torch.ones((8, dh // 2), device="cuda"), torch.zeros((8, dh // 2), device="cuda")
+    q = torch.full((6, heads, dh), 7.0, dtype=TYPES[dtype], device="cuda")
+    _, err = zq.zoqat_op_cache_append(qkv, ints([7, 8, -1, 0, 2 ** 31 - 1, -2 ** 31]), ints([40, 1, 2, 17, 4, 5]), k, v, heads, cos=cos, sin=sin, q_out=q)
+    assert err.item() == 40
+    assert bool((q[[0, 3]] == 1.0).all()) and bool((q[[1, 2, 4, 5]] == 7.0).all())
+    for c in (k, v):
+        want = torch.full((48, kv, dh), 3.0, dtype=TYPES[dtype], device="cuda")
+        want[[40, 17]] = 1.0
+        assert torch.equal(c.reshape(48, kv, dh), want)
+
+
 # ---- attention --------------------------------------------------------------------------------------------------------
 def attention_problem(seed, dtype, heads, kv, dh, page, layout, cached, new, mask="tree", pad=2, gap=0, q_scale=1.0):
     """Everything that no row may see is NaN: unused pages, the slots behind each request's end."""
