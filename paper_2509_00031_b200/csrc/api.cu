@@ -1892,7 +1892,7 @@ int zoqat_op_cache_append(const float* qkv_dev, int64_t ld, const int32_t* row_p
     if (misaligned(qkv_dev, 16) || misaligned(q_out_dev, 16) || misaligned(cos_dev, 16) || misaligned(sin_dev, 16))
         return fail(ZOQAT_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
     if (rows == 0) return ZOQAT_OK;
-    launch_cache_append(qkv_dev, ld, row_pos_dev, slot_dev, rows, n_heads, cos_dev, sin_dev, rope_len, c, q_out_dev, q_stride, err_flag_dev,
+    launch_cache_append(qkv_dev, ld, row_pos_dev, slot_dev, rows, n_heads, cos_dev, sin_dev, cos_dev ? rope_len : 0, c, q_out_dev, q_stride, err_flag_dev,
                         static_cast<cudaStream_t>(stream));
     CUDA_TRY(cudaGetLastError());
     return ZOQAT_OK;

@@ -43,7 +43,7 @@ struct CachePlanArgs {
 int launch_cache_plan(const CachePlanArgs& a, cudaStream_t s);       // 0, or -1: set-up failed
 
 void launch_cache_append(const float* qkv, int64_t ld, const int32_t* row_pos, const int32_t* slot, int rows, int n_heads,
-                         const float* cos_t, const float* sin_t, int rope_len, const PagedCache& cache, void* q_out, int64_t q_stride,
+                         const float* cos_t, const float* sin_t, int max_pos, const PagedCache& cache, void* q_out, int64_t q_stride,
                          int32_t* err_flag, cudaStream_t s, bool dependent = false);
 void launch_embed_rows(const int32_t* tokens, const int32_t* row_pos, const float* embed, const float* pos_embed, int rows, int d, int vocab,
                        int max_pos, float* h, int32_t* err_flag, cudaStream_t s);

@@ -196,11 +196,12 @@ template <> struct Pack8<__half> {
 };
 
 // One thread per 8 + 8 elements (i .. i+7 and their partners d_head / 2 further) of a head of a row: q heads, then k heads,
-// then v heads, as they stand in the row.
+// then v heads, as they stand in the row.  max_pos > 0: positions lie in [0, max_pos), with or without tables (a model may add
+// its position embeddings before).
 template <typename T>
 __global__ void __launch_bounds__(256)
 cache_append_kernel(const float* __restrict__ qkv, int64_t ld, const int32_t* __restrict__ row_pos, const int32_t* __restrict__ slot,
-                    int n_heads, const float* __restrict__ cos_t, const float* __restrict__ sin_t, int rope_len, PagedCache cache,
+                    int n_heads, const float* __restrict__ cos_t, const float* __restrict__ sin_t, int max_pos, PagedCache cache,
                     T* __restrict__ q_out, int64_t q_stride, int32_t* __restrict__ err_flag) {
     const int half = cache.d_head >> 1, chunks = half >> 3;         // 4 (d_head 64) or 8 (d_head 128) chunks a head
     const int item = blockIdx.y * 256 + threadIdx.x;
@@ -215,9 +216,9 @@ cache_append_kernel(const float* __restrict__ qkv, int64_t ld, const int32_t* __
         return;
     }
     int pos = 0;
-    if (cos_t) {                                                    // a row without a rotation is skipped whole, its v as well
+    if (max_pos > 0) {                                              // such a row is skipped whole, its v as well
         pos = __ldg(row_pos + row);
-        if (pos < 0 || pos >= rope_len) {
+        if (pos < 0 || pos >= max_pos) {
             if (item == 0) atomicExch(err_flag, kErrBadSlot);
             return;
         }
@@ -313,12 +314,12 @@ int launch_cache_plan(const CachePlanArgs& a, cudaStream_t s) {
 }
 
 void launch_cache_append(const float* qkv, int64_t ld, const int32_t* row_pos, const int32_t* slot, int rows, int n_heads,
-                         const float* cos_t, const float* sin_t, int rope_len, const PagedCache& cache, void* q_out, int64_t q_stride,
+                         const float* cos_t, const float* sin_t, int max_pos, const PagedCache& cache, void* q_out, int64_t q_stride,
                          int32_t* err_flag, cudaStream_t s, bool dependent) {
     const int items = (n_heads + 2 * cache.n_kv_heads) * (cache.d_head / 16);
     const dim3 grid(rows, (items + 255) / 256);
 #define ZQ_APPEND(T) launch_kernel(cache_append_kernel<T>, grid, dim3(256), 0, s, dependent, qkv, ld, row_pos, slot, n_heads, cos_t, \
-                                   sin_t, rope_len, cache, static_cast<T*>(q_out), q_stride, err_flag)
+                                   sin_t, max_pos, cache, static_cast<T*>(q_out), q_stride, err_flag)
     if (cache.type == kTypeF32) ZQ_APPEND(float);
     else if (cache.type == kTypeBf16) ZQ_APPEND(__nv_bfloat16);
     else ZQ_APPEND(__half);

@@ -803,3 +803,26 @@ def test_tree_step_refuses_and_reports(zq):
         model.zoqat_check()
     assert e.value.status == zq.ERR_INVALID_ARG
     model.zoqat_check()
+
+
+@pytest.mark.parametrize("name", ["opt_w3a8", "llama_w4a8"])
+def test_tree_step_leaves_the_pages_of_rows_with_a_bad_position(zq, name):
+    # models with position embeddings and models with rotary tables alike: no key and no value of such a row is stored
+    shape, model = packed_model(zq, name, 2, 64)
+    sv = Serving(zq, shape, model, 1, 16, "f32", max_rows=2)
+    _, _, plan = sv.step([[3, 4]])
+    model.zoqat_check()
+    for pos, kept in (([0, 64], 0), ([64, 1], 1), ([0, -1], 0)):
+        for k, v in sv.caches:
+            k.fill_(5.0); v.fill_(5.0)
+        model.zoqat_decode_tree_step(ints([3, 4]), dict(plan, row_pos=ints(pos)), sv.table, sv.caches)
+        with pytest.raises(zq.ZoqatError) as e:
+            model.zoqat_check()
+        assert e.value.status == zq.ERR_INVALID_ARG
+        model.zoqat_check()
+        page, off = [x // 16 for x in plan["slot"].tolist()], [x % 16 for x in plan["slot"].tolist()]
+        for k, v in sv.caches:
+            for c in (k, v):
+                assert bool((c[page[kept], off[kept]] != 5.0).any())
+                c[page[kept], off[kept]] = 5.0
+                assert bool((c == 5.0).all()), (pos, "a row that was to be skipped")
