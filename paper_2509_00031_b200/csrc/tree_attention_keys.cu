@@ -262,7 +262,8 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
             const uint32_t s_at = tmem_s + (uint32_t)(buf * N) + t_lane;
             await(s_full(buf), (t >> 1) & 1u);
             uint64_t vis = ~0ull;                                // queries that see this key
-            if ((c.kt + 1) * kKeys > C) {                        // drafts in the tile, or its end
+            const bool tail = (c.kt + 1) * kKeys > C;            // drafts in the tile, or its end
+            if (tail) {
                 const int key = c.kt * kKeys + me, j = key - C;
                 if (key >= C) {
                     vis = 0;
@@ -284,9 +285,14 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                         }
                     }
                 }
+            }
+            // Where the tile ends its piece, or holds drafts, the products of two tiles ago have run.  They belong to piece P - 2 or
+            // a later one, whose first product waited for the outputs of piece P - 4: what is kept by piece modulo 4 (references, sums,
+            // marks, the phase of piece_done) may be written.  A piece ends with its item, in a tile with drafts, or with the run.
+            if (t >= 2 && (tail || t == n_tiles - 1)) await(o_full(pb == 2 ? 0 : pb + 1), (pb == 2 ? round : round - 1u) & 1u);
+            if (tail) {
+                // (the V tile's slot was last used at least two tiles ago: only this tile's phase is open)
                 const uint32_t vseq = t == n_tiles - 1 ? 2u * n_tiles - 1u : 2u * t + 2u;
-                // the V tile's slot was last used at least two tiles ago: behind that product, only this tile's phase is open
-                if (t >= 2) await(o_full(pb == 2 ? 0 : pb + 1), (pb == 2 ? round : round - 1u) & 1u);
                 await(ring_full(vseq % NS), (vseq / NS) & 1u);
                 if (tree_clean_values<DH, Ops::kExpMask>(sp + (vseq % NS) * Cfg::kTileBytes, max(C - c.kt * kKeys, 0), c.r.L - c.kt * kKeys, me))
                     odd_piece[piece & 3u] = piece + 1;

@@ -474,6 +474,53 @@ def test_wide_trees_with_steep_scores(zq, dtype):
     assert bool((off <= bound).all()), (float(off.max()), float((off / bound.clamp(min=1e-30)).max()))
 
 
+def run_pieces(items, ctas, cost=4):
+    """The runs of key tiles that the tensor-core kernels deal out: items of so many tiles, each with a constant for opening and closing it,
+    laid out one after the other and cut into equal runs -> per CTA its pieces [item, first tile, tiles]."""
+    total = sum(items) + cost * len(items)
+    ctas = min(ctas, total)
+    q, r = divmod(total, ctas)
+    out, unit, c = [[] for _ in range(ctas)], 0, 0
+    for i, n in enumerate(items):
+        for kt in range(n):
+            while unit + cost + kt >= q * (c + 1) + min(c + 1, r):
+                c += 1
+            if out[c] and out[c][-1][0] == i:
+                out[c][-1][2] += 1
+            else:
+                out[c].append([i, kt, 1])
+        unit += cost + n
+    return out
+
+
+@pytest.mark.parametrize("dtype,group,n,seed,batch,share", [("bf16", 4, 1, 133, 813, 0.305), ("f16", 4, 4, 241, 769, 0.242), ("bf16", 8, 8, 125, 770, 0.297),
+                                                           ("f16", 4, 2, 212, 503, 0.218)])
+def test_short_items_before_the_first_tile_of_a_long_one(zq, dtype, group, n, seed, batch, share):
+    # runs that end in the first tile of a longer item, without drafts in it, behind three items of one tile: the last piece then follows
+    # the ones before it at the shortest distance there is.  Drafts hold infinities, whose repair keeps the output warps longest.
+    rng = np.random.default_rng(seed)
+    rng.integers(500, 1100), rng.uniform(0.1, 0.5)
+    cached = [int(rng.integers(0, 100)) if rng.random() > share else int(rng.integers(129, 500)) for _ in range(batch)]
+    items, free = [-(-(c + n) // 128) for c in cached], [c // 128 for c in cached]
+    runs = run_pieces(items, torch.cuda.get_device_properties(0).multi_processor_count)
+    assert sum(len(r) >= 4 and r[-1][1:] == [0, 1] and items[r[-1][0]] > 1 and free[r[-1][0]] > 0 and all(x[2] == 1 for x in r[-4:-1]) for r in runs) > 2
+    pr = attention_problem(seed, dtype, group, 1, 128, 16, "token", cached, [n] * batch, "tree")
+    hit = torch.zeros((pr["rows"], 1, 128), dtype=torch.bool, device="cuda")
+    for b, c in enumerate(cached):
+        at = c + n - 1
+        pr["v"][pr["table"][b, at // 16].item(), at % 16, :, b % 128] = float("inf")
+        pr["vals"][b][n - 1 + c, :, b % 128] = float("inf")
+        for i in range(n):
+            hit[pr["start"][b] + i, 0, b % 128] = n - 1 in pr["seen"][b][i]
+    want, bound = attention_oracle(pr)
+    first = run_attention(zq, pr)
+    got = first[:pr["rows"]].double()
+    hit = hit.expand_as(got)
+    assert bool((got[hit] == float("inf")).all()) and bool(((got - want).abs() <= bound)[~hit].all())
+    for _ in range(20):
+        assert torch.equal(run_attention(zq, pr)[:pr["rows"]], first[:pr["rows"]])
+
+
 def test_no_rows(zq):
     k, v = [torch.randn((4, 16, 2, 64), device="cuda").to(torch.bfloat16) for _ in range(2)]
     keep = k.clone()
