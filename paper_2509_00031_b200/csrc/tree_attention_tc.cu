@@ -78,7 +78,8 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     auto o_full = [&](int g) { return bars + 8u * (2 * NS + 6 + g); };
     auto o_empty = [&](int g) { return bars + 8u * (2 * NS + 8 + g); };
     volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc);
-    // [4], by piece: piece + 1 with a non-finite draft value (the groups are within two tiles of one another)
+    // [4], by piece: piece + 1 with a non-finite draft value.  No product of piece P before both groups have read the outputs of
+    // piece P - 2, and scores of piece P follow the first product of piece P - 1: whoever marks piece P, piece P - 4 has been read.
     volatile uint32_t* odd_piece = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 8);
     long long* part = reinterpret_cast<long long*>(sp + Cfg::kOffMisc + 32);
     TreeRun* run = reinterpret_cast<TreeRun*>(sp + Cfg::kOffMisc + 32 + 192);
@@ -156,7 +157,10 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
                     if (g < groups) {
-                        // a new piece's first product overwrites outputs that have been read
+                        // A new piece's first product overwrites outputs that have been read.  Where the second group sits the piece
+                        // out, its last outputs are waited for as well: through pieces of up to 128 queries the first would otherwise
+                        // run ahead of it and reuse its marks.
+                        if (first && groups == 1 && uses[1] > 0 && !mbar_poll(o_empty(1), (uses[1] - 1) & 1u)) { ok = false; break; }
                         if ((first && uses[g] > 0 && !mbar_poll(o_empty(g), (uses[g] - 1) & 1u)) || !mbar_poll(p_full(g), done[g] & 1u)) { ok = false; break; }
                         ++done[g];
                         tc_fence_after();

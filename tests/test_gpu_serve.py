@@ -521,6 +521,31 @@ def test_short_items_before_the_first_tile_of_a_long_one(zq, dtype, group, n, se
         assert torch.equal(run_attention(zq, pr)[:pr["rows"]], first[:pr["rows"]])
 
 
+@pytest.mark.parametrize("dtype,dh,seed", [("bf16", 128, 1), ("f16", 64, 2)])
+def test_full_and_half_filled_tiles_of_a_wide_tree_by_turns(zq, dtype, dh, seed):
+    # items whose tiles of 256 queries are full, then several with up to 128: the second group of softmax warps sits pieces out.
+    # Infinities stand in drafts of all of them, so that both groups repair outputs in every piece.
+    new = [64, 5, 9, 1, 7, 64, 30, 3, 3, 3, 3, 40, 33, 2, 31, 64] * 6
+    rng = np.random.default_rng(seed)
+    cached = [int(x) for x in rng.integers(0, 300, len(new))]
+    heads, kv = 12, 3
+    assert 3 * sum(new) * heads // kv > 2 * 64 * len(new)                # more than 64 wanted: the wide kernel
+    pr = attention_problem(seed, dtype, heads, kv, dh, 16, "token", cached, new, "tree")
+    hit = torch.zeros((pr["rows"], heads, dh), dtype=torch.bool, device="cuda")
+    for b, (c, n) in enumerate(zip(cached, new)):
+        at, e = c + n // 2, b % dh
+        pr["v"][pr["table"][b, at // 16].item(), at % 16, :, e] = -float("inf")
+        pr["vals"][b][at, :, e] = -float("inf")
+        for i in range(n):
+            hit[pr["start"][b] + i, :, e] = n // 2 in pr["seen"][b][i]
+    want, bound = attention_oracle(pr)
+    first = run_attention(zq, pr)
+    got = first[:pr["rows"]].double()
+    assert bool((got[hit] == -float("inf")).all()) and bool(((got - want).abs() <= bound)[~hit].all())
+    for _ in range(20):
+        assert torch.equal(run_attention(zq, pr)[:pr["rows"]], first[:pr["rows"]])
+
+
 def test_no_rows(zq):
     k, v = [torch.randn((4, 16, 2, 64), device="cuda").to(torch.bfloat16) for _ in range(2)]
     keep = k.clone()
