@@ -27,6 +27,7 @@
 //               Maxima over the keys are formed only when a piece begins or a reference moves.
 //   warps 8-11  outputs of a finished piece, from the other one of two TMEM accumulators, while the next piece runs
 // Rounding, masked values and bounded waits as in tree_attention_tc.cu, but for the sums, which are those of the rounded weights.
+// Accesses to tensor memory are by whole warps: where lanes may have gone apart before (masks, tails, repairs) they meet first.
 #include "tree_attention_tc.cuh"
 #include "../../include/zoqat.h"
 
@@ -139,6 +140,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
     if (tid < 4) odd_piece[tid] = 0;
     if (tid == 64) { prefetch_tmap(&map_k); prefetch_tmap(&map_v); }
     if (warp == 1) {
+        __syncwarp();
         tmem_alloc(base + Cfg::kOffMisc, 512);
         tmem_relinquish();
     }
@@ -151,6 +153,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
     const uint32_t tmem = *tmem_slot;          // (allocated before the barriers in tree_find_run)
     if (!Cfg::kAdd && warp >= 4 && warp < 8) { // the matrix of ones: 16 keys' worth, the same for every step
         tc_fence_after();
+        __syncwarp();
         store8(tmem + 6u * N + ((uint32_t)((warp & 3) * 32) << 16), Ops::pack(1.0f, 1.0f));
         tmem_store_wait();
     }
@@ -314,6 +317,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
 #pragma unroll 1
                 for (int n0 = 0; n0 < nq; n0 += 16 * CH) {       // (once where the threads add up)
                     uint32_t s[CH][16];
+                    __syncwarp();
 #pragma unroll
                     for (int k = 0; k < CH; ++k) load16(s_at + (uint32_t)(n0 + 16 * k), s[k]);
                     float4 r[4 * CH];
@@ -362,6 +366,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                 for (int k = 0; 16 * k < nq; ++k) {
                     const uint32_t seen = (uint32_t)(vis >> (16 * k));
                     uint32_t s[16];
+                    __syncwarp();
                     load16(s_at + 16u * k, s);
                     tmem_ld_wait();
                     float v[16];
@@ -387,6 +392,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                     for (int n0 = 0; n0 < nq; n0 += 16) {
                         uint32_t o[16], l[16];
                         const uint32_t at = (uint32_t)((piece & 1u) * N + n0) + t_lane;
+                        __syncwarp();
                         load16(tmem_o + at, o);
                         if (!Cfg::kAdd) load16(tmem_l + at, l);
                         tmem_ld_wait();
@@ -413,6 +419,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                 for (int k = 0; 16 * k < nq; ++k) {
                     const uint32_t seen = (uint32_t)(vis >> (16 * k));
                     uint32_t s[16], w[8];
+                    __syncwarp();
                     load16(s_at + 16u * k, s);
                     tmem_ld_wait();
 #pragma unroll
@@ -486,6 +493,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                 for (int n0 = 0; n0 < nq; n0 += 16) {
                     uint32_t o[16], l[16];
                     const uint32_t at = (uint32_t)((piece & 1u) * N + n0) + t_lane;
+                    __syncwarp();
                     load16(tmem_o + at, o);
                     if (Cfg::kAdd) {
                         const float4* of = reinterpret_cast<const float4*>(sp + Cfg::kOffSum) + (piece & 3u) * N + n0;

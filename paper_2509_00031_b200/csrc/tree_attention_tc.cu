@@ -92,6 +92,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     if (tid < 4) odd_piece[tid] = 0;
     if (tid == 32) { prefetch_tmap(&map_k); prefetch_tmap(&map_v); }
     if (warp == 1) {
+        __syncwarp();
         tmem_alloc(base + Cfg::kOffMisc, 512);
         tmem_relinquish();
     }
@@ -238,6 +239,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                         for (int q = 0; q < 4; ++q) {
                             const uint32_t vis = row < nq ? visible_word(c.kt * kKeys + 32 * q, C, c.r.n, tok, mask, p.mask_words) : 0u;
                             uint32_t s[32];
+                            __syncwarp();                        // tensor memory is accessed by whole warps
                             tmem_ld32(ts + 32u * q, s);
                             load32_wait(s);
 #pragma unroll
@@ -253,6 +255,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) t4[(e >> 1) & 3] = fmaxf(t4[(e >> 1) & 3], fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
                     };
+                    __syncwarp();
                     tmem_ld32(ts, sa);
 #pragma unroll
                     for (int q = 0; q < 4; q += 2) {
@@ -329,12 +332,12 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                         for (int c0 = 0; c0 < DH; c0 += 32) {
                             uint32_t oa[32];
                             float o[32];
+                            __syncwarp();                        // lanes part below: rows without a query, repairs
                             tmem_ld32(to + (uint32_t)c0, oa);
                             load32_wait(oa);
 #pragma unroll
                             for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(oa[e]);
-                            if (row >= nq) continue;
-                            if (repair) {                        // non-finite values of drafts this row sees, within the piece's tiles
+                            if (repair && row < nq) {            // non-finite values of drafts this row sees, within the piece's tiles
                                 for (int j = 0; j < c.r.n; ++j) {
                                     const int key = C + j, kt = key / kKeys;
                                     if (kt < kt_first || kt > c.kt || !(visible_word(key, C, c.r.n, tok, mask, p.mask_words) & 1u)) continue;
@@ -347,7 +350,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                                     }
                                 }
                             }
-                            if (whole) {
+                            if (whole && row < nq) {
 #pragma unroll
                                 for (int e = 0; e < 32; e += 8) {
                                     uint4 w;
@@ -355,7 +358,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                                     w.z = Ops::pack(o[e + 4] * inv, o[e + 5] * inv); w.w = Ops::pack(o[e + 6] * inv, o[e + 7] * inv);
                                     *reinterpret_cast<uint4*>(dst + c0 + e) = w;
                                 }
-                            } else {
+                            } else if (row < nq) {
                                 float* po = slot + 2 * kTileRows + (size_t)trow * DH + c0;
 #pragma unroll
                                 for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(po + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);

@@ -546,6 +546,27 @@ def test_full_and_half_filled_tiles_of_a_wide_tree_by_turns(zq, dtype, dh, seed)
         assert torch.equal(run_attention(zq, pr)[:pr["rows"]], first[:pr["rows"]])
 
 
+@pytest.mark.parametrize("dtype,heads,kv,dh,new", [("bf16", 4, 4, 128, [9, 3, 7]), ("f16", 2, 1, 64, [13, 9, 5]), ("bf16", 6, 2, 64, [21, 10, 3]),
+                                                   ("f16", 8, 2, 128, [30, 5, 41]), ("bf16", 14, 2, 128, [50, 33, 18])])
+def test_lanes_that_see_different_drafts(zq, dtype, heads, kv, dh, new):
+    # every row has a random mask of its own, a third of the rows sees no draft, tiles are partly filled, and two drafts of every request
+    # hold infinities: the lanes of a warp go different ways in the masks, in the tail of V and in the repair of the outputs
+    pr = attention_problem(17, dtype, heads, kv, dh, 8, "joint", [125, 0, 510], new, "random")
+    hit = torch.zeros((pr["rows"], heads, dh), dtype=torch.bool, device="cuda")
+    for b, (c, n) in enumerate(zip([125, 0, 510], new)):
+        for j, e in ((n - 1, 3), (n // 2, dh - 1)):
+            pr["v"][pr["table"][b, (c + j) // 8].item(), (c + j) % 8, :, e] = float("inf")
+            pr["vals"][b][c + j, :, e] = float("inf")
+            for i in range(n):
+                hit[pr["start"][b] + i, :, e] = j in pr["seen"][b][i]
+    want, bound = attention_oracle(pr)
+    first = run_attention(zq, pr)
+    got = first[:pr["rows"]].double()
+    assert bool((got[hit] == float("inf")).all()) and bool(((got - want).abs() <= bound)[~hit].all())
+    for _ in range(5):
+        assert torch.equal(run_attention(zq, pr)[:pr["rows"]], first[:pr["rows"]])
+
+
 def test_no_rows(zq):
     k, v = [torch.randn((4, 16, 2, 64), device="cuda").to(torch.bfloat16) for _ in range(2)]
     keep = k.clone()
