@@ -9,7 +9,7 @@
 //                         Bound by latency: a launch, two chained loads and two block scans; 12 us a call from Python for 8
 //                         to 1024 requests, the host's share included.
 //   cache_append_kernel   (a, b) -> (a cos - b sin, b cos + a sin) for q and k, then one rounding into the cache's type.
-//                         Bound by memory: 8191 rows of 40 + 2 * 8 heads of 128 into binary16, 356 MB in 65.6 us, 84 % of the
+//                         Bound by memory: 8191 rows of 40 + 2 * 8 heads of 128 into binary16, 356 MB in 63.5 us, 87 % of the
 //                         rate of a plain copy.
 //   embed_rows_kernel     the residual rows of drafted tokens (each row has a position of its own).
 //   widen_kernel          attention outputs of a 16-bit cache for the fp32 activation quantisers of a model's step.
@@ -209,19 +209,12 @@ cache_append_kernel(const float* __restrict__ qkv, int64_t ld, const int32_t* __
     const int n_kv = cache.n_kv_heads;
     grid_dependency_wait();                                         // (in a step of the model the projections come before)
     const int64_t row = blockIdx.x;
-    const int sl = __ldg(slot + row);
+    const int sl = __ldg(slot + row), pos = max_pos > 0 ? __ldg(row_pos + row) : 0;      // both on their way at once
     if (head >= n_heads + 2 * n_kv || sl < 0) return;
-    if (sl >= cache.n_pages * cache.page_size) {
+    // a row with a slot or position outside is skipped whole, its v as well
+    if (sl >= cache.n_pages * cache.page_size || pos < 0 || (max_pos > 0 && pos >= max_pos)) {
         if (item == 0) atomicExch(err_flag, kErrBadSlot);
         return;
-    }
-    int pos = 0;
-    if (max_pos > 0) {                                              // such a row is skipped whole, its v as well
-        pos = __ldg(row_pos + row);
-        if (pos < 0 || pos >= max_pos) {
-            if (item == 0) atomicExch(err_flag, kErrBadSlot);
-            return;
-        }
     }
     const float* src = qkv + row * ld + (int64_t)head * cache.d_head + 8 * ch;
     float a[8], b[8];
