@@ -24,7 +24,7 @@
 //   warps 1, 2  one thread issues the scores, one tile ahead, another the products with the weights
 //   warps 4-7   softmax.  All keys of a query share one reference; it moves only when a score passes it by more than 2^8, which
 //               the warps tell one another once per tile, after computing the weights as if it did not.
-//               Maxima over the keys are formed only when a piece begins or a reference moves.
+//               Maxima over the keys are formed only when a piece begins or a reference moves (or lies beyond 2^20).
 //   warps 8-11  outputs of a finished piece, from the other one of two TMEM accumulators, while the next piece runs
 // Rounding, masked values and bounded waits as in tree_attention_tc.cu, but for the sums, which are those of the rounded weights.
 // Accesses to tensor memory are by whole warps: where lanes may have gone apart before (masks, tails, repairs) they meet first.
@@ -35,14 +35,13 @@ namespace zq {
 namespace {
 
 constexpr int kKeyThreads = 384;
-constexpr float kNoRef = -1.0e30f;       // reference of a query that has seen nothing: any score passes it
 
 template <int DH, int N> struct KeyCfg {
     static constexpr int kTileBytes = kKeys * DH * 2;
     static constexpr int kQBytes = N * DH * 2, kPBytes = N * kKeys * 2;
     static constexpr bool kAdd = N == 16;                                   // the threads add up the weights
     static constexpr int kSumBytes = kAdd ? 4 * N * 16 : 0;                 // [4 pieces][N][4 warps] floats
-    static constexpr int kFixed = 2 * kQBytes + 3 * kPBytes + N * 16 + 6 * N * 4 + 2 * N * kMaskWords * 4 + kSumBytes + 1024;
+    static constexpr int kFixed = 2 * kQBytes + 3 * kPBytes + N * 16 + 8 * N * 4 + 2 * N * kMaskWords * 4 + kSumBytes + 1024;
     static constexpr int kFit = (232448 - kFixed) / kTileBytes;
     // an even number: K tiles (odd places of the sequence) and V tiles (even places) then have slots of their own, so that each
     // slot is consumed by one thread in order and no one can wait for a phase before the one ahead of it has completed
@@ -50,8 +49,8 @@ template <int DH, int N> struct KeyCfg {
     static constexpr int kOffQ = kStages * kTileBytes;
     static constexpr int kOffP = kOffQ + 2 * kQBytes;
     static constexpr int kOffRed = kOffP + 3 * kPBytes;                     // [N][4 warps] floats
-    static constexpr int kOffRef = kOffRed + N * 16;                        // [2][N] floats, then [4][N]: those of the last pieces
-    static constexpr int kOffMask = kOffRef + 6 * N * 4;                    // [2][N drafts][kMaskWords]
+    static constexpr int kOffRef = kOffRed + N * 16;                        // [2][N] floats, then [4][N]: those of the last pieces, then [2][N] stand-ins
+    static constexpr int kOffMask = kOffRef + 8 * N * 4;                    // [2][N drafts][kMaskWords]
     static constexpr int kOffSum = kOffMask + 2 * N * kMaskWords * 4;
     static constexpr int kOffBar = kOffSum + kSumBytes;
     // ring full, ring empty; q full, q empty, s full, s empty (2 each), p full, o full (3 each), o empty, out full (2), piece done (4)
@@ -311,7 +310,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
             if (!opens) {
                 // the weights as if no reference moved; whether one does, the warps then tell one another
                 constexpr int CH = N == 16 ? 1 : 2;              // chunks of 16 or 32
-                const float4* ref4 = reinterpret_cast<const float4*>(refs + cur * N);
+                const float4* ref4 = reinterpret_cast<const float4*>(refs + (6 + cur) * N);
                 float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 uint32_t w[2 * CH][4];
 #pragma unroll 1
@@ -381,7 +380,10 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                 if (me < N) {
                     const float4 r = *reinterpret_cast<const float4*>(red + me * 4);
                     const float top = fmaxf(fmaxf(r.x, r.y), fmaxf(r.z, r.w)) - Ops::kBias;
-                    new_ref[me] = me < nq ? fmaxf(top, opens ? kNoRef : old_ref[me]) : INFINITY;     // columns without a query: weight 0
+                    const float ref = me < nq ? fmaxf(top, opens ? kNoRef : old_ref[me]) : INFINITY; // columns without a query: weight 0
+                    new_ref[me] = ref;
+                    // a far reference needs rounded products (tree_shift): its stand-in has every tile with a key for the query come here
+                    refs[(6 + (cur ^ 1u)) * N + me] = me < nq && tree_far(ref) ? kNoRef : ref;
                 }
                 meet();
                 if (!opens) {
@@ -429,7 +431,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                         float v[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            v[e] = (seen >> (4 * e4 + e)) & 1u ? tree_ex2(fmaf(__uint_as_float(s[4 * e4 + e]), p.scale_log2, -ref[e])) : 0.0f;
+                            v[e] = tree_ex2((seen >> (4 * e4 + e)) & 1u ? tree_shift(__uint_as_float(s[4 * e4 + e]), p.scale_log2, ref[e]) : -INFINITY);
                         w[2 * e4] = Ops::pack(v[0], v[1]);
                         w[2 * e4 + 1] = Ops::pack(v[2], v[3]);
                     }

@@ -36,7 +36,8 @@ namespace zq {
 namespace {
 
 constexpr int kTcThreads = 384, kRows = 128, kTileRows = 2 * kRows;     // rows per group, rows per tile
-constexpr float kNoRef = -1.0e30f;       // reference of a row that has seen nothing: any score passes it
+
+template <bool V> struct FarScores { static constexpr bool value = V; };
 
 template <int DH> struct TcCfg {
     static constexpr int kTileBytes = kKeys * DH * 2;                       // one K or V tile
@@ -267,11 +268,12 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                         highest(sb);
                     }
                     // weights 2^(score - reference): the largest is 2^kBias .. 2^(kBias + 8)
-                    const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * p.scale_log2 - Ops::kBias;
+                    // (the scaled maximum is rounded by itself, as the scores are below: see tree_shift)
+                    const float high = __fmul_rn(fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])), p.scale_log2), top = high - Ops::kBias;
                     if (opens) {
                         m_ref = fmaxf(top, kNoRef);
                     } else {
-                        const bool grow = row < nq && top > m_ref + kTreeSlack;
+                        const bool grow = row < nq && high - m_ref > Ops::kBias + kTreeSlack;
                         if (__any_sync(0xffffffffu, grow)) {     // rare: move the reference, bring the row's outputs and sum to it
                             const float f = grow ? tree_ex2(m_ref - top) : 1.0f;
 #pragma unroll 1
@@ -290,11 +292,13 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                     }
                     const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), minus = make_float2(-m_ref, -m_ref);
                     float2 sum2[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-                    auto weigh = [&](const uint32_t (&s)[32], int q) {
+                    auto weigh = [&](const uint32_t (&s)[32], int q, auto far) {
                         uint32_t w[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            float2 y = tree_fma2(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), scale2, minus);
+                            float2 y = make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
+                            if constexpr (far.value) y = make_float2(tree_shift(y.x, p.scale_log2, m_ref), tree_shift(y.y, p.scale_log2, m_ref));
+                            else y = tree_fma2(y, scale2, minus);
                             y.x = tree_ex2(y.x);
                             y.y = tree_ex2(y.y);
                             sum2[e & 1] = tree_add2(sum2[e & 1], y);
@@ -302,15 +306,19 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                         }
                         store16(ts + 16u * q, w);                // over scores that have been read
                     };
+                    auto weigh_all = [&](auto far) {
 #pragma unroll 1
-                    for (int q = 0; q < 4; q += 2) {
-                        load32_wait(sa);
-                        tmem_ld32(ts + 32u * q + 32u, sb);
-                        weigh(sa, q);
-                        load32_wait(sb);
-                        if (q < 2) tmem_ld32(ts + 64u, sa);
-                        weigh(sb, q + 1);
-                    }
+                        for (int q = 0; q < 4; q += 2) {
+                            load32_wait(sa);
+                            tmem_ld32(ts + 32u * q + 32u, sb);
+                            weigh(sa, q, far);
+                            load32_wait(sb);
+                            if (q < 2) tmem_ld32(ts + 64u, sa);
+                            weigh(sb, q + 1, far);
+                        }
+                    };
+                    if (__any_sync(0xffffffffu, row < nq && tree_far(m_ref))) weigh_all(FarScores<true>{});
+                    else weigh_all(FarScores<false>{});
                     tmem_store_wait();
                     l_run += (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
                 }

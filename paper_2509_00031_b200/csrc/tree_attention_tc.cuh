@@ -9,6 +9,7 @@ namespace zq {
 constexpr int kKeys = 128;           // keys per tile
 constexpr int kMaskWords = 4;        // words of a draft's mask that travel with its query tile (trees of up to 128 drafts)
 constexpr float kTreeSlack = 8.0f;   // a reference may lag the maximum by up to 2^8
+constexpr float kNoRef = -3.0e38f;   // reference of a query that has seen nothing: any score passes it
 
 struct TcParams {
     TreeWork w;
@@ -98,6 +99,12 @@ __device__ __forceinline__ void store16(uint32_t taddr, const uint32_t (&v)[16])
         : "memory");
 }
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// A score in base 2 against its reference: fused where the reference is near, else in two roundings.  References are made from
+// rounded products, so equal ones then cancel exactly; fused, the product's rounding error stays in the exponent - at most 1/16 up
+// to 2^20, but 1 at 2^24 and 64 at 2^30, out of a weight's range.
+__device__ __forceinline__ float tree_shift(float s, float scale, float ref) { return __fsub_rn(__fmul_rn(s, scale), ref); }
+__device__ __forceinline__ bool tree_far(float ref) { return fabsf(ref) > 1048576.0f && ref != kNoRef; }
 
 // Bits of the 32 keys from k0 on that draft i sees.
 __device__ __forceinline__ uint32_t visible_word(int k0, int C, int n, int i, const uint32_t* mask, int words) {

@@ -567,6 +567,42 @@ def test_lanes_that_see_different_drafts(zq, dtype, heads, kv, dh, new):
         assert torch.equal(run_attention(zq, pr)[:pr["rows"]], first[:pr["rows"]])
 
 
+@pytest.mark.parametrize("dtype,qa,ka", [("f16", 30000.0, 512.0), ("f16", -30000.0, 512.0), ("bf16", 2.0 ** 60, 2.0 ** 50), ("bf16", 2.0 ** 62, -2.0 ** 55),
+                                         ("f32", 2.0 ** 60, -2.0 ** 50), ("f16", 2048.0, 512.0), ("bf16", 2.0 ** 12, 2.0 ** 15)])
+@pytest.mark.parametrize("heads,new,cached", [(1, [2, 1], [300, 900]), (4, [6, 5], [300, 900]), (8, [6, 5], [900, 20]), (8, [40, 30], [900, 129])])
+def test_scores_of_any_size(zq, dtype, qa, ka, heads, new, cached):
+    # one product a score, exact in binary32, up to 2^117: the softmax is an even one over the keys with the largest score, however large
+    pr = attention_problem(23, dtype, heads, 1, 128, 16, "token", cached, new, "tree")
+    rng = np.random.default_rng(4)
+    rows = pr["rows"]
+    pr["q"][:rows] = 0
+    pr["q"][:rows, :, 0] = qa
+    want = torch.zeros((rows, heads, 128), dtype=torch.float64, device="cuda")
+    size = want.clone()
+    for b, (c, n) in enumerate(zip(cached, new)):
+        step = torch.from_numpy(rng.integers(1, 90, c + n)).cuda()
+        pr["keys"][b].zero_()
+        pr["keys"][b][:, 0, 0] = (ka * step).to(TYPES[dtype])
+        t = torch.arange(c + n, device="cuda")
+        pr["k"][pr["table"][b].long()[t // 16], t % 16] = pr["keys"][b]
+        v = pr["vals"][b][:, 0].double()
+        s = pr["keys"][b][:, 0, 0].double() * qa
+        assert bool((s.float().double() == s).all())
+        for i in range(n):
+            vis = t < c
+            for j in pr["seen"][b][i]:
+                vis[c + j] = True
+            best = vis & (s == s[vis].max())
+            want[pr["start"][b] + i] = v[best].mean(0)
+            size[pr["start"][b] + i] = v[best].abs().mean(0)
+    got, err = zq.zoqat_op_tree_attention(pr["q"], pr["k"], pr["v"], pr["table"], pr["kv_len"], pr["row_start"], tree_mask=pr["mask"], scale=1.0)
+    assert err.item() == 0
+    # the weights of all keys with the largest score are the same number; 16-bit weights and the output are rounded, sums are binary32
+    half = torch.finfo(TYPES[dtype]).eps / 2
+    bound = half * want.abs() + (0 if dtype == "f32" else half) * size * (1 + half) + 64 * 2.0 ** -24 * size + (2.0 ** -25 if dtype == "f16" else 0)
+    assert bool(((got[:rows].double() - want).abs() <= bound).all())
+
+
 def test_no_rows(zq):
     k, v = [torch.randn((4, 16, 2, 64), device="cuda").to(torch.bfloat16) for _ in range(2)]
     keep = k.clone()
