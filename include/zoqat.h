@@ -692,7 +692,8 @@ int zoqat_op_cache_append(const float* qkv_dev, int64_t ld, const int32_t* row_p
  * Sums and the softmax are held in fp32; in bf16 / fp16 the softmax weights are rounded to the cache's type for the product with
  * V.  The keys are dealt out evenly over the SMs, long contexts in several pieces that are joined in a fixed order: the same
  * call gives the same bits.  bf16 and fp16 need page_size 8, 16, 32, 64 or a multiple of 128, and with several heads and pages a
- * page_stride that is a multiple of head_stride (ZOQAT_ERR_UNSUPPORTED otherwise).  scratch_dev:
+ * page_stride that is a multiple of head_stride, fewer than 2^31 strides of a head through all pages and a slot_stride under 2^36
+ * (ZOQAT_ERR_UNSUPPORTED otherwise).  scratch_dev:
  * zoqat_op_tree_attention_scratch_bytes() bytes, 256-byte aligned, for one call at a time (calls that may overlap, e.g. two graphs
  * in flight, each need their own).  rows = 0 is allowed (nothing is done).  *err_flag_dev is set to 41 (a request whose lengths or
  * rows contradict each other: it is left out), 42 (a page outside the pool: its keys and values count as zeros), 43 (a bounded

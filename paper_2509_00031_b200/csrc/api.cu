@@ -1829,6 +1829,10 @@ int attention_limits(const PagedCache& c, int max_pages, int64_t rows, int n_hea
         return fail(ZOQAT_ERR_UNSUPPORTED, "page_size %d (bf16 / fp16: 8, 16, 32, 64 or a multiple of 128)", c.page_size);
     if (c.n_kv_heads > 1 && c.n_pages > 1 && c.page_stride % c.head_stride)
         return fail(ZOQAT_ERR_UNSUPPORTED, "bf16 / fp16: page_stride must be a multiple of head_stride");
+    // the tensor maps count heads through all pages in 32 bits and step over 8 slots in 40
+    const int64_t unit = c.n_kv_heads > 1 ? c.head_stride : c.page_stride, per_page = c.n_pages > 1 ? c.page_stride / unit : 1;
+    if (per_page > INT32_MAX || (int64_t)(c.n_pages - 1) * per_page + c.n_kv_heads >= INT32_MAX || c.slot_stride >= ((int64_t)1 << 36))
+        return fail(ZOQAT_ERR_UNSUPPORTED, "bf16 / fp16: 2^31 or more heads through all pages, or slot_stride of 2^36 or more");
     return ZOQAT_OK;
 }
 

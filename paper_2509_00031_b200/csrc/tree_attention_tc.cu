@@ -475,10 +475,8 @@ int launch_tree_attention_tc(const TreeAttnArgs& a, cudaStream_t s, bool depende
     alignas(64) CUtensorMap map_k, map_v;
     // {64 columns, 8 keys, halves, groups of 8 keys, heads of all pages}
     const int64_t ss = a.cache.slot_stride, unit = a.cache.n_kv_heads > 1 ? a.cache.head_stride : a.cache.page_stride;
-    if (a.cache.n_pages > 1 && a.cache.page_stride % unit) return ZOQAT_ERR_UNSUPPORTED;
     p.page_units = a.cache.n_pages > 1 ? (int)(a.cache.page_stride / unit) : 1;
-    const int64_t units = (int64_t)(a.cache.n_pages - 1) * p.page_units + a.cache.n_kv_heads;
-    if (a.cache.page_stride / unit > INT32_MAX || units >= INT32_MAX) return ZOQAT_ERR_UNSUPPORTED;
+    const int64_t units = (int64_t)(a.cache.n_pages - 1) * p.page_units + a.cache.n_kv_heads;      // (the caller has checked that they fit)
     p.units = (int)units;
     p.page_shift = -1;
     for (int b = 3; b < 31; ++b)

@@ -955,3 +955,24 @@ def test_tree_step_leaves_the_pages_of_rows_with_a_bad_position(zq, name):
                 assert bool((c[page[kept], off[kept]] != 5.0).any())
                 c[page[kept], off[kept]] = 5.0
                 assert bool((c == 5.0).all()), (pos, "a row that was to be skipped")
+
+
+def test_tree_step_checks_every_cache_before_it_starts(zq):
+    # a cache that the attention cannot address is refused before the first layer has stored anything
+    shape, model = packed_model(zq, "llama_w4a8", 2, 64)
+    sv = Serving(zq, shape, model, 1, 16, "bf16", max_rows=2)
+    _, _, plan = sv.step([[3]])
+    for k, v in sv.caches:
+        k.fill_(5.0); v.fill_(5.0)
+    dev = torch.cuda.current_device()
+    good = [zq._caches(dev, k, v) for k, v in sv.caches]
+    tokens, nxt, scratch = ints([1, 2]), ints([9, 9]), torch.empty(48 << 20, dtype=torch.uint8, device="cuda")
+    tb = zq.TreeBatch(sv.table.data_ptr(), plan["kv_len"].data_ptr(), plan["row_start"].data_ptr(), plan["row_pos"].data_ptr(), plan["slot"].data_ptr(),
+                      plan["tree_mask"].data_ptr(), 1, sv.table.shape[1], 1, 0)
+    for n_pages, page, slot in ((1 << 20, 128 << 12, 256), (2, 1 << 37, 1 << 36)):
+        last = zq.PagedCache(good[1].k, good[1].v, good[1].type, n_pages, 16, 2, 128, 0, page, slot, 128)
+        rc = zq.lib().zoqat_decode_tree_step(model.handle, tokens.data_ptr(), 2, tb, (zq.PagedCache * 2)(good[0], last), None, None, nxt.data_ptr(),
+                                             scratch.data_ptr(), scratch.numel(), torch.cuda.current_stream().cuda_stream)
+        assert rc == zq.ERR_UNSUPPORTED
+    torch.cuda.synchronize()
+    assert nxt.tolist() == [9, 9] and all(bool((c == 5.0).all()) for kv in sv.caches for c in kv)

@@ -109,6 +109,16 @@ def test_attention_refuses_what_is_not_built_and_small_scratch(zq):
     assert L.zoqat_op_tree_attention_scratch_bytes(0, 64, None) == zq.ERR_INVALID_ARG
 
 
+def test_attention_refuses_caches_that_tensor_maps_do_not_hold(zq):
+    for kw in (dict(slot_stride=1 << 36, page_stride=1 << 37), dict(slot_stride=1 << 37, page_stride=1 << 37),
+               dict(n_pages=1 << 20, page_stride=128 << 12), dict(n_pages=3, page_stride=128 << 30)):
+        assert attend(zq, cache(zq, **kw)) == zq.ERR_UNSUPPORTED, kw
+    # one page, or one key head: the strides of what is there once do not count
+    assert attend(zq, cache(zq, n_pages=1, page_stride=1 << 37, slot_stride=1 << 36)) == zq.ERR_UNSUPPORTED
+    assert attend(zq, cache(zq, n_pages=1 << 20, page_stride=128 << 12, type=zq.TYPE_F32), nbytes=1 << 10) == zq.ERR_WORKSPACE_SMALL
+    assert attend(zq, cache(zq, n_pages=1 << 20, page_stride=128 << 12, n_kv_heads=1), nbytes=1 << 10) == zq.ERR_WORKSPACE_SMALL
+
+
 def rules(zq, desc=None, **kw):
     a = dict(logits=A, type=0, ld=100, rows=4, vocab=100)
     b = dict(out=2 * A, out_ld=100, token=3 * A, stream=None)
