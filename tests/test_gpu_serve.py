@@ -603,6 +603,83 @@ def test_scores_of_any_size(zq, dtype, qa, ka, heads, new, cached):
     assert bool(((got[:rows].double() - want).abs() <= bound).all())
 
 
+LONG_REQUESTS = [
+    # dtype, heads, kv, dh, page, layout, cached, new, mask
+    ("bf16", 4, 4, 128, 16, "token", [129] + [40] * 40, [300] + [1] * 40, "tree"),     # one wide request among single tokens: tiles of 16 queries
+    ("f16", 4, 2, 64, 32, "head", [0] + [300] * 40, [300] + [1] * 40, "tree"),         # of 32
+    ("bf16", 8, 2, 64, 16, "joint", [250] + [7, 500] * 20, [290] + [1, 2] * 20, "random"),    # of 64
+    ("f32", 4, 2, 128, 24, "token", [129] + [40] * 12, [300] + [1] * 12, "tree"),
+    ("f16", 4, 2, 128, 64, "token", [0, 129], [700, 513], None),                       # chunks of a prompt
+    ("bf16", 8, 2, 64, 16, "head", [129, 0], [700, 257], "tree"),
+    ("f32", 2, 1, 64, 16, "head", [0, 129], [700, 513], None),
+    ("bf16", 2, 2, 128, 128, "token", [0], [1000], "tree"),                            # masks of 32 words
+    ("bf16", 8, 2, 128, 384, "token", [1200, 383, 0], [9, 2, 700], None),              # pages that are no power of two
+    ("f16", 4, 4, 64, 640, "head", [1300, 639, 5], [1, 3, 2], "tree"),
+]
+
+
+@pytest.mark.parametrize("case", LONG_REQUESTS, ids=lambda c: "-".join(str(x) for x in c[:6]) + f"-n{max(c[7])}-{c[8]}")
+def test_requests_with_many_rows(zq, case):
+    dtype, heads, kv, dh, page, layout, cached, new, mask = case
+    pr = attention_problem(29, dtype, heads, kv, dh, page, layout, cached, new, mask)
+    got = run_attention(zq, pr)
+    want, bound = attention_oracle(pr)
+    off = (got[:pr["rows"]].double() - want).abs()
+    assert bool((off <= bound).all()), (float(off.max()), float((off / bound.clamp(min=1e-30)).max()))
+    assert torch.equal(run_attention(zq, pr)[:pr["rows"]], got[:pr["rows"]])
+
+
+@pytest.mark.parametrize("dtype,heads,kv,new", [("bf16", 2, 2, [300] + [1] * 30), ("f16", 4, 2, [300] + [1] * 30), ("f16", 8, 2, [300, 290]), ("f32", 4, 2, [300, 3])])
+@pytest.mark.parametrize("cached", [0, 70])
+def test_rows_that_see_late_drafts_only(zq, dtype, heads, kv, new, cached):
+    # rows whose first tiles of drafts are hidden whole, rows that see one draft, rows that see none
+    pr = attention_problem(31, dtype, heads, kv, 128, 16, "token", [cached] * len(new), new, "tree")
+    rng = np.random.default_rng(8)
+    pr["seen"] = [[[set(range(140, n, 3)), {n - 1}, set(), set(np.nonzero(rng.random(n) < 0.1)[0].tolist())][i % 4] & set(range(n)) for i in range(n)] for n in new]
+    words = pr["mask"].shape[1]
+    pr["mask"][:pr["rows"]] = ints([words_of(s, words) for r in pr["seen"] for s in r])
+    got = run_attention(zq, pr)
+    want, bound = attention_oracle(pr)
+    off = (got[:pr["rows"]].double() - want).abs()
+    assert bool((off <= bound).all()), (float(off.max()), float((off / bound.clamp(min=1e-30)).max()))
+    if cached == 0:
+        assert bool((got[2] == 0).all())
+
+
+@pytest.mark.parametrize("dtype,heads,kv,new", [("bf16", 8, 2, [5, 6, 4]), ("f16", 16, 2, [40, 33, 64]), ("f32", 4, 2, [2, 3, 1])])
+def test_two_streams_at_once(zq, dtype, heads, kv, new):
+    # a scratch each, eager calls and two graphs in flight; every call gives the bits of a call alone
+    prs = [attention_problem(41 + i, dtype, heads, kv, 128, 16, "token", c, new, "tree") for i, c in enumerate(([900, 3000, 40], [2100, 11, 700]))]
+    alone = [run_attention(zq, pr) for pr in prs]
+    streams = [torch.cuda.Stream() for _ in prs]
+    scratch = [torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda") for _ in prs]
+    outs, errs = [torch.full_like(pr["q"], 5.0) for pr in prs], [torch.zeros(1, dtype=torch.int32, device="cuda") for _ in prs]
+    torch.cuda.synchronize()
+
+    def call(i):
+        pr = prs[i]
+        zq.zoqat_op_tree_attention(pr["q"], pr["k"], pr["v"], pr["table"], pr["kv_len"], pr["row_start"], tree_mask=pr["mask"], out=outs[i], scratch=scratch[i],
+                                   err=errs[i])
+
+    graphs = []
+    for i, s in enumerate(streams):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            call(i)
+        graphs.append(g)
+    for rounds in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                outs[i].fill_(5.0)
+                if rounds % 2:
+                    call(i)
+                else:
+                    graphs[i].replay()
+    torch.cuda.synchronize()
+    for i, pr in enumerate(prs):
+        assert errs[i].item() == 0 and torch.equal(outs[i][:pr["rows"]], alone[i][:pr["rows"]]) and bool((outs[i][pr["rows"]:] == 5.0).all())
+
+
 def test_no_rows(zq):
     k, v = [torch.randn((4, 16, 2, 64), device="cuda").to(torch.bfloat16) for _ in range(2)]
     keep = k.clone()
