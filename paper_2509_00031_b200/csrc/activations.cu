@@ -588,7 +588,7 @@ void launch_norm_act_operand(const float* x, int64_t rows, int cols, int norm_ki
     } else {
         const size_t smem = (size_t)cols * sizeof(float);
         static DeviceOnce attr;
-        if (attr.first()) { cudaFuncSetAttribute(norm_act_operand_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024); }
+        attr.done([] { return allow_smem(norm_act_operand_kernel, 160 * 1024); });
         launch_kernel(norm_act_operand_kernel, dim3((unsigned)rows), dim3(kRowThreads), smem, s, dependent, x, cols, norm_kind, gain, bias, norm_eps, a_bits, op, row_step, normed, sm, planes);
     }
     count_launch();
@@ -607,7 +607,7 @@ void launch_ffn_act_operand(const float* x, int64_t rows, int cols, int gated, i
     } else {
         const size_t smem = (size_t)cols * sizeof(float);
         static DeviceOnce attr;
-        if (attr.first()) { cudaFuncSetAttribute(ffn_act_operand_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024); }
+        attr.done([] { return allow_smem(ffn_act_operand_kernel, 160 * 1024); });
         launch_kernel(ffn_act_operand_kernel, dim3((unsigned)rows), dim3(kRowThreads), smem, s, dependent, x, cols, gated, a_bits, op, row_step, sm, planes, pre);
     }
     count_launch();

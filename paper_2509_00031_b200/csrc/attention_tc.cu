@@ -653,11 +653,7 @@ int attention_tc_launch(const float* qkv, int batch, int seq, int n_heads, const
         !make_half_map(&m_vth, vth, seq, D, bhs, seq_pad, D) || !make_half_map(&m_vtl, vtl, seq, D, bhs, seq_pad, D))
         return ZOQAT_ERR_CUDA;
     static DeviceOnce attr;
-    if (attr.first() &&
-        cudaFuncSetAttribute(attention_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes) != cudaSuccess) {
-        attr.retry();
-        return ZOQAT_ERR_CUDA;
-    }
+    if (!attr.done([] { return allow_smem(attention_tc_kernel<D>, Cfg::kSmemBytes); })) return ZOQAT_ERR_CUDA;
     AttParams p;
     p.seq = seq; p.n_heads = n_heads; p.batch = batch;
     p.n_qt = (seq + BQ - 1) / BQ;

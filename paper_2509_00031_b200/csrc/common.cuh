@@ -15,22 +15,25 @@ constexpr int kErrWaitAccEmpty = 4;  // MMA warp: accumulator never drained
 constexpr int kErrCodeRange = 32;    // 8-bit operands: a weight code minus its zero point does not fit a signed byte
 constexpr int kErrBadLabel = 16;     // cross-entropy: a label >= vocab (not a wait; the position's loss is reported as 0)
 
-// Per-device one-time set-up (function attributes, cached device properties): true the first time it is called with this
-// word while device `ordinal < 64` is current; ordinals beyond that always get true and simply repeat the set-up.
+// Per-device one-time set-up (function attributes, cached device properties).  done(set_up) is true once a set-up of the current
+// device has succeeded.  The mark is put behind the set-up, so no thread goes on while another is still at it; threads that come
+// at once may each run it, which is harmless.  Devices from 64 on repeat it every time.
 struct DeviceOnce {
     unsigned long long seen = 0;
-    bool first() {
+    template <typename F> bool done(F set_up) {
         int dev = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return true;
-        const unsigned long long bit = 1ull << dev;
-        return (__atomic_fetch_or(&seen, bit, __ATOMIC_ACQ_REL) & bit) == 0;
-    }
-    // forget the current device (its set-up failed and must be tried again)
-    void retry() {
-        int dev = 0;
-        if (cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 64) __atomic_fetch_and(&seen, ~(1ull << dev), __ATOMIC_ACQ_REL);
+        const unsigned long long bit = cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 64 ? 1ull << dev : 0;
+        if (__atomic_load_n(&seen, __ATOMIC_ACQUIRE) & bit) return true;
+        if (!set_up()) return false;
+        __atomic_fetch_or(&seen, bit, __ATOMIC_RELEASE);
+        return true;
     }
 };
+#ifdef __CUDACC__
+template <typename K> inline bool allow_smem(K* kernel, int bytes) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
+}
+#endif
 // The inverse-distribution table of the direction generator is uploaded to the current device on first use; false if
 // that failed (callers report it instead of launching a generator kernel on a missing table).
 bool generator_table_ready();

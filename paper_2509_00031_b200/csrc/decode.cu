@@ -509,7 +509,7 @@ int launch_decode_gemv(const void* wq, const float2* qparams, int N, int K, int 
 #define ZQ_GEMV(MBV)                                                                                                      \
     {                                                                                                                     \
         static DeviceOnce attr;                                                                                         \
-        if (attr.first()) { cudaFuncSetAttribute(decode_gemv_kernel<MBV>, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024); } \
+        attr.done([] { return allow_smem(decode_gemv_kernel<MBV>, 160 * 1024); }); \
         launch_kernel(decode_gemv_kernel<MBV>, dim3(grid), dim3(kGemvThreads), smem, s, true, w4, qparams, N, K, gshift, act, row_step, bias, accumulate, out); \
     }
     if (mb == 1) ZQ_GEMV(1) else if (mb == 2) ZQ_GEMV(2) else if (mb == 4) ZQ_GEMV(4) else if (mb == 8) ZQ_GEMV(8) else return -1;
@@ -529,7 +529,7 @@ int launch_decode_gemv_fp(const void* wq, const float2* qparams, int N, int K, i
 #define ZQ_GEMV_FP(MBV)                                                                                                   \
     {                                                                                                                     \
         static DeviceOnce attr;                                                                                         \
-        if (attr.first()) { cudaFuncSetAttribute(decode_gemv_fp_kernel<MBV>, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024); } \
+        attr.done([] { return allow_smem(decode_gemv_fp_kernel<MBV>, 160 * 1024); }); \
         launch_kernel(decode_gemv_fp_kernel<MBV>, dim3(grid), dim3(kGemvThreads), smem, s, true, w4, qparams, N, K, gshift, act, bias, accumulate, out); \
     }
     if (mb == 1) ZQ_GEMV_FP(1) else if (mb == 2) ZQ_GEMV_FP(2) else if (mb == 4) ZQ_GEMV_FP(4) else if (mb == 8) ZQ_GEMV_FP(8) else return -1;
@@ -555,7 +555,7 @@ int launch_decode_head(const __nv_bfloat16* w, int V, int d, int mb, const __nv_
     else if (mb == 4) launch_kernel(decode_head_kernel<4>, dim3(grid), dim3(kGemvThreads), smem, s, true, w4, V, d, x, logits);
     else if (mb == 8) {
         static DeviceOnce attr;
-        if (attr.first()) { cudaFuncSetAttribute(decode_head_kernel<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024); }
+        attr.done([] { return allow_smem(decode_head_kernel<8>, 160 * 1024); });
         launch_kernel(decode_head_kernel<8>, dim3(grid), dim3(kGemvThreads), smem, s, true, w4, V, d, x, logits);
     } else return -1;
     count_launch();

@@ -737,11 +737,7 @@ int launch_tc(const GemmArgs& a, cudaStream_t s) {
         map_out = map_a;      // never dereferenced
     }
     static DeviceOnce attr;
-    if (attr.first() &&
-        cudaFuncSetAttribute(gemm_tc_kernel<BN, CG, I8>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes) != cudaSuccess) {
-        attr.retry();
-        return ZOQAT_ERR_CUDA;
-    }
+    if (!attr.done([] { return allow_smem(gemm_tc_kernel<BN, CG, I8>, Cfg::kSmemBytes); })) return ZOQAT_ERR_CUDA;
     const int units = num_sms() / CG;                      // persistent CTAs (CG = 1) or CTA pairs (CG = 2)
     {
         const TileOrder o = choose_order(a.M, a.N, a.K, p.tiles_m, p.tiles_n, BM * CG, BN, units, I8 ? 1 : 2);

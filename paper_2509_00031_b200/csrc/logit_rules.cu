@@ -315,10 +315,7 @@ int launch_rules_vec(const T* logits, int64_t ld, int rows, int vocab, const Log
     const int slice = ((vocab + slices - 1) / slices + 31) / 32 * 32, cap = slice < kMaxMarked ? slice : kMaxMarked;
     const size_t smem = ((r.history || r.draft_token || r.bias_token) ? (size_t)cap * 10 + slice / 4 : 0) + (r.allowed ? slice / 8 : 0);
     static DeviceOnce attr;
-    if (attr.first() && cudaFuncSetAttribute(logit_rules_kernel<T, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxMarked * 10 + kMaxSlice / 8 * 3) != cudaSuccess) {
-        attr.retry();
-        return -1;
-    }
+    if (!attr.done([] { return allow_smem(logit_rules_kernel<T, VEC>, kMaxMarked * 10 + kMaxSlice / 8 * 3); })) return -1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ranks, rows);
     cfg.blockDim = dim3(kRuleThreads);

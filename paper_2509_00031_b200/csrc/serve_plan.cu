@@ -293,11 +293,7 @@ int launch_cache_plan(const CachePlanArgs& a, cudaStream_t s) {
     const size_t smem = (size_t)2 * (a.batch + 1) * sizeof(int32_t);
     if (a.batch > kMaxPlanBatch) return -1;
     static DeviceOnce attr;
-    if (attr.first() && cudaFuncSetAttribute(cache_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             (int)(2 * (kMaxPlanBatch + 1) * sizeof(int32_t))) != cudaSuccess) {
-        attr.retry();
-        return -1;
-    }
+    if (!attr.done([] { return allow_smem(cache_plan_kernel, (int)(2 * (kMaxPlanBatch + 1) * sizeof(int32_t))); })) return -1;
     // one row (and its tables' share) a thread up to a wave of the 148 SMs
     int grid = (a.max_rows + kPlanThreads - 1) / kPlanThreads;
     grid = grid < 1 ? 1 : (grid > 148 ? 148 : grid);

@@ -295,11 +295,7 @@ tree_attention_simt_kernel(SimtParams p) {
 template <int DH>
 int simt_launch(const SimtParams& p, int grid, int combine_y, cudaStream_t s, bool dependent) {
     static DeviceOnce attr;
-    if (attr.first() && cudaFuncSetAttribute(tree_attention_simt_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             SimtCfg<DH>::kSmemBytes) != cudaSuccess) {
-        attr.retry();
-        return ZOQAT_ERR_CUDA;
-    }
+    if (!attr.done([] { return allow_smem(tree_attention_simt_kernel<DH>, SimtCfg<DH>::kSmemBytes); })) return ZOQAT_ERR_CUDA;
     if (launch_kernel(tree_attention_simt_kernel<DH>, dim3(grid), dim3(kSimtThreads), SimtCfg<DH>::kSmemBytes, s, dependent, p) != cudaSuccess)
         return ZOQAT_ERR_CUDA;
     count_launch();

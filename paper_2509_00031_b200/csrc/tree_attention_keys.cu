@@ -577,10 +577,7 @@ template <int DH, int N, typename T>
 int keys_launch(const TcParams& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int grid, cudaStream_t s, bool dependent) {
     using Cfg = KeyCfg<DH, N>;
     static DeviceOnce attr;
-    if (attr.first() && cudaFuncSetAttribute(tree_attention_keys_kernel<DH, N, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes) != cudaSuccess) {
-        attr.retry();
-        return ZOQAT_ERR_CUDA;
-    }
+    if (!attr.done([] { return allow_smem(tree_attention_keys_kernel<DH, N, T>, Cfg::kSmemBytes); })) return ZOQAT_ERR_CUDA;
     TcParams q = p;
     q.smem_bytes = Cfg::kSmemBytes;
     return launch_kernel(tree_attention_keys_kernel<DH, N, T>, dim3(grid), dim3(kKeyThreads), Cfg::kSmemBytes, s, dependent, map_k, map_v, q) == cudaSuccess

@@ -432,11 +432,7 @@ bool encode(CUtensorMap* map, int type, const void* base, int rank, const cuuint
 template <int DH, typename T>
 int tc_launch(const TcParams& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int grid, cudaStream_t s, bool dependent) {
     static DeviceOnce attr;
-    if (attr.first() &&
-        cudaFuncSetAttribute(tree_attention_tc_kernel<DH, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcCfg<DH>::kSmemBytes) != cudaSuccess) {
-        attr.retry();
-        return ZOQAT_ERR_CUDA;
-    }
+    if (!attr.done([] { return allow_smem(tree_attention_tc_kernel<DH, T>, TcCfg<DH>::kSmemBytes); })) return ZOQAT_ERR_CUDA;
     TcParams q = p;
     q.smem_bytes = TcCfg<DH>::kSmemBytes;
     return launch_kernel(tree_attention_tc_kernel<DH, T>, dim3(grid), dim3(kTcThreads), TcCfg<DH>::kSmemBytes, s, dependent, map_k, map_v, q) == cudaSuccess

@@ -1185,9 +1185,7 @@ static void row_launch(const LearnedOperandArgs& a, cudaStream_t s) {
     // static + dynamic shared memory exceed the default limit from NI = 2 on: every instantiation opts in
     const size_t smem = (size_t)NI * 16 * kThreads * sizeof(float);
     static DeviceOnce attr;
-    if (attr.first() && cudaFuncSetAttribute(weight_operand_row_kernel<NI, UPD, I8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             (int)smem) != cudaSuccess)
-        attr.retry();
+    attr.done([&] { return allow_smem(weight_operand_row_kernel<NI, UPD, I8>, (int)smem); });
     const int per_sm = NI == 1 ? 4 : (NI == 2 ? 3 : 2);
     const int64_t cap = (int64_t)148 * per_sm * 3;         // about three waves: the tail balances itself
     const int grid = (int)(a.rows < cap ? a.rows : cap);
