@@ -35,6 +35,12 @@ int cuda_fail(cudaError_t e, const char* what) {
     return fail(ZOQAT_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
+// A launch function gave up: with the CUDA error behind it, which is taken back, so that the next call does not report it as its own.
+int launch_fail(int code, const char* what) {
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? fail(code, "%s", what) : fail(code, "%s: %s", what, cudaGetErrorString(e));
+}
+
 #define CUDA_TRY(expr)                                              \
     do {                                                            \
         cudaError_t e__ = (expr);                                   \
@@ -1876,7 +1882,7 @@ int zoqat_op_cache_plan(const int32_t* cached_len_dev, const int32_t* new_len_de
     CachePlanArgs a{cached_len_dev, new_len_dev, batch, page_size, n_pages, max_pages, free_pages_dev, free_capacity, n_free_dev,
                     block_table_dev, parents_dev, max_rows, mask_words, kv_len_dev, row_start_dev, row_request_dev, row_pos_dev,
                     slot_dev, tree_mask_dev, n_free_out_dev, status_dev};
-    if (launch_cache_plan(a, static_cast<cudaStream_t>(stream)) != 0) return fail(ZOQAT_ERR_CUDA, "cache plan: kernel set-up failed");
+    if (launch_cache_plan(a, static_cast<cudaStream_t>(stream)) != 0) return launch_fail(ZOQAT_ERR_CUDA, "cache plan");
     CUDA_TRY(cudaGetLastError());
     return ZOQAT_OK;
 }
@@ -1936,7 +1942,7 @@ int zoqat_op_tree_attention(const void* q_dev, int64_t q_stride, const zoqat_pag
     a.out = out_dev; a.out_stride = out_stride; a.scratch = static_cast<uint8_t*>(scratch_dev); a.err_flag = err_flag_dev;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int rc = tc ? launch_tree_attention_tc(a, s, false) : launch_tree_attention_simt(a, s, false);
-    if (rc != ZOQAT_OK) return fail(rc, "tree attention launch failed");
+    if (rc != ZOQAT_OK) return launch_fail(rc, "tree attention");
     CUDA_TRY(cudaGetLastError());
     return ZOQAT_OK;
 }
@@ -1952,7 +1958,7 @@ int zoqat_op_logit_rules(const void* logits_dev, int type, int64_t ld, int rows,
     const size_t e = (size_t)type_bytes(type);
     if (misaligned(logits_dev, e) || misaligned(out_dev, e)) return fail(ZOQAT_ERR_INVALID_ARG, "misaligned pointer");
     if (launch_logit_rules(logits_dev, type, ld, rows, vocab, r, out_dev, out_ld, token_dev, static_cast<cudaStream_t>(stream)) != 0)
-        return fail(ZOQAT_ERR_CUDA, "logit rules: launch failed");
+        return launch_fail(ZOQAT_ERR_CUDA, "logit rules");
     CUDA_TRY(cudaGetLastError());
     return ZOQAT_OK;
 }
@@ -2015,7 +2021,7 @@ int zoqat_decode_tree_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows
         a.row_start = plan->row_start; a.tree_mask = plan->tree_mask; a.mask_words = plan->mask_words; a.batch = plan->batch; a.rows = rows; a.n_heads = H;
         a.scale = (float)(1.0 / std::sqrt((double)dh)); a.out = half ? static_cast<void*>(att16) : w.att; a.out_stride = d;
         a.scratch = static_cast<uint8_t*>(scratch_dev); a.err_flag = w.err_flag;
-        if (int rc = half ? launch_tree_attention_tc(a, s, true) : launch_tree_attention_simt(a, s, true)) return fail(rc, "tree attention launch failed");
+        if (int rc = half ? launch_tree_attention_tc(a, s, true) : launch_tree_attention_simt(a, s, true)) return launch_fail(rc, "tree attention");
         if (half) launch_widen(att16, p.type, (int64_t)rows * d, w.att, s);
         launch_norm_act_operand(w.att, rows, d, 0, nullptr, nullptr, 0.f, c.a_bits, w.xa, w.row_step, nullptr, s, SmoothAct(), true, planes);
         if (int rc = gemv(dl.w_o, dl.q_o, d, d, Ly.vec[ZOQAT_ROLE_BO], 1, w.h)) return rc;
@@ -2029,7 +2035,7 @@ int zoqat_decode_tree_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows
     float* logits = logits_dev ? logits_dev : D.logits;
     if (launch_decode_head(D.head, c.vocab, d, rows, w.xa, logits, s) != 0) return fail(ZOQAT_ERR_UNSUPPORTED, "vocabulary projection rejected");
     if (rules) {
-        if (launch_logit_rules(logits, kTypeF32, c.vocab, rows, c.vocab, r, logits, c.vocab, next_token_dev, s) != 0) return fail(ZOQAT_ERR_CUDA, "logit rules: launch failed");
+        if (launch_logit_rules(logits, kTypeF32, c.vocab, rows, c.vocab, r, logits, c.vocab, next_token_dev, s) != 0) return launch_fail(ZOQAT_ERR_CUDA, "logit rules");
     } else if (next_token_dev) {
         launch_decode_argmax(logits, rows, c.vocab, next_token_dev, s);
     }

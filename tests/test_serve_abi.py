@@ -145,3 +145,13 @@ def test_rules_refuse_sizes_that_are_not_built(zq):
     for kw in (dict(rows=0), dict(rows=65536), dict(vocab=0), dict(vocab=(1 << 30) + 1)):
         assert rules(zq, dict(row_request=A), **kw) == zq.ERR_UNSUPPORTED
     assert zq.lib().zoqat_op_logit_rules(A, 0, 100, 4, 100, None, A, 100, A, None) == zq.ERR_INVALID_ARG
+
+
+def test_a_launch_that_fails_names_the_cuda_error(zq):
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("the calls would run")
+    for call, who in ((lambda: plan(zq), b"cache plan: "), (lambda: attend(zq, cache(zq, type=zq.TYPE_F32)), b"tree attention: "), (lambda: rules(zq), b"logit rules: ")):
+        assert call() == zq.ERR_CUDA
+        text = zq.lib().zoqat_last_error()
+        assert text.startswith(who) and len(text) > len(who) + 5, text
