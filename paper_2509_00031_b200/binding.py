@@ -491,12 +491,6 @@ def _caches(dev, k, v):
     return PagedCache(k.data_ptr(), v.data_ptr(), ty, s[0], s[1], s[2], s[3], 0, st[0], st[1], st[2])
 
 
-def paged_cache(k_cache, v_cache):
-    """zoqat_paged_cache_t of two tensors [n_pages, page_size, n_kv_heads, d_head] with the same strides (a cache laid out head by
-    head is passed as its transposed view)."""
-    return _caches(torch.cuda.current_device(), k_cache, v_cache)
-
-
 def zoqat_op_cache_plan(cached_len, new_len, page_size, n_pages, free_pages, n_free, block_table, max_rows, parents=None, mask_words=0, out=None):
     """-> dict of int32 tensors: kv_len, row_start, row_request, row_pos, slot, n_free, status and, with mask_words, tree_mask.
     block_table is extended in place.  out: such a dict of an earlier call to write into (its status word is or-ed)."""

@@ -82,7 +82,6 @@ logit_rules_kernel(const T* logits, int64_t ld, int rows, int vocab, int slice, 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = cluster_ctarank(), ranks = cluster_nctarank();
     const int64_t row = blockIdx.y;
-    grid_dependency_wait();
     const int req = R.row_request ? __ldg(R.row_request + row) : (int)row;
     if (req < 0 || req >= R.batch) return;      // the same answer in every CTA of the cluster: the row is left as it is
 
@@ -306,7 +305,7 @@ logit_rules_kernel(const T* logits, int64_t ld, int rows, int vocab, int slice, 
 
 template <typename T, int VEC>
 int launch_rules_vec(const T* logits, int64_t ld, int rows, int vocab, const LogitRules& r, T* out, int64_t out_ld, int32_t* token,
-                 cudaStream_t s, bool dependent) {
+                 cudaStream_t s) {
     // at least 1024 tokens to a CTA, and no more CTAs of a cluster than it takes to fill the SMs (1 / 2 / 4 / 8 CTAs a row, histories
     // of 700, us: 8 rows of 32000 16 / 14 / 14 / 13; 64 of 50272 21 / 16 / 16 / 25; 256 of 50272 29 / 35 / 47 / 74)
     int ranks = 1;
@@ -321,13 +320,11 @@ int launch_rules_vec(const T* logits, int64_t ld, int rows, int vocab, const Log
     cfg.blockDim = dim3(kRuleThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute at[2];
+    cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = ranks; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
-    cfg.numAttrs = dependent ? 2 : 1;
+    cfg.numAttrs = 1;
     if (cudaLaunchKernelEx(&cfg, logit_rules_kernel<T, VEC>, logits, ld, rows, vocab, slice, cap, r, out, out_ld, token) != cudaSuccess) return -1;
     count_launch();
     return 0;
@@ -335,20 +332,20 @@ int launch_rules_vec(const T* logits, int64_t ld, int rows, int vocab, const Log
 
 template <typename T>
 int launch_rules(const T* logits, int64_t ld, int rows, int vocab, const LogitRules& r, T* out, int64_t out_ld, int32_t* token,
-                 cudaStream_t s, bool dependent) {
+                 cudaStream_t s) {
     // every row begins at 16 bytes: vectors (a row of an odd vocabulary packed tightly does not)
     const uintptr_t at = reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(out) | (uintptr_t)(ld * sizeof(T)) | (uintptr_t)(out_ld * sizeof(T));
-    if (at % 16 == 0) return launch_rules_vec<T, 16 / sizeof(T)>(logits, ld, rows, vocab, r, out, out_ld, token, s, dependent);
-    return launch_rules_vec<T, 1>(logits, ld, rows, vocab, r, out, out_ld, token, s, dependent);
+    if (at % 16 == 0) return launch_rules_vec<T, 16 / sizeof(T)>(logits, ld, rows, vocab, r, out, out_ld, token, s);
+    return launch_rules_vec<T, 1>(logits, ld, rows, vocab, r, out, out_ld, token, s);
 }
 
 }  // namespace
 
 int launch_logit_rules(const void* logits, int type, int64_t ld, int rows, int vocab, const LogitRules& r, void* out, int64_t out_ld,
-                       int32_t* token, cudaStream_t s, bool dependent) {
-    if (type == kTypeF32) return launch_rules(static_cast<const float*>(logits), ld, rows, vocab, r, static_cast<float*>(out), out_ld, token, s, dependent);
-    if (type == kTypeBf16) return launch_rules(static_cast<const __nv_bfloat16*>(logits), ld, rows, vocab, r, static_cast<__nv_bfloat16*>(out), out_ld, token, s, dependent);
-    return launch_rules(static_cast<const __half*>(logits), ld, rows, vocab, r, static_cast<__half*>(out), out_ld, token, s, dependent);
+                       int32_t* token, cudaStream_t s) {
+    if (type == kTypeF32) return launch_rules(static_cast<const float*>(logits), ld, rows, vocab, r, static_cast<float*>(out), out_ld, token, s);
+    if (type == kTypeBf16) return launch_rules(static_cast<const __nv_bfloat16*>(logits), ld, rows, vocab, r, static_cast<__nv_bfloat16*>(out), out_ld, token, s);
+    return launch_rules(static_cast<const __half*>(logits), ld, rows, vocab, r, static_cast<__half*>(out), out_ld, token, s);
 }
 
 }  // namespace zq

@@ -89,6 +89,6 @@ struct LogitRules {
     int mask_words;
 };
 int launch_logit_rules(const void* logits, int type, int64_t ld, int rows, int vocab, const LogitRules& r, void* out, int64_t out_ld,
-                       int32_t* token, cudaStream_t s, bool dependent = false);           // 0, or -1: launch set-up failed
+                       int32_t* token, cudaStream_t s);           // 0, or -1: launch set-up failed
 
 }  // namespace zq

@@ -299,7 +299,7 @@ int simt_launch(const SimtParams& p, int grid, int combine_y, cudaStream_t s, bo
     if (launch_kernel(tree_attention_simt_kernel<DH>, dim3(grid), dim3(kSimtThreads), SimtCfg<DH>::kSmemBytes, s, dependent, p) != cudaSuccess)
         return ZOQAT_ERR_CUDA;
     count_launch();
-    if (launch_kernel(tree_combine_kernel<float, DH>, dim3(grid, combine_y), dim3(256), 0, s, true, p.scratch, kSimtRows, p.w.group, p.w.n_heads, p.out,
+    if (launch_kernel(tree_combine_kernel<float, DH>, dim3(grid, combine_y), dim3(256), 0, s, true, p.scratch, kSimtRows, p.w.group, p.out,
                       p.out_stride) != cudaSuccess)
         return ZOQAT_ERR_CUDA;
     count_launch();
@@ -322,7 +322,7 @@ size_t tree_attention_scratch_bytes(int type, int d_head) {
 
 int launch_tree_attention_simt(const TreeAttnArgs& a, cudaStream_t s, bool dependent) {
     SimtParams p{};
-    p.w = TreeWork{a.kv_len, a.row_start, a.block_table, a.batch, a.rows, a.n_heads, a.cache.n_kv_heads, a.max_pages, a.cache.page_size,
+    p.w = TreeWork{a.kv_len, a.row_start, a.block_table, a.batch, a.rows, a.cache.n_kv_heads, a.max_pages, a.cache.page_size,
                    a.n_heads / a.cache.n_kv_heads, kSimtRows, kSimtKeys, 4, a.err_flag};
     p.q = static_cast<const float*>(a.q); p.q_stride = a.q_stride; p.cache = a.cache;
     p.tree_mask = a.tree_mask; p.mask_words = a.mask_words;

@@ -18,7 +18,7 @@ namespace zq {
 
 struct TreeWork {
     const int32_t *kv_len, *row_start, *block_table;
-    int batch, rows, n_heads, n_kv, max_pages, page_size;
+    int batch, rows, n_kv, max_pages, page_size;
     int group;               // query heads per key head
     int tile_rows;           // queries per row tile
     int key_tile;            // keys per key tile
@@ -178,7 +178,7 @@ template <> __device__ __forceinline__ __half tree_round<__half>(float v) { retu
 // warp order; a query that saw no key gives zeros.  All of it in binary32, one rounding at the end.
 template <typename T, int DH>
 __global__ void __launch_bounds__(256)
-tree_combine_kernel(uint8_t* scratch, int tile_rows, int group, int n_heads, T* out, int64_t out_stride) {
+tree_combine_kernel(uint8_t* scratch, int tile_rows, int group, T* out, int64_t out_stride) {
     constexpr int VPL = DH / 32;
     __shared__ float acc_s[8][DH], m_s[8], l_s[8];
     grid_dependency_wait();

@@ -441,7 +441,7 @@ int tc_launch(const TcParams& p, const CUtensorMap& map_k, const CUtensorMap& ma
 
 template <int DH, typename T>
 int combine_launch(const TcParams& p, int grid, int y, cudaStream_t s) {
-    return launch_kernel(tree_combine_kernel<T, DH>, dim3(grid, y), dim3(256), 0, s, true, p.scratch, p.w.tile_rows, p.w.group, p.w.n_heads,
+    return launch_kernel(tree_combine_kernel<T, DH>, dim3(grid, y), dim3(256), 0, s, true, p.scratch, p.w.tile_rows, p.w.group,
                          static_cast<T*>(p.out), p.out_stride) == cudaSuccess ? ZOQAT_OK : ZOQAT_ERR_CUDA;
 }
 
@@ -460,7 +460,7 @@ int launch_tree_attention_tc(const TreeAttnArgs& a, cudaStream_t s, bool depende
     const long long drafts = (long long)a.rows * group;
     const long long want = a.rows <= a.batch ? group : (3 * drafts + 2 * a.batch - 1) / (2 * a.batch);     // 1.5 x the average
     const int nq = want <= 16 ? 16 : (want <= 32 ? 32 : (want <= 64 ? 64 : kRows));
-    p.w = TreeWork{a.kv_len, a.row_start, a.block_table, a.batch, a.rows, a.n_heads, a.cache.n_kv_heads, a.max_pages, a.cache.page_size,
+    p.w = TreeWork{a.kv_len, a.row_start, a.block_table, a.batch, a.rows, a.cache.n_kv_heads, a.max_pages, a.cache.page_size,
                    group, nq < kRows ? nq : kTileRows, kKeys, 4, a.err_flag};
     p.q = a.q; p.q_stride = a.q_stride;
     p.box_keys = a.cache.page_size < kKeys ? a.cache.page_size : kKeys;
