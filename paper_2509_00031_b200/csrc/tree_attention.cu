@@ -114,7 +114,7 @@ __device__ __forceinline__ void tile_step(const SimtParams& p, const TreeCursor&
         s[r] += __shfl_xor_sync(0xffffffffu, s[r], 1);
         s[r] += __shfl_xor_sync(0xffffffffu, s[r], 2);
         s[r] += __shfl_xor_sync(0xffffffffu, s[r], 4);
-        s[r] *= p.scale_log2;
+        s[r] = __fmul_rn(s[r], p.scale_log2);              // rounded by itself: the reference is such a product
         if (tail) {
             bool vis = t < C;
             if (!vis && t < c.r.L && r < nq) {
