@@ -676,8 +676,8 @@ int zoqat_op_cache_plan(const int32_t* cached_len_dev, const int32_t* new_len_de
  * aligned, ld % 4 == 0): q heads, k heads, v heads.  q and k are rotated by the tables' row row_pos_dev[r] (cos_dev / sin_dev fp32
  * [rope_len, d_head / 2], pairs (i, i + d_head / 2); both NULL: no rotation, row_pos_dev unused), rounded once to the cache's
  * type; q goes to q_out_dev (of that type, [rows, n_heads, d_head], rows q_stride elements apart), k and v into slot slot_dev[r].
- * A row with a negative slot is skipped, its q_out row left as it is; a slot or position outside the cache / the tables is
- * skipped too and sets *err_flag_dev to 40.  Two rows with the same slot: either may win, element by element.  rows = 0 is
+ * A row with a negative slot is skipped, its q_out row left as it is; so is, whole, a row whose slot or position lies outside the
+ * cache / the tables, and it sets *err_flag_dev to 40.  Two rows with the same slot: either may win, element by element.  rows = 0 is
  * allowed (nothing is done). */
 int zoqat_op_cache_append(const float* qkv_dev, int64_t ld, const int32_t* row_pos_dev, const int32_t* slot_dev, int rows,
                           int n_heads, const float* cos_dev, const float* sin_dev, int rope_len,
@@ -748,8 +748,9 @@ typedef struct zoqat_tree_batch {
 } zoqat_tree_batch_t;
 
 /* Feeds tokens_dev[rows] (rows in {1, 2, 4, 8}; of all requests, back to back; rows behind the last are padding) through the
- * model and writes logits_dev fp32 [rows, vocab] - row r's prediction of the token after it - and / or next_token_dev int32
- * [rows]: the greedy choice, under `rules` (zoqat_op_logit_rules, applied to the logits in place) unless that is NULL.
+ * model (a token outside [0, vocab) as an embedding of zeros) and writes logits_dev fp32 [rows, vocab] - row r's prediction of the
+ * token after it - and / or next_token_dev int32 [rows]: the greedy choice, under `rules` (zoqat_op_logit_rules, applied to the
+ * logits in place) unless that is NULL.
  * caches: n_layers descriptions (host memory, read before the call returns), n_kv_heads = n_heads, any type; the rows' keys and values
  * are written before they are attended to.  Needs zoqat_decode_begin (its batch is the most rows that may leave logits_dev
  * NULL; the cache it lays out is not used).  scratch_dev as for zoqat_op_tree_attention.  Logits of padding rows are unspecified.

@@ -6,8 +6,8 @@
 //                         the requests; the k-th new page of request b is free[n_free - 1 - (first_b + k)].  One launch:
 //                         every CTA scans all requests itself (a few kB from L2) and then writes its share of the rows and
 //                         of the tables, so no CTA waits for another and no scratch is needed.
-//                         Bound by latency: a launch, two chained loads and two block scans; 12 us a call from Python for 8
-//                         to 1024 requests, the host's share included.
+//                         Bound by latency: a launch, two chained loads and two block scans; 12 to 13 us a call from
+//                         Python; replayed from a graph 3.3 us for 8 requests of one token, 4.7 for 64 prompts, 8.6 for 1024 trees.
 //   cache_append_kernel   (a, b) -> (a cos - b sin, b cos + a sin) for q and k, then one rounding into the cache's type.
 //                         Bound by memory: 8191 rows of 40 + 2 * 8 heads of 128 into binary16, 356 MB in 63.5 us, 87 % of the
 //                         rate of a plain copy.

@@ -5,11 +5,11 @@
 //                                                                            the drafts j (t = C + j) whose mask bit is set
 //
 // With up to 8 queries per key head a key costs 2 * 8 * d_head fused multiply-adds against 8 * d_head bytes from memory: the
-// kernel is bound by reading the cache: 5.6 TB/s for 8 x 32 heads of 4096 keys at d_head 128.  A CTA of 8 warps takes key tiles of
-// 32 keys through two stages filled by cp.async, two CTAs per SM (8 x 32 heads of 1 to 1020 keys: 59.5 us; one CTA with a ring of
+// kernel is bound by reading the cache: 5.7 TB/s for 8 x 32 heads of 4096 keys at d_head 128.  A CTA of 8 warps takes key tiles of
+// 32 keys through two stages filled by cp.async, two CTAs per SM (8 x 32 heads of 1 to 1020 keys: 59.8 us; one CTA with a ring of
 // five stages, 128 KB in flight, 65: two hide one another's joins); each warp owns 4 keys of every tile and keeps its own running maximum, sum and output
 // for all 8 queries in registers, so the warps meet once per tile, where a stage is handed over, and once per item, when
-// their results are joined in shared memory.
+// their results are joined in shared memory.  Two CTAs per SM leave 128 registers a thread: at d_head 128 ptxas spills 108 bytes.
 //   scores  8 lanes per key, each an eighth of its elements (every K element is read from shared memory once), joined by three
 //           shuffles per query
 //   output  a lane owns 4 (2) columns of all queries; every V element is read once

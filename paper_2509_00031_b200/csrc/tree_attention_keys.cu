@@ -7,16 +7,17 @@
 //   l[query] += sum_key P^T            N = 16: every thread adds up its keys' weights, the threads' sums are joined when a piece
 //                                      ends; else by a third product with a matrix of ones, which leaves the sums in every TMEM
 //                                      lane.  The tensor pipe spends some 45 cycles on a product of 128 x N x 16 however small N
-//                                      is, and at d_head 64 the third product is 8 of a tile's 20 (16 x 32 heads of 8192 keys:
-//                                      225 us with it, 187 without); joining 32 sums costs short pieces more than that
+//                                      is, and at d_head 64 the third product is 8 of a tile's 20 (16 x 32 heads of 8192 keys in
+//                                      pages laid out head by head: 225 us with it, 187 without); joining 32 sums costs short pieces more than that
 //                                      (64 requests of 300 keys, 4 drafts of 4 heads: 51 us with it, 64 without).
 //
 // so the softmax costs 128 * N exponentials per tile of 128 keys, spread over all four schedulers, whatever the tile's number of
 // live queries N = 16, 32 or 64 is; with queries as rows (tree_attention_tc.cu) a single query would cost a whole warp's 128
 // exponentials on one scheduler, and the kernel would be bound by them instead of by reading the cache.  What bounds it is
 // the cache: 64 KB a tile at d_head 128, some 2800 cycles of an SM's share of the memory, against 700 to 1100 of the tensor pipe
-// and 8 N of the exponential units.  Measured, bf16, one token for each of 16 x 32 heads: 6.5 TB/s at 8192 keys and d_head 128, 5.3
-// at 2048; 5.7 and 3.5 at d_head 64.  What short contexts lose is fixed: 4 us until the first scores, 3 for the last piece's
+// and 8 N of the exponential units.  Measured, bf16, one token for each of 16 x 32 heads, replayed from a graph: 6.5 TB/s at 8192 keys
+// and d_head 128, 5.7 at 2048; at d_head 64 5.6 and 3.7 with pages laid out head by head, 4.0 and 3.6 slot by slot (a head's keys are then
+// rows of 128 bytes 4 KB apart).  What short contexts lose is fixed: 4 us until the first scores, 3 for the last piece's
 // output, 4 for the launch that joins split pieces, and up to 8 between the first and the last CTA to finish.
 //
 // One persistent CTA per SM, 12 warps; the key tiles of all requests are dealt out in equal runs (tree_attention.cuh):

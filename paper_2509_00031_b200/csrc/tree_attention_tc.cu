@@ -6,9 +6,11 @@
 // This file: many queries per key head (wide trees, grouped heads); the host sends fewer to tree_attention_keys.cu.  The queries
 // that read one key head - every draft times the g heads of the group - share row tiles of 256, so each cached byte is fetched once
 // per request, key head and 256 queries.  For 256 queries a tile of 128 keys at d_head 128 costs 2048 cycles of the tensor pipe
-// and 2048 of the exponential unit against some 2800 of an SM's share of the memory; measured 4350: a group's weights, then its
-// two products of some 700 cycles each, half hidden behind the other group's.  4 contexts of 60-120 thousand keys, 64 drafts of
-// 4 heads: 430 us.  (Two tiles of 128 queries apart: 540, the second reads the keys again long after they have left L2.)
+// and 2048 of the exponential unit against some 2800 of an SM's share of the memory; measured 5040 over a whole call (4 contexts of
+// 65536 keys), 4350 of them in a traced copy's steady state: a group's weights, then its two products of some 700 cycles each, half
+// hidden behind the other group's.  4 contexts of 60-120 thousand keys, 64 drafts of 4 heads: 434 us a call as long as the clock stays near
+// 1.9 GHz (up to a hundred calls), 500 in longer loops, which the 1 kW power limit holds at 1.6 GHz.  The other forms below were timed in
+// the short way.  (Two tiles of 128 queries apart: 540, the second reads the keys again long after they have left L2.)
 //
 // One persistent CTA per SM, 12 warps; the key tiles of all requests are dealt out in equal runs (tree_attention.cuh):
 //   warp 0      K and V tiles by TMA into a ring; warp 3: the query tile of the next piece
