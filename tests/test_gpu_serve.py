@@ -849,6 +849,101 @@ def test_rules_choice_with_ties_infinities_and_nan(zq):
     assert tok.tolist() == [0, -1, 8999, 4000]
 
 
+# ---- the largest sizes ---------------------------------------------------------------------------------------------------
+def test_plan_of_the_largest_batch(zq):
+    # 16384 requests, more rows than one pass of the grid; chains, checked in closed form
+    rng = np.random.default_rng(5)
+    batch, page, words = 16384, 16, 1
+    cached, new = rng.integers(0, 100, batch), rng.integers(0, 32, batch)
+    held, kv = -(-cached // page), cached + new
+    need = -(-kv // page) - held
+    start, first = np.concatenate([[0], np.cumsum(new)]), np.concatenate([[0], np.cumsum(need)])
+    max_pages, n_pages, rows = 9, int(held.sum() + need.sum()) + 3, int(new.sum())
+    assert rows > 148 * 1024
+    order = rng.permutation(n_pages)
+    table = np.full((batch, max_pages), -7)
+    table[np.arange(max_pages)[None] < held[:, None]] = order[:held.sum()]
+    free = order[held.sum():]
+    t = torch.from_numpy(table).to(torch.int32).cuda()
+    got = zq.zoqat_op_cache_plan(ints(cached.tolist()), ints(new.tolist()), page, n_pages, ints(free.tolist()), ints([len(free)]), t, rows + 7, mask_words=words)
+    fresh = (np.arange(max_pages)[None] >= held[:, None]) & (np.arange(max_pages)[None] < (held + need)[:, None])
+    table[fresh] = free[len(free) - 1 - np.arange(need.sum())]
+    request = np.repeat(np.arange(batch), new)
+    i = np.arange(rows) - start[request]
+    at = cached[request] + i
+    pad = lambda x, v: np.concatenate([x, np.full(7, v)])  # noqa: E731
+    want = dict(kv_len=kv, row_start=start, row_request=pad(request, -1), row_pos=pad(at, -1), slot=pad(table[request, at // page] * page + at % page, -1),
+                n_free=[len(free) - first[-1]], status=[0])
+    for n, w in want.items():
+        assert np.array_equal(got[n].cpu().numpy(), w), n
+    mask = pad((1 << (i + 1).astype(np.int64)) - 1, 0)
+    assert np.array_equal(got["tree_mask"][:, 0].cpu().numpy().view(np.uint32).astype(np.int64), mask) and np.array_equal(t.cpu().numpy(), table)
+
+
+@pytest.mark.parametrize("dtype,layout", [("bf16", "token"), ("f16", "head"), ("f32", "token")])
+def test_pages_behind_32_bits(zq, dtype, layout):
+    # a cache of more than 2^32 elements, its last pages in use: append, then attention with few and with many queries
+    page, kv, dh, heads = 16, 8, 128, 32
+    n_pages = 2 ** 32 // (page * kv * dh) + 200
+    shape = (n_pages, page, kv, dh) if layout == "token" else (n_pages, kv, page, dh)
+    k, v = [torch.empty(shape, dtype=TYPES[dtype], device="cuda") for _ in range(2)]
+    if layout == "head":
+        k, v = k.transpose(1, 2), v.transpose(1, 2)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for n in (1, 40):
+        C = 300
+        L, used = C + n, -(-(C + n) // page)
+        pages = [n_pages - 1 - 5 * i for i in range(used)]
+        qkv = torch.randn((L, (heads + 2 * kv) * dh), generator=gen, device="cuda")
+        slot = [pages[t // page] * page + t % page for t in range(L)]
+        q, err = zq.zoqat_op_cache_append(qkv, ints([0] * L), ints(slot), k, v, heads)
+        assert err.item() == 0
+        x = qkv.view(L, heads + 2 * kv, dh)
+        t = torch.arange(L, device="cuda")
+        at = torch.tensor(pages, device="cuda")[t // page]
+        assert torch.equal(k[at, t % page], x[:, heads:heads + kv].to(TYPES[dtype])) and torch.equal(v[at, t % page], x[:, heads + kv:].to(TYPES[dtype]))
+        pr = dict(dtype=dtype, q=q[C:], k=k, v=v, table=ints([pages]), kv_len=ints([L]), row_start=ints([0, n]), mask=None, rows=n, start=[0, n], new=[n], L=[L],
+                  keys=[x[:, heads:heads + kv].to(TYPES[dtype])], vals=[x[:, heads + kv:].to(TYPES[dtype])], seen=[[set(range(i + 1)) for i in range(n)]],
+                  heads=heads, kv=kv, dh=dh, scale=1.0 / math.sqrt(dh))
+        got = run_attention(zq, pr)
+        want, bound = attention_oracle(pr)
+        assert bool(((got.double() - want).abs() <= bound).all())
+
+
+def test_requests_that_share_pages(zq):
+    # two requests with the same prefix pages, each with drafts in a page of its own; and the same request twice
+    pr = attention_problem(6, "bf16", 8, 2, 128, 16, "token", [96, 96], [3, 3], "tree")
+    pr["table"][1, :6] = pr["table"][0, :6]
+    pr["keys"][1][:96], pr["vals"][1][:96] = pr["keys"][0][:96], pr["vals"][0][:96]
+    want, bound = attention_oracle(pr)
+    got = run_attention(zq, pr)
+    assert bool(((got[:6].double() - want).abs() <= bound).all())
+    pr["table"][1] = pr["table"][0]
+    pr["q"][3:6], pr["mask"][3:6] = pr["q"][:3], pr["mask"][:3]
+    got = run_attention(zq, pr)
+    assert bool(((got[:3].double() - want[:3]).abs() <= bound[:3]).all()) and bool(((got[3:6].double() - want[:3]).abs() <= bound[:3]).all())
+
+
+def test_rules_on_the_largest_batch(zq):
+    # 65535 rows of logits, 2.6e9 elements: the last rows as in a call of their own
+    rows, V, batch = 65535, 40008, 7
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    logits = torch.empty((rows, V), dtype=torch.bfloat16, device="cuda")
+    few = torch.randn((64, V), generator=gen, device="cuda").to(torch.bfloat16)
+    logits.view(-1)[: 64 * V] = few.view(-1)
+    logits[64:] = 0
+    logits[-64:] = few.flip(0)
+    allowed = torch.randint(-2 ** 31, 2 ** 31, (rows, -(-V // 32)), generator=gen, device="cuda").to(torch.int32)
+    request = (torch.arange(rows, device="cuda") % batch).to(torch.int32)
+    history = torch.randint(0, V, (batch, 500), generator=gen, device="cuda").to(torch.int32)
+    kw = dict(history=history, history_len=ints([500, 0, 3, 77, 500, 250, 1]), repetition=torch.full((batch,), 1.2, device="cuda"),
+              presence=torch.full((batch,), 0.3, device="cuda"), frequency=torch.full((batch,), 0.1, device="cuda"))
+    out, tok = zq.zoqat_op_logit_rules(logits, zq.LogitRules(row_request=request, allowed=allowed, **kw))
+    for part in (slice(0, 64), slice(rows - 64, rows)):
+        one, t1 = zq.zoqat_op_logit_rules(logits[part].clone(), zq.LogitRules(row_request=request[part].clone(), allowed=allowed[part].clone(), **kw))
+        assert torch.equal(out[part], one) and torch.equal(tok[part], t1)
+
+
 # ---- the operators together ---------------------------------------------------------------------------------------------
 MODELS = {
     "llama_w4a8": dict(arch="llama", n_layers=2, d_model=256, n_heads=2, d_ffn=512, vocab=600, w_bits=4, w_group=64, a_bits=8),
