@@ -310,15 +310,16 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                     };
                     auto weigh_all = [&](auto far) {
 #pragma unroll 1
-                        for (int q = 0; q < 4; q += 2) {
-                            load32_wait(sa);
+                        for (int q = 0; q < 4; q += 2) {         // (no load is under way where the branches and the loop turn)
                             tmem_ld32(ts + 32u * q + 32u, sb);
                             weigh(sa, q, far);
                             load32_wait(sb);
                             if (q < 2) tmem_ld32(ts + 64u, sa);
                             weigh(sb, q + 1, far);
+                            load32_wait(sa);
                         }
                     };
+                    load32_wait(sa);
                     if (__any_sync(0xffffffffu, row < nq && tree_far(m_ref))) weigh_all(FarScores<true>{});
                     else weigh_all(FarScores<false>{});
                     tmem_store_wait();

@@ -100,9 +100,9 @@ __device__ __forceinline__ void store16(uint32_t taddr, const uint32_t (&v)[16])
 }
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// A score in base 2 against its reference: fused where the reference is near, else in two roundings.  References are made from
-// rounded products, so equal ones then cancel exactly; fused, the product's rounding error stays in the exponent - at most 1/16 up
-// to 2^20, but 1 at 2^24 and 64 at 2^30, out of a weight's range.
+// A score in base 2 against its reference, in two roundings: references are made from rounded products, so equal ones cancel
+// exactly.  Fused, the product's rounding error stays in the exponent: 1 at scores of 2^24, 64 at 2^30, out of a weight's range, but at
+// most 1/16 up to 2^20, where the kernels use the fused form.  tree_far: beyond that.
 __device__ __forceinline__ float tree_shift(float s, float scale, float ref) { return __fsub_rn(__fmul_rn(s, scale), ref); }
 __device__ __forceinline__ bool tree_far(float ref) { return fabsf(ref) > 1048576.0f && ref != kNoRef; }
 
