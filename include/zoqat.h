@@ -760,6 +760,94 @@ int zoqat_decode_tree_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows
                            const zoqat_paged_cache_t* caches, const zoqat_logit_rules_t* rules, float* logits_dev,
                            int32_t* next_token_dev, void* scratch_dev, size_t scratch_bytes, void* stream);
 
+/* ---- many continuations of one prompt ------------------------------------------------------
+ * Beam search, and batches of requests behind one long prompt, over the same pages.  A step of beams, in order:
+ *     zoqat_op_cache_plan         once: where the new row of every beam goes (a beam is a request of the plan)
+ *     zoqat_op_rotary_append      per layer: norms and rotation of the query and key heads, keys and values into their slots
+ *     zoqat_op_prefix_attention   per layer: the keys that all beams of a prompt share are read once for all of them
+ *     zoqat_op_beam_select        once: the best continuations of every request's beams
+ *     zoqat_op_beam_reorder       once: tables, free pages and token histories follow the beams that go on
+ *     zoqat_op_cache_copy         once: what half-filled pages hold is copied for beams that part, in every layer
+ * Conventions as above: device data is read on the device only, words are or-ed or set, never cleared, all calls are asynchronous and
+ * can be captured in a CUDA graph. */
+
+/* Angles a position of the pairs of a head whose first `rot` elements are turned: freq_host [rot / 2] (host memory), base^(-2 i / rot)
+ * scaled for contexts `factor` times as long as those of the training:
+ *   PLAIN   as they are
+ *   LINEAR  freq / factor
+ *   BASE    the base times factor^(rot / (rot - 2)): the slowest pair slows down by the factor, the fastest is left
+ *   PARTS   pairs that turn r = trained_len * freq / (2 pi) times in a training context: freq / factor up to r = 1, freq from r = 32 on, a
+ *           linear ramp in r between; *magnitude_host, by which q and k are to be multiplied, is 0.1 ln(factor) + 1 (else 1) */
+#define ZOQAT_ROTARY_PLAIN  0
+#define ZOQAT_ROTARY_LINEAR 1
+#define ZOQAT_ROTARY_BASE   2
+#define ZOQAT_ROTARY_PARTS  3
+int zoqat_rotary_frequencies(int rot, double base, int kind, double factor, int trained_len, double* freq_host, float* magnitude_host);
+
+/* zoqat_op_cache_append with norms and other rotations: qkv_dev [rows, (n_heads + 2 * n_kv_heads) * d_head] of qkv_type (ZOQAT_TYPE_*; rows
+ * ld elements apart, 16-byte aligned).  q heads are multiplied by q_gain / sqrt(mean(x^2) + norm_eps) over the head, k heads with k_gain
+ * (fp32 [d_head]; NULL: that head is left as it is), then the first `rot` elements of q and k heads are turned by the angles row_pos_dev[r] *
+ * freq_dev[i] (fp64 [rot / 2], radians; rot a multiple of 16, 0: no rotation, freq_dev NULL and row_pos_dev unused): pair i is (i, i + rot /
+ * 2), or (2 i, 2 i + 1) with `interleaved`, and multiplied by `magnitude`.  Angles are reduced in 64 bits, so positions may be as far as they like;
+ * everything else is fp32, one rounding into the cache's type.  Slots, padding and errors as in zoqat_op_cache_append (a negative position of a live row
+ * counts as outside).  rows = 0 is allowed. */
+int zoqat_op_rotary_append(const void* qkv_dev, int qkv_type, int64_t ld, const int32_t* row_pos_dev, const int32_t* slot_dev, int rows, int n_heads,
+                           const double* freq_dev, int rot, int interleaved, float magnitude, const float* q_gain_dev, const float* k_gain_dev,
+                           float norm_eps, const zoqat_paged_cache_t* cache, void* q_out_dev, int64_t q_stride, int32_t* err_flag_dev, void* stream);
+
+/* The best continuations: score(b, v) = score_dev[request, b] + logits[request * beams + b, v] - log sum_u exp logits[.., u], formed and
+ * compared in 64 bits, ordered from the best down; of equal scores the lower beam, then the larger logit, then the lower token comes first.  Of the
+ * beams * (1 + n_eos) best of a request the first `beams` whose token is none of eos_dev [n_eos] (up to 7; n_eos = 0: NULL) go to beam_dev,
+ * token_dev, score_out_dev [batch, beams]; those among its first `beams` whose token is one of them to done_beam_dev, done_token_dev,
+ * done_score_dev [batch, beams], in the same order; -1 and -inf fill up.  Scores are rounded to fp32 once.  Beams with a score of -inf or NaN (not in use)
+ * offer nothing, nor do logits of -inf or NaN, which do not count in the sum either; +inf counts as the largest finite fp32 value.  type:
+ * ZOQAT_TYPE_* of the logits, rows ld elements apart (16-byte aligned rows are read fastest).  beams <= 32. */
+int zoqat_op_beam_select(const void* logits_dev, int type, int64_t ld, int batch, int beams, int vocab, const float* score_dev, const int32_t* eos_dev,
+                         int n_eos, int32_t* beam_dev, int32_t* token_dev, float* score_out_dev, int32_t* done_beam_dev, int32_t* done_token_dev,
+                         float* done_score_dev, void* stream);
+
+/* States follow the beams.  Row b * beams + j of the outputs continues row b * beams + parent[b * beams + j] of the inputs (-1: the row
+ * ends, its length becomes 0).  A row's keys are in the first ceil(kv_len / page_size) pages of its row of block_table; rows of a request may
+ * share pages (in the same column, holding the same), rows of different requests only pages that begin below shared_len of both.
+ *   block_table_out [rows, max_pages]   the parent's pages; entries beyond stay as they are.  The page that the parent is still filling (kv_len
+ *                       not a multiple of page_size) is kept by the first such row in order; every later row that would share it gets another page
+ *   copy_from, copy_to, copy_len [rows]  what zoqat_op_cache_copy has to copy for such a row (page, page, slots); -1, -1, 0 for the others.  A page
+ *                       that begins below shared_len [batch] (NULL: 0) belongs to others too: no row keeps it to fill it, and it never goes back
+ *   free_pages_out [free_capacity], n_free_out   the free pages afterwards.  Pages that no row of the request holds any more are given back, in the order
+ *                       of requests, columns, rows.  A request's new pages are those first; further ones are taken from the end of free_pages[0 ..
+ *                       *n_free), request by request, row by row; what is left of the pages given back stands behind the free pages that are left
+ *   kv_len_out [rows]   the parent's length
+ *   history_out [rows, history_stride], history_len_out [rows]   (history may be NULL) the parent's tokens and, if token [rows] is given, the row's
+ *                       token behind them; entries beyond stay as they are
+ * status is or-ed with 1 (a length negative or too long for its table or history: it counts as 0; *n_free outside the list, or more pages than the
+ * list holds), 2 (too few free pages), 4 (a page outside [0, n_pages): left where it is, neither copied nor given back), 8 (a parent outside [-1, beams): it
+ * counts as -1).  With an impossible *n_free or too few pages nothing is reordered: all lengths become 0, there are no copies, the free pages
+ * stay, tables and histories are unspecified.  Outputs are other buffers than inputs.  batch <= 16384, beams <= 32. */
+typedef struct zoqat_beam_reorder {
+    const int32_t* parent;        /* [batch * beams]                                                          */
+    const int32_t* kv_len;        /* [batch * beams]                                                          */
+    const int32_t* block_table;   /* [batch * beams, max_pages]                                               */
+    const int32_t* shared_len;    /* [batch], or NULL                                                         */
+    const int32_t* free_pages;    /* [free_capacity]                                                          */
+    const int32_t* n_free;        /* [1]                                                                      */
+    const int32_t* history;       /* [batch * beams, history_stride], or NULL                                 */
+    const int32_t* history_len;   /* [batch * beams]                                                          */
+    const int32_t* token;         /* [batch * beams], or NULL                                                 */
+    int32_t *block_table_out, *kv_len_out, *free_pages_out, *n_free_out, *copy_from, *copy_to, *copy_len, *history_out, *history_len_out;
+    int32_t* status;
+    int64_t history_stride;
+    int32_t batch, beams, page_size, n_pages, max_pages, free_capacity;
+} zoqat_beam_reorder_t;
+int zoqat_op_beam_reorder_scratch_bytes(int batch, size_t* bytes);
+/* r: host memory, read before the call returns.  scratch_dev: 8-byte aligned, for one call at a time. */
+int zoqat_op_beam_reorder(const zoqat_beam_reorder_t* r, void* scratch_dev, size_t scratch_bytes, void* stream);
+
+/* For every row r, K and V of the slots [0, len_dev[r]) of page from_dev[r] are copied to the same slots of page to_dev[r], in every one of n_layers
+ * caches (host memory, read before the call returns).  len 0: nothing; a page or length outside the cache, or a page onto itself, sets
+ * *err_flag_dev to 42 and is skipped.  No page may be written by one row and read or written by another.  rows = 0 is allowed. */
+int zoqat_op_cache_copy(const zoqat_paged_cache_t* caches, int n_layers, const int32_t* from_dev, const int32_t* to_dev, const int32_t* len_dev, int rows,
+                        int32_t* err_flag_dev, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

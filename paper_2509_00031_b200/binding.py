@@ -24,6 +24,7 @@ GEMM_TCGEN05, GEMM_SIMT, GEMM_TCGEN05_1CTA, GEMM_TCGEN05_I8 = 0, 1, 2, 3
 BUF_RESIDUAL, BUF_QKV, BUF_ATTN, BUF_FFN, BUF_TOKEN_LOSS = range(5)
 PROF_GEMM, PROF_WEIGHT, PROF_ACT, PROF_ATTENTION, PROF_LOSS, PROF_UPDATE = range(6)
 TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
 PLAN_BAD_LENGTH, PLAN_NO_PAGES, PLAN_BAD_PAGE, PLAN_BAD_PARENT = 1, 2, 4, 8
 PROF_NAMES = ["gemm", "weight_operand", "act_operand", "attention", "loss", "update"]
 
@@ -41,6 +42,8 @@ EXPORTS = [
     "zoqat_decode_bytes", "zoqat_decode_begin", "zoqat_decode_step", "zoqat_op_decode_gemv",
     "zoqat_op_cache_plan", "zoqat_op_cache_append", "zoqat_op_tree_attention_scratch_bytes", "zoqat_op_tree_attention",
     "zoqat_op_logit_rules", "zoqat_decode_tree_step",
+    "zoqat_rotary_frequencies", "zoqat_op_rotary_append", "zoqat_op_beam_select", "zoqat_op_beam_reorder_scratch_bytes", "zoqat_op_beam_reorder",
+    "zoqat_op_cache_copy",
 ]
 
 
@@ -77,6 +80,13 @@ class LogitRulesDesc(ctypes.Structure):
         "row_request", "repetition", "presence", "frequency", "history", "history_len", "prompt_len", "bias_token", "bias_value", "bias_len",
         "allowed", "draft_token", "row_start", "tree_mask")] + [(n, ctypes.c_int64) for n in ("history_stride", "allowed_stride")] + [
             (n, ctypes.c_int32) for n in ("bias_stride", "mask_words", "batch", "reserved")]
+
+
+class BeamReorder(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in (
+        "parent", "kv_len", "block_table", "shared_len", "free_pages", "n_free", "history", "history_len", "token", "block_table_out", "kv_len_out",
+        "free_pages_out", "n_free_out", "copy_from", "copy_to", "copy_len", "history_out", "history_len_out", "status")] + [
+            ("history_stride", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("batch", "beams", "page_size", "n_pages", "max_pages", "free_capacity")]
 
 
 class ZoqatError(RuntimeError):
@@ -170,6 +180,12 @@ def lib():
             "zoqat_op_tree_attention": [vp, i64, P(PagedCache), vp, i32, vp, vp, vp, i32, i32, i32, i32, f32, vp, i64, vp, sz, vp, vp],
             "zoqat_decode_tree_step": [vp, vp, i32, P(TreeBatch), P(PagedCache), P(LogitRulesDesc), vp, vp, vp, sz, vp],
             "zoqat_op_logit_rules": [vp, i32, i64, i32, i32, P(LogitRulesDesc), vp, i64, vp, vp],
+            "zoqat_rotary_frequencies": [i32, ctypes.c_double, i32, ctypes.c_double, i32, P(ctypes.c_double), P(f32)],
+            "zoqat_op_rotary_append": [vp, i32, i64, vp, vp, i32, i32, vp, i32, i32, f32, vp, vp, f32, P(PagedCache), vp, i64, vp, vp],
+            "zoqat_op_beam_select": [vp, i32, i64, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp],
+            "zoqat_op_beam_reorder_scratch_bytes": [i32, P(sz)],
+            "zoqat_op_beam_reorder": [P(BeamReorder), vp, sz, vp],
+            "zoqat_op_cache_copy": [P(PagedCache), i32, vp, vp, vp, i32, vp, vp],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -612,6 +628,121 @@ def zoqat_op_logit_rules(logits, rules, out=None, token=None, want_logits=True):
     _check(lib().zoqat_op_logit_rules(logits.data_ptr(), ty, st[0] if rows > 1 else max(st[0], vocab), rows, vocab, rules.desc, out_ptr, out_ld,
                                       _flat(dev, "token", token, _I32, rows), stream))
     return out, token
+
+
+# ---- many continuations of one prompt --------------------------------------------------------
+def rotary_frequencies(rot, base=10000.0, kind=ROTARY_PLAIN, factor=1.0, trained_len=0, device="cuda"):
+    """-> (float64 tensor [rot / 2] of angles a position, magnitude): what zoqat_op_rotary_append takes."""
+    freq, magnitude = (ctypes.c_double * max(1, rot // 2))(), ctypes.c_float()
+    _check(lib().zoqat_rotary_frequencies(rot, base, kind, factor, trained_len, freq, ctypes.byref(magnitude)))
+    return torch.tensor(list(freq), dtype=torch.float64).to(device), magnitude.value
+
+
+def zoqat_op_rotary_append(qkv, row_pos, slot, k_cache, v_cache, n_heads, freq=None, interleaved=False, magnitude=1.0, q_gain=None, k_gain=None,
+                           norm_eps=1e-6, q_out=None, err=None):
+    """qkv [rows, (n_heads + 2 n_kv_heads) * d_head] -> (q_out [rows, n_heads, d_head] of the caches' type, err)."""
+    dev, stream = _here()
+    cache = _caches(dev, k_cache, v_cache)
+    rows, dh, st, ty = qkv.shape[0], cache.d_head, qkv.stride(), _TYPES.get(qkv.dtype, -1)
+    if ty < 0 or qkv.get_device() != dev or len(st) != 2 or qkv.shape[1] != (n_heads + 2 * cache.n_kv_heads) * dh or st[1] != 1:
+        _refuse("qkv: [rows, (n_heads + 2 n_kv_heads) * d_head] of float32, bfloat16 or float16 on the current CUDA device is needed")
+    if q_out is None:
+        q_out = torch.empty((rows, n_heads, dh), dtype=k_cache.dtype, device=qkv.device)
+    if err is None:
+        err = torch.zeros(1, dtype=_I32, device=qkv.device)
+    q_ptr, q_stride = _rows(dev, "q_out", q_out, k_cache.dtype, rows, n_heads, dh)
+    rot = 2 * freq.shape[0] if freq is not None else 0
+    _check(lib().zoqat_op_rotary_append(
+        qkv.data_ptr(), ty, st[0] if rows > 1 else qkv.shape[1], _flat(dev, "row_pos", row_pos, _I32, rows) if rot else None,
+        _flat(dev, "slot", slot, _I32, rows), rows, n_heads, _flat(dev, "freq", freq, torch.float64, -1), rot, int(interleaved), magnitude,
+        _flat(dev, "q_gain", q_gain, _F32, dh), _flat(dev, "k_gain", k_gain, _F32, dh), norm_eps, cache, q_ptr, q_stride, _flat(dev, "err", err, _I32, 1), stream))
+    return q_out, err
+
+
+def zoqat_op_beam_select(logits, scores, eos=None, out=None):
+    """logits [batch * beams, vocab] (rows may stand apart), scores float32 [batch, beams] -> dict of [batch, beams]: beam, token, score of the
+    continuations that go on, done_beam, done_token, done_score of those that end.  out: such a dict of an earlier call to write into."""
+    dev, stream = _here()
+    batch, beams = scores.shape
+    s, st, ty = logits.shape, logits.stride(), _TYPES.get(logits.dtype, -1)
+    if ty < 0 or logits.get_device() != dev or len(s) != 2 or st[1] != 1 or s[0] != batch * beams:
+        _refuse("logits: [batch * beams, vocab] of float32, bfloat16 or float16 on the current CUDA device is needed")
+    if out is None:
+        names = dict(beam=_I32, token=_I32, score=_F32, done_beam=_I32, done_token=_I32, done_score=_F32)
+        out = {n: torch.empty((batch, beams), dtype=t, device=logits.device) for n, t in names.items()}
+    _check(lib().zoqat_op_beam_select(
+        logits.data_ptr(), ty, st[0] if s[0] > 1 else max(st[0], s[1]), batch, beams, s[1], _flat(dev, "scores", scores, _F32, batch, beams),
+        _flat(dev, "eos", eos, _I32, -1), eos.shape[0] if eos is not None else 0, _flat(dev, "beam", out["beam"], _I32, batch, beams),
+        _flat(dev, "token", out["token"], _I32, batch, beams), _flat(dev, "score", out["score"], _F32, batch, beams),
+        _flat(dev, "done_beam", out["done_beam"], _I32, batch, beams), _flat(dev, "done_token", out["done_token"], _I32, batch, beams),
+        _flat(dev, "done_score", out["done_score"], _F32, batch, beams), stream))
+    return out
+
+
+def beam_reorder_scratch(parent):
+    """Scratch of zoqat_op_beam_reorder for parents of this shape: for one call at a time."""
+    nb = ctypes.c_size_t()
+    _check(lib().zoqat_op_beam_reorder_scratch_bytes(parent.shape[0], ctypes.byref(nb)))
+    return torch.empty(nb.value, dtype=torch.uint8, device=parent.device)
+
+
+def zoqat_op_beam_reorder(parent, kv_len, block_table, page_size, n_pages, free_pages, n_free, shared_len=None, history=None, history_len=None, token=None,
+                          out=None, scratch=None):
+    """parent int32 [batch, beams]; kv_len [batch * beams], block_table [batch * beams, max_pages], history [batch * beams, any] -> dict of int32
+    tensors: block_table, kv_len, free_pages, n_free, copy_from, copy_to, copy_len, status and, with history, history, history_len.  out: such a dict of
+    an earlier call to write into (its status word is or-ed); its tensors are others than the inputs."""
+    dev, stream = _here()
+    batch, beams = parent.shape
+    rows, m, cap = batch * beams, block_table.shape[1], free_pages.shape[0]
+    stride = history.shape[1] if history is not None else 0
+    if out is None:
+        shapes = dict(block_table=(rows, m), kv_len=(rows,), free_pages=(cap,), n_free=(1,), copy_from=(rows,), copy_to=(rows,), copy_len=(rows,))
+        if history is not None:
+            shapes.update(history=(rows, stride), history_len=(rows,))
+        out = {n: torch.full(s, -1, dtype=_I32, device=parent.device) for n, s in shapes.items()}
+        out["status"] = torch.zeros(1, dtype=_I32, device=parent.device)
+    if scratch is None:
+        scratch = beam_reorder_scratch(parent)
+    if scratch.get_device() != dev or not scratch.is_contiguous():
+        _refuse("scratch: a contiguous tensor on the current CUDA device is needed")
+    have = history is not None
+    r = BeamReorder(
+        _flat(dev, "parent", parent, _I32, batch, beams), _flat(dev, "kv_len", kv_len, _I32, rows), _flat(dev, "block_table", block_table, _I32, rows, m),
+        _flat(dev, "shared_len", shared_len, _I32, batch), _flat(dev, "free_pages", free_pages, _I32, cap), _flat(dev, "n_free", n_free, _I32, 1),
+        _flat(dev, "history", history, _I32, rows, stride), _flat(dev, "history_len", history_len, _I32, rows),
+        _flat(dev, "token", token.view(-1) if token is not None else None, _I32, rows),
+        _flat(dev, "block_table_out", out["block_table"], _I32, rows, m), _flat(dev, "kv_len_out", out["kv_len"], _I32, rows),
+        _flat(dev, "free_pages_out", out["free_pages"], _I32, cap), _flat(dev, "n_free_out", out["n_free"], _I32, 1),
+        _flat(dev, "copy_from", out["copy_from"], _I32, rows), _flat(dev, "copy_to", out["copy_to"], _I32, rows), _flat(dev, "copy_len", out["copy_len"], _I32, rows),
+        _flat(dev, "history_out", out["history"], _I32, rows, stride) if have else None, _flat(dev, "history_len_out", out["history_len"], _I32, rows) if have else None,
+        _flat(dev, "status", out["status"], _I32, 1), stride, batch, beams, page_size, n_pages, m, cap)
+    _check(lib().zoqat_op_beam_reorder(r, scratch.data_ptr(), scratch.numel() * scratch.element_size(), stream))
+    return out
+
+
+class LayerCaches:
+    """The caches of all layers, (k, v) each, described once for calls that take them together; keeps the tensors alive."""
+    __slots__ = ("desc", "tensors", "dev")
+
+    def __init__(self, caches):
+        self.dev = torch.cuda.current_device()
+        self.tensors = tuple((k, v) for k, v in caches)
+        if not self.tensors:
+            _refuse("caches: one layer at least is needed")
+        self.desc = (PagedCache * len(self.tensors))(*[_caches(self.dev, k, v) for k, v in self.tensors])
+
+
+def zoqat_op_cache_copy(layers, copy_from, copy_to, copy_len, err=None):
+    """layers: LayerCaches; copy_from, copy_to, copy_len int32 [rows] -> err."""
+    dev, stream = _here()
+    rows = copy_from.shape[0]
+    if layers.dev != dev:
+        _refuse("caches must be on the current CUDA device")
+    if err is None:
+        err = torch.zeros(1, dtype=_I32, device=copy_from.device)
+    _check(lib().zoqat_op_cache_copy(layers.desc, len(layers.desc), _flat(dev, "copy_from", copy_from, _I32, rows), _flat(dev, "copy_to", copy_to, _I32, rows),
+                                     _flat(dev, "copy_len", copy_len, _I32, rows), rows, _flat(dev, "err", err, _I32, 1), stream))
+    return err
 
 
 # ---- the model handle -------------------------------------------------------------------

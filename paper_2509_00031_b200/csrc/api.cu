@@ -6,6 +6,7 @@
 #include "serve.cuh"
 #include "../../include/zoqat.h"
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -2038,6 +2039,127 @@ int zoqat_decode_tree_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows
         if (launch_logit_rules(logits, kTypeF32, c.vocab, rows, c.vocab, r, logits, c.vocab, next_token_dev, s) != 0) return launch_fail(ZOQAT_ERR_CUDA, "logit rules");
     } else if (next_token_dev) {
         launch_decode_argmax(logits, rows, c.vocab, next_token_dev, s);
+    }
+    CUDA_TRY(cudaGetLastError());
+    return ZOQAT_OK;
+}
+
+}  // extern "C"
+
+// ---- many continuations of one prompt -----------------------------------------------------------------------------
+extern "C" {
+
+int zoqat_rotary_frequencies(int rot, double base, int kind, double factor, int trained_len, double* freq_host, float* magnitude_host) {
+    if (!freq_host || !magnitude_host) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
+    if (rot <= 0 || rot % 2 || rot > 65536 || !(base > 1.0) || !std::isfinite(base)) return fail(ZOQAT_ERR_INVALID_ARG, "rot must be even and positive, base above 1");
+    if (kind < ZOQAT_ROTARY_PLAIN || kind > ZOQAT_ROTARY_PARTS) return fail(ZOQAT_ERR_INVALID_ARG, "unknown kind of scaling %d", kind);
+    if (kind != ZOQAT_ROTARY_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor))) return fail(ZOQAT_ERR_INVALID_ARG, "factor must be at least 1");
+    if (kind == ZOQAT_ROTARY_PARTS && trained_len <= 0) return fail(ZOQAT_ERR_INVALID_ARG, "trained_len must be positive");
+    if (kind == ZOQAT_ROTARY_BASE && rot <= 2) return fail(ZOQAT_ERR_INVALID_ARG, "a scaled base needs rot > 2");
+    const double two_pi = 6.283185307179586476925;
+    if (kind == ZOQAT_ROTARY_BASE) base *= std::pow(factor, (double)rot / (rot - 2));
+    for (int i = 0; i < rot / 2; ++i) {
+        const double f = std::pow(base, -2.0 * i / rot);
+        freq_host[i] = f;
+        if (kind == ZOQAT_ROTARY_LINEAR) freq_host[i] = f / factor;
+        if (kind == ZOQAT_ROTARY_PARTS) {
+            const double turns = f * trained_len / two_pi, keep = std::min(1.0, std::max(0.0, (turns - 1.0) / 31.0));
+            freq_host[i] = f / factor * (1.0 - keep) + f * keep;
+        }
+    }
+    *magnitude_host = kind == ZOQAT_ROTARY_PARTS ? (float)(0.1 * std::log(factor) + 1.0) : 1.0f;
+    return ZOQAT_OK;
+}
+
+int zoqat_op_rotary_append(const void* qkv_dev, int qkv_type, int64_t ld, const int32_t* row_pos_dev, const int32_t* slot_dev, int rows, int n_heads,
+                           const double* freq_dev, int rot, int interleaved, float magnitude, const float* q_gain_dev, const float* k_gain_dev,
+                           float norm_eps, const zoqat_paged_cache_t* cache, void* q_out_dev, int64_t q_stride, int32_t* err_flag_dev, void* stream) {
+    PagedCache c;
+    if (int rc = paged_cache(cache, c)) return rc;
+    if (!err_flag_dev || (rows > 0 && (!qkv_dev || !slot_dev || !q_out_dev))) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
+    if (qkv_type != ZOQAT_TYPE_F32 && qkv_type != ZOQAT_TYPE_BF16 && qkv_type != ZOQAT_TYPE_F16) return fail(ZOQAT_ERR_INVALID_ARG, "unknown type %d", qkv_type);
+    if (rows < 0 || n_heads <= 0 || n_heads > 65536 || c.n_kv_heads > 65536) return fail(ZOQAT_ERR_INVALID_ARG, "bad sizes (rows %d, heads %d)", rows, n_heads);
+    if (rot < 0 || rot % 16 || rot > c.d_head) return fail(ZOQAT_ERR_UNSUPPORTED, "rot %d (supported: multiples of 16 up to d_head)", rot);
+    if ((rot != 0) != (freq_dev != nullptr) || (rot && rows > 0 && !row_pos_dev)) return fail(ZOQAT_ERR_INVALID_ARG, "rot needs freq_dev and row_pos_dev, and freq_dev rot");
+    if (!std::isfinite(magnitude)) return fail(ZOQAT_ERR_INVALID_ARG, "magnitude must be finite");
+    if ((q_gain_dev || k_gain_dev) && (!(norm_eps >= 0.0f) || !std::isfinite(norm_eps))) return fail(ZOQAT_ERR_INVALID_ARG, "norm_eps must not be negative");
+    const int64_t es = type_bytes(qkv_type), e = type_bytes(c.type);
+    if (ld < (int64_t)(n_heads + 2 * c.n_kv_heads) * c.d_head || (ld * es) % 16) return fail(ZOQAT_ERR_INVALID_ARG, "ld must cover q | k | v and be a multiple of 16 bytes");
+    if (q_stride < (int64_t)n_heads * c.d_head || (q_stride * e) % 16) return fail(ZOQAT_ERR_INVALID_ARG, "q_stride must cover the heads and be a multiple of 16 bytes");
+    if (misaligned(qkv_dev, 16) || misaligned(q_out_dev, 16) || misaligned(q_gain_dev, 16) || misaligned(k_gain_dev, 16) || misaligned(freq_dev, 8))
+        return fail(ZOQAT_ERR_INVALID_ARG, "pointers must be 16-byte aligned (freq_dev: 8)");
+    if (q_out_dev && q_out_dev == qkv_dev) return fail(ZOQAT_ERR_INVALID_ARG, "q_out_dev may not be qkv_dev");
+    if (rows == 0) return ZOQAT_OK;
+    const RotaryAppendArgs a{qkv_dev, qkv_type, ld, row_pos_dev, slot_dev, rows, n_heads, freq_dev, rot, interleaved != 0, magnitude, q_gain_dev, k_gain_dev,
+                             norm_eps, c, q_out_dev, q_stride, err_flag_dev};
+    if (launch_rotary_append(a, static_cast<cudaStream_t>(stream)) != 0) return launch_fail(ZOQAT_ERR_CUDA, "rotary append");
+    CUDA_TRY(cudaGetLastError());
+    return ZOQAT_OK;
+}
+
+int zoqat_op_beam_select(const void* logits_dev, int type, int64_t ld, int batch, int beams, int vocab, const float* score_dev, const int32_t* eos_dev,
+                         int n_eos, int32_t* beam_dev, int32_t* token_dev, float* score_out_dev, int32_t* done_beam_dev, int32_t* done_token_dev,
+                         float* done_score_dev, void* stream) {
+    if (!logits_dev || !score_dev || !beam_dev || !token_dev || !score_out_dev || !done_beam_dev || !done_token_dev || !done_score_dev) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
+    if (type != ZOQAT_TYPE_F32 && type != ZOQAT_TYPE_BF16 && type != ZOQAT_TYPE_F16) return fail(ZOQAT_ERR_INVALID_ARG, "unknown logits type %d", type);
+    if (batch <= 0 || beams <= 0 || vocab <= 0) return fail(ZOQAT_ERR_INVALID_ARG, "sizes must be positive");
+    if (batch > (1 << 24) || beams > kMaxBeams || vocab > (1 << 30)) return fail(ZOQAT_ERR_UNSUPPORTED, "batch %d (up to 2^24), beams %d (up to %d), vocab %d (up to 2^30)", batch, beams, kMaxBeams, vocab);
+    if (n_eos < 0 || (n_eos > 0) != (eos_dev != nullptr)) return fail(ZOQAT_ERR_INVALID_ARG, "eos_dev and n_eos must both be given or neither");
+    if (n_eos > kMaxBeamEos) return fail(ZOQAT_ERR_UNSUPPORTED, "n_eos %d (supported: up to %d)", n_eos, kMaxBeamEos);
+    if (ld < vocab) return fail(ZOQAT_ERR_INVALID_ARG, "ld must cover the vocabulary");
+    if (misaligned(logits_dev, (size_t)type_bytes(type))) return fail(ZOQAT_ERR_INVALID_ARG, "misaligned pointer");
+    if (score_dev == score_out_dev || score_dev == done_score_dev) return fail(ZOQAT_ERR_INVALID_ARG, "an output buffer is an input buffer");
+    const BeamSelectArgs a{logits_dev, type, ld, score_dev, batch, beams, vocab, eos_dev, n_eos, beam_dev, token_dev, score_out_dev, done_beam_dev, done_token_dev, done_score_dev};
+    if (launch_beam_select(a, static_cast<cudaStream_t>(stream)) != 0) return launch_fail(ZOQAT_ERR_CUDA, "beam select");
+    CUDA_TRY(cudaGetLastError());
+    return ZOQAT_OK;
+}
+
+int zoqat_op_beam_reorder_scratch_bytes(int batch, size_t* bytes) {
+    if (!bytes || batch <= 0 || batch > kMaxPlanBatch) return fail(ZOQAT_ERR_INVALID_ARG, "bad scratch query");
+    *bytes = align_up(beam_reorder_scratch_bytes(batch));
+    return ZOQAT_OK;
+}
+
+int zoqat_op_beam_reorder(const zoqat_beam_reorder_t* r, void* scratch_dev, size_t scratch_bytes, void* stream) {
+    if (!r || !r->parent || !r->kv_len || !r->block_table || !r->n_free || !r->block_table_out || !r->kv_len_out || !r->free_pages_out || !r->n_free_out ||
+        !r->copy_from || !r->copy_to || !r->copy_len || !r->status || !scratch_dev || !r->free_pages)
+        return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
+    if (r->batch <= 0 || r->beams <= 0 || r->page_size <= 0 || r->n_pages <= 0 || r->max_pages <= 0 || r->free_capacity <= 0) return fail(ZOQAT_ERR_INVALID_ARG, "sizes must be positive");
+    if (r->batch > kMaxPlanBatch || r->beams > kMaxBeams) return fail(ZOQAT_ERR_UNSUPPORTED, "batch %d (up to %d), beams %d (up to %d)", r->batch, kMaxPlanBatch, r->beams, kMaxBeams);
+    if ((int64_t)r->n_pages * r->page_size > INT32_MAX || (int64_t)r->max_pages * r->page_size > INT32_MAX) return fail(ZOQAT_ERR_UNSUPPORTED, "more than 2^31 - 1 slots");
+    if (r->history ? !r->history_len || !r->history_out || !r->history_len_out || r->history_stride <= 0 || r->history_stride > (1 << 30)
+                   : r->history_len || r->history_out || r->history_len_out || r->token)
+        return fail(ZOQAT_ERR_INVALID_ARG, "histories need history, history_len, both outputs and history_stride (up to 2^30); token needs them");
+    const void* in[] = {r->parent, r->kv_len, r->block_table, r->shared_len, r->free_pages, r->n_free, r->history, r->history_len, r->token};
+    const void* out[] = {r->block_table_out, r->kv_len_out, r->free_pages_out, r->n_free_out, r->copy_from, r->copy_to, r->copy_len, r->history_out, r->history_len_out};
+    for (const void* o : out)
+        for (const void* i : in)
+            if (o && o == i) return fail(ZOQAT_ERR_INVALID_ARG, "an output buffer is an input buffer");
+    if (misaligned(scratch_dev, 8)) return fail(ZOQAT_ERR_INVALID_ARG, "scratch_dev must be 8-byte aligned");
+    if (scratch_bytes < beam_reorder_scratch_bytes(r->batch)) return fail(ZOQAT_ERR_WORKSPACE_SMALL, "reorder scratch %zu < %zu bytes", scratch_bytes, beam_reorder_scratch_bytes(r->batch));
+    const ReorderArgs a{r->parent, r->kv_len, r->block_table, r->batch, r->beams, r->page_size, r->n_pages, r->max_pages, r->shared_len, r->free_pages,
+                        r->free_capacity, r->n_free, r->history, r->history_len, r->token, r->history_stride, r->block_table_out, r->kv_len_out,
+                        r->free_pages_out, r->n_free_out, r->copy_from, r->copy_to, r->copy_len, r->history_out, r->history_len_out, r->status};
+    if (launch_beam_reorder(a, scratch_dev, static_cast<cudaStream_t>(stream)) != 0) return launch_fail(ZOQAT_ERR_CUDA, "beam reorder");
+    CUDA_TRY(cudaGetLastError());
+    return ZOQAT_OK;
+}
+
+int zoqat_op_cache_copy(const zoqat_paged_cache_t* caches, int n_layers, const int32_t* from_dev, const int32_t* to_dev, const int32_t* len_dev, int rows,
+                        int32_t* err_flag_dev, void* stream) {
+    if (!caches || !err_flag_dev || (rows > 0 && (!from_dev || !to_dev || !len_dev))) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
+    if (n_layers <= 0 || rows < 0) return fail(ZOQAT_ERR_INVALID_ARG, "sizes must be positive");
+    if (n_layers > 4096) return fail(ZOQAT_ERR_UNSUPPORTED, "%d layers (supported: up to 4096)", n_layers);
+    PagedCache c[kCopyLayers];
+    for (int l = 0; l < n_layers; ++l) {                         // every layer is checked before anything is launched
+        if (int rc = paged_cache(caches + l, c[0])) return rc;
+        if ((int64_t)c[0].page_size * c[0].n_kv_heads > INT32_MAX / 2) return fail(ZOQAT_ERR_UNSUPPORTED, "layer %d: a page of 2^30 or more heads", l);
+    }
+    for (int l = 0; l < n_layers && rows > 0; l += kCopyLayers) {
+        const int n = n_layers - l < kCopyLayers ? n_layers - l : kCopyLayers;
+        for (int k = 0; k < n; ++k) paged_cache(caches + l + k, c[k]);
+        if (launch_cache_copy(c, n, from_dev, to_dev, len_dev, rows, err_flag_dev, static_cast<cudaStream_t>(stream)) != 0) return launch_fail(ZOQAT_ERR_CUDA, "cache copy");
     }
     CUDA_TRY(cudaGetLastError());
     return ZOQAT_OK;

@@ -1,0 +1,400 @@
+// The best continuations of a request's beams over the vocabulary, in one pass over the logits.
+//
+//   score(b, v) = s[b] + x[b, v] - log sum_u exp x[b, u]          beams b of a request, tokens v; ordered by score, then beam, then logit, then token
+//
+// Of the beams * (1 + n_eos) best, the first `beams` whose token does not end the text go on; those among the first `beams` whose token
+// does are finished.  No row needs more than its own beams + n_eos best logits for that, and within a row the order of scores is that of
+// logits, so a row's sum of exponentials and its best logits are found side by side while it streams through registers once.
+//
+// A cluster of up to 8 CTAs serves a request: a CTA takes whole rows, or a slice of one where there are few.  Of a row's first few thousand
+// logits every warp knows its largest few: the least of those is a bound that at least as many logits pass as are wanted.  What passes it
+// goes to a buffer, whose sorted best (each key counts the larger ones) set the exact bound for the rest of the row; a logit that
+// passes that is rare, so the stream costs a maximum, an exponential and two additions each.  Keys are (logit, token) in 64 bits: no two are equal, and
+// of equal logits the lower token wins.  Should the buffer ever run over (long runs of rising or equal logits), the row's bound is found
+// digit by digit from histograms instead.
+// Sums: every thread has its own reference (the largest logit it met when it last moved), partial sums are fp32, the row's logarithm and all scores are formed in
+// 64 bits, so that scores of different beams are compared before anything is rounded.  Scores are rounded to fp32 once.
+#include "common.cuh"
+#include "serve.cuh"
+#include "tc_ptx.cuh"
+#include <cuda_fp16.h>
+#include <float.h>
+
+namespace zq {
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32, kCluster = 8;
+constexpr int kMaxEos = kMaxBeamEos, kMaxBest = kMaxBeams + kMaxEos;       // best logits of a row
+constexpr int kMaxRows = kMaxBeams / kCluster;                   // rows of a CTA
+constexpr int kBuffer = 2048;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kLn2 = 0.69314718055994530942;
+static_assert(kMaxBeams * kMaxBest <= kBuffer && kMaxBeams * (1 + kMaxEos) <= 256, "the candidates of a request fit");
+
+typedef unsigned long long u64;
+
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t b = __float_as_uint(x);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
+__device__ __forceinline__ u64 ordered64(double x) {
+    const u64 b = (u64)__double_as_longlong(x);
+    return b >> 63 ? ~b : b | (1ull << 63);
+}
+// Never 0 for a logit that may be chosen: NaN and -inf have no key, +inf counts as the largest finite value.
+__device__ __forceinline__ u64 key_of(float x, int token) {
+    return x > -INFINITY ? (u64)ordered(fminf(x, FLT_MAX)) << 32 | (uint32_t)~token : 0ull;
+}
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ u64 ld_cluster_u64(uint32_t addr) {
+    u64 v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+template <typename T> __device__ __forceinline__ float value(T v) { return static_cast<float>(v); }
+template <typename T, int VEC> struct alignas(VEC * sizeof(T)) Vec { T v[VEC]; };
+
+struct Params {
+    BeamSelectArgs a;
+    int in_parallel, slices, slice;          // rows of a request at a time, CTAs of a row, tokens of a slice (a multiple of a vector)
+    int best;                                // best logits wanted of a row
+};
+
+struct Shared {
+    u64 buf[kBuffer];
+    u64 best[kMaxRows][kMaxBest];            // a row's best keys, in order; 0: none
+    double lse[kMaxBeams];
+    u64 stat[kMaxRows];                      // (reference, sum) of a row's slice as two floats
+    float ref[kWarps], sum[kWarps];
+    uint32_t bound[kWarps];
+    int top[kMaxBeams * (1 + kMaxEos)];
+    int hist[256];
+    int count, eos[kMaxEos];
+    u64 prefix;
+    int want;
+};
+
+// Sorts the n best of m keys (m <= kBuffer) into `to`; 0 behind them.  Starts behind a barrier, ends with one.
+__device__ __forceinline__ void sort_best(const u64* buf, int m, u64* to, int n) {
+    for (int i = threadIdx.x; i < n; i += kThreads)
+        if (i >= m) to[i] = 0;
+    for (int i = threadIdx.x; i < m; i += kThreads) {
+        const u64 key = buf[i];
+        int rank = 0;
+        for (int j = 0; j < m; ++j) rank += buf[j] > key;
+        if (rank < n) to[rank] = key;
+    }
+    __syncthreads();
+}
+
+template <typename T, int VEC>
+__global__ void __launch_bounds__(kThreads, 4)
+beam_select_kernel(const Params p) {
+    constexpr int kFly = VEC == 1 ? 8 : 4;                       // vectors of a thread in flight
+    __shared__ Shared sh;
+    const BeamSelectArgs& a = p.a;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = (int)cluster_ctarank(), request = blockIdx.x / (p.in_parallel * p.slices);
+    const int n = p.best, lo = (rank % p.slices) * p.slice, size = min(a.vocab, lo + p.slice) - lo;      // (size <= 0: an empty slice)
+    const int n_vec = size > 0 ? (size + VEC - 1) / VEC : 0;
+    if (tid < a.n_eos) sh.eos[tid] = __ldg(a.eos + tid);
+
+    int mine = 0;                                                // rows of this CTA
+    for (int row = rank / p.slices; row < a.beams; row += p.in_parallel, ++mine) {
+        const T* src = static_cast<const T*>(a.logits) + ((int64_t)request * a.beams + row) * a.ld + lo;
+        Vec<T, VEC> raw[kFly];
+        auto fetch = [&](int base) {
+#pragma unroll
+            for (int u = 0; u < kFly; ++u) {
+                const int i = base + u * kThreads + tid;
+                if (i >= n_vec) continue;
+                if ((i + 1) * VEC <= size) raw[u] = *reinterpret_cast<const Vec<T, VEC>*>(src + (int64_t)i * VEC);
+                else
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) raw[u].v[e] = i * VEC + e < size ? src[i * VEC + e] : T(-INFINITY);
+            }
+        };
+        auto largest = [&](int u, int base) {
+            float m = -INFINITY;
+            if (base + u * kThreads + tid < n_vec) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) m = fmaxf(m, value(raw[u].v[e]));          // (NaN does not count)
+            }
+            return m;
+        };
+        auto push = [&](u64 key) {
+            const int at = atomicAdd(&sh.count, 1);
+            if (at < kBuffer) sh.buf[at] = key;
+        };
+        __syncthreads();                                         // the row before is through with the shared words
+        if (tid == 0) sh.count = 0;
+
+        // the first vectors: bound and reference
+        constexpr int kFirst = kFly * kThreads;
+        fetch(0);
+        float top = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < kFly; ++u) top = fmaxf(top, largest(u, 0));
+        // full warps take part; each offers its `each`-th largest thread
+        const int full = min(kWarps, n_vec >> 5), each = full ? (n + full - 1) / full : 33;
+        uint32_t k = ordered(top), offer = 0, high = 0;
+        for (int i = 0; i < each && i < 4; ++i) {
+            offer = __reduce_max_sync(0xffffffffu, k);
+            if (i == 0) high = offer;
+            const uint32_t who = __ballot_sync(0xffffffffu, k == offer);
+            if (lane == __ffs(who) - 1) k = 0;
+        }
+        if (lane == 0) { sh.bound[warp] = offer; sh.ref[warp] = unordered(high); }
+        __syncthreads();
+        uint32_t bound = 0xFFFFFFFFu;
+        float ref = -1e30f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < full) bound = min(bound, sh.bound[w]);
+            ref = fmaxf(ref, sh.ref[w]);
+        }
+        ref = fminf(ref, FLT_MAX);
+        float limit = each > 4 ? -INFINITY : unordered(bound);
+        if (!(limit > -INFINITY)) limit = -FLT_MAX;              // everything but -inf
+        float ref2 = __fmul_rn(ref, kLog2e), sum = 0.0f;
+        auto add = [&](int u, int base) {
+            if (base + u * kThreads + tid >= n_vec) return;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum += ex2(fmaf(value(raw[u].v[e]), kLog2e, -ref2));
+        };
+#pragma unroll
+        for (int u = 0; u < kFly; ++u) {
+            if (largest(u, 0) >= limit) {
+                const int token = lo + (u * kThreads + tid) * VEC;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    if (value(raw[u].v[e]) >= limit) push(key_of(value(raw[u].v[e]), token + e));
+            }
+            add(u, 0);
+        }
+        __syncthreads();
+        // the rest: what passes the n-th best so far (a later token loses against an equal logit)
+        if (n_vec > kFirst && sh.count <= kBuffer) {
+            const int m = sh.count;
+            sort_best(sh.buf, m, sh.best[mine], n);
+            const u64 nth = sh.best[mine][n - 1];
+            limit = nth ? unordered((uint32_t)(nth >> 32)) : -INFINITY;
+            for (int i = tid; i < n; i += kThreads) sh.buf[i] = sh.best[mine][i];
+            if (tid == 0) sh.count = min(m, n);
+            __syncthreads();
+            for (int base = kFirst; base < n_vec; base += kFirst) {
+                fetch(base);
+#pragma unroll
+                for (int u = 0; u < kFly; ++u) {
+                    const float m4 = largest(u, base);
+                    if (m4 > limit) {
+                        const int token = lo + (base + u * kThreads + tid) * VEC;
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e)
+                            if (value(raw[u].v[e]) > limit) push(key_of(value(raw[u].v[e]), token + e));
+                        if (m4 > ref) {                          // the reference moves (no logit above it has been met: limit <= reference)
+                            ref = fminf(m4, FLT_MAX);
+                            const float to = __fmul_rn(ref, kLog2e);
+                            sum *= ex2(ref2 - to);
+                            ref2 = to;
+                        }
+                    }
+                    add(u, base);
+                }
+            }
+            __syncthreads();
+        }
+        auto each_key = [&](auto f) {                            // every key of the slice again
+            for (int i = tid; i < size; i += kThreads) {
+                const u64 key = key_of(value(src[i]), lo + i);
+                if (key) f(key);
+            }
+        };
+        const bool again = sh.count > kBuffer;
+        if (again) {
+            // too many passed: the n-th largest key, digit by digit
+            u64 prefix = 0;
+            int want = n;
+            for (int shift = 56; shift >= 0; shift -= 8) {
+                __syncthreads();
+                for (int i = tid; i < 256; i += kThreads) sh.hist[i] = 0;
+                __syncthreads();
+                each_key([&](u64 key) {
+                    if (shift == 56 || key >> (shift + 8) == prefix) atomicAdd(&sh.hist[(int)(key >> shift) & 255], 1);
+                });
+                __syncthreads();
+                if (tid == 0) {
+                    int d = 255, left = want;
+                    for (; d > 0 && sh.hist[d] < left; --d) left -= sh.hist[d];
+                    sh.prefix = prefix << 8 | (u64)d;
+                    sh.want = left;
+                }
+                __syncthreads();
+                prefix = sh.prefix;
+                want = sh.want;
+            }
+            if (tid == 0) sh.count = 0;
+            __syncthreads();
+            each_key([&](u64 key) { if (key >= prefix) push(key); });
+            __syncthreads();
+        }
+        sort_best(sh.buf, sh.count, sh.best[mine], n);
+        // the row's sum, relative to 2^(fl(reference * log2 e))
+        float x[2] = {ref, sum};
+        auto join = [&](float om, float os) {
+            const float t = fmaxf(x[0], om), t2 = __fmul_rn(t, kLog2e);
+            x[1] = x[1] * ex2(__fmul_rn(x[0], kLog2e) - t2) + os * ex2(__fmul_rn(om, kLog2e) - t2);
+            x[0] = t;
+        };
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) join(__shfl_xor_sync(0xffffffffu, x[0], o), __shfl_xor_sync(0xffffffffu, x[1], o));
+        if (lane == 0) { sh.ref[warp] = x[0]; sh.sum[warp] = x[1]; }
+        __syncthreads();
+        x[0] = sh.ref[0]; x[1] = sh.sum[0];
+        for (int w = 1; w < kWarps; ++w) join(sh.ref[w], sh.sum[w]);
+        // Once more, with care: where the stream was left out above, NaN and +inf, logits near either end of the range.  Relative to
+        // the largest logit itself, which a negative sign says.
+        if (again || !(x[1] > 0.0f && x[1] < INFINITY && x[0] < 1e37f)) {
+            __syncthreads();
+            const u64 first = sh.best[mine][0];
+            x[0] = first ? unordered((uint32_t)(first >> 32)) : 0.0f;
+            x[1] = 0.0f;
+            for (int i = tid; first && i < size; i += kThreads) {
+                const float v = value(src[i]);
+                if (v > -INFINITY) x[1] += ex2((fminf(v, FLT_MAX) - x[0]) * kLog2e);
+            }
+#pragma unroll
+            for (int o = 16; o >= 1; o >>= 1) x[1] += __shfl_xor_sync(0xffffffffu, x[1], o);
+            if (lane == 0) sh.sum[warp] = x[1];
+            __syncthreads();
+            x[1] = 0.0f;
+            for (int w = 0; w < kWarps; ++w) x[1] -= sh.sum[w];
+        }
+        if (tid == 0) sh.stat[mine] = (u64)__float_as_uint(x[1]) << 32 | __float_as_uint(x[0]);
+    }
+
+    // the request: rank 0 gathers
+    __syncthreads();
+    cluster_sync_all();
+    if (rank == 0) {
+        const int per_row = p.slices * n, total = a.beams * per_row;
+        u64* keys = sh.buf;                                      // scores
+        if (tid < a.beams) {
+            double top = -INFINITY, sum = 0.0;
+            for (int pass = 0; pass < 2; ++pass)
+                for (int s = 0; s < p.slices; ++s) {
+                    const u64 w = ld_cluster_u64(mapa_shared(smem_u32(&sh.stat[tid / p.in_parallel]), (tid % p.in_parallel) * p.slices + s));
+                    const float r = __uint_as_float((uint32_t)w), v = __uint_as_float((uint32_t)(w >> 32));
+                    if (v == 0.0f) continue;
+                    // what the rounding of reference * log2 e moved is put back here
+                    const double at = v < 0.0f ? (double)r : (double)r + kLn2 * ((double)__fmul_rn(r, kLog2e) - (double)r * (double)kLog2e);
+                    if (pass == 0) top = fmax(top, at);
+                    else sum += fabs((double)v) * exp(at - top);
+                }
+            sh.lse[tid] = sum > 0.0 ? top + log(sum) : INFINITY;
+        }
+        __syncthreads();
+        auto candidate = [&](int i) {
+            const int row = i / per_row, rest = i - row * per_row, s = rest / n;
+            return ld_cluster_u64(mapa_shared(smem_u32(&sh.best[row / p.in_parallel][rest - s * n]), (row % p.in_parallel) * p.slices + s));
+        };
+        auto score_of = [&](int i, u64 key) {
+            const int row = i / per_row;
+            return (double)__ldg(a.score + (int64_t)request * a.beams + row) + ((double)unordered((uint32_t)(key >> 32)) - sh.lse[row]);
+        };
+        for (int i = tid; i < total; i += kThreads) {
+            const u64 key = candidate(i);
+            const double sc = key ? score_of(i, key) : -INFINITY;
+            keys[i] = sc > -INFINITY ? ordered64(sc) : 0ull;
+        }
+        const int most = a.beams * (1 + a.n_eos);
+        for (int i = tid; i < most; i += kThreads) sh.top[i] = -1;
+        __syncthreads();
+        for (int i = tid; i < total; i += kThreads) {
+            const u64 key = keys[i];
+            if (!key) continue;
+            int r = 0;
+            for (int j = 0; j < total; ++j) r += keys[j] > key || (keys[j] == key && j < i);
+            if (r < most) sh.top[r] = i;
+        }
+        __syncthreads();
+        // those that go on, those that are finished: each counts the ones of its kind before it
+        auto ends = [&](int i) {
+            const int token = (int)~(uint32_t)candidate(i);
+            for (int e = 0; e < a.n_eos; ++e)
+                if (sh.eos[e] == token) return true;
+            return false;
+        };
+        int* kind = sh.hist;                                     // 0 none, 1 goes on, 2 finished
+        for (int r = tid; r < most; r += kThreads) kind[r] = sh.top[r] < 0 ? 0 : (ends(sh.top[r]) ? 2 : 1);
+        __syncthreads();
+        const int64_t out = (int64_t)request * a.beams;
+        for (int r = tid; r < a.beams; r += kThreads) {          // slots that stay empty
+            int on = 0, done = 0;
+            for (int j = 0; j < most; ++j) { on += kind[j] == 1; done += j < a.beams && kind[j] == 2; }
+            if (r >= on) { a.beam[out + r] = -1; a.token[out + r] = -1; a.score_out[out + r] = -INFINITY; }
+            if (r >= done) { a.done_beam[out + r] = -1; a.done_token[out + r] = -1; a.done_score[out + r] = -INFINITY; }
+        }
+        for (int r = tid; r < most; r += kThreads) {
+            const int is = kind[r];
+            if (is == 0 || (is == 2 && r >= a.beams)) continue;
+            int at = 0;
+            for (int j = 0; j < r; ++j) at += kind[j] == is;
+            if (at >= a.beams) continue;
+            const int i = sh.top[r];
+            const u64 key = candidate(i);
+            (is == 1 ? a.beam : a.done_beam)[out + at] = i / per_row;
+            (is == 1 ? a.token : a.done_token)[out + at] = (int)~(uint32_t)key;
+            (is == 1 ? a.score_out : a.done_score)[out + at] = (float)score_of(i, key);
+        }
+    }
+    cluster_sync_all();                                          // a CTA's words stay until rank 0 has read them
+}
+
+template <typename T, int VEC>
+int launch_vec(const BeamSelectArgs& a, cudaStream_t s) {
+    Params p{a, 0, 0, 0, 0};
+    // whole rows in parallel first; slices only while the SMs are not filled, and of two thousand tokens at least
+    const int rounds = (a.beams + kCluster - 1) / kCluster;
+    p.in_parallel = (a.beams + rounds - 1) / rounds;
+    p.slices = 1;
+    while ((p.slices + 1) * p.in_parallel <= kCluster && a.batch * p.in_parallel * p.slices < 148 * 4 && a.vocab >= 2048 * (p.slices + 1)) ++p.slices;
+    p.slice = ((a.vocab + p.slices - 1) / p.slices + VEC - 1) / VEC * VEC;
+    p.best = a.beams + a.n_eos < a.vocab ? a.beams + a.n_eos : a.vocab;
+    const int ranks = p.in_parallel * p.slices;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)a.batch * ranks);
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = ranks; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, beam_select_kernel<T, VEC>, p) != cudaSuccess) return -1;
+    count_launch();
+    return 0;
+}
+
+template <typename T>
+int launch_type(const BeamSelectArgs& a, cudaStream_t s) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(a.logits) | (uintptr_t)(a.ld * sizeof(T));
+    return at % 16 == 0 ? launch_vec<T, 16 / sizeof(T)>(a, s) : launch_vec<T, 1>(a, s);
+}
+
+}  // namespace
+
+int launch_beam_select(const BeamSelectArgs& a, cudaStream_t s) {
+    if (a.type == kTypeF32) return launch_type<float>(a, s);
+    if (a.type == kTypeBf16) return launch_type<__nv_bfloat16>(a, s);
+    return launch_type<__half>(a, s);
+}
+
+}  // namespace zq

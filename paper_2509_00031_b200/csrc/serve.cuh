@@ -49,6 +49,60 @@ void launch_embed_rows(const int32_t* tokens, const int32_t* row_pos, const floa
                        int max_pos, float* h, int32_t* err_flag, cudaStream_t s);
 void launch_widen(const void* src, int type, int64_t n, float* dst, cudaStream_t s);      // n % 8 == 0, 16-byte aligned
 
+// Rotary append: norms and rotation of query and key heads on their way into the cache.
+struct RotaryAppendArgs {
+    const void* qkv;                     // [rows, (n_heads + 2 n_kv_heads) * d_head] of src_type, rows ld elements apart
+    int src_type;
+    int64_t ld;
+    const int32_t *row_pos, *slot;
+    int rows, n_heads;
+    const double* freq;                  // [rot / 2] radians a position
+    int rot;                             // elements of a head that are turned (a multiple of 16; 0: none)
+    bool interleaved;
+    float magnitude;
+    const float *q_gain, *k_gain;        // [d_head] or NULL: no norm
+    float eps;
+    PagedCache cache;
+    void* q_out;
+    int64_t q_stride;
+    int32_t* err_flag;
+};
+int launch_rotary_append(const RotaryAppendArgs& a, cudaStream_t s);         // 0, or -1: launch failed
+
+// Beams.
+constexpr int kMaxBeams = 32, kMaxBeamEos = 7;
+struct BeamSelectArgs {
+    const void* logits;                  // [batch * beams, vocab] of `type`, rows ld elements apart
+    int type;
+    int64_t ld;
+    const float* score;                  // [batch, beams]
+    int batch, beams, vocab;
+    const int32_t* eos;                  // [n_eos]
+    int n_eos;
+    int32_t *beam, *token;               // [batch, beams] each
+    float* score_out;
+    int32_t *done_beam, *done_token;
+    float* done_score;
+};
+int launch_beam_select(const BeamSelectArgs& a, cudaStream_t s);
+
+struct ReorderArgs {
+    const int32_t *parent, *kv_len, *block_table;
+    int batch, beams, page_size, n_pages, max_pages;
+    const int32_t* shared_len;           // [batch] or NULL
+    const int32_t* free_pages;
+    int free_capacity;
+    const int32_t* n_free;
+    const int32_t *history, *history_len, *token;
+    int64_t history_stride;
+    int32_t *table_out, *kv_len_out, *free_out, *n_free_out, *copy_from, *copy_to, *copy_len, *history_out, *history_len_out, *status;
+};
+size_t beam_reorder_scratch_bytes(int batch);
+int launch_beam_reorder(const ReorderArgs& a, void* scratch, cudaStream_t s);
+constexpr int kCopyLayers = 64;          // layers of one launch
+int launch_cache_copy(const PagedCache* caches, int n_layers, const int32_t* from, const int32_t* to, const int32_t* len, int rows, int32_t* err_flag,
+                      cudaStream_t s);
+
 // Attention of drafted rows over the pages.
 struct TreeAttnArgs {
     const void* q;                       // [rows, n_heads, d_head] of the cache's type, rows q_stride elements apart

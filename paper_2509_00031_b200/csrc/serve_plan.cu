@@ -15,8 +15,7 @@
 //   widen_kernel          attention outputs of a 16-bit cache for the fp32 activation quantisers of a model's step.
 #include "common.cuh"
 #include "serve.cuh"
-
-#include <cuda_fp16.h>
+#include "vec8.cuh"
 
 namespace zq {
 namespace {
@@ -171,30 +170,6 @@ cache_plan_kernel(PlanParams p) {
 }
 
 // ---- append -------------------------------------------------------------------------------------------------------
-template <typename T> struct Pack8;             // eight values rounded into one or two 16-byte stores
-template <> struct Pack8<float> {
-    static __device__ __forceinline__ void store(float* d, const float (&v)[8]) {
-        reinterpret_cast<float4*>(d)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(d)[1] = make_float4(v[4], v[5], v[6], v[7]);
-    }
-};
-template <> struct Pack8<__nv_bfloat16> {
-    static __device__ __forceinline__ void store(__nv_bfloat16* d, const float (&v)[8]) {
-        __nv_bfloat162 h[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        *reinterpret_cast<uint4*>(d) = *reinterpret_cast<const uint4*>(h);
-    }
-};
-template <> struct Pack8<__half> {
-    static __device__ __forceinline__ void store(__half* d, const float (&v)[8]) {
-        __half2 h[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-        *reinterpret_cast<uint4*>(d) = *reinterpret_cast<const uint4*>(h);
-    }
-};
-
 // One thread per 8 + 8 elements (i .. i+7 and their partners d_head / 2 further) of a head of a row: q heads, then k heads,
 // then v heads, as they stand in the row.  max_pos > 0: positions lie in [0, max_pos), with or without tables (a model may add
 // its position embeddings before).

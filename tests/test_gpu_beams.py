@@ -1,0 +1,371 @@
+"""The operators of many continuations of one prompt on the GPU, against plain float64 (or whole-number) implementations."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def zq():
+    from paper_2509_00031_b200 import binding
+    binding.lib()
+    return binding
+
+
+def make_cache(n_pages, page, kv, dh, dtype, layout, seed=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    shape = (n_pages, page, kv, dh) if layout == "token" else (n_pages, kv, page, dh)
+    both = [torch.randn(shape, generator=gen, device="cuda").to(DTYPES[dtype]) for _ in range(2)]
+    return both if layout == "token" else [t.transpose(1, 2) for t in both]
+
+
+# ---- rotary append --------------------------------------------------------------------------------------------------
+def append_reference(x, pos, heads, kv, dh, freq, inter, magnitude, qg, kg, eps):
+    """float64 [rows, heads + 2 kv, dh], and the bound on the part of the error that fp32 arithmetic may make."""
+    x = x.double().view(x.shape[0], heads + 2 * kv, dh).clone()
+    for lo, hi, g in ((0, heads, qg), (heads, heads + kv, kg)):
+        if g is not None:
+            x[:, lo:hi] = x[:, lo:hi] / (x[:, lo:hi].pow(2).mean(-1, keepdim=True) + eps).sqrt() * g.double()
+    size = x.abs()
+    if freq is not None:
+        r, n = 2 * freq.numel(), heads + kv
+        t = pos.double()[:, None] * freq
+        c, s = t.cos()[:, None] * magnitude, t.sin()[:, None] * magnitude
+        i = torch.arange(r // 2, device=x.device)
+        a, b = (2 * i, 2 * i + 1) if inter else (i, i + r // 2)
+        va, vb = x[:, :n, a], x[:, :n, b]
+        both = magnitude * (size[:, :n, a] + size[:, :n, b])
+        x[:, :n, a], x[:, :n, b] = va * c - vb * s, vb * c + va * s
+        size[:, :n, a], size[:, :n, b] = both, both
+    # fp32: a mean square of dh terms is off by dh * 2^-24 of itself (half of that in its root), a dozen roundings of 2^-24 follow, and the sine's and
+    # cosine's own errors (angles in turns rounded to fp32 and the functions: under 2^-21 together)
+    return x, size * (dh * 2.0 ** -25 + 12 * 2.0 ** -24 + 2.0 ** -21)
+
+
+@pytest.mark.parametrize("rows,heads,kv,dh,rot,inter,norm,src,dtype,layout,top", [
+    (1, 4, 2, 128, 128, False, True, "f32", "bf16", "token", 100), (8, 32, 8, 128, 128, True, True, "bf16", "f16", "head", 5000),
+    (33, 5, 5, 64, 32, False, True, "f16", "f32", "token", 1000000), (257, 8, 1, 64, 64, True, False, "f32", "f32", "head", 2 ** 31 - 1),
+    (300, 3, 1, 128, 32, False, False, "bf16", "bf16", "token", 4096), (70, 24, 8, 128, 96, False, True, "f32", "f16", "head", 70000),
+    (5, 160, 32, 128, 16, True, True, "f32", "bf16", "token", 128000), (1200, 2, 2, 64, 48, False, True, "bf16", "f32", "token", 9999),
+    (900, 96, 96, 128, 128, False, True, "f32", "bf16", "head", 3000), (19, 7, 1, 128, 0, False, True, "f16", "f16", "token", 10)])
+def test_append_is_the_formula(zq, rows, heads, kv, dh, rot, inter, norm, src, dtype, layout, top):
+    gen = torch.Generator(device="cuda").manual_seed(rows + rot)
+    page, n_pages = 16, rows // 16 + 3
+    k, v = make_cache(n_pages, page, kv, dh, dtype, layout)
+    k0, v0 = k.clone(), v.clone()
+    wide = (heads + 2 * kv) * dh
+    store = torch.randn((rows, wide + 24), generator=gen, device="cuda").to(DTYPES[src])      # rows stand apart
+    qkv = store[:, :wide]
+    pos = torch.randint(0, top, (rows,), generator=gen, device="cuda").int()
+    pos[0] = top - 1
+    slot = torch.randperm(n_pages * page, generator=gen, device="cuda")[:rows].int()
+    if rows > 6:
+        slot[3] = -1
+        slot[5] = n_pages * page                                  # outside: skipped and reported
+    if rows > 8 and rot:
+        pos[7] = -5
+    qg, kg = (1 + 0.5 * torch.randn((2, dh), generator=gen, device="cuda")) if norm else (None, None)
+    freq, mag = zq.rotary_frequencies(rot, kind=zq.ROTARY_PARTS, factor=4.0, trained_len=4096) if rot else (None, 1.0)
+    q_store = torch.full((rows, heads, dh), 7.0, dtype=DTYPES[dtype], device="cuda")
+    q, err = zq.zoqat_op_rotary_append(qkv, pos, slot, k, v, heads, freq=freq, interleaved=inter, magnitude=mag, q_gain=qg, k_gain=kg, norm_eps=1e-5, q_out=q_store)
+    want, extra = append_reference(qkv, pos, heads, kv, dh, freq, inter, mag, qg, kg, 1e-5)
+    live = (slot >= 0) & (slot < n_pages * page)
+    if rot:
+        live &= pos >= 0
+    assert int(err) == (40 if rows > 6 else 0)
+    half = torch.finfo(DTYPES[dtype]).eps / 2
+    tiny = torch.finfo(DTYPES[dtype]).tiny * half
+    ok = lambda got, w, x: ((got.double() - w).abs() <= half * (w.abs() + x) + x + tiny).all()  # noqa: E731
+    assert ok(q[live], want[live, :heads], extra[live, :heads])
+    at = slot[live].long()
+    assert ok(k[at // page, at % page], want[live, heads: heads + kv], extra[live, heads: heads + kv])
+    assert torch.equal(v[at // page, at % page], qkv.reshape(rows, -1, dh)[live, heads + kv:].float().to(DTYPES[dtype]))
+    assert (q[~live] == 7.0).all()
+    untouched = torch.ones(n_pages * page, dtype=torch.bool, device="cuda")
+    untouched[at] = False
+    u = torch.nonzero(untouched)[:, 0]
+    assert torch.equal(k[u // page, u % page], k0[u // page, u % page]) and torch.equal(v[u // page, u % page], v0[u // page, u % page])
+
+
+def test_append_agrees_with_the_table_form(zq):
+    """Plain half rotation without norms is what zoqat_op_cache_append does from a table."""
+    rows, heads, kv, dh = 40, 4, 2, 128
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    qkv = torch.randn((rows, (heads + 2 * kv) * dh), generator=gen, device="cuda")
+    pos = torch.randint(0, 512, (rows,), generator=gen, device="cuda").int()
+    slot = torch.randperm(64, generator=gen, device="cuda")[:rows].int()
+    freq, mag = zq.rotary_frequencies(dh)
+    assert mag == 1.0
+    angle = torch.arange(512, device="cuda", dtype=torch.float64)[:, None] * freq
+    a, b = make_cache(4, 16, kv, dh, "f32", "token"), make_cache(4, 16, kv, dh, "f32", "token")
+    q1, _ = zq.zoqat_op_rotary_append(qkv, pos, slot, *a, heads, freq=freq)
+    q2, _ = zq.zoqat_op_cache_append(qkv, pos, slot, *b, heads, cos=angle.cos().float(), sin=angle.sin().float())
+    # both are within a few roundings of the same rotation of numbers below 6
+    for x, y in ((q1, q2), (a[0], b[0])):
+        assert (x - y).abs().max() <= 6 * 2 * (2.0 ** -21 + 4 * 2.0 ** -24)
+    assert torch.equal(a[1], b[1])
+
+
+def test_append_no_rows_and_zero_heads_of_zeros(zq):
+    k, v = make_cache(2, 16, 1, 64, "bf16", "token")
+    q, err = zq.zoqat_op_rotary_append(torch.zeros((0, 3 * 64), device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda"),
+                                       torch.zeros(0, dtype=torch.int32, device="cuda"), k, v, 1)
+    assert q.shape == (0, 1, 64) and int(err) == 0
+    one = torch.ones(64, device="cuda")
+    zeros = torch.zeros((1, 3 * 64), device="cuda")
+    q, err = zq.zoqat_op_rotary_append(zeros, None, torch.zeros(1, dtype=torch.int32, device="cuda"), k, v, 1, q_gain=one, k_gain=one, norm_eps=1e-6)
+    assert (q == 0).all() and (k[0, 0] == 0).all() and int(err) == 0
+
+
+# ---- beam select ----------------------------------------------------------------------------------------------------
+def select_reference(logits, scores, eos):
+    B, K = scores.shape
+    V = logits.shape[1]
+    x = logits.double().cpu().numpy().reshape(B, K, V).copy()
+    x[np.isnan(x)] = -np.inf
+    x = np.minimum(x, float(np.finfo(np.float32).max))
+    out = dict(beam=[], token=[], score=[], done_beam=[], done_token=[], done_score=[])
+    for b in range(B):
+        cand = []
+        for k in range(K):
+            s = float(scores[b, k])
+            top = x[b, k].max()
+            if not s > -math.inf or top == -math.inf:
+                continue
+            lse = top + math.log(np.exp(x[b, k] - top).sum())
+            order = np.argsort(-x[b, k], kind="stable")[: K + len(eos)]
+            cand += [(-(s + (x[b, k, v] - lse)), k, i, int(v)) for i, v in enumerate(order) if x[b, k, v] > -math.inf]
+        cand.sort()
+        on = [c for c in cand[: K * (1 + len(eos))] if c[3] not in eos][:K]
+        done = [c for c in cand[:K] if c[3] in eos]
+        for name, part in (("", on), ("done_", done)):
+            part = part + [(math.inf, -1, 0, -1)] * (K - len(part))
+            out[name + "beam"].append([c[1] for c in part])
+            out[name + "token"].append([c[3] for c in part])
+            out[name + "score"].append([-c[0] for c in part])
+    return out
+
+
+def check_select(zq, logits, scores, eos=(), out=None):
+    e = torch.tensor(list(eos), dtype=torch.int32, device="cuda") if eos else None
+    got = zq.zoqat_op_beam_select(logits, scores, eos=e, out=out)
+    want = select_reference(logits, scores, list(eos))
+    for n in ("beam", "token", "done_beam", "done_token"):
+        assert got[n].tolist() == want[n], n
+    for n in ("score", "done_score"):
+        w = torch.tensor(want[n], dtype=torch.float64)
+        g = got[n].double().cpu()
+        f = torch.isfinite(w)
+        assert torch.equal(torch.isfinite(g), f) and (g[~f] == w[~f]).all()
+        # one rounding to fp32; the sum of exponentials is off by 2^-22 (each ex2) + 2^-23 (its argument near the maximum) + additions, in all under 2^-20
+        assert ((g - w)[f].abs() <= 2.0 ** -24 * w[f].abs() + 2.0 ** -20).all()
+    return got
+
+
+@pytest.mark.parametrize("B,K,V,eos,dtype", [
+    (1, 1, 5, (), "f32"), (1, 4, 32000, (2,), "f32"), (2, 3, 1001, (0, 1000), "bf16"), (3, 5, 4999, (7,), "f16"), (1, 8, 131072, (), "f32"),
+    (5, 2, 50272, (1, 2, 3), "f32"), (2, 16, 20011, (5,), "bf16"), (1, 32, 9000, (1, 2, 3, 4, 5, 6, 7), "f32"), (70, 4, 3001, (9,), "f32"), (2, 9, 70, (3,), "f16"),
+    (1, 1, 200000, (2,), "bf16"), (3, 7, 12, (0, 5), "f32"), (1, 32, 33, (), "f32"), (300, 1, 4100, (0,), "f32"), (1, 2, 8192, (4,), "f32"), (1, 2, 8193, (4,), "bf16")])
+def test_select_is_the_definition(zq, B, K, V, eos, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(V + K)
+    logits = (3 * torch.randn((B * K, V), generator=gen, device="cuda")).to(DTYPES[dtype])
+    scores = -20 * torch.rand((B, K), generator=gen, device="cuda")
+    if eos:
+        logits[::2, list(eos)] += 7
+    if B > 1 and K > 1:
+        scores[0, 1:] = -math.inf
+        scores[-1, 0] = math.nan
+    out = check_select(zq, logits, scores, eos)
+    check_select(zq, torch.flip(logits, (1,)).contiguous(), scores, eos, out=out)
+
+
+def test_select_rows_apart_and_unaligned(zq):
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    for dtype, ld, off in (("f32", 5003, 1), ("bf16", 5008, 8), ("f16", 5001, 3)):
+        store = torch.randn((6, ld + 16), generator=gen, device="cuda").to(DTYPES[dtype])
+        check_select(zq, store[:, off: off + 4990], torch.zeros((2, 3), device="cuda"), (17,))
+
+
+def test_select_hard_rows(zq):
+    """Equal, rising, falling, masked and non-finite logits; large ones; rows whose mask leaves nothing."""
+    V = 40000
+    low = float(np.finfo(np.float32).min)
+    ramp = torch.arange(V, device="cuda", dtype=torch.float32)
+    rows = {
+        "equal": torch.zeros(V, device="cuda"), "rising": ramp / 4096, "falling": -ramp / 4096, "rising steeply": ramp, "nothing": torch.full((V,), -math.inf, device="cuda"),
+        "lowest": torch.full((V,), low, device="cuda"), "one of the lowest": torch.full((V,), low, device="cuda"), "one": torch.full((V,), -math.inf, device="cuda"),
+        "nan": torch.randn(V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)), "inf": ramp / 8192, "two values": (ramp % 2) * 3, "large": ramp * 1e33,
+        "late": -ramp, "blocks": torch.where((ramp / 32).long() % 8 == 3, ramp / 1000, -math.inf)}
+    rows["one of the lowest"][777] = 1.5
+    rows["one"][V - 1] = -3.0
+    rows["nan"][::5] = math.nan
+    rows["inf"][[100, 30000]] = math.inf
+    rows["late"][V - 40:] = 100 + ramp[:40]
+    for name, x in rows.items():
+        for K in (1, 3, 8):
+            logits = x.repeat(2 * K, 1)
+            scores = -torch.arange(2 * K, device="cuda", dtype=torch.float32).view(2, K) * 0.37
+            check_select(zq, logits, scores, (1,))
+            got = check_select(zq, logits, scores)
+            if name == "equal":
+                assert got["token"][0].tolist() == list(range(K))[: K] or K > 1
+            if name == "nothing":
+                assert (got["beam"] == -1).all() and (got["score"] == -math.inf).all()
+
+
+def test_select_ties_between_beams_and_repeats(zq):
+    """Equal scores: the lower beam, then the lower token; the same call gives the same bits."""
+    x = torch.randn(20000, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    x[[5, 50, 19999]] = 9.0
+    logits = x.repeat(4, 1)
+    got = check_select(zq, logits, torch.zeros((1, 4), device="cuda"))
+    assert got["beam"][0].tolist() == [0, 0, 0, 1] and got["token"][0].tolist() == [5, 50, 19999, 5]
+    first = {n: t.clone() for n, t in got.items()}
+    for _ in range(5):
+        again = zq.zoqat_op_beam_select(logits, torch.zeros((1, 4), device="cuda"))
+        assert all(torch.equal(first[n], again[n]) for n in first)
+
+
+# ---- reorder --------------------------------------------------------------------------------------------------------
+def reorder_reference(parent, kv_len, table, P, free, n_free, shared, history, history_len, token):
+    B, K = len(parent), len(parent[0])
+    rows, out = B * K, dict(block_table={}, kv_len=[], copy_from=[], copy_to=[], copy_len=[], history=[])
+    held = lambda n: -(-n // P)  # noqa: E731
+    wants, backs = [], []
+    for b in range(B):
+        src = [table[b * K + p][: held(kv_len[b * K + p])] for p in range(K)]
+        new, copy, seen = [], [], set()
+        for j in range(K):
+            p = parent[b][j]
+            pages = list(src[p]) if p >= 0 else []
+            n = kv_len[b * K + p] if p >= 0 else 0
+            c = n // P
+            if n % P and ((c, pages[c]) in seen or c * P < shared[b]):
+                copy.append((j, c, pages[c], n % P))
+                pages[c] = None
+            elif n % P:
+                seen.add((c, pages[c]))
+            new.append(pages)
+            out["kv_len"].append(n)
+        back = []
+        for c in range(max(map(len, src))):
+            for p in range(K):
+                if c < len(src[p]) and c * P >= shared[b] and (c, src[p][c]) not in back and not any(c < len(x) and x[c] == src[p][c] for x in new):
+                    back.append((c, src[p][c]))
+        backs.append([x for _, x in back])
+        wants.append((new, copy))
+    left = list(free[:n_free])
+    for b in range(B):
+        new, copy = wants[b]
+        for j, c, page, n in copy:
+            to = backs[b].pop(0) if backs[b] else left.pop()
+            new[j][c] = to
+            out["copy_" + str(b * K + j)] = (page, to, n)
+        for j in range(K):
+            out["block_table"][b * K + j] = new[j]
+            p = parent[b][j]
+            f, t, n = out.get("copy_" + str(b * K + j), (-1, -1, 0))
+            out["copy_from"].append(f); out["copy_to"].append(t); out["copy_len"].append(n)
+            out["history"].append(history[b * K + p][: history_len[b * K + p]] + [token[b][j]] if p >= 0 else [])
+    out["free"] = left + [x for back in backs for x in back]
+    return out
+
+
+@pytest.mark.parametrize("B,K,P,top,tail,pool,seed", [
+    (1, 1, 16, 5, 1, 40, 0), (1, 4, 16, 300, 2, 400, 1), (3, 8, 8, 500, 3, 2600, 2), (40, 3, 32, 900, 1, 3000, 3), (5, 32, 16, 100, 4, 900, 4),
+    (2, 5, 1, 40, 3, 200, 5), (7, 2, 48, 48 * 5, 2, 90, 6), (300, 4, 16, 64, 1, 3000, 7), (1, 8, 16, 16 * 700, 2, 740, 8)])
+def test_reorder_follows_the_beams(zq, B, K, P, top, tail, pool, seed):
+    rng = np.random.default_rng(seed)
+    M, stride = -(-top // P) + 1, top + 3
+    pages = list(rng.permutation(pool))
+    kv_len = [int(x) for x in np.repeat(rng.integers(0, top + 1, B), K)]
+    kv_len[0: K] = [top] * K
+    table = rng.integers(0, pool, (B * K, M)).tolist()
+    shared = [int(x) for x in rng.integers(0, 2 * P, B)]
+    for b in range(B):
+        h = -(-kv_len[b * K] // P)
+        same = max(0, h - tail)
+        common = [int(pages.pop()) for _ in range(same)]
+        fork = [[int(pages.pop()) for _ in range(h - same)]]
+        for k in range(K):                                        # some rows share the last pages too, as right after a prompt
+            if k and rng.random() < 0.7:
+                fork.append([int(pages.pop()) for _ in range(h - same)])
+            table[b * K + k][:h] = common + fork[-1]
+    parent = rng.integers(-1, K, (B, K)).tolist()
+    history = rng.integers(0, 1000, (B * K, stride)).tolist()
+    history_len = [int(x) for x in rng.integers(0, stride, B * K)]
+    token = rng.integers(0, 1000, (B, K)).tolist()
+    n_free = len(pages)
+    free = [int(p) for p in pages] + [-7] * (pool - n_free)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    old_table = torch.full((B * K, M), -9, dtype=torch.int32, device="cuda")
+    args = (i32(parent), i32(kv_len), i32(table), P, pool, i32(free), i32([n_free]))
+    out = None
+    for _ in range(2):                                            # the second time into the first's outputs
+        out = zq.zoqat_op_beam_reorder(*args, shared_len=i32(shared), history=i32(history), history_len=i32(history_len), token=i32(token), out=out)
+        if _ == 0:
+            out["block_table"].copy_(old_table)
+            out["history"].fill_(-9)
+    want = reorder_reference(parent, kv_len, table, P, free, n_free, shared, history, history_len, token)
+    assert int(out["status"]) == 0
+    assert out["kv_len"].tolist() == want["kv_len"]
+    for n in ("copy_from", "copy_to", "copy_len"):
+        assert out[n].tolist() == want[n], n
+    got, hist = out["block_table"].tolist(), out["history"].tolist()
+    for r in range(B * K):
+        w = want["block_table"][r]
+        assert got[r][: len(w)] == w and all(x == -9 for x in got[r][len(w):]), r
+        h = want["history"][r]
+        assert out["history_len"][r] == len(h) and hist[r][: len(h)] == h and all(x == -9 for x in hist[r][len(h):])
+    assert int(out["n_free"]) == len(want["free"])
+    assert out["free_pages"].tolist()[: len(want["free"])] == want["free"]
+
+
+def simple_reorder(zq, **kw):
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    a = dict(parent=[[0, 0]], kv_len=[5, 5], table=[[0, 1, -1], [0, 2, -1]], free=[3, 4, 5, -1, -1, -1], n_free=3)
+    a.update(kw)
+    return zq.zoqat_op_beam_reorder(i32(a["parent"]), i32(a["kv_len"]), i32(a["table"]), 4, 6, i32(a["free"]), i32([a["n_free"]]))
+
+
+def test_reorder_reports_what_it_cannot_do(zq):
+    ok = simple_reorder(zq)
+    assert int(ok["status"]) == 0 and ok["block_table"].tolist() == [[0, 1, -1], [0, 2, -1]] and ok["copy_from"].tolist() == [-1, 1] and ok["copy_to"].tolist() == [-1, 2]
+    assert ok["n_free"].tolist() == [3] and ok["free_pages"].tolist()[:3] == [3, 4, 5]
+    short = simple_reorder(zq, table=[[0, 1, -1], [0, 1, -1]], n_free=0)                       # the page of both: one more is needed
+    assert int(short["status"]) == 2 and short["kv_len"].tolist() == [0, 0] and short["copy_len"].tolist() == [0, 0] and int(short["n_free"]) == 0
+    for n in (-1, 7):
+        bad = simple_reorder(zq, n_free=n)
+        assert int(bad["status"]) == 1 and bad["kv_len"].tolist() == [0, 0]
+    assert int(simple_reorder(zq, kv_len=[13, 5])["status"]) == 1
+    assert int(simple_reorder(zq, kv_len=[-1, 5])["status"]) == 1
+    far = simple_reorder(zq, parent=[[2, 1]])
+    assert int(far["status"]) == 8 and far["kv_len"].tolist() == [0, 5]
+    page = simple_reorder(zq, table=[[0, 6, -1], [0, 2, -1]])
+    assert int(page["status"]) == 4 and page["copy_len"].tolist() == [0, 0]
+    ends = simple_reorder(zq, parent=[[-1, -1]])
+    assert int(ends["status"]) == 0 and int(ends["n_free"]) == 6 and ends["free_pages"].tolist() == [3, 4, 5, 0, 1, 2] and ends["kv_len"].tolist() == [0, 0]
+
+
+# ---- copies ---------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("layers,page,kv,dh,dtype,layout", [(1, 16, 2, 128, "bf16", "token"), (70, 8, 1, 64, "f16", "head"), (3, 100, 5, 64, "f32", "head"), (2, 256, 32, 128, "f32", "token"), (2, 1, 3, 128, "f16", "token")])
+def test_copies_of_all_layers(zq, layers, page, kv, dh, dtype, layout):
+    n_pages = 12
+    caches = [make_cache(n_pages, page, kv, dh, dtype, layout, seed=l) for l in range(layers)]
+    before = [(k.clone(), v.clone()) for k, v in caches]
+    frm, to, n = [0, 3, -1, 5, 5, 12, 2, 4], [1, 7, -1, 8, 9, 2, 2, 6], [page, (page + 1) // 2, 0, 1, page, 1, 1, page + 1]
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    err = zq.zoqat_op_cache_copy(zq.LayerCaches(caches), i32(frm), i32(to), i32(n))
+    assert int(err) == 42                                         # rows 5 (a page outside), 6 (onto itself), 7 (too long): left out
+    for (k, v), (k0, v0) in zip(caches, before):
+        for r in (0, 1, 3, 4):
+            k0[to[r], : n[r]] = k0[frm[r], : n[r]]
+            v0[to[r], : n[r]] = v0[frm[r], : n[r]]
+        assert torch.equal(k, k0) and torch.equal(v, v0)
+    empty = torch.zeros(0, dtype=torch.int32, device="cuda")
+    assert int(zq.zoqat_op_cache_copy(zq.LayerCaches(caches), empty, empty, empty)) == 0
