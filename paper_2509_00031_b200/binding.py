@@ -42,7 +42,7 @@ EXPORTS = [
     "zoqat_decode_bytes", "zoqat_decode_begin", "zoqat_decode_step", "zoqat_op_decode_gemv",
     "zoqat_op_cache_plan", "zoqat_op_cache_append", "zoqat_op_tree_attention_scratch_bytes", "zoqat_op_tree_attention",
     "zoqat_op_logit_rules", "zoqat_decode_tree_step",
-    "zoqat_rotary_frequencies", "zoqat_op_rotary_append", "zoqat_op_beam_select", "zoqat_op_beam_reorder_scratch_bytes", "zoqat_op_beam_reorder",
+    "zoqat_rotary_frequencies", "zoqat_op_rotary_append", "zoqat_op_prefix_attention_scratch_bytes", "zoqat_op_prefix_attention", "zoqat_op_beam_select", "zoqat_op_beam_reorder_scratch_bytes", "zoqat_op_beam_reorder",
     "zoqat_op_cache_copy",
 ]
 
@@ -182,6 +182,8 @@ def lib():
             "zoqat_op_logit_rules": [vp, i32, i64, i32, i32, P(LogitRulesDesc), vp, i64, vp, vp],
             "zoqat_rotary_frequencies": [i32, ctypes.c_double, i32, ctypes.c_double, i32, P(ctypes.c_double), P(f32)],
             "zoqat_op_rotary_append": [vp, i32, i64, vp, vp, i32, i32, vp, i32, i32, f32, vp, vp, f32, P(PagedCache), vp, i64, vp, vp],
+            "zoqat_op_prefix_attention_scratch_bytes": [i32, i32, i32, i32, P(sz)],
+            "zoqat_op_prefix_attention": [vp, i64, P(PagedCache), vp, i32, vp, vp, vp, vp, vp, i32, vp, i32, i32, i32, i32, f32, vp, i64, vp, sz, vp, vp],
             "zoqat_op_beam_select": [vp, i32, i64, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp],
             "zoqat_op_beam_reorder_scratch_bytes": [i32, P(sz)],
             "zoqat_op_beam_reorder": [P(BeamReorder), vp, sz, vp],
@@ -657,6 +659,45 @@ def zoqat_op_rotary_append(qkv, row_pos, slot, k_cache, v_cache, n_heads, freq=N
         _flat(dev, "slot", slot, _I32, rows), rows, n_heads, _flat(dev, "freq", freq, torch.float64, -1), rot, int(interleaved), magnitude,
         _flat(dev, "q_gain", q_gain, _F32, dh), _flat(dev, "k_gain", k_gain, _F32, dh), norm_eps, cache, q_ptr, q_stride, _flat(dev, "err", err, _I32, 1), stream))
     return q_out, err
+
+
+def prefix_attention_scratch(q, k_cache, rows=None):
+    """Scratch of zoqat_op_prefix_attention for queries like q (or this many rows of them): for one call at a time."""
+    nb = ctypes.c_size_t()
+    _check(lib().zoqat_op_prefix_attention_scratch_bytes(_TYPES.get(k_cache.dtype, -1), k_cache.shape[3], q.shape[0] if rows is None else rows, q.shape[1], ctypes.byref(nb)))
+    return torch.empty(nb.value, dtype=torch.uint8, device=q.device)
+
+
+def zoqat_op_prefix_attention(q, k_cache, v_cache, block_table, kv_len, row_start, group_start, prefix_len, request_group, tree_mask=None, scale=None, out=None,
+                              scratch=None, err=None):
+    """zoqat_op_tree_attention for requests in groups (group_start int32 [groups + 1], request_group [batch]) that share their first prefix_len [groups]
+    keys -> (out, err)."""
+    dev, stream = _here()
+    cache = _caches(dev, k_cache, v_cache)
+    rows, heads, dh = q.shape
+    batch, groups = kv_len.shape[0], prefix_len.shape[0]
+    q_ptr, q_stride = _rows(dev, "q", q, k_cache.dtype, rows, heads, cache.d_head)
+    words = 0
+    if tree_mask is not None:
+        words = tree_mask.shape[1]
+        if tree_mask.shape[0] < rows:
+            _refuse("tree_mask: too few rows")
+    if out is None:
+        out = torch.empty((rows, heads, dh), dtype=q.dtype, device=q.device)
+    out_ptr, out_stride = _rows(dev, "out", out, k_cache.dtype, rows, heads, dh)
+    if scratch is None:
+        scratch = prefix_attention_scratch(q, k_cache)
+    if err is None:
+        err = torch.zeros(1, dtype=_I32, device=q.device)
+    if scratch.get_device() != dev or not scratch.is_contiguous():
+        _refuse("scratch: a contiguous tensor on the current CUDA device is needed")
+    _check(lib().zoqat_op_prefix_attention(
+        q_ptr, q_stride, cache, _flat(dev, "block_table", block_table, _I32, batch, -1), block_table.shape[1], _flat(dev, "kv_len", kv_len, _I32, batch),
+        _flat(dev, "row_start", row_start, _I32, batch + 1), _flat(dev, "group_start", group_start, _I32, groups + 1), _flat(dev, "prefix_len", prefix_len, _I32, groups),
+        _flat(dev, "request_group", request_group, _I32, batch), groups, _flat(dev, "tree_mask", tree_mask, _I32, -1, words), words, batch, rows, heads,
+        dh ** -0.5 if scale is None else scale, out_ptr, out_stride, scratch.data_ptr(), scratch.numel() * scratch.element_size(),
+        _flat(dev, "err", err, _I32, 1), stream))
+    return out, err
 
 
 def zoqat_op_beam_select(logits, scores, eos=None, out=None):

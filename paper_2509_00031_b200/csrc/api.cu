@@ -1843,6 +1843,29 @@ int attention_limits(const PagedCache& c, int max_pages, int64_t rows, int n_hea
     return ZOQAT_OK;
 }
 
+// Checks the arguments of an attention over the pages and puts them together.
+int attention_args(TreeAttnArgs& a, const void* q_dev, int64_t q_stride, const zoqat_paged_cache_t* cache, const int32_t* block_table_dev, int max_pages,
+                   const int32_t* kv_len_dev, const int32_t* row_start_dev, const uint32_t* tree_mask_dev, int mask_words, int batch, int rows, int n_heads,
+                   float scale, void* out_dev, int64_t out_stride, void* scratch_dev, int32_t* err_flag_dev) {
+    if (int rc = paged_cache(cache, a.cache)) return rc;
+    const PagedCache& c = a.cache;
+    if (!block_table_dev || !kv_len_dev || !row_start_dev || !scratch_dev || !err_flag_dev || (rows > 0 && (!q_dev || !out_dev))) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
+    if (batch <= 0 || rows < 0 || n_heads <= 0 || max_pages <= 0) return fail(ZOQAT_ERR_INVALID_ARG, "sizes must be positive");
+    if (n_heads % c.n_kv_heads) return fail(ZOQAT_ERR_INVALID_ARG, "n_kv_heads must divide n_heads");
+    if (int rc = attention_limits(c, max_pages, rows, n_heads)) return rc;
+    if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(ZOQAT_ERR_INVALID_ARG, "scale must be positive");
+    if (tree_mask_dev ? mask_words <= 0 || mask_words > (1 << 20) : rows > 0 && mask_words != 0) return fail(ZOQAT_ERR_INVALID_ARG, "tree_mask_dev and mask_words must both be given or neither");
+    const int64_t e = type_bytes(c.type), wide = (int64_t)n_heads * c.d_head;
+    if (q_stride < wide || out_stride < wide || (q_stride * e) % 16 || (out_stride * e) % 16 || q_stride >= ((int64_t)1 << 38)) return fail(ZOQAT_ERR_INVALID_ARG, "row strides must cover the heads and be multiples of 16 bytes");
+    if (misaligned(q_dev, 16) || misaligned(out_dev, 16)) return fail(ZOQAT_ERR_INVALID_ARG, "q_dev and out_dev must be 16-byte aligned");
+    if (q_dev && q_dev == out_dev) return fail(ZOQAT_ERR_INVALID_ARG, "out_dev may not be q_dev");
+    if (misaligned(scratch_dev, 256)) return fail(ZOQAT_ERR_INVALID_ARG, "scratch_dev must be 256-byte aligned");
+    a.q = q_dev; a.q_stride = q_stride; a.block_table = block_table_dev; a.max_pages = max_pages; a.kv_len = kv_len_dev; a.row_start = row_start_dev;
+    a.tree_mask = tree_mask_dev; a.mask_words = mask_words; a.batch = batch; a.rows = rows; a.n_heads = n_heads; a.scale = scale;
+    a.out = out_dev; a.out_stride = out_stride; a.scratch = static_cast<uint8_t*>(scratch_dev); a.err_flag = err_flag_dev;
+    return ZOQAT_OK;
+}
+
 int logit_rules(const zoqat_logit_rules_t* c, int rows, int vocab, LogitRules& r) {
     if (!c) return fail(ZOQAT_ERR_INVALID_ARG, "rules are NULL");
     if (rows <= 0 || rows > 65535 || vocab <= 0 || vocab > (1 << 30)) return fail(ZOQAT_ERR_UNSUPPORTED, "rows %d (1..65535), vocab %d (1..2^30)", rows, vocab);
@@ -1921,28 +1944,14 @@ int zoqat_op_tree_attention(const void* q_dev, int64_t q_stride, const zoqat_pag
                             int mask_words, int batch, int rows, int n_heads, float scale, void* out_dev, int64_t out_stride,
                             void* scratch_dev, size_t scratch_bytes, int32_t* err_flag_dev, void* stream) {
     TreeAttnArgs a{};
-    if (int rc = paged_cache(cache, a.cache)) return rc;
-    const PagedCache& c = a.cache;
-    if (!block_table_dev || !kv_len_dev || !row_start_dev || !scratch_dev || !err_flag_dev || (rows > 0 && (!q_dev || !out_dev))) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
-    if (batch <= 0 || rows < 0 || n_heads <= 0 || max_pages <= 0) return fail(ZOQAT_ERR_INVALID_ARG, "sizes must be positive");
-    if (n_heads % c.n_kv_heads) return fail(ZOQAT_ERR_INVALID_ARG, "n_kv_heads must divide n_heads");
-    if (int rc = attention_limits(c, max_pages, rows, n_heads)) return rc;
-    if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(ZOQAT_ERR_INVALID_ARG, "scale must be positive");
-    if (tree_mask_dev ? mask_words <= 0 || mask_words > (1 << 20) : rows > 0 && mask_words != 0) return fail(ZOQAT_ERR_INVALID_ARG, "tree_mask_dev and mask_words must both be given or neither");
-    const int64_t e = type_bytes(c.type), wide = (int64_t)n_heads * c.d_head;
-    if (q_stride < wide || out_stride < wide || (q_stride * e) % 16 || (out_stride * e) % 16 || q_stride >= ((int64_t)1 << 38)) return fail(ZOQAT_ERR_INVALID_ARG, "row strides must cover the heads and be multiples of 16 bytes");
-    if (misaligned(q_dev, 16) || misaligned(out_dev, 16)) return fail(ZOQAT_ERR_INVALID_ARG, "q_dev and out_dev must be 16-byte aligned");
-    if (q_dev && q_dev == out_dev) return fail(ZOQAT_ERR_INVALID_ARG, "out_dev may not be q_dev");
-    if (misaligned(scratch_dev, 256)) return fail(ZOQAT_ERR_INVALID_ARG, "scratch_dev must be 256-byte aligned");
-    const size_t need = tree_attention_scratch_bytes(c.type, c.d_head);
+    if (int rc = attention_args(a, q_dev, q_stride, cache, block_table_dev, max_pages, kv_len_dev, row_start_dev, tree_mask_dev, mask_words, batch, rows, n_heads, scale,
+                                out_dev, out_stride, scratch_dev, err_flag_dev))
+        return rc;
+    const size_t need = tree_attention_scratch_bytes(a.cache.type, a.cache.d_head);
     if (scratch_bytes < need) return fail(ZOQAT_ERR_WORKSPACE_SMALL, "attention scratch %zu < %zu bytes", scratch_bytes, need);
-    const bool tc = c.type != ZOQAT_TYPE_F32;
     if (rows == 0) return ZOQAT_OK;
-    a.q = q_dev; a.q_stride = q_stride; a.block_table = block_table_dev; a.max_pages = max_pages; a.kv_len = kv_len_dev; a.row_start = row_start_dev;
-    a.tree_mask = tree_mask_dev; a.mask_words = mask_words; a.batch = batch; a.rows = rows; a.n_heads = n_heads; a.scale = scale;
-    a.out = out_dev; a.out_stride = out_stride; a.scratch = static_cast<uint8_t*>(scratch_dev); a.err_flag = err_flag_dev;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const int rc = tc ? launch_tree_attention_tc(a, s, false) : launch_tree_attention_simt(a, s, false);
+    const int rc = a.cache.type != ZOQAT_TYPE_F32 ? launch_tree_attention_tc(a, s, false) : launch_tree_attention_simt(a, s, false);
     if (rc != ZOQAT_OK) return launch_fail(rc, "tree attention");
     CUDA_TRY(cudaGetLastError());
     return ZOQAT_OK;
@@ -2093,6 +2102,35 @@ int zoqat_op_rotary_append(const void* qkv_dev, int qkv_type, int64_t ld, const 
     const RotaryAppendArgs a{qkv_dev, qkv_type, ld, row_pos_dev, slot_dev, rows, n_heads, freq_dev, rot, interleaved != 0, magnitude, q_gain_dev, k_gain_dev,
                              norm_eps, c, q_out_dev, q_stride, err_flag_dev};
     if (launch_rotary_append(a, static_cast<cudaStream_t>(stream)) != 0) return launch_fail(ZOQAT_ERR_CUDA, "rotary append");
+    CUDA_TRY(cudaGetLastError());
+    return ZOQAT_OK;
+}
+
+int zoqat_op_prefix_attention_scratch_bytes(int type, int d_head, int rows, int n_heads, size_t* bytes) {
+    if (!bytes || (type != ZOQAT_TYPE_F32 && type != ZOQAT_TYPE_BF16 && type != ZOQAT_TYPE_F16) || rows < 0 || n_heads <= 0) return fail(ZOQAT_ERR_INVALID_ARG, "bad attention scratch query");
+    if (d_head != 64 && d_head != 128) return fail(ZOQAT_ERR_UNSUPPORTED, "head size %d (supported: 64, 128)", d_head);
+    if ((int64_t)rows * n_heads > INT32_MAX) return fail(ZOQAT_ERR_UNSUPPORTED, "sizes pass 2^31");
+    *bytes = prefix_scratch(nullptr, type, d_head, rows, n_heads).bytes;
+    return ZOQAT_OK;
+}
+
+int zoqat_op_prefix_attention(const void* q_dev, int64_t q_stride, const zoqat_paged_cache_t* cache, const int32_t* block_table_dev, int max_pages,
+                              const int32_t* kv_len_dev, const int32_t* row_start_dev, const int32_t* group_start_dev, const int32_t* prefix_len_dev,
+                              const int32_t* request_group_dev, int groups, const uint32_t* tree_mask_dev, int mask_words, int batch, int rows, int n_heads,
+                              float scale, void* out_dev, int64_t out_stride, void* scratch_dev, size_t scratch_bytes, int32_t* err_flag_dev, void* stream) {
+    PrefixAttnArgs a{};
+    if (int rc = attention_args(a.t, q_dev, q_stride, cache, block_table_dev, max_pages, kv_len_dev, row_start_dev, tree_mask_dev, mask_words, batch, rows, n_heads, scale,
+                                out_dev, out_stride, scratch_dev, err_flag_dev))
+        return rc;
+    if (!group_start_dev || !prefix_len_dev || !request_group_dev) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
+    if (groups <= 0) return fail(ZOQAT_ERR_INVALID_ARG, "groups must be positive");
+    if (groups > INT32_MAX - batch) return fail(ZOQAT_ERR_UNSUPPORTED, "sizes pass 2^31");
+    const size_t need = prefix_scratch(nullptr, a.t.cache.type, a.t.cache.d_head, rows, n_heads).bytes;
+    if (scratch_bytes < need) return fail(ZOQAT_ERR_WORKSPACE_SMALL, "attention scratch %zu < %zu bytes", scratch_bytes, need);
+    if (rows == 0) return ZOQAT_OK;
+    a.group_start = group_start_dev; a.prefix_len = prefix_len_dev; a.request_group = request_group_dev; a.groups = groups;
+    const int rc = launch_prefix_attention(a, scratch_dev, static_cast<cudaStream_t>(stream), false);
+    if (rc != ZOQAT_OK) return launch_fail(rc, "prefix attention");
     CUDA_TRY(cudaGetLastError());
     return ZOQAT_OK;
 }

@@ -121,6 +121,18 @@ struct TreeAttnArgs {
     int32_t* err_flag;
 };
 size_t tree_attention_scratch_bytes(int type, int d_head);
+
+// The same with a prefix shared by groups of requests.
+struct PrefixAttnArgs {
+    TreeAttnArgs t;                      // (t.scratch unused)
+    const int32_t *group_start, *prefix_len, *request_group;     // [groups + 1], [groups], [batch]
+    int groups;
+};
+struct PrefixScratch { uint8_t* pieces[2]; void* entries; float* partial; size_t bytes; };
+PrefixScratch prefix_scratch(void* base, int type, int d_head, int64_t rows, int n_heads);
+int launch_prefix_attention(const PrefixAttnArgs& a, void* scratch, cudaStream_t s, bool dependent);      // 0 or a ZOQAT_ERR_* code
+int launch_prefix_simt(const PrefixAttnArgs& a, const PrefixScratch& at, cudaStream_t s, bool dependent);
+int launch_prefix_tc(const PrefixAttnArgs& a, const PrefixScratch& at, int tile_shared, int tile_own, cudaStream_t s, bool dependent);
 int tree_grid();                         // CTAs of the attention kernels on the current device
 int launch_tree_attention_simt(const TreeAttnArgs& a, cudaStream_t s, bool dependent);   // fp32; 0 or a ZOQAT_ERR_* code
 int launch_tree_attention_tc(const TreeAttnArgs& a, cudaStream_t s, bool dependent);     // bf16 / fp16

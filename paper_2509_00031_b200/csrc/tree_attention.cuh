@@ -16,7 +16,21 @@
 
 namespace zq {
 
+constexpr int kSimtKeys = 32, kSimtRows = 8;             // keys of a key tile, queries of a row tile: the CUDA-core kernel's
+constexpr int kKeys = 128;                               // keys of a key tile: the tensor-core kernels'
+
+// A request's part of the work: n rows from row0 on, keys up to L, in n_rt row tiles and the key tiles [first_tile(), n_kt); n_rt * n_kt = 0: nothing to do.
+// drafts(): how many of the last keys are the rows' own.  table(b): its row of the block table.
+struct TreeRequest {
+    int n, L, row0, n_rt, n_kt;
+    __device__ __forceinline__ int first_tile() const { return 0; }
+    __device__ __forceinline__ int drafts() const { return n; }
+    __device__ __forceinline__ int table(int b) const { return b; }
+};
+
 struct TreeWork {
+    using Request = TreeRequest;
+    static constexpr bool kPrefix = false;
     const int32_t *kv_len, *row_start, *block_table;
     int batch, rows, n_kv, max_pages, page_size;
     int group;               // query heads per key head
@@ -25,8 +39,6 @@ struct TreeWork {
     int item_cost;           // work of an item besides its key tiles, in tiles
     int32_t* err_flag;
 };
-
-struct TreeRequest { int n, L, row0, n_rt, n_kt; };      // n_rt * n_kt = 0: nothing to do
 
 __device__ __forceinline__ TreeRequest tree_request(const TreeWork& w, int b) {
     TreeRequest r;
@@ -42,26 +54,108 @@ __device__ __forceinline__ TreeRequest tree_request(const TreeWork& w, int b) {
     r.n_kt = (r.L + w.key_tile - 1) / w.key_tile;
     return r;
 }
+
+// ---- a long prefix shared by groups of requests ---------------------------------------------------------------------
+// The work list then holds, for every group, one part over the keys that all of its requests share - all their rows in row tiles, every key
+// seen by all - and, for every request, one part over the keys behind them.  The border is the shared length rounded down to whole key
+// tiles: the few shared keys behind it are read by every request through its own block table, which names the same pages (a border
+// inside a tile would cost each request a tile with masked keys instead).  Both parts leave (reference, sum, output) of their rows, joined by
+// prefix_join_kernel (prefix_attention.cu).
+struct PrefixRequest : TreeRequest {
+    int kt0, row, own;                       // first tile, row of the block table, 1: the part of one request
+    __device__ __forceinline__ int first_tile() const { return kt0; }
+    __device__ __forceinline__ int drafts() const { return own ? n : 0; }
+    __device__ __forceinline__ int table(int) const { return row; }
+};
+struct PrefixWork : TreeWork {               // batch: parts in this launch
+    using Request = PrefixRequest;
+    static constexpr bool kPrefix = true;
+    const int32_t *group_start, *prefix_len, *request_group;
+    int groups, requests;
+    int first;                               // the launch's first part: 0 .. groups - 1 are groups, then come the requests
+    int2* entries;                           // [2][rows * heads]: where a query's shared (0) and own (1) pieces are
+    float* partial;                          // [2][rows * heads][d_head + 4]: output, reference, sum of parts that one CTA finished
+};
+__device__ __forceinline__ int prefix_border(const PrefixWork& w, int len) { return len / w.key_tile * w.key_tile; }
+
+// The shared part of group g; n_kt = 0: it has none, or (ok = false) its description contradicts itself.
+__device__ __forceinline__ PrefixRequest prefix_shared(const PrefixWork& w, int g, bool& ok) {
+    PrefixRequest r{};
+    const int b0 = __ldg(w.group_start + g), b1 = __ldg(w.group_start + g + 1), len = __ldg(w.prefix_len + g);
+    ok = b0 >= 0 && b1 >= b0 && b1 <= w.requests;
+    if (!ok) return r;
+    const int lo = __ldg(w.row_start + b0), n = __ldg(w.row_start + b1) - lo;
+    if (n == 0) return r;                    // (a group without rows may have any length)
+    ok = lo >= 0 && n > 0 && lo <= w.rows - n && len >= 0 && len <= (long long)w.max_pages * w.page_size;
+    if (!ok) return r;
+    r.row0 = lo; r.n = n; r.row = b0;
+    r.L = prefix_border(w, len);
+    r.n_rt = (int)(((long long)n * w.group + w.tile_rows - 1) / w.tile_rows);
+    r.n_kt = r.L / w.key_tile;
+    return r;
+}
+// The part of request b alone; its group's description is prefix_shared's to check.
+__device__ __forceinline__ PrefixRequest prefix_own(const PrefixWork& w, int b, bool& ok) {
+    PrefixRequest r{};
+    const int g = __ldg(w.request_group + b);
+    r.row0 = __ldg(w.row_start + b);
+    r.n = __ldg(w.row_start + b + 1) - r.row0;
+    r.L = __ldg(w.kv_len + b);
+    r.row = b; r.own = 1;
+    ok = r.n >= 0 && r.row0 >= 0 && r.row0 <= w.rows - r.n && r.L <= (long long)w.max_pages * w.page_size && g >= 0 && g < w.groups;
+    int len = 0;
+    if (ok) {
+        len = __ldg(w.prefix_len + g);
+        ok = __ldg(w.group_start + g) <= b && b < __ldg(w.group_start + g + 1) && (r.n == 0 || (len >= 0 && len <= r.L - r.n));
+    }
+    if (!ok || r.n == 0) { r.n = r.n_rt = r.n_kt = 0; return r; }
+    r.kt0 = prefix_border(w, len) / w.key_tile;
+    r.n_rt = (int)(((long long)r.n * w.group + w.tile_rows - 1) / w.tile_rows);
+    r.n_kt = (r.L + w.key_tile - 1) / w.key_tile;
+    return r;
+}
+__device__ __forceinline__ PrefixRequest tree_request(const PrefixWork& w, int part) {
+    bool ok;
+    part += w.first;
+    const PrefixRequest r = part < w.groups ? prefix_shared(w, part, ok) : prefix_own(w, part - w.groups, ok);
+    if (!ok) atomicExch(w.err_flag, kErrBadRequest);
+    return r;
+}
+// Where the query's piece is: whole in `partial` (y = -1), or query y of the pieces of the CTAs x & 0xFFFF .. x >> 16.
+__device__ __forceinline__ int64_t prefix_query(const PrefixWork& w, const PrefixRequest& r, int query, int h) {
+    const int token = query / w.group;
+    return ((int64_t)r.own * w.rows + r.row0 + token) * ((int64_t)w.n_kv * w.group) + (int64_t)h * w.group + (query - token * w.group);
+}
+
+// The prefix part of a work description: `parts` of them from `first` on.
+inline void prefix_work(const PrefixAttnArgs& a, const PrefixScratch& at, int first, int parts, PrefixWork& w) {
+    w.group_start = a.group_start; w.prefix_len = a.prefix_len; w.request_group = a.request_group;
+    w.groups = a.groups; w.requests = a.t.batch; w.first = first; w.batch = parts;
+    w.entries = static_cast<int2*>(at.entries); w.partial = at.partial;
+}
+
 // Position in the sequence of key tiles.  next() moves on by one tile; tiles of requests without work do not exist.
-struct TreeCursor {
-    TreeRequest r;
+template <class W> struct TreeCursorT {
+    typename W::Request r;
     int b, h, rt, kt;
-    __device__ __forceinline__ void load(const TreeWork& w) { r = tree_request(w, b); }
+    __device__ __forceinline__ void load(const W& w) { r = tree_request(w, b); }
     // first query of the row tile and how many it has
-    __device__ __forceinline__ int first_query(const TreeWork& w) const { return rt * w.tile_rows; }
-    __device__ __forceinline__ int queries(const TreeWork& w) const { return min(w.tile_rows, r.n * w.group - rt * w.tile_rows); }
-    __device__ __forceinline__ bool item_begins() const { return kt == 0; }
+    __device__ __forceinline__ int first_query(const W& w) const { return rt * w.tile_rows; }
+    __device__ __forceinline__ int queries(const W& w) const { return min(w.tile_rows, r.n * w.group - rt * w.tile_rows); }
+    __device__ __forceinline__ bool item_begins() const { return kt == r.first_tile(); }
     __device__ __forceinline__ bool item_ends() const { return kt == r.n_kt - 1; }
-    __device__ __forceinline__ void next(const TreeWork& w) {
+    __device__ __forceinline__ void next(const W& w) {
         if (++kt < r.n_kt) return;
-        kt = 0;
+        kt = r.first_tile();
         if (++rt < r.n_rt) return;
         rt = 0;
         if (++h < w.n_kv) return;
         h = 0;
         do { if (++b >= w.batch) return; load(w); } while (r.n_kt == 0);
+        kt = r.first_tile();
     }
 };
+using TreeCursor = TreeCursorT<TreeWork>;
 
 // a / b for a >= 0, b > 0; almost always in 32 bits, which is several times faster
 __device__ __forceinline__ long long tree_div(long long a, long long b) {
@@ -69,7 +163,8 @@ __device__ __forceinline__ long long tree_div(long long a, long long b) {
 }
 
 // The run of a CTA: the tiles [begin, end) of all tiles in order.  tail_cta: where the item ends that the run's end cuts in two.
-struct TreeRun { long long begin, end; int tail_cta; TreeCursor at; };
+template <class W> struct TreeRunT { long long begin, end; int tail_cta; TreeCursorT<W> at; };
+using TreeRun = TreeRunT<TreeWork>;
 
 // Run c of `total` work in `ctas` runs begins here: the first total % ctas runs have one unit more than the others.
 __device__ __forceinline__ long long tree_run_begin(long long total, int ctas, int c) {
@@ -84,16 +179,17 @@ __device__ __forceinline__ int tree_cta_of(long long x, long long total, int cta
 
 // The run of this CTA; called by all threads of the block (part: two words per warp, out: shared).  Ends with a barrier.
 // An item's units are its constant, then its tiles: a tile belongs to the CTA whose run holds its unit.
-__device__ __forceinline__ void tree_find_run(const TreeWork& w, long long* part, TreeRun* out) {
+template <class W>
+__device__ __forceinline__ void tree_find_run(const W& w, long long* part, TreeRunT<W>* out) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
     const int per = (w.batch + blockDim.x - 1) / blockDim.x;
     const int b0 = min(tid * per, w.batch), b1 = min(b0 + per, w.batch);
     long long tiles = 0, items = 0;
     for (int b = b0; b < b1; ++b) {
-        const TreeRequest r = tree_request(w, b);
+        const typename W::Request r = tree_request(w, b);
         const long long n = r.n_kt ? (long long)w.n_kv * r.n_rt : 0;
         items += n;
-        tiles += n * r.n_kt;
+        tiles += n * (r.n_kt - r.first_tile());
     }
     long long up_tiles = tiles, up_items = items;
 #pragma unroll
@@ -121,26 +217,28 @@ __device__ __forceinline__ void tree_find_run(const TreeWork& w, long long* part
         for (int e = 0; e < 2; ++e) {
             if (edge[e] < lo || edge[e] >= hi) continue;           // exactly one thread goes on (none for the end of the last run)
             long long rest = edge[e] - lo, at_tile = up_tiles - tiles, unit = lo;
-            TreeCursor c;
-            int cost = 1;
+            TreeCursorT<W> c;
+            int cost = 1, tiles_of = 0;
             for (c.b = b0; c.b < b1; ++c.b) {
                 c.load(w);
                 if (c.r.n_kt == 0) continue;
-                cost = c.r.n_kt + w.item_cost;
+                tiles_of = c.r.n_kt - c.r.first_tile();
+                cost = tiles_of + w.item_cost;
                 const long long n = (long long)w.n_kv * c.r.n_rt;
                 if (rest < n * cost) break;
                 rest -= n * cost;
                 unit += n * cost;
-                at_tile += n * c.r.n_kt;
+                at_tile += n * tiles_of;
             }
             const long long item = tree_div(rest, cost), head = tree_div(item, c.r.n_rt);
             const int off = (int)(rest - item * cost);
-            c.kt = max(0, off - w.item_cost);
+            const int in = max(0, off - w.item_cost);
+            c.kt = c.r.first_tile() + in;
             c.rt = (int)(item - head * c.r.n_rt);
             c.h = (int)head;
-            at_tile += item * c.r.n_kt + c.kt;
+            at_tile += item * tiles_of + in;
             if (e == 0) { out->begin = at_tile; out->at = c; }
-            else { out->end = at_tile; out->tail_cta = c.kt > 0 ? tree_cta_of(unit + (item + 1) * cost - 1, total, ctas) : -1; }
+            else { out->end = at_tile; out->tail_cta = in > 0 ? tree_cta_of(unit + (item + 1) * cost - 1, total, ctas) : -1; }
         }
     }
     __syncthreads();

@@ -37,7 +37,7 @@ namespace {
 
 constexpr int kKeyThreads = 384;
 
-template <int DH, int N> struct KeyCfg {
+template <int DH, int N, class W> struct KeyCfg {
     static constexpr int kTileBytes = kKeys * DH * 2;
     static constexpr int kQBytes = N * DH * 2, kPBytes = N * kKeys * 2;
     static constexpr bool kAdd = N == 16;                                   // the threads add up the weights
@@ -57,7 +57,7 @@ template <int DH, int N> struct KeyCfg {
     // ring full, ring empty; q full, q empty, s full, s empty (2 each), p full, o full (3 each), o empty, out full (2), piece done (4)
     static constexpr int kBars = 2 * kStages + 18 + 4;
     static constexpr int kOffMisc = kOffBar + kBars * 8;
-    static constexpr int kUsedBytes = kOffMisc + 32 + 192 + (int)sizeof(TreeRun);
+    static constexpr int kUsedBytes = kOffMisc + 32 + 192 + (int)sizeof(TreeRunT<W>);
     static constexpr int kSmemBytes = kUsedBytes + 1024 > 232448 ? 232448 : kUsedBytes + 1024;
     static_assert(kUsedBytes <= 232448 && kStages >= 4, "shared memory");
 };
@@ -94,10 +94,10 @@ __device__ __forceinline__ void store8(uint32_t taddr, uint32_t v) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %1, %1, %1, %1, %1, %1, %1};" ::"r"(taddr), "r"(v) : "memory");
 }
 
-template <int DH, int N, typename T>
+template <int DH, int N, typename T, class W>
 __global__ void __launch_bounds__(kKeyThreads, 1)
-tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const TcParams p) {
-    using Cfg = KeyCfg<DH, N>;
+tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const TcParamsT<W> p) {
+    using Cfg = KeyCfg<DH, N, W>;
     using Ops = HalfOps<T>;
     constexpr int NS = Cfg::kStages;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -129,7 +129,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
     volatile uint32_t* odd_piece = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 16);    // [4]: piece + 1 with a non-finite draft value
     float* const refs = reinterpret_cast<float*>(sp + Cfg::kOffRef);
     long long* part = reinterpret_cast<long long*>(sp + Cfg::kOffMisc + 32);
-    TreeRun* run = reinterpret_cast<TreeRun*>(sp + Cfg::kOffMisc + 32 + 192);
+    TreeRunT<W>* run = reinterpret_cast<TreeRunT<W>*>(sp + Cfg::kOffMisc + 32 + 192);
 
     if (tid < Cfg::kBars) {
         const int i = tid - 2 * NS;              // one barrier a thread
@@ -171,7 +171,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
     } else if (warp == 1 && n_tiles > 0) {
         // ---------------- the scores: S^T of the next tile as soon as its buffer has been read
         if (lane == 0) {
-            TreeCursor c = run->at;
+            TreeCursorT<W> c = run->at;
             uint32_t piece = 0, b = 0;
             bool ok = true;
             for (int t = 0; t < n_tiles; ++t, c.next(p.w)) {
@@ -201,7 +201,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
         // ---------------- the outputs and sums: a thread of its own, so that waiting for weights holds no scores back
         if (lane == 0) {
             constexpr uint32_t kIdescL = kIdesc | (1u << 16), kIdescO = kIdescL | (1u << 15);   // V^T (15) and P^T (16) run along their rows, not along the keys
-            TreeCursor c = run->at;
+            TreeCursorT<W> c = run->at;
             uint32_t piece = 0;
             bool ok = true, first = true;              // first: the tile opens its piece
             uint32_t g = 0, round = 0;                 // buffer of the weights: t % 3, t / 3
@@ -233,7 +233,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
         const int quarter = warp & 3, me = quarter * 32 + lane;
         const uint32_t t_lane = (uint32_t)(quarter * 32) << 16;
         float* const red = reinterpret_cast<float*>(sp + Cfg::kOffRed);
-        TreeCursor c = run->at;
+        TreeCursorT<W> c = run->at;
         bool ok = true, opens = true;
         int q0 = 0, nq = 0;
         float sums[Cfg::kAdd ? N : 1] = {};                      // of this thread's weights
@@ -261,7 +261,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
         for (int t = 0; t < n_tiles; ++t) {
             const int buf = t & 1;
             if (opens) { q0 = c.first_query(p.w); nq = c.queries(p.w); }
-            const int C = c.r.L - c.r.n;
+            const int C = c.r.L - c.r.drafts();
             const uint32_t s_at = tmem_s + (uint32_t)(buf * N) + t_lane;
             await(s_full(buf), (t >> 1) & 1u);
             uint64_t vis = ~0ull;                                // queries that see this key
@@ -291,8 +291,9 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
             }
             // Where the tile ends its piece, or holds drafts, the products of two tiles ago have run.  They belong to piece P - 2 or
             // a later one, whose first product waited for the outputs of piece P - 4: what is kept by piece modulo 4 (references, sums,
-            // marks, the phase of piece_done) may be written.  A piece ends with its item, in a tile with drafts, or with the run.
-            if (t >= 2 && (tail || t == n_tiles - 1)) await(o_full(pb == 2 ? 0 : pb + 1), (pb == 2 ? round : round - 1u) & 1u);
+            // marks, the phase of piece_done) may be written.  A piece ends with its item, in a tile with drafts (a shared prefix: in any),
+            // or with the run.
+            if (t >= 2 && (tail || (W::kPrefix && c.item_ends()) || t == n_tiles - 1)) await(o_full(pb == 2 ? 0 : pb + 1), (pb == 2 ? round : round - 1u) & 1u);
             if (tail) {
                 // (the V tile's slot was last used at least two tiles ago: only this tile's phase is open)
                 const uint32_t vseq = t == n_tiles - 1 ? 2u * n_tiles - 1u : 2u * t + 2u;
@@ -475,7 +476,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
         // ---------------- outputs of a piece: thread = column of d_head
         const int quarter = warp & 3, me = quarter * 32 + lane;
         const uint32_t t_lane = (uint32_t)(quarter * 32) << 16;
-        TreeCursor c = run->at;
+        TreeCursorT<W> c = run->at;
         bool split_front = !c.item_begins(), ok = true;
         uint32_t piece = 0;
         int kt_first = c.kt;
@@ -483,7 +484,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
         for (int t = 0; t < n_tiles && ok; ++t) {
             const bool item_ends = c.item_ends();
             if (item_ends || t == n_tiles - 1) {
-                const int q0 = c.first_query(p.w), nq = c.queries(p.w), C = c.r.L - c.r.n;
+                const int q0 = c.first_query(p.w), nq = c.queries(p.w), C = c.r.L - c.r.drafts();
                 const bool whole = item_ends && !split_front;
                 if (!wait_all(piece_done(piece & 3u), (piece >> 2) & 1u) || !wait_all(out_full(piece & 1u), (piece >> 1) & 1u)) { ok = false; break; }
                 tc_fence_after();
@@ -530,7 +531,17 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                                 if (i == e) o[i] = __float_as_uint(__uint_as_float(o[i]) + odd);
                         }
                     }
-                    if (whole) {
+                    if (W::kPrefix && whole && me < DH) {
+                        if constexpr (W::kPrefix) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                if (n0 + e < nq) {
+                                    float* to = p.w.partial + prefix_query(p.w, c.r, q0 + n0 + e, c.h) * (DH + 4);
+                                    to[me] = __uint_as_float(o[e]);
+                                    if (me == 0) { to[DH] = ref[n0 + e]; to[DH + 1] = __uint_as_float(l[e]); }
+                                }
+                        }
+                    } else if (!W::kPrefix && whole) {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             const float sum = __uint_as_float(l[e]), x = __uint_as_float(o[e]) * (1.0f / sum);
@@ -550,7 +561,10 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(o_empty(piece & 1u));
-                if (!item_ends && !split_front && me == 0) {     // begins here, goes on in the next CTAs
+                if constexpr (W::kPrefix) {
+                    if (!split_front && me < nq)
+                        p.w.entries[prefix_query(p.w, c.r, q0 + me, c.h)] = item_ends ? make_int2(0, -1) : make_int2((int)blockIdx.x | run->tail_cta << 16, me);
+                } else if (!item_ends && !split_front && me == 0) {     // begins here, goes on in the next CTAs
                     TreeTail tl{};
                     tl.last_cta = run->tail_cta;
                     tl.queries = nq; tl.row0 = c.r.row0; tl.q0 = q0; tl.h = c.h;
@@ -574,20 +588,21 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
     }
 }
 
-template <int DH, int N, typename T>
-int keys_launch(const TcParams& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int grid, cudaStream_t s, bool dependent) {
-    using Cfg = KeyCfg<DH, N>;
+template <int DH, int N, typename T, class W>
+int keys_launch(const TcParamsT<W>& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int grid, cudaStream_t s, bool dependent) {
+    using Cfg = KeyCfg<DH, N, W>;
     static DeviceOnce attr;
-    if (!attr.done([] { return allow_smem(tree_attention_keys_kernel<DH, N, T>, Cfg::kSmemBytes); })) return ZOQAT_ERR_CUDA;
-    TcParams q = p;
+    if (!attr.done([] { return allow_smem(tree_attention_keys_kernel<DH, N, T, W>, Cfg::kSmemBytes); })) return ZOQAT_ERR_CUDA;
+    TcParamsT<W> q = p;
     q.smem_bytes = Cfg::kSmemBytes;
-    return launch_kernel(tree_attention_keys_kernel<DH, N, T>, dim3(grid), dim3(kKeyThreads), Cfg::kSmemBytes, s, dependent, map_k, map_v, q) == cudaSuccess
+    return launch_kernel(tree_attention_keys_kernel<DH, N, T, W>, dim3(grid), dim3(kKeyThreads), Cfg::kSmemBytes, s, dependent, map_k, map_v, q) == cudaSuccess
                ? ZOQAT_OK : ZOQAT_ERR_CUDA;
 }
 
 }  // namespace
 
-int launch_tree_keys(const TcParams& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int dh, int type, int nq, int grid, cudaStream_t s, bool dependent) {
+template <class W>
+int launch_tree_keys(const TcParamsT<W>& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int dh, int type, int nq, int grid, cudaStream_t s, bool dependent) {
 #define ZQ_KEYS(DH, T) \
     return nq == 16 ? keys_launch<DH, 16, T>(p, map_k, map_v, grid, s, dependent) \
                     : (nq == 32 ? keys_launch<DH, 32, T>(p, map_k, map_v, grid, s, dependent) : keys_launch<DH, 64, T>(p, map_k, map_v, grid, s, dependent))
@@ -596,5 +611,7 @@ int launch_tree_keys(const TcParams& p, const CUtensorMap& map_k, const CUtensor
     ZQ_KEYS(128, __half);
 #undef ZQ_KEYS
 }
+template int launch_tree_keys(const TcParamsT<TreeWork>&, const CUtensorMap&, const CUtensorMap&, int, int, int, int, cudaStream_t, bool);
+template int launch_tree_keys(const TcParamsT<PrefixWork>&, const CUtensorMap&, const CUtensorMap&, int, int, int, int, cudaStream_t, bool);
 
 }  // namespace zq

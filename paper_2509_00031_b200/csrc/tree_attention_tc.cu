@@ -41,22 +41,22 @@ constexpr int kTcThreads = 384, kRows = 128, kTileRows = 2 * kRows;     // rows 
 
 template <bool V> struct FarScores { static constexpr bool value = V; };
 
-template <int DH> struct TcCfg {
+template <int DH, class W> struct TcCfg {
     static constexpr int kTileBytes = kKeys * DH * 2;                       // one K or V tile
     static constexpr int kStages = DH == 128 ? 5 : 8;
     static constexpr int kOffRing = kTileRows * DH * 2;                     // the query tile comes first
     static constexpr int kOffBar = kOffRing + kStages * kTileBytes;
     static constexpr int kBars = 2 * kStages + 10;
     static constexpr int kOffMisc = kOffBar + kBars * 8;                    // TMEM base, non-finite marks, run
-    static constexpr int kUsedBytes = kOffMisc + 32 + 192 + (int)sizeof(TreeRun);
+    static constexpr int kUsedBytes = kOffMisc + 32 + 192 + (int)sizeof(TreeRunT<W>);
     static constexpr int kSmemBytes = kUsedBytes + 1024 > 232448 ? 232448 : kUsedBytes + 1024;
     static_assert(kUsedBytes <= 232448, "shared memory");
 };
 
-template <int DH, typename T>
+template <int DH, typename T, class W>
 __global__ void __launch_bounds__(kTcThreads, 1)
-tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const TcParams p) {
-    using Cfg = TcCfg<DH>;
+tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const TcParamsT<W> p) {
+    using Cfg = TcCfg<DH, W>;
     using Ops = HalfOps<T>;
     constexpr int NS = Cfg::kStages;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -85,7 +85,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     // piece P - 2, and scores of piece P follow the first product of piece P - 1: whoever marks piece P, piece P - 4 has been read.
     volatile uint32_t* odd_piece = reinterpret_cast<uint32_t*>(sp + Cfg::kOffMisc + 8);
     long long* part = reinterpret_cast<long long*>(sp + Cfg::kOffMisc + 32);
-    TreeRun* run = reinterpret_cast<TreeRun*>(sp + Cfg::kOffMisc + 32 + 192);
+    TreeRunT<W>* run = reinterpret_cast<TreeRunT<W>*>(sp + Cfg::kOffMisc + 32 + 192);
 
     if (tid < Cfg::kBars) {
         const int i = tid - 2 * NS;              // one barrier a thread; a group's four warps arrive for p_full and o_empty
@@ -121,7 +121,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     } else if (warp == 1 && n_tiles > 0) {
         // ---------------- the products, of the groups by turns
         if (lane == 0) {
-            TreeCursor c = run->at;
+            TreeCursorT<W> c = run->at;
             uint32_t piece = 0, seq = 0, done[2] = {0, 0}, uses[2] = {0, 0};     // pieces, tiles of the ring; tiles and pieces of each group
             int groups = 0;
             bool ok = true, first = true, last = n_tiles == 1 || c.item_ends();  // the tile opens, closes its piece
@@ -204,7 +204,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         const int g = (warp >> 2) - 1, quarter = warp & 3, row = quarter * 32 + lane;        // row of the group
         const uint32_t t_lane = (uint32_t)(quarter * 32) << 16;
         const uint32_t ts = tmem_s + 128u * g + t_lane, to = tmem_o + 128u * g + t_lane;
-        TreeCursor c = run->at;
+        TreeCursorT<W> c = run->at;
         bool split_front = !c.item_begins(), ok = true, opens = true;
         float m_ref = kNoRef, l_run = 0.0f;
         int kt_first = 0, q0 = 0, nq = 0, tok = 0, hg = 0;       // of the group: first query, queries
@@ -221,7 +221,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 if (p.tree_mask && row < nq) mask = p.tree_mask + (size_t)(c.r.row0 + tok) * p.mask_words;
                 m_ref = kNoRef; l_run = 0.0f;
             }
-            const int C = c.r.L - c.r.n;
+            const int C = c.r.L - c.r.drafts();
             const bool warp_live = quarter * 32 < nq, item_ends = c.item_ends(), piece_ends = item_ends || t == n_tiles - 1;
             if (nq > 0) {
                 const bool tail = (c.kt + 1) * kKeys > C;
@@ -361,7 +361,14 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                                     }
                                 }
                             }
-                            if (whole && row < nq) {
+                            if (W::kPrefix && whole && row < nq) {
+                                if constexpr (W::kPrefix) {
+                                    float* po = p.w.partial + prefix_query(p.w, c.r, q0 + row, c.h) * (DH + 4) + c0;
+#pragma unroll
+                                    for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(po + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                                    if (c0 == 0) { po[DH] = m_ref; po[DH + 1] = l_run; }
+                                }
+                            } else if (whole && row < nq) {
 #pragma unroll
                                 for (int e = 0; e < 32; e += 8) {
                                     uint4 w;
@@ -375,6 +382,10 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                                 for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(po + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                             }
                         }
+                        if constexpr (W::kPrefix) {
+                            if (!split_front && row < nq)
+                                p.w.entries[prefix_query(p.w, c.r, q0 + row, c.h)] = item_ends ? make_int2(0, -1) : make_int2((int)blockIdx.x | run->tail_cta << 16, trow);
+                        }
                         if (!whole && row < nq) { slot[trow] = m_ref; slot[kTileRows + trow] = l_run; }
                     }
                     tc_fence_before();
@@ -383,7 +394,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 }
             }
             if (piece_ends) {
-                if (!item_ends && !split_front && tid == 128) {  // begins here, goes on in the next CTAs
+                if (!W::kPrefix && !item_ends && !split_front && tid == 128) {  // begins here, goes on in the next CTAs
                     TreeTail tl{};
                     tl.last_cta = run->tail_cta;
                     tl.queries = c.queries(p.w); tl.row0 = c.r.row0; tl.q0 = c.first_query(p.w); tl.h = c.h;
@@ -432,13 +443,13 @@ bool encode(CUtensorMap* map, int type, const void* base, int rank, const cuuint
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int DH, typename T>
-int tc_launch(const TcParams& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int grid, cudaStream_t s, bool dependent) {
+template <int DH, typename T, class W>
+int tc_launch(const TcParamsT<W>& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int grid, cudaStream_t s, bool dependent) {
     static DeviceOnce attr;
-    if (!attr.done([] { return allow_smem(tree_attention_tc_kernel<DH, T>, TcCfg<DH>::kSmemBytes); })) return ZOQAT_ERR_CUDA;
-    TcParams q = p;
-    q.smem_bytes = TcCfg<DH>::kSmemBytes;
-    return launch_kernel(tree_attention_tc_kernel<DH, T>, dim3(grid), dim3(kTcThreads), TcCfg<DH>::kSmemBytes, s, dependent, map_k, map_v, q) == cudaSuccess
+    if (!attr.done([] { return allow_smem(tree_attention_tc_kernel<DH, T, W>, TcCfg<DH, W>::kSmemBytes); })) return ZOQAT_ERR_CUDA;
+    TcParamsT<W> q = p;
+    q.smem_bytes = TcCfg<DH, W>::kSmemBytes;
+    return launch_kernel(tree_attention_tc_kernel<DH, T, W>, dim3(grid), dim3(kTcThreads), TcCfg<DH, W>::kSmemBytes, s, dependent, map_k, map_v, q) == cudaSuccess
                ? ZOQAT_OK : ZOQAT_ERR_CUDA;
 }
 
@@ -449,6 +460,63 @@ int combine_launch(const TcParams& p, int grid, int y, cudaStream_t s) {
 }
 
 }  // namespace
+
+// Everything but the tiles: p.w's own fields, what the kernels need to know of the cache, and the tensor maps of K and V.
+template <class W>
+static int tc_params(const TreeAttnArgs& a, TcParamsT<W>& p, CUtensorMap& map_k, CUtensorMap& map_v) {
+    static_cast<TreeWork&>(p.w) = TreeWork{a.kv_len, a.row_start, a.block_table, a.batch, a.rows, a.cache.n_kv_heads, a.max_pages, a.cache.page_size,
+                                           a.n_heads / a.cache.n_kv_heads, 0, kKeys, 4, a.err_flag};
+    p.q = a.q; p.q_stride = a.q_stride;
+    p.box_keys = a.cache.page_size < kKeys ? a.cache.page_size : kKeys;
+    p.n_pages = a.cache.n_pages; p.mask_words = a.mask_words; p.tree_mask = a.tree_mask;
+    p.scale_log2 = (float)(1.4426950408889634 * (double)a.scale);
+    p.out = a.out; p.out_stride = a.out_stride; p.scratch = a.scratch;
+    p.v = a.cache.v; p.page_stride = a.cache.page_stride; p.slot_stride = a.cache.slot_stride; p.head_stride = a.cache.head_stride;
+    // {64 columns, 8 keys, halves, groups of 8 keys, heads of all pages}
+    const int dh = a.cache.d_head;
+    const int64_t ss = a.cache.slot_stride, unit = a.cache.n_kv_heads > 1 ? a.cache.head_stride : a.cache.page_stride;
+    p.page_units = a.cache.n_pages > 1 ? (int)(a.cache.page_stride / unit) : 1;
+    const int64_t units = (int64_t)(a.cache.n_pages - 1) * p.page_units + a.cache.n_kv_heads;      // (the caller has checked that they fit)
+    p.units = (int)units;
+    p.page_shift = -1;
+    for (int b = 3; b < 31; ++b)
+        if (a.cache.page_size == 1 << b) p.page_shift = b;
+    const cuuint64_t kd[5] = {64, 8, (cuuint64_t)dh / 64, (cuuint64_t)a.cache.page_size / 8, (cuuint64_t)units};
+    const cuuint64_t kst[4] = {(cuuint64_t)ss * 2, 128, (cuuint64_t)ss * 16, (cuuint64_t)unit * 2};
+    const cuuint32_t kb[5] = {64, 8, (cuuint32_t)dh / 64, (cuuint32_t)p.box_keys / 8, 1};
+    return encode(&map_k, a.cache.type, a.cache.k, 5, kd, kst, kb) && encode(&map_v, a.cache.type, a.cache.v, 5, kd, kst, kb) ? ZOQAT_OK : ZOQAT_ERR_CUDA;
+}
+
+// queries per tile that holds `want` of them
+static int tc_tile(long long want) { return want <= 16 ? 16 : (want <= 32 ? 32 : (want <= 64 ? 64 : kRows)); }
+
+template <class W>
+static int tc_kernel(const TcParamsT<W>& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int dh, int type, int nq, int grid, cudaStream_t s, bool dependent) {
+    if (nq < kRows) return launch_tree_keys(p, map_k, map_v, dh, type, nq, grid, s, dependent);
+    if (type == kTypeBf16) return dh == 64 ? tc_launch<64, __nv_bfloat16>(p, map_k, map_v, grid, s, dependent) : tc_launch<128, __nv_bfloat16>(p, map_k, map_v, grid, s, dependent);
+    return dh == 64 ? tc_launch<64, __half>(p, map_k, map_v, grid, s, dependent) : tc_launch<128, __half>(p, map_k, map_v, grid, s, dependent);
+}
+
+int launch_prefix_tc(const PrefixAttnArgs& a, const PrefixScratch& at, int tile_shared, int tile_own, cudaStream_t s, bool dependent) {
+    const int dh = a.t.cache.d_head, type = a.t.cache.type, grid = tree_grid(), parts = a.groups + a.t.batch;
+    TcParamsT<PrefixWork> p{};
+    alignas(64) CUtensorMap map_k, map_v;
+    if (int rc = tc_params(a.t, p, map_k, map_v)) return rc;
+    const int nq = tc_tile(tile_shared), nq_own = tc_tile(tile_own);
+    const bool one = nq == nq_own;
+    p.w.tile_rows = nq < kRows ? nq : kTileRows;
+    prefix_work(a, at, 0, one ? parts : a.groups, p.w);
+    p.scratch = at.pieces[0];
+    if (int rc = tc_kernel(p, map_k, map_v, dh, type, nq, grid, s, dependent)) return rc;
+    count_launch();
+    if (one) return ZOQAT_OK;
+    p.w.tile_rows = nq_own < kRows ? nq_own : kTileRows;
+    prefix_work(a, at, a.groups, a.t.batch, p.w);
+    p.scratch = at.pieces[1];
+    const int rc = tc_kernel(p, map_k, map_v, dh, type, nq_own, grid, s, true);
+    if (rc == ZOQAT_OK) count_launch();
+    return rc;
+}
 
 int launch_tree_attention_tc(const TreeAttnArgs& a, cudaStream_t s, bool dependent) {
     const int dh = a.cache.d_head, type = a.cache.type;
@@ -462,34 +530,13 @@ int launch_tree_attention_tc(const TreeAttnArgs& a, cudaStream_t s, bool depende
     // large, hence the margin of a half for batches whose trees differ.
     const long long drafts = (long long)a.rows * group;
     const long long want = a.rows <= a.batch ? group : (3 * drafts + 2 * a.batch - 1) / (2 * a.batch);     // 1.5 x the average
-    const int nq = want <= 16 ? 16 : (want <= 32 ? 32 : (want <= 64 ? 64 : kRows));
-    p.w = TreeWork{a.kv_len, a.row_start, a.block_table, a.batch, a.rows, a.cache.n_kv_heads, a.max_pages, a.cache.page_size,
-                   group, nq < kRows ? nq : kTileRows, kKeys, 4, a.err_flag};
-    p.q = a.q; p.q_stride = a.q_stride;
-    p.box_keys = a.cache.page_size < kKeys ? a.cache.page_size : kKeys;
-    p.n_pages = a.cache.n_pages; p.mask_words = a.mask_words; p.tree_mask = a.tree_mask;
-    p.scale_log2 = (float)(1.4426950408889634 * (double)a.scale);
-    p.out = a.out; p.out_stride = a.out_stride; p.scratch = a.scratch;
-    p.v = a.cache.v; p.page_stride = a.cache.page_stride; p.slot_stride = a.cache.slot_stride; p.head_stride = a.cache.head_stride;
+    const int nq = tc_tile(want);
     alignas(64) CUtensorMap map_k, map_v;
-    // {64 columns, 8 keys, halves, groups of 8 keys, heads of all pages}
-    const int64_t ss = a.cache.slot_stride, unit = a.cache.n_kv_heads > 1 ? a.cache.head_stride : a.cache.page_stride;
-    p.page_units = a.cache.n_pages > 1 ? (int)(a.cache.page_stride / unit) : 1;
-    const int64_t units = (int64_t)(a.cache.n_pages - 1) * p.page_units + a.cache.n_kv_heads;      // (the caller has checked that they fit)
-    p.units = (int)units;
-    p.page_shift = -1;
-    for (int b = 3; b < 31; ++b)
-        if (a.cache.page_size == 1 << b) p.page_shift = b;
-    const cuuint64_t kd[5] = {64, 8, (cuuint64_t)dh / 64, (cuuint64_t)a.cache.page_size / 8, (cuuint64_t)units};
-    const cuuint64_t kst[4] = {(cuuint64_t)ss * 2, 128, (cuuint64_t)ss * 16, (cuuint64_t)unit * 2};
-    const cuuint32_t kb[5] = {64, 8, (cuuint32_t)dh / 64, (cuuint32_t)p.box_keys / 8, 1};
-    if (!encode(&map_k, type, a.cache.k, 5, kd, kst, kb) || !encode(&map_v, type, a.cache.v, 5, kd, kst, kb)) return ZOQAT_ERR_CUDA;
+    if (int rc = tc_params(a, p, map_k, map_v)) return rc;
+    p.w.tile_rows = nq < kRows ? nq : kTileRows;
     const int grid = tree_grid();
     const int y = want < 2 ? 1 : (want < 32 ? (int)(want + 1) / 2 : 16);      // CTAs that share the queries of a split item
-    int rc;
-    if (nq < kRows) rc = launch_tree_keys(p, map_k, map_v, dh, type, nq, grid, s, dependent);
-    else if (type == kTypeBf16) rc = dh == 64 ? tc_launch<64, __nv_bfloat16>(p, map_k, map_v, grid, s, dependent) : tc_launch<128, __nv_bfloat16>(p, map_k, map_v, grid, s, dependent);
-    else rc = dh == 64 ? tc_launch<64, __half>(p, map_k, map_v, grid, s, dependent) : tc_launch<128, __half>(p, map_k, map_v, grid, s, dependent);
+    int rc = tc_kernel(p, map_k, map_v, dh, type, nq, grid, s, dependent);
     if (rc != ZOQAT_OK) return rc;
     count_launch();
     if (type == kTypeBf16) rc = dh == 64 ? combine_launch<64, __nv_bfloat16>(p, grid, y, s) : combine_launch<128, __nv_bfloat16>(p, grid, y, s);

@@ -6,13 +6,12 @@
 
 namespace zq {
 
-constexpr int kKeys = 128;           // keys per tile
 constexpr int kMaskWords = 4;        // words of a draft's mask that travel with its query tile (trees of up to 128 drafts)
 constexpr float kTreeSlack = 8.0f;   // a reference may lag the maximum by up to 2^8
 constexpr float kNoRef = -3.0e38f;   // reference of a query that has seen nothing: any score passes it
 
-struct TcParams {
-    TreeWork w;
+template <class W> struct TcParamsT {
+    W w;
     const void* q;
     int64_t q_stride;
     int box_keys;                // keys of one K / V box: a page, or 128 of a larger one
@@ -28,6 +27,7 @@ struct TcParams {
     int64_t page_stride, slot_stride, head_stride;
     uint32_t smem_bytes;
 };
+using TcParams = TcParamsT<TreeWork>;
 
 template <typename T> struct HalfOps;
 template <> struct HalfOps<__nv_bfloat16> {
@@ -135,14 +135,14 @@ template <int DH> __host__ __device__ constexpr int tree_group_bytes() { return 
 // tile ahead: K(0), K(1), V(0), K(2), V(1), ...
 // Every lane fetches one page (or 128 keys of a larger one), and
 // reads its entry of the block table two tiles ahead.
-template <int DH, int NS, int LEAD>
-__device__ __forceinline__ void tree_load_keys(const TcParams& p, const CUtensorMap* map_k, const CUtensorMap* map_v, const TreeRun* run,
+template <int DH, int NS, int LEAD, class W>
+__device__ __forceinline__ void tree_load_keys(const TcParamsT<W>& p, const CUtensorMap* map_k, const CUtensorMap* map_v, const TreeRunT<W>* run,
                                                uint32_t ring, uint32_t full, uint32_t empty) {
     constexpr int kTileBytes = kKeys * DH * 2, kGroup = tree_group_bytes<DH>();
     const int lane = threadIdx.x & 31;
     const int n_box = kKeys / p.box_keys, n_tiles = (int)(run->end - run->begin);
     const uint32_t box_bytes = (uint32_t)(p.box_keys >> 3) * kGroup;
-    TreeCursor c = run->at;
+    TreeCursorT<W> c = run->at;
     uint32_t seq = 0;
     bool ok = true;
     struct Box { int page, group, h, live; bool mine; };         // page: as the table has it, looked at when the box is fetched
@@ -154,7 +154,7 @@ __device__ __forceinline__ void tree_load_keys(const TcParams& p, const CUtensor
         if (!x.mine) return;
         const int idx = p.page_shift >= 0 ? key0 >> p.page_shift : key0 / p.w.page_size;
         x.group = (key0 - idx * p.w.page_size) >> 3;
-        x.page = __ldg(p.w.block_table + (size_t)c.b * p.w.max_pages + idx);
+        x.page = __ldg(p.w.block_table + (size_t)c.r.table(c.b) * p.w.max_pages + idx);
     };
     auto fetch = [&](const CUtensorMap* map, const Box& x) -> bool {
         const int slot = seq % NS;
@@ -192,14 +192,14 @@ __device__ __forceinline__ void tree_load_keys(const TcParams& p, const CUtensor
 // swizzle, [half][NQ rows], BUFFERS buffers in turn.  Rows behind the tile's last query keep what they hold; their results are
 // not used.  full counts one arrival per warp.  masks (may be NULL): [2][NQ][kMaskWords], the first words of the drafts' masks, draft by draft; done: four
 // barriers, by piece modulo 4, after which a piece's masks are no longer read.
-template <int DH, int NQ, int THREADS, int BUFFERS, typename T>
-__device__ __forceinline__ void tree_load_queries(const TcParams& p, const TreeRun* run, uint8_t* q_tiles, uint32_t* masks, uint32_t done, uint32_t full,
+template <int DH, int NQ, int THREADS, int BUFFERS, typename T, class W>
+__device__ __forceinline__ void tree_load_queries(const TcParamsT<W>& p, const TreeRunT<W>* run, uint8_t* q_tiles, uint32_t* masks, uint32_t done, uint32_t full,
                                                   uint32_t empty, int lane) {
     constexpr int kChunks = DH / 8, kTileBytes = NQ * DH * 2, kRowsPer = THREADS / kChunks, kMost = NQ >= 256 ? 16 : 8,
                   kFly = NQ / kRowsPer < kMost ? NQ / kRowsPer : kMost;
     const int ch = lane % kChunks;               // a thread copies its 16 bytes of every kRowsPer-th row, kFly rows in flight
     const int n_tiles = (int)(run->end - run->begin);
-    TreeCursor c = run->at;
+    TreeCursorT<W> c = run->at;
     uint32_t piece = 0;
     for (int t = 0; t < n_tiles; ++t, c.next(p.w)) {
         if (t != 0 && !c.item_begins()) continue;
@@ -266,14 +266,15 @@ __device__ __forceinline__ bool tree_clean_values(uint8_t* v, int first_draft, i
 }
 
 // Where the key stands in the cache, or -1 (bad page).
-__device__ __forceinline__ int64_t tree_value_offset(const TcParams& p, const TreeCursor& c, int key) {
+template <class W>
+__device__ __forceinline__ int64_t tree_value_offset(const TcParamsT<W>& p, const TreeCursorT<W>& c, int key) {
     const int idx = key / p.w.page_size;
-    const int pg = __ldg(p.w.block_table + (size_t)c.b * p.w.max_pages + idx);
+    const int pg = __ldg(p.w.block_table + (size_t)c.r.table(c.b) * p.w.max_pages + idx);
     if (pg < 0 || pg >= p.n_pages) return -1;
     return pg * p.page_stride + (key - idx * p.w.page_size) * p.slot_stride + c.h * p.head_stride;
 }
 
 // few queries per key head: keys are the rows of the products (tree_attention_keys.cu); nq: queries per tile (16, 32, 64)
-int launch_tree_keys(const TcParams& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int dh, int type, int nq, int grid, cudaStream_t s, bool dependent);
+template <class W> int launch_tree_keys(const TcParamsT<W>& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int dh, int type, int nq, int grid, cudaStream_t s, bool dependent);
 
 }  // namespace zq

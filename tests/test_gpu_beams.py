@@ -369,3 +369,205 @@ def test_copies_of_all_layers(zq, layers, page, kv, dh, dtype, layout):
         assert torch.equal(k, k0) and torch.equal(v, v0)
     empty = torch.zeros(0, dtype=torch.int32, device="cuda")
     assert int(zq.zoqat_op_cache_copy(zq.LayerCaches(caches), empty, empty, empty)) == 0
+
+
+# ---- attention over a shared prefix ---------------------------------------------------------------------------------
+def ints(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def prefix_problem(seed, dtype, heads, kv, dh, page, layout, prefix, per, cached, new, mask="tree", pad=2, gap=0, q_scale=1.0, share=True):
+    """cached: keys of each request between the prefix and its new rows.  Everything that no row may see is NaN."""
+    from test_gpu_serve import ancestors, rand_parents, words_of
+    rng = np.random.default_rng(seed)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    group = [g for g, n in enumerate(per) for _ in range(n)]
+    L = [prefix[g] + c + n for g, c, n in zip(group, cached, new)]
+    whole = [p // page if share else 0 for p in prefix]
+    held = [-(-x // page) for x in L]
+    n_pages = sum(w for w, n in zip(whole, per) if n) + sum(h - whole[g] for g, h in zip(group, held)) + 2
+    order = rng.permutation(n_pages).tolist()
+    shape = (n_pages, kv, page, dh) if layout == "head" else (n_pages, page, kv, dh)
+    k, v = [torch.full(shape, float("nan"), device="cuda", dtype=DTYPES[dtype]) for _ in range(2)]
+    if layout == "head":
+        k, v = k.transpose(1, 2), v.transpose(1, 2)
+    rand = lambda n: torch.randn((n, kv, dh), generator=gen, device="cuda").to(DTYPES[dtype])  # noqa: E731
+    first = [(rand(p), rand(p)) for p in prefix]
+    pages_of = []
+    for w, n in zip(whole, per):
+        w = w if n else 0
+        pages_of.append(order[:w])
+        order = order[w:]
+    table, keys, vals = [], [], []
+    for b, g in enumerate(group):
+        mine = pages_of[g] + order[: held[b] - whole[g]]
+        order = order[held[b] - whole[g]:]
+        table.append(mine + [-3] * (max(held) + 1 - len(mine)))
+        keys.append(torch.cat([first[g][0], rand(L[b] - prefix[g])]))
+        vals.append(torch.cat([first[g][1], rand(L[b] - prefix[g])]))
+        t = torch.arange(L[b], device="cuda")
+        pg = torch.tensor(mine + [0], device="cuda")[t // page]
+        k[pg, t % page], v[pg, t % page] = keys[-1], vals[-1]
+    rows = sum(new)
+    q = torch.full((rows + pad, heads + gap, dh), float("nan"), dtype=DTYPES[dtype], device="cuda")[:, :heads]
+    q[:rows] = (q_scale * torch.randn((rows, heads, dh), generator=gen, device="cuda")).to(DTYPES[dtype])
+    words = max(1, -(-max(new) // 32))
+    seen = []
+    for n in new:
+        if mask == "tree":
+            par = rand_parents(rng, [n])
+            seen.append([set(ancestors(par, i)) for i in range(n)])
+        elif mask == "random":
+            seen.append([set(np.nonzero(rng.random(n) < 0.3)[0].tolist()) if i % 3 else set() for i in range(n)])
+        else:
+            seen.append([set(range(i + 1)) for i in range(n)])
+    start, gs = [0], [0]
+    for n in new:
+        start.append(start[-1] + n)
+    for n in per:
+        gs.append(gs[-1] + n)
+    bits = [words_of(s, words) for r in seen for s in r] + [[-1] * words] * pad
+    return dict(dtype=dtype, q=q, k=k, v=v, table=ints(table), kv_len=ints(L), row_start=ints(start), mask=ints(bits) if mask else None, rows=rows, start=start, new=new, L=L,
+                keys=keys, vals=vals, seen=seen, heads=heads, kv=kv, dh=dh, scale=1.0 / math.sqrt(dh), group_start=ints(gs), prefix_len=ints(prefix), group=ints(group))
+
+
+def run_prefix(zq, pr, out=None, **kw):
+    out = torch.full_like(pr["q"], 5.0) if out is None else out
+    got, err = zq.zoqat_op_prefix_attention(pr["q"], pr["k"], pr["v"], pr["table"], pr["kv_len"], pr["row_start"], pr["group_start"], pr["prefix_len"], pr["group"],
+                                            tree_mask=pr["mask"], out=out, **kw)
+    assert int(err) == 0
+    assert (got[pr["rows"]:] == 5.0).all()                        # rows behind the last request
+    return got
+
+
+def check_prefix(zq, pr, **kw):
+    from test_gpu_serve import attention_oracle
+    got = run_prefix(zq, pr, **kw)
+    want, bound = attention_oracle(pr)                            # (joining two parts is a few of the roundings its bound allows for sums)
+    off = (got[: pr["rows"]].double() - want).abs()
+    assert bool((off <= bound).all()), (float(off.max()), float((off / bound.clamp(min=1e-30)).max()))
+    assert torch.equal(run_prefix(zq, pr, **kw)[: pr["rows"]], got[: pr["rows"]])
+    return got
+
+
+PREFIX = [
+    # dtype, heads, kv, dh, page, layout, prefix, per, own cached, new, mask
+    ("bf16", 2, 2, 128, 16, "token", [300], [1], [0], [1], "tree"),
+    ("f32", 4, 2, 64, 16, "token", [300], [3], [0, 5, 40], [1, 1, 1], None),
+    ("bf16", 8, 2, 128, 16, "token", [1000, 0, 127], [4, 3, 2], [0, 1, 2, 300, 0, 9, 200, 0, 5], [1, 1, 1, 1, 1, 1, 1, 1, 1], None),     # groups without a whole tile
+    ("f16", 8, 2, 64, 64, "head", [128, 129, 1280], [1, 5, 0], [0, 1, 2, 300, 0, 9], [1, 2, 0, 3, 1, 4], "random"),                      # a group without requests
+    ("bf16", 14, 2, 128, 32, "token", [700, 650], [9, 3], list(range(12)), [1] * 12, None),       # 7 query heads per key head, tiles that cut a request's heads apart
+    ("f16", 16, 1, 128, 16, "token", [2000], [40], [3 * i for i in range(40)], [1] * 40, None),     # many queries of one prefix: the wide kernel
+    ("bf16", 8, 2, 64, 128, "head", [900, 400], [50, 60], [i % 7 for i in range(110)], [1 + i % 3 for i in range(110)], "tree"),
+    ("bf16", 32, 8, 128, 64, "token", [3000], [33], [50 * i for i in range(33)], [1] * 33, None),
+    ("f16", 4, 4, 128, 16, "token", [513], [130], [i for i in range(130)], [1] * 130, None),
+    ("bf16", 4, 4, 64, 16, "token", [100] * 70, [1] * 70, [i for i in range(70)], [1] * 70, None),  # nothing worth sharing
+    ("bf16", 8, 1, 128, 16, "token", [20000], [2], [0, 1], [1, 1], None),                          # one prefix over all CTAs
+    ("f32", 8, 1, 128, 64, "head", [9000, 31], [4, 2], [0, 100, 7, 8, 0, 1], [1, 2, 1, 1, 3, 1], "tree"),
+    ("f32", 6, 2, 64, 24, "token", [200, 95, 96], [3, 1, 6], [i for i in range(10)], [1] * 10, None),
+    ("bf16", 20, 1, 64, 8, "token", [640, 260], [3, 4], [5, 0, 7, 130, 0, 64, 1], [33, 2, 40, 1, 0, 5, 17], "random"),          # wide own parts too
+    ("f16", 8, 2, 128, 256, "head", [1023, 1024, 1025], [5, 5, 5], [0, 0, 1, 255, 256] * 3, [1] * 15, None),
+]
+
+
+@pytest.mark.parametrize("case", PREFIX, ids=lambda c: "-".join(str(x) for x in c[:6]) + f"-g{len(c[6])}-b{len(c[8])}-{c[10]}")
+def test_prefix_attention_is_the_definition(zq, case):
+    check_prefix(zq, prefix_problem(11, *case))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_prefix_attention_steep_scores_strided_rows_and_copied_prefixes(zq, dtype):
+    pr = prefix_problem(5, dtype, 8, 2, 128, 16, "token", [520, 300], [6, 4], [i for i in range(10)], [2] * 10, "tree", gap=3, q_scale=20.0, share=False)
+    store = torch.full((pr["q"].shape[0], pr["heads"] + 1, 128), 5.0, dtype=DTYPES[dtype], device="cuda")
+    got = check_prefix(zq, pr, out=store[:, : pr["heads"]])
+    assert (store[:, pr["heads"]:] == 5.0).all()
+    scratch = torch.full((zq.prefix_attention_scratch(pr["q"], pr["k"], rows=4 * pr["q"].shape[0]).numel(),), 255, dtype=torch.uint8, device="cuda")
+    assert torch.equal(run_prefix(zq, pr, scratch=scratch), got)  # what the scratch held does not matter
+
+
+@pytest.mark.parametrize("dtype,per", [("bf16", [6, 4]), ("f16", [40, 30]), ("f32", [3, 2])])
+def test_prefix_attention_is_tree_attention(zq, dtype, per):
+    n = sum(per)
+    pr = prefix_problem(3, dtype, 8, 2, 128, 16, "token", [700, 140], per, [5 * i for i in range(n)], [1 + i % 2 for i in range(n)], "tree")
+    got = run_prefix(zq, pr)
+    other, _ = zq.zoqat_op_tree_attention(pr["q"], pr["k"], pr["v"], pr["table"], pr["kv_len"], pr["row_start"], tree_mask=pr["mask"])
+    from test_gpu_serve import attention_oracle
+    _, bound = attention_oracle(pr)
+    assert bool(((got[: pr["rows"]].double() - other[: pr["rows"]].double()).abs() <= 2 * bound).all())
+
+
+@pytest.mark.parametrize("dtype,per", [("bf16", [2, 3, 2]), ("f16", [30, 40, 30]), ("f32", [2, 3, 2])])
+def test_prefix_attention_reports_contradictions_and_leaves_rows(zq, dtype, per):
+    n = sum(per)
+    pr = prefix_problem(4, dtype, 4, 2, 64, 16, "token", [300, 200, 150], per, [3] * n, [1] * n, None)
+    good = run_prefix(zq, pr)
+    g1, g2 = per[0], per[0] + per[1]
+    def call(**kw):
+        a = dict(pr, **kw)
+        out = torch.full_like(pr["q"], 5.0)
+        _, err = zq.zoqat_op_prefix_attention(a["q"], a["k"], a["v"], a["table"], a["kv_len"], a["row_start"], a["group_start"], a["prefix_len"], a["group"], out=out)
+        return out, int(err)
+    def changed(t, i, x):
+        t = t.clone()
+        t[i] = x
+        return t
+    same = lambda out, rows: torch.equal(out[rows], good[rows])  # noqa: E731
+    first, last = slice(0, g1), slice(g2, n)
+    for bad in (changed(pr["prefix_len"], 1, -1), changed(pr["prefix_len"], 1, 10 ** 6), changed(pr["prefix_len"], 1, 204)):      # group 1: more than its requests hold
+        out, err = call(prefix_len=bad)
+        assert err == 41 and same(out, first) and same(out, last) and (out[g1:g2] == 5.0).all()
+    for bad in (-1, 3, 0, 2 ** 30):                               # a request in no group, or in one that is not its own
+        out, err = call(group=changed(pr["group"], g1, bad))
+        assert err == 41 and (out[g1] == 5.0).all() and same(out, first) and same(out, slice(g1 + 1, n))
+    out, err = call(group_start=changed(pr["group_start"], 3, n + 5))
+    assert err == 41 and same(out, slice(0, g2)) and (out[g2:] == 5.0).all()
+    out, err = call(kv_len=changed(pr["kv_len"], g1, 10 ** 7))
+    assert err == 41 and (out[g1] == 5.0).all() and same(out, first) and same(out, slice(g1 + 1, n))
+    page = pr["table"].clone()
+    page[0, 1] = 10 ** 6                                          # in the shared part: its keys and values count as zeros
+    out, err = call(table=page)
+    assert err == 42 and torch.isfinite(out[:n].float()).all() and same(out, slice(g1, n))
+
+
+def test_prefix_attention_captured_as_lengths_change(zq):
+    from test_gpu_serve import attention_oracle
+    n = 9
+    pr = prefix_problem(9, "bf16", 8, 2, 128, 16, "token", [900, 300], [5, 4], [40] * n, [1] * n, None)
+    out, err, scratch = torch.zeros_like(pr["q"]), torch.zeros(1, dtype=torch.int32, device="cuda"), zq.prefix_attention_scratch(pr["q"], pr["k"])
+    call = lambda: zq.zoqat_op_prefix_attention(pr["q"], pr["k"], pr["v"], pr["table"], pr["kv_len"], pr["row_start"], pr["group_start"], pr["prefix_len"],  # noqa: E731
+                                                pr["group"], out=out, scratch=scratch, err=err)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for prefix, own in (([900, 300], [10, 41, 1, 2, 3, 40, 30, 20, 1]), ([130, 127], [1] * 9), ([0, 0], [30] * 9)):
+        L = [prefix[0 if b < 5 else 1] + own[b] for b in range(n)]
+        pr["kv_len"].copy_(ints(L))
+        pr["prefix_len"].copy_(ints(prefix))
+        out.fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        now = dict(pr, L=L, keys=[k[:x] for k, x in zip(pr["keys"], L)], vals=[v[:x] for v, x in zip(pr["vals"], L)])
+        want, bound = attention_oracle(now)
+        assert int(err) == 0 and bool(((out[:n].double() - want).abs() <= bound).all()) and (out[n:] == 5.0).all()
+
+
+def test_prefix_attention_two_streams_at_once(zq):
+    prs = [prefix_problem(21 + i, "bf16", 8, 2, 128, 16, "token", [1500 - 700 * i], [40], [7 * j for j in range(40)], [1] * 40, None) for i in range(2)]
+    alone = [run_prefix(zq, pr) for pr in prs]
+    streams = [torch.cuda.Stream() for _ in prs]
+    outs = [torch.full_like(pr["q"], 5.0) for pr in prs]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for pr, s, o in zip(prs, streams, outs):
+            with torch.cuda.stream(s):
+                zq.zoqat_op_prefix_attention(pr["q"], pr["k"], pr["v"], pr["table"], pr["kv_len"], pr["row_start"], pr["group_start"], pr["prefix_len"], pr["group"], out=o)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, a) for o, a in zip(outs, alone))
+
+
+def test_prefix_attention_no_rows(zq):
+    k, v = make_cache(4, 16, 2, 64, "bf16", "token")
+    out, err = zq.zoqat_op_prefix_attention(torch.empty((0, 4, 64), dtype=torch.bfloat16, device="cuda"), k, v, ints([[0]]), ints([0]), ints([0, 0]), ints([0, 1]), ints([0]), ints([0]))
+    assert out.shape == (0, 4, 64) and int(err) == 0
