@@ -20,7 +20,7 @@ struct JoinParams {
     PrefixWork w;                            // tile_rows: unused
     uint8_t* pieces[2];                      // of the shared and the own parts
     int tile_rows[2];
-    int grid;                                // CTAs that wrote them
+    int workers[2];                          // that wrote them
     void* out;
     int64_t out_stride;
 };
@@ -31,35 +31,27 @@ template <typename T, int DH, bool WIDE>
 __global__ void __launch_bounds__(256)
 prefix_join_kernel(const JoinParams p) {
     constexpr int VPL = DH / 32;
-    __shared__ int request_s;
     __shared__ float acc_s[WIDE ? 8 : 1][DH], m_s[8], l_s[8];
     const PrefixWork& w = p.w;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = blockIdx.x, heads = w.n_kv * w.group;
-    if (tid == 0) request_s = -1;
     grid_dependency_wait();
-    __syncthreads();
-    for (int b = tid; b < w.requests; b += 256)
-        if (__ldg(w.row_start + b) <= row && row < __ldg(w.row_start + b + 1)) request_s = b;
-    __syncthreads();
-    const int b = request_s;
-    if (b < 0) return;                                           // no request's row: left as it is
-    bool ok;
-    const PrefixRequest own = prefix_own(w, b, ok);
-    if (!ok || own.n_kt == 0 || row < own.row0 || row >= own.row0 + own.n) return;
-    const PrefixRequest shared = prefix_shared(w, __ldg(w.request_group + b), ok);
-    if (!ok) return;
+    const int sides = w.row_sides[row];
+    if (sides == 0) return;                                      // no request's row: left as it is
     const int h = WIDE ? blockIdx.y : blockIdx.y * 8 + warp;
     if (!WIDE && h >= heads) return;
     const int first = WIDE ? warp : 0, step = WIDE ? 8 : 1;      // pieces of this warp
     float m = -INFINITY, l = 0.0f, acc[VPL];
 #pragma unroll
     for (int j = 0; j < VPL; ++j) acc[j] = 0.0f;
-    for (int side = shared.n_kt > 0 ? 0 : 1; side < 2; ++side) {
-        const int64_t at = ((int64_t)side * w.rows + row) * heads + h;
-        const int2 e = w.entries[at];
+    const int64_t query = (int64_t)row * heads + h;
+    int2 entry[2];
+    for (int side = 0; side < 2; ++side) entry[side] = w.entries[side * (int64_t)w.rows * heads + query];      // (anything where there is no part)
+    for (int side = sides == 3 ? 0 : 1; side < 2; ++side) {
+        const int64_t at = side * (int64_t)w.rows * heads + query;
+        const int2 e = entry[side];
         const bool whole = e.y < 0;
         const int c0 = whole ? 0 : e.x & 0xFFFF, pieces = whole ? 1 : (e.x >> 16) - c0 + 1;
-        if (!whole && (c0 + pieces > p.grid || e.y >= p.tile_rows[side])) continue;      // (a wait ran out: nothing was written)
+        if (!whole && (c0 + pieces > p.workers[side] || e.y >= p.tile_rows[side])) continue;      // (a wait ran out: nothing was written)
         for (int p0 = first; p0 < pieces; p0 += 4 * step) {      // four pieces in flight
             float pm[4], pl[4], po[4][VPL];
 #pragma unroll
@@ -68,11 +60,13 @@ prefix_join_kernel(const JoinParams p) {
                 pm[u] = -INFINITY; pl[u] = 0.0f;
 #pragma unroll
                 for (int j = 0; j < VPL; ++j) po[u][j] = 0.0f;
-                if (k >= pieces || (k > 0 && !tree_front(p.pieces[side])[c0 + k])) continue;
+                if (k >= pieces) continue;
                 const float* slot = whole ? nullptr : tree_slot(p.pieces[side], k == 0 ? 2 * c0 + 1 : 2 * (c0 + k), p.tile_rows[side], DH);
                 const float* o = whole ? w.partial + at * (DH + 4) : slot + 2 * p.tile_rows[side] + (size_t)e.y * DH;
+                const bool there = whole || k == 0 || prefix_front(p.pieces[side])[c0 + k];
                 pm[u] = whole ? o[DH] : slot[e.y];
                 pl[u] = whole ? o[DH + 1] : slot[p.tile_rows[side] + e.y];
+                if (!there) pl[u] = 0.0f;                        // (its worker had no tile of the part)
 #pragma unroll
                 for (int j = 0; j < VPL; ++j) po[u][j] = o[lane * VPL + j];
             }
@@ -134,6 +128,7 @@ PrefixScratch prefix_scratch(void* base, int type, int d_head, int64_t rows, int
     at.pieces[1] = type == kTypeF32 ? at.pieces[0] : take(tree_attention_scratch_bytes(type, d_head));
     at.entries = take((size_t)rows * n_heads * 2 * sizeof(int2));
     at.partial = reinterpret_cast<float*>(take((size_t)rows * n_heads * 2 * (d_head + 4) * sizeof(float)));
+    at.row_sides = reinterpret_cast<int*>(take((size_t)rows * sizeof(int)));
     at.bytes = used;
     return at;
 }
@@ -146,25 +141,21 @@ int launch_prefix_attention(const PrefixAttnArgs& a, void* scratch, cudaStream_t
     static_cast<TreeWork&>(p.w) = TreeWork{t.kv_len, t.row_start, t.block_table, t.batch, t.rows, t.cache.n_kv_heads, t.max_pages, t.cache.page_size, group, 1, kSimtKeys, 0, t.err_flag};
     prefix_work(a, at, 0, 0, p.w);
     p.pieces[0] = p.pieces[1] = at.pieces[0];
-    p.grid = tree_grid();
+    p.workers[0] = p.workers[1] = tree_grid();
     p.out = t.out; p.out_stride = t.out_stride;
     if (t.cache.type == kTypeF32) {
         p.tile_rows[0] = p.tile_rows[1] = kSimtRows;
-        p.grid *= 2;
+        p.workers[0] = p.workers[1] = 2 * tree_grid();
         if (int rc = launch_prefix_simt(a, at, s, dependent)) return rc;
         return t.cache.d_head == 64 ? join<float, 64>(p, s) : join<float, 128>(p, s);
     }
     // Queries per tile from averages (the host does not know the lengths).
     const long long queries = (long long)t.rows * group;
-    const long long own = t.rows <= t.batch ? group : (3 * queries + 2 * t.batch - 1) / (2 * t.batch);       // 1.5 x the average
-    const long long shared = (queries + a.groups - 1) / a.groups;
-    int tile_shared = shared <= 64 ? (int)shared : 256, tile_own = own <= 64 ? (int)own : 256;
-    if (tile_shared <= 64 && tile_own <= 64) tile_shared = tile_own = tile_shared > tile_own ? tile_shared : tile_own;
-    p.w.key_tile = kKeys;
-    auto rows_of = [](int n) { return n <= 16 ? 16 : (n <= 32 ? 32 : (n <= 64 ? 64 : 256)); };
-    p.tile_rows[0] = rows_of(tile_shared); p.tile_rows[1] = rows_of(tile_own);
+    const long long want[2] = {(queries + a.groups - 1) / a.groups, t.rows <= t.batch ? group : (3 * queries + 2 * t.batch - 1) / (2 * t.batch)};     // (1.5 x the average)
+    for (int side = 0; side < 2; ++side) p.tile_rows[side] = want[side] <= 8 ? 8 : want[side] <= 16 ? 16 : (want[side] <= 32 ? 32 : (want[side] <= 64 ? 64 : 256));
     if (p.tile_rows[0] != p.tile_rows[1]) p.pieces[1] = at.pieces[1];
-    if (int rc = launch_prefix_tc(a, at, tile_shared, tile_own, s, dependent)) return rc;
+    for (int side = 0; side < 2; ++side) p.workers[side] = p.tile_rows[side] <= kNarrowRows ? p.workers[side] * kNarrowWarps : p.workers[side];
+    if (int rc = launch_prefix_tc(a, at, p.tile_rows, s, dependent)) return rc;
     if (t.cache.type == kTypeBf16) return t.cache.d_head == 64 ? join<__nv_bfloat16, 64>(p, s) : join<__nv_bfloat16, 128>(p, s);
     return t.cache.d_head == 64 ? join<__half, 64>(p, s) : join<__half, 128>(p, s);
 }

@@ -128,11 +128,12 @@ struct PrefixAttnArgs {
     const int32_t *group_start, *prefix_len, *request_group;     // [groups + 1], [groups], [batch]
     int groups;
 };
-struct PrefixScratch { uint8_t* pieces[2]; void* entries; float* partial; size_t bytes; };
+struct PrefixScratch { uint8_t* pieces[2]; void* entries; float* partial; int* row_sides; size_t bytes; };
 PrefixScratch prefix_scratch(void* base, int type, int d_head, int64_t rows, int n_heads);
 int launch_prefix_attention(const PrefixAttnArgs& a, void* scratch, cudaStream_t s, bool dependent);      // 0 or a ZOQAT_ERR_* code
 int launch_prefix_simt(const PrefixAttnArgs& a, const PrefixScratch& at, cudaStream_t s, bool dependent);
-int launch_prefix_tc(const PrefixAttnArgs& a, const PrefixScratch& at, int tile_shared, int tile_own, cudaStream_t s, bool dependent);
+// tile: queries per tile of the shared and the own parts, 8, 16, 32, 64 or 256
+int launch_prefix_tc(const PrefixAttnArgs& a, const PrefixScratch& at, const int (&tile)[2], cudaStream_t s, bool dependent);
 int tree_grid();                         // CTAs of the attention kernels on the current device
 int launch_tree_attention_simt(const TreeAttnArgs& a, cudaStream_t s, bool dependent);   // fp32; 0 or a ZOQAT_ERR_* code
 int launch_tree_attention_tc(const TreeAttnArgs& a, cudaStream_t s, bool dependent);     // bf16 / fp16

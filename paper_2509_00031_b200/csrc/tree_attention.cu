@@ -177,13 +177,9 @@ tree_attention_simt_kernel(SimtParamsT<W> p) {
     float* l_s = m_s + 8 * kSimtRows;
     int64_t* offs = reinterpret_cast<int64_t*>(sm + Cfg::kOffKeys);
     TreeTail* tails = reinterpret_cast<TreeTail*>(p.scratch);
-    grid_dependency_wait();
-    tree_find_run(p.w, part, &run);
-    if (tid == 0) {
-        tails[blockIdx.x].last_cta = -1;
-        tree_front(p.scratch)[blockIdx.x] = run.begin < run.end && !run.at.item_begins();
-    }
-    if (run.begin >= run.end) return;
+    tree_start(p.w, part, &run, sm);
+    if (tid == 0) tree_announce<W>(p.scratch, run.begin < run.end && !run.at.item_begins());
+    if (run.begin >= run.end) { tree_finish(p.w); return; }
 
     TreeCursorT<W> c = run.at, ahead = run.at;
     bool split_front = !c.item_begins();                   // the first piece continues an item of an earlier CTA
@@ -302,6 +298,7 @@ tree_attention_simt_kernel(SimtParamsT<W> p) {
         c.next(p.w);
     }
     cp_async_wait<0>();
+    tree_finish(p.w);
 }
 
 template <int DH, class W>

@@ -18,6 +18,7 @@ namespace zq {
 
 constexpr int kSimtKeys = 32, kSimtRows = 8;             // keys of a key tile, queries of a row tile: the CUDA-core kernel's
 constexpr int kKeys = 128;                               // keys of a key tile: the tensor-core kernels'
+constexpr int kNarrowKeys = 16, kNarrowRows = 16, kNarrowWarps = 12;      // the warps' kernel (prefix_narrow.cu): a run per warp
 
 // A request's part of the work: n rows from row0 on, keys up to L, in n_rt row tiles and the key tiles [first_tile(), n_kt); n_rt * n_kt = 0: nothing to do.
 // drafts(): how many of the last keys are the rows' own.  table(b): its row of the block table.
@@ -72,11 +73,14 @@ struct PrefixWork : TreeWork {               // batch: parts in this launch
     static constexpr bool kPrefix = true;
     const int32_t *group_start, *prefix_len, *request_group;
     int groups, requests;
+    int border;                              // keys that the border is a multiple of: a multiple of every key tile in use
     int first;                               // the launch's first part: 0 .. groups - 1 are groups, then come the requests
+    int* row_sides;                          // [rows]
+    bool late_wait;                          // the launch before left nothing that this one reads: waited for at the end
     int2* entries;                           // [2][rows * heads]: where a query's shared (0) and own (1) pieces are
     float* partial;                          // [2][rows * heads][d_head + 4]: output, reference, sum of parts that one CTA finished
 };
-__device__ __forceinline__ int prefix_border(const PrefixWork& w, int len) { return len / w.key_tile * w.key_tile; }
+__device__ __forceinline__ int prefix_border(const PrefixWork& w, int len) { return len / w.border * w.border; }
 
 // The shared part of group g; n_kt = 0: it has none, or (ok = false) its description contradicts itself.
 __device__ __forceinline__ PrefixRequest prefix_shared(const PrefixWork& w, int g, bool& ok) {
@@ -121,6 +125,20 @@ __device__ __forceinline__ PrefixRequest tree_request(const PrefixWork& w, int p
     if (!ok) atomicExch(w.err_flag, kErrBadRequest);
     return r;
 }
+// What the joining launch needs to know of every row, so that it does not have to look for the row's request: 0 not a row of any (valid) request, 1 own keys only, 3 a
+// shared part too.  By all threads of one CTA of the launch that has the requests' own parts.
+__device__ __forceinline__ void prefix_map_rows(const PrefixWork& w) {
+    for (int r = threadIdx.x; r < w.rows; r += blockDim.x) w.row_sides[r] = 0;
+    __syncthreads();
+    for (int b = threadIdx.x; b < w.requests; b += blockDim.x) {
+        bool ok;
+        const PrefixRequest own = prefix_own(w, b, ok);
+        if (own.n_kt == 0) continue;
+        const PrefixRequest shared = prefix_shared(w, __ldg(w.request_group + b), ok);
+        // (rows that another request claims as well may get either's word)
+        for (int i = 0; ok && i < own.n; ++i) w.row_sides[own.row0 + i] = shared.n_kt > 0 ? 3 : 1;
+    }
+}
 // Where the query's piece is: whole in `partial` (y = -1), or query y of the pieces of the CTAs x & 0xFFFF .. x >> 16.
 __device__ __forceinline__ int64_t prefix_query(const PrefixWork& w, const PrefixRequest& r, int query, int h) {
     const int token = query / w.group;
@@ -129,9 +147,10 @@ __device__ __forceinline__ int64_t prefix_query(const PrefixWork& w, const Prefi
 
 // The prefix part of a work description: `parts` of them from `first` on.
 inline void prefix_work(const PrefixAttnArgs& a, const PrefixScratch& at, int first, int parts, PrefixWork& w) {
+    w.border = a.t.cache.type == kTypeF32 ? kSimtKeys : kKeys;
     w.group_start = a.group_start; w.prefix_len = a.prefix_len; w.request_group = a.request_group;
     w.groups = a.groups; w.requests = a.t.batch; w.first = first; w.batch = parts;
-    w.entries = static_cast<int2*>(at.entries); w.partial = at.partial;
+    w.entries = static_cast<int2*>(at.entries); w.partial = at.partial; w.row_sides = at.row_sides;
 }
 
 // Position in the sequence of key tiles.  next() moves on by one tile; tiles of requests without work do not exist.
@@ -244,6 +263,88 @@ __device__ __forceinline__ void tree_find_run(const W& w, long long* part, TreeR
     __syncthreads();
 }
 
+// The same for lists of parts, whose descriptions take several dependent reads: the threads keep those that they scanned in shared memory, and the edges of
+// the runs are looked up side by side.  N workers per CTA (1, or its warps): out[0 .. N - 1] are their runs, *end the part in which the last of them ends.
+struct PrefixScan {
+    static constexpr int kMost = 384;        // threads of a block, and parts whose descriptions are kept
+    long long units[kMost], tiles[kMost];    // before the parts of each thread
+    PrefixRequest part[kMost];               // one part to a thread
+    long long sums[2 * kMost / 32];
+    int kept;                                // descriptions in `part`
+};
+__device__ __forceinline__ void prefix_load(const PrefixWork& w, const PrefixScan& scan, int b, PrefixRequest& r) {
+    if (b < scan.kept) r = scan.part[b];
+    else r = tree_request(w, b);
+}
+template <int N>
+__device__ __forceinline__ void prefix_find_runs(const PrefixWork& w, PrefixScan& scan, TreeRunT<PrefixWork>* out) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+    const int per = (w.batch + blockDim.x - 1) / blockDim.x;
+    const int b0 = min(tid * per, w.batch), b1 = min(b0 + per, w.batch);
+    long long tiles = 0, items = 0;
+    for (int b = b0; b < b1; ++b) {
+        const PrefixRequest r = tree_request(w, b);
+        const long long n = r.n_kt ? (long long)w.n_kv * r.n_rt : 0;
+        items += n;
+        tiles += n * (r.n_kt - r.kt0);
+        if (per == 1) scan.part[b] = r;
+    }
+    long long up_tiles = tiles, up_items = items;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long u = __shfl_up_sync(0xffffffffu, up_tiles, o), v = __shfl_up_sync(0xffffffffu, up_items, o);
+        if (lane >= o) { up_tiles += u; up_items += v; }
+    }
+    if (lane == 31) { scan.sums[2 * warp] = up_tiles; scan.sums[2 * warp + 1] = up_items; }
+    if (tid == 0) scan.kept = per == 1 ? w.batch : 0;
+    __syncthreads();
+    long long all_tiles = 0, all_items = 0;
+    for (int k = 0; k < warps; ++k) {
+        if (k == warp) { up_tiles += all_tiles; up_items += all_items; }
+        all_tiles += scan.sums[2 * k];
+        all_items += scan.sums[2 * k + 1];
+    }
+    scan.units[tid] = (up_tiles - tiles) + w.item_cost * (up_items - items);
+    scan.tiles[tid] = up_tiles - tiles;
+    const long long total = all_tiles + w.item_cost * all_items, most = (long long)gridDim.x * N;
+    const int workers = total < most ? (int)total : (int)most, me = blockIdx.x * N + tid;
+    if (tid < N && me >= workers) { out[tid].begin = out[tid].end = 0; }
+    if (tid < N && me == workers - 1) { out[tid].end = all_tiles; out[tid].tail_cta = -1; }
+    __syncthreads();
+    if (tid <= N && me < workers) {
+        const long long edge = tree_run_begin(total, workers, me);
+        int lo = 0, hi = blockDim.x;                           // the last thread whose parts begin at or before the edge
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (scan.units[mid] <= edge) lo = mid;
+            else hi = mid;
+        }
+        long long rest = edge - scan.units[lo], at_tile = scan.tiles[lo], unit = scan.units[lo];
+        TreeCursorT<PrefixWork> c;
+        int cost = 1, tiles_of = 0;
+        for (c.b = lo * per; c.b < w.batch; ++c.b) {
+            prefix_load(w, scan, c.b, c.r);
+            if (c.r.n_kt == 0) continue;
+            tiles_of = c.r.n_kt - c.r.kt0;
+            cost = tiles_of + w.item_cost;
+            const long long n = (long long)w.n_kv * c.r.n_rt;
+            if (rest < n * cost) break;
+            rest -= n * cost;
+            unit += n * cost;
+            at_tile += n * tiles_of;
+        }
+        const long long item = tree_div(rest, cost), head = tree_div(item, c.r.n_rt);
+        const int in = max(0, (int)(rest - item * cost) - w.item_cost);
+        c.kt = c.r.kt0 + in;
+        c.rt = (int)(item - head * c.r.n_rt);
+        c.h = (int)head;
+        at_tile += item * tiles_of + in;
+        if (tid < N) { out[tid].begin = at_tile; out[tid].at = c; }
+        if (tid > 0) { out[tid - 1].end = at_tile; out[tid - 1].tail_cta = in > 0 ? tree_cta_of(unit + (item + 1) * cost - 1, total, workers) : -1; }
+    }
+    __syncthreads();
+}
+
 // ---- partial results ------------------------------------------------------------------------------------------------
 // One descriptor per CTA, a word that says whether its front slot is in use, then 2 * G slots of [tile_rows] references, [tile_rows] sums and [tile_rows][d_head] outputs (fp32).
 struct TreeTail { int last_cta, queries, row0, q0, h, pad[3]; };   // an item that begins in this CTA and ends in last_cta; -1: none
@@ -255,6 +356,30 @@ __host__ __device__ inline size_t tree_slot_floats(int tile_rows, int dh) { retu
 
 // which CTAs have a front piece: one that continues an item of an earlier CTA (slot 2 c; slot 2 c + 1: one that goes on in the next)
 __device__ __forceinline__ int* tree_front(uint8_t* scratch) { return reinterpret_cast<int*>(scratch + kFrontOffset); }
+// (parts of a shared prefix have no descriptors, their workers may be many)
+constexpr int kMaxWorkers = kMaxTreeGrid / 2 * kNarrowWarps;
+static_assert(kMaxWorkers * sizeof(int) <= kTailBytes && kMaxWorkers >= kMaxTreeGrid && kMaxWorkers < 32768, "front words, places of pieces");
+__device__ __forceinline__ int* prefix_front(uint8_t* scratch) { return reinterpret_cast<int*>(scratch); }
+// what a CTA says before its run
+template <class W> __device__ __forceinline__ void tree_announce(uint8_t* scratch, bool front) {
+    if (W::kPrefix) { prefix_front(scratch)[blockIdx.x] = front; return; }
+    reinterpret_cast<TreeTail*>(scratch)[blockIdx.x].last_cta = -1;
+    tree_front(scratch)[blockIdx.x] = front;
+}
+// The run of this CTA, as soon as the launch before has left what it reads; ends with a barrier.  scan: sizeof(PrefixScan) bytes of shared memory that are not in use
+// yet (lists of parts only).
+__device__ __forceinline__ void tree_start(const TreeWork& w, long long* part, TreeRun* run, void*) {
+    grid_dependency_wait();
+    tree_find_run(w, part, run);
+}
+__device__ __forceinline__ void tree_start(const PrefixWork& w, long long*, TreeRunT<PrefixWork>* run, void* scan) {
+    if (!w.late_wait) grid_dependency_wait();
+    grid_dependency_release();
+    prefix_find_runs<1>(w, *static_cast<PrefixScan*>(scan), run);
+    if (blockIdx.x == gridDim.x - 1 && w.first + w.batch > w.groups) prefix_map_rows(w);
+}
+__device__ __forceinline__ void tree_finish(const TreeWork&) {}
+__device__ __forceinline__ void tree_finish(const PrefixWork& w) { if (w.late_wait) grid_dependency_wait(); }
 
 __device__ __forceinline__ float* tree_slot(uint8_t* scratch, int index, int tile_rows, int dh) {
     return reinterpret_cast<float*>(scratch + kTailBytes) + (size_t)index * tree_slot_floats(tile_rows, dh);

@@ -59,7 +59,7 @@ template <int DH, int N, class W> struct KeyCfg {
     static constexpr int kOffMisc = kOffBar + kBars * 8;
     static constexpr int kUsedBytes = kOffMisc + 32 + 192 + (int)sizeof(TreeRunT<W>);
     static constexpr int kSmemBytes = kUsedBytes + 1024 > 232448 ? 232448 : kUsedBytes + 1024;
-    static_assert(kUsedBytes <= 232448 && kStages >= 4, "shared memory");
+    static_assert(kUsedBytes <= 232448 && kStages >= 4 && sizeof(PrefixScan) <= kStages * kTileBytes, "shared memory");
 };
 
 // f over the warp's 32 lanes of v[i], for 16 values at once: lanes 2 i and 2 i + 1 return that of v[i].
@@ -107,10 +107,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if ((base - raw) + (uint32_t)Cfg::kUsedBytes > p.smem_bytes) {           // uniform: nothing has been set up yet
         if (tid == 0) atomicExch(p.w.err_flag, kErrTreeWait);
-        if (tid == 0) {
-            reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x].last_cta = -1;
-            tree_front(p.scratch)[blockIdx.x] = 0;
-        }
+        if (tid == 0) tree_announce<W>(p.scratch, false);
         return;
     }
     const uint32_t bars = base + Cfg::kOffBar;
@@ -144,12 +141,9 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
         tmem_alloc(base + Cfg::kOffMisc, 512);
         tmem_relinquish();
     }
-    grid_dependency_wait();                    // lengths, queries and the drafts' keys come from the kernels before
-    tree_find_run(p.w, part, run);
-    if (tid == 0) {
-        reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x].last_cta = -1;
-        tree_front(p.scratch)[blockIdx.x] = run->begin < run->end && !run->at.item_begins();
-    }
+    tree_start(p.w, part, run, sp);            // lengths, queries and the drafts' keys come from the kernels before
+    if (tid == 0) tree_announce<W>(p.scratch, run->begin < run->end && !run->at.item_begins());
+    if (W::kPrefix) fence_async_smem();        // the scan lay where tiles will
     const uint32_t tmem = *tmem_slot;          // (allocated before the barriers in tree_find_run)
     if (!Cfg::kAdd && warp >= 4 && warp < 8) { // the matrix of ones: 16 keys' worth, the same for every step
         tc_fence_after();
@@ -586,6 +580,7 @@ tree_attention_keys_kernel(const __grid_constant__ CUtensorMap map_k, const __gr
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
+    tree_finish(p.w);
 }
 
 template <int DH, int N, typename T, class W>

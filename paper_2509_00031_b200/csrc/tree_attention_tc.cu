@@ -50,7 +50,7 @@ template <int DH, class W> struct TcCfg {
     static constexpr int kOffMisc = kOffBar + kBars * 8;                    // TMEM base, non-finite marks, run
     static constexpr int kUsedBytes = kOffMisc + 32 + 192 + (int)sizeof(TreeRunT<W>);
     static constexpr int kSmemBytes = kUsedBytes + 1024 > 232448 ? 232448 : kUsedBytes + 1024;
-    static_assert(kUsedBytes <= 232448, "shared memory");
+    static_assert(kUsedBytes <= 232448 && sizeof(PrefixScan) <= kStages * kTileBytes, "shared memory");
 };
 
 template <int DH, typename T, class W>
@@ -66,15 +66,13 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if ((base - raw) + (uint32_t)Cfg::kUsedBytes > p.smem_bytes) {           // uniform: nothing has been set up yet
         if (tid == 0) atomicExch(p.w.err_flag, kErrTreeWait);
-        if (tid == 0) {
-            reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x].last_cta = -1;
-            tree_front(p.scratch)[blockIdx.x] = 0;
-        }
+        if (tid == 0) tree_announce<W>(p.scratch, false);
         return;
     }
     const uint32_t bars = base + Cfg::kOffBar;
     auto ring_full = [&](int s) { return bars + 8u * s; };
     auto ring_empty = [&](int s) { return bars + 8u * (NS + s); };
+    // (parts of a shared prefix: the queries of group g are there)
     const uint32_t q_full = bars + 8u * (2 * NS), q_empty = q_full + 8u;
     auto s_full = [&](int g) { return bars + 8u * (2 * NS + 2 + g); };
     auto p_full = [&](int g) { return bars + 8u * (2 * NS + 4 + g); };
@@ -89,7 +87,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
 
     if (tid < Cfg::kBars) {
         const int i = tid - 2 * NS;              // one barrier a thread; a group's four warps arrive for p_full and o_empty
-        mbar_init(bars + 8u * tid, i == 4 || i == 5 || i >= 8 ? 4 : 1);
+        mbar_init(bars + 8u * tid, i == 4 || i == 5 || i >= 8 || (W::kPrefix && i >= 0 && i < 2) ? 4 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (tid < 4) odd_piece[tid] = 0;
@@ -99,12 +97,9 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         tmem_alloc(base + Cfg::kOffMisc, 512);
         tmem_relinquish();
     }
-    grid_dependency_wait();                    // lengths, queries and the drafts' keys come from the kernels before
-    tree_find_run(p.w, part, run);
-    if (tid == 0) {
-        reinterpret_cast<TreeTail*>(p.scratch)[blockIdx.x].last_cta = -1;
-        tree_front(p.scratch)[blockIdx.x] = run->begin < run->end && !run->at.item_begins();
-    }
+    tree_start(p.w, part, run, sp + Cfg::kOffRing);            // lengths, queries and the drafts' keys come from the kernels before
+    if (tid == 0) tree_announce<W>(p.scratch, run->begin < run->end && !run->at.item_begins());
+    if (W::kPrefix) fence_async_smem();        // the scan lay where tiles will
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -116,14 +111,21 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
 
     if (warp == 0 && n_tiles > 0) {
         tree_load_keys<DH, NS, 0>(p, &map_k, &map_v, run, base + Cfg::kOffRing, ring_full(0), ring_empty(0));
-    } else if (warp == 3 && n_tiles > 0) {
+    } else if (warp == 3 && n_tiles > 0 && !W::kPrefix) {
         tree_load_queries<DH, kTileRows, 32, 1, T>(p, run, sp, nullptr, 0u, q_full, q_empty, lane);
     } else if (warp == 1 && n_tiles > 0) {
         // ---------------- the products, of the groups by turns
         if (lane == 0) {
             TreeCursorT<W> c = run->at;
             uint32_t piece = 0, seq = 0, done[2] = {0, 0}, uses[2] = {0, 0};     // pieces, tiles of the ring; tiles and pieces of each group
+            uint32_t asked[2] = {0, 0};                          // pieces of each group whose queries have been waited for
             int groups = 0;
+            auto queries_there = [&](int n) {
+                if constexpr (!W::kPrefix) return mbar_poll(q_full, piece & 1u);
+                for (int g = 0; g < n; ++g)
+                    if (!mbar_poll(q_full + 8u * g, asked[g]++ & 1u)) return false;
+                return true;
+            };
             bool ok = true, first = true, last = n_tiles == 1 || c.item_ends();  // the tile opens, closes its piece
             auto scores = [&](int g, uint32_t at) {
                 tc_fence_after();
@@ -137,12 +139,12 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 umma_commit(s_full(g));
             };
             auto filled = [&](uint32_t at) { return mbar_poll(ring_full(at % NS), (at / NS) & 1u); };
-            ok = mbar_poll(q_full, 0u) && filled(0u);
+            groups = c.queries(p.w) > kRows ? 2 : 1;
+            ok = queries_there(groups) && filled(0u);
             if (ok) {
-                groups = c.queries(p.w) > kRows ? 2 : 1;
                 for (int g = 0; g < groups; ++g) scores(g, 0u);
                 umma_commit(ring_empty(0));
-                if (last) umma_commit(q_empty);
+                if (last && !W::kPrefix) umma_commit(q_empty);
                 piece = seq = 1;
             }
             // O += P V of this tile, then S of the next - over the weights: the products of one thread run in order - for one group,
@@ -184,13 +186,13 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 }
                 if (!ok) break;
                 if (more && next_opens) {                        // other queries: behind the last products with the ones before
-                    if (!mbar_poll(q_full, piece & 1u) || !filled(k_at)) { ok = false; break; }
+                    if (!queries_there(next_groups) || !filled(k_at)) { ok = false; break; }
                     ++piece;
                     for (int g = 0; g < next_groups; ++g) scores(g, k_at);
                 }
                 if (more) {
                     umma_commit(ring_empty(k_at % NS));
-                    if (next_last) umma_commit(q_empty);
+                    if (next_last && !W::kPrefix) umma_commit(q_empty);
                 }
                 seq += 2;
                 groups = next_groups;
@@ -211,6 +213,26 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         uint32_t piece = 0, done = 0, uses = 0;                  // pieces; tiles and pieces of this group
         const uint32_t* mask = nullptr;
         auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_poll(bar, parity)) != 0; };
+        // Parts of a shared prefix: pieces are short, so the group brings its own queries, a row to a thread, as soon as the products with the rows before have
+        // run (one warp for all 256 rows takes 8 us).
+        auto bring_queries = [&](const TreeCursorT<W>& at) {
+            const int first = at.first_query(p.w) + g * kRows, n = min(kRows, at.queries(p.w) - g * kRows);
+            if (n <= 0) return;
+            if (row < n) {
+                const int token = (first + row) / p.w.group, head = first + row - token * p.w.group;
+                const T* src = static_cast<const T*>(p.q) + (int64_t)(at.r.row0 + token) * p.q_stride + (int64_t)(at.h * p.w.group + head) * DH;
+                uint8_t* dst = sp + (g * kRows + row) * 128;
+                uint4 x[DH / 8];
+#pragma unroll
+                for (int i = 0; i < DH / 8; ++i) x[i] = __ldg(reinterpret_cast<const uint4*>(src) + i);
+#pragma unroll
+                for (int i = 0; i < DH / 8; ++i) *reinterpret_cast<uint4*>(dst + (i >> 3) * (kTileRows * 128) + (((i & 7) ^ (row & 7)) << 4)) = x[i];
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_full + 8u * g);
+        };
+        if (W::kPrefix) bring_queries(c);
         for (int t = 0; t < n_tiles && ok; ++t) {
             if (opens) {
                 q0 = c.first_query(p.w) + g * kRows;
@@ -328,6 +350,11 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full(g));
+                if (W::kPrefix && piece_ends && t + 1 < n_tiles) {
+                    TreeCursorT<W> after = c;
+                    after.next(p.w);
+                    bring_queries(after);
+                }
                 if (piece_ends) {
                     if (!wait_all(o_full(g), uses & 1u)) { ok = false; break; }
                     ++uses;
@@ -393,6 +420,11 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
                     if (lane == 0) mbar_arrive(o_empty(g));
                 }
             }
+            if (W::kPrefix && nq <= 0 && piece_ends && t + 1 < n_tiles) {        // (the group sat this piece out)
+                TreeCursorT<W> after = c;
+                after.next(p.w);
+                bring_queries(after);
+            }
             if (piece_ends) {
                 if (!W::kPrefix && !item_ends && !split_front && tid == 128) {  // begins here, goes on in the next CTAs
                     TreeTail tl{};
@@ -416,6 +448,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
+    tree_finish(p.w);
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------
@@ -463,11 +496,11 @@ int combine_launch(const TcParams& p, int grid, int y, cudaStream_t s) {
 
 // Everything but the tiles: p.w's own fields, what the kernels need to know of the cache, and the tensor maps of K and V.
 template <class W>
-static int tc_params(const TreeAttnArgs& a, TcParamsT<W>& p, CUtensorMap& map_k, CUtensorMap& map_v) {
+static int tc_params(const TreeAttnArgs& a, int tile_keys, TcParamsT<W>& p, CUtensorMap& map_k, CUtensorMap& map_v) {
     static_cast<TreeWork&>(p.w) = TreeWork{a.kv_len, a.row_start, a.block_table, a.batch, a.rows, a.cache.n_kv_heads, a.max_pages, a.cache.page_size,
                                            a.n_heads / a.cache.n_kv_heads, 0, kKeys, 4, a.err_flag};
     p.q = a.q; p.q_stride = a.q_stride;
-    p.box_keys = a.cache.page_size < kKeys ? a.cache.page_size : kKeys;
+    p.box_keys = a.cache.page_size < tile_keys ? a.cache.page_size : tile_keys;
     p.n_pages = a.cache.n_pages; p.mask_words = a.mask_words; p.tree_mask = a.tree_mask;
     p.scale_log2 = (float)(1.4426950408889634 * (double)a.scale);
     p.out = a.out; p.out_stride = a.out_stride; p.scratch = a.scratch;
@@ -497,25 +530,33 @@ static int tc_kernel(const TcParamsT<W>& p, const CUtensorMap& map_k, const CUte
     return dh == 64 ? tc_launch<64, __half>(p, map_k, map_v, grid, s, dependent) : tc_launch<128, __half>(p, map_k, map_v, grid, s, dependent);
 }
 
-int launch_prefix_tc(const PrefixAttnArgs& a, const PrefixScratch& at, int tile_shared, int tile_own, cudaStream_t s, bool dependent) {
+int launch_prefix_tc(const PrefixAttnArgs& a, const PrefixScratch& at, const int (&tile)[2], cudaStream_t s, bool dependent) {
     const int dh = a.t.cache.d_head, type = a.t.cache.type, grid = tree_grid(), parts = a.groups + a.t.batch;
-    TcParamsT<PrefixWork> p{};
-    alignas(64) CUtensorMap map_k, map_v;
-    if (int rc = tc_params(a.t, p, map_k, map_v)) return rc;
-    const int nq = tc_tile(tile_shared), nq_own = tc_tile(tile_own);
-    const bool one = nq == nq_own;
-    p.w.tile_rows = nq < kRows ? nq : kTileRows;
-    prefix_work(a, at, 0, one ? parts : a.groups, p.w);
-    p.scratch = at.pieces[0];
-    if (int rc = tc_kernel(p, map_k, map_v, dh, type, nq, grid, s, dependent)) return rc;
-    count_launch();
-    if (one) return ZOQAT_OK;
-    p.w.tile_rows = nq_own < kRows ? nq_own : kTileRows;
-    prefix_work(a, at, a.groups, a.t.batch, p.w);
-    p.scratch = at.pieces[1];
-    const int rc = tc_kernel(p, map_k, map_v, dh, type, nq_own, grid, s, true);
-    if (rc == ZOQAT_OK) count_launch();
-    return rc;
+    const bool one = tile[0] == tile[1];
+    for (int side = 0; side < (one ? 1 : 2); ++side) {
+        TcParamsT<PrefixWork> p{};
+        alignas(64) CUtensorMap map_k, map_v;
+        if (int rc = tc_params(a.t, tile[side] <= kNarrowRows ? kNarrowKeys : kKeys, p, map_k, map_v)) return rc;
+        p.w.tile_rows = tile[side];
+        prefix_work(a, at, side ? a.groups : 0, one ? parts : (side ? a.t.batch : a.groups), p.w);
+        p.w.late_wait = side == 1;
+        p.scratch = at.pieces[side];
+        int rc;
+        if (tile[side] <= kNarrowRows) {
+            p.w.key_tile = kNarrowKeys;
+            // opening and closing a part in the time of two tiles of 16 keys
+            p.w.item_cost = 2;
+            rc = launch_prefix_narrow(p, map_k, map_v, dh, type, grid, s, dependent);
+        } else {
+            p.w.key_tile = kKeys;
+            p.w.item_cost = 4;
+            rc = tc_kernel(p, map_k, map_v, dh, type, tile[side] < kTileRows ? tile[side] : kRows, grid, s, dependent);
+            count_launch();
+        }
+        if (rc != ZOQAT_OK) return rc;
+        dependent = true;
+    }
+    return ZOQAT_OK;
 }
 
 int launch_tree_attention_tc(const TreeAttnArgs& a, cudaStream_t s, bool dependent) {
@@ -532,7 +573,7 @@ int launch_tree_attention_tc(const TreeAttnArgs& a, cudaStream_t s, bool depende
     const long long want = a.rows <= a.batch ? group : (3 * drafts + 2 * a.batch - 1) / (2 * a.batch);     // 1.5 x the average
     const int nq = tc_tile(want);
     alignas(64) CUtensorMap map_k, map_v;
-    if (int rc = tc_params(a, p, map_k, map_v)) return rc;
+    if (int rc = tc_params(a, kKeys, p, map_k, map_v)) return rc;
     p.w.tile_rows = nq < kRows ? nq : kTileRows;
     const int grid = tree_grid();
     const int y = want < 2 ? 1 : (want < 32 ? (int)(want + 1) / 2 : 16);      // CTAs that share the queries of a split item
