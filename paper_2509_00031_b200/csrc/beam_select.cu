@@ -9,9 +9,9 @@
 // A cluster of up to 8 CTAs serves a request: a CTA takes whole rows, or a slice of one where there are few.  Of a row's first few thousand
 // logits every warp knows its largest few: the least of those is a bound that at least as many logits pass as are wanted.  What passes it
 // goes to a buffer, whose sorted best (each key counts the larger ones) set the exact bound for the rest of the row; a logit that
-// passes that is rare, so the stream costs a maximum, an exponential and two additions each.  Keys are (logit, token) in 64 bits: no two are equal, and
-// of equal logits the lower token wins.  Should the buffer ever run over (long runs of rising or equal logits), the row's bound is found
-// digit by digit from histograms instead.
+// passes that is rare, so the stream costs a maximum, an exponential and two additions each, sixteen bytes at a time, the next on their way while some are
+// worked on.  Keys are (logit, token) in 64 bits: no two are equal, and of equal logits the lower token wins.  Should the buffer ever run over (long runs
+// of rising or equal logits), the row's bound is found digit by digit from histograms instead.
 // Sums: every thread has its own reference (the largest logit it met when it last moved), partial sums are fp32, the row's logarithm and all scores are formed in
 // 64 bits, so that scores of different beams are compared before anything is rounded.  Scores are rounded to fp32 once.
 #include "common.cuh"
@@ -19,17 +19,17 @@
 #include "tc_ptx.cuh"
 #include <cuda_fp16.h>
 #include <float.h>
+#include <type_traits>
 
 namespace zq {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kCluster = 8;
 constexpr int kMaxEos = kMaxBeamEos, kMaxBest = kMaxBeams + kMaxEos;       // best logits of a row
-constexpr int kMaxRows = kMaxBeams / kCluster;                   // rows of a CTA
-constexpr int kBuffer = 2048;
+constexpr int kBuffer = 2048, kMaxCandidates = kMaxBeams * kMaxBest;       // (a row in several slices: at most 8 rows' worth)
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.69314718055994530942;
-static_assert(kMaxBeams * kMaxBest <= kBuffer && kMaxBeams * (1 + kMaxEos) <= 256, "the candidates of a request fit");
+static_assert(kMaxBeams * (1 + kMaxEos) <= 256, "the best of a request");
 
 typedef unsigned long long u64;
 
@@ -59,7 +59,34 @@ __device__ __forceinline__ u64 ld_cluster_u64(uint32_t addr) {
 }
 
 template <typename T> __device__ __forceinline__ float value(T v) { return static_cast<float>(v); }
+// VEC logits at a time: 16 bytes where the rows allow it, else single ones
 template <typename T, int VEC> struct alignas(VEC * sizeof(T)) Vec { T v[VEC]; };
+// the largest; NaN does not count
+template <typename T, int VEC> __device__ __forceinline__ float largest(const Vec<T, VEC>& x) {
+    if constexpr (VEC == 1) return value(x.v[0]);
+    else if constexpr (sizeof(T) == 4) return fmaxf(fmaxf(x.v[0], x.v[1]), fmaxf(x.v[2], x.v[3]));
+    else {
+        typedef typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type T2;
+        const T2* y = reinterpret_cast<const T2*>(x.v);
+        const T2 m = __hmax2(__hmax2(y[0], y[1]), __hmax2(y[2], y[3]));
+        return fmaxf(value(m.x), value(m.y));
+    }
+}
+// sum += 2^(x log2 e - ref2), over pairs
+template <typename T, int VEC> __device__ __forceinline__ void add_powers(const Vec<T, VEC>& x, float ref2, float2& sum) {
+    if constexpr (VEC == 1) {
+        sum.x += ex2(fmaf(value(x.v[0]), kLog2e, -ref2));
+    } else {
+        const float2 scale = make_float2(kLog2e, kLog2e), minus = make_float2(-ref2, -ref2);
+#pragma unroll
+        for (int e = 0; e < VEC; e += 2) {
+            float2 y = tree_fma2(make_float2(value(x.v[e]), value(x.v[e + 1])), scale, minus);
+            y.x = ex2(y.x);
+            y.y = ex2(y.y);
+            sum = tree_add2(sum, y);
+        }
+    }
+}
 
 struct Params {
     BeamSelectArgs a;
@@ -69,9 +96,9 @@ struct Params {
 
 struct Shared {
     u64 buf[kBuffer];
-    u64 best[kMaxRows][kMaxBest];            // a row's best keys, in order; 0: none
+    u64 best[kMaxCandidates];                // a row's best keys in order, row after row of this CTA; 0: none
+    u64 stat[kMaxBeams];                     // (reference, sum) of a row's slice as two floats
     double lse[kMaxBeams];
-    u64 stat[kMaxRows];                      // (reference, sum) of a row's slice as two floats
     float ref[kWarps], sum[kWarps];
     uint32_t bound[kWarps];
     int top[kMaxBeams * (1 + kMaxEos)];
@@ -95,54 +122,52 @@ __device__ __forceinline__ void sort_best(const u64* buf, int m, u64* to, int n)
 }
 
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads, 4)
+__global__ void __launch_bounds__(kThreads, 3)
 beam_select_kernel(const Params p) {
-    constexpr int kFly = VEC == 1 ? 8 : 4;                       // vectors of a thread in flight
+    constexpr int kFly = VEC == 1 ? 8 : 4, kRound = kFly * kThreads;       // vectors of a thread in flight, vectors of a round
     __shared__ Shared sh;
     const BeamSelectArgs& a = p.a;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = (int)cluster_ctarank(), request = blockIdx.x / (p.in_parallel * p.slices);
-    const int n = p.best, lo = (rank % p.slices) * p.slice, size = min(a.vocab, lo + p.slice) - lo;      // (size <= 0: an empty slice)
-    const int n_vec = size > 0 ? (size + VEC - 1) / VEC : 0;
+    const int n = p.best, lo = (rank % p.slices) * p.slice, size = max(0, min(a.vocab, lo + p.slice) - lo);
+    const int n_vec = (size + VEC - 1) / VEC, n_whole = size / VEC;
     if (tid < a.n_eos) sh.eos[tid] = __ldg(a.eos + tid);
 
-    int mine = 0;                                                // rows of this CTA
+    auto row_of = [&](int row) { return static_cast<const T*>(a.logits) + ((int64_t)request * a.beams + row) * a.ld + lo; };
+    typedef Vec<T, VEC> V;
+    auto fetch = [&](V (&x)[kFly], const T* src, int base) {     // vectors base + u * kThreads + tid; -inf behind the slice
+        const V* at = reinterpret_cast<const V*>(src) + base + tid;
+        if (base + kRound <= n_whole) {
+#pragma unroll
+            for (int u = 0; u < kFly; ++u) x[u] = at[u * kThreads];
+            return;
+        }
+#pragma unroll
+        for (int u = 0; u < kFly; ++u) {
+            const int i = base + u * kThreads + tid;
+            if (i < n_whole) { x[u] = at[u * kThreads]; continue; }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) x[u].v[e] = i * VEC + e < size ? src[i * VEC + e] : T(-INFINITY);
+        }
+    };
+    auto push = [&](u64 key) {
+        const int at = atomicAdd(&sh.count, 1);
+        if (at < kBuffer) sh.buf[at] = key;
+    };
+    V now[kFly], ahead[kFly];
+    int mine = 0;                                                // rows of this CTA so far
+    if (rank / p.slices < a.beams) fetch(now, row_of(rank / p.slices), 0);
     for (int row = rank / p.slices; row < a.beams; row += p.in_parallel, ++mine) {
-        const T* src = static_cast<const T*>(a.logits) + ((int64_t)request * a.beams + row) * a.ld + lo;
-        Vec<T, VEC> raw[kFly];
-        auto fetch = [&](int base) {
-#pragma unroll
-            for (int u = 0; u < kFly; ++u) {
-                const int i = base + u * kThreads + tid;
-                if (i >= n_vec) continue;
-                if ((i + 1) * VEC <= size) raw[u] = *reinterpret_cast<const Vec<T, VEC>*>(src + (int64_t)i * VEC);
-                else
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) raw[u].v[e] = i * VEC + e < size ? src[i * VEC + e] : T(-INFINITY);
-            }
-        };
-        auto largest = [&](int u, int base) {
-            float m = -INFINITY;
-            if (base + u * kThreads + tid < n_vec) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) m = fmaxf(m, value(raw[u].v[e]));          // (NaN does not count)
-            }
-            return m;
-        };
-        auto push = [&](u64 key) {
-            const int at = atomicAdd(&sh.count, 1);
-            if (at < kBuffer) sh.buf[at] = key;
-        };
+        const T* src = row_of(row);
+        u64* const best = sh.best + mine * n;
         __syncthreads();                                         // the row before is through with the shared words
         if (tid == 0) sh.count = 0;
 
-        // the first vectors: bound and reference
-        constexpr int kFirst = kFly * kThreads;
-        fetch(0);
+        // the first round: bound and reference.  Full warps take part; each offers its `each`-th largest thread
         float top = -INFINITY;
 #pragma unroll
-        for (int u = 0; u < kFly; ++u) top = fmaxf(top, largest(u, 0));
-        // full warps take part; each offers its `each`-th largest thread
+        for (int u = 0; u < kFly; ++u) top = fmaxf(top, largest(now[u]));
+        if (kRound < n_vec) fetch(ahead, src, kRound);
         const int full = min(kWarps, n_vec >> 5), each = full ? (n + full - 1) / full : 33;
         uint32_t k = ordered(top), offer = 0, high = 0;
         for (int i = 0; i < each && i < 4; ++i) {
@@ -163,54 +188,70 @@ beam_select_kernel(const Params p) {
         ref = fminf(ref, FLT_MAX);
         float limit = each > 4 ? -INFINITY : unordered(bound);
         if (!(limit > -INFINITY)) limit = -FLT_MAX;              // everything but -inf
-        float ref2 = __fmul_rn(ref, kLog2e), sum = 0.0f;
-        auto add = [&](int u, int base) {
-            if (base + u * kThreads + tid >= n_vec) return;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) sum += ex2(fmaf(value(raw[u].v[e]), kLog2e, -ref2));
-        };
+        float ref2 = __fmul_rn(ref, kLog2e);
+        float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int u = 0; u < kFly; ++u) {
-            if (largest(u, 0) >= limit) {
+            if (largest(now[u]) >= limit) {
                 const int token = lo + (u * kThreads + tid) * VEC;
 #pragma unroll
                 for (int e = 0; e < VEC; ++e)
-                    if (value(raw[u].v[e]) >= limit) push(key_of(value(raw[u].v[e]), token + e));
+                    if (value(now[u].v[e]) >= limit) push(key_of(value(now[u].v[e]), token + e));
             }
-            add(u, 0);
+            add_powers(now[u], ref2, sum);
         }
         __syncthreads();
         // the rest: what passes the n-th best so far (a later token loses against an equal logit)
-        if (n_vec > kFirst && sh.count <= kBuffer) {
-            const int m = sh.count;
-            sort_best(sh.buf, m, sh.best[mine], n);
-            const u64 nth = sh.best[mine][n - 1];
-            limit = nth ? unordered((uint32_t)(nth >> 32)) : -INFINITY;
-            for (int i = tid; i < n; i += kThreads) sh.buf[i] = sh.best[mine][i];
-            if (tid == 0) sh.count = min(m, n);
-            __syncthreads();
-            for (int base = kFirst; base < n_vec; base += kFirst) {
-                fetch(base);
+        if (n_vec > kRound && sh.count <= kBuffer) {
+            auto tighten = [&]() {
+                const int m = sh.count;
+                sort_best(sh.buf, m, best, n);
+                const u64 nth = best[n - 1];
+                limit = nth ? unordered((uint32_t)(nth >> 32)) : -INFINITY;
+                for (int i = tid; i < n; i += kThreads) sh.buf[i] = best[i];
+                if (tid == 0) sh.count = min(m, n);
+                __syncthreads();
+            };
+            tighten();
+            auto work = [&](const V (&x)[kFly], int base) {
+                float m4 = largest(x[0]);
 #pragma unroll
-                for (int u = 0; u < kFly; ++u) {
-                    const float m4 = largest(u, base);
-                    if (m4 > limit) {
-                        const int token = lo + (base + u * kThreads + tid) * VEC;
+                for (int u = 1; u < kFly; ++u) m4 = fmaxf(m4, largest(x[u]));
+                if (m4 > limit) {
+                    const int token = lo + (base + tid) * VEC;
+#pragma unroll
+                    for (int u = 0; u < kFly; ++u) {
+                        if (!(largest(x[u]) > limit)) continue;
 #pragma unroll
                         for (int e = 0; e < VEC; ++e)
-                            if (value(raw[u].v[e]) > limit) push(key_of(value(raw[u].v[e]), token + e));
-                        if (m4 > ref) {                          // the reference moves (no logit above it has been met: limit <= reference)
-                            ref = fminf(m4, FLT_MAX);
-                            const float to = __fmul_rn(ref, kLog2e);
-                            sum *= ex2(ref2 - to);
-                            ref2 = to;
-                        }
+                            if (value(x[u].v[e]) > limit) push(key_of(value(x[u].v[e]), token + u * kThreads * VEC + e));
                     }
-                    add(u, base);
+                    if (m4 > ref) {                              // the reference moves (no logit above it has been met: limit <= reference)
+                        ref = fminf(m4, FLT_MAX);
+                        const float to = __fmul_rn(ref, kLog2e), f = ex2(ref2 - to);
+                        sum.x *= f;
+                        sum.y *= f;
+                        ref2 = to;
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < kFly; ++u) add_powers(x[u], ref2, sum);
+            };
+            for (int base = kRound; base < n_vec; base += 2 * kRound) {
+                if (base + kRound < n_vec) fetch(now, src, base + kRound);
+                work(ahead, base);
+                if (base + kRound >= n_vec) break;
+                if (base + 2 * kRound < n_vec) fetch(ahead, src, base + 2 * kRound);
+                work(now, base + kRound);
+                // once more where most of the row is still to come (a bound from a k-th of it lets n (k - 1) of the rest pass)
+                if (base == kRound && n_vec > 8 * kRound) {
+                    __syncthreads();
+                    if (sh.count <= kBuffer) tighten();
                 }
             }
             __syncthreads();
         }
+        if (row + p.in_parallel < a.beams) fetch(now, row_of(row + p.in_parallel), 0);
         auto each_key = [&](auto f) {                            // every key of the slice again
             for (int i = tid; i < size; i += kThreads) {
                 const u64 key = key_of(value(src[i]), lo + i);
@@ -245,9 +286,8 @@ beam_select_kernel(const Params p) {
             each_key([&](u64 key) { if (key >= prefix) push(key); });
             __syncthreads();
         }
-        sort_best(sh.buf, sh.count, sh.best[mine], n);
         // the row's sum, relative to 2^(fl(reference * log2 e))
-        float x[2] = {ref, sum};
+        float x[2] = {ref, sum.x + sum.y};
         auto join = [&](float om, float os) {
             const float t = fmaxf(x[0], om), t2 = __fmul_rn(t, kLog2e);
             x[1] = x[1] * ex2(__fmul_rn(x[0], kLog2e) - t2) + os * ex2(__fmul_rn(om, kLog2e) - t2);
@@ -256,14 +296,14 @@ beam_select_kernel(const Params p) {
 #pragma unroll
         for (int o = 16; o >= 1; o >>= 1) join(__shfl_xor_sync(0xffffffffu, x[0], o), __shfl_xor_sync(0xffffffffu, x[1], o));
         if (lane == 0) { sh.ref[warp] = x[0]; sh.sum[warp] = x[1]; }
-        __syncthreads();
+        sort_best(sh.buf, sh.count, best, n);
         x[0] = sh.ref[0]; x[1] = sh.sum[0];
         for (int w = 1; w < kWarps; ++w) join(sh.ref[w], sh.sum[w]);
         // Once more, with care: where the stream was left out above, NaN and +inf, logits near either end of the range.  Relative to
         // the largest logit itself, which a negative sign says.
         if (again || !(x[1] > 0.0f && x[1] < INFINITY && x[0] < 1e37f)) {
             __syncthreads();
-            const u64 first = sh.best[mine][0];
+            const u64 first = best[0];
             x[0] = first ? unordered((uint32_t)(first >> 32)) : 0.0f;
             x[1] = 0.0f;
             for (int i = tid; first && i < size; i += kThreads) {
@@ -280,92 +320,99 @@ beam_select_kernel(const Params p) {
         if (tid == 0) sh.stat[mine] = (u64)__float_as_uint(x[1]) << 32 | __float_as_uint(x[0]);
     }
 
-    // the request: rank 0 gathers
+    // the request: rank 0 gathers keys and sums, the other CTAs stay until they have been read
     __syncthreads();
     cluster_sync_all();
+    const int per_row = p.slices * n, total = a.beams * per_row;
+    u64* const keys = sh.buf;
+    static_assert(kMaxCandidates <= kBuffer && kCluster * (kCluster + kMaxEos) <= kMaxCandidates, "the candidates of a request fit");
     if (rank == 0) {
-        const int per_row = p.slices * n, total = a.beams * per_row;
-        u64* keys = sh.buf;                                      // scores
+        for (int i = tid; i < total; i += kThreads) {
+            const int row = i / per_row, rest = i - row * per_row, s = rest / n;
+            keys[i] = ld_cluster_u64(mapa_shared(smem_u32(sh.best + row / p.in_parallel * n + rest - s * n), (row % p.in_parallel) * p.slices + s));
+        }
         if (tid < a.beams) {
             double top = -INFINITY, sum = 0.0;
+            u64 w[kCluster];
+            for (int s = 0; s < p.slices; ++s) w[s] = ld_cluster_u64(mapa_shared(smem_u32(sh.stat + tid / p.in_parallel), (tid % p.in_parallel) * p.slices + s));
             for (int pass = 0; pass < 2; ++pass)
                 for (int s = 0; s < p.slices; ++s) {
-                    const u64 w = ld_cluster_u64(mapa_shared(smem_u32(&sh.stat[tid / p.in_parallel]), (tid % p.in_parallel) * p.slices + s));
-                    const float r = __uint_as_float((uint32_t)w), v = __uint_as_float((uint32_t)(w >> 32));
+                    const float r = __uint_as_float((uint32_t)w[s]), v = __uint_as_float((uint32_t)(w[s] >> 32));
                     if (v == 0.0f) continue;
                     // what the rounding of reference * log2 e moved is put back here
                     const double at = v < 0.0f ? (double)r : (double)r + kLn2 * ((double)__fmul_rn(r, kLog2e) - (double)r * (double)kLog2e);
                     if (pass == 0) top = fmax(top, at);
-                    else sum += fabs((double)v) * exp(at - top);
+                    else sum += fabs((double)v) * (p.slices > 1 ? exp(at - top) : 1.0);
                 }
             sh.lse[tid] = sum > 0.0 ? top + log(sum) : INFINITY;
         }
-        __syncthreads();
-        auto candidate = [&](int i) {
-            const int row = i / per_row, rest = i - row * per_row, s = rest / n;
-            return ld_cluster_u64(mapa_shared(smem_u32(&sh.best[row / p.in_parallel][rest - s * n]), (row % p.in_parallel) * p.slices + s));
-        };
-        auto score_of = [&](int i, u64 key) {
-            const int row = i / per_row;
-            return (double)__ldg(a.score + (int64_t)request * a.beams + row) + ((double)unordered((uint32_t)(key >> 32)) - sh.lse[row]);
-        };
-        for (int i = tid; i < total; i += kThreads) {
-            const u64 key = candidate(i);
-            const double sc = key ? score_of(i, key) : -INFINITY;
-            keys[i] = sc > -INFINITY ? ordered64(sc) : 0ull;
-        }
-        const int most = a.beams * (1 + a.n_eos);
-        for (int i = tid; i < most; i += kThreads) sh.top[i] = -1;
-        __syncthreads();
-        for (int i = tid; i < total; i += kThreads) {
-            const u64 key = keys[i];
-            if (!key) continue;
-            int r = 0;
-            for (int j = 0; j < total; ++j) r += keys[j] > key || (keys[j] == key && j < i);
-            if (r < most) sh.top[r] = i;
-        }
-        __syncthreads();
-        // those that go on, those that are finished: each counts the ones of its kind before it
-        auto ends = [&](int i) {
-            const int token = (int)~(uint32_t)candidate(i);
+    }
+    cluster_sync_all();
+    if (rank != 0) return;
+    auto score_of = [&](int i) {
+        const int row = i / per_row;
+        return (double)__ldg(a.score + (int64_t)request * a.beams + row) + ((double)unordered((uint32_t)(keys[i] >> 32)) - sh.lse[row]);
+    };
+    u64* const order = sh.best;                                  // (all have read their keys)
+    for (int i = tid; i < total; i += kThreads) {
+        const double sc = keys[i] ? score_of(i) : -INFINITY;
+        order[i] = sc > -INFINITY ? ordered64(sc) : 0ull;
+    }
+    const int most = a.beams * (1 + a.n_eos);
+    for (int i = tid; i < most; i += kThreads) sh.top[i] = -1;
+    __syncthreads();
+    for (int i = tid; i < total; i += kThreads) {
+        const u64 key = order[i];
+        if (!key) continue;
+        int r = 0;
+        for (int j = 0; j < total; ++j) r += order[j] > key || (order[j] == key && j < i);
+        if (r < most) sh.top[r] = i;
+    }
+    __syncthreads();
+    // those that go on, those that are finished: each counts the ones of its kind before it
+    int* kind = sh.hist;                                         // 0 none, 1 goes on, 2 finished
+    for (int r = tid; r < most; r += kThreads) {
+        int is = 0;
+        if (sh.top[r] >= 0) {
+            const int token = (int)~(uint32_t)keys[sh.top[r]];
+            is = 1;
             for (int e = 0; e < a.n_eos; ++e)
-                if (sh.eos[e] == token) return true;
-            return false;
-        };
-        int* kind = sh.hist;                                     // 0 none, 1 goes on, 2 finished
-        for (int r = tid; r < most; r += kThreads) kind[r] = sh.top[r] < 0 ? 0 : (ends(sh.top[r]) ? 2 : 1);
-        __syncthreads();
-        const int64_t out = (int64_t)request * a.beams;
-        for (int r = tid; r < a.beams; r += kThreads) {          // slots that stay empty
-            int on = 0, done = 0;
-            for (int j = 0; j < most; ++j) { on += kind[j] == 1; done += j < a.beams && kind[j] == 2; }
+                if (sh.eos[e] == token) is = 2;
+            if (is == 2 && r >= a.beams) is = 0;
+        }
+        kind[r] = is;
+    }
+    __syncthreads();
+    const int64_t out = (int64_t)request * a.beams;
+    for (int r = tid; r < most; r += kThreads) {
+        const int is = kind[r];
+        int at = 0, on = 0, done = 0;
+        for (int j = 0; j < most; ++j) {
+            at += j < r && kind[j] == is;
+            on += kind[j] == 1;
+            done += kind[j] == 2;
+        }
+        if (r < a.beams) {                                       // slots that stay empty
             if (r >= on) { a.beam[out + r] = -1; a.token[out + r] = -1; a.score_out[out + r] = -INFINITY; }
             if (r >= done) { a.done_beam[out + r] = -1; a.done_token[out + r] = -1; a.done_score[out + r] = -INFINITY; }
         }
-        for (int r = tid; r < most; r += kThreads) {
-            const int is = kind[r];
-            if (is == 0 || (is == 2 && r >= a.beams)) continue;
-            int at = 0;
-            for (int j = 0; j < r; ++j) at += kind[j] == is;
-            if (at >= a.beams) continue;
-            const int i = sh.top[r];
-            const u64 key = candidate(i);
-            (is == 1 ? a.beam : a.done_beam)[out + at] = i / per_row;
-            (is == 1 ? a.token : a.done_token)[out + at] = (int)~(uint32_t)key;
-            (is == 1 ? a.score_out : a.done_score)[out + at] = (float)score_of(i, key);
-        }
+        if (is == 0 || at >= a.beams) continue;
+        const int i = sh.top[r];
+        (is == 1 ? a.beam : a.done_beam)[out + at] = i / per_row;
+        (is == 1 ? a.token : a.done_token)[out + at] = (int)~(uint32_t)keys[i];
+        (is == 1 ? a.score_out : a.done_score)[out + at] = (float)score_of(i);
     }
-    cluster_sync_all();                                          // a CTA's words stay until rank 0 has read them
 }
 
 template <typename T, int VEC>
 int launch_vec(const BeamSelectArgs& a, cudaStream_t s) {
     Params p{a, 0, 0, 0, 0};
-    // whole rows in parallel first; slices only while the SMs are not filled, and of two thousand tokens at least
-    const int rounds = (a.beams + kCluster - 1) / kCluster;
-    p.in_parallel = (a.beams + rounds - 1) / rounds;
+    // Whole rows in parallel, as many as keep all CTAs resident (three to an SM: with more, clusters wait for one another); slices only while
+    // the SMs are not filled, and of two thousand tokens at least.
+    int rounds = (a.beams + kCluster - 1) / kCluster;
+    for (p.in_parallel = (a.beams + rounds - 1) / rounds; p.in_parallel > 1 && (int64_t)a.batch * p.in_parallel > 148 * 3; p.in_parallel = (a.beams + rounds - 1) / rounds) ++rounds;
     p.slices = 1;
-    while ((p.slices + 1) * p.in_parallel <= kCluster && a.batch * p.in_parallel * p.slices < 148 * 4 && a.vocab >= 2048 * (p.slices + 1)) ++p.slices;
+    while ((p.slices + 1) * p.in_parallel <= kCluster && (int64_t)a.batch * p.in_parallel * (p.slices + 1) <= 148 * 3 && a.vocab >= 2048 * (p.slices + 1)) ++p.slices;
     p.slice = ((a.vocab + p.slices - 1) / p.slices + VEC - 1) / VEC * VEC;
     p.best = a.beams + a.n_eos < a.vocab ? a.beams + a.n_eos : a.vocab;
     const int ranks = p.in_parallel * p.slices;
