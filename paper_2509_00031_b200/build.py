@@ -14,7 +14,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libzoqat.so")
 SOURCES = ["api.cu", "weights.cu", "activations.cu", "attention.cu", "attention_tc.cu", "gemm_simt.cu", "gemm_tc.cu", "decode.cu",
            "serve_plan.cu", "tree_attention.cu", "tree_attention_tc.cu", "tree_attention_keys.cu", "logit_rules.cu",
-           "rotary_append.cu", "prefix_attention.cu", "prefix_narrow.cu", "beam_select.cu", "beam_reorder.cu"]
+           "rotary_append.cu", "prefix_attention.cu", "prefix_narrow.cu", "prefix_narrow_f32.cu", "beam_select.cu", "beam_reorder.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 

@@ -124,8 +124,12 @@ PrefixScratch prefix_scratch(void* base, int type, int d_head, int64_t rows, int
     uint8_t* p = static_cast<uint8_t*>(base);
     size_t used = 0;
     auto take = [&](size_t bytes) { const size_t o = used; used += (bytes + 255) / 256 * 256; return p ? p + o : nullptr; };
-    at.pieces[0] = take(tree_attention_scratch_bytes(type, d_head));
-    at.pieces[1] = type == kTypeF32 ? at.pieces[0] : take(tree_attention_scratch_bytes(type, d_head));
+    // two slots to a worker: 148 of 256 queries, or their warps of up to 16
+    const size_t f32 = kTailBytes + 2 * (size_t)(kMaxTreeGrid / 2 * kF32Warps) * tree_slot_floats(kF32Rows, d_head) * 4;
+    const size_t narrow = kTailBytes + 2 * (size_t)kMaxWorkers * tree_slot_floats(kNarrowRows, d_head) * 4, wide = tree_attention_scratch_bytes(type, d_head);
+    const size_t pieces = type == kTypeF32 ? f32 : (narrow > wide ? narrow : wide);
+    at.pieces[0] = take(pieces);
+    at.pieces[1] = type == kTypeF32 ? at.pieces[0] : take(pieces);
     at.entries = take((size_t)rows * n_heads * 2 * sizeof(int2));
     at.partial = reinterpret_cast<float*>(take((size_t)rows * n_heads * 2 * (d_head + 4) * sizeof(float)));
     at.row_sides = reinterpret_cast<int*>(take((size_t)rows * sizeof(int)));
@@ -138,15 +142,15 @@ int launch_prefix_attention(const PrefixAttnArgs& a, void* scratch, cudaStream_t
     const PrefixScratch at = prefix_scratch(scratch, t.cache.type, t.cache.d_head, t.rows, t.n_heads);
     JoinParams p{};
     const int group = t.n_heads / t.cache.n_kv_heads;
-    static_cast<TreeWork&>(p.w) = TreeWork{t.kv_len, t.row_start, t.block_table, t.batch, t.rows, t.cache.n_kv_heads, t.max_pages, t.cache.page_size, group, 1, kSimtKeys, 0, t.err_flag};
+    static_cast<TreeWork&>(p.w) = TreeWork{t.kv_len, t.row_start, t.block_table, t.batch, t.rows, t.cache.n_kv_heads, t.max_pages, t.cache.page_size, group, 1, 1, 0, t.err_flag};
     prefix_work(a, at, 0, 0, p.w);
     p.pieces[0] = p.pieces[1] = at.pieces[0];
     p.workers[0] = p.workers[1] = tree_grid();
     p.out = t.out; p.out_stride = t.out_stride;
     if (t.cache.type == kTypeF32) {
-        p.tile_rows[0] = p.tile_rows[1] = kSimtRows;
-        p.workers[0] = p.workers[1] = 2 * tree_grid();
-        if (int rc = launch_prefix_simt(a, at, s, dependent)) return rc;
+        p.tile_rows[0] = p.tile_rows[1] = kF32Rows;
+        p.workers[0] = p.workers[1] = kF32Warps * tree_grid();
+        if (int rc = launch_prefix_f32(a, at, s, dependent)) return rc;
         return t.cache.d_head == 64 ? join<float, 64>(p, s) : join<float, 128>(p, s);
     }
     // Queries per tile from averages (the host does not know the lengths).

@@ -48,23 +48,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     return y;
 }
 
-// A cursor over tiles that looks parts up in the CTA's copies.
-struct Cursor {
-    PrefixRequest r;
-    int b, h, rt, kt;
-    __device__ __forceinline__ void next(const PrefixWork& w, const PrefixScan& scan) {
-        if (++kt < r.n_kt) return;
-        if (++rt >= r.n_rt) {
-            rt = 0;
-            if (++h >= w.n_kv) {
-                h = 0;
-                do { if (++b >= w.batch) return; prefix_load(w, scan, b, r); } while (r.n_kt == 0);
-            }
-        }
-        kt = r.kt0;
-    }
-};
-
 template <int DH, int NQ, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
 prefix_narrow_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TcParamsT<PrefixWork> p) {
@@ -93,7 +76,7 @@ prefix_narrow_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
 
     if (n_tiles > 0) {
     const uint32_t ring = ((smem_u32(smem) + 1023u) & ~1023u) + warp * (NS * Cfg::kStage), bar = smem_u32(&bars[warp][0]);
-    Cursor c, ahead;
+    PrefixCursor c, ahead;
     c.r = run.at.r; c.b = run.at.b; c.h = run.at.h; c.rt = run.at.rt; c.kt = run.at.kt;
     ahead = c;
     // the boxes of a tile (two where pages have 8 slots), looked up a tile before they are requested

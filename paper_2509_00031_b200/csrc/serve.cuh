@@ -131,7 +131,7 @@ struct PrefixAttnArgs {
 struct PrefixScratch { uint8_t* pieces[2]; void* entries; float* partial; int* row_sides; size_t bytes; };
 PrefixScratch prefix_scratch(void* base, int type, int d_head, int64_t rows, int n_heads);
 int launch_prefix_attention(const PrefixAttnArgs& a, void* scratch, cudaStream_t s, bool dependent);      // 0 or a ZOQAT_ERR_* code
-int launch_prefix_simt(const PrefixAttnArgs& a, const PrefixScratch& at, cudaStream_t s, bool dependent);
+int launch_prefix_f32(const PrefixAttnArgs& a, const PrefixScratch& at, cudaStream_t s, bool dependent);
 // tile: queries per tile of the shared and the own parts, 8, 16, 32, 64 or 256
 int launch_prefix_tc(const PrefixAttnArgs& a, const PrefixScratch& at, const int (&tile)[2], cudaStream_t s, bool dependent);
 int tree_grid();                         // CTAs of the attention kernels on the current device

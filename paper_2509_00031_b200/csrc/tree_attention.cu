@@ -19,7 +19,7 @@
 namespace zq {
 namespace {
 
-constexpr int kSimtThreads = 256, kSimtStages = 2;
+constexpr int kSimtThreads = 256, kSimtKeys = 32, kSimtRows = 8, kSimtStages = 2;
 constexpr int kWarpKeys = kSimtKeys / 8, kKeyLanes = 32 / kWarpKeys;      // keys of a tile per warp, lanes per key
 
 template <int DH> struct SimtCfg {
@@ -32,8 +32,8 @@ template <int DH> struct SimtCfg {
     static constexpr int kSmemBytes = (kOffKeys + 4 * kSimtKeys) * 4;
 };
 
-template <class W> struct SimtParamsT {
-    W w;
+struct SimtParams {
+    TreeWork w;
     const float* q;
     int64_t q_stride;
     PagedCache cache;
@@ -44,7 +44,6 @@ template <class W> struct SimtParamsT {
     int64_t out_stride;
     uint8_t* scratch;
 };
-using SimtParams = SimtParamsT<TreeWork>;
 
 __device__ __forceinline__ void cp_async16(float* dst, const float* src, bool live) {
     const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
@@ -55,15 +54,14 @@ __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commi
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // Where the keys of the cursor's tile stand in the cache, in elements; -1: behind the request's end, or on a bad page.
-template <class W>
-__device__ __forceinline__ void find_keys(const SimtParamsT<W>& p, const TreeCursorT<W>& c, int64_t* offs) {
+__device__ __forceinline__ void find_keys(const SimtParams& p, const TreeCursor& c, int64_t* offs) {
     const int key = threadIdx.x;
     if (key >= kSimtKeys) return;
     const int t = c.kt * kSimtKeys + key;
     int64_t off = -1;
     if (t < c.r.L) {
         const int pg = t / p.w.page_size;
-        const int page = __ldg(p.w.block_table + (size_t)c.r.table(c.b) * p.w.max_pages + pg);
+        const int page = __ldg(p.w.block_table + (size_t)c.b * p.w.max_pages + pg);
         if (page < 0 || page >= p.cache.n_pages) atomicExch(p.w.err_flag, kErrBadPage);
         else off = page * p.cache.page_stride + (t - pg * p.w.page_size) * p.cache.slot_stride + c.h * p.cache.head_stride;
     }
@@ -71,8 +69,8 @@ __device__ __forceinline__ void find_keys(const SimtParamsT<W>& p, const TreeCur
 }
 
 // Requests the keys and values of a tile; keys without a place become zeros.
-template <int DH, class W>
-__device__ __forceinline__ void load_tile(const SimtParamsT<W>& p, const int64_t* offs, float* stage) {
+template <int DH>
+__device__ __forceinline__ void load_tile(const SimtParams& p, const int64_t* offs, float* stage) {
     constexpr int kPer = DH / 4;                           // 16-byte chunks of a key
     constexpr int kStep = kSimtThreads / kPer;
     const int ch = threadIdx.x % kPer;
@@ -88,8 +86,8 @@ __device__ __forceinline__ void load_tile(const SimtParamsT<W>& p, const int64_t
 }
 
 // One tile for MR queries of the row tile (q0: the first).  m, l, acc: the warp's running state (l: per lane).
-template <int DH, int MR, class W>
-__device__ __forceinline__ void tile_step(const SimtParamsT<W>& p, const TreeCursorT<W>& c, int q0, int nq, const float* stage, const float* qs, float* ps,
+template <int DH, int MR>
+__device__ __forceinline__ void tile_step(const SimtParams& p, const TreeCursor& c, int q0, int nq, const float* stage, const float* qs, float* ps,
                                           float (&m)[kSimtRows], float (&l)[kSimtRows], float (&acc)[kSimtRows][DH / 32]) {
     constexpr int VPL = DH / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -108,7 +106,7 @@ __device__ __forceinline__ void tile_step(const SimtParamsT<W>& p, const TreeCur
             s[r] = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, s[r]))));
         }
     }
-    const int C = c.r.L - c.r.drafts(), t = c.kt * kSimtKeys + key;
+    const int C = c.r.L - c.r.n, t = c.kt * kSimtKeys + key;
     const bool tail = (c.kt + 1) * kSimtKeys > C;          // some of the tile's keys are drafts, or lie behind the end
     uint32_t seen[MR];                                     // bit kKeyLanes * j: key j of this warp counts for query r
 #pragma unroll
@@ -161,14 +159,14 @@ __device__ __forceinline__ void tile_step(const SimtParamsT<W>& p, const TreeCur
     __syncwarp();                                          // ps is written again by the next tile
 }
 
-template <int DH, class W>
+template <int DH>
 __global__ void __launch_bounds__(kSimtThreads, 2)
-tree_attention_simt_kernel(SimtParamsT<W> p) {
+tree_attention_simt_kernel(SimtParams p) {
     using Cfg = SimtCfg<DH>;
     constexpr int VPL = DH / 32;
     extern __shared__ __align__(16) float sm[];
     __shared__ long long part[16];
-    __shared__ TreeRunT<W> run;
+    __shared__ TreeRun run;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     float* qs = sm + Cfg::kOffQ;
     float* ps = sm + Cfg::kOffP + warp * kSimtRows * kWarpKeys;
@@ -177,11 +175,15 @@ tree_attention_simt_kernel(SimtParamsT<W> p) {
     float* l_s = m_s + 8 * kSimtRows;
     int64_t* offs = reinterpret_cast<int64_t*>(sm + Cfg::kOffKeys);
     TreeTail* tails = reinterpret_cast<TreeTail*>(p.scratch);
-    tree_start(p.w, part, &run, sm);
-    if (tid == 0) tree_announce<W>(p.scratch, run.begin < run.end && !run.at.item_begins());
-    if (run.begin >= run.end) { tree_finish(p.w); return; }
+    grid_dependency_wait();
+    tree_find_run(p.w, part, &run);
+    if (tid == 0) {
+        tails[blockIdx.x].last_cta = -1;
+        tree_front(p.scratch)[blockIdx.x] = run.begin < run.end && !run.at.item_begins();
+    }
+    if (run.begin >= run.end) return;
 
-    TreeCursorT<W> c = run.at, ahead = run.at;
+    TreeCursor c = run.at, ahead = run.at;
     bool split_front = !c.item_begins();                   // the first piece continues an item of an earlier CTA
     float m[kSimtRows], l[kSimtRows], acc[kSimtRows][VPL];
     const long long n_tiles = run.end - run.begin;
@@ -264,17 +266,7 @@ tree_attention_simt_kernel(SimtParamsT<W> p) {
 #pragma unroll
                     for (int e = 0; e < VPL; ++e) o[e] = fmaf(acc_s[(w * kSimtRows + r) * DH + lane * VPL + e], f, o[e]);
                 }
-                if constexpr (W::kPrefix) {
-                    const int64_t at = prefix_query(p.w, c.r, q0 + r, c.h);
-                    float* to = whole ? p.w.partial + at * (DH + 4) : slot + 2 * kSimtRows + r * DH;
-#pragma unroll
-                    for (int e = 0; e < VPL; ++e) to[lane * VPL + e] = o[e];
-                    if (lane == 0) {
-                        if (whole) { to[DH] = top; to[DH + 1] = sum; }
-                        else { slot[r] = top; slot[kSimtRows + r] = sum; }
-                        if (!split_front) p.w.entries[at] = ends ? make_int2(0, -1) : make_int2((int)blockIdx.x | run.tail_cta << 16, r);
-                    }
-                } else if (whole) {
+                if (whole) {
                     const int tok = (q0 + r) / p.w.group, hg = q0 + r - tok * p.w.group;
                     float* dst = p.out + (int64_t)(c.r.row0 + tok) * p.out_stride + (int64_t)(c.h * p.w.group + hg) * DH + lane * VPL;
 #pragma unroll
@@ -285,7 +277,7 @@ tree_attention_simt_kernel(SimtParamsT<W> p) {
                     for (int e = 0; e < VPL; ++e) slot[2 * kSimtRows + r * DH + lane * VPL + e] = o[e];
                 }
             }
-            if (!W::kPrefix && !ends && !split_front && tid == 0) {       // begins here, goes on in the next CTAs
+            if (!ends && !split_front && tid == 0) {       // begins here, goes on in the next CTAs
                 TreeTail t{};
                 t.last_cta = run.tail_cta;
                 t.queries = nq; t.row0 = c.r.row0; t.q0 = q0; t.h = c.h;
@@ -298,22 +290,15 @@ tree_attention_simt_kernel(SimtParamsT<W> p) {
         c.next(p.w);
     }
     cp_async_wait<0>();
-    tree_finish(p.w);
-}
-
-template <int DH, class W>
-int simt_kernel_launch(const SimtParamsT<W>& p, int grid, cudaStream_t s, bool dependent) {
-    static DeviceOnce attr;
-    if (!attr.done([] { return allow_smem(tree_attention_simt_kernel<DH, W>, SimtCfg<DH>::kSmemBytes); })) return ZOQAT_ERR_CUDA;
-    if (launch_kernel(tree_attention_simt_kernel<DH, W>, dim3(grid), dim3(kSimtThreads), SimtCfg<DH>::kSmemBytes, s, dependent, p) != cudaSuccess)
-        return ZOQAT_ERR_CUDA;
-    count_launch();
-    return ZOQAT_OK;
 }
 
 template <int DH>
 int simt_launch(const SimtParams& p, int grid, int combine_y, cudaStream_t s, bool dependent) {
-    if (int rc = simt_kernel_launch<DH>(p, grid, s, dependent)) return rc;
+    static DeviceOnce attr;
+    if (!attr.done([] { return allow_smem(tree_attention_simt_kernel<DH>, SimtCfg<DH>::kSmemBytes); })) return ZOQAT_ERR_CUDA;
+    if (launch_kernel(tree_attention_simt_kernel<DH>, dim3(grid), dim3(kSimtThreads), SimtCfg<DH>::kSmemBytes, s, dependent, p) != cudaSuccess)
+        return ZOQAT_ERR_CUDA;
+    count_launch();
     if (launch_kernel(tree_combine_kernel<float, DH>, dim3(grid, combine_y), dim3(256), 0, s, true, p.scratch, kSimtRows, p.w.group, p.out,
                       p.out_stride) != cudaSuccess)
         return ZOQAT_ERR_CUDA;
@@ -335,28 +320,14 @@ size_t tree_attention_scratch_bytes(int type, int d_head) {
     return kTailBytes + 2 * (size_t)(type == kTypeF32 ? kMaxTreeGrid : kMaxTreeGrid / 2) * tree_slot_floats(tile_rows, d_head) * 4;
 }
 
-template <class W>
-static SimtParamsT<W> simt_params(const TreeAttnArgs& a) {
-    SimtParamsT<W> p{};
-    static_cast<TreeWork&>(p.w) = TreeWork{a.kv_len, a.row_start, a.block_table, a.batch, a.rows, a.cache.n_kv_heads, a.max_pages, a.cache.page_size,
-                                           a.n_heads / a.cache.n_kv_heads, kSimtRows, kSimtKeys, 4, a.err_flag};
+int launch_tree_attention_simt(const TreeAttnArgs& a, cudaStream_t s, bool dependent) {
+    SimtParams p{};
+    p.w = TreeWork{a.kv_len, a.row_start, a.block_table, a.batch, a.rows, a.cache.n_kv_heads, a.max_pages, a.cache.page_size,
+                   a.n_heads / a.cache.n_kv_heads, kSimtRows, kSimtKeys, 4, a.err_flag};
     p.q = static_cast<const float*>(a.q); p.q_stride = a.q_stride; p.cache = a.cache;
     p.tree_mask = a.tree_mask; p.mask_words = a.mask_words;
     p.scale_log2 = (float)(1.4426950408889634 * (double)a.scale);
     p.out = static_cast<float*>(a.out); p.out_stride = a.out_stride; p.scratch = a.scratch;
-    return p;
-}
-
-int launch_prefix_simt(const PrefixAttnArgs& a, const PrefixScratch& at, cudaStream_t s, bool dependent) {
-    SimtParamsT<PrefixWork> p = simt_params<PrefixWork>(a.t);
-    prefix_work(a, at, 0, a.groups + a.t.batch, p.w);
-    p.scratch = at.pieces[0];
-    const int grid = 2 * tree_grid();
-    return a.t.cache.d_head == 64 ? simt_kernel_launch<64>(p, grid, s, dependent) : simt_kernel_launch<128>(p, grid, s, dependent);
-}
-
-int launch_tree_attention_simt(const TreeAttnArgs& a, cudaStream_t s, bool dependent) {
-    const SimtParams p = simt_params<TreeWork>(a);
     const int grid = 2 * tree_grid();                      // two CTAs per SM
     return a.cache.d_head == 64 ? simt_launch<64>(p, grid, kSimtRows, s, dependent) : simt_launch<128>(p, grid, kSimtRows, s, dependent);
 }

@@ -16,9 +16,9 @@
 
 namespace zq {
 
-constexpr int kSimtKeys = 32, kSimtRows = 8;             // keys of a key tile, queries of a row tile: the CUDA-core kernel's
 constexpr int kKeys = 128;                               // keys of a key tile: the tensor-core kernels'
 constexpr int kNarrowKeys = 16, kNarrowRows = 16, kNarrowWarps = 12;      // the warps' kernel (prefix_narrow.cu): a run per warp
+constexpr int kF32Rows = 8, kF32Border = 32, kF32Warps = 10;             // its fp32 sibling (prefix_narrow_f32.cu); the border between parts
 
 // A request's part of the work: n rows from row0 on, keys up to L, in n_rt row tiles and the key tiles [first_tile(), n_kt); n_rt * n_kt = 0: nothing to do.
 // drafts(): how many of the last keys are the rows' own.  table(b): its row of the block table.
@@ -147,7 +147,7 @@ __device__ __forceinline__ int64_t prefix_query(const PrefixWork& w, const Prefi
 
 // The prefix part of a work description: `parts` of them from `first` on.
 inline void prefix_work(const PrefixAttnArgs& a, const PrefixScratch& at, int first, int parts, PrefixWork& w) {
-    w.border = a.t.cache.type == kTypeF32 ? kSimtKeys : kKeys;
+    w.border = a.t.cache.type == kTypeF32 ? kF32Border : kKeys;
     w.group_start = a.group_start; w.prefix_len = a.prefix_len; w.request_group = a.request_group;
     w.groups = a.groups; w.requests = a.t.batch; w.first = first; w.batch = parts;
     w.entries = static_cast<int2*>(at.entries); w.partial = at.partial; w.row_sides = at.row_sides;
@@ -276,6 +276,22 @@ __device__ __forceinline__ void prefix_load(const PrefixWork& w, const PrefixSca
     if (b < scan.kept) r = scan.part[b];
     else r = tree_request(w, b);
 }
+// A cursor over tiles that looks parts up in the CTA's copies.
+struct PrefixCursor {
+    PrefixRequest r;
+    int b, h, rt, kt;
+    __device__ __forceinline__ void next(const PrefixWork& w, const PrefixScan& scan) {
+        if (++kt < r.n_kt) return;
+        if (++rt >= r.n_rt) {
+            rt = 0;
+            if (++h >= w.n_kv) {
+                h = 0;
+                do { if (++b >= w.batch) return; prefix_load(w, scan, b, r); } while (r.n_kt == 0);
+            }
+        }
+        kt = r.kt0;
+    }
+};
 template <int N>
 __device__ __forceinline__ void prefix_find_runs(const PrefixWork& w, PrefixScan& scan, TreeRunT<PrefixWork>* out) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
