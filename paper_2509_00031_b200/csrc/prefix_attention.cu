@@ -11,6 +11,7 @@
 // over the pieces of the shared part, then of the own, in the order of the keys; in fp32, one rounding at the end.  prefix_join_kernel does that:
 // a warp per query and head, or, where there are few queries (whose parts are then split over many CTAs), eight warps.
 #include "tree_attention.cuh"
+#include <type_traits>
 #include "../../include/zoqat.h"
 
 namespace zq {
@@ -25,67 +26,75 @@ struct JoinParams {
     int64_t out_stride;
 };
 
-struct Sum { float m, l; };
-
 template <typename T, int DH, bool WIDE>
 __global__ void __launch_bounds__(256)
-prefix_join_kernel(const JoinParams p) {
-    constexpr int VPL = DH / 32;
+prefix_join_kernel(const __grid_constant__ JoinParams p) {
+    constexpr int VPL = DH / 32, kFly = WIDE ? 4 : 8;            // columns of a lane; pieces of a warp in flight
+    typedef typename std::conditional<VPL == 4, float4, float2>::type Vec;
     __shared__ float acc_s[WIDE ? 8 : 1][DH], m_s[8], l_s[8];
     const PrefixWork& w = p.w;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = blockIdx.x, heads = w.n_kv * w.group;
-    grid_dependency_wait();
-    const int sides = w.row_sides[row];
-    if (sides == 0) return;                                      // no request's row: left as it is
     const int h = WIDE ? blockIdx.y : blockIdx.y * 8 + warp;
     if (!WIDE && h >= heads) return;
-    const int first = WIDE ? warp : 0, step = WIDE ? 8 : 1;      // pieces of this warp
+    const int64_t query = (int64_t)row * heads + h, side_queries = (int64_t)w.rows * heads;
+    grid_dependency_wait();
+    const int sides = w.row_sides[row];
+    const int2 e0 = w.entries[query], e1 = w.entries[side_queries + query];      // (anything where there is no part)
+    if (sides == 0) return;                                      // no request's row: left as it is
+    // pieces of the shared part, then of the own one.  (Places that no worker can have: a wait ran out and nothing was written)
+    int n[2], c0[2];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        const int2 e = side ? e1 : e0;
+        c0[side] = e.x & 0xFFFF;
+        n[side] = e.y < 0 ? 1 : (e.x >> 16) - c0[side] + 1;
+        if (e.y >= 0 && (n[side] < 0 || c0[side] + n[side] > p.workers[side] || e.y >= p.tile_rows[side])) n[side] = 0;
+    }
+    if (sides != 3) n[0] = 0;
+    const int pieces = n[0] + n[1], first = WIDE ? warp : 0, step = WIDE ? 8 : 1;
     float m = -INFINITY, l = 0.0f, acc[VPL];
 #pragma unroll
     for (int j = 0; j < VPL; ++j) acc[j] = 0.0f;
-    const int64_t query = (int64_t)row * heads + h;
-    int2 entry[2];
-    for (int side = 0; side < 2; ++side) entry[side] = w.entries[side * (int64_t)w.rows * heads + query];      // (anything where there is no part)
-    for (int side = sides == 3 ? 0 : 1; side < 2; ++side) {
-        const int64_t at = side * (int64_t)w.rows * heads + query;
-        const int2 e = entry[side];
-        const bool whole = e.y < 0;
-        const int c0 = whole ? 0 : e.x & 0xFFFF, pieces = whole ? 1 : (e.x >> 16) - c0 + 1;
-        if (!whole && (c0 + pieces > p.workers[side] || e.y >= p.tile_rows[side])) continue;      // (a wait ran out: nothing was written)
-        for (int p0 = first; p0 < pieces; p0 += 4 * step) {      // four pieces in flight
-            float pm[4], pl[4], po[4][VPL];
+    for (int p0 = first; p0 < pieces; p0 += kFly * step) {
+        float pm[kFly], pl[kFly];
+        Vec po[kFly];
+        bool there[kFly];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int k = p0 + u * step;
-                pm[u] = -INFINITY; pl[u] = 0.0f;
-#pragma unroll
-                for (int j = 0; j < VPL; ++j) po[u][j] = 0.0f;
-                if (k >= pieces) continue;
-                const float* slot = whole ? nullptr : tree_slot(p.pieces[side], k == 0 ? 2 * c0 + 1 : 2 * (c0 + k), p.tile_rows[side], DH);
-                const float* o = whole ? w.partial + at * (DH + 4) : slot + 2 * p.tile_rows[side] + (size_t)e.y * DH;
-                const bool there = whole || k == 0 || prefix_front(p.pieces[side])[c0 + k];
-                pm[u] = whole ? o[DH] : slot[e.y];
-                pl[u] = whole ? o[DH + 1] : slot[p.tile_rows[side] + e.y];
-                if (!there) pl[u] = 0.0f;                        // (its worker had no tile of the part)
-#pragma unroll
-                for (int j = 0; j < VPL; ++j) po[u][j] = o[lane * VPL + j];
+        for (int u = 0; u < kFly; ++u) {
+            const int i = p0 + u * step, side = i >= n[0], k = i - (side ? n[0] : 0), y = side ? e1.y : e0.y, c = side ? c0[1] : c0[0];
+            pl[u] = 0.0f;
+            there[u] = i < pieces;
+            if (!there[u]) continue;
+            const int rows = p.tile_rows[side];
+            const float *o = w.partial + (side * side_queries + query) * (DH + 4), *ref = o + DH, *sum = o + DH + 1;
+            if (y >= 0) {
+                const float* slot = tree_slot(p.pieces[side], k == 0 ? 2 * c + 1 : 2 * (c + k), rows, DH);
+                ref = slot + y; sum = slot + rows + y; o = slot + 2 * rows + (size_t)y * DH;
+                if (k > 0) there[u] = prefix_front(p.pieces[side])[c + k];       // (else: its worker had no tile of the part)
             }
+            pm[u] = *ref;
+            pl[u] = *sum;
+            po[u] = *reinterpret_cast<const Vec*>(o + lane * VPL);
+        }
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (pl[u] == 0.0f) continue;                     // nothing seen in this piece (NaN sums go on)
-                const float top = fmaxf(m, pm[u]);
-                const float fa = m == -INFINITY ? 0.0f : tree_ex2(m - top), fb = tree_ex2(pm[u] - top);
-                l = l * fa + pl[u] * fb;
+        for (int u = 0; u < kFly; ++u) {
+            if (!there[u] || pl[u] == 0.0f) continue;            // nothing seen in this piece (NaN sums go on)
+            const float top = fmaxf(m, pm[u]);
+            const float fa = m == -INFINITY ? 0.0f : tree_ex2(m - top), fb = tree_ex2(pm[u] - top);
+            const float* o = reinterpret_cast<const float*>(&po[u]);
+            l = l * fa + pl[u] * fb;
 #pragma unroll
-                for (int j = 0; j < VPL; ++j) acc[j] = acc[j] * fa + po[u][j] * fb;
-                m = top;
-            }
+            for (int j = 0; j < VPL; ++j) acc[j] = acc[j] * fa + o[j] * fb;
+            m = top;
         }
     }
     T* dst = static_cast<T*>(p.out) + (int64_t)row * p.out_stride + (int64_t)h * DH;
     if (!WIDE) {
+        T x[VPL];
 #pragma unroll
-        for (int j = 0; j < VPL; ++j) dst[lane * VPL + j] = tree_round<T>(l == 0.0f ? 0.0f : acc[j] / l);
+        for (int j = 0; j < VPL; ++j) x[j] = tree_round<T>(l == 0.0f ? 0.0f : acc[j] / l);
+        struct alignas(VPL * sizeof(T)) Out { T x[VPL]; };
+        *reinterpret_cast<Out*>(dst + lane * VPL) = *reinterpret_cast<const Out*>(x);
         return;
     }
     if (lane == 0) { m_s[warp] = m; l_s[warp] = l; }

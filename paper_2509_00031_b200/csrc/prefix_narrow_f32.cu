@@ -66,7 +66,7 @@ prefix_f32_kernel(const __grid_constant__ F32Params p) {
     grid_dependency_wait();
     grid_dependency_release();
     prefix_find_runs<kWarps>(w, scan, runs);
-    if (blockIdx.x == gridDim.x - 1) prefix_map_rows(w);
+    if (blockIdx.x == gridDim.x - 1) prefix_map_rows(w, scan);
     const TreeRunT<PrefixWork>& run = runs[warp];
     const int n_tiles = (int)(run.end - run.begin);
     if (lane == 0) prefix_front(p.scratch)[worker] = n_tiles > 0 && !run.at.item_begins();

@@ -80,7 +80,9 @@ struct PrefixWork : TreeWork {               // batch: parts in this launch
     int2* entries;                           // [2][rows * heads]: where a query's shared (0) and own (1) pieces are
     float* partial;                          // [2][rows * heads][d_head + 4]: output, reference, sum of parts that one CTA finished
 };
-__device__ __forceinline__ int prefix_border(const PrefixWork& w, int len) { return len / w.border * w.border; }
+// a / b rounded down or up for a power of two b (a + b < 2^31)
+__device__ __forceinline__ int prefix_down(int a, int b) { return a >> (31 - __clz(b)); }
+__device__ __forceinline__ int prefix_up(int a, int b) { return (int)((unsigned)(a + b - 1) >> (31 - __clz(b))); }
 
 // The shared part of group g; n_kt = 0: it has none, or (ok = false) its description contradicts itself.
 __device__ __forceinline__ PrefixRequest prefix_shared(const PrefixWork& w, int g, bool& ok) {
@@ -93,29 +95,27 @@ __device__ __forceinline__ PrefixRequest prefix_shared(const PrefixWork& w, int 
     ok = lo >= 0 && n > 0 && lo <= w.rows - n && len >= 0 && len <= (long long)w.max_pages * w.page_size;
     if (!ok) return r;
     r.row0 = lo; r.n = n; r.row = b0;
-    r.L = prefix_border(w, len);
-    r.n_rt = (int)(((long long)n * w.group + w.tile_rows - 1) / w.tile_rows);
-    r.n_kt = r.L / w.key_tile;
+    r.L = prefix_down(len, w.border) * w.border;
+    r.n_rt = prefix_up(n * w.group, w.tile_rows);
+    r.n_kt = prefix_down(r.L, w.key_tile);
     return r;
 }
 // The part of request b alone; its group's description is prefix_shared's to check.
 __device__ __forceinline__ PrefixRequest prefix_own(const PrefixWork& w, int b, bool& ok) {
     PrefixRequest r{};
-    const int g = __ldg(w.request_group + b);
+    const int g = __ldg(w.request_group + b), end = __ldg(w.row_start + b + 1);
     r.row0 = __ldg(w.row_start + b);
-    r.n = __ldg(w.row_start + b + 1) - r.row0;
     r.L = __ldg(w.kv_len + b);
+    const bool grouped = g >= 0 && g < w.groups;
+    const int of = grouped ? g : 0, len = __ldg(w.prefix_len + of), b0 = __ldg(w.group_start + of), b1 = __ldg(w.group_start + of + 1);     // (all on their way at once)
+    r.n = end - r.row0;
     r.row = b; r.own = 1;
-    ok = r.n >= 0 && r.row0 >= 0 && r.row0 <= w.rows - r.n && r.L <= (long long)w.max_pages * w.page_size && g >= 0 && g < w.groups;
-    int len = 0;
-    if (ok) {
-        len = __ldg(w.prefix_len + g);
-        ok = __ldg(w.group_start + g) <= b && b < __ldg(w.group_start + g + 1) && (r.n == 0 || (len >= 0 && len <= r.L - r.n));
-    }
-    if (!ok || r.n == 0) { r.n = r.n_rt = r.n_kt = 0; return r; }
-    r.kt0 = prefix_border(w, len) / w.key_tile;
-    r.n_rt = (int)(((long long)r.n * w.group + w.tile_rows - 1) / w.tile_rows);
-    r.n_kt = (r.L + w.key_tile - 1) / w.key_tile;
+    ok = r.n >= 0 && r.row0 >= 0 && r.row0 <= w.rows - r.n && r.L <= (long long)w.max_pages * w.page_size && grouped && b0 <= b && b < b1 &&
+         (r.n == 0 || (len >= 0 && len <= r.L - r.n));
+    if (!ok || r.n == 0) { r.n = 0; return r; }
+    r.kt0 = prefix_down(prefix_down(len, w.border) * w.border, w.key_tile);
+    r.n_rt = prefix_up(r.n * w.group, w.tile_rows);
+    r.n_kt = prefix_up(r.L, w.key_tile);
     return r;
 }
 __device__ __forceinline__ PrefixRequest tree_request(const PrefixWork& w, int part) {
@@ -124,20 +124,6 @@ __device__ __forceinline__ PrefixRequest tree_request(const PrefixWork& w, int p
     const PrefixRequest r = part < w.groups ? prefix_shared(w, part, ok) : prefix_own(w, part - w.groups, ok);
     if (!ok) atomicExch(w.err_flag, kErrBadRequest);
     return r;
-}
-// What the joining launch needs to know of every row, so that it does not have to look for the row's request: 0 not a row of any (valid) request, 1 own keys only, 3 a
-// shared part too.  By all threads of one CTA of the launch that has the requests' own parts.
-__device__ __forceinline__ void prefix_map_rows(const PrefixWork& w) {
-    for (int r = threadIdx.x; r < w.rows; r += blockDim.x) w.row_sides[r] = 0;
-    __syncthreads();
-    for (int b = threadIdx.x; b < w.requests; b += blockDim.x) {
-        bool ok;
-        const PrefixRequest own = prefix_own(w, b, ok);
-        if (own.n_kt == 0) continue;
-        const PrefixRequest shared = prefix_shared(w, __ldg(w.request_group + b), ok);
-        // (rows that another request claims as well may get either's word)
-        for (int i = 0; ok && i < own.n; ++i) w.row_sides[own.row0 + i] = shared.n_kt > 0 ? 3 : 1;
-    }
 }
 // Where the query's piece is: whole in `partial` (y = -1), or query y of the pieces of the CTAs x & 0xFFFF .. x >> 16.
 __device__ __forceinline__ int64_t prefix_query(const PrefixWork& w, const PrefixRequest& r, int query, int h) {
@@ -276,6 +262,21 @@ __device__ __forceinline__ void prefix_load(const PrefixWork& w, const PrefixSca
     if (b < scan.kept) r = scan.part[b];
     else r = tree_request(w, b);
 }
+// What the joining launch needs to know of every row, so that it does not have to look for the row's request: 0 not a row of any (valid) request, 1 own keys only, 3 a
+// shared part too.  By all threads of one CTA of the launch that has the requests' own parts.
+__device__ __forceinline__ void prefix_map_rows(const PrefixWork& w, const PrefixScan& scan) {
+    for (int r = threadIdx.x; r < w.rows; r += blockDim.x) w.row_sides[r] = 0;
+    __syncthreads();
+    for (int b = threadIdx.x; b < w.requests; b += blockDim.x) {
+        PrefixRequest own, shared;
+        prefix_load(w, scan, w.groups - w.first + b, own);
+        if (own.n_kt == 0) continue;
+        bool ok;
+        shared = prefix_shared(w, __ldg(w.request_group + b), ok);
+        // (rows that another request claims as well may get either's word)
+        for (int i = 0; ok && i < own.n; ++i) w.row_sides[own.row0 + i] = shared.n_kt > 0 ? 3 : 1;
+    }
+}
 // A cursor over tiles that looks parts up in the CTA's copies.
 struct PrefixCursor {
     PrefixRequest r;
@@ -392,7 +393,7 @@ __device__ __forceinline__ void tree_start(const PrefixWork& w, long long*, Tree
     if (!w.late_wait) grid_dependency_wait();
     grid_dependency_release();
     prefix_find_runs<1>(w, *static_cast<PrefixScan*>(scan), run);
-    if (blockIdx.x == gridDim.x - 1 && w.first + w.batch > w.groups) prefix_map_rows(w);
+    if (blockIdx.x == gridDim.x - 1 && w.first + w.batch > w.groups) prefix_map_rows(w, *static_cast<PrefixScan*>(scan));
 }
 __device__ __forceinline__ void tree_finish(const TreeWork&) {}
 __device__ __forceinline__ void tree_finish(const PrefixWork& w) { if (w.late_wait) grid_dependency_wait(); }
