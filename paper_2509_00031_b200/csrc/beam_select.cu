@@ -24,7 +24,7 @@
 namespace zq {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32, kCluster = 8;
+constexpr int kMaxThreads = 512, kCluster = 8;       // threads of a CTA, CTAs of a cluster at most
 constexpr int kMaxEos = kMaxBeamEos, kMaxBest = kMaxBeams + kMaxEos;       // best logits of a row
 constexpr int kBuffer = 2048, kMaxCandidates = kMaxBeams * kMaxBest;       // (a row in several slices: at most 8 rows' worth)
 constexpr float kLog2e = 1.4426950408889634f;
@@ -42,9 +42,9 @@ __device__ __forceinline__ u64 ordered64(double x) {
     const u64 b = (u64)__double_as_longlong(x);
     return b >> 63 ? ~b : b | (1ull << 63);
 }
-// Never 0 for a logit that may be chosen: NaN and -inf have no key, +inf counts as the largest finite value.
+// Never 0 for a logit that may be chosen: NaN and -inf have no key, +inf counts as the largest finite value; both zeros are the same.
 __device__ __forceinline__ u64 key_of(float x, int token) {
-    return x > -INFINITY ? (u64)ordered(fminf(x, FLT_MAX)) << 32 | (uint32_t)~token : 0ull;
+    return x > -INFINITY ? (u64)ordered(fminf(x, FLT_MAX) + 0.0f) << 32 | (uint32_t)~token : 0ull;
 }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -61,6 +61,7 @@ __device__ __forceinline__ u64 ld_cluster_u64(uint32_t addr) {
 template <typename T> __device__ __forceinline__ float value(T v) { return static_cast<float>(v); }
 // VEC logits at a time: 16 bytes where the rows allow it, else single ones
 template <typename T, int VEC> struct alignas(VEC * sizeof(T)) Vec { T v[VEC]; };
+template <typename T, int THREADS> constexpr int kResident = THREADS == 512 ? 2 : (sizeof(T) == 4 ? 4 : 3);      // CTAs of an SM (registers: 16-bit logits take more)
 // the largest; NaN does not count
 template <typename T, int VEC> __device__ __forceinline__ float largest(const Vec<T, VEC>& x) {
     if constexpr (VEC == 1) return value(x.v[0]);
@@ -99,8 +100,8 @@ struct Shared {
     u64 best[kMaxCandidates];                // a row's best keys in order, row after row of this CTA; 0: none
     u64 stat[kMaxBeams];                     // (reference, sum) of a row's slice as two floats
     double lse[kMaxBeams];
-    float ref[kWarps], sum[kWarps];
-    uint32_t bound[kWarps];
+    float ref[kMaxThreads / 32], sum[kMaxThreads / 32], score[kMaxBeams];
+    uint32_t bound[kMaxThreads / 32];
     int top[kMaxBeams * (1 + kMaxEos)];
     int hist[256];
     int count, eos[kMaxEos];
@@ -108,23 +109,38 @@ struct Shared {
     int want;
 };
 
-// Sorts the n best of m keys (m <= kBuffer) into `to`; 0 behind them.  Starts behind a barrier, ends with one.
+// Sorts the n best of m keys (m <= kBuffer) into `to`; 0 behind them.  Four lanes to a key: each counts a quarter of the larger ones.  Starts behind a barrier,
+// ends with one.
+template <int kThreads>
 __device__ __forceinline__ void sort_best(const u64* buf, int m, u64* to, int n) {
     for (int i = threadIdx.x; i < n; i += kThreads)
         if (i >= m) to[i] = 0;
-    for (int i = threadIdx.x; i < m; i += kThreads) {
-        const u64 key = buf[i];
+    for (int i0 = 0; i0 < m; i0 += kThreads / 4) {
+        const int i = i0 + threadIdx.x / 4;
+        const u64 key = i < m ? buf[i] : 0ull;
         int rank = 0;
-        for (int j = 0; j < m; ++j) rank += buf[j] > key;
-        if (rank < n) to[rank] = key;
+        if (i < m)
+            for (int j = threadIdx.x & 3; j < m; j += 4) rank += buf[j] > key;
+        rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+        rank += __shfl_xor_sync(0xffffffffu, rank, 2);
+        if (i < m && rank < n && (threadIdx.x & 3) == 0) to[rank] = key;
     }
     __syncthreads();
 }
 
+// Asks for the 64 KB behind a row's first two rounds, so that the memory is busy while the bound is found.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads, 3)
-beam_select_kernel(const Params p) {
-    constexpr int kFly = VEC == 1 ? 8 : 4, kRound = kFly * kThreads;       // vectors of a thread in flight, vectors of a round
+__device__ __forceinline__ void prefetch_row(const T* src, int size, int from) {
+    constexpr int kBytes = 4096;
+    const int64_t at = (int64_t)from * sizeof(T) + (int64_t)threadIdx.x * kBytes, end = (int64_t)size * sizeof(T) / 16 * 16;
+    if (VEC > 1 && threadIdx.x < 65536 / kBytes && at < end)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<const char*>(src) + at), "r"((int)(end - at < kBytes ? end - at : kBytes)) : "memory");
+}
+
+template <typename T, int VEC, int kThreads>
+__global__ void __launch_bounds__(kThreads, kResident<T, kThreads>)
+beam_select_kernel(const __grid_constant__ Params p) {
+    constexpr int kWarps = kThreads / 32, kFly = VEC == 1 ? 8 : 4, kRound = kFly * kThreads;       // vectors of a thread in flight, vectors of a round
     __shared__ Shared sh;
     const BeamSelectArgs& a = p.a;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -132,6 +148,7 @@ beam_select_kernel(const Params p) {
     const int n = p.best, lo = (rank % p.slices) * p.slice, size = max(0, min(a.vocab, lo + p.slice) - lo);
     const int n_vec = (size + VEC - 1) / VEC, n_whole = size / VEC;
     if (tid < a.n_eos) sh.eos[tid] = __ldg(a.eos + tid);
+    if (rank == 0 && tid < a.beams) sh.score[tid] = __ldg(a.score + (int64_t)request * a.beams + tid);
 
     auto row_of = [&](int row) { return static_cast<const T*>(a.logits) + ((int64_t)request * a.beams + row) * a.ld + lo; };
     typedef Vec<T, VEC> V;
@@ -156,7 +173,10 @@ beam_select_kernel(const Params p) {
     };
     V now[kFly], ahead[kFly];
     int mine = 0;                                                // rows of this CTA so far
-    if (rank / p.slices < a.beams) fetch(now, row_of(rank / p.slices), 0);
+    if (rank / p.slices < a.beams) {
+        fetch(now, row_of(rank / p.slices), 0);
+        prefetch_row<T, VEC>(row_of(rank / p.slices), size, 2 * kRound * VEC);
+    }
     for (int row = rank / p.slices; row < a.beams; row += p.in_parallel, ++mine) {
         const T* src = row_of(row);
         u64* const best = sh.best + mine * n;
@@ -205,7 +225,7 @@ beam_select_kernel(const Params p) {
         if (n_vec > kRound && sh.count <= kBuffer) {
             auto tighten = [&]() {
                 const int m = sh.count;
-                sort_best(sh.buf, m, best, n);
+                sort_best<kThreads>(sh.buf, m, best, n);
                 const u64 nth = best[n - 1];
                 limit = nth ? unordered((uint32_t)(nth >> 32)) : -INFINITY;
                 for (int i = tid; i < n; i += kThreads) sh.buf[i] = best[i];
@@ -251,7 +271,10 @@ beam_select_kernel(const Params p) {
             }
             __syncthreads();
         }
-        if (row + p.in_parallel < a.beams) fetch(now, row_of(row + p.in_parallel), 0);
+        if (row + p.in_parallel < a.beams) {
+            fetch(now, row_of(row + p.in_parallel), 0);
+            prefetch_row<T, VEC>(row_of(row + p.in_parallel), size, kRound * VEC);
+        }
         auto each_key = [&](auto f) {                            // every key of the slice again
             for (int i = tid; i < size; i += kThreads) {
                 const u64 key = key_of(value(src[i]), lo + i);
@@ -283,7 +306,7 @@ beam_select_kernel(const Params p) {
             }
             if (tid == 0) sh.count = 0;
             __syncthreads();
-            each_key([&](u64 key) { if (key >= prefix) push(key); });
+            each_key([&](u64 key) { if (key >= prefix) sh.buf[atomicAdd(&sh.count, 1)] = key; });      // (n of them)
             __syncthreads();
         }
         // the row's sum, relative to 2^(fl(reference * log2 e))
@@ -296,7 +319,7 @@ beam_select_kernel(const Params p) {
 #pragma unroll
         for (int o = 16; o >= 1; o >>= 1) join(__shfl_xor_sync(0xffffffffu, x[0], o), __shfl_xor_sync(0xffffffffu, x[1], o));
         if (lane == 0) { sh.ref[warp] = x[0]; sh.sum[warp] = x[1]; }
-        sort_best(sh.buf, sh.count, best, n);
+        sort_best<kThreads>(sh.buf, sh.count, best, n);
         x[0] = sh.ref[0]; x[1] = sh.sum[0];
         for (int w = 1; w < kWarps; ++w) join(sh.ref[w], sh.sum[w]);
         // Once more, with care: where the stream was left out above, NaN and +inf, logits near either end of the range.  Relative to
@@ -351,7 +374,7 @@ beam_select_kernel(const Params p) {
     if (rank != 0) return;
     auto score_of = [&](int i) {
         const int row = i / per_row;
-        return (double)__ldg(a.score + (int64_t)request * a.beams + row) + ((double)unordered((uint32_t)(keys[i] >> 32)) - sh.lse[row]);
+        return (double)sh.score[row] + ((double)unordered((uint32_t)(keys[i] >> 32)) - sh.lse[row]);
     };
     u64* const order = sh.best;                                  // (all have read their keys)
     for (int i = tid; i < total; i += kThreads) {
@@ -404,30 +427,36 @@ beam_select_kernel(const Params p) {
     }
 }
 
-template <typename T, int VEC>
-int launch_vec(const BeamSelectArgs& a, cudaStream_t s) {
-    Params p{a, 0, 0, 0, 0};
-    // Whole rows in parallel, as many as keep all CTAs resident (three to an SM: with more, clusters wait for one another); slices only while
-    // the SMs are not filled, and of two thousand tokens at least.
-    int rounds = (a.beams + kCluster - 1) / kCluster;
-    for (p.in_parallel = (a.beams + rounds - 1) / rounds; p.in_parallel > 1 && (int64_t)a.batch * p.in_parallel > 148 * 3; p.in_parallel = (a.beams + rounds - 1) / rounds) ++rounds;
-    p.slices = 1;
-    while ((p.slices + 1) * p.in_parallel <= kCluster && (int64_t)a.batch * p.in_parallel * (p.slices + 1) <= 148 * 3 && a.vocab >= 2048 * (p.slices + 1)) ++p.slices;
-    p.slice = ((a.vocab + p.slices - 1) / p.slices + VEC - 1) / VEC * VEC;
-    p.best = a.beams + a.n_eos < a.vocab ? a.beams + a.n_eos : a.vocab;
+template <typename T, int VEC, int THREADS>
+int launch_threads(const Params& p, cudaStream_t s) {
     const int ranks = p.in_parallel * p.slices;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)a.batch * ranks);
-    cfg.blockDim = dim3(kThreads);
+    cfg.gridDim = dim3((unsigned)p.a.batch * ranks);
+    cfg.blockDim = dim3(THREADS);
     cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = ranks; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, beam_select_kernel<T, VEC>, p) != cudaSuccess) return -1;
+    if (cudaLaunchKernelEx(&cfg, beam_select_kernel<T, VEC, THREADS>, p) != cudaSuccess) return -1;
     count_launch();
     return 0;
+}
+
+template <typename T, int VEC>
+int launch_vec(const BeamSelectArgs& a, cudaStream_t s) {
+    Params p{a, 0, 0, 0, 0};
+    // Whole rows in parallel, as many as keep all CTAs resident (with more, clusters wait for one another); slices only while the SMs have
+    // less than two CTAs, and of two thousand tokens at least.
+    int rounds = (a.beams + kCluster - 1) / kCluster;
+    for (p.in_parallel = (a.beams + rounds - 1) / rounds; p.in_parallel > 1 && (int64_t)a.batch * p.in_parallel > 148 * kResident<T, 256>; p.in_parallel = (a.beams + rounds - 1) / rounds) ++rounds;
+    p.slices = 1;
+    while ((p.slices + 1) * p.in_parallel <= kCluster && (int64_t)a.batch * p.in_parallel * (p.slices + 1) <= 148 * 2 && a.vocab >= 2048 * (p.slices + 1)) ++p.slices;
+    p.slice = ((a.vocab + p.slices - 1) / p.slices + VEC - 1) / VEC * VEC;
+    p.best = a.beams + a.n_eos < a.vocab ? a.beams + a.n_eos : a.vocab;
+    // few CTAs: wide ones (two to an SM leave no room for clusters to be placed)
+    return (int64_t)a.batch * p.in_parallel * p.slices <= 148 ? launch_threads<T, VEC, 512>(p, s) : launch_threads<T, VEC, 256>(p, s);
 }
 
 template <typename T>

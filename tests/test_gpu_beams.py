@@ -200,7 +200,7 @@ def test_select_hard_rows(zq):
         "equal": torch.zeros(V, device="cuda"), "rising": ramp / 4096, "falling": -ramp / 4096, "rising steeply": ramp, "nothing": torch.full((V,), -math.inf, device="cuda"),
         "lowest": torch.full((V,), low, device="cuda"), "one of the lowest": torch.full((V,), low, device="cuda"), "one": torch.full((V,), -math.inf, device="cuda"),
         "nan": torch.randn(V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)), "inf": ramp / 8192, "two values": (ramp % 2) * 3, "large": ramp * 1e33,
-        "late": -ramp, "blocks": torch.where((ramp / 32).long() % 8 == 3, ramp / 1000, -math.inf)}
+        "late": -ramp, "zeros of both signs": torch.where(ramp % 3 == 1, -0.0, 0.0), "few zeros": torch.where(ramp % 1000 == 7, (ramp % 2000 == 7) * -0.0, -1.0), "blocks": torch.where((ramp / 32).long() % 8 == 3, ramp / 1000, -math.inf)}
     rows["one of the lowest"][777] = 1.5
     rows["one"][V - 1] = -3.0
     rows["nan"][::5] = math.nan
