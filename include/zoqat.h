@@ -768,6 +768,7 @@ int zoqat_decode_tree_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows
  *     zoqat_op_beam_select        once: the best continuations of every request's beams
  *     zoqat_op_beam_reorder       once: tables, free pages and token histories follow the beams that go on
  *     zoqat_op_cache_copy         once: what half-filled pages hold is copied for beams that part, in every layer
+ * and zoqat_decode_prefix_step() is zoqat_decode_tree_step() with the shared prefixes read once.
  * Conventions as above: device data is read on the device only, words are or-ed or set, never cleared, all calls are asynchronous and
  * can be captured in a CUDA graph. */
 
@@ -807,6 +808,20 @@ int zoqat_op_prefix_attention(const void* q_dev, int64_t q_stride, const zoqat_p
                               const int32_t* kv_len_dev, const int32_t* row_start_dev, const int32_t* group_start_dev, const int32_t* prefix_len_dev,
                               const int32_t* request_group_dev, int groups, const uint32_t* tree_mask_dev, int mask_words, int batch, int rows, int n_heads,
                               float scale, void* out_dev, int64_t out_stride, void* scratch_dev, size_t scratch_bytes, int32_t* err_flag_dev, void* stream);
+
+/* Groups of requests that share a prefix, as zoqat_op_prefix_attention takes them (device memory). */
+typedef struct zoqat_prefix_groups {
+    const int32_t* group_start;    /* [groups + 1]                                                            */
+    const int32_t* prefix_len;     /* [groups]                                                                */
+    const int32_t* request_group;  /* [batch of the plan]                                                     */
+    int32_t groups, reserved;
+} zoqat_prefix_groups_t;
+
+/* zoqat_decode_tree_step whose requests share prefixes: beams of a prompt, or requests behind one.  scratch_dev: zoqat_op_prefix_attention_scratch_bytes()
+ * bytes for these rows, the model's heads and the caches' type.  Everything else as there. */
+int zoqat_decode_prefix_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows, const zoqat_tree_batch_t* plan, const zoqat_prefix_groups_t* groups,
+                             const zoqat_paged_cache_t* caches, const zoqat_logit_rules_t* rules, float* logits_dev,
+                             int32_t* next_token_dev, void* scratch_dev, size_t scratch_bytes, void* stream);
 
 /* The best continuations: score(b, v) = score_dev[request, b] + logits[request * beams + b, v] - log sum_u exp logits[.., u], formed and
  * compared in 64 bits, ordered from the best down; of equal scores the lower beam, then the larger logit, then the lower token comes first.  Of the

@@ -43,7 +43,7 @@ EXPORTS = [
     "zoqat_op_cache_plan", "zoqat_op_cache_append", "zoqat_op_tree_attention_scratch_bytes", "zoqat_op_tree_attention",
     "zoqat_op_logit_rules", "zoqat_decode_tree_step",
     "zoqat_rotary_frequencies", "zoqat_op_rotary_append", "zoqat_op_prefix_attention_scratch_bytes", "zoqat_op_prefix_attention", "zoqat_op_beam_select", "zoqat_op_beam_reorder_scratch_bytes", "zoqat_op_beam_reorder",
-    "zoqat_op_cache_copy",
+    "zoqat_op_cache_copy", "zoqat_decode_prefix_step",
 ]
 
 
@@ -80,6 +80,10 @@ class LogitRulesDesc(ctypes.Structure):
         "row_request", "repetition", "presence", "frequency", "history", "history_len", "prompt_len", "bias_token", "bias_value", "bias_len",
         "allowed", "draft_token", "row_start", "tree_mask")] + [(n, ctypes.c_int64) for n in ("history_stride", "allowed_stride")] + [
             (n, ctypes.c_int32) for n in ("bias_stride", "mask_words", "batch", "reserved")]
+
+
+class PrefixGroups(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("group_start", "prefix_len", "request_group")] + [(n, ctypes.c_int32) for n in ("groups", "reserved")]
 
 
 class BeamReorder(ctypes.Structure):
@@ -187,6 +191,7 @@ def lib():
             "zoqat_op_beam_select": [vp, i32, i64, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp],
             "zoqat_op_beam_reorder_scratch_bytes": [i32, P(sz)],
             "zoqat_op_beam_reorder": [P(BeamReorder), vp, sz, vp],
+            "zoqat_decode_prefix_step": [vp, vp, i32, P(TreeBatch), P(PrefixGroups), P(PagedCache), P(LogitRulesDesc), vp, vp, vp, sz, vp],
             "zoqat_op_cache_copy": [P(PagedCache), i32, vp, vp, vp, i32, vp, vp],
         }
         for name, args in sigs.items():
@@ -916,6 +921,15 @@ class ZoqatModel:
     def zoqat_decode_tree_step(self, tokens, plan, block_table, caches, rules=None, logits=None, next_token=None, scratch=None):
         """tokens int32 [rows] (1, 2, 4 or 8) at the rows of `plan` (the dict of zoqat_op_cache_plan); caches: (k, v) per layer, each
         [n_pages, page_size, n_heads, d_head]; rules: LogitRules or None.  Returns (logits [rows, vocab], next_token [rows])."""
+        return self._tree_step(tokens, plan, block_table, None, caches, rules, logits, next_token, scratch)
+
+    def zoqat_decode_prefix_step(self, tokens, plan, block_table, group_start, prefix_len, request_group, caches, rules=None, logits=None, next_token=None,
+                                 scratch=None):
+        """zoqat_decode_tree_step for requests in groups (group_start int32 [groups + 1], request_group [batch]) that share their first prefix_len
+        [groups] keys."""
+        return self._tree_step(tokens, plan, block_table, (group_start, prefix_len, request_group), caches, rules, logits, next_token, scratch)
+
+    def _tree_step(self, tokens, plan, block_table, groups, caches, rules, logits, next_token, scratch):
         dev, stream = _here()
         rows, batch = tokens.shape[0], plan["kv_len"].shape[0]
         mask = plan.get("tree_mask")
@@ -935,11 +949,21 @@ class ZoqatModel:
             next_token = torch.empty(rows, dtype=torch.int32, device=tokens.device)
         if scratch is None:
             nb = ctypes.c_size_t()
-            _check(lib().zoqat_op_tree_attention_scratch_bytes(descs[0].type, descs[0].d_head, ctypes.byref(nb)))
+            if groups is None:
+                _check(lib().zoqat_op_tree_attention_scratch_bytes(descs[0].type, descs[0].d_head, ctypes.byref(nb)))
+            else:
+                _check(lib().zoqat_op_prefix_attention_scratch_bytes(descs[0].type, descs[0].d_head, rows, self.shape["n_heads"], ctypes.byref(nb)))
             scratch = torch.empty(nb.value, dtype=torch.uint8, device=tokens.device)
-        _check(lib().zoqat_decode_tree_step(self.handle, _flat(dev, "tokens", tokens, _I32, rows), rows, tb, descs, rules.desc if rules is not None else None,
-                                            _flat(dev, "logits", logits, _F32, rows, self.shape["vocab"]), _flat(dev, "next_token", next_token, _I32, rows),
-                                            scratch.data_ptr(), scratch.numel() * scratch.element_size(), stream))
+        rest = (descs, rules.desc if rules is not None else None, _flat(dev, "logits", logits, _F32, rows, self.shape["vocab"]),
+                _flat(dev, "next_token", next_token, _I32, rows), scratch.data_ptr(), scratch.numel() * scratch.element_size(), stream)
+        ids = _flat(dev, "tokens", tokens, _I32, rows)
+        if groups is None:
+            _check(lib().zoqat_decode_tree_step(self.handle, ids, rows, tb, *rest))
+        else:
+            start, length, of = groups
+            n = length.shape[0]
+            pg = PrefixGroups(_flat(dev, "group_start", start, _I32, n + 1), _flat(dev, "prefix_len", length, _I32, n), _flat(dev, "request_group", of, _I32, batch), n, 0)
+            _check(lib().zoqat_decode_prefix_step(self.handle, ids, rows, tb, pg, *rest))
         return logits, next_token
 
     def zoqat_init_qparams(self):

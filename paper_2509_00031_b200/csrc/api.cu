@@ -1973,9 +1973,10 @@ int zoqat_op_logit_rules(const void* logits_dev, int type, int64_t ld, int rows,
     return ZOQAT_OK;
 }
 
-int zoqat_decode_tree_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows, const zoqat_tree_batch_t* plan,
-                           const zoqat_paged_cache_t* caches, const zoqat_logit_rules_t* rules, float* logits_dev,
-                           int32_t* next_token_dev, void* scratch_dev, size_t scratch_bytes, void* stream) {
+// The step of zoqat_decode_tree_step; with groups the requests' shared prefixes are attended to once.
+static int tree_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows, const zoqat_tree_batch_t* plan, const zoqat_prefix_groups_t* groups,
+                     const zoqat_paged_cache_t* caches, const zoqat_logit_rules_t* rules, float* logits_dev,
+                     int32_t* next_token_dev, void* scratch_dev, size_t scratch_bytes, void* stream) {
     if (!m || !tokens_dev || !plan || !caches || !scratch_dev) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
     DecodeState& D = m->dec;
     if (!D.ready) return fail(ZOQAT_ERR_BAD_STATE, "call zoqat_decode_begin first");
@@ -1986,6 +1987,8 @@ int zoqat_decode_tree_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows
     if (!plan->block_table || !plan->kv_len || !plan->row_start || !plan->row_pos || !plan->slot) return fail(ZOQAT_ERR_INVALID_ARG, "the plan has a NULL array");
     if (plan->batch <= 0 || plan->max_pages <= 0 || (plan->tree_mask ? plan->mask_words <= 0 || plan->mask_words > (1 << 20) : plan->mask_words != 0))
         return fail(ZOQAT_ERR_INVALID_ARG, "bad plan sizes");
+    if (groups && (!groups->group_start || !groups->prefix_len || !groups->request_group || groups->groups <= 0 || groups->groups > INT32_MAX - plan->batch))
+        return fail(ZOQAT_ERR_INVALID_ARG, "the groups have a NULL array or a bad number");
     if (misaligned(scratch_dev, 256)) return fail(ZOQAT_ERR_INVALID_ARG, "scratch_dev must be 256-byte aligned");
     const bool llama = c.arch == ZOQAT_ARCH_LLAMA;
     const int d = c.d_model, F = c.d_ffn, H = c.n_heads, dh = d / H, G = c.w_group;
@@ -1998,7 +2001,8 @@ int zoqat_decode_tree_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows
         if (int rc = paged_cache(caches + l, p)) return rc;
         if (p.n_kv_heads != H || p.d_head != dh) return fail(ZOQAT_ERR_INVALID_ARG, "layer %d: the cache has %d heads of %d, the model %d of %d", l, p.n_kv_heads, p.d_head, H, dh);
         if (int rc = attention_limits(p, plan->max_pages, rows, H)) return rc;
-        if (scratch_bytes < tree_attention_scratch_bytes(p.type, dh)) return fail(ZOQAT_ERR_WORKSPACE_SMALL, "attention scratch %zu < %zu bytes", scratch_bytes, tree_attention_scratch_bytes(p.type, dh));
+        const size_t need = groups ? prefix_scratch(nullptr, p.type, dh, rows, H).bytes : tree_attention_scratch_bytes(p.type, dh);
+        if (scratch_bytes < need) return fail(ZOQAT_ERR_WORKSPACE_SMALL, "attention scratch %zu < %zu bytes", scratch_bytes, need);
     }
     Workspace& w = m->ws;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -2031,7 +2035,14 @@ int zoqat_decode_tree_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows
         a.row_start = plan->row_start; a.tree_mask = plan->tree_mask; a.mask_words = plan->mask_words; a.batch = plan->batch; a.rows = rows; a.n_heads = H;
         a.scale = (float)(1.0 / std::sqrt((double)dh)); a.out = half ? static_cast<void*>(att16) : w.att; a.out_stride = d;
         a.scratch = static_cast<uint8_t*>(scratch_dev); a.err_flag = w.err_flag;
-        if (int rc = half ? launch_tree_attention_tc(a, s, true) : launch_tree_attention_simt(a, s, true)) return launch_fail(rc, "tree attention");
+        int rc;
+        if (groups) {
+            const PrefixAttnArgs pa{a, groups->group_start, groups->prefix_len, groups->request_group, groups->groups};
+            rc = launch_prefix_attention(pa, scratch_dev, s, true);
+        } else {
+            rc = half ? launch_tree_attention_tc(a, s, true) : launch_tree_attention_simt(a, s, true);
+        }
+        if (rc != ZOQAT_OK) return launch_fail(rc, groups ? "prefix attention" : "tree attention");
         if (half) launch_widen(att16, p.type, (int64_t)rows * d, w.att, s);
         launch_norm_act_operand(w.att, rows, d, 0, nullptr, nullptr, 0.f, c.a_bits, w.xa, w.row_step, nullptr, s, SmoothAct(), true, planes);
         if (int rc = gemv(dl.w_o, dl.q_o, d, d, Ly.vec[ZOQAT_ROLE_BO], 1, w.h)) return rc;
@@ -2051,6 +2062,19 @@ int zoqat_decode_tree_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows
     }
     CUDA_TRY(cudaGetLastError());
     return ZOQAT_OK;
+}
+
+int zoqat_decode_tree_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows, const zoqat_tree_batch_t* plan,
+                           const zoqat_paged_cache_t* caches, const zoqat_logit_rules_t* rules, float* logits_dev,
+                           int32_t* next_token_dev, void* scratch_dev, size_t scratch_bytes, void* stream) {
+    return tree_step(m, tokens_dev, rows, plan, nullptr, caches, rules, logits_dev, next_token_dev, scratch_dev, scratch_bytes, stream);
+}
+
+int zoqat_decode_prefix_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows, const zoqat_tree_batch_t* plan, const zoqat_prefix_groups_t* groups,
+                             const zoqat_paged_cache_t* caches, const zoqat_logit_rules_t* rules, float* logits_dev,
+                             int32_t* next_token_dev, void* scratch_dev, size_t scratch_bytes, void* stream) {
+    if (!groups) return fail(ZOQAT_ERR_INVALID_ARG, "NULL argument");
+    return tree_step(m, tokens_dev, rows, plan, groups, caches, rules, logits_dev, next_token_dev, scratch_dev, scratch_bytes, stream);
 }
 
 }  // extern "C"
@@ -2194,7 +2218,8 @@ int zoqat_op_cache_copy(const zoqat_paged_cache_t* caches, int n_layers, const i
         if (int rc = paged_cache(caches + l, c[0])) return rc;
         if ((int64_t)c[0].page_size * c[0].n_kv_heads > INT32_MAX / 2) return fail(ZOQAT_ERR_UNSUPPORTED, "layer %d: a page of 2^30 or more heads", l);
     }
-    for (int l = 0; l < n_layers && rows > 0; l += kCopyLayers) {
+    if (rows == 0) return ZOQAT_OK;
+    for (int l = 0; l < n_layers; l += kCopyLayers) {
         const int n = n_layers - l < kCopyLayers ? n_layers - l : kCopyLayers;
         for (int k = 0; k < n; ++k) paged_cache(caches + l + k, c[k]);
         if (launch_cache_copy(c, n, from_dev, to_dev, len_dev, rows, err_flag_dev, static_cast<cudaStream_t>(stream)) != 0) return launch_fail(ZOQAT_ERR_CUDA, "cache copy");

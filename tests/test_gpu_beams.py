@@ -571,3 +571,147 @@ def test_prefix_attention_no_rows(zq):
     k, v = make_cache(4, 16, 2, 64, "bf16", "token")
     out, err = zq.zoqat_op_prefix_attention(torch.empty((0, 4, 64), dtype=torch.bfloat16, device="cuda"), k, v, ints([[0]]), ints([0]), ints([0, 0]), ints([0, 1]), ints([0]), ints([0]))
     assert out.shape == (0, 4, 64) and int(err) == 0
+
+
+# ---- a beam search through a packed model ---------------------------------------------------------------------------
+def beam_search(zq, shape, model, prompts, K, page, dtype, steps, eos, shared):
+    """Beams of all prompts as requests of one batch, advanced by the operators alone.  shared: the prompts' keys are attended to once (zoqat_decode_prefix_step).
+    Returns (tokens, score) of every beam at the end, the finished ones as (tokens, score), and the number of pages copied."""
+    G, B, V, n_pages, M = len(prompts), len(prompts) * K, shape["vocab"], 400, 24
+    dh, longest = shape["d_model"] // shape["n_heads"], max(map(len, prompts)) + steps + 1
+    caches = [make_cache(n_pages, page, shape["n_heads"], dh, dtype, "token", seed=l) for l in range(shape["n_layers"])]
+    M = -(-longest // page) + 1
+    layers = zq.LayerCaches(caches)
+    table = torch.full((B, M), -1, dtype=torch.int32, device="cuda")
+    free = torch.randperm(n_pages, generator=torch.Generator().manual_seed(3)).to(torch.int32).cuda()
+    n_free, cached = ints([n_pages]), ints([0] * B)
+    # the prompts, through the first beam of each
+    todo, last = [list(p) for p in prompts], [None] * G
+    while any(todo):
+        share = [min(len(t), 8 // G) for t in todo]
+        flat = [x for t, n in zip(todo, share) for x in t[:n]]
+        plan = zq.zoqat_op_cache_plan(cached, ints([share[b // K] if b % K == 0 else 0 for b in range(B)]), page, n_pages, free, n_free, table, 8)
+        logits, _ = model.zoqat_decode_tree_step(ints(flat + [0] * (8 - len(flat))), plan, table, caches)
+        at = 0
+        for g in range(G):
+            at += share[g]
+            if share[g]:
+                last[g] = logits[at - 1].clone()
+        todo = [t[n:] for t, n in zip(todo, share)]
+        cached, n_free = plan["kv_len"], plan["n_free"]
+    groups = (ints([g * K for g in range(G + 1)]), ints([len(p) for p in prompts]), ints([b // K for b in range(B)]))
+    logits = torch.stack(last).repeat_interleave(K, 0)
+    score = torch.full((G, K), -math.inf, device="cuda")
+    score[:, 0] = 0.0
+    history = torch.zeros((B, longest), dtype=torch.int32, device="cuda")
+    for b in range(B):
+        history[b, : len(prompts[b // K])] = ints(prompts[b // K])
+    history_len = ints([len(prompts[b // K]) if b % K == 0 else 0 for b in range(B)])
+    done, copies = [], 0
+    for step in range(steps):
+        best = zq.zoqat_op_beam_select(logits, score, eos=ints(eos))
+        for g in range(G):                                        # finished ones: the parent's tokens, then the one that ends
+            for k in range(K):
+                if int(best["done_beam"][g, k]) >= 0:
+                    row = g * K + int(best["done_beam"][g, k])
+                    done.append((history[row, : int(history_len[row])].tolist() + [int(best["done_token"][g, k])], float(best["done_score"][g, k])))
+        out = zq.zoqat_op_beam_reorder(best["beam"], cached, table, page, n_pages, free, n_free, history=history, history_len=history_len, token=best["token"])
+        zq.zoqat_op_cache_copy(layers, out["copy_from"], out["copy_to"], out["copy_len"], err=out["status"])
+        assert int(out["status"]) == 0
+        table, cached, free, n_free, history, history_len = (out[n] for n in ("block_table", "kv_len", "free_pages", "n_free", "history", "history_len"))
+        copies += int((out["copy_len"] > 0).sum())
+        held = {p for b in range(B) for p in table[b, : -(-int(cached[b]) // page)].tolist()}
+        spare = free[: int(n_free)].tolist()
+        assert len(held) + len(spare) == n_pages and held.isdisjoint(spare) and held | set(spare) == set(range(n_pages))      # no page is lost or held twice
+        score = best["score"]
+        plan = zq.zoqat_op_cache_plan(cached, ints([1] * B), page, n_pages, free, n_free, table, B)
+        assert int(plan["status"]) == 0
+        if shared:
+            logits, _ = model.zoqat_decode_prefix_step(best["token"].view(-1).clamp(min=0), plan, table, *groups, caches)
+        else:
+            logits, _ = model.zoqat_decode_tree_step(best["token"].view(-1).clamp(min=0), plan, table, caches)
+        model.zoqat_check()
+        cached, n_free = plan["kv_len"], plan["n_free"]
+    live = [(history[b, : int(history_len[b])].tolist(), float(score.view(-1)[b])) for b in range(B)]
+    return live, done, copies
+
+
+@pytest.mark.parametrize("name,dtype,page,K,lengths", [("llama_w4a8", "f32", 16, 4, (37, 70)), ("llama_w4", "bf16", 16, 4, (135, 150)), ("opt_w3a8", "f32", 5, 8, (40,)),
+                                                       ("llama_w4a8", "f16", 8, 2, (5, 130, 140, 131))])
+def test_beam_search_through_a_packed_model(zq, name, dtype, page, K, lengths):
+    from test_gpu_serve import packed_model, sequential_logits
+    shape, model = packed_model(zq, name, 8, 192)
+    _, other = packed_model(zq, name, 2, 192)
+    rng = np.random.default_rng(4)
+    prompts = [rng.integers(3, shape["vocab"], n).tolist() for n in lengths]
+    eos = [int(x) for x in rng.integers(3, shape["vocab"], 2)]
+    live, done, copies = beam_search(zq, shape, model, prompts, K, page, dtype, 7, eos, shared=True)
+    assert copies > 0
+    # every hypothesis' score is the sum of its tokens' log-probabilities by the one-token path, which keeps no pages: a row that followed the wrong
+    # beam, or lost a key of its page, is off by whole units.  Per token the logits differ by up to 2 % (5 % with bf16 keys) of their scale
+    # (a difference of one code in one activation; see the test of drafts), the log of their sum by as much again.
+    tol = {"f32": 2e-2, "f16": 2e-2, "bf16": 5e-2}[dtype]
+    for tokens, score in (live[:: max(1, len(live) // 4)] + done[:2]):
+        p = next(p for p in prompts if tokens[: len(p)] == p)
+        want, bound = 0.0, 0.0
+        for i in range(len(p), len(tokens)):
+            logits = sequential_logits(other, tokens[:i], 2).double()
+            want += float(torch.log_softmax(logits, 0)[tokens[i]])
+            bound += 2 * tol * float(logits.abs().max())
+        assert abs(score - want) <= bound, (score, want, bound)
+    for g in range(len(prompts)):
+        mine = [s for _, s in live[g * K: (g + 1) * K]]
+        assert mine == sorted(mine, reverse=True) and len({tuple(t) for t, _ in live[g * K: (g + 1) * K]}) == K
+
+
+def test_prefix_step_is_the_tree_step(zq):
+    """The same search with and without the shared prefix: the same first beams, the same scores up to the attention's rounding."""
+    from test_gpu_serve import packed_model
+    shape, model = packed_model(zq, "llama_w4a8", 8, 192)
+    prompts = [list(range(3, 60)), list(range(100, 190))]
+    one, two = [beam_search(zq, shape, model, prompts, 4, 16, "f32", 3, [1], shared) for shared in (True, False)]
+    for (a, x), (b, y) in zip(one[0], two[0]):
+        assert abs(x - y) <= 0.05 * max(1.0, abs(y))
+    with pytest.raises(zq.ZoqatError):
+        model.zoqat_decode_prefix_step(ints([1]), dict(kv_len=ints([1]), row_start=ints([0, 1]), row_pos=ints([0]), slot=ints([0])), ints([[0]]), ints([0, 1]), ints([0]),
+                                       ints([0]), [make_cache(4, 16, 2, 64, "f32", "token")] * 2, scratch=torch.empty(1 << 16, dtype=torch.uint8, device="cuda"))
+
+
+def test_the_operators_of_a_layer_in_a_row(zq):
+    """A layer's new rows with head norms and interleaved rotation at far positions, into pages and through the shared-prefix attention: against float64 from end to end."""
+    G, K, prefix, heads, kv, dh, page = 2, 3, [300, 170], 4, 2, 64, 16
+    B, gen = G * K, torch.Generator(device="cuda").manual_seed(8)
+    freq, mag = zq.rotary_frequencies(32, kind=zq.ROTARY_LINEAR, factor=8.0)
+    qg, kg = 1 + 0.2 * torch.randn((2, dh), generator=gen, device="cuda")
+    L = [prefix[b // K] + 1 for b in range(B)]
+    n_pages = 100
+    k, v = make_cache(n_pages, page, kv, dh, "bf16", "token")
+    table, free = torch.full((B, 24), -1, dtype=torch.int32, device="cuda"), torch.arange(n_pages, dtype=torch.int32, device="cuda")
+    wide = (heads + 2 * kv) * dh
+    # the prompts' rows through the first beam of each group, then their pages for all beams
+    plan = zq.zoqat_op_cache_plan(ints([0] * B), ints([prefix[b // K] if b % K == 0 else 0 for b in range(B)]), page, n_pages, free, ints([n_pages]), table, sum(prefix))
+    x = torch.randn((sum(prefix), wide), generator=gen, device="cuda")
+    far = 100000
+    zq.zoqat_op_rotary_append(x, plan["row_pos"] + far, plan["slot"], k, v, heads, freq=freq, interleaved=True, magnitude=mag, q_gain=qg, k_gain=kg)
+    out = zq.zoqat_op_beam_reorder(ints([[0] * K] * G), plan["kv_len"], table, page, n_pages, free, plan["n_free"])
+    zq.zoqat_op_cache_copy(zq.LayerCaches([(k, v)]), out["copy_from"], out["copy_to"], out["copy_len"])
+    step = zq.zoqat_op_cache_plan(out["kv_len"], ints([1] * B), page, n_pages, out["free_pages"], out["n_free"], out["block_table"], B)
+    y = torch.randn((B, wide), generator=gen, device="cuda")
+    q, err = zq.zoqat_op_rotary_append(y, step["row_pos"] + far, step["slot"], k, v, heads, freq=freq, interleaved=True, magnitude=mag, q_gain=qg, k_gain=kg)
+    got, err2 = zq.zoqat_op_prefix_attention(q, k, v, out["block_table"], step["kv_len"], step["row_start"], ints([0, K, 2 * K]), ints(prefix), ints([0] * K + [1] * K))
+    assert int(err) == int(err2) == 0 and step["kv_len"].tolist() == L
+    ref = lambda z, pos: append_reference(z, pos, heads, kv, dh, freq, True, mag, qg, kg, 1e-6)[0]  # noqa: E731
+    start = [0, prefix[0]]
+    for b in range(B):
+        g = b // K
+        pos = torch.arange(prefix[g] + 1, device="cuda") + far
+        rows = ref(torch.cat([x[start[g]: start[g] + prefix[g]], y[b: b + 1]]), pos)
+        for h in range(heads):
+            qq, kk, vv = rows[-1, h], rows[:, heads + h // 2], rows[:, heads + kv + h // 2]
+            w = torch.softmax(kk @ qq / math.sqrt(dh), 0)
+            want, size = w @ vv, w @ vv.abs()
+            # queries, keys, values, weights and outputs are rounded to bf16 once (2^-8 each): a score moves by two of those of the sum of its products'
+            # sizes, a weight relatively by twice that, and fp32's share (angles of far positions among it) is under a tenth of it
+            half, products = 2.0 ** -8, float((kk.abs() @ qq.abs()).max()) / math.sqrt(dh)
+            bound = 1.1 * ((4 * half * products + 2 * half) * size + half * want.abs())
+            assert bool(((got[b, h].double() - want).abs() <= bound).all())
