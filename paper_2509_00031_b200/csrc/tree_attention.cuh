@@ -80,9 +80,9 @@ struct PrefixWork : TreeWork {               // batch: parts in this launch
     int2* entries;                           // [2][rows * heads]: where a query's shared (0) and own (1) pieces are
     float* partial;                          // [2][rows * heads][d_head + 4]: output, reference, sum of parts that one CTA finished
 };
-// a / b rounded down or up for a power of two b (a + b < 2^31)
+// a / b rounded down or up for a power of two b
 __device__ __forceinline__ int prefix_down(int a, int b) { return a >> (31 - __clz(b)); }
-__device__ __forceinline__ int prefix_up(int a, int b) { return (int)((unsigned)(a + b - 1) >> (31 - __clz(b))); }
+__device__ __forceinline__ int prefix_up(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) >> (31 - __clz(b))); }
 
 // The shared part of group g; n_kt = 0: it has none, or (ok = false) its description contradicts itself.
 __device__ __forceinline__ PrefixRequest prefix_shared(const PrefixWork& w, int g, bool& ok) {

@@ -715,3 +715,94 @@ def test_the_operators_of_a_layer_in_a_row(zq):
             half, products = 2.0 ** -8, float((kk.abs() @ qq.abs()).max()) / math.sqrt(dh)
             bound = 1.1 * ((4 * half * products + 2 * half) * size + half * want.abs())
             assert bool(((got[b, h].double() - want).abs() <= bound).all())
+
+
+def test_a_captured_step_of_beams(zq):
+    """Selection, reordering, copies and attention in one graph: replayed on new logits and scores it gives what the calls give."""
+    G, K, V, page, n_pages, prefix = 2, 4, 9000, 16, 120, 200
+    B, rng = G * K, torch.Generator(device="cuda").manual_seed(6)
+    caches = [make_cache(n_pages, page, 2, 64, "bf16", "token", seed=l) for l in range(3)]
+    keep = [(k.clone(), v.clone()) for k, v in caches]
+    layers = zq.LayerCaches(caches)
+    common = list(range(12))
+    table = torch.full((B, 20), -1, dtype=torch.int32, device="cuda")
+    for b in range(B):
+        table[b, :13] = ints([x + 40 * (b // K) for x in common] + [20 + b % K + 40 * (b // K)])
+    kv_len = ints([prefix + 3] * B)
+    free, n_free = torch.arange(80, 120, dtype=torch.int32, device="cuda"), ints([40])
+    logits, score = torch.zeros((B, V), device="cuda"), torch.zeros((G, K), device="cuda")
+    q = torch.randn((B, 4, 64), generator=rng, device="cuda").to(torch.bfloat16)
+    rows, groups = ints(list(range(B + 1))), (ints([0, K, B]), ints([prefix - 8] * G), ints([0] * K + [1] * K))
+    scratch, attention, err = zq.beam_reorder_scratch(score), zq.prefix_attention_scratch(q, caches[0][0]), torch.zeros(1, dtype=torch.int32, device="cuda")
+    state = {}
+
+    def step(best=None, out=None, att=None):
+        best = zq.zoqat_op_beam_select(logits, score, eos=None, out=best)
+        out = zq.zoqat_op_beam_reorder(best["beam"], kv_len, table, page, n_pages, free, n_free, out=out, scratch=scratch)
+        zq.zoqat_op_cache_copy(layers, out["copy_from"], out["copy_to"], out["copy_len"], err=err)
+        att, _ = zq.zoqat_op_prefix_attention(q, *caches[0], out["block_table"], out["kv_len"], rows, *groups, out=att, scratch=attention, err=err)
+        return best, out, att
+
+    state = step()                                                # warm, and buffers for the graph
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step(*state)
+    for i in range(4):
+        logits.copy_(3 * torch.randn((B, V), generator=rng, device="cuda"))
+        score.copy_(-5 * torch.rand((G, K), generator=rng, device="cuda"))
+        for (k, v), (k0, v0) in zip(caches, keep):
+            k.copy_(k0)
+            v.copy_(v0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [{n: t.clone() for n, t in d.items()} for d in state[:2]] + [state[2].clone()] + [t.clone() for kv in caches for t in kv]
+        for (k, v), (k0, v0) in zip(caches, keep):
+            k.copy_(k0)
+            v.copy_(v0)
+        best, out, att = step()
+        live = lambda d: {n: t for n, t in d.items() if n not in ("block_table", "free_pages")}  # noqa: E731
+        assert all(torch.equal(got[0][n], best[n]) for n in best) and all(torch.equal(got[1][n], out[n]) for n in live(out))
+        assert torch.equal(got[1]["block_table"][:, :13], out["block_table"][:, :13]) and torch.equal(got[2], att)
+        assert all(torch.equal(x, y) for x, y in zip(got[3:], [t for kv in caches for t in kv])) and int(err) == 0 and int(out["status"]) == 0
+
+
+def test_large_batches_and_far_pages(zq):
+    """The largest batch of the selection's and the reordering's rules, and copies in pages that lie behind 2^32 elements."""
+    B, K = 16384, 4
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    parent = torch.randint(-1, K, (B, K), generator=gen, device="cuda").int()
+    table = torch.arange(B * K, dtype=torch.int32, device="cuda").view(B * K, 1)
+    kv_len = torch.randint(0, 5, (B * K,), generator=gen, device="cuda").int()
+    kv_len = kv_len.view(B, K)[:, :1].expand(B, K).contiguous().view(-1)
+    n_pages = 3 * B * K
+    free = torch.full((n_pages,), -1, dtype=torch.int32, device="cuda")
+    free[: 2 * B * K] = torch.arange(B * K, n_pages, dtype=torch.int32, device="cuda")
+    out = zq.zoqat_op_beam_reorder(parent, kv_len, table, 4, n_pages, free, ints([2 * B * K]))
+    want = reorder_reference(parent.tolist(), kv_len.tolist(), table.tolist(), 4, free.tolist(), 2 * B * K, [0] * B, [[0]] * (B * K), [0] * (B * K), [[0] * K] * B)
+    assert int(out["status"]) == 0 and out["kv_len"].tolist() == want["kv_len"] and int(out["n_free"]) == len(want["free"])
+    for n in ("copy_from", "copy_to", "copy_len"):
+        assert out[n].tolist() == want[n], n
+    assert out["free_pages"].tolist()[: len(want["free"])] == want["free"]
+    logits = torch.randn((B * 2, 700), generator=gen, device="cuda")
+    got = zq.zoqat_op_beam_select(logits, torch.zeros((B, 2), device="cuda"))
+    both = torch.log_softmax(logits.double(), 1).view(B, 2, 700).flatten(1)
+    top = both.max(1)
+    assert torch.equal(got["beam"][:, 0].long() * 700 + got["token"][:, 0], top.indices) and bool(((got["score"][:, 0].double() - top.values).abs() < 1e-5).all())
+    # 2 pages of 2^31 elements and more apart
+    stride = (1 << 31) + 4096
+    store = torch.empty(3 * stride, dtype=torch.bfloat16, device="cuda")
+    k = torch.as_strided(store, (3, 16, 2, 64), (stride, 128, 64, 1))
+    v = torch.as_strided(store, (3, 16, 2, 64), (stride, 128, 64, 1), 2048)
+    for t in (k, v):
+        t.copy_(torch.randn((3, 16, 2, 64), generator=gen, device="cuda").to(torch.bfloat16))
+    k0, v0 = k.clone(), v.clone()
+    err = zq.zoqat_op_cache_copy(zq.LayerCaches([(k, v)]), ints([0]), ints([2]), ints([9]))
+    assert int(err) == 0 and torch.equal(k[2, :9], k0[0, :9]) and torch.equal(k[2, 9:], k0[2, 9:]) and torch.equal(v[2, :9], v0[0, :9]) and torch.equal(v[1], v0[1])
+    qkv = torch.randn((2, 4 * 64 + 2 * 2 * 64), generator=gen, device="cuda")
+    q, err = zq.zoqat_op_rotary_append(qkv, ints([3, 4]), ints([2 * 16 + 15, 16]), k, v, 4, freq=zq.rotary_frequencies(64)[0])
+    assert int(err) == 0 and torch.equal(v[2, 15], qkv.view(2, -1, 64)[0, 6:].to(torch.bfloat16)) and torch.equal(v[1, 0], qkv.view(2, -1, 64)[1, 6:].to(torch.bfloat16))
+    out, err = zq.zoqat_op_prefix_attention(q, k, v, ints([[0, 2], [0, 1]]), ints([32, 17]), ints([0, 1, 2]), ints([0, 2]), ints([16]), ints([0, 0]))
+    other, _ = zq.zoqat_op_tree_attention(q, k, v, ints([[0, 2], [0, 1]]), ints([32, 17]), ints([0, 1, 2]))
+    # each of the two is off by the rounding of its weights and of its output: 2^-8 of the values' sizes, twice, and fp32's share
+    assert int(err) == 0 and float((out.double() - other.double()).abs().max()) <= 2 * 2.1 * 2.0 ** -8 * float(v[[0, 1, 2]].abs().max())
