@@ -495,6 +495,19 @@ def _flat(dev, name, t, dtype, n0, n1=None):
     return t.data_ptr()
 
 
+def _ints(dev, *named):
+    """Addresses of contiguous int32 tensors on device `dev`, each (name, tensor or None, shape)."""
+    at = []
+    for name, t, shape in named:
+        if t is None:
+            at.append(None)
+        elif t.dtype is _I32 and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+            at.append(t.data_ptr())
+        else:
+            _refuse(f"{name}: a contiguous int32 tensor of shape {shape} on the current CUDA device is needed")
+    return at
+
+
 def _rows(dev, name, t, dtype, rows, heads, d_head):
     """(address, row stride) of [>= rows, heads, d_head] whose rows may stand apart."""
     s, st = t.shape, t.stride()
@@ -751,17 +764,15 @@ def zoqat_op_beam_reorder(parent, kv_len, block_table, page_size, n_pages, free_
         scratch = beam_reorder_scratch(parent)
     if scratch.get_device() != dev or not scratch.is_contiguous():
         _refuse("scratch: a contiguous tensor on the current CUDA device is needed")
+    row, table, past = (rows,), (rows, m), (rows, stride)
     have = history is not None
-    r = BeamReorder(
-        _flat(dev, "parent", parent, _I32, batch, beams), _flat(dev, "kv_len", kv_len, _I32, rows), _flat(dev, "block_table", block_table, _I32, rows, m),
-        _flat(dev, "shared_len", shared_len, _I32, batch), _flat(dev, "free_pages", free_pages, _I32, cap), _flat(dev, "n_free", n_free, _I32, 1),
-        _flat(dev, "history", history, _I32, rows, stride), _flat(dev, "history_len", history_len, _I32, rows),
-        _flat(dev, "token", token.view(-1) if token is not None else None, _I32, rows),
-        _flat(dev, "block_table_out", out["block_table"], _I32, rows, m), _flat(dev, "kv_len_out", out["kv_len"], _I32, rows),
-        _flat(dev, "free_pages_out", out["free_pages"], _I32, cap), _flat(dev, "n_free_out", out["n_free"], _I32, 1),
-        _flat(dev, "copy_from", out["copy_from"], _I32, rows), _flat(dev, "copy_to", out["copy_to"], _I32, rows), _flat(dev, "copy_len", out["copy_len"], _I32, rows),
-        _flat(dev, "history_out", out["history"], _I32, rows, stride) if have else None, _flat(dev, "history_len_out", out["history_len"], _I32, rows) if have else None,
-        _flat(dev, "status", out["status"], _I32, 1), stride, batch, beams, page_size, n_pages, m, cap)
+    r = BeamReorder(*_ints(
+        dev, ("parent", parent, (batch, beams)), ("kv_len", kv_len, row), ("block_table", block_table, table), ("shared_len", shared_len, (batch,)),
+        ("free_pages", free_pages, (cap,)), ("n_free", n_free, (1,)), ("history", history, past), ("history_len", history_len, row),
+        ("token", token, row if token is None or len(token.shape) == 1 else (batch, beams)), ("block_table_out", out["block_table"], table),
+        ("kv_len_out", out["kv_len"], row), ("free_pages_out", out["free_pages"], (cap,)), ("n_free_out", out["n_free"], (1,)), ("copy_from", out["copy_from"], row),
+        ("copy_to", out["copy_to"], row), ("copy_len", out["copy_len"], row), ("history_out", out["history"] if have else None, past),
+        ("history_len_out", out["history_len"] if have else None, row), ("status", out["status"], (1,))), stride, batch, beams, page_size, n_pages, m, cap)
     _check(lib().zoqat_op_beam_reorder(r, scratch.data_ptr(), scratch.numel() * scratch.element_size(), stream))
     return out
 
