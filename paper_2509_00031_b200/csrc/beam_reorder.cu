@@ -11,6 +11,7 @@
 //   beam_place_kernel   (dependent launch) every CTA sums the counts of the requests before its own, lists its pages in the order column,
 //                       row, hands them to its new rows and writes what is left behind the free pages
 // The order of all lists is fixed by rows and columns, so the same call gives the same pages.
+//   beam_reorder_kernel both in one, for few requests
 //   cache_copy_kernel   slots of pages, for all layers in one launch; bound by memory
 #include "common.cuh"
 #include "serve.cuh"
@@ -34,35 +35,37 @@ struct Request {
     int shared, status;
 };
 
+// By one warp.
+__device__ __forceinline__ void read_request_warp(const ReorderArgs& a, int b, Request& r) {
+    const int lane = threadIdx.x & 31, K = a.beams, P = a.page_size;
+    const bool mine = lane < K;
+    int bad = 0;
+    int len = mine ? __ldg(a.kv_len + (int64_t)b * K + lane) : 0, parent = mine ? __ldg(a.parent + (int64_t)b * K + lane) : -1;
+    if (len < 0 || len > (int64_t)a.max_pages * P) { len = 0; bad |= kPlanBadLength; }
+    if (parent < -1 || parent >= K) { parent = -1; bad |= kPlanBadParent; }
+    int shared = a.shared_len ? __ldg(a.shared_len + b) : 0;
+    if (shared < 0) { shared = 0; bad |= kPlanBadLength; }
+    const int new_len = __shfl_sync(0xffffffffu, len, parent < 0 ? 0 : parent);
+    const bool part = parent >= 0 && new_len % P != 0;
+    const int last = new_len / P;                                // < max_pages: the page exists
+    const int page = part ? __ldg(a.block_table + ((int64_t)b * K + parent) * a.max_pages + last) : -1;
+    bool keep = part && (int64_t)last * P >= shared;
+    for (int j = 0; j < K; ++j) {
+        const int pg = __shfl_sync(0xffffffffu, page, j), lt = __shfl_sync(0xffffffffu, last, j);
+        const bool pt = __shfl_sync(0xffffffffu, (int)part, j);
+        if (j < lane && pt && pg == page && lt == last) keep = false;
+    }
+    if (part && (page < 0 || page >= a.n_pages)) { bad |= kPlanBadPage; keep = true; }      // nothing to copy from
+    if (mine) { r.len[lane] = len; r.held[lane] = len / P + (len % P != 0); r.parent[lane] = parent; }
+    const unsigned copies = __ballot_sync(0xffffffffu, part && !keep);
+    const unsigned full = __reduce_or_sync(0xffffffffu, parent >= 0 ? 1u << parent : 0u);
+    const unsigned kept = __reduce_or_sync(0xffffffffu, keep ? 1u << parent : 0u);
+    bad = __reduce_or_sync(0xffffffffu, (unsigned)bad);
+    if (lane == 0) { r.full = full; r.kept = kept; r.copies = copies; r.shared = shared; r.status = bad; }
+}
 // Called by all threads; the first warp fills `r`.  Ends with a barrier.
 __device__ __forceinline__ void read_request(const ReorderArgs& a, int b, Request& r) {
-    const int lane = threadIdx.x & 31, K = a.beams, P = a.page_size;
-    if (threadIdx.x < 32) {
-        const bool mine = lane < K;
-        int bad = 0;
-        int len = mine ? __ldg(a.kv_len + (int64_t)b * K + lane) : 0, parent = mine ? __ldg(a.parent + (int64_t)b * K + lane) : -1;
-        if (len < 0 || len > (int64_t)a.max_pages * P) { len = 0; bad |= kPlanBadLength; }
-        if (parent < -1 || parent >= K) { parent = -1; bad |= kPlanBadParent; }
-        int shared = a.shared_len ? __ldg(a.shared_len + b) : 0;
-        if (shared < 0) { shared = 0; bad |= kPlanBadLength; }
-        const int new_len = __shfl_sync(0xffffffffu, len, parent < 0 ? 0 : parent);
-        const bool part = parent >= 0 && new_len % P != 0;
-        const int last = new_len / P;                            // < max_pages: the page exists
-        const int page = part ? __ldg(a.block_table + ((int64_t)b * K + parent) * a.max_pages + last) : -1;
-        bool keep = part && (int64_t)last * P >= shared;
-        for (int j = 0; j < K; ++j) {
-            const int pg = __shfl_sync(0xffffffffu, page, j), lt = __shfl_sync(0xffffffffu, last, j);
-            const bool pt = __shfl_sync(0xffffffffu, (int)part, j);
-            if (j < lane && pt && pg == page && lt == last) keep = false;
-        }
-        if (part && (page < 0 || page >= a.n_pages)) { bad |= kPlanBadPage; keep = true; }      // nothing to copy from
-        if (mine) { r.len[lane] = len; r.held[lane] = (len + P - 1) / P; r.parent[lane] = parent; }
-        const unsigned copies = __ballot_sync(0xffffffffu, part && !keep);
-        const unsigned full = __reduce_or_sync(0xffffffffu, parent >= 0 ? 1u << parent : 0u);
-        const unsigned kept = __reduce_or_sync(0xffffffffu, keep ? 1u << parent : 0u);
-        bad = __reduce_or_sync(0xffffffffu, (unsigned)bad);
-        if (lane == 0) { r.full = full; r.kept = kept; r.copies = copies; r.shared = shared; r.status = bad; }
-    }
+    if (threadIdx.x < 32) read_request_warp(a, b, r);
     __syncthreads();
 }
 
@@ -99,6 +102,34 @@ __device__ __forceinline__ int block_sum(int x, int* part) {
     return sum;
 }
 
+// Tables and histories, row by row: rows first, first + step, ... of a request.
+__device__ __forceinline__ void move_rows(const ReorderArgs& a, const Request& r, int64_t row0, int first, int step) {
+    const int tid = threadIdx.x;
+    for (int j = first; j < a.beams; j += step) {
+        const int from = r.parent[j];
+        const int64_t src = row0 + (from < 0 ? 0 : from), dst = row0 + j;
+        const int n = from < 0 ? 0 : r.held[from], skip = (r.copies >> j) & 1u ? n - 1 : -1;      // (a copied page's entry is another's to write)
+        int bad = 0;
+        for (int c = tid; c < n; c += kThreads) {
+            const int page = __ldg(a.block_table + src * a.max_pages + c);
+            if (page < 0 || page >= a.n_pages) bad = kPlanBadPage;
+            if (c != skip) a.table_out[dst * a.max_pages + c] = page;
+        }
+        if (a.history) {
+            int64_t h = from < 0 ? 0 : __ldg(a.history_len + src);
+            const int64_t room = a.history_stride - (a.token ? 1 : 0);
+            if (h < 0 || h > room) { bad |= kPlanBadLength; h = 0; }
+            for (int64_t i = tid; i < h; i += kThreads) a.history_out[dst * a.history_stride + i] = __ldg(a.history + src * a.history_stride + i);
+            if (tid == 0) {
+                const bool more = a.token && from >= 0 && h <= room;
+                if (more) a.history_out[dst * a.history_stride + h] = __ldg(a.token + dst);
+                a.history_len_out[dst] = (int)h + (more ? 1 : 0);
+            }
+        }
+        if (bad) atomicOr(a.status, bad);
+    }
+}
+
 __global__ void __launch_bounds__(kThreads)
 beam_count_kernel(const ReorderParams p) {
     __shared__ Request r;
@@ -120,53 +151,23 @@ beam_count_kernel(const ReorderParams p) {
         }
         return;
     }
-    // tables and histories, row by row (a copied page's entry is put right by the second launch)
-    for (int j = blockIdx.y - 1; j < K; j += gridDim.y - 1) {
-        const int from = r.parent[j];
-        const int64_t src = row0 + (from < 0 ? 0 : from), dst = row0 + j;
-        const int n = from < 0 ? 0 : r.held[from];
-        int bad = 0;
-        for (int c = tid; c < n; c += kThreads) {
-            const int page = __ldg(a.block_table + src * a.max_pages + c);
-            if (page < 0 || page >= a.n_pages) bad = kPlanBadPage;
-            a.table_out[dst * a.max_pages + c] = page;
-        }
-        if (a.history) {
-            int64_t h = from < 0 ? 0 : __ldg(a.history_len + src);
-            const int64_t room = a.history_stride - (a.token ? 1 : 0);
-            if (h < 0 || h > room) { bad |= kPlanBadLength; h = 0; }
-            for (int64_t i = tid; i < h; i += kThreads) a.history_out[dst * a.history_stride + i] = __ldg(a.history + src * a.history_stride + i);
-            if (tid == 0) {
-                const bool more = a.token && from >= 0 && h <= room;
-                if (more) a.history_out[dst * a.history_stride + h] = __ldg(a.token + dst);
-                a.history_len_out[dst] = (int)h + (more ? 1 : 0);
-            }
-        }
-        if (bad) atomicOr(a.status, bad);
-    }
+    move_rows(a, r, row0, blockIdx.y - 1, gridDim.y - 1);
 }
 
-__global__ void __launch_bounds__(kThreads)
-beam_place_kernel(const ReorderParams p) {
-    __shared__ Request r;
-    __shared__ int part[kThreads / 32];
-    __shared__ int mine[kMaxBeams];                              // pages that the request's own new rows take over
-    const ReorderArgs& a = p.a;
-    const int b = blockIdx.x, K = a.beams, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+// Gives the request's new rows their pages and lists those it gives back; counts: [batch][2].
+__device__ __forceinline__ void place_pages(const ReorderArgs& a, const Request& r, int b, const int32_t* counts, int n_free, int* part, int* mine) {
+    const int K = a.beams, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t row0 = (int64_t)b * K;
-    read_request(a, b, r);                                       // (inputs only: may run ahead of the counts)
-    int n_free = __ldg(a.n_free);
-    grid_dependency_wait();
     int taken = 0, given = 0, taken_before = 0, given_before = 0, most = 0;
     for (int i = tid; i < a.batch; i += kThreads) {
-        const int gone = p.counts[2 * i], want = p.counts[2 * i + 1], inside = min(gone, want);
+        const int gone = counts[2 * i], want = counts[2 * i + 1], inside = min(gone, want);
         taken += want - inside;
         given += gone - inside;
         if (i < b) { taken_before += want - inside; given_before += gone - inside; }
     }
     taken = block_sum(taken, part); given = block_sum(given, part);
     taken_before = block_sum(taken_before, part); given_before = block_sum(given_before, part);
-    const int own_gone = p.counts[2 * b], own_want = p.counts[2 * b + 1], inside = min(own_gone, own_want);
+    const int own_gone = counts[2 * b], own_want = counts[2 * b + 1], inside = min(own_gone, own_want);
     // nothing is reordered where lengths are impossible or pages are short
     int bad = n_free < 0 || n_free > a.free_capacity ? kPlanBadLength : 0;
     if (bad) n_free = 0;
@@ -227,6 +228,52 @@ beam_place_kernel(const ReorderParams p) {
     }
 }
 
+__global__ void __launch_bounds__(kThreads)
+beam_place_kernel(const ReorderParams p) {
+    __shared__ Request r;
+    __shared__ int part[kThreads / 32];
+    __shared__ int mine[kMaxBeams];                              // pages that the request's own new rows take over
+    read_request(p.a, blockIdx.x, r);                            // (inputs only: may run ahead of the counts)
+    const int n_free = __ldg(p.a.n_free);
+    grid_dependency_wait();
+    place_pages(p.a, r, blockIdx.x, p.counts, n_free, part, mine);
+}
+
+// Few requests: every CTA counts for all of them itself, its warps shared out, so one launch does it.
+__global__ void __launch_bounds__(kThreads)
+beam_reorder_kernel(const ReorderParams p) {
+    __shared__ Request all[kThreads / 32];
+    __shared__ int32_t counts[2 * (kThreads / 32)];
+    __shared__ int part[kThreads / 32];
+    __shared__ int mine[kMaxBeams];
+    const ReorderArgs& a = p.a;
+    const int b = blockIdx.x, K = a.beams, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (blockIdx.y > 0) {
+        read_request(a, b, all[0]);
+        move_rows(a, all[0], (int64_t)b * K, blockIdx.y - 1, gridDim.y - 1);
+        return;
+    }
+    const int n_free = __ldg(a.n_free);
+    if (tid < 2 * a.batch) counts[tid] = 0;
+    if (warp < a.batch) read_request_warp(a, warp, all[warp]);
+    __syncthreads();
+    const int share = kThreads / 32 / a.batch, of = warp / share;          // warps of a request
+    if (of < a.batch) {
+        const Request& r = all[of];
+        int most = 0, n = 0;
+        for (int k = 0; k < K; ++k) most = max(most, r.held[k]);
+        for (int c = (warp - of * share) * 32 + lane; c < most; c += 32 * share) n += __popc(pages_gone(a, r, (int64_t)of * K, c));
+        n = __reduce_add_sync(0xffffffffu, n);
+        if (lane == 0) {
+            atomicAdd(counts + 2 * of, n);
+            if (warp == of * share) counts[2 * of + 1] = __popc(r.copies);
+            if (warp == b * share && r.status) atomicOr(a.status, r.status);
+        }
+    }
+    __syncthreads();
+    place_pages(a, all[b], b, counts, n_free, part, mine);
+}
+
 // ---- copies ---------------------------------------------------------------------------------------------------------
 struct CopyParams {
     void* kv[2 * kCopyLayers];               // k and v of every layer
@@ -276,6 +323,12 @@ size_t beam_reorder_scratch_bytes(int batch) { return (size_t)batch * 2 * sizeof
 int launch_beam_reorder(const ReorderArgs& a, void* scratch, cudaStream_t s) {
     ReorderParams p{a, static_cast<int32_t*>(scratch)};
     const int y = 1 + (a.beams < 148 * 4 / a.batch ? a.beams : (a.beams + 3) / 4);
+    // one launch while a request's warps get through its columns in a few rounds (the second launch costs the host 2 us and the device 4)
+    if (a.batch <= kThreads / 32 && a.max_pages <= 256) {
+        if (launch_kernel(beam_reorder_kernel, dim3(a.batch, y), dim3(kThreads), 0, s, false, p) != cudaSuccess) return -1;
+        count_launch();
+        return 0;
+    }
     if (launch_kernel(beam_count_kernel, dim3(a.batch, y), dim3(kThreads), 0, s, false, p) != cudaSuccess) return -1;
     count_launch();
     if (launch_kernel(beam_place_kernel, dim3(a.batch), dim3(kThreads), 0, s, true, p) != cudaSuccess) return -1;
