@@ -68,8 +68,8 @@ prefix_narrow_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     if (tid == 0) { prefetch_tmap(&map_k); prefetch_tmap(&map_v); }
     if (!w.late_wait) grid_dependency_wait();
     grid_dependency_release();
-    prefix_find_runs<kWarps>(w, scan, runs);
-    if (blockIdx.x == gridDim.x - 1) prefix_map_rows(w, scan);
+    const int ctas = prefix_find_runs<kWarps>(w, scan, runs);
+    if ((int)blockIdx.x == max(ctas, 1) - 1 && w.first + w.batch > w.groups) prefix_map_rows(w, scan);
     const TreeRunT<PrefixWork>& run = runs[warp];
     const int n_tiles = (int)(run.end - run.begin);
     if (lane == 0) prefix_front(p.scratch)[worker] = n_tiles > 0 && !run.at.item_begins();

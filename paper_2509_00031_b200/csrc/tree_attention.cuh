@@ -77,6 +77,9 @@ struct PrefixWork : TreeWork {               // batch: parts in this launch
     int first;                               // the launch's first part: 0 .. groups - 1 are groups, then come the requests
     int* row_sides;                          // [rows]
     bool late_wait;                          // the launch before left nothing that this one reads: waited for at the end
+    // Where groups and requests go to different kernels, the two launches share the SMs out (prefix_share); other_time = 0: the launch has them all.
+    int tile_time, other_time;               // of a key tile on an SM, here and in the other launch, in the same unit
+    int other_rows, other_keys, other_cost;  // tile_rows, key_tile, item_cost of the other launch
     int2* entries;                           // [2][rows * heads]: where a query's shared (0) and own (1) pieces are
     float* partial;                          // [2][rows * heads][d_head + 4]: output, reference, sum of parts that one CTA finished
 };
@@ -249,13 +252,28 @@ __device__ __forceinline__ void tree_find_run(const W& w, long long* part, TreeR
     __syncthreads();
 }
 
+// How many of `grid` CTAs the groups' launch has, from the time of one SM that both need (the requests' launch has the others): both end at the same time then,
+// and reading the keys of one overlaps the arithmetic of the other.  128 requests behind 16001 keys, 1 to 1500 own (128 queries a tile / a warp's runs), the groups' on 148 CTAs
+// and the requests' on as many behind them 147 us, side by side on 64 + 84 / 80 + 68 / 96 + 52 CTAs 120 / 106 / 130; 8 x 8 beams behind 3000 to 16000 keys, 17 to 300 own (keys
+// as rows / a warp's runs) 92 against 87 / 80 / 87 on 96 / 128 / 134 CTAs.  A single group has items of one length: a whole number of CTAs for each
+// spares every CTA the second item that it would open (in the first example 72 CTAs, which is no multiple of 16 items, take 139 us).
+__device__ __forceinline__ int prefix_share(long long shared, long long own, long long items, int grid, bool even) {
+    if (shared == 0) return 0;
+    const long long sum = shared + own;
+    const int most = own ? grid - 1 : grid;
+    int ctas = (int)((2 * grid * shared + sum) / (2 * sum));
+    ctas = max(1, min(ctas, most));
+    if (even && items <= ctas) ctas = min((ctas + (int)items / 2) / (int)items, most / (int)items) * (int)items;
+    return ctas;
+}
+
 // The same for lists of parts, whose descriptions take several dependent reads: the threads keep those that they scanned in shared memory, and the edges of
 // the runs are looked up side by side.  N workers per CTA (1, or its warps): out[0 .. N - 1] are their runs, *end the part in which the last of them ends.
 struct PrefixScan {
     static constexpr int kMost = 384;        // threads of a block, and parts whose descriptions are kept
     long long units[kMost], tiles[kMost];    // before the parts of each thread
     PrefixRequest part[kMost];               // one part to a thread
-    long long sums[2 * kMost / 32];
+    long long sums[4 * kMost / 32];
     int kept;                                // descriptions in `part`
 };
 __device__ __forceinline__ void prefix_load(const PrefixWork& w, const PrefixScan& scan, int b, PrefixRequest& r) {
@@ -293,8 +311,9 @@ struct PrefixCursor {
         kt = r.kt0;
     }
 };
+// Returns how many CTAs have runs.
 template <int N>
-__device__ __forceinline__ void prefix_find_runs(const PrefixWork& w, PrefixScan& scan, TreeRunT<PrefixWork>* out) {
+__device__ __forceinline__ int prefix_find_runs(const PrefixWork& w, PrefixScan& scan, TreeRunT<PrefixWork>* out) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
     const int per = (w.batch + blockDim.x - 1) / blockDim.x;
     const int b0 = min(tid * per, w.batch), b1 = min(b0 + per, w.batch);
@@ -306,24 +325,63 @@ __device__ __forceinline__ void prefix_find_runs(const PrefixWork& w, PrefixScan
         tiles += n * (r.n_kt - r.kt0);
         if (per == 1) scan.part[b] = r;
     }
+    long long other_tiles = 0, other_items = 0;
+    if (w.other_time) {
+        PrefixWork o = w;
+        o.tile_rows = w.other_rows; o.key_tile = w.other_keys;
+        o.first = w.first ? 0 : w.groups;
+        const int parts = w.first ? w.groups : w.requests;
+        for (int b = tid; b < parts; b += blockDim.x) {
+            const PrefixRequest r = tree_request(o, b);
+            const long long n = r.n_kt ? (long long)w.n_kv * r.n_rt : 0;
+            other_items += n;
+            other_tiles += n * (r.n_kt - r.kt0);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            other_tiles += __shfl_xor_sync(0xffffffffu, other_tiles, o);
+            other_items += __shfl_xor_sync(0xffffffffu, other_items, o);
+        }
+    }
     long long up_tiles = tiles, up_items = items;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const long long u = __shfl_up_sync(0xffffffffu, up_tiles, o), v = __shfl_up_sync(0xffffffffu, up_items, o);
         if (lane >= o) { up_tiles += u; up_items += v; }
     }
-    if (lane == 31) { scan.sums[2 * warp] = up_tiles; scan.sums[2 * warp + 1] = up_items; }
+    if (lane == 31) { scan.sums[4 * warp] = up_tiles; scan.sums[4 * warp + 1] = up_items; scan.sums[4 * warp + 2] = other_tiles; scan.sums[4 * warp + 3] = other_items; }
     if (tid == 0) scan.kept = per == 1 ? w.batch : 0;
     __syncthreads();
     long long all_tiles = 0, all_items = 0;
+    other_tiles = other_items = 0;
     for (int k = 0; k < warps; ++k) {
         if (k == warp) { up_tiles += all_tiles; up_items += all_items; }
-        all_tiles += scan.sums[2 * k];
-        all_items += scan.sums[2 * k + 1];
+        all_tiles += scan.sums[4 * k];
+        all_items += scan.sums[4 * k + 1];
+        other_tiles += scan.sums[4 * k + 2];
+        other_items += scan.sums[4 * k + 3];
     }
-    scan.units[tid] = (up_tiles - tiles) + w.item_cost * (up_items - items);
+    int ctas = gridDim.x, item_cost = w.item_cost;
+    if (w.other_time) {
+        const long long mine = w.tile_time * (all_tiles + item_cost * all_items), theirs = w.other_time * (other_tiles + w.other_cost * other_items);
+        const bool even = w.groups == 1;
+        if (w.first) ctas -= prefix_share(theirs, mine, other_items, gridDim.x, even);
+        else {
+            ctas = prefix_share(mine, theirs, all_items, gridDim.x, even);
+            if (even && all_items > 0 && ctas >= all_items) {    // an item's units a multiple of its CTAs, so that runs begin where items do
+                const int each = ctas / (int)all_items, units = (int)(all_tiles / all_items) + item_cost;
+                item_cost += (units + each - 1) / each * each - units;
+            }
+        }
+        if ((int)blockIdx.x >= ctas) {
+            if (tid < N) { out[tid].begin = out[tid].end = 0; }
+            __syncthreads();
+            return ctas;
+        }
+    }
+    scan.units[tid] = (up_tiles - tiles) + item_cost * (up_items - items);
     scan.tiles[tid] = up_tiles - tiles;
-    const long long total = all_tiles + w.item_cost * all_items, most = (long long)gridDim.x * N;
+    const long long total = all_tiles + item_cost * all_items, most = (long long)ctas * N;
     const int workers = total < most ? (int)total : (int)most, me = blockIdx.x * N + tid;
     if (tid < N && me >= workers) { out[tid].begin = out[tid].end = 0; }
     if (tid < N && me == workers - 1) { out[tid].end = all_tiles; out[tid].tail_cta = -1; }
@@ -343,7 +401,7 @@ __device__ __forceinline__ void prefix_find_runs(const PrefixWork& w, PrefixScan
             prefix_load(w, scan, c.b, c.r);
             if (c.r.n_kt == 0) continue;
             tiles_of = c.r.n_kt - c.r.kt0;
-            cost = tiles_of + w.item_cost;
+            cost = tiles_of + item_cost;
             const long long n = (long long)w.n_kv * c.r.n_rt;
             if (rest < n * cost) break;
             rest -= n * cost;
@@ -351,7 +409,7 @@ __device__ __forceinline__ void prefix_find_runs(const PrefixWork& w, PrefixScan
             at_tile += n * tiles_of;
         }
         const long long item = tree_div(rest, cost), head = tree_div(item, c.r.n_rt);
-        const int in = max(0, (int)(rest - item * cost) - w.item_cost);
+        const int in = max(0, (int)(rest - item * cost) - item_cost);
         c.kt = c.r.kt0 + in;
         c.rt = (int)(item - head * c.r.n_rt);
         c.h = (int)head;
@@ -360,6 +418,7 @@ __device__ __forceinline__ void prefix_find_runs(const PrefixWork& w, PrefixScan
         if (tid > 0) { out[tid - 1].end = at_tile; out[tid - 1].tail_cta = in > 0 ? tree_cta_of(unit + (item + 1) * cost - 1, total, workers) : -1; }
     }
     __syncthreads();
+    return ctas;
 }
 
 // ---- partial results ------------------------------------------------------------------------------------------------
@@ -392,8 +451,8 @@ __device__ __forceinline__ void tree_start(const TreeWork& w, long long* part, T
 __device__ __forceinline__ void tree_start(const PrefixWork& w, long long*, TreeRunT<PrefixWork>* run, void* scan) {
     if (!w.late_wait) grid_dependency_wait();
     grid_dependency_release();
-    prefix_find_runs<1>(w, *static_cast<PrefixScan*>(scan), run);
-    if (blockIdx.x == gridDim.x - 1 && w.first + w.batch > w.groups) prefix_map_rows(w, *static_cast<PrefixScan*>(scan));
+    const int ctas = prefix_find_runs<1>(w, *static_cast<PrefixScan*>(scan), run);
+    if ((int)blockIdx.x == max(ctas, 1) - 1 && w.first + w.batch > w.groups) prefix_map_rows(w, *static_cast<PrefixScan*>(scan));
 }
 __device__ __forceinline__ void tree_finish(const TreeWork&) {}
 __device__ __forceinline__ void tree_finish(const PrefixWork& w) { if (w.late_wait) grid_dependency_wait(); }

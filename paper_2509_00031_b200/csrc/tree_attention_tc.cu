@@ -530,26 +530,35 @@ static int tc_kernel(const TcParamsT<W>& p, const CUtensorMap& map_k, const CUte
     return dh == 64 ? tc_launch<64, __half>(p, map_k, map_v, grid, s, dependent) : tc_launch<128, __half>(p, map_k, map_v, grid, s, dependent);
 }
 
+// Of the launch with `tile` queries a tile: keys of a key tile, units of opening and closing a part, time of a tile on an SM in 0.1 us.  The times are what they are
+// where the SM and not the memory is the bound, d_head 128: a tile of 256 queries and 128 keys 2.5 us, of up to 64 queries 1.2, of a warp's 16 keys 0.11.
+struct PrefixTile { int keys, cost, time; };
+static PrefixTile prefix_tile(int tile) {
+    if (tile <= kNarrowRows) return PrefixTile{kNarrowKeys, 3, 1};
+    return tile < kTileRows ? PrefixTile{kKeys, 8, 11} : PrefixTile{kKeys, 8, 24};
+}
+
 int launch_prefix_tc(const PrefixAttnArgs& a, const PrefixScratch& at, const int (&tile)[2], cudaStream_t s, bool dependent) {
     const int dh = a.t.cache.d_head, type = a.t.cache.type, grid = tree_grid(), parts = a.groups + a.t.batch;
     const bool one = tile[0] == tile[1];
     for (int side = 0; side < (one ? 1 : 2); ++side) {
+        const PrefixTile own = prefix_tile(tile[side]), other = prefix_tile(tile[!side]);
         TcParamsT<PrefixWork> p{};
         alignas(64) CUtensorMap map_k, map_v;
-        if (int rc = tc_params(a.t, tile[side] <= kNarrowRows ? kNarrowKeys : kKeys, p, map_k, map_v)) return rc;
+        if (int rc = tc_params(a.t, own.keys, p, map_k, map_v)) return rc;
         p.w.tile_rows = tile[side];
+        p.w.key_tile = own.keys;
+        p.w.item_cost = own.cost;
         prefix_work(a, at, side ? a.groups : 0, one ? parts : (side ? a.t.batch : a.groups), p.w);
+        if (!one) {
+            p.w.tile_time = own.time; p.w.other_time = other.time;
+            p.w.other_rows = tile[!side]; p.w.other_keys = other.keys; p.w.other_cost = other.cost;
+        }
         p.w.late_wait = side == 1;
         p.scratch = at.pieces[side];
         int rc;
-        if (tile[side] <= kNarrowRows) {
-            p.w.key_tile = kNarrowKeys;
-            // opening and closing a part in the time of two tiles of 16 keys
-            p.w.item_cost = 2;
-            rc = launch_prefix_narrow(p, map_k, map_v, dh, type, grid, s, dependent);
-        } else {
-            p.w.key_tile = kKeys;
-            p.w.item_cost = 4;
+        if (tile[side] <= kNarrowRows) rc = launch_prefix_narrow(p, map_k, map_v, dh, type, grid, s, dependent);
+        else {
             rc = tc_kernel(p, map_k, map_v, dh, type, tile[side] < kTileRows ? tile[side] : kRows, grid, s, dependent);
             count_launch();
         }

@@ -498,6 +498,7 @@ def test_prefix_attention_is_tree_attention(zq, dtype, per):
 
 @pytest.mark.parametrize("dtype,per", [("bf16", [2, 3, 2]), ("f16", [30, 40, 30]), ("f32", [2, 3, 2])])
 def test_prefix_attention_reports_contradictions_and_leaves_rows(zq, dtype, per):
+    from test_gpu_serve import attention_oracle
     n = sum(per)
     pr = prefix_problem(4, dtype, 4, 2, 64, 16, "token", [300, 200, 150], per, [3] * n, [1] * n, None)
     good = run_prefix(zq, pr)
@@ -511,7 +512,10 @@ def test_prefix_attention_reports_contradictions_and_leaves_rows(zq, dtype, per)
         t = t.clone()
         t[i] = x
         return t
-    same = lambda out, rows: torch.equal(out[rows], good[rows])  # noqa: E731
+    # (where the parts of a request are cut depends on all requests' lengths, so the others' outputs are held to the definition, not to the bits of another batch)
+    want, bound = attention_oracle(pr)
+    same = lambda out, rows: bool(((out[: pr["rows"]].double() - want).abs() <= bound)[rows].all())  # noqa: E731
+    assert same(good, slice(0, n))
     first, last = slice(0, g1), slice(g2, n)
     for bad in (changed(pr["prefix_len"], 1, -1), changed(pr["prefix_len"], 1, 10 ** 6), changed(pr["prefix_len"], 1, 204)):      # group 1: more than its requests hold
         out, err = call(prefix_len=bad)
