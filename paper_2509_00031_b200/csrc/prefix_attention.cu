@@ -118,6 +118,8 @@ prefix_join_kernel(const __grid_constant__ JoinParams p) {
 template <typename T, int DH>
 int join(const JoinParams& p, cudaStream_t s) {
     const int heads = p.w.n_kv * p.w.group;
+    // Eight warps a query while the queries are fewer than the warps that fit on the SMs: 512 / 1024 / 1536 / 2048 / 4096 queries and heads of one group behind
+    // 16000 keys 46 / 47 / 53 / 56 / 78 us against 52 / 50 / 56 / 56 / 75 with one, behind 2000 25 / 28 / 32 / 37 / 49 against 29 / 29 / 31 / 35 / 44.
     const bool wide = (int64_t)p.w.rows * heads <= 148 * 8;
     const cudaError_t rc = wide ? launch_kernel(prefix_join_kernel<T, DH, true>, dim3(p.w.rows, heads), dim3(256), 0, s, true, p)
                                 : launch_kernel(prefix_join_kernel<T, DH, false>, dim3(p.w.rows, (heads + 7) / 8), dim3(256), 0, s, true, p);
@@ -133,7 +135,7 @@ PrefixScratch prefix_scratch(void* base, int type, int d_head, int64_t rows, int
     uint8_t* p = static_cast<uint8_t*>(base);
     size_t used = 0;
     auto take = [&](size_t bytes) { const size_t o = used; used += (bytes + 255) / 256 * 256; return p ? p + o : nullptr; };
-    // two slots to a worker: 148 of 256 queries, or their warps of up to 16
+    // two slots to a worker: 148 of 256 queries, or their warps of up to 8
     const size_t f32 = kTailBytes + 2 * (size_t)(kMaxTreeGrid / 2 * kF32Warps) * tree_slot_floats(kF32Rows, d_head) * 4;
     const size_t narrow = kTailBytes + 2 * (size_t)kMaxWorkers * tree_slot_floats(kNarrowRows, d_head) * 4, wide = tree_attention_scratch_bytes(type, d_head);
     const size_t pieces = type == kTypeF32 ? f32 : (narrow > wide ? narrow : wide);
@@ -162,10 +164,15 @@ int launch_prefix_attention(const PrefixAttnArgs& a, void* scratch, cudaStream_t
         if (int rc = launch_prefix_f32(a, at, s, dependent)) return rc;
         return t.cache.d_head == 64 ? join<float, 64>(p, s) : join<float, 128>(p, s);
     }
-    // Queries per tile from averages (the host does not know the lengths).
+    // Queries per tile from averages (the host does not know the lengths; rows behind the last request count too, hence borders a little above the tiles).  us at tiles of
+    // 8 / 32 / 64 / 256, 8 key heads of 128, bf16.  8 groups behind 8000 keys, own keys few: 4 queries 55 / 79 / 78 / 108; 8: 58 / 77 / 77 / 98; 16: 68 / 78 / 79 / 100; 32: 173 / 75 /
+    // 76 / 100; 64: 245 / 106 / 83 / 98; 128: 441 / 176 / 125 / 108.  64 requests with 700 own keys: 8 queries 80 / 109 / 100 / 169; 16: 84 / 102 / 104 / 121; 24: 125 / 123 / 126 / 137;
+    // 32: 141 / 129 / 132 / 148; 64: 219 / 261 / 242 / 181 (short parts: what it costs to open a tile counts, hence the margin of a half).
     const long long queries = (long long)t.rows * group;
-    const long long want[2] = {(queries + a.groups - 1) / a.groups, t.rows <= t.batch ? group : (3 * queries + 2 * t.batch - 1) / (2 * t.batch)};     // (1.5 x the average)
-    for (int side = 0; side < 2; ++side) p.tile_rows[side] = want[side] <= 8 ? 8 : want[side] <= 16 ? 16 : (want[side] <= 32 ? 32 : (want[side] <= 64 ? 64 : 256));
+    const long long shared = (queries + a.groups - 1) / a.groups, own = (queries + t.batch - 1) / t.batch;
+    auto tile = [](long long want) { return want <= 32 ? 32 : (want <= 64 ? 64 : 256); };
+    p.tile_rows[0] = shared <= 18 ? kNarrowRows : tile(shared - shared / 8);
+    p.tile_rows[1] = own <= 18 ? kNarrowRows : tile(own + own / 2);
     if (p.tile_rows[0] != p.tile_rows[1]) p.pieces[1] = at.pieces[1];
     for (int side = 0; side < 2; ++side) p.workers[side] = p.tile_rows[side] <= kNarrowRows ? p.workers[side] * kNarrowWarps : p.workers[side];
     if (int rc = launch_prefix_tc(a, at, p.tile_rows, s, dependent)) return rc;

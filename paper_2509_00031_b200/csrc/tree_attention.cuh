@@ -17,7 +17,7 @@
 namespace zq {
 
 constexpr int kKeys = 128;                               // keys of a key tile: the tensor-core kernels'
-constexpr int kNarrowKeys = 16, kNarrowRows = 16, kNarrowWarps = 12;      // the warps' kernel (prefix_narrow.cu): a run per warp
+constexpr int kNarrowKeys = 32, kNarrowRows = 8, kNarrowWarps = 12;      // the warps' kernel (prefix_narrow.cu): a run per warp
 constexpr int kF32Rows = 8, kF32Border = 32, kF32Warps = 10;             // its fp32 sibling (prefix_narrow_f32.cu); the border between parts
 
 // A request's part of the work: n rows from row0 on, keys up to L, in n_rt row tiles and the key tiles [first_tile(), n_kt); n_rt * n_kt = 0: nothing to do.
@@ -331,7 +331,7 @@ __device__ __forceinline__ int prefix_find_runs(const PrefixWork& w, PrefixScan&
         o.tile_rows = w.other_rows; o.key_tile = w.other_keys;
         o.first = w.first ? 0 : w.groups;
         const int parts = w.first ? w.groups : w.requests;
-        for (int b = tid; b < parts; b += blockDim.x) {
+        for (int b = blockDim.x - 1 - tid; b < parts; b += blockDim.x) {                 // (other warps than those that read this launch's few parts)
             const PrefixRequest r = tree_request(o, b);
             const long long n = r.n_kt ? (long long)w.n_kv * r.n_rt : 0;
             other_items += n;

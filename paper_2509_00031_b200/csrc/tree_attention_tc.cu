@@ -534,8 +534,8 @@ static int tc_kernel(const TcParamsT<W>& p, const CUtensorMap& map_k, const CUte
 // where the SM and not the memory is the bound, d_head 128: a tile of 256 queries and 128 keys 2.5 us, of up to 64 queries 1.2, of a warp's 16 keys 0.11.
 struct PrefixTile { int keys, cost, time; };
 static PrefixTile prefix_tile(int tile) {
-    if (tile <= kNarrowRows) return PrefixTile{kNarrowKeys, 3, 1};
-    return tile < kTileRows ? PrefixTile{kKeys, 8, 11} : PrefixTile{kKeys, 8, 24};
+    if (tile <= kNarrowRows) return PrefixTile{kNarrowKeys, 2, 2};
+    return tile < kTileRows ? PrefixTile{kKeys, 8, 11} : PrefixTile{kKeys, 8, 25};
 }
 
 int launch_prefix_tc(const PrefixAttnArgs& a, const PrefixScratch& at, const int (&tile)[2], cudaStream_t s, bool dependent) {
