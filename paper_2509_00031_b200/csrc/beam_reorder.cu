@@ -19,7 +19,7 @@
 namespace zq {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kFew = 4;      // requests that one launch serves
 
 struct ReorderParams {
     ReorderArgs a;
@@ -91,15 +91,20 @@ __device__ __forceinline__ unsigned pages_gone(const ReorderArgs& a, const Reque
     return gone;
 }
 
-// Sum over the block (called by all threads; ends with a barrier).
-__device__ __forceinline__ int block_sum(int x, int* part) {
-    x = __reduce_add_sync(0xffffffffu, x);
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
+// Sums over the block (called by all threads; part: N words a warp; ends with a barrier).
+template <int N>
+__device__ __forceinline__ void block_sums(int (&x)[N], int* part) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] = __reduce_add_sync(0xffffffffu, x[i]);
+        if ((threadIdx.x & 31) == 0) part[(threadIdx.x >> 5) * N + i] = x[i];
+        x[i] = 0;
+    }
     __syncthreads();
-    int sum = 0;
-    for (int w = 0; w < kThreads / 32; ++w) sum += part[w];
+    for (int w = 0; w < kThreads / 32; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] += part[w * N + i];
     __syncthreads();
-    return sum;
 }
 
 // Tables and histories, row by row: rows first, first + step, ... of a request.
@@ -140,12 +145,12 @@ beam_count_kernel(const ReorderParams p) {
     grid_dependency_release();                                   // the second launch may get ready
     read_request(a, b, r);
     if (blockIdx.y == 0) {
-        int most = 0, n = 0;
+        int most = 0, n[1] = {0};
         for (int k = 0; k < K; ++k) most = max(most, r.held[k]);
-        for (int c = tid; c < most; c += kThreads) n += __popc(pages_gone(a, r, row0, c));
-        n = block_sum(n, part);
+        for (int c = tid; c < most; c += kThreads) n[0] += __popc(pages_gone(a, r, row0, c));
+        block_sums(n, part);
         if (tid == 0) {
-            p.counts[2 * b] = n;
+            p.counts[2 * b] = n[0];
             p.counts[2 * b + 1] = __popc(r.copies);
             if (r.status) atomicOr(a.status, r.status);
         }
@@ -154,19 +159,19 @@ beam_count_kernel(const ReorderParams p) {
     move_rows(a, r, row0, blockIdx.y - 1, gridDim.y - 1);
 }
 
-// Gives the request's new rows their pages and lists those it gives back; counts: [batch][2].
-__device__ __forceinline__ void place_pages(const ReorderArgs& a, const Request& r, int b, const int32_t* counts, int n_free, int* part, int* mine) {
+// Gives the request's new rows their pages and lists those it gives back; counts: [batch][2], first: rows that give back a page in column threadIdx.x, part: 4 words a warp.
+__device__ __forceinline__ void place_pages(const ReorderArgs& a, const Request& r, int b, const int32_t* counts, int n_free, unsigned first, int* part, int* mine) {
     const int K = a.beams, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t row0 = (int64_t)b * K;
-    int taken = 0, given = 0, taken_before = 0, given_before = 0, most = 0;
+    int sums[4] = {0, 0, 0, 0}, most = 0;                        // pages taken from the free ones and given to them, by all requests and by those before this one
     for (int i = tid; i < a.batch; i += kThreads) {
         const int gone = counts[2 * i], want = counts[2 * i + 1], inside = min(gone, want);
-        taken += want - inside;
-        given += gone - inside;
-        if (i < b) { taken_before += want - inside; given_before += gone - inside; }
+        sums[0] += want - inside;
+        sums[1] += gone - inside;
+        if (i < b) { sums[2] += want - inside; sums[3] += gone - inside; }
     }
-    taken = block_sum(taken, part); given = block_sum(given, part);
-    taken_before = block_sum(taken_before, part); given_before = block_sum(given_before, part);
+    block_sums(sums, part);
+    const int taken = sums[0], given = sums[1], taken_before = sums[2], given_before = sums[3];
     const int own_gone = counts[2 * b], own_want = counts[2 * b + 1], inside = min(own_gone, own_want);
     // nothing is reordered where lengths are impossible or pages are short
     int bad = n_free < 0 || n_free > a.free_capacity ? kPlanBadLength : 0;
@@ -184,7 +189,7 @@ __device__ __forceinline__ void place_pages(const ReorderArgs& a, const Request&
     int done = 0;
     for (int c0 = 0; c0 < most && own_gone > 0 && !bad; c0 += kThreads) {
         const int c = c0 + tid;
-        const unsigned gone = c < most ? pages_gone(a, r, row0, c) : 0u;
+        const unsigned gone = c0 == 0 ? first : (c < most ? pages_gone(a, r, row0, c) : 0u);
         int n = __popc(gone), up = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -231,20 +236,27 @@ __device__ __forceinline__ void place_pages(const ReorderArgs& a, const Request&
 __global__ void __launch_bounds__(kThreads)
 beam_place_kernel(const ReorderParams p) {
     __shared__ Request r;
-    __shared__ int part[kThreads / 32];
+    __shared__ int part[4 * kThreads / 32];
     __shared__ int mine[kMaxBeams];                              // pages that the request's own new rows take over
-    read_request(p.a, blockIdx.x, r);                            // (inputs only: may run ahead of the counts)
-    const int n_free = __ldg(p.a.n_free);
+    const ReorderArgs& a = p.a;
+    read_request(a, blockIdx.x, r);                              // (inputs only: may run ahead of the counts)
+    const int n_free = __ldg(a.n_free);
+    bool held = false;
+    for (int k = 0; k < a.beams; ++k) held = held || (int)threadIdx.x < r.held[k];
+    const unsigned first = held ? pages_gone(a, r, (int64_t)blockIdx.x * a.beams, threadIdx.x) : 0u;
     grid_dependency_wait();
-    place_pages(p.a, r, blockIdx.x, p.counts, n_free, part, mine);
+    place_pages(a, r, blockIdx.x, p.counts, n_free, first, part, mine);
 }
 
-// Few requests: every CTA counts for all of them itself, its warps shared out, so one launch does it.
+// Few requests: every CTA counts for all of them itself, its warps shared out, so one launch does it.  1 / 4 / 8 requests of four beams with up to 2000 tokens, with the copies of
+// 24 layers: called from Python 21.9 / 21.8 / 21.9 us against 24.6 / 24.4 / 24.3 with two launches, replayed from a graph, where a launch costs the host nothing, 8.3 / 13.5 / 15.5
+// against 9.2 / 12.4 / 13.3: two warps a request are enough, one is not.
 __global__ void __launch_bounds__(kThreads)
 beam_reorder_kernel(const ReorderParams p) {
-    __shared__ Request all[kThreads / 32];
-    __shared__ int32_t counts[2 * (kThreads / 32)];
-    __shared__ int part[kThreads / 32];
+    __shared__ Request all[kFew];
+    __shared__ int32_t counts[2 * kFew];
+    __shared__ int part[4 * kThreads / 32];
+    __shared__ unsigned gone_s[kThreads];                        // of this CTA's request, by column
     __shared__ int mine[kMaxBeams];
     const ReorderArgs& a = p.a;
     const int b = blockIdx.x, K = a.beams, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -255,6 +267,7 @@ beam_reorder_kernel(const ReorderParams p) {
     }
     const int n_free = __ldg(a.n_free);
     if (tid < 2 * a.batch) counts[tid] = 0;
+    gone_s[tid] = 0;
     if (warp < a.batch) read_request_warp(a, warp, all[warp]);
     __syncthreads();
     const int share = kThreads / 32 / a.batch, of = warp / share;          // warps of a request
@@ -262,7 +275,11 @@ beam_reorder_kernel(const ReorderParams p) {
         const Request& r = all[of];
         int most = 0, n = 0;
         for (int k = 0; k < K; ++k) most = max(most, r.held[k]);
-        for (int c = (warp - of * share) * 32 + lane; c < most; c += 32 * share) n += __popc(pages_gone(a, r, (int64_t)of * K, c));
+        for (int c = (warp - of * share) * 32 + lane; c < most; c += 32 * share) {
+            const unsigned gone = pages_gone(a, r, (int64_t)of * K, c);
+            if (of == b) gone_s[c] = gone;
+            n += __popc(gone);
+        }
         n = __reduce_add_sync(0xffffffffu, n);
         if (lane == 0) {
             atomicAdd(counts + 2 * of, n);
@@ -271,7 +288,7 @@ beam_reorder_kernel(const ReorderParams p) {
         }
     }
     __syncthreads();
-    place_pages(a, all[b], b, counts, n_free, part, mine);
+    place_pages(a, all[b], b, counts, n_free, gone_s[tid], part, mine);
 }
 
 // ---- copies ---------------------------------------------------------------------------------------------------------
@@ -324,7 +341,7 @@ int launch_beam_reorder(const ReorderArgs& a, void* scratch, cudaStream_t s) {
     ReorderParams p{a, static_cast<int32_t*>(scratch)};
     const int y = 1 + (a.beams < 148 * 4 / a.batch ? a.beams : (a.beams + 3) / 4);
     // one launch while a request's warps get through its columns in a few rounds (the second launch costs the host 2 us and the device 4)
-    if (a.batch <= kThreads / 32 && a.max_pages <= 256) {
+    if (a.batch <= kFew && a.max_pages <= kThreads) {
         if (launch_kernel(beam_reorder_kernel, dim3(a.batch, y), dim3(kThreads), 0, s, false, p) != cudaSuccess) return -1;
         count_launch();
         return 0;
