@@ -12,6 +12,9 @@
 // passes that is rare, so the stream costs a maximum, an exponential and two additions each, sixteen bytes at a time, the next on their way while some are
 // worked on.  Keys are (logit, token) in 64 bits: no two are equal, and of equal logits the lower token wins.  Should the buffer ever run over (long runs
 // of rising or equal logits), the row's bound is found digit by digit from histograms instead.
+// 64 x 8 beams of 50272 logits: fp32 30 us, 16 of them the 103 MB at the rate of a copy, bf16 27; 96 x 3 of 128256 bf16 with nine tenths masked 33 (11); 4 of 32000 fp32 12.5.  The stream
+// itself runs at 7 TB/s (16-bit logits: bound by the exponentials); 5.5 us go before it (start, first bound, sorting) and 7 behind it (sorting, sums, the cluster, logarithms in 64
+// bits, ranking), in short dependent steps that all CTAs go through at the same time.
 // Sums: every thread has its own reference (the largest logit it met when it last moved), partial sums are fp32, the row's logarithm and all scores are formed in
 // 64 bits, so that scores of different beams are compared before anything is rounded.  Scores are rounded to fp32 once.
 #include "common.cuh"
@@ -61,7 +64,8 @@ __device__ __forceinline__ u64 ld_cluster_u64(uint32_t addr) {
 template <typename T> __device__ __forceinline__ float value(T v) { return static_cast<float>(v); }
 // VEC logits at a time: 16 bytes where the rows allow it, else single ones
 template <typename T, int VEC> struct alignas(VEC * sizeof(T)) Vec { T v[VEC]; };
-template <typename T, int THREADS> constexpr int kResident = THREADS == 512 ? 2 : (sizeof(T) == 4 ? 4 : 3);      // CTAs of an SM (registers: 16-bit logits take more)
+// CTAs of an SM (64 x 8 rows of 50272 bf16: with three CTAs, which spares the compiler a few words of stack, half of the rows wait for the others, 31.0 us against 26.9)
+template <int THREADS> constexpr int kResident = THREADS == 512 ? 2 : 4;
 // the largest; NaN does not count
 template <typename T, int VEC> __device__ __forceinline__ float largest(const Vec<T, VEC>& x) {
     if constexpr (VEC == 1) return value(x.v[0]);
@@ -128,6 +132,40 @@ __device__ __forceinline__ void sort_best(const u64* buf, int m, u64* to, int n)
     __syncthreads();
 }
 
+// The logits of a thread's vectors that are above the limit (EQUAL: or at it) go to the buffer; x[0] begins with `token`, x[1] stride further on.  Rare, so it is short: the vector
+// is picked out first, whichever it is (comparisons and pushes of every element of every vector: the same logits 45.7 us in place of 31.0, most of it the code's own way
+// through the instruction caches).
+template <bool EQUAL, typename T, int VEC, int N>
+__device__ __forceinline__ void push(Shared& sh, const Vec<T, VEC> (&x)[N], float limit, int token, int stride) {
+    unsigned hit = 0;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        const float v = largest(x[u]);
+        hit |= (EQUAL ? v >= limit : v > limit) ? 1u << u : 0u;
+    }
+#pragma unroll 1
+    for (; hit; hit &= hit - 1) {
+        const int u = __ffs(hit) - 1;
+        Vec<T, VEC> y = x[0];
+#pragma unroll
+        for (int k = 1; k < N; ++k)
+            if (u == k) y = x[k];
+        unsigned which = 0;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const float v = value(y.v[e]);
+            which |= (EQUAL ? v >= limit : v > limit) ? 1u << e : 0u;
+        }
+        int at = atomicAdd(&sh.count, __popc(which));
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            if (!((which >> e) & 1u)) continue;
+            if (at < kBuffer) sh.buf[at] = key_of(value(y.v[e]), token + u * stride + e);
+            ++at;
+        }
+    }
+}
+
 // Asks for the 64 KB behind a row's first two rounds, so that the memory is busy while the bound is found.
 template <typename T, int VEC>
 __device__ __forceinline__ void prefetch_row(const T* src, int size, int from) {
@@ -138,7 +176,7 @@ __device__ __forceinline__ void prefetch_row(const T* src, int size, int from) {
 }
 
 template <typename T, int VEC, int kThreads>
-__global__ void __launch_bounds__(kThreads, kResident<T, kThreads>)
+__global__ void __launch_bounds__(kThreads, kResident<kThreads>)
 beam_select_kernel(const __grid_constant__ Params p) {
     constexpr int kWarps = kThreads / 32, kFly = VEC == 1 ? 8 : 4, kRound = kFly * kThreads;       // vectors of a thread in flight, vectors of a round
     __shared__ Shared sh;
@@ -166,10 +204,6 @@ beam_select_kernel(const __grid_constant__ Params p) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) x[u].v[e] = i * VEC + e < size ? src[i * VEC + e] : T(-INFINITY);
         }
-    };
-    auto push = [&](u64 key) {
-        const int at = atomicAdd(&sh.count, 1);
-        if (at < kBuffer) sh.buf[at] = key;
     };
     V now[kFly], ahead[kFly];
     int mine = 0;                                                // rows of this CTA so far
@@ -210,16 +244,9 @@ beam_select_kernel(const __grid_constant__ Params p) {
         if (!(limit > -INFINITY)) limit = -FLT_MAX;              // everything but -inf
         float ref2 = __fmul_rn(ref, kLog2e);
         float2 sum = make_float2(0.0f, 0.0f);
+        push<true>(sh, now, limit, lo + tid * VEC, kThreads * VEC);
 #pragma unroll
-        for (int u = 0; u < kFly; ++u) {
-            if (largest(now[u]) >= limit) {
-                const int token = lo + (u * kThreads + tid) * VEC;
-#pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if (value(now[u].v[e]) >= limit) push(key_of(value(now[u].v[e]), token + e));
-            }
-            add_powers(now[u], ref2, sum);
-        }
+        for (int u = 0; u < kFly; ++u) add_powers(now[u], ref2, sum);
         __syncthreads();
         // the rest: what passes the n-th best so far (a later token loses against an equal logit)
         if (n_vec > kRound && sh.count <= kBuffer) {
@@ -238,14 +265,7 @@ beam_select_kernel(const __grid_constant__ Params p) {
 #pragma unroll
                 for (int u = 1; u < kFly; ++u) m4 = fmaxf(m4, largest(x[u]));
                 if (m4 > limit) {
-                    const int token = lo + (base + tid) * VEC;
-#pragma unroll
-                    for (int u = 0; u < kFly; ++u) {
-                        if (!(largest(x[u]) > limit)) continue;
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e)
-                            if (value(x[u].v[e]) > limit) push(key_of(value(x[u].v[e]), token + u * kThreads * VEC + e));
-                    }
+                    push<false>(sh, x, limit, lo + (base + tid) * VEC, kThreads * VEC);
                     if (m4 > ref) {                              // the reference moves (no logit above it has been met: limit <= reference)
                         ref = fminf(m4, FLT_MAX);
                         const float to = __fmul_rn(ref, kLog2e), f = ex2(ref2 - to);
@@ -450,7 +470,7 @@ int launch_vec(const BeamSelectArgs& a, cudaStream_t s) {
     // Whole rows in parallel, as many as keep all CTAs resident (with more, clusters wait for one another); slices only while the SMs have
     // less than two CTAs, and of two thousand tokens at least.
     int rounds = (a.beams + kCluster - 1) / kCluster;
-    for (p.in_parallel = (a.beams + rounds - 1) / rounds; p.in_parallel > 1 && (int64_t)a.batch * p.in_parallel > 148 * kResident<T, 256>; p.in_parallel = (a.beams + rounds - 1) / rounds) ++rounds;
+    for (p.in_parallel = (a.beams + rounds - 1) / rounds; p.in_parallel > 1 && (int64_t)a.batch * p.in_parallel > 148 * kResident<256>; p.in_parallel = (a.beams + rounds - 1) / rounds) ++rounds;
     p.slices = 1;
     while ((p.slices + 1) * p.in_parallel <= kCluster && (int64_t)a.batch * p.in_parallel * (p.slices + 1) <= 148 * 2 && a.vocab >= 2048 * (p.slices + 1)) ++p.slices;
     p.slice = ((a.vocab + p.slices - 1) / p.slices + VEC - 1) / VEC * VEC;

@@ -14,10 +14,10 @@
 //                    keys are put together by byte permutations, and the rows g, g + 8 of m-tile t are the columns 8 p(g) + t of the halves
 // The running maximum is exact for every tile; outputs are brought to a new one only when it moved.  Weights are rounded to the cache's type for the second product,
 // sums are of the unrounded ones, in fp32.  Waits are bounded and report through *err_flag.
-// 64 requests of 4 queries a head, 8 key heads of 128, 700 own keys behind 2000 shared by eight: 67 us, 37 of them the caches' 247 MB at the rate of a copy.  Bound by memory on all
-// SMs (6.8 TB/s); an SM alone takes in 76 GB/s, which is what 12 tiles' requests in flight give.  Tiles of 16 keys in the same memory issue a third more instructions a key
-// and keep two maxima, two sets of shuffles in a row (that call: 70 us; 64 requests of 8 to 300 keys behind 128 others' long ones: 4 % slower).  Tiles of 16
-// queries for parts with more than eight: never the fastest (8 groups of 16 queries behind 8000 keys 90 us; two tiles of eight, the second from L2, 68; keys as rows 78).
+// 64 requests of 4 queries a head, 8 key heads of 128, 700 own keys behind 2000 shared by eight: 67 us, 38 of them the caches' 249 MB at the rate of a copy.  Bound by memory on all
+// SMs (6.8 TB/s); an SM alone takes in 76 GB/s.  Tiles of 16 keys in the same memory issue a third more instructions a key and go through two maxima and sets of shuffles one
+// after the other (that call 69 us, 128 requests behind 16001 keys with 1 to 1500 own 111 against 105).  Tiles of 16
+// queries for parts with more than eight were never the fastest: 8 groups of 16 queries behind 8000 keys 90 us; two tiles of eight, the second from L2, 68; keys as rows 78.
 #include "tree_attention_tc.cuh"
 #include "../../include/zoqat.h"
 

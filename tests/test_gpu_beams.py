@@ -191,6 +191,20 @@ def test_select_rows_apart_and_unaligned(zq):
         check_select(zq, store[:, off: off + 4990], torch.zeros((2, 3), device="cuda"), (17,))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V,ld,off,B,K", [(1, 1, 0, 3, 2), (2, 9, 5, 2, 3), (7, 7, 0, 9, 1), (9, 11, 1, 5, 2), (255, 259, 2, 3, 4), (4095, 4097, 3, 2, 8), (20001, 20003, 7, 1, 3), (50257, 50257, 0, 4, 5),
+                                          (100003, 100003, 1, 1, 16), (9000, 9001, 1, 200, 2)])
+def test_select_rows_that_begin_anywhere(zq, dtype, V, ld, off, B, K):
+    """What stands around a row (large numbers, infinities, NaN) is not the row's."""
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    store = torch.empty(B * K * ld + off + 16, device="cuda", dtype=DTYPES[dtype])
+    store[0::3], store[1::3], store[2::3] = 3e4, float("inf"), float("nan")
+    logits = store[off: off + B * K * ld].view(B * K, ld)[:, :V]
+    logits.copy_(torch.randn((B * K, V), generator=gen, device="cuda"))
+    logits[0, 0], logits[B * K - 1, V - 1] = 9.0, 9.0              # the best at the ends
+    check_select(zq, logits, torch.randn((B, K), generator=gen, device="cuda"), (V - 1,))
+
+
 def test_select_hard_rows(zq):
     """Equal, rising, falling, masked and non-finite logits; large ones; rows whose mask leaves nothing."""
     V = 40000
