@@ -481,6 +481,13 @@ PREFIX = [
     ("f32", 6, 2, 64, 24, "token", [200, 95, 96], [3, 1, 6], [i for i in range(10)], [1] * 10, None),
     ("bf16", 20, 1, 64, 8, "token", [640, 260], [3, 4], [5, 0, 7, 130, 0, 64, 1], [33, 2, 40, 1, 0, 5, 17], "random"),          # wide own parts too
     ("f16", 8, 2, 128, 256, "head", [1023, 1024, 1025], [5, 5, 5], [0, 0, 1, 255, 256] * 3, [1] * 15, None),
+    # groups and requests in kernels of their own, which share the SMs out
+    ("bf16", 8, 2, 128, 16, "token", [100], [40], [i for i in range(40)], [1] * 40, None),                                      # nothing for the groups' kernel
+    ("f16", 60, 60, 64, 16, "token", [400], [700], [i % 50 for i in range(700)], [1] * 700, None),                              # a group with more items than CTAs
+    ("bf16", 8, 2, 64, 32, "head", [128 + i for i in range(70)], [6] * 70, [i % 40 for i in range(420)], [1] * 420, None),      # more parts than a CTA keeps
+    ("f16", 20, 1, 128, 16, "token", [700, 300], [1, 1], [5, 200], [3, 3], "tree"),                                             # wide tiles for requests, narrower for groups
+    ("bf16", 8, 8, 128, 8, "token", [5000], [150], [0] * 150, [1] * 150, None),                                                 # next to nothing of their own
+    ("f16", 4, 2, 64, 8, "head", [1, 260], [2, 3], [0, 30, 31, 32, 33], [1, 2, 1, 3, 2], "random"),                             # four boxes a tile
 ]
 
 
