@@ -262,7 +262,7 @@ __device__ __forceinline__ int64_t tree_value_offset(const TcParamsT<W>& p, cons
 }
 
 // few queries per key head: keys are the rows of the products (tree_attention_keys.cu); nq: queries per tile (16, 32, 64)
-// up to 16 queries per tile of a part: a run per warp (prefix_narrow.cu)
+// up to 8 queries per tile of a part: a run per warp (prefix_narrow.cu)
 int launch_prefix_narrow(const TcParamsT<PrefixWork>& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int dh, int type, int grid, cudaStream_t s, bool dependent);
 
 template <class W> int launch_tree_keys(const TcParamsT<W>& p, const CUtensorMap& map_k, const CUtensorMap& map_v, int dh, int type, int nq, int grid, cudaStream_t s, bool dependent);
