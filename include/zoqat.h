@@ -797,11 +797,12 @@ int zoqat_op_rotary_append(const void* qkv_dev, int qkv_type, int64_t ld, const 
                            float norm_eps, const zoqat_paged_cache_t* cache, void* q_out_dev, int64_t q_stride, int32_t* err_flag_dev, void* stream);
 
 /* zoqat_op_tree_attention for requests that share a long prefix: requests group_start_dev[g] .. group_start_dev[g + 1] - 1 ([groups + 1]) form
- * group g, and the first prefix_len_dev[g] keys of each of them ([groups]) are the same - their rows of block_table name the same pages, or
- * pages that hold the same; request_group_dev [batch] names each request's group.  All keys of the prefix are seen by all rows (prefix_len <= kv_len - rows
+ * group g, and the first prefix_len_dev[g] keys of each of them that has rows ([groups]) are the same - their rows of block_table name the same pages, or
+ * pages that hold the same; request_group_dev [batch] names each request's group.  Requests without rows keep their place: their lengths and rows of block_table
+ * may hold anything.  All keys of the prefix are seen by all rows (prefix_len <= kv_len - rows
  * of the request).  The result is that of zoqat_op_tree_attention up to rounding, the prefix is read once for the whole group (through the table of its first
- * request, in whole tiles of 128 keys, fp32 32; what is left of it through each request's own).  Everything else as there, the limits of page sizes
- * and strides among it.  *err_flag_dev is also set to 41 where groups and requests contradict each other: the group or request is left out.  scratch_dev:
+ * request that has rows and holds it, in whole tiles of 128 keys, fp32 32; what is left of it through each request's own).  Everything else as there, the limits
+ * of page sizes and strides among it.  *err_flag_dev is also set to 41 where groups and requests contradict each other: the group or request is left out.  scratch_dev:
  * zoqat_op_prefix_attention_scratch_bytes() bytes for this many rows or fewer, 256-byte aligned, for one call at a time. */
 int zoqat_op_prefix_attention_scratch_bytes(int type, int d_head, int rows, int n_heads, size_t* bytes);
 int zoqat_op_prefix_attention(const void* q_dev, int64_t q_stride, const zoqat_paged_cache_t* cache, const int32_t* block_table_dev, int max_pages,

@@ -87,7 +87,27 @@ struct PrefixWork : TreeWork {               // batch: parts in this launch
 __device__ __forceinline__ int prefix_down(int a, int b) { return a >> (31 - __clz(b)); }
 __device__ __forceinline__ int prefix_up(int a, int b) { return (int)(((unsigned)a + (unsigned)b - 1u) >> (31 - __clz(b))); }
 
-// The shared part of group g; n_kt = 0: it has none, or (ok = false) its description contradicts itself.
+// A prefix is read through the table of the group's first request that has rows and holds its shared keys.  (The row of a request without rows says nothing: it may have ended, and
+// its pages be others' by now.)  Where no request holds them, each contradicts the group, and no row takes what comes of the shared part: any row of the table will do.
+// Not inlined: the attention kernels meet parts in many places, and all of this in each of them costs 4 us of 70 (8 groups of 32 queries a key head behind 8000 keys).
+static __device__ __noinline__ int prefix_row(const int32_t* group_start, const int32_t* prefix_len, const int32_t* request_group, const int32_t* row_start, const int32_t* kv_len,
+                                              int rows, long long most, int g) {
+    const int b0 = __ldg(group_start + g), b1 = __ldg(group_start + g + 1), len = __ldg(prefix_len + g);
+    for (int b = b0; b < b1; ++b) {
+        const int at = __ldg(row_start + b), n = __ldg(row_start + b + 1) - at, have = __ldg(kv_len + b), of = __ldg(request_group + b);
+        if (n > 0 && at >= 0 && at <= rows - n && of == g && have <= most && len <= (long long)have - n) return b;
+        if (n != 0) continue;
+        int lo = b, hi = b1;                 // a run of requests without rows: lo is the last one known of, or b1 - 1
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (__ldg(row_start + mid + 1) == at) lo = mid;
+            else hi = mid;
+        }
+        b = lo;
+    }
+    return b0;
+}
+// The shared part of group g, its table not looked for; n_kt = 0: it has none, or (ok = false) its description contradicts itself.
 __device__ __forceinline__ PrefixRequest prefix_shared(const PrefixWork& w, int g, bool& ok) {
     PrefixRequest r{};
     const int b0 = __ldg(w.group_start + g), b1 = __ldg(w.group_start + g + 1), len = __ldg(w.prefix_len + g);
@@ -97,7 +117,7 @@ __device__ __forceinline__ PrefixRequest prefix_shared(const PrefixWork& w, int 
     if (n == 0) return r;                    // (a group without rows may have any length)
     ok = lo >= 0 && n > 0 && lo <= w.rows - n && len >= 0 && len <= (long long)w.max_pages * w.page_size;
     if (!ok) return r;
-    r.row0 = lo; r.n = n; r.row = b0;
+    r.row0 = lo; r.n = n;
     r.L = prefix_down(len, w.border) * w.border;
     r.n_rt = prefix_up(n * w.group, w.tile_rows);
     r.n_kt = prefix_down(r.L, w.key_tile);
@@ -127,6 +147,10 @@ __device__ __forceinline__ PrefixRequest tree_request(const PrefixWork& w, int p
     const PrefixRequest r = part < w.groups ? prefix_shared(w, part, ok) : prefix_own(w, part - w.groups, ok);
     if (!ok) atomicExch(w.err_flag, kErrBadRequest);
     return r;
+}
+__device__ __forceinline__ void prefix_find_row(const PrefixWork& w, int part, PrefixRequest& r) {
+    if (r.own || r.n_kt == 0) return;
+    r.row = prefix_row(w.group_start, w.prefix_len, w.request_group, w.row_start, w.kv_len, w.rows, (long long)w.max_pages * w.page_size, w.first + part);
 }
 // Where the query's piece is: whole in `partial` (y = -1), or query y of the pieces of the CTAs x & 0xFFFF .. x >> 16.
 __device__ __forceinline__ int64_t prefix_query(const PrefixWork& w, const PrefixRequest& r, int query, int h) {
@@ -164,6 +188,13 @@ template <class W> struct TreeCursorT {
     }
 };
 using TreeCursor = TreeCursorT<TreeWork>;
+// next() for whoever looks pages up
+__device__ __forceinline__ void tree_next(const TreeWork& w, TreeCursor& c) { c.next(w); }
+__device__ __forceinline__ void tree_next(const PrefixWork& w, TreeCursorT<PrefixWork>& c) {
+    const int b = c.b;
+    c.next(w);
+    if (c.b != b) prefix_find_row(w, c.b, c.r);
+}
 
 // a / b for a >= 0, b > 0; almost always in 32 bits, which is several times faster
 __device__ __forceinline__ long long tree_div(long long a, long long b) {
@@ -278,7 +309,7 @@ struct PrefixScan {
 };
 __device__ __forceinline__ void prefix_load(const PrefixWork& w, const PrefixScan& scan, int b, PrefixRequest& r) {
     if (b < scan.kept) r = scan.part[b];
-    else r = tree_request(w, b);
+    else { r = tree_request(w, b); prefix_find_row(w, b, r); }
 }
 // What the joining launch needs to know of every row, so that it does not have to look for the row's request: 0 not a row of any (valid) request, 1 own keys only, 3 a
 // shared part too.  By all threads of one CTA of the launch that has the requests' own parts.
@@ -319,11 +350,14 @@ __device__ __forceinline__ int prefix_find_runs(const PrefixWork& w, PrefixScan&
     const int b0 = min(tid * per, w.batch), b1 = min(b0 + per, w.batch);
     long long tiles = 0, items = 0;
     for (int b = b0; b < b1; ++b) {
-        const PrefixRequest r = tree_request(w, b);
+        PrefixRequest r = tree_request(w, b);
         const long long n = r.n_kt ? (long long)w.n_kv * r.n_rt : 0;
         items += n;
         tiles += n * (r.n_kt - r.kt0);
-        if (per == 1) scan.part[b] = r;
+        if (per == 1) {
+            prefix_find_row(w, b, r);
+            scan.part[b] = r;
+        }
     }
     long long other_tiles = 0, other_items = 0;
     if (w.other_time) {

@@ -159,10 +159,10 @@ __device__ __forceinline__ void tree_load_keys(const TcParamsT<W>& p, const CUte
     };
     Box last{}, cur{}, next{}, after{};                          // last: the tile whose V is still to come
     look_up(cur);
-    if (n_tiles > 1) { c.next(p.w); look_up(next); }
+    if (n_tiles > 1) { tree_next(p.w, c); look_up(next); }
     for (int t = 0; t < n_tiles + LEAD && ok; ++t) {
         if (t < n_tiles && !fetch(map_k, cur)) { ok = false; break; }
-        if (t + 2 < n_tiles) { c.next(p.w); look_up(after); }
+        if (t + 2 < n_tiles) { tree_next(p.w, c); look_up(after); }
         if (LEAD == 0) last = cur;
         if (t >= LEAD && !fetch(map_v, last)) { ok = false; break; }
         last = cur;

@@ -1,0 +1,80 @@
+"""Batches that change while they run: requests that have ended."""
+import pytest
+import torch
+
+from test_gpu_beams import prefix_problem
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def zq():
+    from paper_2509_00031_b200 import binding
+    binding.lib()
+    return binding
+
+
+# ---- attention over a shared prefix: requests that have ended -----------------------------------------------------------
+def attend(zq, pr, **kw):
+    a = dict(pr, **kw)
+    out = torch.full_like(pr["q"], 5.0)
+    _, err = zq.zoqat_op_prefix_attention(a["q"], a["k"], a["v"], a["table"], a["kv_len"], a["row_start"], a["group_start"], a["prefix_len"], a["group"], tree_mask=a["mask"], out=out)
+    return out, int(err)
+
+
+def held_to(pr, out, requests, untouched=()):
+    from test_gpu_serve import attention_oracle
+    want, bound = attention_oracle(pr)
+    off = (out[: pr["rows"]].double() - want).abs() <= bound
+    for b in requests:
+        assert bool(off[pr["start"][b]: pr["start"][b + 1]].all()), b
+    for b in untouched:
+        assert bool((out[pr["start"][b]: pr["start"][b + 1]] == 5.0).all()), b
+    assert bool((out[pr["rows"]:] == 5.0).all())
+
+
+ENDED = [
+    # dtype, heads, kv, dh, page, layout, prefix, per, own cached, new, mask: the requests without rows have ended
+    ("bf16", 8, 2, 128, 16, "token", [700, 300], [4, 3], [3] * 7, [0, 1, 1, 1, 0, 0, 2], "random"),       # few queries: a run per warp, both sides in one launch
+    ("f32", 4, 2, 64, 64, "head", [700, 300], [4, 3], [3] * 7, [0, 1, 1, 1, 0, 0, 2], None),
+    ("f32", 8, 1, 128, 16, "token", [500], [3], [0, 1, 2], [0, 0, 3], None),
+    ("f16", 8, 2, 128, 32, "token", [640], [12], [i for i in range(12)], [0] * 3 + [1] * 9, None),          # keys as rows
+    ("bf16", 16, 1, 64, 16, "token", [900], [40], [2 * i for i in range(40)], [0] * 17 + [1] * 23, None),   # 256 queries a tile
+    ("f16", 20, 1, 128, 16, "head", [600], [2], [5, 9], [0, 30], None),                                    # 256 queries a tile, both sides in one launch
+    ("bf16", 4, 4, 64, 16, "token", [400, 200], [70, 30], [1] * 100, [0] * 66 + [1] * 4 + [0, 1] * 15, None),
+    ("f16", 8, 2, 64, 16, "token", [300, 260, 200], [3, 2, 1], [1] * 6, [0, 0, 0, 1, 1, 0], None),          # groups that have ended whole
+    ("bf16", 8, 2, 64, 32, "head", [128 + i for i in range(70)], [6] * 70, [i % 40 for i in range(420)], [0, 0, 1, 0, 1, 1] * 70, None),   # more parts than a CTA keeps
+]
+
+
+@pytest.mark.parametrize("row", ["gone", "reused", "short"])
+@pytest.mark.parametrize("case", ENDED, ids=lambda c: "-".join(str(x) for x in c[:6]) + f"-b{len(c[8])}")
+def test_a_prefix_is_read_through_a_request_that_holds_it(zq, case, row):
+    """A request that has ended keeps its place in the batch: no rows, no keys, and a row of the table that names no pages, or pages that are others' by now."""
+    pr = prefix_problem(13, *case)
+    ended = [b for b, n in enumerate(pr["new"]) if n == 0]
+    table, kv_len = pr["table"].clone(), pr["kv_len"].clone()
+    table[ended] = -1 if row == "gone" else int(pr["table"][pr["new"].index(1) if 1 in pr["new"] else -1, 2])
+    kv_len[ended] = 100 if row == "short" else 0
+    out, err = attend(zq, pr, table=table, kv_len=kv_len)
+    assert err == 0
+    held_to(pr, out, range(len(pr["new"])))
+
+
+@pytest.mark.parametrize("dtype,per,new", [("bf16", [3, 2], 1), ("f16", [40, 30], 1), ("f16", [12, 12], 2), ("f32", [3, 2], 1)])
+def test_a_first_request_that_contradicts_its_group_is_left_out_alone(zq, dtype, per, new):
+    n = sum(per)
+    pr = prefix_problem(14, dtype, 8, 2, 64, 16, "token", [400, 300], per, [4] * n, [new] * n, None)
+    table, kv_len = pr["table"].clone(), pr["kv_len"].clone()
+    table[:2] = -1
+    kv_len[:2] = 400 + new - 1                                    # a key short of the prefix
+    out, err = attend(zq, pr, table=table, kv_len=kv_len)
+    assert err == 41
+    held_to(pr, out, range(2, n), untouched=(0, 1))
+    group = pr["group"].clone()
+    group[per[0]] = 0                                             # the second group's first request names the other one
+    table = pr["table"].clone()
+    table[per[0]] = -1
+    out, err = attend(zq, pr, table=table, group=group)
+    assert err == 41
+    held_to(pr, out, [b for b in range(n) if b != per[0]], untouched=(per[0],))
