@@ -78,3 +78,17 @@ def test_a_first_request_that_contradicts_its_group_is_left_out_alone(zq, dtype,
     out, err = attend(zq, pr, table=table, group=group)
     assert err == 41
     held_to(pr, out, [b for b in range(n) if b != per[0]], untouched=(per[0],))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_lengths_at_the_ends_of_their_type_are_left_out(zq, dtype):
+    """A length less its rows has to be formed in more than 32 bits: the least number less one is the largest."""
+    n = 5
+    pr = prefix_problem(15, dtype, 8, 2, 64, 16, "token", [300], [n], [4] * n, [1, 2, 1, 3, 1], None)
+    for length in (-2 ** 31, -2 ** 31 + 2, 2 ** 31 - 1, -1):
+        for b in (0, 3):
+            kv_len = pr["kv_len"].clone()
+            kv_len[b] = length
+            out, err = attend(zq, pr, kv_len=kv_len)
+            assert err == 41
+            held_to(pr, out, [i for i in range(n) if i != b], untouched=(b,))
