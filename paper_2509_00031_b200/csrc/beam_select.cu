@@ -408,7 +408,19 @@ beam_select_kernel(const __grid_constant__ Params p) {
         const u64 key = order[i];
         if (!key) continue;
         int r = 0;
-        for (int j = 0; j < total; ++j) r += order[j] > key || (order[j] == key && j < i);
+        if (p.slices == 1) {
+            for (int j = 0; j < total; ++j) r += order[j] > key || (order[j] == key && j < i);
+        } else {
+            // a row's slices stand one after the other, each in its own order: of equal scores of a row the larger key comes first.  Without branches (with them, and for all
+            // rows: 4 us more for 4 x 32000 and for 64 x 8 x 50272 alike)
+            const int row0 = i / per_row * per_row;
+            const u64 mine = keys[i];
+            for (int j = 0; j < total; ++j) {
+                const u64 other = order[j], its = keys[j];
+                const bool before = (unsigned)(j - row0) < (unsigned)per_row ? its > mine : j < i;
+                r += (int)(other > key) | ((int)(other == key) & (int)before);
+            }
+        }
         if (r < most) sh.top[r] = i;
     }
     __syncthreads();

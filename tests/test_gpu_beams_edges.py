@@ -1,8 +1,10 @@
-"""Batches that change while they run: requests that have ended."""
+"""Batches that change while they run: requests that have ended, and equal scores."""
+import math
+
 import pytest
 import torch
 
-from test_gpu_beams import prefix_problem
+from test_gpu_beams import check_select, ints, prefix_problem
 
 pytestmark = pytest.mark.gpu
 
@@ -92,3 +94,53 @@ def test_lengths_at_the_ends_of_their_type_are_left_out(zq, dtype):
             out, err = attend(zq, pr, kv_len=kv_len)
             assert err == 41
             held_to(pr, out, [i for i in range(n) if i != b], untouched=(b,))
+
+
+# ---- selection: equal scores -------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("K,V", [(4, 32000), (1, 32000), (3, 20003), (2, 40001)])
+def test_equal_scores_come_larger_logit_first_wherever_a_row_is_cut(zq, K, V, dtype):
+    """Beside a beam score of large magnitude every logit of a row gives the same score, or nearly: the order within a beam is that of logits all the same.  Rows
+    of one request are cut into slices, those of a hundred are not."""
+    gen = torch.Generator(device="cuda").manual_seed(K)
+    x = torch.randn((K, V), generator=gen, device="cuda")
+    at = torch.linspace(7, V - 3, 40, device="cuda").long()
+    x[:, at] = 9.0 + torch.arange(40, device="cuda") * (2.0 ** -20 if dtype == "f32" else 2.0 ** -7)       # rising to the end of the row
+    x[:, at[::5] + 1] = x[:, at[20]].clone()[:, None]                     # some of them twice and more
+    x = x.to({"f32": torch.float32, "f16": torch.float16}[dtype])
+    few = x.clone()
+    few[0] = -math.inf
+    few[0, V // 2: V // 2 + 2] = 1.0                              # two continuations of the first beam: the others have to step in
+    for logits in (x, few):
+        for first, others in ((-1e30, -1e30), (0.0, -1e30), (-1e10, -math.inf), (-1e10, -1e30)):
+            scores = torch.full((1, K), others, device="cuda")
+            scores[0, 0] = first
+            one = check_select(zq, logits, scores, (int(at[37]), 3))
+            many = zq.zoqat_op_beam_select(logits.repeat(100, 1), scores.repeat(100, 1), eos=ints([int(at[37]), 3]))
+            # (the order is the same to the last; a row's sum is cut where the row is, so each of two scores is off by up to what check_select allows)
+            for n, t in one.items():
+                other = t.expand(100, K)
+                if t.dtype is torch.int32:
+                    assert torch.equal(many[n], other), n
+                else:
+                    live = torch.isfinite(other)
+                    assert torch.equal(torch.isfinite(many[n]), live)
+                    assert ((many[n].double() - other.double())[live].abs() <= 2 * (2.0 ** -24 * other.double()[live].abs() + 2.0 ** -20)).all()
+
+
+def test_equal_logits_come_in_the_order_of_tokens(zq):
+    for K in (1, 3, 8):
+        got = zq.zoqat_op_beam_select(torch.zeros((2 * K, 40000), device="cuda"), -torch.arange(2 * K, device="cuda", dtype=torch.float32).view(2, K) * 0.37)
+        assert got["token"].tolist() == [list(range(K))] * 2 and got["beam"].tolist() == [[0] * K] * 2
+
+
+def test_bounds_that_pass_a_threads_own_logits(zq):
+    """Rows whose first thousands of logits are low, and whose rest rises with a few steps: the bound of the best passes what most threads have met."""
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    V = 120000
+    for low, step, spread in ((-300.0, 290.0, 1.0), (-40.0, 40.0, 20.0), (-1e9, 1e9, 3.0)):
+        x = spread * torch.randn((6, V), generator=gen, device="cuda")
+        x[:, :9000] += low
+        x[:, 9000:] += low + step * (torch.arange(V - 9000, device="cuda") // 20000 + 1) / 6
+        check_select(zq, x, torch.zeros((2, 3), device="cuda"), (5,))
+        check_select(zq, x.repeat(40, 1), torch.zeros((80, 3), device="cuda"), (5,))
