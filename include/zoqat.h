@@ -839,7 +839,8 @@ int zoqat_op_beam_select(const void* logits_dev, int type, int64_t ld, int batch
  * ends, its length becomes 0).  A row's keys are in the first ceil(kv_len / page_size) pages of its row of block_table; rows of a request may
  * share pages (in the same column, holding the same), rows of different requests only pages that begin below shared_len of both.
  *   block_table_out [rows, max_pages]   the parent's pages; entries beyond stay as they are.  The page that the parent is still filling (kv_len
- *                       not a multiple of page_size) is kept by the first such row in order; every later row that would share it gets another page
+ *                       not a multiple of page_size) is kept by the first such row in order; every later row that would share it gets another page, and so
+ *                       does the first where a row that goes on is longer and holds that page whole
  *   copy_from, copy_to, copy_len [rows]  what zoqat_op_cache_copy has to copy for such a row (page, page, slots); -1, -1, 0 for the others.  A page
  *                       that begins below shared_len [batch] (NULL: 0) belongs to others too: no row keeps it to fill it, and it never goes back
  *   free_pages_out [free_capacity], n_free_out   the free pages afterwards.  Pages that no row of the request holds any more are given back, in the order

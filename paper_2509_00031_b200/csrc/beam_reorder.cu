@@ -3,9 +3,9 @@
 //
 // Row j of a request continues its row parent[j].  Whole pages are shared by all rows that descend from them and are never copied.
 // The page that a row is still filling can have one owner: the first child in row order keeps it, every further child gets a page of its
-// own with a copy of the slots filled so far.  A page that no row holds any more goes back.  Nothing is counted over steps: all holders
-// of a page are rows of one request and hold it in the same column of their tables (pages shared with other requests lie below
-// shared_len and are left alone), so comparing a column before and after says which pages are gone.
+// own with a copy of the slots filled so far, and so does the first where a longer row goes on that holds the page whole.  A page that no row
+// holds any more goes back.  Nothing is counted over steps: all holders of a page are rows of one request and hold it in the same column of their
+// tables (pages shared with other requests lie below shared_len and are left alone), so comparing a column before and after says which pages are gone.
 //
 //   beam_count_kernel   a CTA per request counts pages given back and wanted; further CTAs copy tables and histories meanwhile
 //   beam_place_kernel   (dependent launch) every CTA sums the counts of the requests before its own, lists its pages in the order column,
@@ -53,9 +53,11 @@ __device__ __forceinline__ void read_request_warp(const ReorderArgs& a, int b, R
     const int page = part ? __ldg(a.block_table + ((int64_t)b * K + parent) * a.max_pages + last) : -1;
     bool keep = part && (int64_t)last * P >= shared;
     for (int j = 0; j < K; ++j) {
-        const int pg = __shfl_sync(0xffffffffu, page, j), lt = __shfl_sync(0xffffffffu, last, j);
+        const int pg = __shfl_sync(0xffffffffu, page, j), lt = __shfl_sync(0xffffffffu, last, j), of = __shfl_sync(0xffffffffu, parent, j);
         const bool pt = __shfl_sync(0xffffffffu, (int)part, j);
         if (j < lane && pt && pg == page && lt == last) keep = false;
+        // a longer row may hold the page whole, and what a shorter one adds would fall among its keys
+        if (keep && of >= 0 && lt > last && __ldg(a.block_table + ((int64_t)b * K + of) * a.max_pages + last) == page) keep = false;
     }
     if (part && (page < 0 || page >= a.n_pages)) { bad |= kPlanBadPage; keep = true; }      // nothing to copy from
     if (mine) { r.len[lane] = len; r.held[lane] = len / P + (len % P != 0); r.parent[lane] = parent; }

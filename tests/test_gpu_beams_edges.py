@@ -1,6 +1,7 @@
-"""Batches that change while they run: requests that have ended, and equal scores."""
+"""Batches that change while they run: requests that have ended, equal scores, beams of different lengths."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -144,3 +145,52 @@ def test_bounds_that_pass_a_threads_own_logits(zq):
         x[:, 9000:] += low + step * (torch.arange(V - 9000, device="cuda") // 20000 + 1) / 6
         check_select(zq, x, torch.zeros((2, 3), device="cuda"), (5,))
         check_select(zq, x.repeat(40, 1), torch.zeros((80, 3), device="cuda"), (5,))
+
+
+# ---- reordering: rows of different lengths -----------------------------------------------------------------------------
+@pytest.mark.parametrize("B,K,P,longest,seed", [(1, 4, 4, 30, 0), (3, 8, 8, 90, 1), (4, 32, 4, 60, 2), (40, 6, 16, 200, 3), (2, 5, 16, 5000, 4), (200, 3, 2, 12, 5)])
+def test_rows_of_any_length_keep_their_keys(zq, B, K, P, longest, seed):
+    """Rows of a request that hold beginnings of one text, of different lengths, in the same pages.  Slots are followed through the reordering, the copies and the rows' next
+    keys: every row reads its own."""
+    rng = np.random.default_rng(seed)
+    M = -(-longest // P) + 1
+    pool = B * K * (M + 1)
+    pages, rows = rng.permutation(pool).tolist(), B * K
+    store = np.full((pool, P), -1, dtype=np.int64)
+    kv_len, table, text = [0] * rows, np.full((rows, M), -1, dtype=np.int64), [[] for _ in range(rows)]
+    for b in range(B):
+        whole = [pages.pop() for _ in range(M)]
+        base = rng.integers(0, 1 << 40, longest)
+        for i, t in enumerate(base):
+            store[whole[i // P], i % P] = t
+        for k in range(K):
+            r, n = b * K + k, int(rng.integers(0, longest + 1))
+            kv_len[r], text[r] = n, base[:n].tolist()
+            table[r, : -(-n // P)] = whole[: -(-n // P)]
+        last = max(kv_len[b * K: b * K + K])
+        pages += whole[-(-last // P):]                            # (pages that nobody holds)
+    rng.shuffle(pages)
+    free = pages + [-7] * (pool - len(pages))
+    parent = rng.integers(-1, K, (B, K))
+    parent[:, 0] = np.where(rng.random(B) < 0.5, rng.integers(0, K, B), parent[:, 0])
+    out = zq.zoqat_op_beam_reorder(ints(parent.tolist()), ints(kv_len), ints(table.tolist()), P, pool, ints(free), ints([len(pages)]))
+    assert int(out["status"]) == 0
+    new_len, new_table = out["kv_len"].tolist(), out["block_table"].cpu().numpy()
+    for f, t, n in zip(out["copy_from"].tolist(), out["copy_to"].tolist(), out["copy_len"].tolist()):
+        if n:
+            store[t, :n] = store[f, :n]
+    want = []
+    for r in range(rows):
+        p = parent[r // K, r % K]
+        want.append(list(text[r // K * K + p]) if p >= 0 else [])
+        assert new_len[r] == len(want[r])
+        if new_len[r] % P:                                        # the next key, where the page has room
+            want[r].append(int(1 << 41) + r)
+            store[new_table[r, new_len[r] // P], new_len[r] % P] = want[r][-1]
+    held = set()
+    for r in range(rows):
+        i = np.arange(len(want[r]))
+        assert bool((store[new_table[r, i // P], i % P] == np.array(want[r], dtype=np.int64)).all()), r
+        held |= set(new_table[r, : -(-new_len[r] // P)].tolist())
+    left = out["free_pages"][: int(out["n_free"])].tolist()
+    assert len(set(left)) == len(left) and held.isdisjoint(left) and held | set(left) == set(range(pool))
