@@ -852,7 +852,7 @@ int zoqat_op_beam_select(const void* logits_dev, int type, int64_t ld, int batch
  * status is or-ed with 1 (a length negative or too long for its table or history: it counts as 0; *n_free outside the list, or more pages than the
  * list holds), 2 (too few free pages), 4 (a page outside [0, n_pages): left where it is, neither copied nor given back), 8 (a parent outside [-1, beams): it
  * counts as -1).  With an impossible *n_free or too few pages nothing is reordered: all lengths become 0, there are no copies, the free pages
- * stay, tables and histories are unspecified.  Outputs are other buffers than inputs.  batch <= 16384, beams <= 32. */
+ * stay, tables and histories are unspecified.  Outputs are other buffers than inputs.  batch <= 16384, beams <= 32; tables and free lists of less than 2^30 entries. */
 typedef struct zoqat_beam_reorder {
     const int32_t* parent;        /* [batch * beams]                                                          */
     const int32_t* kv_len;        /* [batch * beams]                                                          */

@@ -2190,6 +2190,8 @@ int zoqat_op_beam_reorder(const zoqat_beam_reorder_t* r, void* scratch_dev, size
     if (r->batch <= 0 || r->beams <= 0 || r->page_size <= 0 || r->n_pages <= 0 || r->max_pages <= 0 || r->free_capacity <= 0) return fail(ZOQAT_ERR_INVALID_ARG, "sizes must be positive");
     if (r->batch > kMaxPlanBatch || r->beams > kMaxBeams) return fail(ZOQAT_ERR_UNSUPPORTED, "batch %d (up to %d), beams %d (up to %d)", r->batch, kMaxPlanBatch, r->beams, kMaxBeams);
     if ((int64_t)r->n_pages * r->page_size > INT32_MAX || (int64_t)r->max_pages * r->page_size > INT32_MAX) return fail(ZOQAT_ERR_UNSUPPORTED, "more than 2^31 - 1 slots");
+    // (the kernels add up pages of all rows and of the list in 32 bits)
+    if ((int64_t)r->batch * r->beams * r->max_pages >= (1 << 30) || r->free_capacity >= (1 << 30)) return fail(ZOQAT_ERR_UNSUPPORTED, "2^30 or more entries of the table or of the free list");
     if (r->history ? !r->history_len || !r->history_out || !r->history_len_out || r->history_stride <= 0 || r->history_stride > (1 << 30)
                    : r->history_len || r->history_out || r->history_len_out || r->token)
         return fail(ZOQAT_ERR_INVALID_ARG, "histories need history, history_len, both outputs and history_stride (up to 2^30); token needs them");
