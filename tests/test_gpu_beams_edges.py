@@ -1,11 +1,11 @@
-"""Batches that change while they run: requests that have ended, equal scores, beams of different lengths."""
+"""Batches that change while they run: requests that have ended, beams of different lengths, equal scores, and the step of a model compared with the one without groups."""
 import math
 
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_beams import check_select, ints, prefix_problem
+from test_gpu_beams import check_select, ints, make_cache, prefix_problem
 
 pytestmark = pytest.mark.gpu
 
@@ -194,3 +194,57 @@ def test_rows_of_any_length_keep_their_keys(zq, B, K, P, longest, seed):
         held |= set(new_table[r, : -(-new_len[r] // P)].tolist())
     left = out["free_pages"][: int(out["n_free"])].tolist()
     assert len(set(left)) == len(left) and held.isdisjoint(left) and held | set(left) == set(range(pool))
+
+
+# ---- the step of a packed model ----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("name,dtype,prefix,own", [("llama_w4a8", "f32", [150, 90], [5, 0]), ("llama_w4a8", "bf16", [140, 131], [9, 30]), ("llama_w4", "f16", [160, 129], [1, 2])])
+def test_one_step_with_and_without_the_shared_prefix(zq, name, dtype, prefix, own):
+    """The same tokens, plan and caches through both steps: logits agree, and do not where a tile of the prefix is another one."""
+    from test_gpu_serve import packed_model
+    shape, model = packed_model(zq, name, 8, 192)
+    H, dh, page, n_pages, K = shape["n_heads"], shape["d_model"] // shape["n_heads"], 16, 80, 4
+    B = 2 * K
+    caches = [make_cache(n_pages, page, H, dh, dtype, "token", seed=l) for l in range(shape["n_layers"])]
+    cached = [prefix[b // K] + own[b // K] for b in range(B)]
+    rng = np.random.default_rng(2)
+    order = rng.permutation(n_pages).tolist()
+    table = torch.full((B, 13), -1, dtype=torch.int32, device="cuda")
+    for g in range(2):
+        whole = [order.pop() for _ in range(prefix[g] // page)]
+        for b in range(g * K, g * K + K):
+            rest = -(-cached[b] // page) - len(whole)
+            mine = whole + [order.pop() for _ in range(rest)]
+            table[b, : len(mine)] = ints(mine)
+            for k, v in caches:                                   # what is left of the prefix lies in a page of each request's own
+                for t in (k, v):
+                    t[mine[len(whole)], : prefix[g] % page] = t[int(table[g * K, len(whole)]), : prefix[g] % page]
+    plan = zq.zoqat_op_cache_plan(ints(cached), ints([1] * B), page, n_pages, ints(order), ints([len(order)]), table, B)
+    assert int(plan["status"]) == 0
+    tokens = ints(rng.integers(0, shape["vocab"], B).tolist())
+    groups = (ints([0, K, B]), ints(prefix), ints([0] * K + [1] * K))
+
+    def step(groups, table):
+        mine = [(k.clone(), v.clone()) for k, v in caches]
+        if groups is None:
+            got = model.zoqat_decode_tree_step(tokens, plan, table, mine)
+        else:
+            got = model.zoqat_decode_prefix_step(tokens, plan, table, *groups, mine)
+        model.zoqat_check()
+        return got
+
+    want, best = step(None, table)
+    got, choice = step(groups, table)
+    # The attentions of the two differ by a few roundings (of their weights with 16-bit caches); behind them an activation may come out one code further, which moves
+    # logits by up to 2 % of their scale (5 % with bf16 keys), as in the test of drafts.
+    tol = {"f32": 2e-2, "f16": 2e-2, "bf16": 5e-2}[dtype] * float(want.abs().max())
+    assert float((got - want).abs().max()) <= tol
+    top = want.topk(2, 1).values
+    clear = top[:, 0] - top[:, 1] > 2 * tol
+    assert torch.equal(choice[clear], best[clear])
+    # the control: the second half of the shared tile of 128 keys names the pages of the first
+    other = table.clone()
+    other[:, 4:8] = table[:, 0:4]
+    wrong, _ = step(groups, other)
+    for g, n in enumerate(prefix):
+        if n >= 128:
+            assert float((wrong - want)[g * K: g * K + K].abs().max()) > 2 * tol
