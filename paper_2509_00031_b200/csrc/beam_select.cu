@@ -15,8 +15,9 @@
 // 64 x 8 beams of 50272 logits: fp32 30 us, 16 of them the 103 MB at the rate of a copy, bf16 27; 96 x 3 of 128256 bf16 with nine tenths masked 33 (11); 4 of 32000 fp32 12.5.  The stream
 // itself runs at 7 TB/s (16-bit logits: bound by the exponentials); 5.5 us go before it (start, first bound, sorting) and 7 behind it (sorting, sums, the cluster, logarithms in 64
 // bits, ranking), in short dependent steps that all CTAs go through at the same time.
-// Sums: every thread has its own reference (the largest logit it met when it last moved), partial sums are fp32, the row's logarithm and all scores are formed in
-// 64 bits, so that scores of different beams are compared before anything is rounded.  Scores are rounded to fp32 once.
+// Sums: every thread has its own reference (the largest logit it met when it last moved).  Partial sums are fp32, a round's vectors by themselves and then the rounds: among
+// few different logits the roundings of equal terms all go one way, and 131072 of them one by one put a score off by 9 half units of its last place, in two steps by one.  The
+// row's logarithm and all scores are formed in 64 bits, so that scores of different beams are compared before anything is rounded.  Scores are rounded to fp32 once.
 #include "common.cuh"
 #include "serve.cuh"
 #include "tc_ptx.cuh"
@@ -274,8 +275,10 @@ beam_select_kernel(const __grid_constant__ Params p) {
                         ref2 = to;
                     }
                 }
+                float2 part = make_float2(0.0f, 0.0f);
 #pragma unroll
-                for (int u = 0; u < kFly; ++u) add_powers(x[u], ref2, sum);
+                for (int u = 0; u < kFly; ++u) add_powers(x[u], ref2, part);
+                sum = tree_add2(sum, part);
             };
             for (int base = kRound; base < n_vec; base += 2 * kRound) {
                 if (base + kRound < n_vec) fetch(now, src, base + kRound);
@@ -349,9 +352,13 @@ beam_select_kernel(const __grid_constant__ Params p) {
             const u64 first = best[0];
             x[0] = first ? unordered((uint32_t)(first >> 32)) : 0.0f;
             x[1] = 0.0f;
-            for (int i = tid; first && i < size; i += kThreads) {
-                const float v = value(src[i]);
-                if (v > -INFINITY) x[1] += ex2((fminf(v, FLT_MAX) - x[0]) * kLog2e);
+            for (int i0 = tid; first && i0 < size; i0 += 32 * kThreads) {
+                float part = 0.0f;
+                for (int i = i0; i < size && i < i0 + 32 * kThreads; i += kThreads) {
+                    const float v = value(src[i]);
+                    if (v > -INFINITY) part += ex2((fminf(v, FLT_MAX) - x[0]) * kLog2e);
+                }
+                x[1] += part;
             }
 #pragma unroll
             for (int o = 16; o >= 1; o >>= 1) x[1] += __shfl_xor_sync(0xffffffffu, x[1], o);

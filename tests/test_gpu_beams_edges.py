@@ -147,6 +147,25 @@ def test_bounds_that_pass_a_threads_own_logits(zq):
         check_select(zq, x.repeat(40, 1), torch.zeros((80, 3), device="cuda"), (5,))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("ld", [131072, 131073])
+def test_sums_of_many_equal_logits(zq, dtype, ld):
+    """Few different logits: the roundings of a sum's equal terms do not cancel out."""
+    V, rows = 131072, 160
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn((rows, ld), generator=gen, device="cuda")
+    one = torch.full_like(x, 0.37)
+    one[:, 5] = 1.3
+    for y in (one, (x > 0).float() * -0.6, x.round()):
+        y = y.to({"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[dtype])[:, :V]
+        got = zq.zoqat_op_beam_select(y, torch.zeros((rows, 1), device="cuda"))["score"][:, 0].double()
+        want = y.double().amax(1) - torch.logsumexp(y.double(), 1)
+        # an exponential is off by 2^-22, its argument (up to 8) by 2^-22 ln 2.  A term goes through at most 32 additions within its part of the row, then the thread's parts
+        # (8192 logits each, with rows that do not begin on 16 bytes 2048), 5 steps over the lanes and 8 over the warps, each off by 2^-24; and the score is rounded once
+        steps = 32 + V // (8192 if ld % 8 == 0 else 2048) + 13
+        assert bool(((got - want).abs() <= 2 * 2.0 ** -22 + steps * 2.0 ** -24 + 2.0 ** -24 * want.abs()).all())
+
+
 # ---- reordering: rows of different lengths -----------------------------------------------------------------------------
 @pytest.mark.parametrize("B,K,P,longest,seed", [(1, 4, 4, 30, 0), (3, 8, 8, 90, 1), (4, 32, 4, 60, 2), (40, 6, 16, 200, 3), (2, 5, 16, 5000, 4), (200, 3, 2, 12, 5)])
 def test_rows_of_any_length_keep_their_keys(zq, B, K, P, longest, seed):
