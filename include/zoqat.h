@@ -798,8 +798,8 @@ int zoqat_op_rotary_append(const void* qkv_dev, int qkv_type, int64_t ld, const 
 
 /* zoqat_op_tree_attention for requests that share a long prefix: requests group_start_dev[g] .. group_start_dev[g + 1] - 1 ([groups + 1]) form
  * group g, and the first prefix_len_dev[g] keys of each of them that has rows ([groups]) are the same - their rows of block_table name the same pages, or
- * pages that hold the same; request_group_dev [batch] names each request's group.  Requests without rows keep their place: their lengths and rows of block_table
- * may hold anything.  All keys of the prefix are seen by all rows (prefix_len <= kv_len - rows
+ * pages that hold the same; request_group_dev [batch] names each request's group.  Requests without rows keep their place: their lengths, rows of
+ * block_table and entries of request_group_dev may hold anything.  All keys of the prefix are seen by all rows (prefix_len <= kv_len - rows
  * of the request).  The result is that of zoqat_op_tree_attention up to rounding, the prefix is read once for the whole group (through the table of its first
  * request that has rows and holds it, in whole tiles of 128 keys, fp32 32; what is left of it through each request's own).  Everything else as there, the limits
  * of page sizes and strides among it.  *err_flag_dev is also set to 41 where groups and requests contradict each other: the group or request is left out.  scratch_dev:

@@ -133,8 +133,9 @@ __device__ __forceinline__ PrefixRequest prefix_own(const PrefixWork& w, int b, 
     const int of = grouped ? g : 0, len = __ldg(w.prefix_len + of), b0 = __ldg(w.group_start + of), b1 = __ldg(w.group_start + of + 1);     // (all on their way at once)
     r.n = end - r.row0;
     r.row = b; r.own = 1;
-    ok = r.n >= 0 && r.row0 >= 0 && r.row0 <= w.rows - r.n && r.L <= (long long)w.max_pages * w.page_size && grouped && b0 <= b && b < b1 &&
-         (r.n == 0 || (len >= 0 && len <= (long long)r.L - r.n));
+    // (a request without rows may say anything: it may have ended)
+    ok = r.n == 0 || (r.n > 0 && r.row0 >= 0 && r.row0 <= w.rows - r.n && r.L <= (long long)w.max_pages * w.page_size && grouped && b0 <= b && b < b1 && len >= 0 &&
+                      len <= (long long)r.L - r.n);
     if (!ok || r.n == 0) { r.n = 0; return r; }
     r.kt0 = prefix_down(prefix_down(len, w.border) * w.border, w.key_tile);
     r.n_rt = prefix_up(r.n * w.group, w.tile_rows);

@@ -64,6 +64,18 @@ def test_a_prefix_is_read_through_a_request_that_holds_it(zq, case, row):
     held_to(pr, out, range(len(pr["new"])))
 
 
+@pytest.mark.parametrize("case", ENDED[:6], ids=lambda c: "-".join(str(x) for x in c[:6]) + f"-b{len(c[8])}")
+def test_requests_that_have_ended_may_say_anything(zq, case):
+    pr = prefix_problem(16, *case)
+    ended = [b for b, n in enumerate(pr["new"]) if n == 0]
+    for length, of in ((2 ** 31 - 1, -1), (-2 ** 31, 2 ** 31 - 1), (10 ** 6, 1), (-1, -2 ** 31)):
+        kv_len, group = pr["kv_len"].clone(), pr["group"].clone()
+        kv_len[ended], group[ended] = length, of
+        out, err = attend(zq, pr, kv_len=kv_len, group=group)
+        assert err == 0
+        held_to(pr, out, range(len(pr["new"])))
+
+
 @pytest.mark.parametrize("dtype,per,new", [("bf16", [3, 2], 1), ("f16", [40, 30], 1), ("f16", [12, 12], 2), ("f32", [3, 2], 1)])
 def test_a_first_request_that_contradicts_its_group_is_left_out_alone(zq, dtype, per, new):
     n = sum(per)
