@@ -778,7 +778,8 @@ int zoqat_decode_tree_step(zoqat_model_t* m, const int32_t* tokens_dev, int rows
  *   LINEAR  freq / factor
  *   BASE    the base times factor^(rot / (rot - 2)): the slowest pair slows down by the factor, the fastest is left
  *   PARTS   pairs that turn r = trained_len * freq / (2 pi) times in a training context: freq / factor up to r = 1, freq from r = 32 on, a
- *           linear ramp in r between; *magnitude_host, by which q and k are to be multiplied, is 0.1 ln(factor) + 1 (else 1) */
+ *           linear ramp in r between; *magnitude_host, by which q and k are to be multiplied, is 0.1 ln(factor) + 1 (else 1).  The ramp's ends
+ *           are fixed; for one with other ends, or over the numbers of the pairs, fill the frequencies yourself: any [rot / 2] will do */
 #define ZOQAT_ROTARY_PLAIN  0
 #define ZOQAT_ROTARY_LINEAR 1
 #define ZOQAT_ROTARY_BASE   2
@@ -842,7 +843,9 @@ int zoqat_op_beam_select(const void* logits_dev, int type, int64_t ld, int batch
  *                       not a multiple of page_size) is kept by the first such row in order; every later row that would share it gets another page, and so
  *                       does the first where a row that goes on is longer and holds that page whole
  *   copy_from, copy_to, copy_len [rows]  what zoqat_op_cache_copy has to copy for such a row (page, page, slots); -1, -1, 0 for the others.  A page
- *                       that begins below shared_len [batch] (NULL: 0) belongs to others too: no row keeps it to fill it, and it never goes back
+ *                       that begins below shared_len [batch] (NULL: 0) belongs to others too: no row keeps it to fill it, and it never goes back.  So a
+ *                       shared_len inside a page is for the one call that parts the rows from that page; from then on they have it as copies of
+ *                       their own, and shared_len is to be the length of the whole pages below it
  *   free_pages_out [free_capacity], n_free_out   the free pages afterwards.  Pages that no row of the request holds any more are given back, in the order
  *                       of requests, columns, rows.  A request's new pages are those first; further ones are taken from the end of free_pages[0 ..
  *                       *n_free), request by request, row by row; what is left of the pages given back stands behind the free pages that are left

@@ -13,7 +13,7 @@
 // The order of all lists is fixed by rows and columns, so the same call gives the same pages.
 //   beam_reorder_kernel both in one, for few requests
 //   cache_copy_kernel   slots of pages, for all layers in one launch; bound by memory
-// 64 requests of eight beams, 100 to 2000 tokens, and the copies of 16 layers (every other row gets one on average, 542 MB read and written): 78 us replayed, 83 those bytes at the
+// 64 requests of eight beams, 100 to 2000 tokens, and the copies of 16 layers (two rows in five get one, 452 MB read and written): 78 us replayed, 69 those bytes at the
 // rate of a copy.
 #include "common.cuh"
 #include "serve.cuh"
@@ -253,8 +253,8 @@ beam_place_kernel(const ReorderParams p) {
 }
 
 // Few requests: every CTA counts for all of them itself, its warps shared out, so one launch does it.  1 / 4 / 8 requests of four beams with up to 2000 tokens, with the copies of
-// 24 layers: called from Python 21.9 / 21.8 / 21.9 us against 24.6 / 24.4 / 24.3 with two launches, replayed from a graph, where a launch costs the host nothing, 8.3 / 13.5 / 15.5
-// against 9.2 / 12.4 / 13.3: two warps a request are enough, one is not.
+// 24 layers: called from Python 21.9 / 21.8 / 21.9 us against 24.6 / 24.4 / 24.3 with two launches, replayed from a graph, where a launch costs the host nothing, 8.3 / 13.8 / 15.5
+// against 9.0 / 12.4 / 13.3: calls gain 3 us with up to four requests, replays lose up to 1.4 with more than one.
 __global__ void __launch_bounds__(kThreads)
 beam_reorder_kernel(const ReorderParams p) {
     __shared__ Request all[kFew];

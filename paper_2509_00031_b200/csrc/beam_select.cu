@@ -10,10 +10,13 @@
 // logits every warp knows its largest few: the least of those is a bound that at least as many logits pass as are wanted.  What passes it
 // goes to a buffer, whose sorted best (each key counts the larger ones) set the exact bound for the rest of the row; a logit that
 // passes that is rare, so the stream costs a maximum, an exponential and two additions each, sixteen bytes at a time, the next on their way while some are
-// worked on.  Keys are (logit, token) in 64 bits: no two are equal, and of equal logits the lower token wins.  Should the buffer ever run over (long runs
-// of rising or equal logits), the row's bound is found digit by digit from histograms instead.
+// worked on.  Keys are (logit, token) in 64 bits: no two are equal, and of equal logits the lower token wins.
+// Should the buffer run over, the row's bound is found digit by digit from histograms instead, ten more passes over the row: right, and slow.  That takes long runs of rising or
+// equal logits; more than 32 best wanted of a row by a CTA of 256 threads, whose eight warps offer four each (64 x 32 beams of 50272 with one ending token 3420 us, without 313);
+// or a first round with fewer live logits than are wanted and thousands behind it (64 x 8 of 50272 whose first 8192 are ruled out 918 us, against 32; one live logit in a thousand 74 us
+// where -inf rules the others out, 865 where -1e9 does).
 // 64 x 8 beams of 50272 logits: fp32 30 us, 16 of them the 103 MB at the rate of a copy, bf16 27; 96 x 3 of 128256 bf16 with nine tenths masked 33 (11); 4 of 32000 fp32 12.5.  The stream
-// itself runs at 7 TB/s (16-bit logits: bound by the exponentials); 5.5 us go before it (start, first bound, sorting) and 7 behind it (sorting, sums, the cluster, logarithms in 64
+// itself runs at 7 TB/s (16-bit logits: bound by the exponentials; rows that do not begin on 16 bytes, 50257 of them, 34 and 31 us); 5.5 us go before it (start, first bound, sorting) and 7 behind it (sorting, sums, the cluster, logarithms in 64
 // bits, ranking), in short dependent steps that all CTAs go through at the same time.
 // Sums: every thread has its own reference (the largest logit it met when it last moved).  Partial sums are fp32, a round's vectors by themselves and then the rounds: among
 // few different logits the roundings of equal terms all go one way, and 131072 of them one by one put a score off by 9 half units of its last place, in two steps by one.  The
@@ -267,7 +270,8 @@ beam_select_kernel(const __grid_constant__ Params p) {
                 for (int u = 1; u < kFly; ++u) m4 = fmaxf(m4, largest(x[u]));
                 if (m4 > limit) {
                     push<false>(sh, x, limit, lo + (base + tid) * VEC, kThreads * VEC);
-                    if (m4 > ref) {                              // the reference moves (no logit above it has been met: limit <= reference)
+                    if (m4 > ref) {                              // the reference moves.  (Logits below the limit may pass it too, once other threads' logits have raised
+                                                                 // the limit: should the sum run over then, the careful pass behind the stream mends it)
                         ref = fminf(m4, FLT_MAX);
                         const float to = __fmul_rn(ref, kLog2e), f = ex2(ref2 - to);
                         sum.x *= f;

@@ -9,9 +9,9 @@
 //   output  a thread has one chunk (4 columns) of every key (d_head 64: of every other key), and 8 queries' weights from shared memory
 // both as pairs of products in one instruction (fma.rn.f32x2).  Eight queries cost 2 x 8 x d_head fused operations a key against 8 x d_head bytes from memory: 128
 // instructions of a warp for 16 keys at d_head 64, where the memory's share is some 190 cycles of the SM.  3 prompts of 500 to 4000 keys, 2 to 6 requests each with 1 to 3
-// drafts, 32 heads of 64: 55.5 us, 20 of them the cache's 131 MB at the rate of a copy (the way of tree_attention.cu, which reads every query from shared memory for every key
+// drafts, 32 heads of 64: 51.3 us, 20 of them the cache's 131 MB at the rate of a copy (the way of tree_attention.cu, which reads every query from shared memory for every key
 // and meets at a barrier for every tile: 110).  Bound by a warp's own chain of some 1000 instructions for a tile, a third of them products, with
-// ten warps an SM (28 % of the issue slots, 30 % of the memory's rate).
+// ten warps an SM (28 % of the issue slots, 32 % of the memory's rate); at d_head 64 the compiler spills 64 bytes a thread and loads 24 again, 168 registers (with 138 and 184: 55.5 us).
 // The running maximum is exact for every tile; everything is binary32.
 #include "tree_attention.cuh"
 #include "tc_ptx.cuh"

@@ -13,7 +13,9 @@
 // halves are paired, and else two that leave neighbouring lanes with neighbouring chunks.  A head is 4 or 8 lanes, its mean square two or three shuffles.  A thread keeps its row and its
 // place within the head and walks over the heads, so sines, cosines and gains are read once and stay in registers (read again for every head, they were two thirds of
 // what passed through L1: 8191 rows of 40 + 2 * 8 heads of 128, bf16 to binary16, 75 us against 53, where 36 are the bytes at the rate of a copy).  What is left is bound by instructions
-// (half of the issue slots) and by waiting for the one head ahead: two ahead cost an SM a third of its CTAs (59 us), four CTAs an SM spill (70).
+// (half of the issue slots) and by waiting for the one head ahead: two ahead cost an SM a third of its CTAs (59 us).  At three CTAs an SM, 80 registers, the compiler spills 24 to 44 bytes a
+// thread (28 to 72 loaded again); at four, 64 registers, 164 to 240 (70 us).
+// Rounding: sums of squares are fp32, and rsqrtf is off by two units of its last place; fp32 results are off by 6e-8 relative to 64 bits (elementary operations one after the other: 4e-8).
 #include "common.cuh"
 #include "serve.cuh"
 #include "tc_ptx.cuh"

@@ -530,8 +530,9 @@ static int tc_kernel(const TcParamsT<W>& p, const CUtensorMap& map_k, const CUte
     return dh == 64 ? tc_launch<64, __half>(p, map_k, map_v, grid, s, dependent) : tc_launch<128, __half>(p, map_k, map_v, grid, s, dependent);
 }
 
-// Of the launch with `tile` queries a tile: keys of a key tile, units of opening and closing a part, time of a tile on an SM in 0.1 us.  The times are what they are
-// where the SM and not the memory is the bound, d_head 128: a tile of 256 queries and 128 keys 2.5 us, of up to 64 queries 1.2, of a warp's 16 keys 0.11.
+// Of the launch with `tile` queries a tile: keys of a key tile, units of opening and closing a part, time of a tile on an SM in 0.1 us.  With keys from L2 (16 groups over the same
+// pages, d_head 128 / 64) a tile of 256 queries and 128 keys takes 2.07 / 1.80 us, of 64 queries 1.19 / 1.13, of 32 1.16 / 1.18, of 8 and 32 keys (twelve warps at it) 0.15 / 0.12. Beside the
+// other launch, which keeps the memory busy, a wide tile takes 2.5 and a warp's tiles 0.22 (76 GB/s an SM) at d_head 128; the constants are those, and serve d_head 64 as well.
 struct PrefixTile { int keys, cost, time; };
 static PrefixTile prefix_tile(int tile) {
     if (tile <= kNarrowRows) return PrefixTile{kNarrowKeys, 2, 2};
