@@ -194,7 +194,7 @@ __device__ __forceinline__ void tree_next(const TreeWork& w, TreeCursor& c) { c.
 __device__ __forceinline__ void tree_next(const PrefixWork& w, TreeCursorT<PrefixWork>& c) {
     const int b = c.b;
     c.next(w);
-    if (c.b != b) prefix_find_row(w, c.b, c.r);
+    if (c.b != b && c.b < w.batch) prefix_find_row(w, c.b, c.r);
 }
 
 // a / b for a >= 0, b > 0; almost always in 32 bits, which is several times faster
